@@ -331,11 +331,12 @@ def _exact_fp8(x, fmt, rows):
     for k in range(0, x.shape[1], 128):
         for r, part in enumerate([x[:, k:k + 128]] if rows == 1 else torch.split(x[:, k:k + 128], rows)):
             amax = part.abs().amax(dim=1, keepdim=True) if rows == 1 else part.abs().amax()
-            e = torch.ceil(torch.log2(amax.clamp(min=1e-300) / FP8_TOP[fmt]))
-            e = torch.where(amax > 0, e.clamp(min=-127), torch.zeros_like(e))
-            v = part * torch.exp2(-e)
-            step = torch.exp2(torch.floor(torch.log2(v.abs().clamp(min=2.0**least))) - bits)
-            q = torch.round(v / step) * step * torch.exp2(e)
+            # from the numbers' own exponents: a logarithm may round at a power of two
+            m, e = torch.frexp(amax / FP8_TOP[fmt])
+            e = torch.where(amax > 0, (e - (m == 0.5).int()).clamp(min=-127), torch.zeros_like(e))
+            v = torch.ldexp(part, -e)
+            step = torch.ldexp(torch.ones_like(v), torch.frexp(v.abs().clamp(min=2.0**least))[1] - 1 - bits)
+            q = torch.ldexp(torch.round(v / step) * step, e)
             out[r * rows if rows > 1 else 0:(r * rows if rows > 1 else 0) + part.shape[0], k:k + 128] = q
     return out
 
@@ -364,7 +365,7 @@ def exact(case, seed):
         N, blocks = case["N"], s["wq"].shape[1] // 128
         r, b = torch.arange(N, device="cuda")[:, None], torch.arange(blocks, device="cuda")[None, :]
         e = s["wscale"][r // 128, b // 4, r % 32, r % 128 // 32, b % 4].double() - 127
-        w = (s["wq"].double() * torch.exp2(e).repeat_interleave(128, dim=1))[:, :case["K"]]
+        w = (s["wq"].double() * torch.pow(2.0, e).repeat_interleave(128, dim=1))[:, :case["K"]]
         y = torch.einsum("mk,nk->mn", _exact_fp8(x, case["format"], 1), w)
         return [y + s["bias"].double() if case["bias"] else y]
     w, dy, grad = s["w"].double(), s["dy"].double(), case["gradient"]
