@@ -380,6 +380,68 @@ qb_status qb_embedding_lookup(const int32_t* ids, int64_t T, const uint32_t* pac
                               const float* q0, int64_t V, int64_t D, int bits, int groups, int accumulate,
                               float* out, void* ws, size_t ws_bytes, void* cuda_stream);
 
+/* Element types and formats of the calls below. */
+enum { QB_F32 = 0, QB_BF16 = 1, QB_F16 = 2 };
+enum { QB_E4M3 = 0, QB_E5M2 = 1 };
+#define QB_MAX_ELEMENTS ((int64_t)1 << 40)
+
+/*
+ * Linears in 8-bit floating point, one power-of-two scale per block of 128 along the contraction.  (No counterpart in the
+ * paper.  The group-wise integer codes above hold weights and activations; gradients, whose sizes differ by orders of
+ * magnitude from token to token, need a scale per block and a format with an exponent.  These calls give fine-tuning the three
+ * products of a linear: forward, and the gradients of its input and of its weights.)
+ *
+ * Per block: e is the least integer with max|x| * 2^-e <= the largest value of the format (448 for QB_E4M3, 57344 for
+ * QB_E5M2; not below -127), code = x * 2^-e rounded to nearest even in the format.  A block of zeros has e = 0.  The scaling is
+ * exact, and nothing saturates.
+ *
+ * Codes are [R][Kp], Kp = K rounded up to 128, the columns behind K zero.  Scales are bytes e + 127, one per row and
+ * block, in the order of the tensor cores: 128 rows and four blocks are 512 bytes, the byte of row r and block j at
+ *     ((r / 128) * ceil(Kp / 512) + j / 4) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + j % 4.
+ * qb_fp8_scale_bytes(R, K) is their size (0 on invalid arguments).  Bytes of rows and blocks that the codes do not have may
+ * hold anything and change nothing.
+ *
+ * qb_quantize_fp8 (activations, gradients): blocks of 1 x 128.  With xqt and xt_scale it writes the transposed codes too
+ * [K][Mp], Mp = M rounded up to 128, in blocks of 128 rows of x (for products that contract over the tokens).
+ * qb_quantize_fp8_weights: blocks of 128 x 128; the transposed codes (N and K swapped) have the same scales.  x is read once.
+ *   x         dev [M][K] of `type`, aligned to its elements                                  (read)
+ *   xq, xqt   dev, 16-byte aligned; x_scale, xt_scale: dev, 16-byte aligned                  (written)
+ * A block with a NaN or an infinity: QB_ERR_NONFINITE in the status word; its NaN and infinities become NaN codes (and reach
+ * the outputs of a product that reads them), its other values are unspecified.
+ *
+ * qb_gemm_fp8: y[m][n] = sum_k a[m][k] * b[n][k] + bias[n], a and b the values that codes and scales stand for, accumulated in
+ * fp32, y fp32 (QB_F32) or rounded to nearest even once (QB_BF16).  K is the codes' row length (a multiple of 128).  The formats
+ * of a and b may differ.  For a linear y = x W^T: forward a = x, b = W; grad_x: a = grad_y, b = W transposed; grad_W: a = grad_y
+ * transposed, b = x transposed.
+ *   bias dev fp32 [N] or NULL (read);  y dev [M][N], aligned to its elements (written)
+ * M, N and K as in qb_gemm.
+ */
+size_t qb_fp8_scale_bytes(int64_t rows, int64_t K);
+qb_status qb_quantize_fp8(const void* x, int type, int64_t M, int64_t K, int format, uint8_t* xq, uint8_t* x_scale,
+                          uint8_t* xqt, uint8_t* xt_scale, void* ws, size_t ws_bytes, void* cuda_stream);
+qb_status qb_quantize_fp8_weights(const void* w, int type, int64_t N, int64_t K, int format, uint8_t* wq, uint8_t* w_scale,
+                                  uint8_t* wqt, uint8_t* wt_scale, void* ws, size_t ws_bytes, void* cuda_stream);
+qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a_format, const uint8_t* b, const uint8_t* b_scale,
+                      int b_format, const float* bias, int64_t M, int64_t N, int64_t K, int out_type, void* y, void* ws,
+                      size_t ws_bytes, void* cuda_stream);
+
+/*
+ * Dropout whose mask is never stored.  (No counterpart in the paper, which fine-tunes BERT with its usual dropout.)
+ *     y[i] = (word(i) >= round(p * 2^32) ? x[i] / (1 - p) : 0) + residual[i],   one rounding to `type` at the end,
+ * word(i) = word i % 4 of Philox4x32 with seven rounds, counter (i / 4, rng[1] + call) as two 64-bit numbers, low words first,
+ * key rng[0] (low word first).  x / (1 - p) is x * (1 / (1 - p)) in fp32.  What is dropped may be infinite or NaN.
+ * The mask depends on i, rng and call alone: the gradient is the same call on grad_y without a residual (with the values that
+ * rng held in the forward pass).  Calls of one step take different `call`; between steps rng[1] moves on by as many, on the
+ * device, so that a captured step draws other masks each time it is replayed.
+ *   x, residual (or NULL)  dev [n] of `type`, aligned to their elements             (read)
+ *   rng                    dev uint64 [2]: seed, offset                             (read)
+ *   p                      0 <= p < 1 (0: nothing is dropped)
+ *   y                      dev [n] of `type`; may be x or residual                  (written)
+ * No workspace, no device-side status.  0 < n <= 2^40.
+ */
+qb_status qb_dropout(const void* x, int type, int64_t n, double p, const uint64_t* rng, uint64_t call, const void* residual,
+                     void* y, void* cuda_stream);
+
 /*
  * Mixed-precision assignment from Hessian spectra (Section 3.2, Eq. 2 and the paragraph after it).
  * Host-only: no GPU work, no stream, all pointers are HOST pointers.

@@ -40,6 +40,7 @@ EXPORTS = (
     "qb_quantize_pack_weights_batch", "qb_gemm_bf16", "qb_layer_linears_bf16",
     "qb_fake_quantize_weights", "qb_fake_quantize_weights_batch", "qb_ste_backward", "qb_quantize_embedding", "qb_embedding_lookup",
     "qb_gemm_i8", "qb_rowsum_i8", "qb_layer_linears_i8", "qb_sensitivity_bits", "qb_probe_wait_limit", "qb_layer_linears_launch_count", "qb_layer_linears_tile_tokens", "qb_quantize_pack_weights_launch_count", "qb_quantize_act_launch_count",
+    "qb_dropout", "qb_fp8_scale_bytes", "qb_quantize_fp8", "qb_quantize_fp8_weights", "qb_gemm_fp8",
 )
 NOALLOC_MAX_GROUPS = 4096
 
@@ -145,6 +146,16 @@ def lib() -> ctypes.CDLL:
     L.qb_layer_linears_i8.restype = i32
     L.qb_rowsum_i8.argtypes = [vp, i64, i64, vp, vp]
     L.qb_rowsum_i8.restype = i32
+    u64 = ctypes.c_uint64
+    L.qb_dropout.argtypes = [vp, i32, i64, ctypes.c_double, vp, u64, vp, vp, vp]
+    L.qb_dropout.restype = i32
+    L.qb_fp8_scale_bytes.argtypes = [i64, i64]
+    L.qb_fp8_scale_bytes.restype = sz
+    for f in (L.qb_quantize_fp8, L.qb_quantize_fp8_weights):
+        f.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, sz, vp]
+        f.restype = i32
+    L.qb_gemm_fp8.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i64, i64, i32, vp, vp, sz, vp]
+    L.qb_gemm_fp8.restype = i32
     L.qb_gemm_bf16.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, ctypes.c_int, ctypes.c_int, vp, vp, sz, vp]
     L.qb_gemm_bf16.restype = i32
     L.qb_layer_linears_bf16.argtypes = [ctypes.POINTER(LinearDescC), i32, vp, sz, vp]
@@ -445,3 +456,49 @@ def layer_linears_bf16(descs, ws: torch.Tensor) -> None:
         assert all(d.y.dtype == torch.bfloat16 for d in descs)
     arr = _descs(descs, LinearDescC, make_desc_array)
     (_native or _ext()).layer_linears_bf16(arr, ws)
+
+
+_FP8_FORMATS = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+_OUT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _one_of(table, dtype, what: str) -> int:
+    if dtype not in table:
+        raise QbertError(QB_ERR_INVALID, f"{what}: one of {', '.join(str(t) for t in table)}, not {dtype}")
+    return table[dtype]
+
+
+def dropout(x: torch.Tensor, p: float, rng: torch.Tensor, call: int = 0, residual: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``qb_dropout``: ``(keep ? x / (1 - p) : 0) + residual``, the mask made from ``rng`` (device int64 [2]: seed, offset) and
+    ``call``.  The gradient of ``x`` is the same call on the gradient, without ``residual`` and with the values that ``rng``
+    held.  ``out`` may be ``x``."""
+    return (_native or _ext()).dropout(x, p, rng, call, residual, out)
+
+
+def fp8_scale_bytes(rows: int, K: int) -> int:
+    return int(lib().qb_fp8_scale_bytes(rows, K))
+
+
+def quantize_fp8(x: torch.Tensor, ws: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, transposed: bool = False,
+                 codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                 codes_t: Optional[torch.Tensor] = None, scales_t: Optional[torch.Tensor] = None):
+    """``qb_quantize_fp8``: fp32, bfloat16 or fp16 [M,K] -> (codes [M, K up to 128], scales), blocks of 1 x 128; with
+    ``transposed`` also (codes [K, M up to 128], scales) in blocks of 128 rows, for products over the tokens."""
+    return (_native or _ext()).quantize_fp8(x, ws, _one_of(_FP8_FORMATS, dtype, "dtype"), bool(transposed), False, codes, scales,
+                                            codes_t, scales_t)
+
+
+def quantize_fp8_weights(w: torch.Tensor, ws: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, transposed: bool = False,
+                         codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                         codes_t: Optional[torch.Tensor] = None, scales_t: Optional[torch.Tensor] = None):
+    """``qb_quantize_fp8_weights``: as ``quantize_fp8`` with one scale per block of 128 x 128."""
+    return (_native or _ext()).quantize_fp8(w, ws, _one_of(_FP8_FORMATS, dtype, "dtype"), bool(transposed), True, codes, scales,
+                                            codes_t, scales_t)
+
+
+def gemm_fp8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, bias: Optional[torch.Tensor],
+             ws: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``qb_gemm_fp8``: ``y[m][n] = sum_k a[m][k] b[n][k] + bias[n]``, fp32 or bfloat16 [M,N].  Of a linear ``y = x W^T``: forward
+    ``a`` = x, ``b`` = W; gradient of x: ``a`` = grad_y, ``b`` = W transposed; of W: ``a`` = grad_y transposed, ``b`` = x transposed."""
+    return (_native or _ext()).gemm_fp8(a, a_scale, b, b_scale, bias, ws, _one_of(_OUT_TYPES, out_dtype, "out_dtype"), y)

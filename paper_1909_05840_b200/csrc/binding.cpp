@@ -14,12 +14,14 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
 #include <utility>
+#include <vector>
 
 #include "qbert.h"
 
@@ -333,6 +335,149 @@ PyObject* embedding_lookup(Args a) {
   return out.get();
 }
 
+// ---- 8-bit floating point, dropout -----------------------------------------------------------------------------------
+// These calls take tensors of the current device alone: its current stream is what they are enqueued on.
+const at::Tensor& here(PyObject* o, const char* what) {
+  const at::Tensor& t = tensor(o);
+  need(t.is_cuda() && t.is_contiguous() && t.device().index() == c10::cuda::current_device(), what);
+  return t;
+}
+// A caller's output has to have the type and the size of what is written.
+void fits(PyObject* o, at::ScalarType type, int64_t count, const char* what) {
+  if (o == Py_None) return;
+  const at::Tensor& t = here(o, what);
+  need(t.scalar_type() == type && t.numel() == count, what);
+}
+int element_type(const at::Tensor& t, const char* what) {
+  switch (t.scalar_type()) {
+    case at::kFloat: return QB_F32;
+    case at::kBFloat16: return QB_BF16;
+    case at::kHalf: return QB_F16;
+    default: fail(PyExc_AssertionError, what);
+  }
+}
+int fp8_format(const at::Tensor& t, const char* what) {
+  switch (t.scalar_type()) {
+    case at::kFloat8_e4m3fn: return QB_E4M3;
+    case at::kFloat8_e5m2: return QB_E5M2;
+    default: fail(PyExc_AssertionError, what);
+  }
+}
+Workspace workspace_here(PyObject* o) {
+  const at::Tensor& t = here(o, "ws: a contiguous CUDA tensor of bytes on the current device");
+  need(t.scalar_type() == at::kByte, "ws: a contiguous CUDA tensor of bytes on the current device");
+  return Workspace(o);
+}
+
+// dropout(x, p, rng, call, residual, out) -> out
+PyObject* dropout(Args a) {
+  const char* const what = "x: a contiguous fp32, bfloat16 or fp16 CUDA tensor on the current device";
+  const at::Tensor& x = here(a[0], what);
+  const int type = element_type(x, what);
+  const double p = PyFloat_AsDouble(a[1]);
+  if (p == -1.0 && PyErr_Occurred()) throw Failed{};
+  const at::Tensor& rng = here(a[2], "rng: int64 [2] on the current device (seed, offset)");
+  need(rng.scalar_type() == at::kLong && rng.numel() == 2, "rng: int64 [2] on the current device (seed, offset)");
+  const uint64_t call = PyLong_AsUnsignedLongLong(a[3]);
+  if (call == (uint64_t)-1 && PyErr_Occurred()) throw Failed{};
+  const int64_t n = x.numel();
+  fits(a[4], x.scalar_type(), n, "residual: contiguous, of the type and size of x");
+  fits(a[5], x.scalar_type(), n, "out: contiguous, of the type and size of x");
+  const at::Device device = x.device();
+  const std::vector<int64_t> shape = x.sizes().vec();
+  const at::ScalarType scalar = x.scalar_type();
+  const void* const x_data = x.const_data_ptr();
+  const uint64_t* const rng_data = static_cast<const uint64_t*>(rng.const_data_ptr());
+  const void* const residual = ptr(a[4]);
+  Out out(a[5]);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    out.make(shape, scalar, device);
+    st = qb_dropout(x_data, type, n, p, rng_data, call, residual, out.data, stream());
+  }
+  check(st, "qb_dropout");
+  return out.get();
+}
+
+// quantize_fp8(x, ws, format, transposed, weights, codes, scales, codes_t, scales_t) -> (codes, scales[, codes_t, scales_t])
+PyObject* quantize_fp8(Args a) {
+  const char* const what = "x: a contiguous fp32, bfloat16 or fp16 CUDA tensor of two dimensions on the current device";
+  const at::Tensor& x = here(a[0], what);
+  need(x.dim() == 2, what);
+  const int type = element_type(x, what), format = (int)integer(a[2]);
+  const Workspace ws = workspace_here(a[1]);
+  const bool transposed = integer(a[3]) != 0, weights = integer(a[4]) != 0;
+  const int64_t M = x.size(0), K = x.size(1), Kp = (K + 127) / 128 * 128, Mp = (M + 127) / 128 * 128;
+  const at::ScalarType code = format == QB_E4M3 ? at::kFloat8_e4m3fn : at::kFloat8_e5m2;
+  fits(a[5], code, M * Kp, "codes: contiguous, of the asked format, [M][K up to 128]");
+  fits(a[6], at::kByte, (int64_t)qb_fp8_scale_bytes(M, K), "scales: contiguous bytes, fp8_scale_bytes(M, K) of them");
+  if (transposed) {
+    fits(a[7], code, K * Mp, "codes_t: contiguous, of the asked format, [K][M up to 128]");
+    fits(a[8], at::kByte, (int64_t)qb_fp8_scale_bytes(K, M), "scales_t: contiguous bytes, fp8_scale_bytes(K, M) of them");
+  }
+  const at::Device device = x.device();
+  const void* const x_data = x.const_data_ptr();
+  Out q(a[5]), s(a[6]), qt(transposed ? a[7] : Py_None), s_t(transposed ? a[8] : Py_None);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    q.make({M, Kp}, code, device);
+    s.make({Mp / 128, (Kp + 511) / 512, 32, 4, 4}, at::kByte, device);
+    if (transposed) {
+      qt.make({K, Mp}, code, device);
+      s_t.make({Kp / 128, (Mp + 511) / 512, 32, 4, 4}, at::kByte, device);
+    }
+    st = (weights ? qb_quantize_fp8_weights : qb_quantize_fp8)(
+        x_data, type, M, K, format, static_cast<uint8_t*>(q.data), static_cast<uint8_t*>(s.data), static_cast<uint8_t*>(qt.data),
+        static_cast<uint8_t*>(s_t.data), ws.data, ws.bytes, stream());
+  }
+  check(st, weights ? "qb_quantize_fp8_weights" : "qb_quantize_fp8");
+  Out* const outs[4] = {&q, &s, &qt, &s_t};
+  const int count = transposed ? 4 : 2;
+  for (int i = 0; i < count; ++i) outs[i]->wrap();
+  PyObject* r = PyTuple_New(count);
+  if (!r) throw Failed{};
+  for (int i = 0; i < count; ++i) PyTuple_SET_ITEM(r, i, outs[i]->get());
+  return r;
+}
+
+// gemm_fp8(a, a_scale, b, b_scale, bias, ws, out_type, y) -> y
+PyObject* gemm_fp8(Args g) {
+  const char* const what_a = "a: contiguous e4m3 or e5m2 codes of two dimensions on the current device";
+  const char* const what_b = "b: contiguous e4m3 or e5m2 codes of two dimensions on the current device, rows as long as a's";
+  const at::Tensor& a = here(g[0], what_a);
+  const at::Tensor& b = here(g[2], what_b);
+  need(a.dim() == 2, what_a);
+  need(b.dim() == 2 && b.size(1) == a.size(1), what_b);
+  const int fa = fp8_format(a, what_a), fb = fp8_format(b, what_b), out_type = (int)integer(g[6]);
+  const int64_t M = a.size(0), N = b.size(0), K = a.size(1);
+  const auto scales = [](PyObject* o, int64_t rows, int64_t k, const char* what) {
+    const at::Tensor& t = here(o, what);
+    need(t.scalar_type() == at::kByte && t.numel() == (int64_t)qb_fp8_scale_bytes(rows, k), what);
+    return static_cast<const uint8_t*>(t.const_data_ptr());
+  };
+  const uint8_t* const sa = scales(g[1], M, K, "a_scale: the bytes that came with a");
+  const uint8_t* const sb = scales(g[3], N, K, "b_scale: the bytes that came with b");
+  fits(g[4], at::kFloat, N, "bias: contiguous fp32 [N] on the current device");
+  const Workspace ws = workspace_here(g[5]);
+  const at::ScalarType type = out_type == QB_F32 ? at::kFloat : at::kBFloat16;
+  fits(g[7], type, M * N, "y: contiguous [M][N] of the asked type on the current device");
+  const at::Device device = a.device();
+  const uint8_t* const a_data = static_cast<const uint8_t*>(a.const_data_ptr());
+  const uint8_t* const b_data = static_cast<const uint8_t*>(b.const_data_ptr());
+  const float* const bias = static_cast<const float*>(ptr(g[4]));
+  Out y(g[7]);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    y.make({M, N}, type, device);
+    st = qb_gemm_fp8(a_data, sa, fa, b_data, sb, fb, bias, M, N, K, out_type, y.data, ws.data, ws.bytes, stream());
+  }
+  check(st, "qb_gemm_fp8");
+  return y.get();
+}
+
 // The calls over an array of descriptors: (array, ws)
 template <class T, qb_status (*F)(const T*, int32_t, void*, size_t, void*)>
 PyObject* over_descs(Args a, const char* what) {
@@ -386,6 +531,9 @@ PyMethodDef g_methods[] = {QB_ENTRY(quantize_act, 5),
                            QB_ENTRY(ste_backward, 6),
                            QB_ENTRY(quantize_embedding, 5),
                            QB_ENTRY(embedding_lookup, 10),
+                           QB_ENTRY(dropout, 6),
+                           QB_ENTRY(quantize_fp8, 9),
+                           QB_ENTRY(gemm_fp8, 8),
                            QB_ENTRY(quantize_act_batch, 2),
                            QB_ENTRY(quantize_pack_weights_batch, 2),
                            QB_ENTRY(fake_quantize_weights_batch, 2),

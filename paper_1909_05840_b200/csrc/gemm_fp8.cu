@@ -1,0 +1,448 @@
+// qb_gemm_fp8: y[m][n] = sum over K of a[m][k] * b[n][k] + bias[n] on 8-bit floating point codes with one power-of-two scale per
+// row and block of 128 along K (qb_quantize_fp8, qb_quantize_fp8_weights).
+//
+// The scales enter inside the tensor cores: tcgen05.mma kind::mxf8f6f4 multiplies each row's 32 products of an instruction
+// by 2^(ea - 127) * 2^(eb - 127), the bytes taken from tensor memory, and accumulates in fp32, so that a tile is summed over all of
+// K in tensor memory at the full 8-bit rate and leaves it once (scales applied outside would cost an accumulator read per
+// block of 128).  A word holds the bytes of four blocks; the instruction descriptor names the byte, so that the scales are copied
+// to tensor memory once per 512 elements of K.
+//
+// One persistent CTA per SM, 12 warps:
+//   warp 0        TMA producer (one lane): codes of A and B (128-byte swizzle, K block of 128), every fourth block the scales
+//   warp 1        issues tcgen05.cp (scales) and tcgen05.mma, owns the tensor memory (one lane)
+//   warps 2..3    idle
+//   warps 4..11   epilogue, two per TMEM lane quarter: tcgen05.ld -> bias -> round -> shared memory -> TMA store
+// A tile is 128 rows of A per CTA x BT rows of B; TMEM lane = row of A, column = row of B.  Large products run as CTA pairs
+// (cta_group::2, 256 x 256): each CTA stages its own 128 rows of A and half of B's rows.  No load is multicast.
+// Two accumulators, so that the epilogue of a tile overlaps the products of the next.  At BT = 256 they and the scales
+// do not fit the 512 columns side by side: the accumulators overlap by 32 columns, which the epilogue reads first.
+// Every wait is bounded: on expiry the CTA records QB_ERR_TIMEOUT and leaves through the normal exit path.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "common.cuh"
+#include "fp8.cuh"
+#include "mbar_wait.cuh"
+#include "ptx.cuh"
+#include "tensormap.cuh"
+
+namespace qb {
+
+struct Fp8Params {
+  CUtensorMap tma, tmb;    // codes, box 128 bytes of K x the CTA's rows
+  CUtensorMap tmsa, tmsb;  // scales as rows of 512 bytes
+  CUtensorMap tmy;         // y, box 32 rows x 128 bytes
+  const float* bias;
+  void* y;
+  void* ws;
+  int32_t M, N, K;
+  int32_t n_tiles, tiles;
+  int32_t words;        // rows of 512 bytes of scales per 128 rows of codes
+  int32_t a_last, b_last;  // last block of 128 rows of A's and of B's scales
+  int32_t tma_store;    // 1: rows of y are 16-byte aligned
+  uint32_t idesc;       // the formats' part of the instruction descriptor
+};
+
+constexpr int kFp8EpilogueWarps = 8;
+constexpr int kFp8FirstEpilogueWarp = 4;
+constexpr int kFp8Threads = 32 * (kFp8FirstEpilogueWarp + kFp8EpilogueWarps);
+
+template <int BT, int CG>
+struct Fp8Cfg {
+  static constexpr int kABytes = 128 * 128;
+  static constexpr int kBBytes = BT / CG * 128;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kScaleBlocksB = (BT + 127) / 128;  // blocks of 128 rows of B's scales that a tile needs
+  static constexpr int kScaleBytes = 512 * (1 + kScaleBlocksB);
+  static constexpr int kStages = BT == 64 ? 6 : 5;
+  static constexpr int kOutBytes = kFp8EpilogueWarps * 32 * 128;
+  static constexpr int kBarBytes = 256;
+  static constexpr int kBiasBytes = 2 * 256 * 4;
+  static constexpr int kSmemBytes = kStages * (kStageBytes + kScaleBytes) + kOutBytes + kBarBytes + kBiasBytes;
+  static constexpr int kScaleCols = 4 * (1 + kScaleBlocksB);
+  static constexpr int kTmemCols = BT == 64 ? 256 : 512;
+  // the second accumulator's first column: behind the first where scales fit too, else 32 columns back
+  static constexpr int kAcc1 = 2 * BT + kScaleCols <= kTmemCols ? BT : BT - 32;
+  static constexpr bool kOverlap = kAcc1 < BT;
+  static constexpr int kScaleCol = kAcc1 + BT;
+  static_assert(kScaleCol + kScaleCols <= kTmemCols, "tensor memory");
+  static_assert(kSmemBytes <= 232448, "shared memory");
+};
+
+// Shared-memory matrix descriptor of a K-major operand with 128-byte swizzle: start address >> 4 (bits 0-13), leading offset
+// (16-29, unused here), 1024 bytes between groups of eight rows (32-45), version 1 (46-47), SWIZZLE_128B (61-63 = 2).
+__device__ __forceinline__ uint64_t fp8_operand_desc(uint32_t smem_addr) {
+  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// The same for 32 rows of 16 bytes without swizzle (scales): 128 bytes between groups of eight rows.
+__device__ __forceinline__ uint64_t fp8_scale_desc(uint32_t smem_addr) {
+  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+// Instruction descriptor for kind::mxf8f6f4 without the byte numbers of the scales (A's in bits 29-30, B's in 4-5): formats in
+// bits 7-9 and 10-12 (e4m3 0, e5m2 1), both operands K-major, N >> 3 in 17-22, scales UE8M0 (23), M >> 4 in 24-28.
+static uint32_t fp8_idesc(int a_format, int b_format, int mma_m, int mma_n) {
+  return ((uint32_t)a_format << 7) | ((uint32_t)b_format << 10) | ((uint32_t)(mma_n >> 3) << 17) | (1u << 23) | ((uint32_t)(mma_m >> 4) << 24);
+}
+
+// Barrier over the epilogue warps (named barrier 1) that also ORs a predicate over them.
+__device__ __forceinline__ bool fp8_epilogue_sync_or(bool pred) {
+  uint32_t res;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(res)
+      : "r"((uint32_t)pred), "n"(32 * kFp8EpilogueWarps)
+      : "memory");
+  return res != 0;
+}
+
+template <int BT, int CG, bool BF16>
+__global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_constant__ Fp8Params gp) {
+  using Cfg = Fp8Cfg<BT, CG>;
+  constexpr int kStages = Cfg::kStages;
+  constexpr int kRows = 128 * CG;  // rows of A per tile of the CTA group
+  const uint32_t rank = CG == 2 ? ptx::cluster_ctarank() : 0u;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t smem_base = ptx::smem_u32(smem);
+  uint8_t* const out_ptr = smem + kStages * Cfg::kStageBytes;  // 1024-byte aligned
+  const uint32_t scale_base = smem_base + kStages * Cfg::kStageBytes + Cfg::kOutBytes;
+  uint8_t* const bar_ptr = smem + kStages * (Cfg::kStageBytes + Cfg::kScaleBytes) + Cfg::kOutBytes;
+  const uint32_t bar_base = ptx::smem_u32(bar_ptr);
+  auto full = [&](int s) { return bar_base + 8u * s; };
+  auto empty = [&](int s) { return bar_base + 8u * (kStages + s); };
+  auto acc_full = [&](int a) { return bar_base + 8u * (2 * kStages + a); };
+  auto acc_empty = [&](int a) { return bar_base + 8u * (2 * kStages + 2 + a); };
+  const uint32_t overlap_read = bar_base + 8u * (2 * kStages + 4);  // the columns that both accumulators have were read
+  const uint32_t drain_bar = bar_base + 8u * (2 * kStages + 5);
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 8 * (2 * kStages + 6));
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* const bias_tile = reinterpret_cast<float*>(bar_ptr + Cfg::kBarBytes);  // [2][256]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if ((smem_base & 1023u) != 0u) {  // never expected; the swizzle needs it
+    pdl_begin();
+    if (threadIdx.x == 0) report_status(gp.ws, QB_ERR_CUDA, (int)smem_base);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      ptx::mbar_init(full(s), 1);
+      ptx::mbar_init(empty(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(acc_full(a), 1);
+      ptx::mbar_init(acc_empty(a), kFp8EpilogueWarps * CG);
+    }
+    ptx::mbar_init(overlap_read, 4 * CG);
+    ptx::mbar_init(drain_bar, 1);
+    *abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_cg<CG>(ptx::smem_u32(tmem_slot), Cfg::kTmemCols);
+    ptx::tmem_relinquish_cg<CG>();
+  }
+  ptx::tcgen05_fence_before_sync();
+  __syncthreads();
+  if constexpr (CG == 2) ptx::cluster_sync_all();
+  ptx::tcgen05_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_begin();
+  // the barriers that the issuer waits on live in the group's first CTA
+  auto lead = [&](uint32_t bar) { return CG == 2 ? ptx::map_to_cta(bar, 0) : bar; };
+
+  const int groups = (int)gridDim.x / CG, group = (int)blockIdx.x / CG;
+  const int k_blocks = gp.K / 128;
+  bool timed_out = false;
+  int where = 0;
+
+  if (warp == 0) {
+    // ---------------- TMA producer ------------------------------------------------------------------
+    if (ptx::elect_one()) {
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int t = group; t < gp.tiles && !timed_out; t += groups) {
+        const int m0 = t / gp.n_tiles * kRows + (int)rank * 128, n0 = t % gp.n_tiles * BT;
+        const int sa = min(m0 / 128, gp.a_last) * gp.words;
+        for (int kb = 0; kb < k_blocks; ++kb) {
+          if (!wait_barrier_relaxed(empty(stage), phase ^ 1u, abort_flag)) {
+            timed_out = true;
+            where = (0 << 16) | stage;
+            break;
+          }
+          const bool scales = (kb & 3) == 0;
+          const uint32_t a_smem = smem_base + stage * Cfg::kStageBytes, b_smem = a_smem + Cfg::kABytes;
+          const uint32_t s_smem = scale_base + stage * Cfg::kScaleBytes;
+          if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), CG * (Cfg::kStageBytes + (scales ? Cfg::kScaleBytes : 0)));
+          auto load = [&](uint32_t dst, const CUtensorMap* tm, int x, int y) {
+            if constexpr (CG == 2) ptx::tma_load_2d_pair(dst, tm, lead(full(stage)), x, y);
+            else ptx::tma_load_2d(dst, tm, full(stage), x, y);
+          };
+          if (scales) {
+            load(s_smem, &gp.tmsa, 0, sa + kb / 4);
+#pragma unroll
+            for (int j = 0; j < Cfg::kScaleBlocksB; ++j)
+              load(s_smem + 512 * (1 + j), &gp.tmsb, 0, min(n0 / 128 + j, gp.b_last) * gp.words + kb / 4);
+          }
+          load(a_smem, &gp.tma, kb * 128, m0);
+          load(b_smem, &gp.tmb, kb * 128, n0 + (int)rank * (BT / CG));
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (timed_out) {  // let copies in flight land before the CTA's shared memory is released
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000ll) {
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer (of a pair: in its first CTA only) ----------------------------------
+    if (rank == 0 && ptx::elect_one()) {
+      const uint64_t a_desc0 = fp8_operand_desc(smem_base), b_desc0 = fp8_operand_desc(smem_base + Cfg::kABytes);
+      const uint64_t s_desc0 = fp8_scale_desc(scale_base);
+      const uint32_t sfa = tmem_base + Cfg::kScaleCol, sfb0 = sfa + 4;
+      int stage = 0, it = 0;
+      uint32_t phase = 0;
+      for (int t = group; t < gp.tiles && !timed_out; t += groups, ++it) {
+        const int a = it & 1;
+        const uint32_t d = tmem_base + (a ? Cfg::kAcc1 : 0);
+        const uint32_t sfb = sfb0 + (uint32_t)(t % gp.n_tiles * BT % 128 / 32);  // where the tile begins in its block of 128 scales
+        bool ok = wait_barrier(acc_empty(a), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag);
+        if (Cfg::kOverlap && ok && it > 0) ok = wait_barrier(overlap_read, (uint32_t)(it - 1) & 1u, abort_flag);
+        if (!ok) {
+          timed_out = true;
+          where = (1 << 16) | 0x100 | a;
+          break;
+        }
+        for (int kb = 0; kb < k_blocks; ++kb) {
+          if (!wait_barrier(full(stage), phase, abort_flag)) {
+            timed_out = true;
+            where = (1 << 16) | stage;
+            break;
+          }
+          ptx::tcgen05_fence_after_sync();
+          const uint32_t id = (uint32_t)kb & 3u;
+          if (id == 0) {
+            const uint64_t s_desc = s_desc0 + (uint64_t)(stage * (Cfg::kScaleBytes >> 4));
+#pragma unroll
+            for (int j = 0; j <= Cfg::kScaleBlocksB; ++j) ptx::tmem_copy_scales_cg<CG>(sfa + 4 * j, s_desc + (uint64_t)(j * (512 >> 4)));
+          }
+          const uint32_t idesc = gp.idesc | (id << 29) | (id << 4);
+          const uint64_t a_desc = a_desc0 + (uint64_t)(stage * (Cfg::kStageBytes >> 4));
+          const uint64_t b_desc = b_desc0 + (uint64_t)(stage * (Cfg::kStageBytes >> 4));
+#pragma unroll
+          for (int j = 0; j < 4; ++j)  // 32 elements of K per instruction: 32 bytes
+            ptx::mma_mxf8_ss_cg<CG>(d, a_desc + 2u * j, b_desc + 2u * j, idesc, sfa, sfb, (kb | j) != 0 ? 1u : 0u);
+          ptx::mma_commit_cg<CG>(empty(stage));
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        if (!timed_out) ptx::mma_commit_cg<CG>(acc_full(a));
+      }
+      if (timed_out) {  // wait (bounded) for what was issued before tensor memory is freed
+        ptx::mma_commit_cg<CG>(drain_bar);
+        const long long t0 = clock64();
+        while (!ptx::mbar_try_wait(drain_bar, 0) && clock64() - t0 < 400000000ll) {
+        }
+      }
+    }
+  } else if (warp >= kFp8FirstEpilogueWarp) {
+    // ---------------- epilogue ----------------------------------------------------------------------
+    constexpr int kCols = BF16 ? 64 : 32;  // columns of a chunk: 128 bytes of y
+    const int ew = warp - kFp8FirstEpilogueWarp, quarter = warp & 3, half = ew >> 2;
+    const int e = threadIdx.x - 32 * kFp8FirstEpilogueWarp;
+    uint8_t* const buf = out_ptr + ew * (32 * 128);
+    const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    auto arrive = [&](uint32_t bar) {  // this warp has read from tensor memory what it announces
+      ptx::tcgen05_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        if (CG == 2 && rank != 0) ptx::mbar_arrive_remote(lead(bar));
+        else ptx::mbar_arrive(bar);
+      }
+    };
+    int it = 0;
+    for (int t = group; t < gp.tiles; t += groups, ++it) {
+      const int a = it & 1;
+      const int m0 = t / gp.n_tiles * kRows + (int)rank * 128 + quarter * 32, n0 = t % gp.n_tiles * BT;
+      bias_tile[a * 256 + e] = gp.bias && e < BT && n0 + e < gp.N ? gp.bias[n0 + e] : 0.0f;
+      const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
+      if (fp8_epilogue_sync_or(!ok)) {  // publishes the bias, and all eight warps give up together
+        timed_out = true;
+        where = (3 << 16) | a;
+        break;
+      }
+      ptx::tcgen05_fence_after_sync();
+      const uint32_t acc = lanes + (a ? Cfg::kAcc1 : 0);
+      const int chunks = m0 < gp.M ? min(BT / kCols, (gp.N - n0 + kCols - 1) / kCols) : 0;
+      // accumulator 0 shares its last 32 columns, accumulator 1 its first: they are read first, by the quarter's first warp
+      const bool down = Cfg::kOverlap && a == 0;
+      if (Cfg::kOverlap && half == 0 && (down ? chunks < BT / kCols : chunks == 0)) arrive(overlap_read);
+      if (half >= chunks) arrive(acc_empty(a));
+#pragma unroll 1
+      for (int i = half; i < chunks; i += 2) {
+        const int c0 = (down ? chunks - 1 - i : i) * kCols;
+        uint32_t v[kCols / 32][32];
+#pragma unroll
+        for (int p = 0; p < kCols / 32; ++p) ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(c0 + 32 * p), v[p]);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int p = 0; p < kCols / 32; ++p) ptx::tmem_ld_regs_ready(v[p]);
+        if (Cfg::kOverlap && i == 0 && (!down || chunks == BT / kCols)) arrive(overlap_read);
+        if (i + 2 >= chunks) arrive(acc_empty(a));
+        const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + a * 256 + c0);
+        if (lane == 0) ptx::tma_store_wait_read0();  // the warp's last store has read the buffer
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {  // 16 bytes of the row at a time; the swizzle keeps the lanes on different banks
+          uint4 w;
+          if constexpr (BF16) {
+            const float4 b0 = b4[2 * j], b1 = b4[2 * j + 1];
+            const uint32_t* const s = &v[j >> 2][(j & 3) * 8];
+            const __nv_bfloat162 p0 = __floats2bfloat162_rn(__uint_as_float(s[0]) + b0.x, __uint_as_float(s[1]) + b0.y);
+            const __nv_bfloat162 p1 = __floats2bfloat162_rn(__uint_as_float(s[2]) + b0.z, __uint_as_float(s[3]) + b0.w);
+            const __nv_bfloat162 p2 = __floats2bfloat162_rn(__uint_as_float(s[4]) + b1.x, __uint_as_float(s[5]) + b1.y);
+            const __nv_bfloat162 p3 = __floats2bfloat162_rn(__uint_as_float(s[6]) + b1.z, __uint_as_float(s[7]) + b1.w);
+            w.x = *reinterpret_cast<const uint32_t*>(&p0);
+            w.y = *reinterpret_cast<const uint32_t*>(&p1);
+            w.z = *reinterpret_cast<const uint32_t*>(&p2);
+            w.w = *reinterpret_cast<const uint32_t*>(&p3);
+          } else {
+            const float4 b0 = b4[j];
+            const uint32_t* const s = &v[0][j * 4];
+            w.x = __float_as_uint(__uint_as_float(s[0]) + b0.x);
+            w.y = __float_as_uint(__uint_as_float(s[1]) + b0.y);
+            w.z = __float_as_uint(__uint_as_float(s[2]) + b0.z);
+            w.w = __float_as_uint(__uint_as_float(s[3]) + b0.w);
+          }
+          *reinterpret_cast<uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = w;
+        }
+        if (gp.tma_store) {
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            ptx::tma_store_2d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0);
+            ptx::tma_store_commit();
+          }
+        } else {  // rows of y of any alignment: a row at a time, the lanes on consecutive columns
+          __syncwarp();
+          const int rows = min(32, gp.M - m0);
+          for (int r = 0; r < rows; ++r) {
+#pragma unroll
+            for (int p = 0; p < kCols / 32; ++p) {
+              const int c = lane + 32 * p, col = n0 + c0 + c;
+              if (col >= gp.N) continue;
+              const size_t at = (size_t)(m0 + r) * gp.N + col;
+              if constexpr (BF16)
+                static_cast<uint16_t*>(gp.y)[at] = *reinterpret_cast<const uint16_t*>(buf + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2);
+              else
+                static_cast<float*>(gp.y)[at] = *reinterpret_cast<const float*>(buf + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4);
+            }
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (lane == 0) ptx::tma_store_wait_read0();
+  }
+  if (timed_out) {
+    *abort_flag = 1;
+    report_status(gp.ws, QB_ERR_TIMEOUT, where);
+  }
+  ptx::tcgen05_fence_before_sync();
+  __syncthreads();
+  if constexpr (CG == 2) ptx::cluster_sync_all();  // the other CTA's MMAs and arrivals reach into this CTA
+  if (warp == 1) {
+    __syncwarp();
+    ptx::tcgen05_fence_after_sync();
+    ptx::tmem_dealloc_cg<CG>(tmem_base, Cfg::kTmemCols);
+  }
+}
+
+template <int BT, int CG, bool BF16>
+static qb_status launch_gemm_fp8(const Fp8Params& gp, int sms, cudaStream_t stream) {
+  using Cfg = Fp8Cfg<BT, CG>;
+  auto kernel = gemm_fp8_kernel<BT, CG, BF16>;
+  static std::atomic<bool> attr_set[64] = {};
+  int dev = 0;
+  QB_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+    QB_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes));
+    if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
+  }
+  const int grid = std::min(gp.tiles, sms / CG) * CG;
+  QB_CUDA_TRY(launch_kernel(kernel, (unsigned)grid, kFp8Threads, Cfg::kSmemBytes, stream, CG, false, gp));
+  return QB_OK;
+}
+
+}  // namespace qb
+
+extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a_format, const uint8_t* b, const uint8_t* b_scale,
+                                 int b_format, const float* bias, int64_t M, int64_t N, int64_t K, int out_type, void* y, void* ws,
+                                 size_t ws_bytes, void* cuda_stream) {
+  using namespace qb;
+  if (!a || !a_scale || !b || !b_scale || !y || M <= 0 || N <= 0 || K <= 0 || M > QB_MAX_MN || N > QB_MAX_MN || K > QB_MAX_K ||
+      a_format < QB_E4M3 || a_format > QB_E5M2 || b_format < QB_E4M3 || b_format > QB_E5M2 || out_type < QB_F32 || out_type > QB_BF16) {
+    set_last_error("qb_gemm_fp8: invalid argument (M=%lld N=%lld K=%lld formats %d, %d, output type %d)", (long long)M, (long long)N,
+                   (long long)K, a_format, b_format, out_type);
+    return QB_ERR_INVALID;
+  }
+  if (K % 128 != 0 || !aligned16(a) || !aligned16(b) || !aligned16(a_scale) || !aligned16(b_scale) ||
+      reinterpret_cast<uintptr_t>(y) % (out_type == QB_F32 ? 4 : 2) != 0) {
+    set_last_error("qb_gemm_fp8: K must be a multiple of 128, codes and scales 16-byte aligned, y aligned to its elements");
+    return QB_ERR_ALIGN;
+  }
+  if (!ws || ws_bytes < kWsMinBytes) {
+    set_last_error("qb_gemm_fp8: workspace null or too small");
+    return QB_ERR_WORKSPACE;
+  }
+  int sms = 0;
+  qb_status st = require_sm100(&sms);
+  if (st != QB_OK) return st;
+  const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m; };
+  if (up(M, 128) * up(N, 64) > (int64_t)1 << 30) {
+    set_last_error("qb_gemm_fp8: more than 2^30 tiles (M=%lld N=%lld)", (long long)M, (long long)N);
+    return QB_ERR_INVALID;
+  }
+  const int cg = sms >= 2 && up(M, 256) * up(N, 256) >= sms / 2 ? 2 : 1;
+  const int bt = cg == 2 ? 256 : (up(M, 128) * up(N, 128) >= sms ? 128 : 64);
+  Fp8Params gp;
+  const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8, u32 = CU_TENSOR_MAP_DATA_TYPE_UINT32;
+  gp.words = (int32_t)fp8_scale_words(K);
+  if ((st = make_matrix_map(&gp.tma, u8, a, M, K, K, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != QB_OK) return st;
+  if ((st = make_matrix_map(&gp.tmb, u8, b, N, K, K, bt / cg, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != QB_OK) return st;
+  if ((st = make_matrix_map(&gp.tmsa, u32, a_scale, up(M, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
+  if ((st = make_matrix_map(&gp.tmsb, u32, b_scale, up(N, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
+  const int size = out_type == QB_F32 ? 4 : 2;
+  gp.tma_store = N * size % 16 == 0 && aligned16(y);
+  if (gp.tma_store) {
+    st = make_matrix_map(&gp.tmy, size == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, y, M, N, N * size, 32,
+                         128 / size, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
+    if (st != QB_OK) return st;
+  } else {
+    gp.tmy = gp.tma;  // not used
+  }
+  gp.bias = bias;
+  gp.y = y;
+  gp.ws = ws;
+  gp.M = (int32_t)M;
+  gp.N = (int32_t)N;
+  gp.K = (int32_t)K;
+  gp.n_tiles = (int32_t)up(N, bt);
+  gp.tiles = (int32_t)(up(M, 128 * cg) * gp.n_tiles);
+  gp.a_last = (int32_t)up(M, 128) - 1;
+  gp.b_last = (int32_t)up(N, 128) - 1;
+  gp.idesc = fp8_idesc(a_format, b_format, 128 * cg, bt);
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  const bool bf16 = out_type == QB_BF16;
+  if (cg == 2) return bf16 ? launch_gemm_fp8<256, 2, true>(gp, sms, stream) : launch_gemm_fp8<256, 2, false>(gp, sms, stream);
+  if (bt == 128) return bf16 ? launch_gemm_fp8<128, 1, true>(gp, sms, stream) : launch_gemm_fp8<128, 1, false>(gp, sms, stream);
+  return bf16 ? launch_gemm_fp8<64, 1, true>(gp, sms, stream) : launch_gemm_fp8<64, 1, false>(gp, sms, stream);
+}
