@@ -443,6 +443,37 @@ qb_status qb_dropout(const void* x, int type, int64_t n, double p, const uint64_
                      void* y, void* cuda_stream);
 
 /*
+ * Softmax cross entropy over a large vocabulary, from the hidden states, without keeping the logits.  (No counterpart in the
+ * paper; BERT's masked-word loss, whose decoder is the word embedding.)
+ *     z[t][v] = sum_d h[t][d] * w[v][d] + bias[v],   lse[t] = log sum_v exp z[t][v],   loss[t] = lse[t] - z[t][targets[t]]
+ * and, with g[t][v] = grad_loss[t] * (exp(z[t][v] - lse[t]) - [v = targets[t]]),
+ *     grad_h = g w,   grad_w = g^T h,   grad_bias[v] = sum_t g[t][v].
+ * The products are accumulated in fp32 and the softmax is held in fp32; g is rounded to bfloat16 for its two products (and not for
+ * grad_bias), grad_h and grad_w once more at the end.  The backward pass forms the logits again, a piece of the vocabulary at a
+ * time.  The sums' order does not change from call to call.
+ * A negative target (padding) has loss 0 and contributes no gradient; its lse is written.  So does a target >= V, and
+ * QB_ERR_INVALID is recorded in the status word (by the forward pass).  A bias of -infinity takes a word out.  NaN and
+ * infinities propagate as in the formulas.
+ *   h, w         dev bfloat16 [T][D], [V][D], 16-byte aligned                (read)
+ *   bias         dev fp32 [V] or NULL                                        (read)
+ *   targets      dev int32 [T]                                               (read)
+ *   loss, lse    dev fp32 [T]                                                (written; lse read by the backward pass)
+ *   grad_loss    dev fp32 [T]: the gradient of each token's loss (1 / T for their mean)    (read)
+ *   grad_h, grad_w   dev bfloat16 [T][D], [V][D], 16-byte aligned, or NULL   (written)
+ *   grad_bias    dev fp32 [V] or NULL; one of the three has to be given      (written)
+ * D is a multiple of 8, at most QB_MAX_VOCAB_D.  The workspace is 256-byte aligned; qb_vocab_loss_workspace_bytes(T, V, D) serves
+ * both calls (0 on invalid arguments).  The backward pass takes less too, in smaller pieces, and refuses what is too little for
+ * pieces of 256 words.
+ */
+#define QB_MAX_VOCAB_D 8192
+size_t qb_vocab_loss_workspace_bytes(int64_t T, int64_t V, int64_t D);
+qb_status qb_vocab_loss(const uint16_t* h, const uint16_t* w, const float* bias, const int32_t* targets, int64_t T, int64_t V,
+                        int64_t D, float* loss, float* lse, void* ws, size_t ws_bytes, void* cuda_stream);
+qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w, const float* bias, const int32_t* targets, const float* lse,
+                                 const float* grad_loss, int64_t T, int64_t V, int64_t D, uint16_t* grad_h, uint16_t* grad_w,
+                                 float* grad_bias, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
  * Mixed-precision assignment from Hessian spectra (Section 3.2, Eq. 2 and the paragraph after it).
  * Host-only: no GPU work, no stream, all pointers are HOST pointers.
  *

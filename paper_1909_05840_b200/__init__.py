@@ -41,6 +41,7 @@ EXPORTS = (
     "qb_fake_quantize_weights", "qb_fake_quantize_weights_batch", "qb_ste_backward", "qb_quantize_embedding", "qb_embedding_lookup",
     "qb_gemm_i8", "qb_rowsum_i8", "qb_layer_linears_i8", "qb_sensitivity_bits", "qb_probe_wait_limit", "qb_layer_linears_launch_count", "qb_layer_linears_tile_tokens", "qb_quantize_pack_weights_launch_count", "qb_quantize_act_launch_count",
     "qb_dropout", "qb_fp8_scale_bytes", "qb_quantize_fp8", "qb_quantize_fp8_weights", "qb_gemm_fp8",
+    "qb_vocab_loss_workspace_bytes", "qb_vocab_loss", "qb_vocab_loss_backward",
 )
 NOALLOC_MAX_GROUPS = 4096
 
@@ -156,6 +157,12 @@ def lib() -> ctypes.CDLL:
         f.restype = i32
     L.qb_gemm_fp8.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i64, i64, i32, vp, vp, sz, vp]
     L.qb_gemm_fp8.restype = i32
+    L.qb_vocab_loss_workspace_bytes.argtypes = [i64, i64, i64]
+    L.qb_vocab_loss_workspace_bytes.restype = sz
+    L.qb_vocab_loss.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
+    L.qb_vocab_loss.restype = i32
+    L.qb_vocab_loss_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    L.qb_vocab_loss_backward.restype = i32
     L.qb_gemm_bf16.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, ctypes.c_int, ctypes.c_int, vp, vp, sz, vp]
     L.qb_gemm_bf16.restype = i32
     L.qb_layer_linears_bf16.argtypes = [ctypes.POINTER(LinearDescC), i32, vp, sz, vp]
@@ -502,3 +509,32 @@ def gemm_fp8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: t
     """``qb_gemm_fp8``: ``y[m][n] = sum_k a[m][k] b[n][k] + bias[n]``, fp32 or bfloat16 [M,N].  Of a linear ``y = x W^T``: forward
     ``a`` = x, ``b`` = W; gradient of x: ``a`` = grad_y, ``b`` = W transposed; of W: ``a`` = grad_y transposed, ``b`` = x transposed."""
     return (_native or _ext()).gemm_fp8(a, a_scale, b, b_scale, bias, ws, _one_of(_OUT_TYPES, out_dtype, "out_dtype"), y)
+
+
+def vocab_loss_workspace_bytes(T: int, V: int, D: int) -> int:
+    return int(lib().qb_vocab_loss_workspace_bytes(T, V, D))
+
+
+def vocab_loss_workspace(T: int, V: int, D: int, device="cuda") -> torch.Tensor:
+    """A zero-initialised workspace for ``vocab_loss`` and ``vocab_loss_backward`` of up to these sizes (and any other call that
+    needs no more)."""
+    ws = torch.empty(max(vocab_loss_workspace_bytes(T, V, D), workspace_bytes(groups=4096)), dtype=torch.uint8, device=device)
+    _check(lib().qb_workspace_init(ws.data_ptr(), ws.numel(), _stream()), "qb_workspace_init")
+    return ws
+
+
+def vocab_loss(h: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], targets: torch.Tensor, ws: torch.Tensor,
+               loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """``qb_vocab_loss``: bfloat16 ``h`` [T,D], ``w`` [V,D], fp32 ``bias`` [V] or None, int32 ``targets`` [T] (negative: ignored) ->
+    (loss fp32 [T], log-sum-exp fp32 [T])."""
+    return (_native or _ext()).vocab_loss(h, w, bias, targets, ws, loss, lse)
+
+
+def vocab_loss_backward(h: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], targets: torch.Tensor, lse: torch.Tensor,
+                        grad_loss: torch.Tensor, ws: torch.Tensor, grad_h: Optional[torch.Tensor] = None,
+                        grad_w: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None,
+                        needs=(True, True, True)):
+    """``qb_vocab_loss_backward``: fp32 ``grad_loss`` [T] -> (grad_h bfloat16 [T,D], grad_w bfloat16 [V,D], grad_bias fp32 [V] or
+    None without ``bias``); ``needs`` says which of them are computed (None for the others)."""
+    need = [bool(n) for n in needs]
+    return (_native or _ext()).vocab_loss_backward(h, w, bias, targets, lse, grad_loss, ws, grad_h, grad_w, grad_bias, *need)

@@ -478,6 +478,95 @@ PyObject* gemm_fp8(Args g) {
   return y.get();
 }
 
+// ---- vocabulary loss ---------------------------------------------------------------------------------------------------
+struct VocabInputs {
+  int64_t T, V, D;
+  const uint16_t *h, *w;
+  const float* bias;
+  const int32_t* targets;
+  at::Device device;
+  static const at::Tensor& matrix(PyObject* o, const char* what) {
+    const at::Tensor& t = here(o, what);
+    need(t.dim() == 2 && t.scalar_type() == at::kBFloat16, what);
+    return t;
+  }
+  VocabInputs(PyObject* ho, PyObject* wo, PyObject* bo, PyObject* to) : device(at::kCUDA) {
+    const at::Tensor& ht = matrix(ho, "h: contiguous bfloat16 [T][D] on the current device");
+    const at::Tensor& wt = matrix(wo, "w: contiguous bfloat16 [V][D] on the current device");
+    T = ht.size(0);
+    D = ht.size(1);
+    V = wt.size(0);
+    need(wt.size(1) == D, "w: contiguous bfloat16 [V][D] on the current device");
+    fits(bo, at::kFloat, V, "bias: contiguous fp32 [V] on the current device");
+    need(to != Py_None, "targets: contiguous int32 [T] on the current device");
+    fits(to, at::kInt, T, "targets: contiguous int32 [T] on the current device");
+    h = static_cast<const uint16_t*>(ht.const_data_ptr());
+    w = static_cast<const uint16_t*>(wt.const_data_ptr());
+    bias = static_cast<const float*>(ptr(bo));
+    targets = static_cast<const int32_t*>(ptr(to));
+    device = ht.device();
+  }
+};
+
+// vocab_loss(h, w, bias, targets, ws, loss, lse) -> (loss, lse)
+PyObject* vocab_loss(Args a) {
+  const VocabInputs in(a[0], a[1], a[2], a[3]);
+  const Workspace ws = workspace_here(a[4]);
+  fits(a[5], at::kFloat, in.T, "loss: contiguous fp32 [T] on the current device");
+  fits(a[6], at::kFloat, in.T, "lse: contiguous fp32 [T] on the current device");
+  Out loss(a[5]), lse(a[6]);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    loss.make({in.T}, at::kFloat, in.device);
+    lse.make({in.T}, at::kFloat, in.device);
+    st = qb_vocab_loss(in.h, in.w, in.bias, in.targets, in.T, in.V, in.D, static_cast<float*>(loss.data), static_cast<float*>(lse.data),
+                       ws.data, ws.bytes, stream());
+  }
+  check(st, "qb_vocab_loss");
+  loss.wrap();
+  lse.wrap();
+  PyObject* r = PyTuple_New(2);
+  if (!r) throw Failed{};
+  PyTuple_SET_ITEM(r, 0, loss.get());
+  PyTuple_SET_ITEM(r, 1, lse.get());
+  return r;
+}
+
+// vocab_loss_backward(h, w, bias, targets, lse, grad_loss, ws, grad_h, grad_w, grad_bias, need_h, need_w, need_bias) -> three gradients
+PyObject* vocab_loss_backward(Args a) {
+  const VocabInputs in(a[0], a[1], a[2], a[3]);
+  need(a[4] != Py_None, "lse: contiguous fp32 [T] on the current device");
+  fits(a[4], at::kFloat, in.T, "lse: contiguous fp32 [T] on the current device");
+  need(a[5] != Py_None, "grad_loss: contiguous fp32 [T] on the current device");
+  fits(a[5], at::kFloat, in.T, "grad_loss: contiguous fp32 [T] on the current device");
+  const Workspace ws = workspace_here(a[6]);
+  fits(a[7], at::kBFloat16, in.T * in.D, "grad_h: contiguous bfloat16 [T][D] on the current device");
+  fits(a[8], at::kBFloat16, in.V * in.D, "grad_w: contiguous bfloat16 [V][D] on the current device");
+  fits(a[9], at::kFloat, in.V, "grad_bias: contiguous fp32 [V] on the current device");
+  const bool want[3] = {integer(a[10]) != 0, integer(a[11]) != 0, integer(a[12]) != 0 && (in.bias || a[9] != Py_None)};
+  Out gh(want[0] ? a[7] : Py_None), gw(want[1] ? a[8] : Py_None), gb(want[2] ? a[9] : Py_None);
+  const float* const lse = static_cast<const float*>(ptr(a[4]));
+  const float* const grad_loss = static_cast<const float*>(ptr(a[5]));
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    if (want[0]) gh.make({in.T, in.D}, at::kBFloat16, in.device);
+    if (want[1]) gw.make({in.V, in.D}, at::kBFloat16, in.device);
+    if (want[2]) gb.make({in.V}, at::kFloat, in.device);
+    st = qb_vocab_loss_backward(in.h, in.w, in.bias, in.targets, lse, grad_loss, in.T, in.V, in.D, static_cast<uint16_t*>(gh.data),
+                                static_cast<uint16_t*>(gw.data), static_cast<float*>(gb.data), ws.data, ws.bytes, stream());
+  }
+  check(st, "qb_vocab_loss_backward");
+  Out* const outs[3] = {&gh, &gw, &gb};
+  for (int i = 0; i < 3; ++i)
+    if (want[i]) outs[i]->wrap();
+  PyObject* r = PyTuple_New(3);
+  if (!r) throw Failed{};
+  for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(r, i, want[i] ? outs[i]->get() : Py_NewRef(Py_None));
+  return r;
+}
+
 // The calls over an array of descriptors: (array, ws)
 template <class T, qb_status (*F)(const T*, int32_t, void*, size_t, void*)>
 PyObject* over_descs(Args a, const char* what) {
@@ -534,6 +623,8 @@ PyMethodDef g_methods[] = {QB_ENTRY(quantize_act, 5),
                            QB_ENTRY(dropout, 6),
                            QB_ENTRY(quantize_fp8, 9),
                            QB_ENTRY(gemm_fp8, 8),
+                           QB_ENTRY(vocab_loss, 7),
+                           QB_ENTRY(vocab_loss_backward, 13),
                            QB_ENTRY(quantize_act_batch, 2),
                            QB_ENTRY(quantize_pack_weights_batch, 2),
                            QB_ENTRY(fake_quantize_weights_batch, 2),

@@ -130,6 +130,13 @@ __device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src_smem
                "r"(src_smem), "r"(x), "r"(y)
                : "memory");
 }
+// The same, adding the fp32 values of the box to those in memory.
+__device__ __forceinline__ void tma_add_2d(const void* tmap, uint32_t src_smem, int32_t x, int32_t y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(tmap)),
+               "r"(src_smem), "r"(x), "r"(y)
+               : "memory");
+}
 __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Wait until at most N bulk-store groups of this thread are still READING shared memory.
 __device__ __forceinline__ void tma_store_wait_read0() {

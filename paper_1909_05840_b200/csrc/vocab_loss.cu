@@ -1,0 +1,801 @@
+// qb_vocab_loss, qb_vocab_loss_backward: softmax cross entropy of hidden states h [T][D] over a vocabulary w [V][D], logits
+// z = h w^T + bias, without keeping the logits.
+//
+// Forward: tiles of 256 tokens x 256 words are multiplied on the tensor cores and reduced to a maximum and a sum of exponentials
+// per token where they lie (tensor memory -> registers); a second kernel joins the tiles of a token.
+// Backward: with the forward pass's lse, g[v][t] = grad_loss[t] * (exp(z[t][v] - lse[t]) - [v = target[t]]) needs no reduction.
+// The vocabulary is taken in pieces: for one piece g is formed (the logits again) and rounded to bfloat16 into the workspace,
+// transposed, while the two products of the piece before it,
+//     grad_w [piece][D] = g h      and      grad_h [T][D] += g^T w,
+// run in the same launch: the three kinds of tile are dealt over the SMs so that all end together.  grad_h is summed over the
+// pieces in fp32 in the workspace (each element by one addition per launch, or into a slab of its own: the order is always the
+// same); a last kernel rounds it and sums the bias's gradient, whose terms never were bfloat16.
+//
+// One product kernel for all of it: CTA pairs (tcgen05 cta_group::2, kind::f16, bfloat16 operands, fp32 accumulators), tiles of
+// 256 x 256, K blocks of 64, a ring of five stages of 32 KB per CTA, two accumulators in tensor memory.  An operand lies in
+// shared memory as the tensor has it: contraction along its rows (K-major) or down its columns (MN-major), two boxes of
+// 64 x 64 per CTA either way, so that nothing is transposed in memory.  12 warps: 0 loads (TMA), 1 issues MMAs,
+// 4..11 epilogue, two per TMEM lane quarter.  Every wait is bounded, as in qb_gemm.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+
+#include "common.cuh"
+#include "mbar_wait.cuh"
+#include "ptx.cuh"
+#include "tensormap.cuh"
+
+namespace qb {
+
+constexpr int kVocabTile = 256;
+constexpr int kVocabEpilogueWarps = 8;
+constexpr int kVocabThreads = 32 * (4 + kVocabEpilogueWarps);
+constexpr int kVocabStages = 5;
+constexpr int kVocabStageBytes = 32768;  // 128 rows of A and 128 of B, 64 elements of K each
+constexpr int kVocabOutBytes = kVocabEpilogueWarps * 4096;
+constexpr int kVocabBarBytes = 256;
+constexpr int kVocabColBytes = 2 * 3 * 256 * 4;  // per accumulator: three values of each of the tile's 256 columns
+constexpr int kVocabSmemBytes = kVocabStages * kVocabStageBytes + kVocabOutBytes + kVocabBarBytes + kVocabColBytes;
+constexpr int kMaxPairs = 80;
+constexpr float kLog2e = 1.4426950408889634f;
+
+enum VocabKind { kLogits = 0, kGradZ = 1, kGradW = 2, kGradH = 3 };
+
+// One kind of tile of a launch.
+struct VocabProblem {
+  int32_t kind;
+  int32_t map_a, map_b;    // tensor maps of the operands
+  int32_t a_mn, b_mn;      // 1: the contraction runs down the columns
+  int32_t n_tiles;         // tile t of a split: row tile t / n_tiles, column tile t % n_tiles
+  int32_t m_tiles;         // not 0: column tile t / m_tiles, row tile t % m_tiles
+  int32_t split_tiles;     // tiles per split of the contraction
+  int32_t k_blocks;        // of one split
+  int32_t k_end;           // of all splits
+  int32_t a_row0, b_row0;  // where the operands' rows begin in their tensors (rows of the tile, or of K where MN-major)
+  int32_t start[kMaxPairs + 1];  // pair g has tiles start[g] .. start[g + 1] - 1
+};
+
+enum { kMapH = 0, kMapW, kMapGNew, kMapGOld, kMapOut, kMapGStore, kMapSlab, kMaps };
+
+struct VocabParams {
+  CUtensorMap map[kMaps];  // h, w, g of this piece, g of the one before; stores: grad_w, g, slabs of grad_h
+  VocabProblem prob[3];
+  int32_t count;
+  int32_t T, V, D;
+  int32_t v0, v_end;    // the piece whose logits are formed
+  int32_t out_v0;       // first word of the piece that grad_w gets
+  int32_t slab_rows;
+  int32_t add;          // grad_h is added to what the slabs hold
+  const float* bias;
+  const int32_t* targets;
+  const float* lse;
+  const float* grad_loss;
+  float2* part;         // forward: [2 * word tile + half][T], maximum and sum (both for powers of two)
+  float* z_target;      // forward: [T]
+  float* part_bias;     // backward: [2 * token tile + half][V], or NULL
+  void* ws;
+};
+
+// Operand of 128 rows (or columns) x 64 elements of K, 128-byte swizzle.  K-major: 1024 bytes between groups of eight rows.
+// MN-major: 64 consecutive elements of M or N are a row of 128 bytes, the next 64 are 8192 bytes on (leading offset), the next
+// eight of K 1024 bytes (stride offset).  Version 1, SWIZZLE_128B as in qb_gemm.
+__device__ __forceinline__ uint64_t vocab_desc(uint32_t smem_addr, int mn) {
+  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)(mn ? 8192 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)2 << 61;
+}
+// Instruction descriptor for kind::f16: D fp32 (bits 4-5 = 1), A and B bfloat16 (7-9, 10-12 = 1), MN-major A and B (15, 16),
+// N >> 3 (17-22), M >> 4 (24-28).
+__device__ __forceinline__ uint32_t vocab_idesc(int a_mn, int b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(kVocabTile >> 3) << 17) |
+         ((uint32_t)(kVocabTile >> 4) << 24);
+}
+
+__device__ __forceinline__ bool vocab_epilogue_sync_or(bool pred) {
+  uint32_t res;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(res)
+      : "r"((uint32_t)pred), "n"(32 * kVocabEpilogueWarps)
+      : "memory");
+  return res != 0;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// A pair's walk over its tiles, all kinds one after the other.
+struct VocabCursor {
+  int i, t, end;
+  __device__ __forceinline__ bool first(const VocabParams& gp, int g) {
+    i = -1;
+    t = end = 0;
+    return next(gp, g);
+  }
+  __device__ __forceinline__ bool next(const VocabParams& gp, int g) {
+    if (i >= 0) ++t;
+    while (t >= end) {
+      if (++i >= gp.count) return false;
+      t = gp.prob[i].start[g];
+      end = gp.prob[i].start[g + 1];
+    }
+    return true;
+  }
+};
+struct VocabTileAt {
+  int m, n, split, k0, k1;  // row and column tile, split, range of K blocks
+  __device__ __forceinline__ VocabTileAt(const VocabProblem& p, int t) {
+    split = t / p.split_tiles;
+    t -= split * p.split_tiles;
+    if (p.m_tiles) {
+      n = t / p.m_tiles;
+      m = t - n * p.m_tiles;
+    } else {
+      m = t / p.n_tiles;
+      n = t - m * p.n_tiles;
+    }
+    k0 = split * p.k_blocks;
+    k1 = min(k0 + p.k_blocks, p.k_end);
+  }
+};
+
+// FORWARD: logits tiles alone; else the three kinds of the backward pass.
+template <bool FORWARD>
+__global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_constant__ VocabParams gp) {
+  constexpr int kStages = kVocabStages;
+  const uint32_t rank = ptx::cluster_ctarank();
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t smem_base = ptx::smem_u32(smem);
+  uint8_t* const out_ptr = smem + kStages * kVocabStageBytes;
+  uint8_t* const bar_ptr = out_ptr + kVocabOutBytes;
+  const uint32_t bar_base = ptx::smem_u32(bar_ptr);
+  auto full = [&](int s) { return bar_base + 8u * s; };
+  auto empty = [&](int s) { return bar_base + 8u * (kStages + s); };
+  auto acc_full = [&](int a) { return bar_base + 8u * (2 * kStages + a); };
+  auto acc_empty = [&](int a) { return bar_base + 8u * (2 * kStages + 2 + a); };
+  const uint32_t drain_bar = bar_base + 8u * (2 * kStages + 4);
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 8 * (2 * kStages + 5));
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* const cols = reinterpret_cast<float*>(bar_ptr + kVocabBarBytes);  // [2][3][256]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if ((smem_base & 1023u) != 0u) {  // never expected; the swizzle needs it
+    pdl_begin();
+    if (threadIdx.x == 0) report_status(gp.ws, QB_ERR_CUDA, (int)smem_base);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      ptx::mbar_init(full(s), 1);
+      ptx::mbar_init(empty(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(acc_full(a), 1);
+      ptx::mbar_init(acc_empty(a), kVocabEpilogueWarps * 2);
+    }
+    ptx::mbar_init(drain_bar, 1);
+    *abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_cg<2>(ptx::smem_u32(tmem_slot), 2 * kVocabTile);
+    ptx::tmem_relinquish_cg<2>();
+  }
+  ptx::tcgen05_fence_before_sync();
+  __syncthreads();
+  ptx::cluster_sync_all();
+  ptx::tcgen05_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_begin();
+  auto lead = [&](uint32_t bar) { return ptx::map_to_cta(bar, 0); };
+  const int g = (int)blockIdx.x / 2;
+  bool timed_out = false;
+  int where = 0;
+
+  if (warp == 0) {
+    // ---------------- TMA producer ------------------------------------------------------------------
+    if (ptx::elect_one()) {
+      int stage = 0;
+      uint32_t phase = 0;
+      VocabCursor c;
+      for (bool have = c.first(gp, g); have && !timed_out; have = c.next(gp, g)) {
+        const VocabProblem& pr = gp.prob[c.i];
+        const VocabTileAt at(pr, c.t);
+        const int a_row = at.m * kVocabTile + (int)rank * 128, b_row = at.n * kVocabTile + (int)rank * 128;
+        const CUtensorMap* const ma = &gp.map[pr.map_a];
+        const CUtensorMap* const mb = &gp.map[pr.map_b];
+        for (int kb = at.k0; kb < at.k1; ++kb) {
+          if (!wait_barrier_relaxed(empty(stage), phase ^ 1u, abort_flag)) {
+            timed_out = true;
+            where = (0 << 16) | stage;
+            break;
+          }
+          const uint32_t a_smem = smem_base + stage * kVocabStageBytes, b_smem = a_smem + kVocabStageBytes / 2, bar = lead(full(stage));
+          if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), 2 * kVocabStageBytes);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {  // 64 rows, or 64 columns, each
+            if (pr.a_mn) ptx::tma_load_2d_pair(a_smem + 8192 * h, ma, bar, a_row + 64 * h, pr.a_row0 + kb * 64);
+            else ptx::tma_load_2d_pair(a_smem + 8192 * h, ma, bar, kb * 64, pr.a_row0 + a_row + 64 * h);
+            if (pr.b_mn) ptx::tma_load_2d_pair(b_smem + 8192 * h, mb, bar, b_row + 64 * h, pr.b_row0 + kb * 64);
+            else ptx::tma_load_2d_pair(b_smem + 8192 * h, mb, bar, kb * 64, pr.b_row0 + b_row + 64 * h);
+          }
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (timed_out) {  // let copies in flight land before the CTA's shared memory is released
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000ll) {
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer (in the pair's first CTA only) ---------------------------------------
+    if (rank == 0 && ptx::elect_one()) {
+      int stage = 0, it = 0;
+      uint32_t phase = 0;
+      VocabCursor c;
+      for (bool have = c.first(gp, g); have && !timed_out; have = c.next(gp, g), ++it) {
+        const VocabProblem& pr = gp.prob[c.i];
+        const VocabTileAt at(pr, c.t);
+        const int a = it & 1;
+        const uint32_t d = tmem_base + (uint32_t)(a * kVocabTile);
+        const uint32_t idesc = vocab_idesc(pr.a_mn, pr.b_mn);
+        const uint64_t a_desc0 = vocab_desc(smem_base, pr.a_mn), b_desc0 = vocab_desc(smem_base + kVocabStageBytes / 2, pr.b_mn);
+        // 16 elements of K per instruction: 32 bytes of a row, or 16 rows of 128 bytes
+        const uint32_t a_step = pr.a_mn ? 2048 >> 4 : 32 >> 4, b_step = pr.b_mn ? 2048 >> 4 : 32 >> 4;
+        if (!wait_barrier(acc_empty(a), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) {
+          timed_out = true;
+          where = (1 << 16) | 0x100 | a;
+          break;
+        }
+        for (int kb = at.k0; kb < at.k1; ++kb) {
+          if (!wait_barrier(full(stage), phase, abort_flag)) {
+            timed_out = true;
+            where = (1 << 16) | stage;
+            break;
+          }
+          ptx::tcgen05_fence_after_sync();
+          const uint64_t a_desc = a_desc0 + (uint64_t)(stage * (kVocabStageBytes >> 4));
+          const uint64_t b_desc = b_desc0 + (uint64_t)(stage * (kVocabStageBytes >> 4));
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            ptx::mma_f16_ss_cg<2>(d, a_desc + (uint64_t)(a_step * j), b_desc + (uint64_t)(b_step * j), idesc, kb != at.k0 || j != 0 ? 1u : 0u);
+          ptx::mma_commit_cg<2>(empty(stage));
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        if (!timed_out) ptx::mma_commit_cg<2>(acc_full(a));
+      }
+      if (timed_out) {  // wait (bounded) for what was issued before tensor memory is freed
+        ptx::mma_commit_cg<2>(drain_bar);
+        const long long t0 = clock64();
+        while (!ptx::mbar_try_wait(drain_bar, 0) && clock64() - t0 < 400000000ll) {
+        }
+      }
+    }
+  } else if (warp >= 4) {
+    // ---------------- epilogue ----------------------------------------------------------------------
+    const int ew = warp - 4, quarter = warp & 3, half = ew >> 2, e = threadIdx.x - 128;
+    uint8_t* const buf = out_ptr + ew * 4096;
+    const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    int it = 0;
+    VocabCursor c;
+    for (bool have = c.first(gp, g); have; have = c.next(gp, g), ++it) {
+      const VocabProblem& pr = gp.prob[c.i];
+      const VocabTileAt at(pr, c.t);
+      const int a = it & 1;
+      const int row0 = at.m * kVocabTile + (int)rank * 128 + quarter * 32, row = row0 + lane;
+      const int col0 = at.n * kVocabTile;
+      float* const tile_cols = cols + a * 768;
+      // what the tile's columns need: words' biases (forward), or the tokens' lse, gradient and target
+      if (FORWARD) {
+        const int v = col0 + e;
+        tile_cols[e] = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] * kLog2e : 0.0f);
+      } else if (pr.kind == kGradZ) {
+        const int t = col0 + e;
+        float lse = INFINITY, gl = 0.0f;
+        int target = -1;
+        if (t < gp.T) {
+          lse = gp.lse[t] * kLog2e;
+          target = gp.targets[t];
+          if (target >= 0 && target < gp.V) gl = gp.grad_loss[t];
+        }
+        tile_cols[e] = lse;
+        tile_cols[256 + e] = gl;
+        reinterpret_cast<int*>(tile_cols)[512 + e] = target;
+      }
+      // the row's own, fetched while the products run
+      int target = -1;
+      float bias = 0.0f;
+      if (FORWARD) {
+        if (row < gp.T) target = gp.targets[row];
+      } else if (pr.kind == kGradZ) {
+        const int v = gp.v0 + row;
+        bias = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] * kLog2e : 0.0f);
+      }
+      const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
+      if (vocab_epilogue_sync_or(!ok)) {  // publishes the columns' values, and all eight warps give up together
+        timed_out = true;
+        where = (3 << 16) | a;
+        break;
+      }
+      ptx::tcgen05_fence_after_sync();
+      const uint32_t acc = lanes + (uint32_t)(a * kVocabTile);
+      auto release = [&]() {  // the warp has read all it needs from the accumulator
+        ptx::tcgen05_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+          if (rank != 0) ptx::mbar_arrive_remote(lead(acc_empty(a)));
+          else ptx::mbar_arrive(acc_empty(a));
+        }
+      };
+      // the 128 bytes of the lane's row in the warp's staging buffer (piece j of 16 bytes), and their way out
+      auto begin_store = [&]() {
+        if (lane == 0) ptx::tma_store_wait_read0();
+        __syncwarp();
+      };
+      auto put = [&](int j, uint4 w) { *reinterpret_cast<uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = w; };
+
+      if constexpr (FORWARD) {
+        const int chunks = row0 < gp.T ? min(8, (gp.V - col0 + 31) / 32) : 0;
+        if (half >= chunks) release();
+        float top = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+        for (int ch = half; ch < chunks; ch += 2) {
+          uint32_t v[32];
+          ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(ch * 32), v);
+          ptx::tmem_ld_wait();
+          ptx::tmem_ld_regs_ready(v);
+          if (ch + 2 >= chunks) release();
+          const int hit = target - (col0 + ch * 32);
+          if (hit >= 0 && hit < 32 && target < gp.V) {
+            float z = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j == hit) z = __uint_as_float(v[j]);
+            if (row < gp.T) gp.z_target[row] = gp.bias ? z + gp.bias[target] : z;
+          }
+          float z[32], most = top;
+          const float4* const b4 = reinterpret_cast<const float4*>(tile_cols + ch * 32);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float4 b = b4[j];
+            z[4 * j] = fmaf(__uint_as_float(v[4 * j]), kLog2e, b.x);
+            z[4 * j + 1] = fmaf(__uint_as_float(v[4 * j + 1]), kLog2e, b.y);
+            z[4 * j + 2] = fmaf(__uint_as_float(v[4 * j + 2]), kLog2e, b.z);
+            z[4 * j + 3] = fmaf(__uint_as_float(v[4 * j + 3]), kLog2e, b.w);
+            most = fmaxf(most, fmaxf(fmaxf(z[4 * j], z[4 * j + 1]), fmaxf(z[4 * j + 2], z[4 * j + 3])));
+          }
+          const float base = most == -INFINITY ? 0.0f : most;  // nothing but -infinity so far: no difference of infinities
+          float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int j = 0; j < 32; ++j) s[j & 3] += exp2_fast(z[j] - base);
+          sum = sum * exp2_fast(top - base) + ((s[0] + s[1]) + (s[2] + s[3]));
+          top = most;
+        }
+        if (row < gp.T) gp.part[(size_t)(2 * at.n + half) * gp.T + row] = make_float2(top, sum);
+      } else if (pr.kind == kGradH) {
+        const int chunks = row0 < gp.T ? min(8, (gp.D - col0 + 31) / 32) : 0;
+        if (half >= chunks) release();
+#pragma unroll 1
+        for (int ch = half; ch < chunks; ch += 2) {
+          uint32_t v[32];
+          ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(ch * 32), v);
+          ptx::tmem_ld_wait();
+          ptx::tmem_ld_regs_ready(v);
+          if (ch + 2 >= chunks) release();
+          begin_store();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) put(j, make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            const int x = col0 + ch * 32, y = at.split * gp.slab_rows + row0;
+            if (gp.add) ptx::tma_add_2d(&gp.map[kMapSlab], ptx::smem_u32(buf), x, y);
+            else ptx::tma_store_2d(&gp.map[kMapSlab], ptx::smem_u32(buf), x, y);
+            ptx::tma_store_commit();
+          }
+        }
+      } else {
+        const bool grad_z = pr.kind == kGradZ;
+        const int rows = grad_z ? gp.v_end - gp.v0 : gp.V - gp.out_v0, width = grad_z ? gp.T : gp.D;
+        // g is formed for all rows of the piece's tiles: the products read whole K blocks of it
+        const int chunks = grad_z || row0 < rows ? min(4, (width - col0 + 63) / 64) : 0;
+        if (half >= chunks) release();
+        float bias_grad = 0.0f;
+#pragma unroll 1
+        for (int ch = half; ch < chunks; ch += 2) {
+          uint32_t v[2][32];
+          ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(ch * 64), v[0]);
+          ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(ch * 64 + 32), v[1]);
+          ptx::tmem_ld_wait();
+          ptx::tmem_ld_regs_ready(v[0]);
+          ptx::tmem_ld_regs_ready(v[1]);
+          if (ch + 2 >= chunks) release();
+          if (grad_z) {
+            const float4* const lse4 = reinterpret_cast<const float4*>(tile_cols + ch * 64);
+            const float4* const gl4 = reinterpret_cast<const float4*>(tile_cols + 256 + ch * 64);
+            const int4* const tg4 = reinterpret_cast<const int4*>(tile_cols + 512 + ch * 64);
+            const int word = gp.v0 + row;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float4 l = lse4[j], gl = gl4[j];
+              const int4 tg = tg4[j];
+              uint32_t* const x = &v[j >> 3][(j & 7) * 4];
+              auto one = [&](uint32_t z, float lse, float w, int target) {
+                const float p = exp2_fast(fmaf(__uint_as_float(z), kLog2e, bias - lse));
+                const float d = w * p - (target == word ? w : 0.0f);
+                bias_grad += d;
+                return __float_as_uint(d);
+              };
+              x[0] = one(x[0], l.x, gl.x, tg.x);
+              x[1] = one(x[1], l.y, gl.y, tg.y);
+              x[2] = one(x[2], l.z, gl.z, tg.z);
+              x[3] = one(x[3], l.w, gl.w, tg.w);
+            }
+          }
+          begin_store();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t* const x = &v[j >> 2][(j & 3) * 8];
+            const auto f = [&](int i) { return __uint_as_float(x[i]); };
+            put(j, make_uint4(pack_bf16(f(0), f(1)), pack_bf16(f(2), f(3)), pack_bf16(f(4), f(5)), pack_bf16(f(6), f(7))));
+          }
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            ptx::tma_store_2d(&gp.map[grad_z ? kMapGStore : kMapOut], ptx::smem_u32(buf), col0 + ch * 64, (grad_z ? 0 : gp.out_v0) + row0);
+            ptx::tma_store_commit();
+          }
+        }
+        if (grad_z && gp.part_bias && gp.v0 + row < gp.V) gp.part_bias[(size_t)(2 * at.n + half) * gp.V + gp.v0 + row] = bias_grad;
+      }
+    }
+    if (lane == 0) ptx::tma_store_wait_read0();
+  }
+  if (timed_out) {
+    *abort_flag = 1;
+    report_status(gp.ws, QB_ERR_TIMEOUT, where);
+  }
+  ptx::tcgen05_fence_before_sync();
+  __syncthreads();
+  ptx::cluster_sync_all();  // the other CTA's MMAs and arrivals reach into this CTA
+  if (warp == 1) {
+    __syncwarp();
+    ptx::tcgen05_fence_after_sync();
+    ptx::tmem_dealloc_cg<2>(tmem_base, 2 * kVocabTile);
+  }
+}
+
+// Joins the tiles' maxima and sums of 32 tokens per block: warp w takes every eighth, then the warps are joined in order.
+__global__ void __launch_bounds__(256) vocab_join_kernel(const float2* part, int parts, const float* z_target, const int32_t* targets, int T,
+                                                         int V, float* loss, float* lse, void* ws) {
+  __shared__ float2 joined[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = blockIdx.x * 32 + lane;
+  pdl_begin();
+  auto join = [](float2 a, float2 b) {
+    const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.0f : top;
+    return make_float2(top, a.y * exp2_fast(a.x - base) + b.y * exp2_fast(b.x - base));
+  };
+  float2 mine = make_float2(-INFINITY, 0.0f);
+  if (t < T) {
+#pragma unroll 4
+    for (int i = warp; i < parts; i += 8) mine = join(mine, part[(size_t)i * T + t]);
+  }
+  joined[warp][lane] = mine;
+  __syncthreads();
+  if (warp != 0 || t >= T) return;
+  for (int w = 1; w < 8; ++w) mine = join(mine, joined[w][lane]);
+  const float l = (mine.x + log2f(mine.y)) * 0.6931471805599453f;
+  const int target = targets[t];
+  lse[t] = l;
+  const bool valid = target >= 0 && target < V;
+  if (target >= V) report_status(ws, QB_ERR_INVALID, t);
+  loss[t] = valid ? l - z_target[t] : 0.0f;
+}
+
+// grad_h = the slabs' sum in bfloat16; grad_bias = the tiles' sum.
+__global__ void __launch_bounds__(256) vocab_finish_kernel(const float* slabs, int splits, int64_t slab, int64_t n, uint16_t* grad_h,
+                                                           const float* part_bias, int parts, int V, float* grad_bias) {
+  pdl_begin();
+  const int64_t stride = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (grad_h)
+    for (int64_t i = first * 8; i < n; i += stride * 8) {  // n is a multiple of 8
+      float4 a = *reinterpret_cast<const float4*>(slabs + i), b = *reinterpret_cast<const float4*>(slabs + i + 4);
+      for (int s = 1; s < splits; ++s) {
+        const float4 c = *reinterpret_cast<const float4*>(slabs + s * slab + i), d = *reinterpret_cast<const float4*>(slabs + s * slab + i + 4);
+        a.x += c.x, a.y += c.y, a.z += c.z, a.w += c.w;
+        b.x += d.x, b.y += d.y, b.z += d.z, b.w += d.w;
+      }
+      *reinterpret_cast<uint4*>(grad_h + i) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+    }
+  if (grad_bias)
+    for (int64_t v = first; v < V; v += stride) {
+      float s = 0.0f;
+      for (int i = 0; i < parts; ++i) s += part_bias[(size_t)i * V + v];
+      grad_bias[v] = s;
+    }
+}
+
+// ---- host side -----------------------------------------------------------------------------------
+static int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m; }
+
+// How the backward pass cuts its work.
+struct VocabPlan {
+  int64_t rows;      // words per piece, a multiple of 256
+  int64_t pieces;
+  int64_t k_split;   // K blocks of a split of grad_h
+  int64_t splits;
+  int64_t g_bytes, slab_rows, slab_bytes, bias_bytes;
+  size_t bytes() const { return (size_t)(1024 + (pieces > 1 ? 2 : 1) * g_bytes + splits * slab_bytes + bias_bytes); }
+};
+constexpr int64_t kPieceBytes = 32 << 20;  // of g: with the piece before it and what the products read it stays in L2
+
+static VocabPlan plan_vocab(int64_t T, int64_t V, int64_t D, int pairs, size_t budget) {
+  VocabPlan p;
+  const int64_t Tp = up(T, 64) * 64, t_tiles = up(T, 256), d_tiles = up(D, 256), all = up(V, 256) * 256;
+  p.slab_rows = t_tiles * 256;
+  p.slab_bytes = up(p.slab_rows * D * 4, 1024) * 1024;
+  p.bias_bytes = up(2 * t_tiles * V * 4, 1024) * 1024;
+  int64_t rows = std::min(all, std::max<int64_t>(256, kPieceBytes / (2 * Tp) / 256 * 256));
+  for (;; rows -= 256) {
+    p.pieces = up(all, rows);
+    p.rows = up(up(V, p.pieces), 256) * 256;
+    p.pieces = up(V, p.rows);
+    p.g_bytes = up(p.rows * Tp * 2, 1024) * 1024;
+    // grad_h's contraction over the piece is split where a tile of it would outlast the launch
+    // (blocks of the first piece, whose splits are what is stored and summed; no piece has more)
+    const int64_t blocks = up(std::min(p.rows, V), 64), v_tiles = p.rows / 256;
+    const int64_t work = t_tiles * d_tiles * blocks + v_tiles * d_tiles * (Tp / 64) + (p.pieces > 1 ? v_tiles * t_tiles * up(D, 64) : 0);
+    p.k_split = std::min(blocks, std::max<int64_t>(16, work / pairs / 2));
+    p.splits = up(blocks, p.k_split);
+    p.k_split = up(blocks, p.splits);
+    p.splits = up(blocks, p.k_split);
+    if (p.bytes() <= budget || rows <= 256) return p;
+  }
+}
+
+// Deals `tiles` tiles of `cost` over the pairs: each to the least loaded one, as level as they come; contiguous tiles per pair.
+static void deal_tiles(VocabProblem& p, int64_t tiles, int64_t cost, int64_t* load, int pairs) {
+  int64_t lo = 0, hi = 0;  // the least level at which they all fit
+  for (int g = 0; g < pairs; ++g) hi = std::max(hi, load[g]);
+  hi += cost * (up(tiles, pairs) + 1);
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    int64_t room = 0;
+    for (int g = 0; g < pairs; ++g) room += mid > load[g] ? (mid - load[g]) / cost : 0;
+    if (room >= tiles) hi = mid;
+    else lo = mid + 1;
+  }
+  int64_t t = 0;
+  for (int g = 0; g < pairs; ++g) {
+    const int64_t n = std::min(tiles - t, lo > load[g] ? (lo - load[g]) / cost : 0);
+    p.start[g] = (int32_t)t;
+    t += n;
+    load[g] += n * cost;
+  }
+  p.start[pairs] = (int32_t)t;
+}
+
+template <bool FORWARD>
+static qb_status launch_vocab(const VocabParams& gp, int pairs, cudaStream_t stream) {
+  auto kernel = vocab_kernel<FORWARD>;
+  static std::atomic<bool> attr_set[64] = {};
+  int dev = 0;
+  QB_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+    QB_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kVocabSmemBytes));
+    if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
+  }
+  QB_CUDA_TRY(launch_kernel(kernel, (unsigned)(2 * pairs), kVocabThreads, kVocabSmemBytes, stream, 2, false, gp));
+  return QB_OK;
+}
+
+static qb_status operand_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols) {
+  return make_matrix_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+static qb_status store_map(CUtensorMap* tm, void* base, int64_t rows, int64_t cols, bool fp32) {
+  return make_matrix_map(tm, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * (fp32 ? 4 : 2),
+                         32, fp32 ? 32 : 64, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
+}
+
+static qb_status validate_vocab(const char* who, bool null, const void* h, const void* w, int64_t T, int64_t V, int64_t D) {
+  if (null || T <= 0 || V <= 0 || D <= 0 || T > QB_MAX_MN || V > QB_MAX_MN || D > QB_MAX_VOCAB_D || up(T, 256) * up(V, 256) > 1 << 30) {
+    set_last_error("%s: null pointer or size out of range (T=%lld V=%lld D=%lld)", who, (long long)T, (long long)V, (long long)D);
+    return QB_ERR_INVALID;
+  }
+  if (D % 8 != 0 || !aligned16(h) || !aligned16(w)) {
+    set_last_error("%s: D must be a multiple of 8, matrices 16-byte aligned", who);
+    return QB_ERR_ALIGN;
+  }
+  return QB_OK;
+}
+static bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+static size_t vocab_forward_bytes(int64_t T, int64_t V) { return (size_t)(1024 + up(T * 4, 1024) * 1024 + 2 * up(V, 256) * T * 8); }
+
+}  // namespace qb
+
+extern "C" size_t qb_vocab_loss_workspace_bytes(int64_t T, int64_t V, int64_t D) {
+  using namespace qb;
+  if (T <= 0 || V <= 0 || D <= 0 || T > QB_MAX_MN || V > QB_MAX_MN || D > QB_MAX_VOCAB_D) return 0;
+  int sms = 148;
+  require_sm100(&sms);  // without a device: for a 148-SM part
+  const size_t back = plan_vocab(T, V, D, std::min(sms / 2, kMaxPairs), ~(size_t)0).bytes();
+  return up(std::max(back, vocab_forward_bytes(T, V)), 256) * 256;
+}
+
+extern "C" qb_status qb_vocab_loss(const uint16_t* h, const uint16_t* w, const float* bias, const int32_t* targets, int64_t T, int64_t V,
+                                   int64_t D, float* loss, float* lse, void* ws, size_t ws_bytes, void* cuda_stream) {
+  using namespace qb;
+  qb_status st = validate_vocab("qb_vocab_loss", !h || !w || !targets || !loss || !lse, h, w, T, V, D);
+  if (st != QB_OK) return st;
+  if (!aligned4(bias) || !aligned4(targets) || !aligned4(loss) || !aligned4(lse)) {
+    set_last_error("qb_vocab_loss: bias, targets, loss and lse must be 4-byte aligned");
+    return QB_ERR_ALIGN;
+  }
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0 || ws_bytes < vocab_forward_bytes(T, V)) {
+    set_last_error("qb_vocab_loss: workspace null, not 256-byte aligned or smaller than %zu bytes", vocab_forward_bytes(T, V));
+    return QB_ERR_WORKSPACE;
+  }
+  int sms = 0;
+  st = require_sm100(&sms);
+  if (st != QB_OK) return st;
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  VocabParams gp = {};
+  if ((st = operand_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
+  if ((st = operand_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
+  char* const scratch = static_cast<char*>(ws) + 1024;
+  gp.z_target = reinterpret_cast<float*>(scratch);
+  gp.part = reinterpret_cast<float2*>(scratch + up(T * 4, 1024) * 1024);
+  gp.T = (int32_t)T;
+  gp.V = (int32_t)V;
+  gp.D = (int32_t)D;
+  gp.bias = bias;
+  gp.targets = targets;
+  gp.ws = ws;
+  gp.count = 1;
+  VocabProblem& p = gp.prob[0];
+  p.kind = kLogits;
+  p.map_a = kMapH;
+  p.map_b = kMapW;
+  p.m_tiles = (int32_t)up(T, 256);  // all tokens of a tile of words one after the other: w is read once, h stays in L2
+  const int64_t tiles = up(V, 256) * p.m_tiles;
+  p.split_tiles = (int32_t)tiles;
+  p.k_blocks = p.k_end = (int32_t)up(D, 64);
+  const int pairs = (int)std::min<int64_t>(tiles, std::min(sms / 2, kMaxPairs));
+  int64_t load[kMaxPairs] = {};
+  deal_tiles(p, tiles, 1, load, pairs);
+  if ((st = launch_vocab<true>(gp, pairs, stream)) != QB_OK) return st;
+  QB_CUDA_TRY(launch_kernel(vocab_join_kernel, (unsigned)up(T, 32), 256, 0, stream, 1, false, gp.part, (int)(2 * up(V, 256)), gp.z_target, targets,
+                            (int)T, (int)V, loss, lse, ws));
+  return QB_OK;
+}
+
+extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w, const float* bias, const int32_t* targets,
+                                            const float* lse, const float* grad_loss, int64_t T, int64_t V, int64_t D, uint16_t* grad_h,
+                                            uint16_t* grad_w, float* grad_bias, void* ws, size_t ws_bytes, void* cuda_stream) {
+  using namespace qb;
+  qb_status st = validate_vocab("qb_vocab_loss_backward", !h || !w || !targets || !lse || !grad_loss || (!grad_h && !grad_w && !grad_bias), h, w,
+                                T, V, D);
+  if (st != QB_OK) return st;
+  if (!aligned4(bias) || !aligned4(targets) || !aligned4(lse) || !aligned4(grad_loss) || !aligned4(grad_bias) || !aligned16(grad_h) ||
+      !aligned16(grad_w)) {
+    set_last_error("qb_vocab_loss_backward: vectors must be 4-byte, matrices 16-byte aligned");
+    return QB_ERR_ALIGN;
+  }
+  int sms = 148;
+  const qb_status device = require_sm100(&sms);
+  const int pairs = std::min(sms / 2, kMaxPairs);
+  const VocabPlan plan = plan_vocab(T, V, D, pairs, ws_bytes);
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0 || ws_bytes < plan.bytes()) {
+    set_last_error("qb_vocab_loss_backward: workspace null, not 256-byte aligned or smaller than %zu bytes", plan.bytes());
+    return QB_ERR_WORKSPACE;
+  }
+  if (device != QB_OK) return device;
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  char* const g0 = static_cast<char*>(ws) + 1024;
+  char* const g1 = plan.pieces > 1 ? g0 + plan.g_bytes : g0;
+  float* const slabs = reinterpret_cast<float*>(g1 + plan.g_bytes);
+  float* const part_bias = reinterpret_cast<float*>(reinterpret_cast<char*>(slabs) + plan.splits * plan.slab_bytes);
+  const int64_t Tp = up(T, 64) * 64, slab = plan.slab_bytes / 4;
+  VocabParams gp = {};
+  CUtensorMap g_load[2], g_store[2];
+  if ((st = operand_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
+  if ((st = operand_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
+  for (int i = 0; i < 2; ++i) {
+    if ((st = operand_map(&g_load[i], i ? g1 : g0, plan.rows, Tp)) != QB_OK) return st;
+    if ((st = store_map(&g_store[i], i ? g1 : g0, plan.rows, Tp, false)) != QB_OK) return st;
+  }
+  if (grad_w && (st = store_map(&gp.map[kMapOut], grad_w, V, D, false)) != QB_OK) return st;
+  // slabs of slab_rows rows, one below the other
+  if ((st = store_map(&gp.map[kMapSlab], slabs, plan.splits * plan.slab_rows, D, true)) != QB_OK) return st;
+  gp.T = (int32_t)T;
+  gp.V = (int32_t)V;
+  gp.D = (int32_t)D;
+  gp.bias = bias;
+  gp.targets = targets;
+  gp.lse = lse;
+  gp.grad_loss = grad_loss;
+  gp.part_bias = grad_bias ? part_bias : nullptr;
+  gp.slab_rows = (int32_t)plan.slab_rows;
+  gp.ws = ws;
+  const int32_t t_tiles = (int32_t)up(T, 256), d_tiles = (int32_t)up(D, 256);
+  for (int64_t i = 0; i <= plan.pieces; ++i) {
+    int64_t load[kMaxPairs] = {};
+    gp.count = 0;
+    const auto add = [&](const VocabProblem& p, int64_t tiles, int64_t cost) {
+      gp.prob[gp.count] = p;
+      deal_tiles(gp.prob[gp.count++], tiles, cost, load, pairs);
+    };
+    if (i > 0) {  // the products of the piece whose g the launch before formed
+      const int64_t v0 = (i - 1) * plan.rows, rows = std::min(plan.rows, V - v0);
+      gp.map[kMapGOld] = g_load[(i - 1) & 1];
+      gp.out_v0 = (int32_t)v0;
+      gp.add = i > 1;
+      VocabProblem p = {};
+      if (grad_h) {
+        p.kind = kGradH;
+        p.map_a = kMapGOld;
+        p.map_b = kMapW;
+        p.a_mn = p.b_mn = 1;
+        p.n_tiles = d_tiles;
+        p.split_tiles = t_tiles * d_tiles;
+        p.k_blocks = (int32_t)plan.k_split;
+        // every split of the first piece stores its slab; what a shorter last piece lacks adds nothing
+        p.k_end = (int32_t)up(rows, 64);
+        p.b_row0 = (int32_t)v0;
+        add(p, (int64_t)up(p.k_end, p.k_blocks) * p.split_tiles, p.k_blocks + 2);
+      }
+      if (grad_w) {
+        p = VocabProblem{};
+        p.kind = kGradW;
+        p.map_a = kMapGOld;
+        p.map_b = kMapH;
+        p.b_mn = 1;
+        p.n_tiles = d_tiles;
+        p.split_tiles = (int32_t)up(rows, 256) * d_tiles;
+        p.k_blocks = p.k_end = (int32_t)(Tp / 64);
+        add(p, p.split_tiles, p.k_blocks + 2);
+      }
+    }
+    if (i < plan.pieces) {
+      const int64_t v0 = i * plan.rows, rows = std::min(plan.rows, V - v0);
+      gp.map[kMapGNew] = g_load[i & 1];
+      gp.map[kMapGStore] = g_store[i & 1];
+      gp.v0 = (int32_t)v0;
+      gp.v_end = (int32_t)(v0 + rows);
+      VocabProblem p = {};
+      p.kind = kGradZ;
+      p.map_a = kMapW;
+      p.map_b = kMapH;
+      p.a_row0 = (int32_t)v0;
+      p.n_tiles = t_tiles;
+      p.split_tiles = (int32_t)up(rows, 256) * t_tiles;
+      p.k_blocks = p.k_end = (int32_t)up(D, 64);
+      add(p, p.split_tiles, p.k_blocks + 2);
+    }
+    if (gp.count == 0) continue;
+    if ((st = launch_vocab<false>(gp, pairs, stream)) != QB_OK) return st;
+  }
+  if (grad_h || grad_bias) {
+    const int64_t n = T * D, items = std::max(grad_h ? n / 8 : 0, grad_bias ? V : 0);
+    QB_CUDA_TRY(launch_kernel(vocab_finish_kernel, (unsigned)std::min<int64_t>(up(items, 256), (int64_t)sms * 8), 256, 0, stream, 1, false, slabs,
+                              (int)plan.splits, slab, n, grad_h, part_bias, 2 * t_tiles, (int)V, grad_bias));
+  }
+  return QB_OK;
+}

@@ -60,3 +60,33 @@ def test_no_cpu_fallback(lib):
     assert lib.qb_dropout(A, 0, 64, 0.1, A, 0, None, A, None) == qb.QB_ERR_CUDA
     assert lib.qb_quantize_fp8(A, 0, 8, 128, 0, A, A, None, None, A, 256, None) == qb.QB_ERR_CUDA
     assert lib.qb_gemm_fp8(A, A, 0, A, A, 0, None, 8, 8, 128, 0, A, A, 256, None) == qb.QB_ERR_CUDA
+
+
+def test_vocab_loss(lib):
+    need = qb.vocab_loss_workspace_bytes(100, 1000, 64)
+    assert need > 0 and need % 256 == 0
+    assert qb.vocab_loss_workspace_bytes(0, 10, 8) == 0 and qb.vocab_loss_workspace_bytes(1, 10, 8193) == 0
+    W = 0x10000
+    ok = dict(h=A, w=A, bias=None, targets=A, T=100, V=1000, D=64, loss=A, lse=A, ws=W, ws_bytes=need)
+
+    def call(**kw):
+        return lib.qb_vocab_loss(*{**ok, **kw}.values(), None)
+    for bad in (dict(h=None), dict(w=None), dict(targets=None), dict(loss=None), dict(lse=None), dict(T=0), dict(V=0), dict(D=0), dict(T=(1 << 24) + 1),
+                dict(V=(1 << 24) + 1), dict(D=8200), dict(T=1 << 24, V=1 << 24)):
+        assert call(**bad) == qb.QB_ERR_INVALID, bad
+    for bad in (dict(D=60), dict(h=A + 8), dict(w=A + 8), dict(bias=A + 2), dict(targets=A + 1), dict(loss=A + 2), dict(lse=A + 2)):
+        assert call(**bad) == qb.QB_ERR_ALIGN, bad
+    for bad in (dict(ws=None), dict(ws=W + 16), dict(ws_bytes=4096)):
+        assert call(**bad) == qb.QB_ERR_WORKSPACE, bad
+    ok = dict(h=A, w=A, bias=A, targets=A, lse=A, gl=A, T=100, V=1000, D=64, gh=A, gw=A, gb=A, ws=W, ws_bytes=need)
+
+    def back(**kw):
+        return lib.qb_vocab_loss_backward(*{**ok, **kw}.values(), None)
+    for bad in (dict(h=None), dict(w=None), dict(targets=None), dict(lse=None), dict(gl=None), dict(gh=None, gw=None, gb=None), dict(T=0), dict(V=-1),
+                dict(D=8200)):
+        assert back(**bad) == qb.QB_ERR_INVALID, bad
+    for bad in (dict(D=60), dict(h=A + 8), dict(w=A + 8), dict(gh=A + 8), dict(gw=A + 8), dict(gb=A + 2), dict(lse=A + 2), dict(gl=A + 2), dict(bias=A + 1),
+                dict(targets=A + 2)):
+        assert back(**bad) == qb.QB_ERR_ALIGN, bad
+    for bad in (dict(ws=None), dict(ws=W + 16), dict(ws_bytes=4096)):
+        assert back(**bad) == qb.QB_ERR_WORKSPACE, bad
