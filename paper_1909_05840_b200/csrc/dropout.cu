@@ -83,13 +83,24 @@ struct Vec {
 };
 
 constexpr int kDropThreads = 256;
-constexpr int kDropUnroll = 2;  // vectors of 16 bytes that a thread has in flight
+constexpr int kDropUnroll = 4;  // vectors of 16 bytes that a thread has in flight
 
-// DROP: p > 0 (with p = 0 nothing is drawn).  RES: a residual is added.
+// A block takes kDropThreads * kDropUnroll vectors and ends.  DROP: p > 0 (with p = 0 nothing is drawn).  RES: a residual is
+// added.
 template <class T, bool VECTOR, bool DROP, bool RES>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const T* residual, T* y, int64_t n, DropArgs a) {
-  constexpr int V = 16 / sizeof(T);
+  constexpr int V = 16 / sizeof(T), U = kDropUnroll;
   pdl_begin();
+  const int64_t base = ((int64_t)blockIdx.x * (kDropThreads * U) + threadIdx.x) * V;
+  Vec<T, V, VECTOR> v[U], r[RES ? U : 1];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = base + (int64_t)u * (kDropThreads * V);
+    if (at < n) {
+      v[u].load(x + at, n - at);
+      if constexpr (RES) r[u].load(residual + at, n - at);
+    }
+  }
   uint32_t k0 = 0, k1 = 0, c2 = 0, c3 = 0;
   if constexpr (DROP) {
     const uint64_t seed = a.rng[0], sub = a.rng[1] + a.call;
@@ -98,55 +109,43 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const
     c2 = (uint32_t)sub;
     c3 = (uint32_t)(sub >> 32);
   }
-  const int64_t step = (int64_t)gridDim.x * (kDropThreads * kDropUnroll * V);
-  for (int64_t base = ((int64_t)blockIdx.x * (kDropThreads * kDropUnroll) + threadIdx.x) * V; base < n; base += step) {
-    Vec<T, V, VECTOR> v[kDropUnroll], r[kDropUnroll];
 #pragma unroll
-    for (int u = 0; u < kDropUnroll; ++u) {
-      const int64_t at = base + (int64_t)u * (kDropThreads * V);
-      if (at < n) {
-        v[u].load(x + at, n - at);
-        if constexpr (RES) r[u].load(residual + at, n - at);
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = base + (int64_t)u * (kDropThreads * V);
+    if (at >= n) return;
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+      uint32_t w[4] = {0, 0, 0, 0};
+      if constexpr (DROP) {
+        const uint64_t c = (uint64_t)at / 4 + q;
+        const uint4 d = philox4x32_7((uint32_t)c, (uint32_t)(c >> 32), c2, c3, k0, k1);
+        w[0] = d.x;
+        w[1] = d.y;
+        w[2] = d.z;
+        w[3] = d.w;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float f = to_float(v[u].e[4 * q + j]);
+        // a select, not a product with 0: what is dropped may be infinite or NaN
+        if constexpr (DROP) f = w[j] >= a.threshold ? __fmul_rn(f, a.scale) : 0.0f;
+        if constexpr (RES) f = __fadd_rn(f, to_float(r[u].e[4 * q + j]));
+        v[u].e[4 * q + j] = from_float<T>(f);
       }
     }
-#pragma unroll
-    for (int u = 0; u < kDropUnroll; ++u) {
-      const int64_t at = base + (int64_t)u * (kDropThreads * V);
-      if (at >= n) break;
-#pragma unroll
-      for (int q = 0; q < V / 4; ++q) {
-        uint32_t w[4] = {0, 0, 0, 0};
-        if constexpr (DROP) {
-          const uint64_t c = (uint64_t)at / 4 + q;
-          const uint4 d = philox4x32_7((uint32_t)c, (uint32_t)(c >> 32), c2, c3, k0, k1);
-          w[0] = d.x;
-          w[1] = d.y;
-          w[2] = d.z;
-          w[3] = d.w;
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float f = to_float(v[u].e[4 * q + j]);
-          // a select, not a product with 0: what is dropped may be infinite or NaN
-          if constexpr (DROP) f = w[j] >= a.threshold ? __fmul_rn(f, a.scale) : 0.0f;
-          if constexpr (RES) f = __fadd_rn(f, to_float(r[u].e[4 * q + j]));
-          v[u].e[4 * q + j] = from_float<T>(f);
-        }
-      }
-      v[u].store(y + at, n - at);
-    }
+    v[u].store(y + at, n - at);
   }
 }
 
 template <class T>
 static qb_status launch_dropout(const void* x, const void* residual, void* y, int64_t n, bool vector, bool drop, const DropArgs& a,
-                                int sms, cudaStream_t stream) {
+                                cudaStream_t stream) {
   auto kernel = vector ? (drop ? (residual ? dropout_kernel<T, true, true, true> : dropout_kernel<T, true, true, false>)
                                : (residual ? dropout_kernel<T, true, false, true> : dropout_kernel<T, true, false, false>))
                        : (drop ? (residual ? dropout_kernel<T, false, true, true> : dropout_kernel<T, false, true, false>)
                                : (residual ? dropout_kernel<T, false, false, true> : dropout_kernel<T, false, false, false>));
   constexpr int64_t per_block = (int64_t)kDropThreads * kDropUnroll * (16 / sizeof(T));
-  const unsigned grid = (unsigned)std::min<int64_t>((n + per_block - 1) / per_block, (int64_t)sms * 8);
+  const unsigned grid = (unsigned)((n + per_block - 1) / per_block);  // n <= 2^40: at most 2^28 blocks
   QB_CUDA_TRY(launch_kernel(kernel, grid, kDropThreads, 0, stream, 1, false, static_cast<const T*>(x), static_cast<const T*>(residual),
                             static_cast<T*>(y), n, a));
   return QB_OK;
@@ -165,8 +164,7 @@ extern "C" qb_status qb_dropout(const void* x, int type, int64_t n, double p, co
     qb::set_last_error("qb_dropout: x, residual and y must be aligned to their elements, rng to 8 bytes");
     return QB_ERR_ALIGN;
   }
-  int sms = 0;
-  qb_status st = qb::require_sm100(&sms);
+  qb_status st = qb::require_sm100(nullptr);
   if (st != QB_OK) return st;
   qb::DropArgs a;
   a.rng = rng;
@@ -176,8 +174,8 @@ extern "C" qb_status qb_dropout(const void* x, int type, int64_t n, double p, co
   const bool vector = all % 16 == 0;  // else the elements one by one: same values
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   switch (type) {
-    case QB_F32: return qb::launch_dropout<float>(x, residual, y, n, vector, a.threshold != 0, a, sms, stream);
-    case QB_BF16: return qb::launch_dropout<__nv_bfloat16>(x, residual, y, n, vector, a.threshold != 0, a, sms, stream);
-    default: return qb::launch_dropout<__half>(x, residual, y, n, vector, a.threshold != 0, a, sms, stream);
+    case QB_F32: return qb::launch_dropout<float>(x, residual, y, n, vector, a.threshold != 0, a, stream);
+    case QB_BF16: return qb::launch_dropout<__nv_bfloat16>(x, residual, y, n, vector, a.threshold != 0, a, stream);
+    default: return qb::launch_dropout<__half>(x, residual, y, n, vector, a.threshold != 0, a, stream);
   }
 }

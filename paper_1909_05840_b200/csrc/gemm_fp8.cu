@@ -11,7 +11,7 @@
 //   warp 0        TMA producer (one lane): codes of A and B (128-byte swizzle, K block of 128), every fourth block the scales
 //   warp 1        issues tcgen05.cp (scales) and tcgen05.mma, owns the tensor memory (one lane)
 //   warps 2..3    idle
-//   warps 4..11   epilogue, two per TMEM lane quarter: tcgen05.ld -> bias -> round -> shared memory -> TMA store
+//   warps 4..11   epilogue, two per TMEM lane quarter: tcgen05.ld -> bias -> round -> shared memory -> whole lines of y
 // A tile is 128 rows of A per CTA x BT rows of B; TMEM lane = row of A, column = row of B.  Large products run as CTA pairs
 // (cta_group::2, 256 x 256): each CTA stages its own 128 rows of A and half of B's rows.  No load is multicast.
 // Two accumulators, so that the epilogue of a tile overlaps the products of the next.  At BT = 256 they and the scales
@@ -34,7 +34,6 @@ namespace qb {
 struct Fp8Params {
   CUtensorMap tma, tmb;    // codes, box 128 bytes of K x the CTA's rows
   CUtensorMap tmsa, tmsb;  // scales as rows of 512 bytes
-  CUtensorMap tmy;         // y, box 32 rows x 128 bytes
   const float* bias;
   void* y;
   void* ws;
@@ -42,7 +41,7 @@ struct Fp8Params {
   int32_t n_tiles, tiles;
   int32_t words;        // rows of 512 bytes of scales per 128 rows of codes
   int32_t a_last, b_last;  // last block of 128 rows of A's and of B's scales
-  int32_t tma_store;    // 1: rows of y are 16-byte aligned
+  int32_t vector;       // 1: rows of y are 16-byte aligned
   uint32_t idesc;       // the formats' part of the instruction descriptor
 };
 
@@ -298,8 +297,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
         if (Cfg::kOverlap && i == 0 && (!down || chunks == BT / kCols)) arrive(overlap_read);
         if (i + 2 >= chunks) arrive(acc_empty(a));
         const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + a * 256 + c0);
-        if (lane == 0) ptx::tma_store_wait_read0();  // the warp's last store has read the buffer
-        __syncwarp();
+        __syncwarp();  // the chunk before has left the buffer
 #pragma unroll
         for (int j = 0; j < 8; ++j) {  // 16 bytes of the row at a time; the swizzle keeps the lanes on different banks
           uint4 w;
@@ -324,16 +322,19 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
           }
           *reinterpret_cast<uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = w;
         }
-        if (gp.tma_store) {
-          ptx::fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            ptx::tma_store_2d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0);
-            ptx::tma_store_commit();
+        __syncwarp();
+        const int rows = min(32, gp.M - m0);
+        if (gp.vector) {  // 16 bytes a lane, four whole lines a store
+          constexpr int kPiece = BF16 ? 8 : 4;  // columns in 16 bytes
+          const int piece = lane & 7, col = n0 + c0 + piece * kPiece;
+          uint8_t* const to = static_cast<uint8_t*>(gp.y) + ((size_t)m0 * gp.N + col) * (16 / kPiece);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3);
+            const uint4 w = *reinterpret_cast<const uint4*>(buf + r * 128 + ((piece ^ (r & 7)) << 4));
+            if (r < rows && col < gp.N) *reinterpret_cast<uint4*>(to + (size_t)r * gp.N * (16 / kPiece)) = w;
           }
         } else {  // rows of y of any alignment: a row at a time, the lanes on consecutive columns
-          __syncwarp();
-          const int rows = min(32, gp.M - m0);
           for (int r = 0; r < rows; ++r) {
 #pragma unroll
             for (int p = 0; p < kCols / 32; ++p) {
@@ -346,11 +347,9 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
                 static_cast<float*>(gp.y)[at] = *reinterpret_cast<const float*>(buf + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4);
             }
           }
-          __syncwarp();
         }
       }
     }
-    if (lane == 0) ptx::tma_store_wait_read0();
   }
   if (timed_out) {
     *abort_flag = 1;
@@ -421,14 +420,7 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
   if ((st = make_matrix_map(&gp.tmsa, u32, a_scale, up(M, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
   if ((st = make_matrix_map(&gp.tmsb, u32, b_scale, up(N, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
   const int size = out_type == QB_F32 ? 4 : 2;
-  gp.tma_store = N * size % 16 == 0 && aligned16(y);
-  if (gp.tma_store) {
-    st = make_matrix_map(&gp.tmy, size == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, y, M, N, N * size, 32,
-                         128 / size, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
-    if (st != QB_OK) return st;
-  } else {
-    gp.tmy = gp.tma;  // not used
-  }
+  gp.vector = N * size % 16 == 0 && aligned16(y);
   gp.bias = bias;
   gp.y = y;
   gp.ws = ws;

@@ -130,13 +130,6 @@ __device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src_smem
                "r"(src_smem), "r"(x), "r"(y)
                : "memory");
 }
-// The same, adding the fp32 values of the box to those in memory.
-__device__ __forceinline__ void tma_add_2d(const void* tmap, uint32_t src_smem, int32_t x, int32_t y) {
-  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
-                   reinterpret_cast<uint64_t>(tmap)),
-               "r"(src_smem), "r"(x), "r"(y)
-               : "memory");
-}
 __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Wait until at most N bulk-store groups of this thread are still READING shared memory.
 __device__ __forceinline__ void tma_store_wait_read0() {
@@ -144,6 +137,13 @@ __device__ __forceinline__ void tma_store_wait_read0() {
 }
 __device__ __forceinline__ void tma_store_wait_read1() {
   asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+}
+
+// Four fp32 values added to those in memory (16-byte aligned), nothing read back.
+__device__ __forceinline__ void red_add_v4(void* p, uint4 v) {
+  asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)),
+               "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w))
+               : "memory");
 }
 
 // ---- register reallocation between warpgroups ------------------------------------------------------
@@ -233,6 +233,15 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst_smem, const void* 
   asm volatile(
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
       ::"r"(dst_smem), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar_cluster), "r"(x), "r"(y)
+      : "memory");
+}
+
+// The same for a tensor of three dimensions (x innermost).
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* tmap, uint32_t bar_cluster, int32_t x, int32_t y,
+                                                 int32_t z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst_smem), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
 

@@ -48,4 +48,24 @@ inline qb_status make_matrix_map(CUtensorMap* tm, CUtensorMapDataType type, cons
   return QB_OK;
 }
 
+// The same matrix as column groups of 128 bytes: coordinates (byte in the group, row, group), boxes of box_rows rows x box_groups
+// groups, 128-byte swizzle.  row_bytes is a multiple of 128 here (a group's part behind a row's end would be the next row's).
+inline qb_status make_group_map(CUtensorMap* tm, CUtensorMapDataType type, int esize, const void* base, int64_t rows, int64_t row_bytes,
+                                int box_rows, int box_groups) {
+  EncodeTiledFn encode = nullptr;
+  qb_status st = get_encode_fn(&encode);
+  if (st != QB_OK) return st;
+  const cuuint64_t dims[3] = {(cuuint64_t)(128 / esize), (cuuint64_t)rows, (cuuint64_t)(row_bytes / 128)};
+  const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, 128};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / esize), (cuuint32_t)box_rows, (cuuint32_t)box_groups};
+  const cuuint32_t elem[3] = {1, 1, 1};
+  const CUresult r = encode(tm, type, 3, const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_last_error("cuTensorMapEncodeTiled failed with CUresult %d (%lld rows of %lld bytes)", (int)r, (long long)rows, (long long)row_bytes);
+    return QB_ERR_CUDA;
+  }
+  return QB_OK;
+}
+
 }  // namespace qb

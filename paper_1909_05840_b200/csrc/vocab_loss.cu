@@ -13,8 +13,8 @@
 //
 // One product kernel for all of it: CTA pairs (tcgen05 cta_group::2, kind::f16, bfloat16 operands, fp32 accumulators), tiles of
 // 256 x 256, K blocks of 64, a ring of five stages of 32 KB per CTA, two accumulators in tensor memory.  An operand lies in
-// shared memory as the tensor has it: contraction along its rows (K-major) or down its columns (MN-major), two boxes of
-// 64 x 64 per CTA either way, so that nothing is transposed in memory.  12 warps: 0 loads (TMA), 1 issues MMAs,
+// shared memory as the tensor has it: contraction along its rows (K-major) or down its columns (MN-major),
+// so that nothing is transposed in memory.  12 warps: 0 loads (TMA), 1 issues MMAs,
 // 4..11 epilogue, two per TMEM lane quarter.  Every wait is bounded, as in qb_gemm.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -42,13 +42,17 @@ constexpr int kVocabSmemBytes = kVocabStages * kVocabStageBytes + kVocabOutBytes
 constexpr int kMaxPairs = 80;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// How an operand lies and is loaded: K-major, one box of 128 rows x 64; MN-major, one box of 64 rows x 2 groups of 64 columns, or
+// (rows that are no multiple of 128 bytes) two boxes of 64 rows x 64 columns.  A box costs the TMA unit about 100 ns here whether it
+// holds 8 KB or 16: with two boxes per operand everywhere, 4,096 x 30,522 x 768 forward took 165 us instead of 121.
+enum VocabForm { kRows = 0, kCols = 1, kCols2 = 2 };
 enum VocabKind { kLogits = 0, kGradZ = 1, kGradW = 2, kGradH = 3 };
 
 // One kind of tile of a launch.
 struct VocabProblem {
   int32_t kind;
   int32_t map_a, map_b;    // tensor maps of the operands
-  int32_t a_mn, b_mn;      // 1: the contraction runs down the columns
+  int32_t a_form, b_form;  // kRows, kCols or kCols2
   int32_t n_tiles;         // tile t of a split: row tile t / n_tiles, column tile t % n_tiles
   int32_t m_tiles;         // not 0: column tile t / m_tiles, row tile t % m_tiles
   int32_t split_tiles;     // tiles per split of the contraction
@@ -58,17 +62,21 @@ struct VocabProblem {
   int32_t start[kMaxPairs + 1];  // pair g has tiles start[g] .. start[g + 1] - 1
 };
 
-enum { kMapH = 0, kMapW, kMapGNew, kMapGOld, kMapOut, kMapGStore, kMapSlab, kMaps };
+enum { kMapH = 0, kMapW, kMapHCols, kMapWCols, kMapG, kMapGCols, kMaps };
 
 struct VocabParams {
-  CUtensorMap map[kMaps];  // h, w, g of this piece, g of the one before; stores: grad_w, g, slabs of grad_h
+  CUtensorMap map[kMaps];  // h, w, and g of the piece before, as rows and as columns
   VocabProblem prob[3];
   int32_t count;
   int32_t T, V, D;
-  int32_t v0, v_end;    // the piece whose logits are formed
+  int32_t v0;           // first word of the piece whose logits are formed
   int32_t out_v0;       // first word of the piece that grad_w gets
   int32_t slab_rows;
   int32_t add;          // grad_h is added to what the slabs hold
+  int32_t g_pitch;      // tokens rounded up to 64
+  uint16_t* g_new;      // [words of a piece][g_pitch]
+  uint16_t* grad_w;     // [V][D]
+  float* slabs;         // [splits][slab_rows][D]
   const float* bias;
   const int32_t* targets;
   const float* lse;
@@ -220,13 +228,18 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           }
           const uint32_t a_smem = smem_base + stage * kVocabStageBytes, b_smem = a_smem + kVocabStageBytes / 2, bar = lead(full(stage));
           if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), 2 * kVocabStageBytes);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {  // 64 rows, or 64 columns, each
-            if (pr.a_mn) ptx::tma_load_2d_pair(a_smem + 8192 * h, ma, bar, a_row + 64 * h, pr.a_row0 + kb * 64);
-            else ptx::tma_load_2d_pair(a_smem + 8192 * h, ma, bar, kb * 64, pr.a_row0 + a_row + 64 * h);
-            if (pr.b_mn) ptx::tma_load_2d_pair(b_smem + 8192 * h, mb, bar, b_row + 64 * h, pr.b_row0 + kb * 64);
-            else ptx::tma_load_2d_pair(b_smem + 8192 * h, mb, bar, kb * 64, pr.b_row0 + b_row + 64 * h);
-          }
+          auto load = [&](uint32_t dst, const CUtensorMap* tm, int form, int mn, int row0) {
+            if (form == kRows) {
+              ptx::tma_load_2d_pair(dst, tm, bar, kb * 64, row0 + mn);
+            } else if (form == kCols) {
+              ptx::tma_load_3d_pair(dst, tm, bar, 0, row0 + kb * 64, mn / 64);
+            } else {
+              ptx::tma_load_2d_pair(dst, tm, bar, mn, row0 + kb * 64);
+              ptx::tma_load_2d_pair(dst + 8192, tm, bar, mn + 64, row0 + kb * 64);
+            }
+          };
+          load(a_smem, ma, pr.a_form, a_row, pr.a_row0);
+          load(b_smem, mb, pr.b_form, b_row, pr.b_row0);
           if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
@@ -250,10 +263,10 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         const VocabTileAt at(pr, c.t);
         const int a = it & 1;
         const uint32_t d = tmem_base + (uint32_t)(a * kVocabTile);
-        const uint32_t idesc = vocab_idesc(pr.a_mn, pr.b_mn);
-        const uint64_t a_desc0 = vocab_desc(smem_base, pr.a_mn), b_desc0 = vocab_desc(smem_base + kVocabStageBytes / 2, pr.b_mn);
+        const uint32_t idesc = vocab_idesc(pr.a_form != kRows, pr.b_form != kRows);
+        const uint64_t a_desc0 = vocab_desc(smem_base, pr.a_form != kRows), b_desc0 = vocab_desc(smem_base + kVocabStageBytes / 2, pr.b_form != kRows);
         // 16 elements of K per instruction: 32 bytes of a row, or 16 rows of 128 bytes
-        const uint32_t a_step = pr.a_mn ? 2048 >> 4 : 32 >> 4, b_step = pr.b_mn ? 2048 >> 4 : 32 >> 4;
+        const uint32_t a_step = pr.a_form != kRows ? 2048 >> 4 : 32 >> 4, b_step = pr.b_form != kRows ? 2048 >> 4 : 32 >> 4;
         if (!wait_barrier(acc_empty(a), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) {
           timed_out = true;
           where = (1 << 16) | 0x100 | a;
@@ -342,12 +355,23 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           else ptx::mbar_arrive(acc_empty(a));
         }
       };
-      // the 128 bytes of the lane's row in the warp's staging buffer (piece j of 16 bytes), and their way out
-      auto begin_store = [&]() {
-        if (lane == 0) ptx::tma_store_wait_read0();
+      // the 128 bytes of the lane's row in the warp's staging buffer (piece j of 16 bytes), and their way out: 16 bytes a lane,
+      // four whole lines a store
+      auto put = [&](int j, uint4 w) { *reinterpret_cast<uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = w; };
+      auto send = [&](uint8_t* to, size_t pitch, int rows, int bytes, bool add) {  // rows and bytes of a row that exist
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = 4 * i + (lane >> 3), piece = lane & 7;
+          const uint4 w = *reinterpret_cast<const uint4*>(buf + r * 128 + ((piece ^ (r & 7)) << 4));
+          if (r < rows && piece * 16 < bytes) {
+            uint8_t* const p = to + (size_t)r * pitch + piece * 16;
+            if (add) ptx::red_add_v4(p, w);
+            else *reinterpret_cast<uint4*>(p) = w;
+          }
+        }
         __syncwarp();
       };
-      auto put = [&](int j, uint4 w) { *reinterpret_cast<uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = w; };
 
       if constexpr (FORWARD) {
         const int chunks = row0 < gp.T ? min(8, (gp.V - col0 + 31) / 32) : 0;
@@ -397,21 +421,15 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           ptx::tmem_ld_wait();
           ptx::tmem_ld_regs_ready(v);
           if (ch + 2 >= chunks) release();
-          begin_store();
 #pragma unroll
           for (int j = 0; j < 8; ++j) put(j, make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-          ptx::fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            const int x = col0 + ch * 32, y = at.split * gp.slab_rows + row0;
-            if (gp.add) ptx::tma_add_2d(&gp.map[kMapSlab], ptx::smem_u32(buf), x, y);
-            else ptx::tma_store_2d(&gp.map[kMapSlab], ptx::smem_u32(buf), x, y);
-            ptx::tma_store_commit();
-          }
+          const int c0 = col0 + ch * 32;
+          send(reinterpret_cast<uint8_t*>(gp.slabs + ((size_t)at.split * gp.slab_rows + row0) * gp.D + c0), (size_t)gp.D * 4, gp.T - row0,
+               (gp.D - c0) * 4, gp.add != 0);
         }
       } else {
         const bool grad_z = pr.kind == kGradZ;
-        const int rows = grad_z ? gp.v_end - gp.v0 : gp.V - gp.out_v0, width = grad_z ? gp.T : gp.D;
+        const int rows = gp.V - gp.out_v0, width = grad_z ? gp.T : gp.D;
         // g is formed for all rows of the piece's tiles: the products read whole K blocks of it
         const int chunks = grad_z || row0 < rows ? min(4, (width - col0 + 63) / 64) : 0;
         if (half >= chunks) release();
@@ -447,24 +465,21 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
               x[3] = one(x[3], l.w, gl.w, tg.w);
             }
           }
-          begin_store();
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const uint32_t* const x = &v[j >> 2][(j & 3) * 8];
             const auto f = [&](int i) { return __uint_as_float(x[i]); };
             put(j, make_uint4(pack_bf16(f(0), f(1)), pack_bf16(f(2), f(3)), pack_bf16(f(4), f(5)), pack_bf16(f(6), f(7))));
           }
-          ptx::fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            ptx::tma_store_2d(&gp.map[grad_z ? kMapGStore : kMapOut], ptx::smem_u32(buf), col0 + ch * 64, (grad_z ? 0 : gp.out_v0) + row0);
-            ptx::tma_store_commit();
-          }
+          const int c0 = col0 + ch * 64;
+          if (grad_z)  // whole K blocks: the rows and columns behind the last word and token too
+            send(reinterpret_cast<uint8_t*>(gp.g_new + (size_t)row0 * gp.g_pitch + c0), (size_t)gp.g_pitch * 2, 32, 128, false);
+          else
+            send(reinterpret_cast<uint8_t*>(gp.grad_w + (size_t)(gp.out_v0 + row0) * gp.D + c0), (size_t)gp.D * 2, rows - row0, (gp.D - c0) * 2, false);
         }
         if (grad_z && gp.part_bias && gp.v0 + row < gp.V) gp.part_bias[(size_t)(2 * at.n + half) * gp.V + gp.v0 + row] = bias_grad;
       }
     }
-    if (lane == 0) ptx::tma_store_wait_read0();
   }
   if (timed_out) {
     *abort_flag = 1;
@@ -480,27 +495,44 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
   }
 }
 
-// Joins the tiles' maxima and sums of 32 tokens per block: warp w takes every eighth, then the warps are joined in order.
-__global__ void __launch_bounds__(256) vocab_join_kernel(const float2* part, int parts, const float* z_target, const int32_t* targets, int T,
-                                                         int V, float* loss, float* lse, void* ws) {
-  __shared__ float2 joined[8][32];
+// Joins the tiles' maxima and sums of 32 tokens per block: every warp a share of the tiles, the maximum first (the loads of
+// kJoinDepth tiles in flight), then the warps in order.
+constexpr int kJoinWarps = 16, kJoinDepth = 8;
+__global__ void __launch_bounds__(32 * kJoinWarps) vocab_join_kernel(const float2* part, int parts, const float* z_target, const int32_t* targets,
+                                                                     int T, int V, float* loss, float* lse, void* ws) {
+  __shared__ float2 joined[kJoinWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = blockIdx.x * 32 + lane;
   pdl_begin();
-  auto join = [](float2 a, float2 b) {
-    const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.0f : top;
-    return make_float2(top, a.y * exp2_fast(a.x - base) + b.y * exp2_fast(b.x - base));
-  };
-  float2 mine = make_float2(-INFINITY, 0.0f);
-  if (t < T) {
-#pragma unroll 4
-    for (int i = warp; i < parts; i += 8) mine = join(mine, part[(size_t)i * T + t]);
+  float top = -INFINITY, sum = 0.0f;
+  for (int i0 = warp; i0 < parts; i0 += kJoinWarps * kJoinDepth) {
+    float2 p[kJoinDepth];
+#pragma unroll
+    for (int d = 0; d < kJoinDepth; ++d) {
+      const int i = i0 + d * kJoinWarps;
+      p[d] = make_float2(-INFINITY, 0.0f);
+      if (i < parts && t < T) p[d] = part[(size_t)i * T + t];
+    }
+    float most = top;
+#pragma unroll
+    for (int d = 0; d < kJoinDepth; ++d) most = fmaxf(most, p[d].x);
+    const float base = most == -INFINITY ? 0.0f : most;
+    sum *= exp2_fast(top - base);
+#pragma unroll
+    for (int d = 0; d < kJoinDepth; ++d) sum += p[d].y * exp2_fast(p[d].x - base);
+    top = most;
   }
-  joined[warp][lane] = mine;
+  joined[warp][lane] = make_float2(top, sum);
   __syncthreads();
   if (warp != 0 || t >= T) return;
-  for (int w = 1; w < 8; ++w) mine = join(mine, joined[w][lane]);
-  const float l = (mine.x + log2f(mine.y)) * 0.6931471805599453f;
+  float most = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) most = fmaxf(most, joined[w][lane].x);
+  const float base = most == -INFINITY ? 0.0f : most;
+  sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) sum += joined[w][lane].y * exp2_fast(joined[w][lane].x - base);
+  const float l = (most + log2f(sum)) * 0.6931471805599453f;
   const int target = targets[t];
   lse[t] = l;
   const bool valid = target >= 0 && target < V;
@@ -516,6 +548,7 @@ __global__ void __launch_bounds__(256) vocab_finish_kernel(const float* slabs, i
   if (grad_h)
     for (int64_t i = first * 8; i < n; i += stride * 8) {  // n is a multiple of 8
       float4 a = *reinterpret_cast<const float4*>(slabs + i), b = *reinterpret_cast<const float4*>(slabs + i + 4);
+#pragma unroll 4
       for (int s = 1; s < splits; ++s) {
         const float4 c = *reinterpret_cast<const float4*>(slabs + s * slab + i), d = *reinterpret_cast<const float4*>(slabs + s * slab + i + 4);
         a.x += c.x, a.y += c.y, a.z += c.z, a.w += c.w;
@@ -526,6 +559,7 @@ __global__ void __launch_bounds__(256) vocab_finish_kernel(const float* slabs, i
   if (grad_bias)
     for (int64_t v = first; v < V; v += stride) {
       float s = 0.0f;
+#pragma unroll 8
       for (int i = 0; i < parts; ++i) s += part_bias[(size_t)i * V + v];
       grad_bias[v] = s;
     }
@@ -605,12 +639,13 @@ static qb_status launch_vocab(const VocabParams& gp, int pairs, cudaStream_t str
   return QB_OK;
 }
 
-static qb_status operand_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols) {
-  return make_matrix_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+// The operand with its rows along M or N, and with its columns along them.
+static qb_status rows_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols) {
+  return make_matrix_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * 2, 128, 64, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-static qb_status store_map(CUtensorMap* tm, void* base, int64_t rows, int64_t cols, bool fp32) {
-  return make_matrix_map(tm, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * (fp32 ? 4 : 2),
-                         32, fp32 ? 32 : 64, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
+static qb_status cols_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols) {
+  if (cols % 64 == 0) return make_group_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols * 2, 64, 2);
+  return make_matrix_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 static qb_status validate_vocab(const char* who, bool null, const void* h, const void* w, int64_t T, int64_t V, int64_t D) {
@@ -657,8 +692,8 @@ extern "C" qb_status qb_vocab_loss(const uint16_t* h, const uint16_t* w, const f
   if (st != QB_OK) return st;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   VocabParams gp = {};
-  if ((st = operand_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
-  if ((st = operand_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
+  if ((st = rows_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
+  if ((st = rows_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
   char* const scratch = static_cast<char*>(ws) + 1024;
   gp.z_target = reinterpret_cast<float*>(scratch);
   gp.part = reinterpret_cast<float2*>(scratch + up(T * 4, 1024) * 1024);
@@ -681,7 +716,7 @@ extern "C" qb_status qb_vocab_loss(const uint16_t* h, const uint16_t* w, const f
   int64_t load[kMaxPairs] = {};
   deal_tiles(p, tiles, 1, load, pairs);
   if ((st = launch_vocab<true>(gp, pairs, stream)) != QB_OK) return st;
-  QB_CUDA_TRY(launch_kernel(vocab_join_kernel, (unsigned)up(T, 32), 256, 0, stream, 1, false, gp.part, (int)(2 * up(V, 256)), gp.z_target, targets,
+  QB_CUDA_TRY(launch_kernel(vocab_join_kernel, (unsigned)up(T, 32), 32 * kJoinWarps, 0, stream, 1, false, gp.part, (int)(2 * up(V, 256)), gp.z_target, targets,
                             (int)T, (int)V, loss, lse, ws));
   return QB_OK;
 }
@@ -714,16 +749,20 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
   float* const part_bias = reinterpret_cast<float*>(reinterpret_cast<char*>(slabs) + plan.splits * plan.slab_bytes);
   const int64_t Tp = up(T, 64) * 64, slab = plan.slab_bytes / 4;
   VocabParams gp = {};
-  CUtensorMap g_load[2], g_store[2];
-  if ((st = operand_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
-  if ((st = operand_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
+  CUtensorMap g_rows[2], g_cols[2];
+  uint16_t* const g[2] = {reinterpret_cast<uint16_t*>(g0), reinterpret_cast<uint16_t*>(g1)};
+  if ((st = rows_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
+  if ((st = rows_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
+  if ((st = cols_map(&gp.map[kMapHCols], h, T, D)) != QB_OK) return st;
+  if ((st = cols_map(&gp.map[kMapWCols], w, V, D)) != QB_OK) return st;
   for (int i = 0; i < 2; ++i) {
-    if ((st = operand_map(&g_load[i], i ? g1 : g0, plan.rows, Tp)) != QB_OK) return st;
-    if ((st = store_map(&g_store[i], i ? g1 : g0, plan.rows, Tp, false)) != QB_OK) return st;
+    if ((st = rows_map(&g_rows[i], g[i], plan.rows, Tp)) != QB_OK) return st;
+    if ((st = cols_map(&g_cols[i], g[i], plan.rows, Tp)) != QB_OK) return st;
   }
-  if (grad_w && (st = store_map(&gp.map[kMapOut], grad_w, V, D, false)) != QB_OK) return st;
-  // slabs of slab_rows rows, one below the other
-  if ((st = store_map(&gp.map[kMapSlab], slabs, plan.splits * plan.slab_rows, D, true)) != QB_OK) return st;
+  const int cols_form = D % 64 == 0 ? kCols : kCols2;
+  gp.g_pitch = (int32_t)Tp;
+  gp.grad_w = grad_w;
+  gp.slabs = slabs;
   gp.T = (int32_t)T;
   gp.V = (int32_t)V;
   gp.D = (int32_t)D;
@@ -744,15 +783,17 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
     };
     if (i > 0) {  // the products of the piece whose g the launch before formed
       const int64_t v0 = (i - 1) * plan.rows, rows = std::min(plan.rows, V - v0);
-      gp.map[kMapGOld] = g_load[(i - 1) & 1];
+      gp.map[kMapG] = g_rows[(i - 1) & 1];
+      gp.map[kMapGCols] = g_cols[(i - 1) & 1];
       gp.out_v0 = (int32_t)v0;
       gp.add = i > 1;
       VocabProblem p = {};
       if (grad_h) {
         p.kind = kGradH;
-        p.map_a = kMapGOld;
-        p.map_b = kMapW;
-        p.a_mn = p.b_mn = 1;
+        p.map_a = kMapGCols;
+        p.map_b = kMapWCols;
+        p.a_form = kCols;
+        p.b_form = cols_form;
         p.n_tiles = d_tiles;
         p.split_tiles = t_tiles * d_tiles;
         p.k_blocks = (int32_t)plan.k_split;
@@ -764,9 +805,9 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
       if (grad_w) {
         p = VocabProblem{};
         p.kind = kGradW;
-        p.map_a = kMapGOld;
-        p.map_b = kMapH;
-        p.b_mn = 1;
+        p.map_a = kMapG;
+        p.map_b = kMapHCols;
+        p.b_form = cols_form;
         p.n_tiles = d_tiles;
         p.split_tiles = (int32_t)up(rows, 256) * d_tiles;
         p.k_blocks = p.k_end = (int32_t)(Tp / 64);
@@ -775,10 +816,8 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
     }
     if (i < plan.pieces) {
       const int64_t v0 = i * plan.rows, rows = std::min(plan.rows, V - v0);
-      gp.map[kMapGNew] = g_load[i & 1];
-      gp.map[kMapGStore] = g_store[i & 1];
+      gp.g_new = g[i & 1];
       gp.v0 = (int32_t)v0;
-      gp.v_end = (int32_t)(v0 + rows);
       VocabProblem p = {};
       p.kind = kGradZ;
       p.map_a = kMapW;
