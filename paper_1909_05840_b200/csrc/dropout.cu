@@ -23,31 +23,74 @@ struct DropArgs {
   float scale;         // 1 / (1 - p)
 };
 
-__device__ __forceinline__ uint4 philox4x32_7(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
+// Seven rounds for counters that differ in their low word alone: what the other words and the keys give in the first rounds is
+// formed once per thread (25 instead of 28 products and xors per four elements, and no key arithmetic).
+struct Philox7 {
+  uint32_t x1, y2, z2, w3, k0[5], k1[4];
+  __device__ __forceinline__ void start(uint64_t seed, uint64_t sub, uint32_t c1) {
+    uint32_t a = (uint32_t)seed, b = (uint32_t)(seed >> 32);
+    const uint64_t p1 = (uint64_t)(uint32_t)sub * 0xCD9E8D57u;  // round 1: the third word
+    x1 = (uint32_t)(sub >> 32) ^ b;
+    const uint64_t p2 = (uint64_t)((uint32_t)(p1 >> 32) ^ c1 ^ a) * 0xD2511F53u;  // round 2: what the first word has become
+    a += 0x9E3779B9u;
+    b += 0xBB67AE85u;
+    y2 = (uint32_t)p1 ^ a;
+    z2 = (uint32_t)(p2 >> 32) ^ b;
+    a += 0x9E3779B9u;
+    b += 0xBB67AE85u;
+    w3 = (uint32_t)p2 ^ b;
 #pragma unroll
-  for (int r = 0; r < 7; ++r) {
-    const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
-    c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
-    c3 = (uint32_t)a;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
+    for (int r = 0; r < 5; ++r) {
+      k0[r] = a;
+      if (r > 0) k1[r - 1] = b;
+      a += 0x9E3779B9u;
+      b += 0xBB67AE85u;
+    }
   }
-  return make_uint4(c0, c1, c2, c3);
-}
+  __device__ __forceinline__ uint4 words(uint32_t c0) const {
+    const uint64_t a1 = (uint64_t)c0 * 0xD2511F53u;
+    const uint64_t b2 = (uint64_t)((uint32_t)(a1 >> 32) ^ x1) * 0xCD9E8D57u;
+    uint32_t w0 = (uint32_t)(b2 >> 32) ^ y2, w1 = (uint32_t)b2, w2 = (uint32_t)a1 ^ z2, w3_;
+    {
+      const uint64_t a = (uint64_t)w0 * 0xD2511F53u, b = (uint64_t)w2 * 0xCD9E8D57u;
+      w0 = (uint32_t)(b >> 32) ^ w1 ^ k0[0];
+      w1 = (uint32_t)b;
+      w2 = (uint32_t)(a >> 32) ^ w3;
+      w3_ = (uint32_t)a;
+    }
+#pragma unroll
+    for (int r = 1; r < 5; ++r) {
+      const uint64_t a = (uint64_t)w0 * 0xD2511F53u, b = (uint64_t)w2 * 0xCD9E8D57u;
+      w0 = (uint32_t)(b >> 32) ^ w1 ^ k0[r];
+      w1 = (uint32_t)b;
+      w2 = (uint32_t)(a >> 32) ^ w3_ ^ k1[r - 1];
+      w3_ = (uint32_t)a;
+    }
+    return make_uint4(w0, w1, w2, w3_);
+  }
+};
 
+// Two neighbouring elements at a time: one conversion instruction rounds and packs both.
 template <class T>
-__device__ __forceinline__ float to_float(T v) {
-  if constexpr (std::is_same_v<T, float>) return v;
-  else if constexpr (std::is_same_v<T, __half>) return __half2float(v);
-  else return __bfloat162float(v);
+__device__ __forceinline__ float2 pair_to_float(const T* e) {
+  if constexpr (std::is_same_v<T, float>) return make_float2(e[0], e[1]);
+  else if constexpr (std::is_same_v<T, __half>) return __half22float2(__halves2half2(e[0], e[1]));
+  else return __bfloat1622float2(__halves2bfloat162(e[0], e[1]));
 }
 template <class T>
-__device__ __forceinline__ T from_float(float v) {
-  if constexpr (std::is_same_v<T, float>) return v;
-  else if constexpr (std::is_same_v<T, __half>) return __float2half_rn(v);
-  else return __float2bfloat16_rn(v);
+__device__ __forceinline__ void pair_from_float(T* e, float2 f) {
+  if constexpr (std::is_same_v<T, float>) {
+    e[0] = f.x;
+    e[1] = f.y;
+  } else if constexpr (std::is_same_v<T, __half>) {
+    const __half2 h = __floats2half2_rn(f.x, f.y);
+    e[0] = __low2half(h);
+    e[1] = __high2half(h);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+    e[0] = __low2bfloat16(h);
+    e[1] = __high2bfloat16(h);
+  }
 }
 
 // One vector of V elements at 16 bytes (VECTOR) or one element after the other.
@@ -83,12 +126,12 @@ struct Vec {
 };
 
 constexpr int kDropThreads = 256;
-constexpr int kDropUnroll = 4;  // vectors of 16 bytes that a thread has in flight
+constexpr int kDropUnroll = 2;  // vectors of 16 bytes that a thread has in flight
 
 // A block takes kDropThreads * kDropUnroll vectors and ends.  DROP: p > 0 (with p = 0 nothing is drawn).  RES: a residual is
 // added.
 template <class T, bool VECTOR, bool DROP, bool RES>
-__global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const T* residual, T* y, int64_t n, DropArgs a) {
+__global__ void __launch_bounds__(kDropThreads, 8) dropout_kernel(const T* x, const T* residual, T* y, int64_t n, DropArgs a) {
   constexpr int V = 16 / sizeof(T), U = kDropUnroll;
   pdl_begin();
   const int64_t base = ((int64_t)blockIdx.x * (kDropThreads * U) + threadIdx.x) * V;
@@ -101,14 +144,11 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const
       if constexpr (RES) r[u].load(residual + at, n - at);
     }
   }
-  uint32_t k0 = 0, k1 = 0, c2 = 0, c3 = 0;
-  if constexpr (DROP) {
-    const uint64_t seed = a.rng[0], sub = a.rng[1] + a.call;
-    k0 = (uint32_t)seed;
-    k1 = (uint32_t)(seed >> 32);
-    c2 = (uint32_t)sub;
-    c3 = (uint32_t)(sub >> 32);
-  }
+  // a block's counters have one high word: its share of them is a power of two, and aligned to it
+  constexpr int kCounters = kDropThreads * U * V / 4;
+  static_assert((kCounters & (kCounters - 1)) == 0, "counters of a block");
+  Philox7 philox;
+  if constexpr (DROP) philox.start(a.rng[0], a.rng[1] + a.call, (uint32_t)((uint64_t)blockIdx.x * kCounters >> 32));
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t at = base + (int64_t)u * (kDropThreads * V);
@@ -117,20 +157,26 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, const
     for (int q = 0; q < V / 4; ++q) {
       uint32_t w[4] = {0, 0, 0, 0};
       if constexpr (DROP) {
-        const uint64_t c = (uint64_t)at / 4 + q;
-        const uint4 d = philox4x32_7((uint32_t)c, (uint32_t)(c >> 32), c2, c3, k0, k1);
+        const uint4 d = philox.words((uint32_t)(at / 4) + q);
         w[0] = d.x;
         w[1] = d.y;
         w[2] = d.z;
         w[3] = d.w;
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float f = to_float(v[u].e[4 * q + j]);
+      for (int j = 0; j < 4; j += 2) {
+        float2 f = pair_to_float(&v[u].e[4 * q + j]);
         // a select, not a product with 0: what is dropped may be infinite or NaN
-        if constexpr (DROP) f = w[j] >= a.threshold ? __fmul_rn(f, a.scale) : 0.0f;
-        if constexpr (RES) f = __fadd_rn(f, to_float(r[u].e[4 * q + j]));
-        v[u].e[4 * q + j] = from_float<T>(f);
+        if constexpr (DROP) {
+          f.x = w[j] >= a.threshold ? __fmul_rn(f.x, a.scale) : 0.0f;
+          f.y = w[j + 1] >= a.threshold ? __fmul_rn(f.y, a.scale) : 0.0f;
+        }
+        if constexpr (RES) {
+          const float2 g = pair_to_float(&r[u].e[4 * q + j]);
+          f.x = __fadd_rn(f.x, g.x);
+          f.y = __fadd_rn(f.y, g.y);
+        }
+        pair_from_float(&v[u].e[4 * q + j], f);
       }
     }
     v[u].store(y + at, n - at);

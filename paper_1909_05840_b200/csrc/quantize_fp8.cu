@@ -18,20 +18,55 @@
 
 namespace qb {
 
-template <class T>
-__device__ __forceinline__ float widen(T v) {
-  if constexpr (std::is_same_v<T, float>) return v;
-  else if constexpr (std::is_same_v<T, __half>) return __half2float(v);
-  else return __bfloat162float(v);
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+// The byte e + 127 for a block whose largest magnitude has these bits (of fp32).  With max = 1.m * 2^E: e = E - 8 (e5m2: E - 15), one
+// more where 1.m > 1.75.  Where the result is below 2^-127 (max|x| < 2^-119) it is held there.  0 and what is not finite: 1.
+template <int FMT>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
+  if (bits == 0u || bits >= 0x7F800000u) return 127u;
+  const int e = (int)(bits >> 23) - (FMT == QB_E4M3 ? 8 : 15) + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return (uint32_t)max(e, 0);
+}
+
+// Four codes, the first in the low byte.  cvt would turn infinities into the largest finite value.
+template <int FMT>
+__device__ __forceinline__ uint32_t codes_of(float x, float y, float z, float w) {
+  uint16_t lo, hi;
+  if constexpr (FMT == QB_E4M3) {
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y), "f"(x));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(w), "f"(z));
+  } else {
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y), "f"(x));
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(w), "f"(z));
+  }
+  return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+__device__ __forceinline__ float finite_or_nan(float f) {
+  return (__float_as_uint(f) & 0x7FFFFFFFu) >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : f;
 }
 
 // Four consecutive values of a row as they lie in memory.  The loads of a thread are all issued before the first value is
-// widened: a conversion beside its load would wait for it, one load after the other.
+// touched: a conversion beside its load would wait for it, one load after the other.
+//
+// Magnitudes stay packed (two 16-bit patterns are compared by one instruction): `Mag` is what the columns keep, `key` orders the
+// largest of the four (the largest key of a warp, then `bits`, gives the magnitude as fp32 bits).  `Inv` is 2^-e as the scaling
+// takes it: fp32, or bfloat16 twice, whose products with bfloat16 values are exact (what falls below its least
+// normal number is far below the formats' and becomes 0 either way).
 template <class T>
 struct Quad {
-  typename std::conditional<sizeof(T) == 4, float4, uint2>::type raw;
+  static constexpr bool kWide = sizeof(T) == 4;
+  static constexpr bool kBf16 = std::is_same_v<T, __nv_bfloat16>;
+  typedef typename std::conditional<kWide, uint4, uint2>::type Raw;
+  typedef typename std::conditional<kWide, uint4, uint2>::type Mag;
+  typedef typename std::conditional<kBf16, uint32_t, float>::type Inv;
+  Raw raw;
   __device__ __forceinline__ void clear() { raw = {}; }
-  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const decltype(raw)*>(p); }
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
   // the first `left` of them, one by one: rows that are not aligned to four values, and a row's end
   __device__ __forceinline__ void load_some(const T* p, int64_t left) {
     clear();
@@ -40,59 +75,85 @@ struct Quad {
     for (int j = 0; j < 4; ++j)
       if (j < left) e[j] = p[j];
   }
-  __device__ __forceinline__ float4 values() const {
-    if constexpr (sizeof(T) == 4) {
-      return raw;
+  __device__ __forceinline__ Mag magnitudes() const {
+    if constexpr (kWide) return make_uint4(raw.x & 0x7FFFFFFFu, raw.y & 0x7FFFFFFFu, raw.z & 0x7FFFFFFFu, raw.w & 0x7FFFFFFFu);
+    else return make_uint2(raw.x & 0x7FFF7FFFu, raw.y & 0x7FFF7FFFu);
+  }
+  static __device__ __forceinline__ Mag larger(Mag a, Mag b) {
+    if constexpr (kWide) return make_uint4(max(a.x, b.x), max(a.y, b.y), max(a.z, b.z), max(a.w, b.w));
+    else return make_uint2(max_u16x2(a.x, b.x), max_u16x2(a.y, b.y));
+  }
+  static __device__ __forceinline__ uint32_t key(Mag m) {
+    if constexpr (kWide) {
+      return max(max(m.x, m.y), max(m.z, m.w));
     } else {
-      const T* const e = reinterpret_cast<const T*>(&raw);
-      return make_float4(widen(e[0]), widen(e[1]), widen(e[2]), widen(e[3]));
+      const uint32_t r = max_u16x2(m.x, m.y);
+      return max(r, r << 16);  // the larger half on top decides
+    }
+  }
+  // fp32 bits of a magnitude that is a key, or the upper half of a word
+  static __device__ __forceinline__ uint32_t bits(uint32_t k) {
+    if constexpr (kWide) return k;
+    else if constexpr (kBf16) return k & 0xFFFF0000u;
+    else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)(k >> 16))));
+  }
+  static __device__ __forceinline__ uint32_t column_bits(Mag m, int j) {
+    if constexpr (kWide) {
+      return j == 0 ? m.x : (j == 1 ? m.y : (j == 2 ? m.z : m.w));
+    } else {
+      const uint32_t w = j < 2 ? m.x : m.y;
+      return bits(j & 1 ? w : w << 16);
+    }
+  }
+  static __device__ __forceinline__ Inv inverse(uint32_t byte) {
+    if constexpr (kBf16) return (254u - byte) * 0x00800080u;
+    else return __uint_as_float((254u - byte) << 23);
+  }
+  // the inverses of columns 2 i and 2 i + 1, and of a whole row, as `codes` takes them
+  struct Pair {
+    Inv a, b;
+  };
+  static __device__ __forceinline__ Pair columns(uint32_t byte0, uint32_t byte1) {
+    if constexpr (kBf16) {
+      const uint32_t both = (254u - byte0) << 7 | (254u - byte1) << 23;
+      return {both, both};
+    } else {
+      return {inverse(byte0), inverse(byte1)};
+    }
+  }
+  __device__ __forceinline__ float4 values() const {
+    if constexpr (kWide) {
+      return make_float4(__uint_as_float(raw.x), __uint_as_float(raw.y), __uint_as_float(raw.z), __uint_as_float(raw.w));
+    } else if constexpr (kBf16) {
+      return make_float4(__uint_as_float(raw.x << 16), __uint_as_float(raw.x & 0xFFFF0000u), __uint_as_float(raw.y << 16),
+                         __uint_as_float(raw.y & 0xFFFF0000u));
+    } else {
+      const __half* const e = reinterpret_cast<const __half*>(&raw);
+      return make_float4(__half2float(e[0]), __half2float(e[1]), __half2float(e[2]), __half2float(e[3]));
+    }
+  }
+  // `lo` for the first two, `hi` for the last two values.  `finite`: the block has no NaN or infinity.
+  template <int FMT>
+  __device__ __forceinline__ uint32_t codes(Pair lo, Pair hi, bool finite) const {
+    if constexpr (kBf16) {
+      if (finite) {
+        Quad q;
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(q.raw.x) : "r"(raw.x), "r"(lo.a));
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(q.raw.y) : "r"(raw.y), "r"(hi.a));
+        const float4 f = q.values();
+        return codes_of<FMT>(f.x, f.y, f.z, f.w);
+      }
+      const auto wide = [](uint32_t pair, bool upper) { return __uint_as_float(upper ? pair & 0xFFFF0000u : pair << 16); };
+      const float4 f = values();
+      return codes_of<FMT>(finite_or_nan(f.x) * wide(lo.a, false), finite_or_nan(f.y) * wide(lo.a, true), finite_or_nan(f.z) * wide(hi.a, false),
+                           finite_or_nan(f.w) * wide(hi.a, true));
+    } else {
+      float4 f = values();
+      if (!finite) f = make_float4(finite_or_nan(f.x), finite_or_nan(f.y), finite_or_nan(f.z), finite_or_nan(f.w));
+      return codes_of<FMT>(__fmul_rn(f.x, lo.a), __fmul_rn(f.y, lo.b), __fmul_rn(f.z, hi.a), __fmul_rn(f.w, hi.b));
     }
   }
 };
-
-__device__ __forceinline__ uint32_t magnitude(float f) { return __float_as_uint(f) & 0x7FFFFFFFu; }
-__device__ __forceinline__ uint32_t magnitude4(float4 v) {
-  return max(max(magnitude(v.x), magnitude(v.y)), max(magnitude(v.z), magnitude(v.w)));
-}
-
-// The byte e + 127 for a block whose largest magnitude has these bits.  With max = 1.m * 2^E: e = E - 8 (e5m2: E - 15), one more
-// where 1.m > 1.75.  Where the result is below 2^-127 (max|x| < 2^-119) it is held there.  0 and what is not finite: 1.
-template <int FMT>
-__device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
-  if (bits == 0u || bits >= 0x7F800000u) return 127u;
-  const int e = (int)(bits >> 23) - (FMT == QB_E4M3 ? 8 : 15) + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-  return (uint32_t)max(e, 0);
-}
-__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
-
-// Four codes, the first in the low byte.  cvt would turn infinities into the largest finite value: they become NaN here.
-template <int FMT>
-__device__ __forceinline__ uint32_t codes4(float4 v, float4 inv, bool finite) {
-  if (!finite) {
-    const float nan = __uint_as_float(0x7FC00000u);
-    if (magnitude(v.x) >= 0x7F800000u) v.x = nan;
-    if (magnitude(v.y) >= 0x7F800000u) v.y = nan;
-    if (magnitude(v.z) >= 0x7F800000u) v.z = nan;
-    if (magnitude(v.w) >= 0x7F800000u) v.w = nan;
-  }
-  v.x = __fmul_rn(v.x, inv.x);
-  v.y = __fmul_rn(v.y, inv.y);
-  v.z = __fmul_rn(v.z, inv.z);
-  v.w = __fmul_rn(v.w, inv.w);
-  uint16_t lo, hi;
-  if constexpr (FMT == QB_E4M3) {
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(v.y), "f"(v.x));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(v.w), "f"(v.z));
-  } else {
-    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(v.y), "f"(v.x));
-    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(v.w), "f"(v.z));
-  }
-  return (uint32_t)lo | ((uint32_t)hi << 16);
-}
-template <int FMT>
-__device__ __forceinline__ uint32_t codes4(float4 v, float inv, bool finite) {
-  return codes4<FMT>(v, make_float4(inv, inv, inv, inv), finite);
-}
 
 struct Fp8Args {
   int64_t M, K;      // x [M][K]
@@ -105,46 +166,66 @@ struct Fp8Args {
   int vector;        // every row starts aligned to four values
 };
 
-// Rows only: a warp takes a segment of 512 columns of a row; lane l holds values 4 l .. 4 l + 3 of each of its four blocks, so
-// that loads and stores are whole lines and a block's maximum is one warp reduction.
+// Rows only: a warp takes two segments of 512 columns of a row (of neighbouring rows at a row's end); lane l holds values
+// 4 l .. 4 l + 3 of each of the eight blocks, so that loads and stores are whole lines and a block's maximum is one warp
+// reduction.  Lane j finishes block j (its scale, the byte), and the factors come back by shuffle.
 constexpr int kRowThreads = 256;
 template <class T, int FMT>
 __global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const T* x, Fp8Args a) {
   const int lane = threadIdx.x & 31;
   const uint32_t kq = (uint32_t)fp8_scale_words(a.Kp), items = (uint32_t)a.M * kq;  // M <= 2^24, kq <= 2^7
-  const uint32_t it = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t it = 2 * (blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5));
   pdl_begin();
   if (it >= items) return;
-  const uint32_t row = it / kq, q = it - row * kq;
-  const int c0 = (int)q * 512 + lane * 4, left = (int)a.K - c0;
-  const T* const p = x + (int64_t)row * a.K + c0;
-  Quad<T> v[4];
-  if (a.vector) {  // K is a multiple of four: what is left of a row is too
+  uint32_t row[2], q[2];
+  row[0] = it / kq;
+  q[0] = it - row[0] * kq;
+  const bool wrap = q[0] + 1 == kq;
+  row[1] = row[0] + (wrap ? 1 : 0);
+  q[1] = wrap ? 0 : q[0] + 1;
+  const int K = (int)a.K;
+  Quad<T> v[8];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int c0 = (int)q[s] * 512 + lane * 4;
+    const T* const p = x + (int64_t)row[s] * a.K + c0;
+    const int left = (s == 0 || it + 1 < items) ? K - c0 : 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      v[j].clear();
-      if (left > j * 128) v[j].load(p + j * 128);
+      Quad<T>& w = v[4 * s + j];
+      if (a.vector) {  // K is a multiple of four: what is left of a row is too
+        w.clear();
+        if (left > j * 128) w.load(p + j * 128);
+      } else {
+        w.load_some(p + j * 128, left - j * 128);
+      }
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j].load_some(p + j * 128, left - j * 128);
   }
-  uint8_t* const out = a.q + (int64_t)row * a.Kp + c0;
-  uint32_t word = 0;
-  bool finite = true;
+  uint32_t mine = 0;  // lane j: the largest key of block j
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float4 f = v[j].values();
-    const uint32_t top = __reduce_max_sync(0xffffffffu, magnitude4(f));
-    const uint32_t byte = scale_byte<FMT>(top);
-    word |= byte << (8 * j);
-    finite = finite && top < 0x7F800000u;
-    const uint32_t code = codes4<FMT>(f, inverse_scale(byte), top < 0x7F800000u);
-    if (c0 + j * 128 < (int)a.Kp) *reinterpret_cast<uint32_t*>(out + j * 128) = code;
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t top = __reduce_max_sync(0xffffffffu, Quad<T>::key(v[j].magnitudes()));
+    if (lane == j) mine = top;
   }
-  if (lane == 0) {
-    *reinterpret_cast<uint32_t*>(a.scale + fp8_scale_offset(row, 4 * q, kq)) = word;
-    if (!finite) report_status(a.ws, QB_ERR_NONFINITE);
+  const uint32_t top = Quad<T>::bits(mine), byte = scale_byte<FMT>(top);
+  const bool finite = __all_sync(0xffffffffu, top < 0x7F800000u);
+  if (lane < 8) {
+    const uint32_t s = lane >> 2, block = 4 * (s ? q[1] : q[0]) + (lane & 3);
+    if (it + s < items) a.scale[fp8_scale_offset(s ? row[1] : row[0], block, kq)] = (uint8_t)byte;
+    if (top >= 0x7F800000u) report_status(a.ws, QB_ERR_NONFINITE);
+  }
+  const typename Quad<T>::Inv inv = Quad<T>::inverse(byte);
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (s == 1 && it + 1 >= items) break;
+    const int c0 = (int)q[s] * 512 + lane * 4;
+    uint8_t* const out = a.q + (int64_t)row[s] * a.Kp + c0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const typename Quad<T>::Inv i = __shfl_sync(0xffffffffu, inv, 4 * s + j);
+      const uint32_t code = v[4 * s + j].template codes<FMT>({i, i}, {i, i}, finite);
+      if (c0 + j * 128 < (int)a.Kp) *reinterpret_cast<uint32_t*>(out + j * 128) = code;
+    }
   }
 }
 
@@ -153,8 +234,11 @@ __global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const T* x, Fp8Ar
 // The transposed codes cross shared memory, where a thread's 16 rows of a column are one 16-byte store, and leave as whole
 // lines.
 template <class T, int FMT, bool SQUARE>
-__global__ void __launch_bounds__(256, 2) fp8_tile_kernel(const T* x, Fp8Args a) {
-  __shared__ uint32_t tops[8][128];
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) fp8_tile_kernel(const T* x, Fp8Args a) {
+  typedef typename Quad<T>::Mag Mag;
+  typedef typename Quad<T>::Pair Pair;
+  __shared__ Mag tops[8][32];
+  __shared__ uint32_t squares[8];
   __shared__ uint4 turned[128 * 8];  // [column][8 pieces of 16 rows], piece p of column c at p ^ (c / 4 % 8)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t k_tiles = (uint32_t)(a.Kp / 128), mt = blockIdx.x / k_tiles, kt = blockIdx.x - mt * k_tiles;
@@ -163,77 +247,67 @@ __global__ void __launch_bounds__(256, 2) fp8_tile_kernel(const T* x, Fp8Args a)
   pdl_begin();
   Quad<T> v[16];
   const T* const p = x + (int64_t)m0 * a.K + k0;
-  if (a.vector) {
+  if (a.vector && rows >= 16 && (int)kt * 128 + 128 <= (int)a.K) {  // all there
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      v[i].clear();
-      if (i < rows && left > 0) v[i].load(p + i * a.K);
-    }
+    for (int i = 0; i < 16; ++i) v[i].load(p + i * a.K);
   } else {
+    // (K a multiple of four: the lane's four columns are all there or none)
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i].load_some(p + i * a.K, i < rows ? left : 0);
   }
-  uint32_t col[4] = {0, 0, 0, 0};
-  uint32_t row_top = 0;  // lane i: of row i
+  Mag col = v[0].magnitudes();
+  uint32_t row_key = 0;  // lane i: of row i
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const float4 f = v[i].values();
-    const uint32_t m[4] = {magnitude(f.x), magnitude(f.y), magnitude(f.z), magnitude(f.w)};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) col[j] = max(col[j], m[j]);
+    const Mag m = v[i].magnitudes();
+    if (i > 0) col = Quad<T>::larger(col, m);
     if constexpr (!SQUARE) {
-      const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(m[0], m[1]), max(m[2], m[3])));
-      if (lane == i) row_top = top;
+      const uint32_t top = __reduce_max_sync(0xffffffffu, Quad<T>::key(m));
+      if (lane == i) row_key = top;
     }
   }
   if constexpr (SQUARE) {
-    const uint32_t mine = __reduce_max_sync(0xffffffffu, max(max(col[0], col[1]), max(col[2], col[3])));
-    if (lane == 0) tops[warp][0] = mine;
+    const uint32_t mine = __reduce_max_sync(0xffffffffu, Quad<T>::key(col));
+    if (lane == 0) squares[warp] = mine;
   } else {
-    if (a.qt) *reinterpret_cast<uint4*>(&tops[warp][lane * 4]) = make_uint4(col[0], col[1], col[2], col[3]);
+    if (a.qt) tops[warp][lane] = col;
   }
   __syncthreads();
   if constexpr (SQUARE) {
 #pragma unroll
-    for (int w = 0; w < 8; ++w) row_top = max(row_top, tops[w][0]);
+    for (int w = 0; w < 8; ++w) row_key = max(row_key, squares[w]);
   }
-  const uint32_t row_byte = scale_byte<FMT>(row_top);
+  const uint32_t row_top = Quad<T>::bits(row_key), row_byte = scale_byte<FMT>(row_top);
   if (lane < 16 && lane < rows) {
     a.scale[fp8_scale_offset(m0 + lane, kt, fp8_scale_words(a.Kp))] = (uint8_t)row_byte;
     if (row_top >= 0x7F800000u) report_status(a.ws, QB_ERR_NONFINITE);
   }
   const bool rows_finite = __all_sync(0xffffffffu, row_top < 0x7F800000u);
-  const float row_inv = inverse_scale(row_byte);
+  const typename Quad<T>::Inv row_inv = Quad<T>::inverse(row_byte);
   uint8_t* const out = a.q + (int64_t)m0 * a.Kp + k0;
   uint32_t code[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const float inv = SQUARE ? row_inv : __shfl_sync(0xffffffffu, row_inv, i);
-    code[i] = codes4<FMT>(v[i].values(), inv, rows_finite);
+    const typename Quad<T>::Inv inv = SQUARE ? row_inv : __shfl_sync(0xffffffffu, row_inv, i);
+    code[i] = v[i].template codes<FMT>(Pair{inv, inv}, Pair{inv, inv}, rows_finite);
     if (i < rows) *reinterpret_cast<uint32_t*>(out + i * a.Kp) = code[i];
   }
   if (!a.qt) return;
   if constexpr (!SQUARE) {  // the columns' own scales
-    uint32_t top[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const uint4 t = *reinterpret_cast<const uint4*>(&tops[w][lane * 4]);
-      top[0] = max(top[0], t.x);
-      top[1] = max(top[1], t.y);
-      top[2] = max(top[2], t.z);
-      top[3] = max(top[3], t.w);
-    }
-    float inv[4];
+    for (int w = 0; w < 8; ++w) col = Quad<T>::larger(col, tops[w][lane]);
+    uint32_t byte[4];
     bool finite = true;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t byte = scale_byte<FMT>(top[j]);
-      inv[j] = inverse_scale(byte);
-      finite = finite && top[j] < 0x7F800000u;
-      if (warp == 0 && j < left) a.scale_t[fp8_scale_offset(k0 + j, mt, fp8_scale_words(a.Mp))] = (uint8_t)byte;
+      const uint32_t top = Quad<T>::column_bits(col, j);
+      byte[j] = scale_byte<FMT>(top);
+      finite = finite && top < 0x7F800000u;
+      if (warp == 0 && j < left) a.scale_t[fp8_scale_offset(k0 + j, mt, fp8_scale_words(a.Mp))] = (uint8_t)byte[j];
     }
+    const Pair lo = Quad<T>::columns(byte[0], byte[1]), hi = Quad<T>::columns(byte[2], byte[3]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) code[i] = codes4<FMT>(v[i].values(), make_float4(inv[0], inv[1], inv[2], inv[3]), finite);
+    for (int i = 0; i < 16; ++i) code[i] = v[i].template codes<FMT>(lo, hi, finite);
   } else if (warp == 0) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -263,7 +337,7 @@ __global__ void __launch_bounds__(256, 2) fp8_tile_kernel(const T* x, Fp8Args a)
 template <class T, int FMT>
 static qb_status launch_fp8(const T* x, const Fp8Args& a, bool square, cudaStream_t stream) {
   if (!square && !a.qt) {
-    const int64_t items = a.M * fp8_scale_words(a.Kp), blocks = (items + kRowThreads / 32 - 1) / (kRowThreads / 32);
+    const int64_t items = a.M * fp8_scale_words(a.Kp), blocks = (items + kRowThreads / 16 - 1) / (kRowThreads / 16);
     QB_CUDA_TRY(launch_kernel(fp8_rows_kernel<T, FMT>, (unsigned)blocks, kRowThreads, 0, stream, 1, false, x, a));
     return QB_OK;
   }
