@@ -414,7 +414,8 @@ enum { QB_E4M3 = 0, QB_E5M2 = 1 };
  * of a and b may differ.  For a linear y = x W^T: forward a = x, b = W; grad_x: a = grad_y, b = W transposed; grad_W: a = grad_y
  * transposed, b = x transposed.
  *   bias dev fp32 [N] or NULL (read);  y dev [M][N], aligned to its elements (written)
- * M, N and K as in qb_gemm.
+ * M, N and K as in qb_gemm.  Any workspace will do; one of 1024 + n * 4 * M * N bytes lets a product of few tiles over a long K (the
+ * gradient of a small weight matrix over many tokens) be summed in up to n parts side by side, always in the same order.
  */
 size_t qb_fp8_scale_bytes(int64_t rows, int64_t K);
 qb_status qb_quantize_fp8(const void* x, int type, int64_t M, int64_t K, int format, uint8_t* xq, uint8_t* x_scale,

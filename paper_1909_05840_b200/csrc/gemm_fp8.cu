@@ -33,16 +33,20 @@ namespace qb {
 
 struct Fp8Params {
   CUtensorMap tma, tmb;    // codes, box 128 bytes of K x the CTA's rows
+  CUtensorMap tmb_half;    // pairs: B's rows for a tile of half the width
   CUtensorMap tmsa, tmsb;  // scales as rows of 512 bytes
   const float* bias;
   void* y;
   void* ws;
   int32_t M, N, K;
   int32_t n_tiles, tiles;
+  int32_t whole;        // tiles below this are BT wide; pairs: the others are halves, two after the other
+  int32_t split_tiles;  // tiles of one split of K (split s writes rows s * M .. of y, fp32)
+  int32_t split_blocks; // blocks of 128 of K per split, a multiple of 4 where there are several
   int32_t words;        // rows of 512 bytes of scales per 128 rows of codes
   int32_t a_last, b_last;  // last block of 128 rows of A's and of B's scales
   int32_t vector;       // 1: rows of y are 16-byte aligned
-  uint32_t idesc;       // the formats' part of the instruction descriptor
+  uint32_t idesc;       // fp8_idesc
 };
 
 constexpr int kFp8EpilogueWarps = 8;
@@ -80,11 +84,33 @@ __device__ __forceinline__ uint64_t fp8_operand_desc(uint32_t smem_addr) {
 __device__ __forceinline__ uint64_t fp8_scale_desc(uint32_t smem_addr) {
   return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
-// Instruction descriptor for kind::mxf8f6f4 without the byte numbers of the scales (A's in bits 29-30, B's in 4-5): formats in
-// bits 7-9 and 10-12 (e4m3 0, e5m2 1), both operands K-major, N >> 3 in 17-22, scales UE8M0 (23), M >> 4 in 24-28.
-static uint32_t fp8_idesc(int a_format, int b_format, int mma_m, int mma_n) {
-  return ((uint32_t)a_format << 7) | ((uint32_t)b_format << 10) | ((uint32_t)(mma_n >> 3) << 17) | (1u << 23) | ((uint32_t)(mma_m >> 4) << 24);
+// Instruction descriptor for kind::mxf8f6f4 without N >> 3 (bits 17-22) and the byte numbers of the scales (A's in bits 29-30, B's
+// in 4-5): formats in bits 7-9 and 10-12 (e4m3 0, e5m2 1), both operands K-major, scales UE8M0 (23), M >> 4 in 24-28.
+static uint32_t fp8_idesc(int a_format, int b_format, int mma_m) {
+  return ((uint32_t)a_format << 7) | ((uint32_t)b_format << 10) | (1u << 23) | ((uint32_t)(mma_m >> 4) << 24);
 }
+
+// Where tile t lies: first row and column, columns, split and its range of K blocks.
+template <int BT, int CG>
+struct Fp8Tile {
+  int m0, n0, width, split, k0, k1;
+  __device__ __forceinline__ Fp8Tile(const Fp8Params& gp, int t) {
+    split = t / gp.split_tiles;
+    t -= split * gp.split_tiles;
+    k0 = split * gp.split_blocks;
+    k1 = min(k0 + gp.split_blocks, gp.K / 128);
+    width = BT;
+    int half = 0;
+    if (CG == 2 && t >= gp.whole) {
+      half = (t - gp.whole) & 1;
+      t = gp.whole + ((t - gp.whole) >> 1);
+      width = BT / 2;
+    }
+    m0 = t / gp.n_tiles;
+    n0 = (t - m0 * gp.n_tiles) * BT + half * (BT / 2);
+    m0 *= 128 * CG;
+  }
+};
 
 // Barrier over the epilogue warps (named barrier 1) that also ORs a predicate over them.
 __device__ __forceinline__ bool fp8_epilogue_sync_or(bool pred) {
@@ -101,7 +127,6 @@ template <int BT, int CG, bool BF16>
 __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_constant__ Fp8Params gp) {
   using Cfg = Fp8Cfg<BT, CG>;
   constexpr int kStages = Cfg::kStages;
-  constexpr int kRows = 128 * CG;  // rows of A per tile of the CTA group
   const uint32_t rank = CG == 2 ? ptx::cluster_ctarank() : 0u;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t smem_base = ptx::smem_u32(smem);
@@ -153,7 +178,6 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
   auto lead = [&](uint32_t bar) { return CG == 2 ? ptx::map_to_cta(bar, 0) : bar; };
 
   const int groups = (int)gridDim.x / CG, group = (int)blockIdx.x / CG;
-  const int k_blocks = gp.K / 128;
   bool timed_out = false;
   int where = 0;
 
@@ -163,9 +187,14 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
       int stage = 0;
       uint32_t phase = 0;
       for (int t = group; t < gp.tiles && !timed_out; t += groups) {
-        const int m0 = t / gp.n_tiles * kRows + (int)rank * 128, n0 = t % gp.n_tiles * BT;
+        const Fp8Tile<BT, CG> tile(gp, t);
+        const bool half = CG == 2 && tile.width < BT;
+        const int m0 = tile.m0 + (int)rank * 128, n0 = tile.n0;
         const int sa = min(m0 / 128, gp.a_last) * gp.words;
-        for (int kb = 0; kb < k_blocks; ++kb) {
+        const int b_row = n0 + (int)rank * (tile.width / CG);
+        const CUtensorMap* const tmb = half ? &gp.tmb_half : &gp.tmb;
+        const uint32_t bytes = CG * (Cfg::kABytes + (half ? Cfg::kBBytes / 2 : Cfg::kBBytes));
+        for (int kb = tile.k0; kb < tile.k1; ++kb) {
           if (!wait_barrier_relaxed(empty(stage), phase ^ 1u, abort_flag)) {
             timed_out = true;
             where = (0 << 16) | stage;
@@ -174,7 +203,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
           const bool scales = (kb & 3) == 0;
           const uint32_t a_smem = smem_base + stage * Cfg::kStageBytes, b_smem = a_smem + Cfg::kABytes;
           const uint32_t s_smem = scale_base + stage * Cfg::kScaleBytes;
-          if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), CG * (Cfg::kStageBytes + (scales ? Cfg::kScaleBytes : 0)));
+          if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), bytes + (scales ? CG * Cfg::kScaleBytes : 0));
           auto load = [&](uint32_t dst, const CUtensorMap* tm, int x, int y) {
             if constexpr (CG == 2) ptx::tma_load_2d_pair(dst, tm, lead(full(stage)), x, y);
             else ptx::tma_load_2d(dst, tm, full(stage), x, y);
@@ -186,7 +215,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
               load(s_smem + 512 * (1 + j), &gp.tmsb, 0, min(n0 / 128 + j, gp.b_last) * gp.words + kb / 4);
           }
           load(a_smem, &gp.tma, kb * 128, m0);
-          load(b_smem, &gp.tmb, kb * 128, n0 + (int)rank * (BT / CG));
+          load(b_smem, tmb, kb * 128, b_row);
           if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
@@ -210,7 +239,9 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
       for (int t = group; t < gp.tiles && !timed_out; t += groups, ++it) {
         const int a = it & 1;
         const uint32_t d = tmem_base + (a ? Cfg::kAcc1 : 0);
-        const uint32_t sfb = sfb0 + (uint32_t)(t % gp.n_tiles * BT % 128 / 32);  // where the tile begins in its block of 128 scales
+        const Fp8Tile<BT, CG> tile(gp, t);
+        const uint32_t sfb = sfb0 + (uint32_t)(tile.n0 % 128 / 32);  // where the tile begins in its block of 128 scales
+        const uint32_t idesc0 = gp.idesc | ((uint32_t)(tile.width >> 3) << 17);
         bool ok = wait_barrier(acc_empty(a), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag);
         if (Cfg::kOverlap && ok && it > 0) ok = wait_barrier(overlap_read, (uint32_t)(it - 1) & 1u, abort_flag);
         if (!ok) {
@@ -218,7 +249,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
           where = (1 << 16) | 0x100 | a;
           break;
         }
-        for (int kb = 0; kb < k_blocks; ++kb) {
+        for (int kb = tile.k0; kb < tile.k1; ++kb) {
           if (!wait_barrier(full(stage), phase, abort_flag)) {
             timed_out = true;
             where = (1 << 16) | stage;
@@ -231,12 +262,12 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
 #pragma unroll
             for (int j = 0; j <= Cfg::kScaleBlocksB; ++j) ptx::tmem_copy_scales_cg<CG>(sfa + 4 * j, s_desc + (uint64_t)(j * (512 >> 4)));
           }
-          const uint32_t idesc = gp.idesc | (id << 29) | (id << 4);
+          const uint32_t idesc = idesc0 | (id << 29) | (id << 4);
           const uint64_t a_desc = a_desc0 + (uint64_t)(stage * (Cfg::kStageBytes >> 4));
           const uint64_t b_desc = b_desc0 + (uint64_t)(stage * (Cfg::kStageBytes >> 4));
 #pragma unroll
           for (int j = 0; j < 4; ++j)  // 32 elements of K per instruction: 32 bytes
-            ptx::mma_mxf8_ss_cg<CG>(d, a_desc + 2u * j, b_desc + 2u * j, idesc, sfa, sfb, (kb | j) != 0 ? 1u : 0u);
+            ptx::mma_mxf8_ss_cg<CG>(d, a_desc + 2u * j, b_desc + 2u * j, idesc, sfa, sfb, kb != tile.k0 || j != 0 ? 1u : 0u);
           ptx::mma_commit_cg<CG>(empty(stage));
           if (++stage == kStages) {
             stage = 0;
@@ -270,7 +301,8 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
     int it = 0;
     for (int t = group; t < gp.tiles; t += groups, ++it) {
       const int a = it & 1;
-      const int m0 = t / gp.n_tiles * kRows + (int)rank * 128 + quarter * 32, n0 = t % gp.n_tiles * BT;
+      const Fp8Tile<BT, CG> tile(gp, t);
+      const int m0 = tile.m0 + (int)rank * 128 + quarter * 32, n0 = tile.n0;
       bias_tile[a * 256 + e] = gp.bias && e < BT && n0 + e < gp.N ? gp.bias[n0 + e] : 0.0f;
       const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
       if (fp8_epilogue_sync_or(!ok)) {  // publishes the bias, and all eight warps give up together
@@ -280,7 +312,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
       }
       ptx::tcgen05_fence_after_sync();
       const uint32_t acc = lanes + (a ? Cfg::kAcc1 : 0);
-      const int chunks = m0 < gp.M ? min(BT / kCols, (gp.N - n0 + kCols - 1) / kCols) : 0;
+      const int chunks = m0 < gp.M ? max(0, min(tile.width / kCols, (gp.N - n0 + kCols - 1) / kCols)) : 0;
       // accumulator 0 shares its last 32 columns, accumulator 1 its first: they are read first, by the quarter's first warp
       const bool down = Cfg::kOverlap && a == 0;
       if (Cfg::kOverlap && half == 0 && (down ? chunks < BT / kCols : chunks == 0)) arrive(overlap_read);
@@ -324,10 +356,11 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
         }
         __syncwarp();
         const int rows = min(32, gp.M - m0);
+        const size_t first_row = (size_t)tile.split * gp.M;
         if (gp.vector) {  // 16 bytes a lane, four whole lines a store
           constexpr int kPiece = BF16 ? 8 : 4;  // columns in 16 bytes
           const int piece = lane & 7, col = n0 + c0 + piece * kPiece;
-          uint8_t* const to = static_cast<uint8_t*>(gp.y) + ((size_t)m0 * gp.N + col) * (16 / kPiece);
+          uint8_t* const to = static_cast<uint8_t*>(gp.y) + ((first_row + m0) * gp.N + col) * (16 / kPiece);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int r = 4 * i + (lane >> 3);
@@ -340,7 +373,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
             for (int p = 0; p < kCols / 32; ++p) {
               const int c = lane + 32 * p, col = n0 + c0 + c;
               if (col >= gp.N) continue;
-              const size_t at = (size_t)(m0 + r) * gp.N + col;
+              const size_t at = (first_row + m0 + r) * gp.N + col;
               if constexpr (BF16)
                 static_cast<uint16_t*>(gp.y)[at] = *reinterpret_cast<const uint16_t*>(buf + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2);
               else
@@ -381,6 +414,69 @@ static qb_status launch_gemm_fp8(const Fp8Params& gp, int sms, cudaStream_t stre
   return QB_OK;
 }
 
+// y = the splits' sum, in their order, + bias.
+template <bool BF16, bool VECTOR>
+__global__ void __launch_bounds__(256) fp8_join_kernel(const float* parts, int splits, int64_t MN, int N, const float* bias, void* y) {
+  constexpr int V = VECTOR ? 4 : 1;
+  pdl_begin();
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V; i < MN; i += (int64_t)gridDim.x * 256 * V) {
+    float v[V];
+    if constexpr (VECTOR) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(parts + i);
+    else v[0] = parts[i];
+    for (int s = 1; s < splits; ++s) {
+      float w[V];
+      if constexpr (VECTOR) *reinterpret_cast<float4*>(w) = *reinterpret_cast<const float4*>(parts + s * MN + i);
+      else w[0] = parts[s * MN + i];
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] += w[j];
+    }
+    const int n = (int)(i % N);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (bias) v[j] += bias[n + j];  // (vectors: N is a multiple of 4)
+      if constexpr (BF16) static_cast<__nv_bfloat16*>(y)[i + j] = __float2bfloat16_rn(v[j]);
+      else static_cast<float*>(y)[i + j] = v[j];
+    }
+  }
+}
+
+// The form of a product: CTAs per tile, columns, for pairs how many tiles are whole, and splits of K.
+struct Fp8Choice {
+  int cg, bt;
+  int32_t tiles, whole, splits, split_blocks;
+};
+// The cheapest by the costs of a tile, in hundredths of a microsecond: a part per block of 128 of K and a fixed part, fitted to the
+// times of whole rounds (24,576 x 1,024 x 4,096 and 18,944 x 4,096 x 1,024: pairs 76.6 and 66.9 us, 128 columns 96.2 and 86.3, 64
+// columns 131.7 and 119.6).  A last round that fills at most half of the pairs is cut into tiles of half the width, which take
+// about 0.7 of the time (6,144 x 1,024 x 4,096, 96 tiles: 25.4 -> 22.1 us).  Where a long K meets few tiles, K is split into
+// runs that are a multiple of 512 (a word of scales), whose sums a second kernel joins: that costs its launch and the traffic of
+// the parts.
+static Fp8Choice choose_fp8(int64_t M, int64_t N, int64_t K, int sms, size_t scratch) {
+  const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m; };
+  static constexpr struct {
+    int cg, bt, block, fixed;
+  } kForms[] = {{2, 256, 34, 126}, {1, 128, 24, 64}, {1, 64, 18, 38}};
+  const int64_t blocks = K / 128;
+  Fp8Choice best = {};
+  int64_t best_cost = 0;
+  for (const auto& f : kForms) {
+    if (f.cg == 2 && sms < 2) continue;
+    const int64_t groups = sms / f.cg, tiles = up(M, 128 * f.cg) * up(N, f.bt);
+    for (int64_t splits = 1; splits == 1 || (4 * splits <= blocks && tiles * (splits - 1) < groups && splits * M * N * 4 <= (int64_t)scratch); ++splits) {
+      const int64_t run = splits == 1 ? blocks : up(up(blocks, splits), 4) * 4;
+      if (up(blocks, run) != splits) continue;
+      const int64_t tile = f.block * run + f.fixed, all = tiles * splits, last = all % groups;
+      const bool halves = f.cg == 2 && splits == 1 && last > 0 && 2 * last <= groups;
+      const int64_t cost = (all / groups) * tile + (halves ? tile * 7 / 10 : (last > 0 ? tile : 0)) + (splits > 1 ? 250 + splits * M * N / 7500 : 0);
+      if (best.cg == 0 || cost < best_cost) {
+        best_cost = cost;
+        best = {f.cg, f.bt, (int32_t)(halves ? all + last : all), (int32_t)(halves ? all - last : all), (int32_t)splits, (int32_t)run};
+      }
+    }
+  }
+  return best;
+}
+
 }  // namespace qb
 
 extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a_format, const uint8_t* b, const uint8_t* b_scale,
@@ -410,31 +506,46 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
     set_last_error("qb_gemm_fp8: more than 2^30 tiles (M=%lld N=%lld)", (long long)M, (long long)N);
     return QB_ERR_INVALID;
   }
-  const int cg = sms >= 2 && up(M, 256) * up(N, 256) >= sms / 2 ? 2 : 1;
-  const int bt = cg == 2 ? 256 : (up(M, 128) * up(N, 128) >= sms ? 128 : 64);
+  const size_t head = 1024;  // the parts of a split product lie behind it
+  const bool roomy = ws_bytes > head && reinterpret_cast<uintptr_t>(ws) % 16 == 0;
+  const Fp8Choice choice = choose_fp8(M, N, K, sms, roomy ? ws_bytes - head : 0);
+  const int cg = choice.cg, bt = choice.bt;
   Fp8Params gp;
   const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8, u32 = CU_TENSOR_MAP_DATA_TYPE_UINT32;
   gp.words = (int32_t)fp8_scale_words(K);
   if ((st = make_matrix_map(&gp.tma, u8, a, M, K, K, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != QB_OK) return st;
   if ((st = make_matrix_map(&gp.tmb, u8, b, N, K, K, bt / cg, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != QB_OK) return st;
+  gp.tmb_half = gp.tmb;
+  if (choice.whole < choice.tiles && (st = make_matrix_map(&gp.tmb_half, u8, b, N, K, K, bt / 4, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != QB_OK) return st;
   if ((st = make_matrix_map(&gp.tmsa, u32, a_scale, up(M, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
   if ((st = make_matrix_map(&gp.tmsb, u32, b_scale, up(N, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
-  const int size = out_type == QB_F32 ? 4 : 2;
-  gp.vector = N * size % 16 == 0 && aligned16(y);
-  gp.bias = bias;
-  gp.y = y;
+  const bool split = choice.splits > 1;
+  float* const parts = reinterpret_cast<float*>(static_cast<char*>(ws) + head);
+  gp.vector = split ? N % 4 == 0 : N * (out_type == QB_F32 ? 4 : 2) % 16 == 0 && aligned16(y);
+  gp.bias = split ? nullptr : bias;
+  gp.y = split ? parts : y;
+  gp.split_blocks = choice.split_blocks;
+  gp.split_tiles = choice.tiles / choice.splits;
   gp.ws = ws;
   gp.M = (int32_t)M;
   gp.N = (int32_t)N;
   gp.K = (int32_t)K;
   gp.n_tiles = (int32_t)up(N, bt);
-  gp.tiles = (int32_t)(up(M, 128 * cg) * gp.n_tiles);
+  gp.tiles = choice.tiles;
+  gp.whole = choice.whole;
   gp.a_last = (int32_t)up(M, 128) - 1;
   gp.b_last = (int32_t)up(N, 128) - 1;
-  gp.idesc = fp8_idesc(a_format, b_format, 128 * cg, bt);
+  gp.idesc = fp8_idesc(a_format, b_format, 128 * cg);
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  const bool bf16 = out_type == QB_BF16;
-  if (cg == 2) return bf16 ? launch_gemm_fp8<256, 2, true>(gp, sms, stream) : launch_gemm_fp8<256, 2, false>(gp, sms, stream);
-  if (bt == 128) return bf16 ? launch_gemm_fp8<128, 1, true>(gp, sms, stream) : launch_gemm_fp8<128, 1, false>(gp, sms, stream);
-  return bf16 ? launch_gemm_fp8<64, 1, true>(gp, sms, stream) : launch_gemm_fp8<64, 1, false>(gp, sms, stream);
+  const bool bf16 = out_type == QB_BF16 && !split;
+  if (cg == 2) st = bf16 ? launch_gemm_fp8<256, 2, true>(gp, sms, stream) : launch_gemm_fp8<256, 2, false>(gp, sms, stream);
+  else if (bt == 128) st = bf16 ? launch_gemm_fp8<128, 1, true>(gp, sms, stream) : launch_gemm_fp8<128, 1, false>(gp, sms, stream);
+  else st = bf16 ? launch_gemm_fp8<64, 1, true>(gp, sms, stream) : launch_gemm_fp8<64, 1, false>(gp, sms, stream);
+  if (st != QB_OK || !split) return st;
+  const bool vector = N % 4 == 0;
+  auto join = out_type == QB_BF16 ? (vector ? fp8_join_kernel<true, true> : fp8_join_kernel<true, false>)
+                                  : (vector ? fp8_join_kernel<false, true> : fp8_join_kernel<false, false>);
+  QB_CUDA_TRY(launch_kernel(join, (unsigned)std::min<int64_t>(up(M * N, vector ? 1024 : 256), (int64_t)sms * 8), 256, 0, stream, 1, false, parts,
+                            choice.splits, M * N, (int)N, bias, y));
+  return QB_OK;
 }

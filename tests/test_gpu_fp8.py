@@ -163,7 +163,8 @@ def check_product(y, a, sa, b, sb, bias, out):
 
 # (M, N, K): one value, odd sizes, every tile form (64 and 128 columns, pairs), several tiles a CTA, partial last tiles
 PRODUCTS = [(1, 1, 128), (1, 9, 768), (5, 64, 256), (77, 130, 640), (128, 128, 128), (300, 520, 1152), (2000, 900, 384), (2048, 1280, 512),
-            (2561, 2600, 768), (4100, 4099, 256), (4096, 5000, 128)]
+            (2561, 2600, 768), (4100, 4099, 256), (4096, 5000, 128),
+            (6144, 1024, 640), (5003, 2304, 256)]
 
 
 @pytest.mark.gpu
@@ -179,6 +180,24 @@ def test_product(ws, M, N, K, out):
     assert qb.read_status(ws) == qb.QB_OK
     check_product(y, a, sa, b, sb, bias, out)
     assert (buffer[M * N:] == 3.0).all()
+
+
+# few tiles over a long contraction: summed in parts side by side where the workspace has room, in one piece where not
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(9, 7, 8192), (256, 300, 24576), (129, 770, 65536), (768, 768, 4224)])
+def test_long_contractions(M, N, K, out):
+    a, sa = qb.quantize_fp8(rows_of(M, K, 1), qb.workspace())
+    b, sb = qb.quantize_fp8(rows_of(N, K, 2), qb.workspace())
+    bias = torch.randn(N, device="cuda")
+    for nbytes in (256, 1024 + 3 * M * N * 4, 1024 + 100 * M * N * 4):
+        ws = torch.zeros(nbytes, dtype=torch.uint8, device="cuda")
+        y = qb.gemm_fp8(a, sa, b, sb, bias, ws, out)
+        check_product(y, a, sa, b, sb, bias, out)
+        assert torch.equal(y, qb.gemm_fp8(a, sa, b, sb, bias, ws, out))
+        shifted = torch.empty(M * N + 1, dtype=out, device="cuda")[1:].view(M, N)
+        assert torch.equal(y, qb.gemm_fp8(a, sa, b, sb, bias, ws, out, y=shifted))
+        assert qb.read_status(ws) == qb.QB_OK
 
 
 @pytest.mark.gpu
