@@ -338,7 +338,7 @@ template <class T, int FMT>
 static qb_status launch_fp8(const T* x, const Fp8Args& a, bool square, cudaStream_t stream) {
   if (!square && !a.qt) {
     const int64_t items = a.M * fp8_scale_words(a.Kp), blocks = (items + kRowThreads / 16 - 1) / (kRowThreads / 16);
-    QB_CUDA_TRY(launch_kernel(fp8_rows_kernel<T, FMT>, (unsigned)blocks, kRowThreads, 0, stream, 1, false, x, a));
+    QB_CUDA_TRY(launch_kernel<kMostL1>(fp8_rows_kernel<T, FMT>, (unsigned)blocks, kRowThreads, 0, stream, 1, false, x, a));
     return QB_OK;
   }
   auto kernel = square ? fp8_tile_kernel<T, FMT, true> : fp8_tile_kernel<T, FMT, false>;
