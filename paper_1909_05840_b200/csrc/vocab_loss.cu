@@ -37,7 +37,11 @@ constexpr int kVocabStages = 5;
 constexpr int kVocabStageBytes = 32768;  // 128 rows of A and 128 of B, 64 elements of K each
 constexpr int kVocabOutBytes = kVocabEpilogueWarps * 4096;
 constexpr int kVocabBarBytes = 256;
-constexpr int kVocabColBytes = 2 * 3 * 256 * 4;  // per accumulator: three values of each of the tile's 256 columns
+// Backward: per accumulator three values of each of the tile's columns.  Forward with few tokens: a maximum and a sum per lane
+// quarter and token.
+constexpr int kVocabColBytes = 2 * 3 * 256 * 4;
+constexpr int kFewTokens = 128;
+static_assert(4 * kFewTokens * 8 <= kVocabColBytes, "columns' values");
 constexpr int kVocabSmemBytes = kVocabStages * kVocabStageBytes + kVocabOutBytes + kVocabBarBytes + kVocabColBytes;
 constexpr int kMaxPairs = 80;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -47,6 +51,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 // holds 8 KB or 16: with two boxes per operand everywhere, 4,096 x 30,522 x 768 forward took 165 us instead of 121.
 enum VocabForm { kRows = 0, kCols = 1, kCols2 = 2 };
 enum VocabKind { kLogits = 0, kGradZ = 1, kGradW = 2, kGradH = 3 };
+// FEW: up to kFewTokens tokens.  They are then the columns of the tiles of logits in the forward pass too, and the tiles are as wide
+// as the tokens (rounded up to 32): a pair loads 256 words and those tokens, not 256 rows of mostly nothing (77 tokens, 30,522
+// x 768: forward 21.8 -> 17.1 us, backward 69 -> 61).  With more tokens narrower tiles do not pay: loads bound the K blocks, so
+// that 613 tokens as 3 x 224 columns took as long as 3 x 256, and the logits are reduced with a token per lane, which needs no
+// exchange between lanes.
 
 // One kind of tile of a launch.
 struct VocabProblem {
@@ -54,6 +63,7 @@ struct VocabProblem {
   int32_t map_a, map_b;    // tensor maps of the operands
   int32_t a_form, b_form;  // kRows, kCols or kCols2
   int32_t n_tiles;         // tile t of a split: row tile t / n_tiles, column tile t % n_tiles
+  int32_t width;           // columns of a tile (FEW, logits; else 256)
   int32_t m_tiles;         // not 0: column tile t / m_tiles, row tile t % m_tiles
   int32_t split_tiles;     // tiles per split of the contraction
   int32_t k_blocks;        // of one split
@@ -96,8 +106,8 @@ __device__ __forceinline__ uint64_t vocab_desc(uint32_t smem_addr, int mn) {
 }
 // Instruction descriptor for kind::f16: D fp32 (bits 4-5 = 1), A and B bfloat16 (7-9, 10-12 = 1), MN-major A and B (15, 16),
 // N >> 3 (17-22), M >> 4 (24-28).
-__device__ __forceinline__ uint32_t vocab_idesc(int a_mn, int b_mn) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(kVocabTile >> 3) << 17) |
+__device__ __forceinline__ uint32_t vocab_idesc(int a_mn, int b_mn, int width) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(width >> 3) << 17) |
          ((uint32_t)(kVocabTile >> 4) << 24);
 }
 
@@ -156,7 +166,7 @@ struct VocabTileAt {
 };
 
 // FORWARD: logits tiles alone; else the three kinds of the backward pass.
-template <bool FORWARD>
+template <bool FORWARD, bool FEW>
 __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_constant__ VocabParams gp) {
   constexpr int kStages = kVocabStages;
   const uint32_t rank = ptx::cluster_ctarank();
@@ -217,7 +227,9 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
       for (bool have = c.first(gp, g); have && !timed_out; have = c.next(gp, g)) {
         const VocabProblem& pr = gp.prob[c.i];
         const VocabTileAt at(pr, c.t);
-        const int a_row = at.m * kVocabTile + (int)rank * 128, b_row = at.n * kVocabTile + (int)rank * 128;
+        const int width = FEW ? pr.width : kVocabTile;
+        const int a_row = at.m * kVocabTile + (int)rank * 128, b_row = at.n * kVocabTile + (int)rank * (width / 2);
+        const uint32_t bytes = kVocabStageBytes + 2 * (width / 2 * 128);
         const CUtensorMap* const ma = &gp.map[pr.map_a];
         const CUtensorMap* const mb = &gp.map[pr.map_b];
         for (int kb = at.k0; kb < at.k1; ++kb) {
@@ -227,7 +239,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
             break;
           }
           const uint32_t a_smem = smem_base + stage * kVocabStageBytes, b_smem = a_smem + kVocabStageBytes / 2, bar = lead(full(stage));
-          if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), 2 * kVocabStageBytes);
+          if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), bytes);
           auto load = [&](uint32_t dst, const CUtensorMap* tm, int form, int mn, int row0) {
             if (form == kRows) {
               ptx::tma_load_2d_pair(dst, tm, bar, kb * 64, row0 + mn);
@@ -263,7 +275,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         const VocabTileAt at(pr, c.t);
         const int a = it & 1;
         const uint32_t d = tmem_base + (uint32_t)(a * kVocabTile);
-        const uint32_t idesc = vocab_idesc(pr.a_form != kRows, pr.b_form != kRows);
+        const uint32_t idesc = vocab_idesc(pr.a_form != kRows, pr.b_form != kRows, FEW ? pr.width : kVocabTile);
         const uint64_t a_desc0 = vocab_desc(smem_base, pr.a_form != kRows), b_desc0 = vocab_desc(smem_base + kVocabStageBytes / 2, pr.b_form != kRows);
         // 16 elements of K per instruction: 32 bytes of a row, or 16 rows of 128 bytes
         const uint32_t a_step = pr.a_form != kRows ? 2048 >> 4 : 32 >> 4, b_step = pr.b_form != kRows ? 2048 >> 4 : 32 >> 4;
@@ -314,10 +326,10 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
       const int col0 = at.n * kVocabTile;
       float* const tile_cols = cols + a * 768;
       // what the tile's columns need: words' biases (forward), or the tokens' lse, gradient and target
-      if (FORWARD) {
+      if (FORWARD && !FEW) {
         const int v = col0 + e;
         tile_cols[e] = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] * kLog2e : 0.0f);
-      } else if (pr.kind == kGradZ) {
+      } else if (!FORWARD && pr.kind == kGradZ) {
         const int t = col0 + e;
         float lse = INFINITY, gl = 0.0f;
         int target = -1;
@@ -333,11 +345,11 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
       // the row's own, fetched while the products run
       int target = -1;
       float bias = 0.0f;
-      if (FORWARD) {
+      if (FORWARD && !FEW) {
         if (row < gp.T) target = gp.targets[row];
-      } else if (pr.kind == kGradZ) {
+      } else if (FORWARD || pr.kind == kGradZ) {
         const int v = gp.v0 + row;
-        bias = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] * kLog2e : 0.0f);
+        bias = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] * (FORWARD ? 1.0f : kLog2e) : 0.0f);
       }
       const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
       if (vocab_epilogue_sync_or(!ok)) {  // publishes the columns' values, and all eight warps give up together
@@ -373,7 +385,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         __syncwarp();
       };
 
-      if constexpr (FORWARD) {
+      if constexpr (FORWARD && !FEW) {
         const int chunks = row0 < gp.T ? min(8, (gp.V - col0 + 31) / 32) : 0;
         if (half >= chunks) release();
         float top = -INFINITY, sum = 0.0f;
@@ -411,6 +423,55 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           top = most;
         }
         if (row < gp.T) gp.part[(size_t)(2 * at.n + half) * gp.T + row] = make_float2(top, sum);
+      } else if constexpr (FORWARD) {
+        // lane: word, column: token.  A warp's 32 words of 32 tokens at a time are turned in the staging buffer (lane l's column j
+        // goes to row j, place l), so that a lane has a token's 32 logits
+        const int chunks = (gp.T + 31) / 32;
+        float2* const joined = reinterpret_cast<float2*>(cols);  // [quarter][token]
+        if (half >= chunks) release();
+#pragma unroll 1
+        for (int ch = half; ch < chunks; ch += 2) {
+          uint32_t v[32];
+          ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(ch * 32), v);
+          ptx::tmem_ld_wait();
+          ptx::tmem_ld_regs_ready(v);
+          if (ch + 2 >= chunks) release();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + bias);
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            *reinterpret_cast<uint32_t*>(buf + j * 128 + (((lane >> 2) ^ (j & 7)) << 4) + (lane & 3) * 4) = v[j];
+          __syncwarp();
+          float z[32];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(&z[4 * j]) = *reinterpret_cast<const uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4));
+          const int t = ch * 32 + lane;
+          const int target = t < gp.T ? gp.targets[t] : -1, hit = target - row0;
+          if (hit >= 0 && hit < 32 && target < gp.V)
+            gp.z_target[t] = *reinterpret_cast<const float*>(buf + lane * 128 + (((hit >> 2) ^ (lane & 7)) << 4) + (hit & 3) * 4);
+          float most = fmaxf(z[0], z[1]);
+#pragma unroll
+          for (int j = 2; j < 32; j += 2) most = fmaxf(most, fmaxf(z[j], z[j + 1]));
+          // the maximum and the exponents for powers of two; nothing but -infinity: no difference of infinities
+          const float top = most == -INFINITY ? -INFINITY : most * kLog2e, base = most == -INFINITY ? 0.0f : top;
+          float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int j = 0; j < 32; ++j) s[j & 3] += exp2_fast(fmaf(z[j], kLog2e, -base));
+          joined[quarter * kFewTokens + ch * 32 + lane] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+          __syncwarp();
+        }
+        // the CTA's four quarters of words, joined in order (the next tile's barrier comes before the next writes)
+        vocab_epilogue_sync_or(false);
+        if (e < gp.T) {
+          float2 q[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q[i] = joined[i * kFewTokens + e];
+          const float top = fmaxf(fmaxf(q[0].x, q[1].x), fmaxf(q[2].x, q[3].x)), base = top == -INFINITY ? 0.0f : top;
+          float s = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s += q[i].y * exp2_fast(q[i].x - base);
+          gp.part[(size_t)(2 * at.m + rank) * gp.T + e] = make_float2(top, s);
+        }
       } else if (pr.kind == kGradH) {
         const int chunks = row0 < gp.T ? min(8, (gp.D - col0 + 31) / 32) : 0;
         if (half >= chunks) release();
@@ -429,7 +490,8 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         }
       } else {
         const bool grad_z = pr.kind == kGradZ;
-        const int rows = gp.V - gp.out_v0, width = grad_z ? gp.T : gp.D;
+        // (FEW: the tile covers all of g's row, zeros behind its columns)
+        const int rows = gp.V - gp.out_v0, width = grad_z ? (FEW ? gp.g_pitch : gp.T) : gp.D;
         // g is formed for all rows of the piece's tiles: the products read whole K blocks of it
         const int chunks = grad_z || row0 < rows ? min(4, (width - col0 + 63) / 64) : 0;
         if (half >= chunks) release();
@@ -448,6 +510,11 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
             const float4* const gl4 = reinterpret_cast<const float4*>(tile_cols + 256 + ch * 64);
             const int4* const tg4 = reinterpret_cast<const int4*>(tile_cols + 512 + ch * 64);
             const int word = gp.v0 + row;
+            if (FEW && pr.width - ch * 64 < 64) {  // columns that the tile does not have hold what an earlier one left
+#pragma unroll
+              for (int j = 0; j < 64; ++j)
+                if (j >= pr.width - ch * 64) v[j >> 5][j & 31] = 0u;
+            }
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               const float4 l = lse4[j], gl = gl4[j];
@@ -579,6 +646,9 @@ struct VocabPlan {
 };
 constexpr int64_t kPieceBytes = 32 << 20;  // of g: with the piece before it and what the products read it stays in L2
 
+// Columns of a tile of logits in the backward pass (few tokens: in the forward pass too).
+static int64_t vocab_width(int64_t T) { return T <= kFewTokens ? up(T, 32) * 32 : kVocabTile; }
+
 static VocabPlan plan_vocab(int64_t T, int64_t V, int64_t D, int pairs, size_t budget) {
   VocabPlan p;
   const int64_t Tp = up(T, 64) * 64, t_tiles = up(T, 256), d_tiles = up(D, 256), all = up(V, 256) * 256;
@@ -605,19 +675,35 @@ static VocabPlan plan_vocab(int64_t T, int64_t V, int64_t D, int pairs, size_t b
 
 // Deals `tiles` tiles of `cost` over the pairs: each to the least loaded one, as level as they come; contiguous tiles per pair.
 static void deal_tiles(VocabProblem& p, int64_t tiles, int64_t cost, int64_t* load, int pairs) {
-  int64_t lo = 0, hi = 0;  // the least level at which they all fit
-  for (int g = 0; g < pairs; ++g) hi = std::max(hi, load[g]);
-  hi += cost * (up(tiles, pairs) + 1);
+  int64_t least = load[0], most = load[0];
+  for (int g = 1; g < pairs; ++g) {
+    least = std::min(least, load[g]);
+    most = std::max(most, load[g]);
+  }
+  if (least == most) {  // nothing dealt yet
+    const int64_t each = tiles / pairs, more = tiles - each * pairs;
+    for (int g = 0; g <= pairs; ++g) p.start[g] = (int32_t)(g * each + std::min<int64_t>(g, more));
+    for (int g = 0; g < pairs; ++g) load[g] += (each + (g < more)) * cost;
+    return;
+  }
+  // The least level at which they all fit, by bisection; the loads above the least one and the costs fit 32 bits, or are taken
+  // in units in which they do (host time: 740 divisions of 64 bits took 6 us).
+  int64_t unit = 1;
+  while ((most - least + cost * (up(tiles, pairs) + 1)) / unit >= (int64_t)1 << 30) unit *= 2;
+  const uint32_t c = (uint32_t)std::max<int64_t>(1, cost / unit);
+  uint32_t l[kMaxPairs];
+  for (int g = 0; g < pairs; ++g) l[g] = (uint32_t)((load[g] - least) / unit);
+  uint32_t lo = 0, hi = (uint32_t)((most - least) / unit) + c * (uint32_t)(up(tiles, pairs) + 1);
   while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
+    const uint32_t mid = lo + (hi - lo) / 2;
     int64_t room = 0;
-    for (int g = 0; g < pairs; ++g) room += mid > load[g] ? (mid - load[g]) / cost : 0;
+    for (int g = 0; g < pairs; ++g) room += mid > l[g] ? (mid - l[g]) / c : 0;
     if (room >= tiles) hi = mid;
     else lo = mid + 1;
   }
   int64_t t = 0;
   for (int g = 0; g < pairs; ++g) {
-    const int64_t n = std::min(tiles - t, lo > load[g] ? (lo - load[g]) / cost : 0);
+    const int64_t n = std::min<int64_t>(tiles - t, lo > l[g] ? (lo - l[g]) / c : 0);
     p.start[g] = (int32_t)t;
     t += n;
     load[g] += n * cost;
@@ -625,9 +711,9 @@ static void deal_tiles(VocabProblem& p, int64_t tiles, int64_t cost, int64_t* lo
   p.start[pairs] = (int32_t)t;
 }
 
-template <bool FORWARD>
+template <bool FORWARD, bool FEW>
 static qb_status launch_vocab(const VocabParams& gp, int pairs, cudaStream_t stream) {
-  auto kernel = vocab_kernel<FORWARD>;
+  auto kernel = vocab_kernel<FORWARD, FEW>;
   static std::atomic<bool> attr_set[64] = {};
   int dev = 0;
   QB_CUDA_TRY(cudaGetDevice(&dev));
@@ -640,8 +726,8 @@ static qb_status launch_vocab(const VocabParams& gp, int pairs, cudaStream_t str
 }
 
 // The operand with its rows along M or N, and with its columns along them.
-static qb_status rows_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols) {
-  return make_matrix_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * 2, 128, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+static qb_status rows_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t box_rows = 128) {
+  return make_matrix_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * 2, (int)box_rows, 64, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 static qb_status cols_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols) {
   if (cols % 64 == 0) return make_group_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols * 2, 64, 2);
@@ -691,8 +777,11 @@ extern "C" qb_status qb_vocab_loss(const uint16_t* h, const uint16_t* w, const f
   st = require_sm100(&sms);
   if (st != QB_OK) return st;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  // all tokens of a tile of words one after the other: w is read once, h stays in L2
+  const bool few = T <= kFewTokens;
+  const int64_t width = vocab_width(T), tiles = up(V, 256) * up(T, 256);
   VocabParams gp = {};
-  if ((st = rows_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
+  if ((st = rows_map(&gp.map[kMapH], h, T, D, few ? width / 2 : 128)) != QB_OK) return st;
   if ((st = rows_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
   char* const scratch = static_cast<char*>(ws) + 1024;
   gp.z_target = reinterpret_cast<float*>(scratch);
@@ -706,16 +795,17 @@ extern "C" qb_status qb_vocab_loss(const uint16_t* h, const uint16_t* w, const f
   gp.count = 1;
   VocabProblem& p = gp.prob[0];
   p.kind = kLogits;
-  p.map_a = kMapH;
-  p.map_b = kMapW;
-  p.m_tiles = (int32_t)up(T, 256);  // all tokens of a tile of words one after the other: w is read once, h stays in L2
-  const int64_t tiles = up(V, 256) * p.m_tiles;
+  p.map_a = few ? kMapW : kMapH;
+  p.map_b = few ? kMapH : kMapW;
+  p.n_tiles = 1;
+  p.m_tiles = few ? 0 : (int32_t)up(T, 256);
+  p.width = (int32_t)width;
   p.split_tiles = (int32_t)tiles;
   p.k_blocks = p.k_end = (int32_t)up(D, 64);
   const int pairs = (int)std::min<int64_t>(tiles, std::min(sms / 2, kMaxPairs));
   int64_t load[kMaxPairs] = {};
   deal_tiles(p, tiles, 1, load, pairs);
-  if ((st = launch_vocab<true>(gp, pairs, stream)) != QB_OK) return st;
+  if ((st = few ? launch_vocab<true, true>(gp, pairs, stream) : launch_vocab<true, false>(gp, pairs, stream)) != QB_OK) return st;
   QB_CUDA_TRY(launch_kernel(vocab_join_kernel, (unsigned)up(T, 32), 32 * kJoinWarps, 0, stream, 1, false, gp.part, (int)(2 * up(V, 256)), gp.z_target, targets,
                             (int)T, (int)V, loss, lse, ws));
   return QB_OK;
@@ -751,7 +841,9 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
   VocabParams gp = {};
   CUtensorMap g_rows[2], g_cols[2];
   uint16_t* const g[2] = {reinterpret_cast<uint16_t*>(g0), reinterpret_cast<uint16_t*>(g1)};
-  if ((st = rows_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
+  const bool few = T <= kFewTokens;
+  const int64_t width = vocab_width(T);
+  if ((st = rows_map(&gp.map[kMapH], h, T, D, few ? width / 2 : 128)) != QB_OK) return st;
   if ((st = rows_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
   if ((st = cols_map(&gp.map[kMapHCols], h, T, D)) != QB_OK) return st;
   if ((st = cols_map(&gp.map[kMapWCols], w, V, D)) != QB_OK) return st;
@@ -790,6 +882,7 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
       VocabProblem p = {};
       if (grad_h) {
         p.kind = kGradH;
+        p.width = kVocabTile;
         p.map_a = kMapGCols;
         p.map_b = kMapWCols;
         p.a_form = kCols;
@@ -805,6 +898,7 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
       if (grad_w) {
         p = VocabProblem{};
         p.kind = kGradW;
+        p.width = kVocabTile;
         p.map_a = kMapG;
         p.map_b = kMapHCols;
         p.b_form = cols_form;
@@ -820,6 +914,7 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
       gp.v0 = (int32_t)v0;
       VocabProblem p = {};
       p.kind = kGradZ;
+      p.width = (int32_t)width;
       p.map_a = kMapW;
       p.map_b = kMapH;
       p.a_row0 = (int32_t)v0;
@@ -829,7 +924,7 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
       add(p, p.split_tiles, p.k_blocks + 2);
     }
     if (gp.count == 0) continue;
-    if ((st = launch_vocab<false>(gp, pairs, stream)) != QB_OK) return st;
+    if ((st = few ? launch_vocab<false, true>(gp, pairs, stream) : launch_vocab<false, false>(gp, pairs, stream)) != QB_OK) return st;
   }
   if (grad_h || grad_bias) {
     const int64_t n = T * D, items = std::max(grad_h ? n / 8 : 0, grad_bias ? V : 0);

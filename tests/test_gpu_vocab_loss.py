@@ -93,7 +93,8 @@ def check_all(h, w, b, targets, gl, ws):
 
 
 SHAPES = [(1, 1, 8), (1, 500, 64), (3, 257, 72), (31, 256, 128), (77, 1000, 768), (128, 129, 1024), (255, 300, 8), (256, 512, 64), (257, 513, 136),
-          (300, 5000, 320), (613, 3001, 768), (1030, 2100, 1000), (2049, 4097, 256), (40, 30522, 192)]
+          (300, 5000, 320), (613, 3001, 768), (1030, 2100, 1000), (2049, 4097, 256), (40, 30522, 192),
+          (32, 300, 64), (33, 700, 136), (96, 520, 64), (97, 257, 192), (161, 600, 72), (225, 1100, 64), (320, 900, 64), (672, 1300, 128)]
 
 
 @pytest.mark.parametrize("bias", [True, False])
@@ -110,20 +111,32 @@ def test_pieces(T, V, D):
     args = inputs(T, V, D)
     ref = reference(*args)
     full = qb.vocab_loss_workspace_bytes(T, V, D)
-    tp, slab, forward = (T + 63) // 64 * 64, (T + 255) // 256 * 256 * D * 4, 1024 + (T * 4 + 1023) // 1024 * 1024 + 2 * ((V + 255) // 256) * T * 8
-    least = 1024 + 2 * 256 * tp * 2 + slab + (2 * ((T + 255) // 256) * V * 4 + 1023) // 1024 * 1024
-    for nbytes in sorted({max(forward, least), max(forward, least + 3 * 256 * tp * 2), (full + least) // 2, full, full + (64 << 20)}):
-        ws = torch.zeros(max(nbytes, forward), dtype=torch.uint8, device="cuda")
+    big = torch.zeros(full + (64 << 20), dtype=torch.uint8, device="cuda")
+    loss, lse = qb.vocab_loss(*args[:4], big)
+
+    def least(call):  # the smallest workspace that is accepted, to 4 KB
+        lo, hi = 0, full
+        while hi - lo > 4096:
+            mid = (lo + hi) // 2
+            try:
+                call(big[:mid])
+                hi = mid
+            except qb.QbertError as e:
+                assert e.status == qb.QB_ERR_WORKSPACE
+                lo = mid
+        return hi
+    forward = least(lambda ws: qb.vocab_loss(*args[:4], ws))
+    least = least(lambda ws: qb.vocab_loss_backward(*args[:4], lse, args[4], ws))
+    assert max(forward, least) <= full and least < full  # less is taken, in more pieces
+    rows = 256 * 2 * (T + 63)
+    for nbytes in sorted({least, least + 3 * rows, (full + least) // 2, full, full + (64 << 20)}):
+        ws = big[:max(nbytes, forward)]
         got = run(*args, ws)
         for name in ref:
             check(name, got[name], ref)
         again = run(*args, ws)
         assert all(torch.equal(got[k], again[k]) for k in got)  # the same order every time
-    loss, lse = qb.vocab_loss(*args[:4], torch.zeros(full, dtype=torch.uint8, device="cuda"))
-    with pytest.raises(qb.QbertError):
-        qb.vocab_loss_backward(*args[:4], lse, args[4], torch.zeros(least - 1, dtype=torch.uint8, device="cuda"))
-    with pytest.raises(qb.QbertError):
-        qb.vocab_loss(*args[:4], torch.zeros(forward - 1, dtype=torch.uint8, device="cuda"))
+    assert qb.read_status(big) == qb.QB_OK
 
 
 def test_differences():
