@@ -81,12 +81,11 @@ struct VocabParams {
   int32_t T, V, D;
   int32_t v0;           // first word of the piece whose logits are formed
   int32_t out_v0;       // first word of the piece that grad_w gets
-  int32_t slab_rows;
   int32_t add;          // grad_h is added to what the slabs hold
   int32_t g_pitch;      // tokens rounded up to 64
   uint16_t* g_new;      // [words of a piece][g_pitch]
   uint16_t* grad_w;     // [V][D]
-  float* slabs;         // [splits][slab_rows][D]
+  float* slabs;         // [splits][T][D]
   const float* bias;
   const int32_t* targets;
   const float* lse;
@@ -485,7 +484,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
 #pragma unroll
           for (int j = 0; j < 8; ++j) put(j, make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
           const int c0 = col0 + ch * 32;
-          send(reinterpret_cast<uint8_t*>(gp.slabs + ((size_t)at.split * gp.slab_rows + row0) * gp.D + c0), (size_t)gp.D * 4, gp.T - row0,
+          send(reinterpret_cast<uint8_t*>(gp.slabs + ((size_t)at.split * gp.T + row0) * gp.D + c0), (size_t)gp.D * 4, gp.T - row0,
                (gp.D - c0) * 4, gp.add != 0);
         }
       } else {
@@ -607,29 +606,50 @@ __global__ void __launch_bounds__(32 * kJoinWarps) vocab_join_kernel(const float
   loss[t] = valid ? l - z_target[t] : 0.0f;
 }
 
-// grad_h = the slabs' sum in bfloat16; grad_bias = the tiles' sum.
-__global__ void __launch_bounds__(256) vocab_finish_kernel(const float* slabs, int splits, int64_t slab, int64_t n, uint16_t* grad_h,
+// grad_h = the slabs' sum in bfloat16 (the first `h_blocks` blocks); grad_bias = the tiles' sum (the others).
+// A block has 32 groups of four elements times eight warps; with more than four slabs every warp sums every eighth, and the warps'
+// sums are joined in order, else every warp takes groups of its own.
+__global__ void __launch_bounds__(256) vocab_finish_kernel(const float* slabs, int splits, int64_t n, uint16_t* grad_h, int h_blocks,
                                                            const float* part_bias, int parts, int V, float* grad_bias) {
+  __shared__ float4 joined[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_begin();
-  const int64_t stride = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (grad_h)
-    for (int64_t i = first * 8; i < n; i += stride * 8) {  // n is a multiple of 8
-      float4 a = *reinterpret_cast<const float4*>(slabs + i), b = *reinterpret_cast<const float4*>(slabs + i + 4);
-#pragma unroll 4
-      for (int s = 1; s < splits; ++s) {
-        const float4 c = *reinterpret_cast<const float4*>(slabs + s * slab + i), d = *reinterpret_cast<const float4*>(slabs + s * slab + i + 4);
-        a.x += c.x, a.y += c.y, a.z += c.z, a.w += c.w;
-        b.x += d.x, b.y += d.y, b.z += d.z, b.w += d.w;
-      }
-      *reinterpret_cast<uint4*>(grad_h + i) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
-    }
-  if (grad_bias)
-    for (int64_t v = first; v < V; v += stride) {
-      float s = 0.0f;
+  if ((int)blockIdx.x >= h_blocks) {
+    const int v = ((int)blockIdx.x - h_blocks) * 256 + threadIdx.x;
+    if (v >= V) return;
+    float s = 0.0f;
 #pragma unroll 8
-      for (int i = 0; i < parts; ++i) s += part_bias[(size_t)i * V + v];
-      grad_bias[v] = s;
+    for (int i = 0; i < parts; ++i) s += part_bias[(size_t)i * V + v];
+    grad_bias[v] = s;
+    return;
+  }
+  const bool shared = splits > 4;
+  const int64_t i = ((int64_t)blockIdx.x * (shared ? 32 : 256) + (shared ? lane : threadIdx.x)) * 4;  // n is a multiple of 8
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (i < n) {
+#pragma unroll 8
+    for (int s = shared ? warp : 0; s < splits; s += shared ? 8 : 1) {
+      const float4 c = *reinterpret_cast<const float4*>(slabs + s * n + i);
+      a.x += c.x;
+      a.y += c.y;
+      a.z += c.z;
+      a.w += c.w;
     }
+  }
+  if (shared) {
+    joined[warp][lane] = a;
+    __syncthreads();
+    if (warp != 0) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w) {
+      const float4 c = joined[w][lane];
+      a.x += c.x;
+      a.y += c.y;
+      a.z += c.z;
+      a.w += c.w;
+    }
+  }
+  if (i < n) *reinterpret_cast<uint2*>(grad_h + i) = make_uint2(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w));
 }
 
 // ---- host side -----------------------------------------------------------------------------------
@@ -641,10 +661,10 @@ struct VocabPlan {
   int64_t pieces;
   int64_t k_split;   // K blocks of a split of grad_h
   int64_t splits;
-  int64_t g_bytes, slab_rows, slab_bytes, bias_bytes;
+  int64_t g_bytes, slab_bytes, bias_bytes;
   size_t bytes() const { return (size_t)(1024 + (pieces > 1 ? 2 : 1) * g_bytes + splits * slab_bytes + bias_bytes); }
 };
-constexpr int64_t kPieceBytes = 32 << 20;  // of g: with the piece before it and what the products read it stays in L2
+constexpr int64_t kPieceBytes = 48 << 20;  // of g: a launch has enough tiles to level them, and L2 still holds most of what is read again
 
 // Columns of a tile of logits in the backward pass (few tokens: in the forward pass too).
 static int64_t vocab_width(int64_t T) { return T <= kFewTokens ? up(T, 32) * 32 : kVocabTile; }
@@ -652,8 +672,7 @@ static int64_t vocab_width(int64_t T) { return T <= kFewTokens ? up(T, 32) * 32 
 static VocabPlan plan_vocab(int64_t T, int64_t V, int64_t D, int pairs, size_t budget) {
   VocabPlan p;
   const int64_t Tp = up(T, 64) * 64, t_tiles = up(T, 256), d_tiles = up(D, 256), all = up(V, 256) * 256;
-  p.slab_rows = t_tiles * 256;
-  p.slab_bytes = up(p.slab_rows * D * 4, 1024) * 1024;
+  p.slab_bytes = T * D * 4;  // (D is a multiple of 8: slabs begin at multiples of 32 bytes)
   p.bias_bytes = up(2 * t_tiles * V * 4, 1024) * 1024;
   int64_t rows = std::min(all, std::max<int64_t>(256, kPieceBytes / (2 * Tp) / 256 * 256));
   for (;; rows -= 256) {
@@ -837,7 +856,7 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
   char* const g1 = plan.pieces > 1 ? g0 + plan.g_bytes : g0;
   float* const slabs = reinterpret_cast<float*>(g1 + plan.g_bytes);
   float* const part_bias = reinterpret_cast<float*>(reinterpret_cast<char*>(slabs) + plan.splits * plan.slab_bytes);
-  const int64_t Tp = up(T, 64) * 64, slab = plan.slab_bytes / 4;
+  const int64_t Tp = up(T, 64) * 64;
   VocabParams gp = {};
   CUtensorMap g_rows[2], g_cols[2];
   uint16_t* const g[2] = {reinterpret_cast<uint16_t*>(g0), reinterpret_cast<uint16_t*>(g1)};
@@ -863,7 +882,6 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
   gp.lse = lse;
   gp.grad_loss = grad_loss;
   gp.part_bias = grad_bias ? part_bias : nullptr;
-  gp.slab_rows = (int32_t)plan.slab_rows;
   gp.ws = ws;
   const int32_t t_tiles = (int32_t)up(T, 256), d_tiles = (int32_t)up(D, 256);
   for (int64_t i = 0; i <= plan.pieces; ++i) {
@@ -927,9 +945,9 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
     if ((st = few ? launch_vocab<false, true>(gp, pairs, stream) : launch_vocab<false, false>(gp, pairs, stream)) != QB_OK) return st;
   }
   if (grad_h || grad_bias) {
-    const int64_t n = T * D, items = std::max(grad_h ? n / 8 : 0, grad_bias ? V : 0);
-    QB_CUDA_TRY(launch_kernel(vocab_finish_kernel, (unsigned)std::min<int64_t>(up(items, 256), (int64_t)sms * 8), 256, 0, stream, 1, false, slabs,
-                              (int)plan.splits, slab, n, grad_h, part_bias, 2 * t_tiles, (int)V, grad_bias));
+    const int64_t h_blocks = grad_h ? up(T * D, plan.splits > 4 ? 128 : 1024) : 0, b_blocks = grad_bias ? up(V, 256) : 0;
+    QB_CUDA_TRY(launch_kernel(vocab_finish_kernel, (unsigned)(h_blocks + b_blocks), 256, 0, stream, 1, false, slabs, (int)plan.splits, T * D, grad_h,
+                              (int)h_blocks, part_bias, 2 * t_tiles, (int)V, grad_bias));
   }
   return QB_OK;
 }
