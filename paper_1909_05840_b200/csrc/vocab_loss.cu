@@ -12,7 +12,7 @@
 // same); a last kernel rounds it and sums the bias's gradient, whose terms never were bfloat16.
 //
 // One product kernel for all of it: CTA pairs (tcgen05 cta_group::2, kind::f16, bfloat16 operands, fp32 accumulators), tiles of
-// 256 x 256, K blocks of 64, a ring of five stages of 32 KB per CTA, two accumulators in tensor memory.  An operand lies in
+// 256 x 256, K blocks of 64, a ring of three stages of two blocks (64 KB per CTA), two accumulators in tensor memory.  An operand lies in
 // shared memory as the tensor has it: contraction along its rows (K-major) or down its columns (MN-major),
 // so that nothing is transposed in memory.  12 warps: 0 loads (TMA), 1 issues MMAs,
 // 4..11 epilogue, two per TMEM lane quarter.  Every wait is bounded, as in qb_gemm.
@@ -33,9 +33,9 @@ namespace qb {
 constexpr int kVocabTile = 256;
 constexpr int kVocabEpilogueWarps = 8;
 constexpr int kVocabThreads = 32 * (4 + kVocabEpilogueWarps);
-constexpr int kVocabStages = 5;
-constexpr int kVocabStageBytes = 32768;  // 128 rows of A and 128 of B, 64 elements of K each
-constexpr int kVocabOutBytes = kVocabEpilogueWarps * 4096;
+constexpr int kVocabStages = 3;
+constexpr int kVocabStageBytes = 65536;  // 128 rows of A and 128 of B, two K blocks of 64 each
+constexpr int kVocabOutBytes = kVocabEpilogueWarps * 2048;
 constexpr int kVocabBarBytes = 256;
 // Backward: per accumulator three values of each of the tile's columns.  Forward with few tokens: a maximum and a sum per lane
 // quarter and token.
@@ -46,10 +46,11 @@ constexpr int kVocabSmemBytes = kVocabStages * kVocabStageBytes + kVocabOutBytes
 constexpr int kMaxPairs = 80;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// How an operand lies and is loaded: K-major, one box of 128 rows x 64; MN-major, one box of 64 rows x 2 groups of 64 columns, or
-// (rows that are no multiple of 128 bytes) two boxes of 64 rows x 64 columns.  A box costs the TMA unit about 100 ns here whether it
-// holds 8 KB or 16: with two boxes per operand everywhere, 4,096 x 30,522 x 768 forward took 165 us instead of 121.
-enum VocabForm { kRows = 0, kCols = 1, kCols2 = 2 };
+// How an operand lies and is loaded, two K blocks of 64 at a time: K-major (128 rows x 2 groups of 64 columns) or MN-major (128 rows x
+// 2 groups of 64 columns, the rows along K); one box of three dimensions, or, where rows are no multiple of 128 bytes, two boxes
+// of one group.  A box costs the TMA unit about 100 ns whatever it holds: with boxes of 8 KB 4,096 x 30,522 x 768 forward took 165 us, of
+// 16 KB 129, of 32 KB 119.
+enum VocabForm { kRows = 0, kRows2 = 1, kCols = 2, kCols2 = 3 };
 enum VocabKind { kLogits = 0, kGradZ = 1, kGradW = 2, kGradH = 3 };
 // FEW: up to kFewTokens tokens.  They are then the columns of the tiles of logits in the forward pass too, and the tiles are as wide
 // as the tokens (rounded up to 32): a pair loads 256 words and those tokens, not 256 rows of mostly nothing (77 tokens, 30,522
@@ -61,7 +62,7 @@ enum VocabKind { kLogits = 0, kGradZ = 1, kGradW = 2, kGradH = 3 };
 struct VocabProblem {
   int32_t kind;
   int32_t map_a, map_b;    // tensor maps of the operands
-  int32_t a_form, b_form;  // kRows, kCols or kCols2
+  int32_t a_form, b_form;
   int32_t n_tiles;         // tile t of a split: row tile t / n_tiles, column tile t % n_tiles
   int32_t width;           // columns of a tile (FEW, logits; else 256)
   int32_t m_tiles;         // not 0: column tile t / m_tiles, row tile t % m_tiles
@@ -72,10 +73,10 @@ struct VocabProblem {
   int32_t start[kMaxPairs + 1];  // pair g has tiles start[g] .. start[g + 1] - 1
 };
 
-enum { kMapH = 0, kMapW, kMapHCols, kMapWCols, kMapG, kMapGCols, kMaps };
+enum { kMapH = 0, kMapHTile, kMapW, kMapG, kMaps };
 
 struct VocabParams {
-  CUtensorMap map[kMaps];  // h, w, and g of the piece before, as rows and as columns
+  CUtensorMap map[kMaps];  // h, h with boxes of a narrower column tile's rows, w, g of the piece before
   VocabProblem prob[3];
   int32_t count;
   int32_t T, V, D;
@@ -96,11 +97,11 @@ struct VocabParams {
   void* ws;
 };
 
-// Operand of 128 rows (or columns) x 64 elements of K, 128-byte swizzle.  K-major: 1024 bytes between groups of eight rows.
-// MN-major: 64 consecutive elements of M or N are a row of 128 bytes, the next 64 are 8192 bytes on (leading offset), the next
+// Operand of 128 rows (or columns) x 128 elements of K, 128-byte swizzle.  K-major: 1024 bytes between groups of eight rows.
+// MN-major: 64 consecutive elements of M or N are a row of 128 bytes, the next 64 are 16384 bytes on (leading offset), the next
 // eight of K 1024 bytes (stride offset).  Version 1, SWIZZLE_128B as in qb_gemm.
 __device__ __forceinline__ uint64_t vocab_desc(uint32_t smem_addr, int mn) {
-  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)(mn ? 8192 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)(mn ? 16384 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
          (uint64_t)2 << 61;
 }
 // Instruction descriptor for kind::f16: D fp32 (bits 4-5 = 1), A and B bfloat16 (7-9, 10-12 = 1), MN-major A and B (15, 16),
@@ -228,10 +229,10 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         const VocabTileAt at(pr, c.t);
         const int width = FEW ? pr.width : kVocabTile;
         const int a_row = at.m * kVocabTile + (int)rank * 128, b_row = at.n * kVocabTile + (int)rank * (width / 2);
-        const uint32_t bytes = kVocabStageBytes + 2 * (width / 2 * 128);
+        const uint32_t bytes = kVocabStageBytes + 2 * (width * 128);
         const CUtensorMap* const ma = &gp.map[pr.map_a];
         const CUtensorMap* const mb = &gp.map[pr.map_b];
-        for (int kb = at.k0; kb < at.k1; ++kb) {
+        for (int kb = at.k0; kb < at.k1; kb += 2) {
           if (!wait_barrier_relaxed(empty(stage), phase ^ 1u, abort_flag)) {
             timed_out = true;
             where = (0 << 16) | stage;
@@ -239,18 +240,21 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           }
           const uint32_t a_smem = smem_base + stage * kVocabStageBytes, b_smem = a_smem + kVocabStageBytes / 2, bar = lead(full(stage));
           if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), bytes);
-          auto load = [&](uint32_t dst, const CUtensorMap* tm, int form, int mn, int row0) {
+          auto load = [&](uint32_t dst, const CUtensorMap* tm, int form, int mn, int row0, int rows) {
             if (form == kRows) {
-              ptx::tma_load_2d_pair(dst, tm, bar, kb * 64, row0 + mn);
+              ptx::tma_load_3d_pair(dst, tm, bar, 0, row0 + mn, kb);
             } else if (form == kCols) {
               ptx::tma_load_3d_pair(dst, tm, bar, 0, row0 + kb * 64, mn / 64);
+            } else if (form == kRows2) {
+              ptx::tma_load_2d_pair(dst, tm, bar, kb * 64, row0 + mn);
+              ptx::tma_load_2d_pair(dst + rows * 128, tm, bar, kb * 64 + 64, row0 + mn);
             } else {
               ptx::tma_load_2d_pair(dst, tm, bar, mn, row0 + kb * 64);
-              ptx::tma_load_2d_pair(dst + 8192, tm, bar, mn + 64, row0 + kb * 64);
+              ptx::tma_load_2d_pair(dst + 16384, tm, bar, mn + 64, row0 + kb * 64);
             }
           };
-          load(a_smem, ma, pr.a_form, a_row, pr.a_row0);
-          load(b_smem, mb, pr.b_form, b_row, pr.b_row0);
+          load(a_smem, ma, pr.a_form, a_row, pr.a_row0, 128);
+          load(b_smem, mb, pr.b_form, b_row, pr.b_row0, width / 2);
           if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
@@ -274,16 +278,19 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         const VocabTileAt at(pr, c.t);
         const int a = it & 1;
         const uint32_t d = tmem_base + (uint32_t)(a * kVocabTile);
-        const uint32_t idesc = vocab_idesc(pr.a_form != kRows, pr.b_form != kRows, FEW ? pr.width : kVocabTile);
-        const uint64_t a_desc0 = vocab_desc(smem_base, pr.a_form != kRows), b_desc0 = vocab_desc(smem_base + kVocabStageBytes / 2, pr.b_form != kRows);
+        const int width = FEW ? pr.width : kVocabTile;
+        const bool a_mn = pr.a_form >= kCols, b_mn = pr.b_form >= kCols;
+        const uint32_t idesc = vocab_idesc(a_mn, b_mn, width);
+        const uint64_t a_desc0 = vocab_desc(smem_base, a_mn), b_desc0 = vocab_desc(smem_base + kVocabStageBytes / 2, b_mn);
         // 16 elements of K per instruction: 32 bytes of a row, or 16 rows of 128 bytes
-        const uint32_t a_step = pr.a_form != kRows ? 2048 >> 4 : 32 >> 4, b_step = pr.b_form != kRows ? 2048 >> 4 : 32 >> 4;
+        const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
+        const uint32_t a_next = a_mn ? 8192 >> 4 : 16384 >> 4, b_next = b_mn ? 8192 >> 4 : (uint32_t)(width / 2 * 128) >> 4;  // second K block
         if (!wait_barrier(acc_empty(a), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) {
           timed_out = true;
           where = (1 << 16) | 0x100 | a;
           break;
         }
-        for (int kb = at.k0; kb < at.k1; ++kb) {
+        for (int kb = at.k0; kb < at.k1; kb += 2) {
           if (!wait_barrier(full(stage), phase, abort_flag)) {
             timed_out = true;
             where = (1 << 16) | stage;
@@ -295,6 +302,11 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             ptx::mma_f16_ss_cg<2>(d, a_desc + (uint64_t)(a_step * j), b_desc + (uint64_t)(b_step * j), idesc, kb != at.k0 || j != 0 ? 1u : 0u);
+          if (kb + 1 < at.k1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              ptx::mma_f16_ss_cg<2>(d, a_desc + (uint64_t)(a_next + a_step * j), b_desc + (uint64_t)(b_next + b_step * j), idesc, 1u);
+          }
           ptx::mma_commit_cg<2>(empty(stage));
           if (++stage == kStages) {
             stage = 0;
@@ -313,7 +325,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
   } else if (warp >= 4) {
     // ---------------- epilogue ----------------------------------------------------------------------
     const int ew = warp - 4, quarter = warp & 3, half = ew >> 2, e = threadIdx.x - 128;
-    uint8_t* const buf = out_ptr + ew * 4096;
+    uint8_t* const buf = out_ptr + ew * 2048;
     const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
     int it = 0;
     VocabCursor c;
@@ -366,22 +378,25 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           else ptx::mbar_arrive(acc_empty(a));
         }
       };
-      // the 128 bytes of the lane's row in the warp's staging buffer (piece j of 16 bytes), and their way out: 16 bytes a lane,
-      // four whole lines a store
-      auto put = [&](int j, uint4 w) { *reinterpret_cast<uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = w; };
-      auto send = [&](uint8_t* to, size_t pitch, int rows, int bytes, bool add) {  // rows and bytes of a row that exist
+      // 64 bytes of the lane's row (four pieces of 16) into the warp's staging buffer, and 32 such rows out of it: 16 bytes a lane,
+      // eight rows a store.  The swizzle keeps eight lanes on different banks either way.
+      auto staged = [&](int r, int piece) { return reinterpret_cast<uint4*>(buf + r * 64 + ((piece ^ ((r >> 1) & 3)) << 4)); };
+      auto send = [&](const uint4 (&w)[4], uint8_t* to, size_t pitch, int rows, int bytes, bool add) {  // rows, bytes of a row that exist
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = 4 * i + (lane >> 3), piece = lane & 7;
-          const uint4 w = *reinterpret_cast<const uint4*>(buf + r * 128 + ((piece ^ (r & 7)) << 4));
+        for (int j = 0; j < 4; ++j) *staged(lane, j) = w[j];
+        __syncwarp();
+        const int piece = lane & 3;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 8 * i + (lane >> 2);
+          const uint4 v = *staged(r, piece);
           if (r < rows && piece * 16 < bytes) {
             uint8_t* const p = to + (size_t)r * pitch + piece * 16;
-            if (add) ptx::red_add_v4(p, w);
-            else *reinterpret_cast<uint4*>(p) = w;
+            if (add) ptx::red_add_v4(p, v);
+            else *reinterpret_cast<uint4*>(p) = v;
           }
         }
-        __syncwarp();
       };
 
       if constexpr (FORWARD && !FEW) {
@@ -437,17 +452,24 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           if (ch + 2 >= chunks) release();
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + bias);
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            *reinterpret_cast<uint32_t*>(buf + j * 128 + (((lane >> 2) ^ (j & 7)) << 4) + (lane & 3) * 4) = v[j];
-          __syncwarp();
-          float z[32];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(&z[4 * j]) = *reinterpret_cast<const uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4));
           const int t = ch * 32 + lane;
           const int target = t < gp.T ? gp.targets[t] : -1, hit = target - row0;
-          if (hit >= 0 && hit < 32 && target < gp.V)
-            gp.z_target[t] = *reinterpret_cast<const float*>(buf + lane * 128 + (((hit >> 2) ^ (lane & 7)) << 4) + (hit & 3) * 4);
+          float z[32];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {  // 16 tokens at a time: rows of 128 bytes
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              *reinterpret_cast<uint32_t*>(buf + j * 128 + (((lane >> 2) ^ (j & 7)) << 4) + (lane & 3) * 4) = v[16 * h + j];
+            __syncwarp();
+            if ((lane >> 4) == h) {
+              const uint8_t* const from = buf + (lane & 15) * 128;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(&z[4 * j]) = *reinterpret_cast<const uint4*>(from + ((j ^ (lane & 7)) << 4));
+              if (hit >= 0 && hit < 32 && target < gp.V)
+                gp.z_target[t] = *reinterpret_cast<const float*>(from + (((hit >> 2) ^ (lane & 7)) << 4) + (hit & 3) * 4);
+            }
+            __syncwarp();
+          }
           float most = fmaxf(z[0], z[1]);
 #pragma unroll
           for (int j = 2; j < 32; j += 2) most = fmaxf(most, fmaxf(z[j], z[j + 1]));
@@ -481,11 +503,15 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           ptx::tmem_ld_wait();
           ptx::tmem_ld_regs_ready(v);
           if (ch + 2 >= chunks) release();
-#pragma unroll
-          for (int j = 0; j < 8; ++j) put(j, make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
           const int c0 = col0 + ch * 32;
-          send(reinterpret_cast<uint8_t*>(gp.slabs + ((size_t)at.split * gp.T + row0) * gp.D + c0), (size_t)gp.D * 4, gp.T - row0,
-               (gp.D - c0) * 4, gp.add != 0);
+          uint8_t* const to = reinterpret_cast<uint8_t*>(gp.slabs + ((size_t)at.split * gp.T + row0) * gp.D + c0);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint4 w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = make_uint4(v[16 * h + 4 * j], v[16 * h + 4 * j + 1], v[16 * h + 4 * j + 2], v[16 * h + 4 * j + 3]);
+            send(w, to + 64 * h, (size_t)gp.D * 4, gp.T - row0, (gp.D - c0) * 4 - 64 * h, gp.add != 0);
+          }
         }
       } else {
         const bool grad_z = pr.kind == kGradZ;
@@ -531,17 +557,21 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
               x[3] = one(x[3], l.w, gl.w, tg.w);
             }
           }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const uint32_t* const x = &v[j >> 2][(j & 3) * 8];
-            const auto f = [&](int i) { return __uint_as_float(x[i]); };
-            put(j, make_uint4(pack_bf16(f(0), f(1)), pack_bf16(f(2), f(3)), pack_bf16(f(4), f(5)), pack_bf16(f(6), f(7))));
-          }
           const int c0 = col0 + ch * 64;
-          if (grad_z)  // whole K blocks: the rows and columns behind the last word and token too
-            send(reinterpret_cast<uint8_t*>(gp.g_new + (size_t)row0 * gp.g_pitch + c0), (size_t)gp.g_pitch * 2, 32, 128, false);
-          else
-            send(reinterpret_cast<uint8_t*>(gp.grad_w + (size_t)(gp.out_v0 + row0) * gp.D + c0), (size_t)gp.D * 2, rows - row0, (gp.D - c0) * 2, false);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint4 w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const auto f = [&](int i) { return __uint_as_float(v[h][8 * j + i]); };
+              w[j] = make_uint4(pack_bf16(f(0), f(1)), pack_bf16(f(2), f(3)), pack_bf16(f(4), f(5)), pack_bf16(f(6), f(7)));
+            }
+            if (grad_z)  // whole K blocks: the rows and columns behind the last word and token too
+              send(w, reinterpret_cast<uint8_t*>(gp.g_new + (size_t)row0 * gp.g_pitch + c0 + 32 * h), (size_t)gp.g_pitch * 2, 32, 64, false);
+            else
+              send(w, reinterpret_cast<uint8_t*>(gp.grad_w + (size_t)(gp.out_v0 + row0) * gp.D + c0 + 32 * h), (size_t)gp.D * 2, rows - row0,
+                   (gp.D - c0) * 2 - 64 * h, false);
+          }
         }
         if (grad_z && gp.part_bias && gp.v0 + row < gp.V) gp.part_bias[(size_t)(2 * at.n + half) * gp.V + gp.v0 + row] = bias_grad;
       }
@@ -686,7 +716,7 @@ static VocabPlan plan_vocab(int64_t T, int64_t V, int64_t D, int pairs, size_t b
     const int64_t work = t_tiles * d_tiles * blocks + v_tiles * d_tiles * (Tp / 64) + (p.pieces > 1 ? v_tiles * t_tiles * up(D, 64) : 0);
     p.k_split = std::min(blocks, std::max<int64_t>(16, work / pairs / 2));
     p.splits = up(blocks, p.k_split);
-    p.k_split = up(blocks, p.splits);
+    p.k_split = up(up(blocks, p.splits), 2) * 2;
     p.splits = up(blocks, p.k_split);
     if (p.bytes() <= budget || rows <= 256) return p;
   }
@@ -745,12 +775,11 @@ static qb_status launch_vocab(const VocabParams& gp, int pairs, cudaStream_t str
 }
 
 // The operand with its rows along M or N, and with its columns along them.
-static qb_status rows_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t box_rows = 128) {
+static int32_t rows_form(int64_t cols) { return cols % 64 == 0 ? kRows : kRows2; }
+static int32_t cols_form(int64_t cols) { return cols % 64 == 0 ? kCols : kCols2; }
+static qb_status operand_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t box_rows = 128) {
+  if (cols % 64 == 0) return make_group_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols * 2, (int)box_rows, 2);
   return make_matrix_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * 2, (int)box_rows, 64, CU_TENSOR_MAP_SWIZZLE_128B);
-}
-static qb_status cols_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols) {
-  if (cols % 64 == 0) return make_group_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols * 2, 64, 2);
-  return make_matrix_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rows, cols, cols * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 static qb_status validate_vocab(const char* who, bool null, const void* h, const void* w, int64_t T, int64_t V, int64_t D) {
@@ -800,8 +829,8 @@ extern "C" qb_status qb_vocab_loss(const uint16_t* h, const uint16_t* w, const f
   const bool few = T <= kFewTokens;
   const int64_t width = vocab_width(T), tiles = up(V, 256) * up(T, 256);
   VocabParams gp = {};
-  if ((st = rows_map(&gp.map[kMapH], h, T, D, few ? width / 2 : 128)) != QB_OK) return st;
-  if ((st = rows_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
+  if ((st = operand_map(&gp.map[kMapHTile], h, T, D, few ? width / 2 : 128)) != QB_OK) return st;
+  if ((st = operand_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
   char* const scratch = static_cast<char*>(ws) + 1024;
   gp.z_target = reinterpret_cast<float*>(scratch);
   gp.part = reinterpret_cast<float2*>(scratch + up(T * 4, 1024) * 1024);
@@ -814,8 +843,9 @@ extern "C" qb_status qb_vocab_loss(const uint16_t* h, const uint16_t* w, const f
   gp.count = 1;
   VocabProblem& p = gp.prob[0];
   p.kind = kLogits;
-  p.map_a = few ? kMapW : kMapH;
-  p.map_b = few ? kMapH : kMapW;
+  p.map_a = few ? kMapW : kMapHTile;
+  p.map_b = few ? kMapHTile : kMapW;
+  p.a_form = p.b_form = rows_form(D);
   p.n_tiles = 1;
   p.m_tiles = few ? 0 : (int32_t)up(T, 256);
   p.width = (int32_t)width;
@@ -858,19 +888,15 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
   float* const part_bias = reinterpret_cast<float*>(reinterpret_cast<char*>(slabs) + plan.splits * plan.slab_bytes);
   const int64_t Tp = up(T, 64) * 64;
   VocabParams gp = {};
-  CUtensorMap g_rows[2], g_cols[2];
+  CUtensorMap g_map[2];
   uint16_t* const g[2] = {reinterpret_cast<uint16_t*>(g0), reinterpret_cast<uint16_t*>(g1)};
   const bool few = T <= kFewTokens;
   const int64_t width = vocab_width(T);
-  if ((st = rows_map(&gp.map[kMapH], h, T, D, few ? width / 2 : 128)) != QB_OK) return st;
-  if ((st = rows_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
-  if ((st = cols_map(&gp.map[kMapHCols], h, T, D)) != QB_OK) return st;
-  if ((st = cols_map(&gp.map[kMapWCols], w, V, D)) != QB_OK) return st;
-  for (int i = 0; i < 2; ++i) {
-    if ((st = rows_map(&g_rows[i], g[i], plan.rows, Tp)) != QB_OK) return st;
-    if ((st = cols_map(&g_cols[i], g[i], plan.rows, Tp)) != QB_OK) return st;
-  }
-  const int cols_form = D % 64 == 0 ? kCols : kCols2;
+  if ((st = operand_map(&gp.map[kMapH], h, T, D)) != QB_OK) return st;
+  if ((st = operand_map(&gp.map[kMapHTile], h, T, D, few ? width / 2 : 128)) != QB_OK) return st;
+  if ((st = operand_map(&gp.map[kMapW], w, V, D)) != QB_OK) return st;
+  for (int i = 0; i < 2; ++i)
+    if ((st = operand_map(&g_map[i], g[i], plan.rows, Tp)) != QB_OK) return st;
   gp.g_pitch = (int32_t)Tp;
   gp.grad_w = grad_w;
   gp.slabs = slabs;
@@ -893,18 +919,17 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
     };
     if (i > 0) {  // the products of the piece whose g the launch before formed
       const int64_t v0 = (i - 1) * plan.rows, rows = std::min(plan.rows, V - v0);
-      gp.map[kMapG] = g_rows[(i - 1) & 1];
-      gp.map[kMapGCols] = g_cols[(i - 1) & 1];
+      gp.map[kMapG] = g_map[(i - 1) & 1];
       gp.out_v0 = (int32_t)v0;
       gp.add = i > 1;
       VocabProblem p = {};
       if (grad_h) {
         p.kind = kGradH;
         p.width = kVocabTile;
-        p.map_a = kMapGCols;
-        p.map_b = kMapWCols;
+        p.map_a = kMapG;
+        p.map_b = kMapW;
         p.a_form = kCols;
-        p.b_form = cols_form;
+        p.b_form = cols_form(D);
         p.n_tiles = d_tiles;
         p.split_tiles = t_tiles * d_tiles;
         p.k_blocks = (int32_t)plan.k_split;
@@ -918,8 +943,9 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
         p.kind = kGradW;
         p.width = kVocabTile;
         p.map_a = kMapG;
-        p.map_b = kMapHCols;
-        p.b_form = cols_form;
+        p.map_b = kMapH;
+        p.a_form = kRows;
+        p.b_form = cols_form(D);
         p.n_tiles = d_tiles;
         p.split_tiles = (int32_t)up(rows, 256) * d_tiles;
         p.k_blocks = p.k_end = (int32_t)(Tp / 64);
@@ -934,7 +960,8 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
       p.kind = kGradZ;
       p.width = (int32_t)width;
       p.map_a = kMapW;
-      p.map_b = kMapH;
+      p.map_b = kMapHTile;
+      p.a_form = p.b_form = rows_form(D);
       p.a_row0 = (int32_t)v0;
       p.n_tiles = t_tiles;
       p.split_tiles = (int32_t)up(rows, 256) * t_tiles;
