@@ -367,18 +367,24 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
             const uint4 w = *reinterpret_cast<const uint4*>(buf + r * 128 + ((piece ^ (r & 7)) << 4));
             if (r < rows && col < gp.N) *reinterpret_cast<uint4*>(to + (size_t)r * gp.N * (16 / kPiece)) = w;
           }
-        } else {  // rows of y of any alignment: a row at a time, the lanes on consecutive columns
-          for (int r = 0; r < rows; ++r) {
-#pragma unroll
-            for (int p = 0; p < kCols / 32; ++p) {
-              const int c = lane + 32 * p, col = n0 + c0 + c;
-              if (col >= gp.N) continue;
-              const size_t at = (first_row + m0 + r) * gp.N + col;
-              if constexpr (BF16)
-                static_cast<uint16_t*>(gp.y)[at] = *reinterpret_cast<const uint16_t*>(buf + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2);
-              else
-                static_cast<float*>(gp.y)[at] = *reinterpret_cast<const float*>(buf + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4);
-            }
+        } else if constexpr (BF16) {  // rows of y of any alignment: a row at a time, the lanes on consecutive words of it
+          const int cols = min(kCols, gp.N - n0 - c0);
+          uint16_t* to = static_cast<uint16_t*>(gp.y) + (first_row + m0) * gp.N + n0 + c0;
+          for (int r = 0; r < rows; ++r, to += gp.N) {
+            // (columns odd .. odd + 1, odd + 3 .. of the row are words of y)
+            const int odd = (int)(reinterpret_cast<uintptr_t>(to) >> 1) & 1, c = 2 * lane + odd;
+            const auto word = [&](int col) { return *reinterpret_cast<const uint32_t*>(buf + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 6) * 2); };
+            uint32_t w = word(2 * lane);
+            if (odd) w = __byte_perm(w, word(min(2 * lane + 2, kCols - 2)), 0x5432);
+            if (c + 1 < cols) *reinterpret_cast<uint32_t*>(to + c) = w;
+            else if (c < cols) to[c] = (uint16_t)w;
+            if (odd && lane == 0) to[0] = (uint16_t)word(0);
+          }
+        } else {  // the lanes on consecutive values of a row
+          const int col = n0 + c0 + lane;
+          if (col < gp.N) {
+            float* to = static_cast<float*>(gp.y) + (first_row + m0) * gp.N + col;
+            for (int r = 0; r < rows; ++r, to += gp.N) *to = *reinterpret_cast<const float*>(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
           }
         }
       }

@@ -67,13 +67,41 @@ struct Quad {
   Raw raw;
   __device__ __forceinline__ void clear() { raw = {}; }
   __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
-  // the first `left` of them, one by one: rows that are not aligned to four values, and a row's end
-  __device__ __forceinline__ void load_some(const T* p, int64_t left) {
-    clear();
-    T* const e = reinterpret_cast<T*>(&raw);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < left) e[j] = p[j];
+  // Rows of any alignment are read by the aligned quads that have something of them: the four values that start `shift` (1 to 3) values
+  // into this quad end in `next`.
+  static __device__ __forceinline__ uint32_t part(uint32_t lo, uint32_t hi, int shift) { return shift & 1 ? __funnelshift_r(lo, hi, 16) : lo; }
+  __device__ __forceinline__ void shift(const Quad& next, int shift) {
+    if (shift == 0) return;
+    if constexpr (kWide) {
+      const Raw a = raw, b = next.raw;
+      if (shift == 1) raw = make_uint4(a.y, a.z, a.w, b.x);
+      else if (shift == 2) raw = make_uint4(a.z, a.w, b.x, b.y);
+      else raw = make_uint4(a.w, b.x, b.y, b.z);
+    } else {
+      const uint32_t w0 = shift < 2 ? raw.x : raw.y, w1 = shift < 2 ? raw.y : next.raw.x, w2 = shift < 2 ? next.raw.x : next.raw.y;
+      raw = make_uint2(part(w0, w1, shift), part(w1, w2, shift));
+    }
+  }
+  // the quad of the lane that follows; lane 31 gets lane 0's `wrap`
+  static __device__ __forceinline__ Quad of_next_lane(const Quad& q, const Quad& wrap, int lane) {
+    Quad r;
+    const int from = (lane + 1) & 31;
+    r.raw.x = __shfl_sync(0xffffffffu, lane == 0 ? wrap.raw.x : q.raw.x, from);
+    r.raw.y = __shfl_sync(0xffffffffu, lane == 0 ? wrap.raw.y : q.raw.y, from);
+    if constexpr (kWide) {
+      r.raw.z = __shfl_sync(0xffffffffu, lane == 0 ? wrap.raw.z : q.raw.z, from);
+      r.raw.w = __shfl_sync(0xffffffffu, lane == 0 ? wrap.raw.w : q.raw.w, from);
+    }
+    return r;
+  }
+  // nothing behind the first `left` values
+  __device__ __forceinline__ void keep(int left) {
+    if (left >= 4) return;
+    if constexpr (kWide) {
+      raw = make_uint4(left > 0 ? raw.x : 0u, left > 1 ? raw.y : 0u, left > 2 ? raw.z : 0u, 0u);
+    } else {
+      raw = make_uint2(left > 1 ? raw.x : (left > 0 ? raw.x & 0xFFFFu : 0u), left > 2 ? raw.y & 0xFFFFu : 0u);
+    }
   }
   __device__ __forceinline__ Mag magnitudes() const {
     if constexpr (kWide) return make_uint4(raw.x & 0x7FFFFFFFu, raw.y & 0x7FFFFFFFu, raw.z & 0x7FFFFFFFu, raw.w & 0x7FFFFFFFu);
@@ -185,19 +213,44 @@ __global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const T* x, Fp8Ar
   q[1] = wrap ? 0 : q[0] + 1;
   const int K = (int)a.K;
   Quad<T> v[8];
+  if (a.vector) {  // every row begins with a quad, and K is a multiple of four: what is left of a row is too
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int c0 = (int)q[s] * 512 + lane * 4;
-    const T* const p = x + (int64_t)row[s] * a.K + c0;
-    const int left = (s == 0 || it + 1 < items) ? K - c0 : 0;
+    for (int s = 0; s < 2; ++s) {
+      const int c0 = (int)q[s] * 512 + lane * 4;
+      const T* const p = x + (int64_t)row[s] * a.K + c0;
+      const int left = (s == 0 || it + 1 < items) ? K - c0 : 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      Quad<T>& w = v[4 * s + j];
-      if (a.vector) {  // K is a multiple of four: what is left of a row is too
-        w.clear();
-        if (left > j * 128) w.load(p + j * 128);
-      } else {
-        w.load_some(p + j * 128, left - j * 128);
+      for (int j = 0; j < 4; ++j) {
+        v[4 * s + j].clear();
+        if (left > j * 128) v[4 * s + j].load(p + j * 128);
+      }
+    }
+  } else {
+    Quad<T> behind[2];  // lane 0: the quad behind the segment
+    int off[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const T* const p = x + (int64_t)row[s] * a.K + (int)q[s] * 512;
+      off[s] = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) & 3;
+      const int left = (s == 0 || it + 1 < items) ? K - (int)q[s] * 512 : 0;  // of the segment and what follows
+      // a quad is read where it has something of the row (what else it has lies in the same 16 bytes)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = j * 128 + lane * 4 - off[s];
+        v[4 * s + j].clear();
+        if (at < left && left > 0) v[4 * s + j].load(p + at);
+      }
+      behind[s].clear();
+      if (lane == 0 && off[s] != 0 && 512 - off[s] < left) behind[s].load(p + 512 - off[s]);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int left = (s == 0 || it + 1 < items) ? K - (int)q[s] * 512 - lane * 4 : 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const Quad<T> next = Quad<T>::of_next_lane(v[4 * s + j], j < 3 ? v[4 * s + (j + 1) % 4] : behind[s], lane);
+        v[4 * s + j].shift(next, off[s]);
+        v[4 * s + j].keep(left - j * 128);
       }
     }
   }
@@ -247,13 +300,40 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) fp8_tile_kernel(c
   pdl_begin();
   Quad<T> v[16];
   const T* const p = x + (int64_t)m0 * a.K + k0;
-  if (a.vector && rows >= 16 && (int)kt * 128 + 128 <= (int)a.K) {  // all there
+  if (a.vector && rows >= 16 && (int)kt * 128 + 128 <= (int)a.K) {  // all there, every row begins with a quad
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i].load(p + i * a.K);
   } else {
-    // (K a multiple of four: the lane's four columns are all there or none)
+    // as in the rows form; the quads behind the tile's columns: lane i has row i's
+    const T* const first = x + (int64_t)m0 * a.K + (int64_t)kt * 128;
+    const int wide = (int)a.K - (int)kt * 128;  // columns of the tile and behind it
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i].load_some(p + i * a.K, i < rows ? left : 0);
+    for (int i = 0; i < 16; ++i) {
+      const T* const r = first + i * a.K;
+      const int at = lane * 4 - ((int)(reinterpret_cast<uintptr_t>(r) / sizeof(T)) & 3);
+      v[i].clear();
+      if (i < rows && at < wide) v[i].load(r + at);
+    }
+    Quad<T> behind;
+    behind.clear();
+    if (lane < 16 && lane < rows) {
+      const T* const r = first + lane * a.K;
+      const int off = (int)(reinterpret_cast<uintptr_t>(r) / sizeof(T)) & 3;
+      if (off != 0 && 128 - off < wide) behind.load(r + 128 - off);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int off = (int)(reinterpret_cast<uintptr_t>(first + i * a.K) / sizeof(T)) & 3;
+      Quad<T> wrap;
+      wrap.raw.x = __shfl_sync(0xffffffffu, behind.raw.x, i);
+      wrap.raw.y = __shfl_sync(0xffffffffu, behind.raw.y, i);
+      if constexpr (sizeof(T) == 4) {
+        wrap.raw.z = __shfl_sync(0xffffffffu, behind.raw.z, i);
+        wrap.raw.w = __shfl_sync(0xffffffffu, behind.raw.w, i);
+      }
+      v[i].shift(Quad<T>::of_next_lane(v[i], wrap, lane), off);
+      v[i].keep(i < rows ? left : 0);
+    }
   }
   Mag col = v[0].magnitudes();
   uint32_t row_key = 0;  // lane i: of row i

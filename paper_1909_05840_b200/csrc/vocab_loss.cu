@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         // g is formed for all rows of the piece's tiles: the products read whole K blocks of it
         const int chunks = grad_z || row0 < rows ? min(4, (width - col0 + 63) / 64) : 0;
         if (half >= chunks) release();
-        float bias_grad = 0.0f;
+        float bias_grad[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
         for (int ch = half; ch < chunks; ch += 2) {
           uint32_t v[2][32];
@@ -545,16 +545,16 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
               const float4 l = lse4[j], gl = gl4[j];
               const int4 tg = tg4[j];
               uint32_t* const x = &v[j >> 3][(j & 7) * 4];
-              auto one = [&](uint32_t z, float lse, float w, int target) {
+              auto one = [&](uint32_t z, float lse, float w, int target, int k) {
                 const float p = exp2_fast(fmaf(__uint_as_float(z), kLog2e, bias - lse));
                 const float d = w * p - (target == word ? w : 0.0f);
-                bias_grad += d;
+                bias_grad[k] += d;
                 return __float_as_uint(d);
               };
-              x[0] = one(x[0], l.x, gl.x, tg.x);
-              x[1] = one(x[1], l.y, gl.y, tg.y);
-              x[2] = one(x[2], l.z, gl.z, tg.z);
-              x[3] = one(x[3], l.w, gl.w, tg.w);
+              x[0] = one(x[0], l.x, gl.x, tg.x, 0);
+              x[1] = one(x[1], l.y, gl.y, tg.y, 1);
+              x[2] = one(x[2], l.z, gl.z, tg.z, 2);
+              x[3] = one(x[3], l.w, gl.w, tg.w, 3);
             }
           }
           const int c0 = col0 + ch * 64;
@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
                    (gp.D - c0) * 2 - 64 * h, false);
           }
         }
-        if (grad_z && gp.part_bias && gp.v0 + row < gp.V) gp.part_bias[(size_t)(2 * at.n + half) * gp.V + gp.v0 + row] = bias_grad;
+        if (grad_z && gp.part_bias && gp.v0 + row < gp.V) gp.part_bias[(size_t)(2 * at.n + half) * gp.V + gp.v0 + row] = (bias_grad[0] + bias_grad[1]) + (bias_grad[2] + bias_grad[3]);
       }
     }
   }

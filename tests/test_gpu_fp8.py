@@ -66,7 +66,7 @@ def poisoned(shape, dtype=torch.uint8):
     return torch.full(shape, 0xFF, dtype=torch.uint8, device="cuda").view(dtype)
 
 
-SHAPES = [(1, 1), (1, 128), (3, 130), (127, 384), (128, 512), (129, 516), (200, 1000), (33, 1541), (513, 768)]
+SHAPES = [(1, 1), (1, 128), (3, 130), (127, 384), (128, 512), (129, 516), (200, 1000), (33, 1541), (513, 768), (130, 127), (67, 513), (40, 1022), (3, 6), (260, 2047)]
 
 
 @pytest.mark.gpu
