@@ -369,22 +369,30 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
           }
         } else if constexpr (BF16) {  // rows of y of any alignment: a row at a time, the lanes on consecutive words of it
           const int cols = min(kCols, gp.N - n0 - c0);
-          uint16_t* to = static_cast<uint16_t*>(gp.y) + (first_row + m0) * gp.N + n0 + c0;
-          for (int r = 0; r < rows; ++r, to += gp.N) {
-            // (columns odd .. odd + 1, odd + 3 .. of the row are words of y)
-            const int odd = (int)(reinterpret_cast<uintptr_t>(to) >> 1) & 1, c = 2 * lane + odd;
-            const auto word = [&](int col) { return *reinterpret_cast<const uint32_t*>(buf + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 6) * 2); };
-            uint32_t w = word(2 * lane);
-            if (odd) w = __byte_perm(w, word(min(2 * lane + 2, kCols - 2)), 0x5432);
-            if (c + 1 < cols) *reinterpret_cast<uint32_t*>(to + c) = w;
-            else if (c < cols) to[c] = (uint16_t)w;
-            if (odd && lane == 0) to[0] = (uint16_t)word(0);
+          uint16_t* const to = static_cast<uint16_t*>(gp.y) + (first_row + m0) * gp.N + n0 + c0;
+          const int first_odd = (int)(reinterpret_cast<uintptr_t>(to) >> 1) & 1, step = gp.N & 1;
+          const auto word = [&](int r, int col) {  // columns col and col + 1 of a row, col even
+            return *reinterpret_cast<const uint32_t*>(buf + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 6) * 2);
+          };
+          for (int r = 0; r < rows; ++r) {
+            // columns odd and odd + 1, odd + 2 and odd + 3 .. are the words of y
+            const int odd = first_odd ^ (step & r), c = 2 * lane + odd;
+            uint32_t w = word(r, 2 * lane);
+            if (odd) w = __byte_perm(w, word(r, min(2 * lane + 2, kCols - 2)), 0x5432);
+            if (c + 1 < cols) *reinterpret_cast<uint32_t*>(to + (size_t)r * gp.N + c) = w;
+          }
+          if (lane < rows) {  // the single columns at the ends, of all rows at once
+            const int odd = first_odd ^ (step & lane);
+            uint16_t* const at = to + (size_t)lane * gp.N;
+            if (odd) at[0] = (uint16_t)word(lane, 0);
+            if ((cols - odd) & 1) at[cols - 1] = (uint16_t)(word(lane, (cols - 1) & ~1) >> ((cols - 1) & 1) * 16);
           }
         } else {  // the lanes on consecutive values of a row
           const int col = n0 + c0 + lane;
           if (col < gp.N) {
-            float* to = static_cast<float*>(gp.y) + (first_row + m0) * gp.N + col;
-            for (int r = 0; r < rows; ++r, to += gp.N) *to = *reinterpret_cast<const float*>(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+            float* const to = static_cast<float*>(gp.y) + (first_row + m0) * gp.N + col;
+            for (int r = 0; r < rows; ++r)
+              to[(size_t)r * gp.N] = *reinterpret_cast<const float*>(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
           }
         }
       }
