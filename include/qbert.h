@@ -403,9 +403,12 @@ enum { QB_E4M3 = 0, QB_E5M2 = 1 };
  *
  * qb_quantize_fp8 (activations, gradients): blocks of 1 x 128.  With xqt and xt_scale it writes the transposed codes too
  * [K][Mp], Mp = M rounded up to 128, in blocks of 128 rows of x (for products that contract over the tokens).
+ * col_sums (with the transposed codes, or NULL) receives the sums of x's columns over its rows in fp32, always in the same order: the
+ * gradient of a linear's bias when x is grad_y.  The workspace then has qb_fp8_sums_workspace_bytes(M, K) bytes.
  * qb_quantize_fp8_weights: blocks of 128 x 128; the transposed codes (N and K swapped) have the same scales.  x is read once.
  *   x         dev [M][K] of `type`, aligned to its elements                                  (read)
  *   xq, xqt   dev, 16-byte aligned; x_scale, xt_scale: dev, 16-byte aligned                  (written)
+ *   col_sums  dev fp32 [K] or NULL                                                           (written)
  * A block with a NaN or an infinity: QB_ERR_NONFINITE in the status word; its NaN and infinities become NaN codes (and reach
  * the outputs of a product that reads them), its other values are unspecified.
  *
@@ -414,12 +417,13 @@ enum { QB_E4M3 = 0, QB_E5M2 = 1 };
  * of a and b may differ.  For a linear y = x W^T: forward a = x, b = W; grad_x: a = grad_y, b = W transposed; grad_W: a = grad_y
  * transposed, b = x transposed.
  *   bias dev fp32 [N] or NULL (read);  y dev [M][N], aligned to its elements (written)
- * M, N and K as in qb_gemm.  Any workspace will do; one of 1024 + n * 4 * M * N bytes lets a product of few tiles over a long K (the
+ * M, N and K up to QB_MAX_MN.  Any workspace will do; one of 1024 + n * 4 * M * N bytes lets a product of few tiles over a long K (the
  * gradient of a small weight matrix over many tokens) be summed in up to n parts side by side, always in the same order.
  */
 size_t qb_fp8_scale_bytes(int64_t rows, int64_t K);
+size_t qb_fp8_sums_workspace_bytes(int64_t M, int64_t K);
 qb_status qb_quantize_fp8(const void* x, int type, int64_t M, int64_t K, int format, uint8_t* xq, uint8_t* x_scale,
-                          uint8_t* xqt, uint8_t* xt_scale, void* ws, size_t ws_bytes, void* cuda_stream);
+                          uint8_t* xqt, uint8_t* xt_scale, float* col_sums, void* ws, size_t ws_bytes, void* cuda_stream);
 qb_status qb_quantize_fp8_weights(const void* w, int type, int64_t N, int64_t K, int format, uint8_t* wq, uint8_t* w_scale,
                                   uint8_t* wqt, uint8_t* wt_scale, void* ws, size_t ws_bytes, void* cuda_stream);
 qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a_format, const uint8_t* b, const uint8_t* b_scale,

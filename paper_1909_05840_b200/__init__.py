@@ -40,7 +40,7 @@ EXPORTS = (
     "qb_quantize_pack_weights_batch", "qb_gemm_bf16", "qb_layer_linears_bf16",
     "qb_fake_quantize_weights", "qb_fake_quantize_weights_batch", "qb_ste_backward", "qb_quantize_embedding", "qb_embedding_lookup",
     "qb_gemm_i8", "qb_rowsum_i8", "qb_layer_linears_i8", "qb_sensitivity_bits", "qb_probe_wait_limit", "qb_layer_linears_launch_count", "qb_layer_linears_tile_tokens", "qb_quantize_pack_weights_launch_count", "qb_quantize_act_launch_count",
-    "qb_dropout", "qb_fp8_scale_bytes", "qb_quantize_fp8", "qb_quantize_fp8_weights", "qb_gemm_fp8",
+    "qb_dropout", "qb_fp8_scale_bytes", "qb_fp8_sums_workspace_bytes", "qb_quantize_fp8", "qb_quantize_fp8_weights", "qb_gemm_fp8",
     "qb_vocab_loss_workspace_bytes", "qb_vocab_loss", "qb_vocab_loss_backward",
 )
 NOALLOC_MAX_GROUPS = 4096
@@ -152,9 +152,12 @@ def lib() -> ctypes.CDLL:
     L.qb_dropout.restype = i32
     L.qb_fp8_scale_bytes.argtypes = [i64, i64]
     L.qb_fp8_scale_bytes.restype = sz
-    for f in (L.qb_quantize_fp8, L.qb_quantize_fp8_weights):
-        f.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, sz, vp]
-        f.restype = i32
+    L.qb_fp8_sums_workspace_bytes.argtypes = [i64, i64]
+    L.qb_fp8_sums_workspace_bytes.restype = sz
+    L.qb_quantize_fp8.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.qb_quantize_fp8.restype = i32
+    L.qb_quantize_fp8_weights.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.qb_quantize_fp8_weights.restype = i32
     L.qb_gemm_fp8.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i64, i64, i32, vp, vp, sz, vp]
     L.qb_gemm_fp8.restype = i32
     L.qb_vocab_loss_workspace_bytes.argtypes = [i64, i64, i64]
@@ -487,13 +490,21 @@ def fp8_scale_bytes(rows: int, K: int) -> int:
     return int(lib().qb_fp8_scale_bytes(rows, K))
 
 
+def fp8_sums_workspace_bytes(M: int, K: int) -> int:
+    return int(lib().qb_fp8_sums_workspace_bytes(M, K))
+
+
 def quantize_fp8(x: torch.Tensor, ws: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, transposed: bool = False,
                  codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
-                 codes_t: Optional[torch.Tensor] = None, scales_t: Optional[torch.Tensor] = None):
+                 codes_t: Optional[torch.Tensor] = None, scales_t: Optional[torch.Tensor] = None, want_sums: bool = False,
+                 sums: Optional[torch.Tensor] = None):
     """``qb_quantize_fp8``: fp32, bfloat16 or fp16 [M,K] -> (codes [M, K up to 128], scales), blocks of 1 x 128; with
-    ``transposed`` also (codes [K, M up to 128], scales) in blocks of 128 rows, for products over the tokens."""
+    ``transposed`` also (codes [K, M up to 128], scales) in blocks of 128 rows, for products over the tokens, and with
+    ``want_sums`` the column sums fp32 [K] behind them (a bias's gradient; ``ws`` of ``fp8_sums_workspace_bytes(M, K)``)."""
+    if want_sums and not transposed:
+        raise QbertError(QB_ERR_INVALID, "want_sums comes with transposed")
     return (_native or _ext()).quantize_fp8(x, ws, _one_of(_FP8_FORMATS, dtype, "dtype"), bool(transposed), False, codes, scales,
-                                            codes_t, scales_t)
+                                            codes_t, scales_t, bool(want_sums), sums)
 
 
 def quantize_fp8_weights(w: torch.Tensor, ws: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, transposed: bool = False,
@@ -501,7 +512,7 @@ def quantize_fp8_weights(w: torch.Tensor, ws: torch.Tensor, dtype: torch.dtype =
                          codes_t: Optional[torch.Tensor] = None, scales_t: Optional[torch.Tensor] = None):
     """``qb_quantize_fp8_weights``: as ``quantize_fp8`` with one scale per block of 128 x 128."""
     return (_native or _ext()).quantize_fp8(w, ws, _one_of(_FP8_FORMATS, dtype, "dtype"), bool(transposed), True, codes, scales,
-                                            codes_t, scales_t)
+                                            codes_t, scales_t, False, None)
 
 
 def gemm_fp8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, bias: Optional[torch.Tensor],

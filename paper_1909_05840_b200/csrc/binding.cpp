@@ -400,7 +400,8 @@ PyObject* dropout(Args a) {
   return out.get();
 }
 
-// quantize_fp8(x, ws, format, transposed, weights, codes, scales, codes_t, scales_t) -> (codes, scales[, codes_t, scales_t])
+// quantize_fp8(x, ws, format, transposed, weights, codes, scales, codes_t, scales_t, want_sums, sums)
+//   -> (codes, scales[, codes_t, scales_t][, sums])
 PyObject* quantize_fp8(Args a) {
   const char* const what = "x: a contiguous fp32, bfloat16 or fp16 CUDA tensor of two dimensions on the current device";
   const at::Tensor& x = here(a[0], what);
@@ -416,9 +417,11 @@ PyObject* quantize_fp8(Args a) {
     fits(a[7], code, K * Mp, "codes_t: contiguous, of the asked format, [K][M up to 128]");
     fits(a[8], at::kByte, (int64_t)qb_fp8_scale_bytes(K, M), "scales_t: contiguous bytes, fp8_scale_bytes(K, M) of them");
   }
+  const bool want_sums = transposed && !weights && integer(a[9]) != 0;
+  if (want_sums) fits(a[10], at::kFloat, K, "sums: contiguous fp32 [K] on the current device");
   const at::Device device = x.device();
   const void* const x_data = x.const_data_ptr();
-  Out q(a[5]), s(a[6]), qt(transposed ? a[7] : Py_None), s_t(transposed ? a[8] : Py_None);
+  Out q(a[5]), s(a[6]), qt(transposed ? a[7] : Py_None), s_t(transposed ? a[8] : Py_None), sums(want_sums ? a[10] : Py_None);
   qb_status st;
   {
     const Unlocked unlocked;
@@ -428,13 +431,15 @@ PyObject* quantize_fp8(Args a) {
       qt.make({K, Mp}, code, device);
       s_t.make({Kp / 128, (Mp + 511) / 512, 32, 4, 4}, at::kByte, device);
     }
-    st = (weights ? qb_quantize_fp8_weights : qb_quantize_fp8)(
-        x_data, type, M, K, format, static_cast<uint8_t*>(q.data), static_cast<uint8_t*>(s.data), static_cast<uint8_t*>(qt.data),
-        static_cast<uint8_t*>(s_t.data), ws.data, ws.bytes, stream());
+    if (want_sums) sums.make({K}, at::kFloat, device);
+    uint8_t *const qd = static_cast<uint8_t*>(q.data), *const sd = static_cast<uint8_t*>(s.data);
+    uint8_t *const qtd = static_cast<uint8_t*>(qt.data), *const st_data = static_cast<uint8_t*>(s_t.data);
+    if (weights) st = qb_quantize_fp8_weights(x_data, type, M, K, format, qd, sd, qtd, st_data, ws.data, ws.bytes, stream());
+    else st = qb_quantize_fp8(x_data, type, M, K, format, qd, sd, qtd, st_data, static_cast<float*>(sums.data), ws.data, ws.bytes, stream());
   }
   check(st, weights ? "qb_quantize_fp8_weights" : "qb_quantize_fp8");
-  Out* const outs[4] = {&q, &s, &qt, &s_t};
-  const int count = transposed ? 4 : 2;
+  Out* const outs[5] = {&q, &s, &qt, &s_t, &sums};
+  const int count = transposed ? (want_sums ? 5 : 4) : 2;
   for (int i = 0; i < count; ++i) outs[i]->wrap();
   PyObject* r = PyTuple_New(count);
   if (!r) throw Failed{};
@@ -621,7 +626,7 @@ PyMethodDef g_methods[] = {QB_ENTRY(quantize_act, 5),
                            QB_ENTRY(quantize_embedding, 5),
                            QB_ENTRY(embedding_lookup, 10),
                            QB_ENTRY(dropout, 6),
-                           QB_ENTRY(quantize_fp8, 9),
+                           QB_ENTRY(quantize_fp8, 11),
                            QB_ENTRY(gemm_fp8, 8),
                            QB_ENTRY(vocab_loss, 7),
                            QB_ENTRY(vocab_loss_backward, 13),

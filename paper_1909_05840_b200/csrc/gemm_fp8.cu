@@ -497,7 +497,7 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
                                  int b_format, const float* bias, int64_t M, int64_t N, int64_t K, int out_type, void* y, void* ws,
                                  size_t ws_bytes, void* cuda_stream) {
   using namespace qb;
-  if (!a || !a_scale || !b || !b_scale || !y || M <= 0 || N <= 0 || K <= 0 || M > QB_MAX_MN || N > QB_MAX_MN || K > QB_MAX_K ||
+  if (!a || !a_scale || !b || !b_scale || !y || M <= 0 || N <= 0 || K <= 0 || M > QB_MAX_MN || N > QB_MAX_MN || K > QB_MAX_MN ||
       a_format < QB_E4M3 || a_format > QB_E5M2 || b_format < QB_E4M3 || b_format > QB_E5M2 || out_type < QB_F32 || out_type > QB_BF16) {
     set_last_error("qb_gemm_fp8: invalid argument (M=%lld N=%lld K=%lld formats %d, %d, output type %d)", (long long)M, (long long)N,
                    (long long)K, a_format, b_format, out_type);
@@ -512,14 +512,14 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
     set_last_error("qb_gemm_fp8: workspace null or too small");
     return QB_ERR_WORKSPACE;
   }
+  const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m; };
+  if (up(M, 128) * up(N, 64) > (int64_t)1 << 30 || std::max(up(M, 128), up(N, 128)) * fp8_scale_words(K) > (int64_t)1 << 30) {
+    set_last_error("qb_gemm_fp8: more than 2^30 tiles, or pieces of scales (M=%lld N=%lld K=%lld)", (long long)M, (long long)N, (long long)K);
+    return QB_ERR_INVALID;
+  }
   int sms = 0;
   qb_status st = require_sm100(&sms);
   if (st != QB_OK) return st;
-  const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m; };
-  if (up(M, 128) * up(N, 64) > (int64_t)1 << 30) {
-    set_last_error("qb_gemm_fp8: more than 2^30 tiles (M=%lld N=%lld)", (long long)M, (long long)N);
-    return QB_ERR_INVALID;
-  }
   const size_t head = 1024;  // the parts of a split product lie behind it
   const bool roomy = ws_bytes > head && reinterpret_cast<uintptr_t>(ws) % 16 == 0;
   const Fp8Choice choice = choose_fp8(M, N, K, sms, roomy ? ws_bytes - head : 0);

@@ -183,6 +183,8 @@ struct Quad {
   }
 };
 
+constexpr size_t kSumsOff = 1024;  // of the tiles' column sums in the workspace
+
 struct Fp8Args {
   int64_t M, K;      // x [M][K]
   int64_t Kp, Mp;    // rounded up to 128
@@ -190,6 +192,7 @@ struct Fp8Args {
   uint8_t* scale;    // of q
   uint8_t* qt;       // [K][Mp] or NULL
   uint8_t* scale_t;
+  float* sums;       // [Mp / 128][K]: the sums of the tiles' columns, or NULL
   void* ws;
   int vector;        // every row starts aligned to four values
 };
@@ -201,7 +204,7 @@ constexpr int kRowThreads = 256;
 template <class T, int FMT>
 __global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const T* x, Fp8Args a) {
   const int lane = threadIdx.x & 31;
-  const uint32_t kq = (uint32_t)fp8_scale_words(a.Kp), items = (uint32_t)a.M * kq;  // M <= 2^24, kq <= 2^7
+  const uint32_t kq = (uint32_t)fp8_scale_words(a.Kp), items = (uint32_t)a.M * kq;  // at most 2^30
   const uint32_t it = 2 * (blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5));
   pdl_begin();
   if (it >= items) return;
@@ -292,6 +295,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) fp8_tile_kernel(c
   typedef typename Quad<T>::Pair Pair;
   __shared__ Mag tops[8][32];
   __shared__ uint32_t squares[8];
+  __shared__ float4 sums[SQUARE ? 1 : 8][32];
   __shared__ uint4 turned[128 * 8];  // [column][8 pieces of 16 rows], piece p of column c at p ^ (c / 4 % 8)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t k_tiles = (uint32_t)(a.Kp / 128), mt = blockIdx.x / k_tiles, kt = blockIdx.x - mt * k_tiles;
@@ -351,8 +355,37 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) fp8_tile_kernel(c
     if (lane == 0) squares[warp] = mine;
   } else {
     if (a.qt) tops[warp][lane] = col;
+    if (a.sums) {
+      float4 t = v[0].values();
+#pragma unroll
+      for (int i = 1; i < 16; ++i) {
+        const float4 f = v[i].values();
+        t.x += f.x;
+        t.y += f.y;
+        t.z += f.z;
+        t.w += f.w;
+      }
+      sums[warp][lane] = t;
+    }
   }
   __syncthreads();
+  if constexpr (!SQUARE) {
+    if (a.sums && warp == 0) {
+      float4 t = sums[0][lane];
+#pragma unroll
+      for (int w = 1; w < 8; ++w) {
+        const float4 f = sums[w][lane];
+        t.x += f.x;
+        t.y += f.y;
+        t.z += f.z;
+        t.w += f.w;
+      }
+      const float part[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < left) a.sums[(int64_t)mt * a.K + k0 + j] = part[j];
+    }
+  }
   if constexpr (SQUARE) {
 #pragma unroll
     for (int w = 0; w < 8; ++w) row_key = max(row_key, squares[w]);
@@ -414,6 +447,24 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) fp8_tile_kernel(c
   }
 }
 
+// out[k] = the tiles' sums of column k: every warp of a block adds up every eighth tile, then the warps are joined in order.
+__global__ void __launch_bounds__(256) fp8_sums_kernel(const float* parts, int tiles, int K, float* out) {
+  __shared__ float joined[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.x * 32 + lane;
+  pdl_begin();
+  float t = 0.0f;
+  if (k < K) {
+#pragma unroll 8
+    for (int i = warp; i < tiles; i += 8) t += parts[(int64_t)i * K + k];
+  }
+  joined[warp][lane] = t;
+  __syncthreads();
+  if (warp != 0 || k >= K) return;
+#pragma unroll
+  for (int w = 1; w < 8; ++w) t += joined[w][lane];
+  out[k] = t;
+}
+
 template <class T, int FMT>
 static qb_status launch_fp8(const T* x, const Fp8Args& a, bool square, cudaStream_t stream) {
   if (!square && !a.qt) {
@@ -432,24 +483,26 @@ static qb_status launch_fp8_format(const void* x, int format, const Fp8Args& a, 
 }
 
 static qb_status quantize_fp8_entry(const char* who, const void* x, int type, int64_t M, int64_t K, int format, uint8_t* q, uint8_t* scale,
-                                    uint8_t* qt, uint8_t* scale_t, void* ws, size_t ws_bytes, void* cuda_stream, bool square) {
-  if (!x || !q || !scale || (qt == nullptr) != (scale_t == nullptr) || M <= 0 || K <= 0 || M > QB_MAX_MN ||
-      K > (qt ? QB_MAX_MN : QB_MAX_K) || type < QB_F32 || type > QB_F16 || format < QB_E4M3 || format > QB_E5M2) {
+                                    uint8_t* qt, uint8_t* scale_t, float* sums, void* ws, size_t ws_bytes, void* cuda_stream, bool square) {
+  if (!x || !q || !scale || (qt == nullptr) != (scale_t == nullptr) || (sums && !qt) || M <= 0 || K <= 0 || M > QB_MAX_MN || K > QB_MAX_MN ||
+      type < QB_F32 || type > QB_F16 || format < QB_E4M3 || format > QB_E5M2) {
     set_last_error("%s: invalid argument (M=%lld K=%lld type=%d format=%d)", who, (long long)M, (long long)K, type, format);
     return QB_ERR_INVALID;
   }
   const int64_t Kp = (K + 127) / 128 * 128, Mp = (M + 127) / 128 * 128;
-  if ((Mp / 128) * (Kp / 128) > (int64_t)1 << 30) {
-    set_last_error("%s: more than 2^30 blocks of 128 x 128 (M=%lld K=%lld)", who, (long long)M, (long long)K);
+  if ((Mp / 128) * (Kp / 128) > (int64_t)1 << 30 || M * fp8_scale_words(Kp) > (int64_t)1 << 30) {
+    set_last_error("%s: more than 2^30 blocks of 128 x 128 or segments of 512 (M=%lld K=%lld)", who, (long long)M, (long long)K);
     return QB_ERR_INVALID;
   }
   const size_t size = type == QB_F32 ? 4 : 2;
-  if (reinterpret_cast<uintptr_t>(x) % size != 0 || !aligned16(q) || !aligned16(scale) || !aligned16(qt) || !aligned16(scale_t)) {
-    set_last_error("%s: x must be aligned to its elements, codes and scales to 16 bytes", who);
+  if (reinterpret_cast<uintptr_t>(x) % size != 0 || !aligned16(q) || !aligned16(scale) || !aligned16(qt) || !aligned16(scale_t) ||
+      reinterpret_cast<uintptr_t>(sums) % 4 != 0) {
+    set_last_error("%s: x and the sums must be aligned to their elements, codes and scales to 16 bytes", who);
     return QB_ERR_ALIGN;
   }
-  if (!ws || ws_bytes < kWsMinBytes) {
-    set_last_error("%s: workspace null or too small", who);
+  const size_t need = sums ? qb_fp8_sums_workspace_bytes(M, K) : kWsMinBytes;
+  if (!ws || ws_bytes < need || (sums && reinterpret_cast<uintptr_t>(ws) % 4 != 0)) {
+    set_last_error("%s: workspace null, not aligned or smaller than %zu bytes", who, need);
     return QB_ERR_WORKSPACE;
   }
   qb_status st = require_sm100(nullptr);
@@ -463,14 +516,18 @@ static qb_status quantize_fp8_entry(const char* who, const void* x, int type, in
   a.scale = scale;
   a.qt = qt;
   a.scale_t = scale_t;
+  a.sums = sums ? reinterpret_cast<float*>(static_cast<char*>(ws) + kSumsOff) : nullptr;
   a.ws = ws;
   a.vector = reinterpret_cast<uintptr_t>(x) % (4 * size) == 0 && K % 4 == 0;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   switch (type) {
-    case QB_F32: return launch_fp8_format<float>(x, format, a, square, stream);
-    case QB_BF16: return launch_fp8_format<__nv_bfloat16>(x, format, a, square, stream);
-    default: return launch_fp8_format<__half>(x, format, a, square, stream);
+    case QB_F32: st = launch_fp8_format<float>(x, format, a, square, stream); break;
+    case QB_BF16: st = launch_fp8_format<__nv_bfloat16>(x, format, a, square, stream); break;
+    default: st = launch_fp8_format<__half>(x, format, a, square, stream);
   }
+  if (st != QB_OK || !sums) return st;
+  QB_CUDA_TRY(launch_kernel(fp8_sums_kernel, (unsigned)((K + 31) / 32), 256, 0, stream, 1, false, a.sums, (int)(Mp / 128), (int)K, sums));
+  return QB_OK;
 }
 
 }  // namespace qb
@@ -480,12 +537,17 @@ extern "C" size_t qb_fp8_scale_bytes(int64_t rows, int64_t K) {
   return (size_t)((rows + 127) / 128 * qb::fp8_scale_words((K + 127) / 128 * 128) * 512);
 }
 
+extern "C" size_t qb_fp8_sums_workspace_bytes(int64_t M, int64_t K) {
+  if (M <= 0 || K <= 0 || M > QB_MAX_MN || K > QB_MAX_MN) return 0;
+  return (size_t)(qb::kSumsOff + (M + 127) / 128 * K * 4);
+}
+
 extern "C" qb_status qb_quantize_fp8(const void* x, int type, int64_t M, int64_t K, int format, uint8_t* xq, uint8_t* x_scale,
-                                     uint8_t* xqt, uint8_t* xt_scale, void* ws, size_t ws_bytes, void* cuda_stream) {
-  return qb::quantize_fp8_entry("qb_quantize_fp8", x, type, M, K, format, xq, x_scale, xqt, xt_scale, ws, ws_bytes, cuda_stream, false);
+                                     uint8_t* xqt, uint8_t* xt_scale, float* col_sums, void* ws, size_t ws_bytes, void* cuda_stream) {
+  return qb::quantize_fp8_entry("qb_quantize_fp8", x, type, M, K, format, xq, x_scale, xqt, xt_scale, col_sums, ws, ws_bytes, cuda_stream, false);
 }
 
 extern "C" qb_status qb_quantize_fp8_weights(const void* w, int type, int64_t N, int64_t K, int format, uint8_t* wq, uint8_t* w_scale,
                                              uint8_t* wqt, uint8_t* wt_scale, void* ws, size_t ws_bytes, void* cuda_stream) {
-  return qb::quantize_fp8_entry("qb_quantize_fp8_weights", w, type, N, K, format, wq, w_scale, wqt, wt_scale, ws, ws_bytes, cuda_stream, true);
+  return qb::quantize_fp8_entry("qb_quantize_fp8_weights", w, type, N, K, format, wq, w_scale, wqt, wt_scale, nullptr, ws, ws_bytes, cuda_stream, true);
 }

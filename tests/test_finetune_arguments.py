@@ -29,12 +29,21 @@ def test_dropout(lib):
 def test_fp8(lib):
     assert qb.fp8_scale_bytes(1, 1) == 512 and qb.fp8_scale_bytes(129, 513) == 4 * 512 and qb.fp8_scale_bytes(128, 512) == 512
     assert qb.fp8_scale_bytes(0, 128) == 0 and qb.fp8_scale_bytes(128, -1) == 0 and qb.fp8_scale_bytes((1 << 24) + 1, 1) == 0
-    ok = dict(x=A, type=0, M=8, K=100, format=0, q=A, s=A, qt=A, st=A, ws=A, ws_bytes=256)
+    assert qb.fp8_sums_workspace_bytes(129, 10) == 1024 + 2 * 10 * 4 and qb.fp8_sums_workspace_bytes(0, 1) == 0
     for f in (lib.qb_quantize_fp8, lib.qb_quantize_fp8_weights):
+        ok = dict(x=A, type=0, M=8, K=100, format=0, q=A, s=A, qt=A, st=A)
+        if f is lib.qb_quantize_fp8:
+            ok["sums"] = None
+        ok.update(ws=A, ws_bytes=256)
+
         def call(**kw):
             return f(*{**ok, **kw}.values(), None)
+        if f is lib.qb_quantize_fp8:
+            assert call(sums=A, qt=None, st=None) == qb.QB_ERR_INVALID
+            assert call(sums=A + 2, ws_bytes=4096) == qb.QB_ERR_ALIGN
+            assert call(sums=A, ws_bytes=1024 + 399) == qb.QB_ERR_WORKSPACE
         for bad in (dict(x=None), dict(q=None), dict(s=None), dict(qt=None), dict(st=None), dict(M=0), dict(K=0), dict(M=(1 << 24) + 1),
-                    dict(K=(1 << 24) + 1), dict(K=65537, qt=None, st=None), dict(M=1 << 24, K=1 << 24), dict(type=3), dict(format=2), dict(format=-1)):
+                    dict(K=(1 << 24) + 1), dict(M=1 << 24, K=1 << 24), dict(M=1 << 24, K=1 << 16, qt=None, st=None), dict(type=3), dict(format=2), dict(format=-1)):
             assert call(**bad) == qb.QB_ERR_INVALID, bad
         for bad in (dict(x=A + 2), dict(type=1, x=A + 1), dict(q=A + 8), dict(s=A + 4), dict(qt=A + 1), dict(st=A + 2)):
             assert call(**bad) == qb.QB_ERR_ALIGN, bad
@@ -44,7 +53,7 @@ def test_fp8(lib):
 
     def gemm(**kw):
         return lib.qb_gemm_fp8(*{**ok, **kw}.values(), None)
-    for bad in (dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(y=None), dict(M=0), dict(N=0), dict(K=0), dict(K=65536 + 128),
+    for bad in (dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(y=None), dict(M=0), dict(N=0), dict(K=0), dict(K=(1 << 24) + 128), dict(M=1 << 24, N=1 << 24), dict(M=1 << 24, K=1 << 24),
                 dict(M=(1 << 24) + 1), dict(N=(1 << 24) + 1), dict(fa=2), dict(fb=-1), dict(out=2), dict(out=-1)):
         assert gemm(**bad) == qb.QB_ERR_INVALID, bad
     for bad in (dict(K=130), dict(a=A + 8), dict(b=A + 8), dict(sa=A + 8), dict(sb=A + 8), dict(y=A + 2), dict(out=1, y=A + 1)):
@@ -58,7 +67,7 @@ def test_no_cpu_fallback(lib):
     if torch.cuda.is_available():
         pytest.skip("a CUDA device is present")
     assert lib.qb_dropout(A, 0, 64, 0.1, A, 0, None, A, None) == qb.QB_ERR_CUDA
-    assert lib.qb_quantize_fp8(A, 0, 8, 128, 0, A, A, None, None, A, 256, None) == qb.QB_ERR_CUDA
+    assert lib.qb_quantize_fp8(A, 0, 8, 128, 0, A, A, None, None, None, A, 256, None) == qb.QB_ERR_CUDA
     assert lib.qb_gemm_fp8(A, A, 0, A, A, 0, None, 8, 8, 128, 0, A, A, 256, None) == qb.QB_ERR_CUDA
 
 

@@ -182,14 +182,40 @@ def test_product(ws, M, N, K, out):
     assert (buffer[M * N:] == 3.0).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M,K", [(1, 1), (130, 9), (613, 768), (1024, 131), (5003, 260)])
+def test_column_sums(M, K, kind):
+    """A bias's gradient beside the codes.  fp32 additions: 16 rows, 8 warps, an eighth of the tiles and 8 warps in a chain, 2^-24 of the
+    terms' absolute sum each."""
+    x = rows_of(M, K, M + K, kind)
+    ws = torch.zeros(qb.fp8_sums_workspace_bytes(M, K), dtype=torch.uint8, device="cuda")
+    plain = qb.quantize_fp8(x, ws, E5M2, transposed=True)
+    sums = torch.full((K + 3,), 7.0, device="cuda")
+    both = qb.quantize_fp8(x, ws, E5M2, transposed=True, want_sums=True, sums=sums[:K])
+    assert len(both) == 5 and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(plain[::2], both[::2]))
+    want, size = x.double().sum(0), x.double().abs().sum(0)
+    assert ((sums[:K].double() - want).abs() <= size * (16 + 8 + M / 1024 + 1 + 8) * 2.0**-24).all() and (sums[K:] == 7.0).all()
+    assert torch.equal(sums[:K], qb.quantize_fp8(x, ws, E5M2, transposed=True, want_sums=True)[4])
+    for bad in (dict(sums=sums), dict(sums=sums[:K].half()), dict(sums=sums[:K].cpu())):
+        with pytest.raises(AssertionError):
+            qb.quantize_fp8(x, ws, E5M2, transposed=True, want_sums=True, **bad)
+    with pytest.raises(qb.QbertError):
+        qb.quantize_fp8(x, ws, want_sums=True)
+    with pytest.raises(qb.QbertError):
+        qb.quantize_fp8(x, ws[:-4], E5M2, transposed=True, want_sums=True)
+
+
 # few tiles over a long contraction: summed in parts side by side where the workspace has room, in one piece where not
 @pytest.mark.gpu
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("M,N,K", [(9, 7, 8192), (256, 300, 24576), (129, 770, 65536), (768, 768, 4224)])
+@pytest.mark.parametrize("M,N,K", [(9, 7, 8192), (256, 300, 24576), (129, 770, 65536), (768, 768, 4224), (70, 40, 131200)])
 def test_long_contractions(M, N, K, out):
     a, sa = qb.quantize_fp8(rows_of(M, K, 1), qb.workspace())
     b, sb = qb.quantize_fp8(rows_of(N, K, 2), qb.workspace())
     bias = torch.randn(N, device="cuda")
+    if K > 65536:  # the contraction of a weight gradient over more tokens than the integer linears take features
+        assert a.shape[1] == K
     for nbytes in (256, 1024 + 3 * M * N * 4, 1024 + 100 * M * N * 4):
         ws = torch.zeros(nbytes, dtype=torch.uint8, device="cuda")
         y = qb.gemm_fp8(a, sa, b, sb, bias, ws, out)
