@@ -160,11 +160,11 @@ struct Quad {
       return make_float4(__half2float(e[0]), __half2float(e[1]), __half2float(e[2]), __half2float(e[3]));
     }
   }
-  // `lo` for the first two, `hi` for the last two values.  `finite`: the block has no NaN or infinity.
-  template <int FMT>
-  __device__ __forceinline__ uint32_t codes(Pair lo, Pair hi, bool finite) const {
+  // `lo` for the first two, `hi` for the last two values.  FINITE: the block has no NaN or infinity.
+  template <int FMT, bool FINITE>
+  __device__ __forceinline__ uint32_t codes(Pair lo, Pair hi) const {
     if constexpr (kBf16) {
-      if (finite) {
+      if constexpr (FINITE) {
         Quad q;
         asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(q.raw.x) : "r"(raw.x), "r"(lo.a));
         asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(q.raw.y) : "r"(raw.y), "r"(hi.a));
@@ -177,7 +177,7 @@ struct Quad {
                            finite_or_nan(f.w) * wide(hi.a, true));
     } else {
       float4 f = values();
-      if (!finite) f = make_float4(finite_or_nan(f.x), finite_or_nan(f.y), finite_or_nan(f.z), finite_or_nan(f.w));
+      if constexpr (!FINITE) f = make_float4(finite_or_nan(f.x), finite_or_nan(f.y), finite_or_nan(f.z), finite_or_nan(f.w));
       return codes_of<FMT>(__fmul_rn(f.x, lo.a), __fmul_rn(f.y, lo.b), __fmul_rn(f.z, hi.a), __fmul_rn(f.w, hi.b));
     }
   }
@@ -271,18 +271,22 @@ __global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const T* x, Fp8Ar
     if (top >= 0x7F800000u) report_status(a.ws, QB_ERR_NONFINITE);
   }
   const typename Quad<T>::Inv inv = Quad<T>::inverse(byte);
+  const auto write = [&](auto all_finite) {
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    if (s == 1 && it + 1 >= items) break;
-    const int c0 = (int)q[s] * 512 + lane * 4;
-    uint8_t* const out = a.q + (int64_t)row[s] * a.Kp + c0;
+    for (int s = 0; s < 2; ++s) {
+      if (s == 1 && it + 1 >= items) break;
+      const int c0 = (int)q[s] * 512 + lane * 4;
+      uint8_t* const out = a.q + (int64_t)row[s] * a.Kp + c0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const typename Quad<T>::Inv i = __shfl_sync(0xffffffffu, inv, 4 * s + j);
-      const uint32_t code = v[4 * s + j].template codes<FMT>({i, i}, {i, i}, finite);
-      if (c0 + j * 128 < (int)a.Kp) *reinterpret_cast<uint32_t*>(out + j * 128) = code;
+      for (int j = 0; j < 4; ++j) {
+        const typename Quad<T>::Inv i = __shfl_sync(0xffffffffu, inv, 4 * s + j);
+        const uint32_t code = v[4 * s + j].template codes<FMT, decltype(all_finite)::value>({i, i}, {i, i});
+        if (c0 + j * 128 < (int)a.Kp) *reinterpret_cast<uint32_t*>(out + j * 128) = code;
+      }
     }
-  }
+  };
+  if (finite) write(std::true_type());
+  else write(std::false_type());
 }
 
 // A tile of 128 x 128 values per block, held in registers (warp w: rows 16 w .. 16 w + 15, lane l: columns 4 l .. 4 l + 3).
@@ -399,12 +403,16 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) fp8_tile_kernel(c
   const typename Quad<T>::Inv row_inv = Quad<T>::inverse(row_byte);
   uint8_t* const out = a.q + (int64_t)m0 * a.Kp + k0;
   uint32_t code[16];
+  const auto write = [&](auto all_finite) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const typename Quad<T>::Inv inv = SQUARE ? row_inv : __shfl_sync(0xffffffffu, row_inv, i);
-    code[i] = v[i].template codes<FMT>(Pair{inv, inv}, Pair{inv, inv}, rows_finite);
-    if (i < rows) *reinterpret_cast<uint32_t*>(out + i * a.Kp) = code[i];
-  }
+    for (int i = 0; i < 16; ++i) {
+      const typename Quad<T>::Inv inv = SQUARE ? row_inv : __shfl_sync(0xffffffffu, row_inv, i);
+      code[i] = v[i].template codes<FMT, decltype(all_finite)::value>(Pair{inv, inv}, Pair{inv, inv});
+      if (i < rows) *reinterpret_cast<uint32_t*>(out + i * a.Kp) = code[i];
+    }
+  };
+  if (rows_finite) write(std::true_type());
+  else write(std::false_type());
   if (!a.qt) return;
   if constexpr (!SQUARE) {  // the columns' own scales
 #pragma unroll
@@ -419,8 +427,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) fp8_tile_kernel(c
       if (warp == 0 && j < left) a.scale_t[fp8_scale_offset(k0 + j, mt, fp8_scale_words(a.Mp))] = (uint8_t)byte[j];
     }
     const Pair lo = Quad<T>::columns(byte[0], byte[1]), hi = Quad<T>::columns(byte[2], byte[3]);
+    if (__all_sync(0xffffffffu, finite)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) code[i] = v[i].template codes<FMT>(lo, hi, finite);
+      for (int i = 0; i < 16; ++i) code[i] = v[i].template codes<FMT, true>(lo, hi);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) code[i] = v[i].template codes<FMT, false>(lo, hi);
+    }
   } else if (warp == 0) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)

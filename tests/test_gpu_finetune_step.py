@@ -43,12 +43,12 @@ class Step:
         loss, lse = qb.vocab_loss(h, self.decoder, self.out_bias, self.targets, ws)
         dh, dec, db = qb.vocab_loss_backward(h, self.decoder, self.out_bias, self.targets, lse, self.grad_loss, ws)
         dy = qb.dropout(dh, P_DROP, self.rng, 1)
-        gq, gs, gqt, gst = qb.quantize_fp8(dy, ws, E5M2, transposed=True)
+        gq, gs, gqt, gst, dbias = qb.quantize_fp8(dy, ws, E5M2, transposed=True, want_sums=True)
         dx = qb.gemm_fp8(gq, gs, wqt, wst, None, ws, torch.float32)
         dx += dh  # the residual's part
         dw = qb.gemm_fp8(gqt, gst, xqt, xst, None, ws, torch.float32)
         self.rng[1] += 1
-        return {"loss": loss, "decoder": dec, "out_bias": db, "x": dx, "w": dw}
+        return {"loss": loss, "decoder": dec, "out_bias": db, "x": dx, "w": dw, "bias": dbias}
 
     def reference(self, offset):
         """The same step in 64 bits, rounded to 8 and 16 bits where the step rounds."""
@@ -80,7 +80,7 @@ class Step:
         dy = (keep * dh / (1 - P_DROP)).bfloat16().double()
         dx = fp8(dy, E5M2, 1) @ fp8(self.w.double(), E4M3, 128) + dh
         dw = fp8(dy.t().contiguous(), E5M2, 1) @ fp8(x.t().contiguous(), E4M3, 1).t()
-        return {"loss": loss, "decoder": g.t() @ h, "out_bias": g.sum(0), "x": dx, "w": dw}
+        return {"loss": loss, "decoder": g.t() @ h, "out_bias": g.sum(0), "x": dx, "w": dw, "bias": dy.sum(0)}
 
 
 @pytest.mark.parametrize("T,V,D", [(70, 1000, 256), (300, 3001, 384)])
@@ -94,7 +94,7 @@ def test_step(T, V, D):
     step = Step(T, V, D, seed=3)
     got, want = step.run(), step.reference(40)
     assert qb.read_status(step.ws) == qb.QB_OK
-    for name, bound in (("loss", 2.0**-10), ("out_bias", 2.0**-10), ("decoder", 0.08), ("x", 0.08), ("w", 0.08)):
+    for name, bound in (("loss", 2.0**-10), ("out_bias", 2.0**-10), ("decoder", 0.08), ("x", 0.08), ("w", 0.08), ("bias", 0.08)):
         off = float((got[name].double() - want[name]).norm() / want[name].norm())
         assert off <= bound, (name, off)
 
