@@ -49,7 +49,6 @@
 #include "common.cuh"
 #include "mbar_wait.cuh"
 #include "ptx.cuh"
-#include "tensormap.cuh"
 
 namespace qb {
 
@@ -918,6 +917,26 @@ static const int g_pair_mode = [] {
   const char* e = std::getenv("QBERT_PAIR");
   return (e && e[0] == '0') ? 0 : 1;
 }();
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static qb_status get_encode_fn(EncodeTiledFn* out) {
+  static EncodeTiledFn cached = nullptr;
+  if (!cached) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    QB_CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
+    if (qres != cudaDriverEntryPointSuccess || !fn) {
+      set_last_error("cuTensorMapEncodeTiled not available from the driver");
+      return QB_ERR_CUDA;
+    }
+    cached = reinterpret_cast<EncodeTiledFn>(fn);
+  }
+  *out = cached;
+  return QB_OK;
+}
 
 // int8 activations [M][K], K contiguous; box = 128 bytes of K x `box_rows` tokens, 128-byte swizzle.
 static qb_status make_x_tensormap(CUtensorMap* tm, const int8_t* xq, int64_t M, int64_t K, int box_rows) {

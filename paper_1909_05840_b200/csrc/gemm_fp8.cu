@@ -26,7 +26,7 @@
 #include "common.cuh"
 #include "fp8.cuh"
 #include "mbar_wait.cuh"
-#include "ptx.cuh"
+#include "ptx_float.cuh"
 #include "tensormap.cuh"
 
 namespace qb {

@@ -139,19 +139,6 @@ __device__ __forceinline__ void tma_store_wait_read1() {
   asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
 }
 
-// 32 bytes, one whole sector (32-byte aligned).
-__device__ __forceinline__ void store_v8(void* p, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
-               "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-// Four fp32 values added to those in memory (16-byte aligned), nothing read back.
-__device__ __forceinline__ void red_add_v4(void* p, uint4 v) {
-  asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)),
-               "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w))
-               : "memory");
-}
-
 // ---- register reallocation between warpgroups ------------------------------------------------------
 // Executed by all warps of a warpgroup (four consecutive warps).  dec releases registers down to N per
 // thread; inc waits until the CTA's pool (threads x registers at launch) has N per thread to give.
@@ -242,15 +229,6 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst_smem, const void* 
       : "memory");
 }
 
-// The same for a tensor of three dimensions (x innermost).
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* tmap, uint32_t bar_cluster, int32_t x, int32_t y,
-                                                 int32_t z) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(dst_smem), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z)
-      : "memory");
-}
-
 template <int CG>
 __device__ __forceinline__ void tmem_alloc_cg(uint32_t slot_smem, uint32_t ncols) {
   if constexpr (CG == 2)
@@ -301,65 +279,6 @@ __device__ __forceinline__ void mma_commit_cg(uint32_t bar) {
   } else {
     mma_commit(bar);
   }
-}
-
-// D[tmem] (+)= (A[smem] * scale_a) * (B[smem] * scale_b), 8-bit floating point operands, fp32 accumulators; one 2^(e - 127)
-// per row of A and of B for the instruction's 32 elements of K, its byte e taken from tensor memory (the byte of the
-// 32-bit words at scale_a / scale_b that the instruction descriptor names).
-template <int CG>
-__device__ __forceinline__ void mma_mxf8_ss_cg(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                               uint32_t scale_a, uint32_t scale_b, uint32_t accumulate) {
-  if constexpr (CG == 2)
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
-        "}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
-        : "memory");
-  else
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
-        "}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
-        : "memory");
-}
-// D[tmem] (+)= A[smem] * B[smem], 16-bit floating point operands (both of one type), fp32 accumulators.
-template <int CG>
-__device__ __forceinline__ void mma_f16_ss_cg(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                              uint32_t accumulate) {
-  if constexpr (CG == 2)
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t"
-        "}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-  else
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
-        "}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-// 32 rows of 16 bytes from shared memory to 32 lanes x 4 columns of tensor memory, the same in all four quarters of the lanes
-// (how the scales of a block-scaled MMA have to lie).  CG = 2: in both CTAs of the pair, each from its own shared
-// memory.  Later MMAs of the issuing thread see the data; mma_commit covers the copy too.
-template <int CG>
-__device__ __forceinline__ void tmem_copy_scales_cg(uint32_t taddr, uint64_t desc) {
-  if constexpr (CG == 2)
-    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-  else
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 
 // Warp-wide load of 32 consecutive 32-bit columns of the warp's 32 lanes (lane i = TMEM lane base+i).

@@ -1,0 +1,76 @@
+// Thin wrappers over the sm_100a PTX that the floating-point products use besides those of ptx.cuh.
+#pragma once
+
+#include "ptx.cuh"
+
+namespace qb {
+namespace ptx {
+
+// Four fp32 values added to those in memory (16-byte aligned), nothing read back.
+__device__ __forceinline__ void red_add_v4(void* p, uint4 v) {
+  asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)),
+               "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w))
+               : "memory");
+}
+
+// tma_load_2d_pair for a tensor of three dimensions (x innermost; x * element size a multiple of 16 bytes).  No multicast.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* tmap, uint32_t bar_cluster, int32_t x, int32_t y,
+                                                 int32_t z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst_smem), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+// D[tmem] (+)= (A[smem] * scale_a) * (B[smem] * scale_b), 8-bit floating point operands, fp32 accumulators; one 2^(e - 127)
+// per row of A and of B for the instruction's 32 elements of K, its byte e taken from tensor memory (the byte of the
+// 32-bit words at scale_a / scale_b that the instruction descriptor names).
+template <int CG>
+__device__ __forceinline__ void mma_mxf8_ss_cg(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                               uint32_t scale_a, uint32_t scale_b, uint32_t accumulate) {
+  if constexpr (CG == 2)
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+        "}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+        "}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
+        : "memory");
+}
+
+// D[tmem] (+)= A[smem] * B[smem] over a pair of CTAs, 16-bit floating point operands (both of one type), fp32 accumulators.
+__device__ __forceinline__ void mma_f16_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                                uint32_t accumulate) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// 32 rows of 16 bytes from shared memory to 32 lanes x 4 columns of tensor memory, the same in all four quarters of the lanes
+// (how the scales of a block-scaled MMA have to lie).  CG = 2: in both CTAs of the pair, each from its own shared
+// memory.  Later MMAs of the issuing thread see the data; mma_commit covers the copy too.
+template <int CG>
+__device__ __forceinline__ void tmem_copy_scales_cg(uint32_t taddr, uint64_t desc) {
+  if constexpr (CG == 2)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+}  // namespace ptx
+}  // namespace qb

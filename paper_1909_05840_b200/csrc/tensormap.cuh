@@ -1,4 +1,4 @@
-// Tensor maps (the descriptors of tiled TMA copies), made on the host.
+// Tensor maps (the descriptors of tiled TMA copies) of the floating-point products, made on the host.
 #pragma once
 
 #include <cuda.h>
@@ -7,12 +7,12 @@
 
 namespace qb {
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+typedef CUresult (*TensormapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-inline qb_status get_encode_fn(EncodeTiledFn* out) {
-  static EncodeTiledFn cached = nullptr;
+inline qb_status tensormap_encoder(TensormapEncodeFn* out) {
+  static TensormapEncodeFn cached = nullptr;
   if (!cached) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult qres;
@@ -21,7 +21,7 @@ inline qb_status get_encode_fn(EncodeTiledFn* out) {
       set_last_error("cuTensorMapEncodeTiled not available from the driver");
       return QB_ERR_CUDA;
     }
-    cached = reinterpret_cast<EncodeTiledFn>(fn);
+    cached = reinterpret_cast<TensormapEncodeFn>(fn);
   }
   *out = cached;
   return QB_OK;
@@ -32,8 +32,8 @@ inline qb_status get_encode_fn(EncodeTiledFn* out) {
 inline qb_status make_matrix_map(CUtensorMap* tm, CUtensorMapDataType type, const void* base, int64_t rows, int64_t cols,
                                  int64_t row_bytes, int box_rows, int box_cols, CUtensorMapSwizzle swizzle,
                                  CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_128B) {
-  EncodeTiledFn encode = nullptr;
-  qb_status st = get_encode_fn(&encode);
+  TensormapEncodeFn encode = nullptr;
+  qb_status st = tensormap_encoder(&encode);
   if (st != QB_OK) return st;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
@@ -52,8 +52,8 @@ inline qb_status make_matrix_map(CUtensorMap* tm, CUtensorMapDataType type, cons
 // groups, 128-byte swizzle.  row_bytes is a multiple of 128 here (a group's part behind a row's end would be the next row's).
 inline qb_status make_group_map(CUtensorMap* tm, CUtensorMapDataType type, int esize, const void* base, int64_t rows, int64_t row_bytes,
                                 int box_rows, int box_groups) {
-  EncodeTiledFn encode = nullptr;
-  qb_status st = get_encode_fn(&encode);
+  TensormapEncodeFn encode = nullptr;
+  qb_status st = tensormap_encoder(&encode);
   if (st != QB_OK) return st;
   const cuuint64_t dims[3] = {(cuuint64_t)(128 / esize), (cuuint64_t)rows, (cuuint64_t)(row_bytes / 128)};
   const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, 128};

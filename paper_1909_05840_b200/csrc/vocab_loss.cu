@@ -25,7 +25,7 @@
 
 #include "common.cuh"
 #include "mbar_wait.cuh"
-#include "ptx.cuh"
+#include "ptx_float.cuh"
 #include "tensormap.cuh"
 
 namespace qb {
@@ -301,11 +301,11 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           const uint64_t b_desc = b_desc0 + (uint64_t)(stage * (kVocabStageBytes >> 4));
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            ptx::mma_f16_ss_cg<2>(d, a_desc + (uint64_t)(a_step * j), b_desc + (uint64_t)(b_step * j), idesc, kb != at.k0 || j != 0 ? 1u : 0u);
+            ptx::mma_f16_ss_pair(d, a_desc + (uint64_t)(a_step * j), b_desc + (uint64_t)(b_step * j), idesc, kb != at.k0 || j != 0 ? 1u : 0u);
           if (kb + 1 < at.k1) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              ptx::mma_f16_ss_cg<2>(d, a_desc + (uint64_t)(a_next + a_step * j), b_desc + (uint64_t)(b_next + b_step * j), idesc, 1u);
+              ptx::mma_f16_ss_pair(d, a_desc + (uint64_t)(a_next + a_step * j), b_desc + (uint64_t)(b_next + b_step * j), idesc, 1u);
           }
           ptx::mma_commit_cg<2>(empty(stage));
           if (++stage == kStages) {
