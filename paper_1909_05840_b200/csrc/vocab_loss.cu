@@ -696,6 +696,10 @@ struct VocabPlan {
 };
 constexpr int64_t kPieceBytes = 48 << 20;  // of g: a launch has enough tiles to level them, and L2 still holds most of what is read again
 
+// Cost of a tile in K blocks: it takes at least as long as its epilogue, about ten (with the K blocks alone 5 tokens x 47,258 x 960
+// backward took 91 us, so 83; 300 tokens x 30,522 x 768 74 and 71).
+static int64_t vocab_tile_cost(int64_t k_blocks) { return std::max<int64_t>(k_blocks, 10) + 2; }
+
 // Columns of a tile of logits in the backward pass (few tokens: in the forward pass too).
 static int64_t vocab_width(int64_t T) { return T <= kFewTokens ? up(T, 32) * 32 : kVocabTile; }
 
@@ -713,7 +717,8 @@ static VocabPlan plan_vocab(int64_t T, int64_t V, int64_t D, int pairs, size_t b
     // grad_h's contraction over the piece is split where a tile of it would outlast the launch
     // (blocks of the first piece, whose splits are what is stored and summed; no piece has more)
     const int64_t blocks = up(std::min(p.rows, V), 64), v_tiles = p.rows / 256;
-    const int64_t work = t_tiles * d_tiles * blocks + v_tiles * d_tiles * (Tp / 64) + (p.pieces > 1 ? v_tiles * t_tiles * up(D, 64) : 0);
+    const int64_t work = t_tiles * d_tiles * blocks + v_tiles * d_tiles * vocab_tile_cost(Tp / 64) +
+                         (p.pieces > 1 ? v_tiles * t_tiles * vocab_tile_cost(up(D, 64)) : 0);
     p.k_split = std::min(blocks, std::max<int64_t>(16, work / pairs / 2));
     p.splits = up(blocks, p.k_split);
     p.k_split = up(up(blocks, p.splits), 2) * 2;
@@ -936,7 +941,7 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
         // every split of the first piece stores its slab; what a shorter last piece lacks adds nothing
         p.k_end = (int32_t)up(rows, 64);
         p.b_row0 = (int32_t)v0;
-        add(p, (int64_t)up(p.k_end, p.k_blocks) * p.split_tiles, p.k_blocks + 2);
+        add(p, (int64_t)up(p.k_end, p.k_blocks) * p.split_tiles, vocab_tile_cost(p.k_blocks));
       }
       if (grad_w) {
         p = VocabProblem{};
@@ -949,7 +954,7 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
         p.n_tiles = d_tiles;
         p.split_tiles = (int32_t)up(rows, 256) * d_tiles;
         p.k_blocks = p.k_end = (int32_t)(Tp / 64);
-        add(p, p.split_tiles, p.k_blocks + 2);
+        add(p, p.split_tiles, vocab_tile_cost(p.k_blocks));
       }
     }
     if (i < plan.pieces) {
@@ -966,7 +971,7 @@ extern "C" qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w
       p.n_tiles = t_tiles;
       p.split_tiles = (int32_t)up(rows, 256) * t_tiles;
       p.k_blocks = p.k_end = (int32_t)up(D, 64);
-      add(p, p.split_tiles, p.k_blocks + 2);
+      add(p, p.split_tiles, vocab_tile_cost(p.k_blocks));
     }
     if (gp.count == 0) continue;
     if ((st = few ? launch_vocab<false, true>(gp, pairs, stream) : launch_vocab<false, false>(gp, pairs, stream)) != QB_OK) return st;
