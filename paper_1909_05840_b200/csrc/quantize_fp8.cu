@@ -7,7 +7,8 @@
 // max|x| is taken on the bit patterns (as unsigned integers they order like the magnitudes, infinities and NaN above every
 // finite value), so that one integer reduction gives the maximum and says whether the block is finite.
 //
-// Bound by memory: x is read once; 1 byte per value and form is written, plus 1/128 for the scales.
+// Bound by memory: x is read once; 1 byte per value and form is written, plus 1/128 for the scales.  24,576 x 4,096 bfloat16: rows 46 us
+// (6.6 TB/s, the copy bandwidth), both forms at once 73 us (5.5 TB/s; fp32 95 us, 6.4 TB/s), weights with both forms 64 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

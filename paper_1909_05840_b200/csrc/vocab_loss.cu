@@ -1,8 +1,8 @@
 // qb_vocab_loss, qb_vocab_loss_backward: softmax cross entropy of hidden states h [T][D] over a vocabulary w [V][D], logits
 // z = h w^T + bias, without keeping the logits.
 //
-// Forward: tiles of 256 tokens x 256 words are multiplied on the tensor cores and reduced to a maximum and a sum of exponentials
-// per token where they lie (tensor memory -> registers); a second kernel joins the tiles of a token.
+// Forward: tiles of 256 tokens x 256 words (up to 128 tokens: of 256 words x the tokens) are multiplied on the tensor cores and reduced
+// to a maximum and a sum of exponentials per token on their way out of tensor memory; a second kernel joins the tiles of a token.
 // Backward: with the forward pass's lse, g[v][t] = grad_loss[t] * (exp(z[t][v] - lse[t]) - [v = target[t]]) needs no reduction.
 // The vocabulary is taken in pieces: for one piece g is formed (the logits again) and rounded to bfloat16 into the workspace,
 // transposed, while the two products of the piece before it,
@@ -13,9 +13,13 @@
 //
 // One product kernel for all of it: CTA pairs (tcgen05 cta_group::2, kind::f16, bfloat16 operands, fp32 accumulators), tiles of
 // 256 x 256, K blocks of 64, a ring of three stages of two blocks (64 KB per CTA), two accumulators in tensor memory.  An operand lies in
-// shared memory as the tensor has it: contraction along its rows (K-major) or down its columns (MN-major),
-// so that nothing is transposed in memory.  12 warps: 0 loads (TMA), 1 issues MMAs,
-// 4..11 epilogue, two per TMEM lane quarter.  Every wait is bounded, as in qb_gemm.
+// shared memory as the tensor has it: contraction along its rows (K-major) or down its columns (MN-major), so that nothing is
+// transposed in memory.  12 warps: 0 loads (TMA), 1 issues MMAs, 4..11 epilogue, two per TMEM lane quarter.  Every wait is
+// bounded, as in qb_gemm.
+//
+// Bound by the tensor cores: 4,096 x 30,522 x 768 forward 119 us (1,613 TFLOP/s; the MMAs alone 109); 3,686 x 30,522 x 1,024 forward 149,
+// backward 505 us (1,372 TFLOP/s over the three products; the MMAs alone 381, loads alone 284).  With few tokens by reading w: 77
+// tokens x 30,522 x 768 forward 15.3 us (w alone 7.3).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
