@@ -317,6 +317,24 @@ def test_captured_and_on_another_stream(ws):
 
 
 @pytest.mark.gpu
+def test_outputs_are_ordinary_tensors(ws):
+    """Codes and scales share an allocation: they outlive each other, and views, copies and in-place calls work on them."""
+    x, w = rows_of(200, 300, 1), rows_of(40, 300, 2)
+    q, s, qt, st = qb.quantize_fp8(x, ws, transposed=True)
+    want = [t.clone() for t in (q, s, qt, st)]
+    y = qb.gemm_fp8(q, s, *qb.quantize_fp8_weights(w, ws), None, ws)
+    del q, qt
+    for _ in range(20):
+        torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(s, want[1]) and torch.equal(st, want[3])
+    assert torch.equal(y, qb.gemm_fp8(want[0], s, *qb.quantize_fp8_weights(w, ws), None, ws))
+    assert s.is_contiguous() and s.view(-1).numel() == qb.fp8_scale_bytes(200, 300) and not s.requires_grad
+    s.fill_(127)
+    assert torch.equal(want[0].cpu().float(), want[0].float().cpu()) and (s == 127).all()
+    assert torch.equal(want[2].float()[:, :200], want[2][:, :200].float())
+
+
+@pytest.mark.gpu
 def test_python_refusals(ws):
     x = rows_of(8, 256, 1)
     q, s = qb.quantize_fp8(x, ws)
