@@ -416,7 +416,7 @@ enum { QB_E4M3 = 0, QB_E5M2 = 1 };
  * fp32, y fp32 (QB_F32) or rounded to nearest even once (QB_BF16).  K is the codes' row length (a multiple of 128).  The formats
  * of a and b may differ.  For a linear y = x W^T: forward a = x, b = W; grad_x: a = grad_y, b = W transposed; grad_W: a = grad_y
  * transposed, b = x transposed.
- *   bias dev fp32 [N] or NULL (read);  y dev [M][N], aligned to its elements (written)
+ *   bias dev fp32 [N] or NULL (read);  y dev [M][N] (written); both aligned to their elements
  * M, N and K up to QB_MAX_MN.  Any workspace will do; one of 1024 + n * 4 * M * N bytes lets a product of few tiles over a long K (the
  * gradient of a small weight matrix over many tokens) be summed in up to n parts side by side, always in the same order.
  */

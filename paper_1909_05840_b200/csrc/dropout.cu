@@ -194,7 +194,7 @@ static qb_status launch_dropout(const void* x, const void* residual, void* y, in
                        : (drop ? (residual ? dropout_kernel<T, false, true, true> : dropout_kernel<T, false, true, false>)
                                : (residual ? dropout_kernel<T, false, false, true> : dropout_kernel<T, false, false, false>));
   constexpr int64_t per_block = (int64_t)kDropThreads * kDropUnroll * (16 / sizeof(T));
-  const unsigned grid = (unsigned)((n + per_block - 1) / per_block);  // n <= 2^40: at most 2^28 blocks
+  const unsigned grid = (unsigned)((n + per_block - 1) / per_block);  // n <= 2^40: at most 2^29 blocks
   QB_CUDA_TRY(launch_kernel<kMostL1>(kernel, grid, kDropThreads, 0, stream, 1, false, static_cast<const T*>(x), static_cast<const T*>(residual),
                             static_cast<T*>(y), n, a));
   return QB_OK;

@@ -509,12 +509,12 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
     return QB_ERR_INVALID;
   }
   if (K % 128 != 0 || !aligned16(a) || !aligned16(b) || !aligned16(a_scale) || !aligned16(b_scale) ||
-      reinterpret_cast<uintptr_t>(y) % (out_type == QB_F32 ? 4 : 2) != 0) {
-    set_last_error("qb_gemm_fp8: K must be a multiple of 128, codes and scales 16-byte aligned, y aligned to its elements");
+      reinterpret_cast<uintptr_t>(bias) % 4 != 0 || reinterpret_cast<uintptr_t>(y) % (out_type == QB_F32 ? 4 : 2) != 0) {
+    set_last_error("qb_gemm_fp8: K must be a multiple of 128, codes and scales 16-byte aligned, bias and y aligned to their elements");
     return QB_ERR_ALIGN;
   }
-  if (!ws || ws_bytes < kWsMinBytes) {
-    set_last_error("qb_gemm_fp8: workspace null or too small");
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 4 != 0 || ws_bytes < kWsMinBytes) {
+    set_last_error("qb_gemm_fp8: workspace null, not aligned or too small");
     return QB_ERR_WORKSPACE;
   }
   const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m; };

@@ -515,7 +515,7 @@ static qb_status quantize_fp8_entry(const char* who, const void* x, int type, in
     return QB_ERR_ALIGN;
   }
   const size_t need = sums ? qb_fp8_sums_workspace_bytes(M, K) : kWsMinBytes;
-  if (!ws || ws_bytes < need || (sums && reinterpret_cast<uintptr_t>(ws) % 4 != 0)) {
+  if (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % 4 != 0) {
     set_last_error("%s: workspace null, not aligned or smaller than %zu bytes", who, need);
     return QB_ERR_WORKSPACE;
   }

@@ -47,7 +47,7 @@ def test_fp8(lib):
             assert call(**bad) == qb.QB_ERR_INVALID, bad
         for bad in (dict(x=A + 2), dict(type=1, x=A + 1), dict(q=A + 8), dict(s=A + 4), dict(qt=A + 1), dict(st=A + 2)):
             assert call(**bad) == qb.QB_ERR_ALIGN, bad
-        for bad in (dict(ws=None), dict(ws_bytes=255)):
+        for bad in (dict(ws=None), dict(ws_bytes=255), dict(ws=A + 2)):
             assert call(**bad) == qb.QB_ERR_WORKSPACE, bad
     ok = dict(a=A, sa=A, fa=0, b=A, sb=A, fb=1, bias=None, M=8, N=9, K=128, out=0, y=A, ws=A, ws_bytes=256)
 
@@ -56,9 +56,9 @@ def test_fp8(lib):
     for bad in (dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(y=None), dict(M=0), dict(N=0), dict(K=0), dict(K=(1 << 24) + 128), dict(M=1 << 24, N=1 << 24), dict(M=1 << 24, K=1 << 24),
                 dict(M=(1 << 24) + 1), dict(N=(1 << 24) + 1), dict(fa=2), dict(fb=-1), dict(out=2), dict(out=-1)):
         assert gemm(**bad) == qb.QB_ERR_INVALID, bad
-    for bad in (dict(K=130), dict(a=A + 8), dict(b=A + 8), dict(sa=A + 8), dict(sb=A + 8), dict(y=A + 2), dict(out=1, y=A + 1)):
+    for bad in (dict(K=130), dict(a=A + 8), dict(b=A + 8), dict(sa=A + 8), dict(sb=A + 8), dict(y=A + 2), dict(out=1, y=A + 1), dict(bias=A + 2)):
         assert gemm(**bad) == qb.QB_ERR_ALIGN, bad
-    for bad in (dict(ws=None), dict(ws_bytes=255)):
+    for bad in (dict(ws=None), dict(ws_bytes=255), dict(ws=A + 2)):
         assert gemm(**bad) == qb.QB_ERR_WORKSPACE, bad
 
 
