@@ -8,7 +8,7 @@
 // finite value), so that one integer reduction gives the maximum and says whether the block is finite.
 //
 // Bound by memory: x is read once; 1 byte per value and form is written, plus 1/128 for the scales.  24,576 x 4,096 bfloat16: rows 46 us
-// (6.6 TB/s, the copy bandwidth), both forms at once 73 us (5.5 TB/s; fp32 95 us, 6.4 TB/s), weights with both forms 64 us.
+// (6.6 TB/s, the copy bandwidth), both forms at once 68 us (5.9 TB/s; fp32 95 us, 6.4 TB/s), weights with both forms 64 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -294,8 +294,9 @@ __global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const T* x, Fp8Ar
 // SQUARE: one scale for the tile (weights), else one per row for the codes and one per column for the transposed codes.
 // The transposed codes cross shared memory, where a thread's 16 rows of a column are one 16-byte store, and leave as whole
 // lines.
-template <class T, int FMT, bool SQUARE>
-__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) fp8_tile_kernel(const T* x, Fp8Args a) {
+// BLOCKS per SM: what a block waits for is hidden by the others.
+template <class T, int FMT, bool SQUARE, int BLOCKS>
+__global__ void __launch_bounds__(256, BLOCKS) fp8_tile_kernel(const T* x, Fp8Args a) {
   typedef typename Quad<T>::Mag Mag;
   typedef typename Quad<T>::Pair Pair;
   __shared__ Mag tops[8][32];
@@ -480,20 +481,27 @@ __global__ void __launch_bounds__(256) fp8_sums_kernel(const float* parts, int t
 }
 
 template <class T, int FMT>
-static qb_status launch_fp8(const T* x, const Fp8Args& a, bool square, cudaStream_t stream) {
+static qb_status launch_fp8(const T* x, const Fp8Args& a, bool square, int sms, cudaStream_t stream) {
   if (!square && !a.qt) {
     const int64_t items = a.M * fp8_scale_words(a.Kp), blocks = (items + kRowThreads / 16 - 1) / (kRowThreads / 16);
     QB_CUDA_TRY(launch_kernel<kMostL1>(fp8_rows_kernel<T, FMT>, (unsigned)blocks, kRowThreads, 0, stream, 1, false, x, a));
     return QB_OK;
   }
-  auto kernel = square ? fp8_tile_kernel<T, FMT, true> : fp8_tile_kernel<T, FMT, false>;
-  QB_CUDA_TRY(launch_kernel(kernel, (unsigned)((a.Mp / 128) * (a.Kp / 128)), 256, 0, stream, 1, false, x, a));
+  const int64_t tiles = (a.Mp / 128) * (a.Kp / 128);
+  // 16 bits: three blocks per SM where they take all tiles at once, else four (bfloat16, rows and columns, 18,944 x 384: 6.3 us, with
+  // four 7.5; 24,576 x 4,096: 73.3 and 68.2; weights 4.9 and 5.6, 64.5 and 63.6).  fp16's rows and columns do not fit 64 registers.
+  constexpr bool kWide = sizeof(T) == 4;
+  constexpr int kFew = kWide ? 2 : 3, kMany = kWide ? 2 : 4, kManyBoth = std::is_same_v<T, __nv_bfloat16> ? 4 : kFew;
+  const bool many = tiles > (int64_t)kFew * sms;
+  auto kernel = square ? (many ? fp8_tile_kernel<T, FMT, true, kMany> : fp8_tile_kernel<T, FMT, true, kFew>)
+                       : (many ? fp8_tile_kernel<T, FMT, false, kManyBoth> : fp8_tile_kernel<T, FMT, false, kFew>);
+  QB_CUDA_TRY(launch_kernel(kernel, (unsigned)tiles, 256, 0, stream, 1, false, x, a));
   return QB_OK;
 }
 template <class T>
-static qb_status launch_fp8_format(const void* x, int format, const Fp8Args& a, bool square, cudaStream_t stream) {
-  return format == QB_E4M3 ? launch_fp8<T, QB_E4M3>(static_cast<const T*>(x), a, square, stream)
-                           : launch_fp8<T, QB_E5M2>(static_cast<const T*>(x), a, square, stream);
+static qb_status launch_fp8_format(const void* x, int format, const Fp8Args& a, bool square, int sms, cudaStream_t stream) {
+  return format == QB_E4M3 ? launch_fp8<T, QB_E4M3>(static_cast<const T*>(x), a, square, sms, stream)
+                           : launch_fp8<T, QB_E5M2>(static_cast<const T*>(x), a, square, sms, stream);
 }
 
 static qb_status quantize_fp8_entry(const char* who, const void* x, int type, int64_t M, int64_t K, int format, uint8_t* q, uint8_t* scale,
@@ -519,7 +527,8 @@ static qb_status quantize_fp8_entry(const char* who, const void* x, int type, in
     set_last_error("%s: workspace null, not aligned or smaller than %zu bytes", who, need);
     return QB_ERR_WORKSPACE;
   }
-  qb_status st = require_sm100(nullptr);
+  int sms = 0;
+  qb_status st = require_sm100(&sms);
   if (st != QB_OK) return st;
   Fp8Args a;
   a.M = M;
@@ -535,9 +544,9 @@ static qb_status quantize_fp8_entry(const char* who, const void* x, int type, in
   a.vector = reinterpret_cast<uintptr_t>(x) % (4 * size) == 0 && K % 4 == 0;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   switch (type) {
-    case QB_F32: st = launch_fp8_format<float>(x, format, a, square, stream); break;
-    case QB_BF16: st = launch_fp8_format<__nv_bfloat16>(x, format, a, square, stream); break;
-    default: st = launch_fp8_format<__half>(x, format, a, square, stream);
+    case QB_F32: st = launch_fp8_format<float>(x, format, a, square, sms, stream); break;
+    case QB_BF16: st = launch_fp8_format<__nv_bfloat16>(x, format, a, square, sms, stream); break;
+    default: st = launch_fp8_format<__half>(x, format, a, square, sms, stream);
   }
   if (st != QB_OK || !sums) return st;
   QB_CUDA_TRY(launch_kernel(fp8_sums_kernel, (unsigned)((K + 31) / 32), 256, 0, stream, 1, false, a.sums, (int)(Mp / 128), (int)K, sums));

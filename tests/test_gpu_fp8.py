@@ -91,6 +91,24 @@ def test_quantize(ws, M, K, kind, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M,K", [(2690, 2690), (2561, 2817)])
+def test_many_tiles(ws, M, K, kind):
+    """More tiles than fit the device at once; rows that are aligned to four values and that are not; the columns' sums."""
+    x = rows_of(M, K, M + K, kind)
+    q = qb.quantize_fp8(x, torch.zeros(qb.fp8_sums_workspace_bytes(M, K), dtype=torch.uint8, device="cuda"), E4M3, True, want_sums=True)
+    check_codes(q[0], q[1], x, E4M3, 1)
+    check_codes(q[2], q[3], x.t().contiguous(), E4M3, 1)
+    # each of the M - 1 additions rounds by half a step of a partial sum, which is at most the sum of magnitudes
+    bound = x.double().abs().sum(dim=0) * (M * 2.0**-24)
+    assert ((q[4].double() - x.double().sum(dim=0)).abs() <= bound).all()
+    w = qb.quantize_fp8_weights(x, ws, E5M2, transposed=True)
+    check_codes(w[0], w[1], x, E5M2, 128)
+    check_codes(w[2], w[3], x.t().contiguous(), E5M2, 128)
+    assert qb.read_status(ws) == qb.QB_OK
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [E4M3, E5M2])
 def test_borders(ws, dtype):
     """Maxima at and beside the format's largest value, the ends of fp32, zeros, ties."""
