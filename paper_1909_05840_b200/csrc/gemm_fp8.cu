@@ -307,7 +307,11 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
     for (int t = group; t < gp.tiles; t += groups, ++it) {
       const int a = it & 1;
       const Fp8Tile<BT, CG> tile(gp, t);
-      const int m0 = tile.m0 + (int)rank * 128 + quarter * 32, n0 = tile.n0;
+      int m0 = tile.m0 + (int)rank * 128 + quarter * 32, n0 = tile.n0;
+      int chunks = m0 < gp.M ? max(0, min(tile.width / kCols, (gp.N - n0 + kCols - 1) / kCols)) : 0;
+      // formed before the wait: the compiler would do the divisions behind it, where the next tile's products wait for this
+      // tile's first columns (18,944 x 4,096 x 1,024: 68.7 us, so 68.2)
+      asm volatile("" : "+r"(m0), "+r"(n0), "+r"(chunks));
       bias_tile[a * 256 + e] = gp.bias && e < BT && n0 + e < gp.N ? gp.bias[n0 + e] : 0.0f;
       const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
       if (fp8_epilogue_sync_or(!ok)) {  // publishes the bias, and all eight warps give up together
@@ -317,7 +321,6 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
       }
       ptx::tcgen05_fence_after_sync();
       const uint32_t acc = lanes + (a ? Cfg::kAcc1 : 0);
-      const int chunks = m0 < gp.M ? max(0, min(tile.width / kCols, (gp.N - n0 + kCols - 1) / kCols)) : 0;
       // accumulator 0 shares its last 32 columns, accumulator 1 its first: they are read first, by the quarter's first warp
       const bool down = Cfg::kOverlap && a == 0;
       if (Cfg::kOverlap && half == 0 && (down ? chunks < BT / kCols : chunks == 0)) arrive(overlap_read);
