@@ -11,17 +11,19 @@
 //   warp 0        TMA producer (one lane): codes of A and B (128-byte swizzle, K block of 128), every fourth block the scales
 //   warp 1        issues tcgen05.cp (scales) and tcgen05.mma, owns the tensor memory (one lane)
 //   warps 2..3    idle
-//   warps 4..11   epilogue, two per TMEM lane quarter: tcgen05.ld -> bias -> round -> shared memory -> whole lines of y
+//   warps 4..11   epilogue, two per TMEM lane quarter: tcgen05.ld -> bias -> round -> shared memory -> TMA store
 // A tile is 128 rows of A per CTA x BT rows of B; TMEM lane = row of A, column = row of B.  Large products run as CTA pairs
 // (cta_group::2, 256 x 256): each CTA stages its own 128 rows of A and half of B's rows.  No load is multicast.
 // Two accumulators, so that the epilogue of a tile overlaps the products of the next.  At BT = 256 they and the scales
 // do not fit the 512 columns side by side: the accumulators overlap by 32 columns, which the epilogue reads first.
 // Every wait is bounded: on expiry the CTA records QB_ERR_TIMEOUT and leaves through the normal exit path.
 //
-// Bound by the tensor cores for long K (24,576 x 1,024 x 4,096: bfloat16 out 75 us, 2,750 TFLOP/s, of which the MMAs alone take 62 us;
-// fp32 out 81), by a part per tile for short K (5,003 x 2,304 x 768: 12.0 us; a tile of pairs takes 1.3 us beside its K blocks) and by
-// writing y (24,576 x 4,096 x 1,024: 86 us, 74 without the stores).  The epilogue sends y through shared memory so that every store is
-// of whole lines; rows that are not 16-byte aligned are stored by words (6,235 x 3,501 x 753: 40 us, with 3,504 columns 22).
+// Bound by loads for long K (24,576 x 1,024 x 4,096: bfloat16 out 75 us, 2,750 TFLOP/s, of which the MMAs alone take 62 us, fp32 out
+// 81: a K block of a pair is 64 KB, and comes at 50 to 60 bytes per clock and SM), by the epilogue up to K = 768 (5,003 x 2,304 x
+// 768: 11.4 us) and by writing y (24,576 x 4,096 x 1,024: 88 us, 74 without the stores).  y leaves by TMA: staging and store pipes are
+// what the epilogue waits for (18,944 x 4,096, K = 128 46.4 us with stores by the warps, 40.4 by TMA; 384 51.0 and 43.8; 768 59.2 and
+// 58.0; 1,024 69.1 and 71.1; 2,048 120.1 and 119.7).  Rows that are not 16-byte aligned are stored by words (6,235 x 3,501 x 753: 40
+// us, with 3,504 columns 22).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -40,6 +42,7 @@ struct Fp8Params {
   CUtensorMap tma, tmb;    // codes, box 128 bytes of K x the CTA's rows
   CUtensorMap tmb_half;    // pairs: B's rows for a tile of half the width
   CUtensorMap tmsa, tmsb;  // scales as rows of 512 bytes
+  CUtensorMap tmy;         // y (or the splits' parts, one after the other) in boxes of 32 rows x 128 bytes
   const float* bias;
   void* y;
   void* ws;
@@ -50,7 +53,7 @@ struct Fp8Params {
   int32_t split_blocks; // blocks of 128 of K per split, a multiple of 4 where there are several
   int32_t words;        // rows of 512 bytes of scales per 128 rows of codes
   int32_t a_last, b_last;  // last block of 128 rows of A's and of B's scales
-  int32_t vector;       // 1: rows of y are 16-byte aligned
+  int32_t tma_store;    // 1: rows of y are 16-byte aligned
   uint32_t idesc;       // fp8_idesc
 };
 
@@ -337,7 +340,8 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
         if (Cfg::kOverlap && i == 0 && (!down || chunks == BT / kCols)) arrive(overlap_read);
         if (i + 2 >= chunks) arrive(acc_empty(a));
         const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + a * 256 + c0);
-        __syncwarp();  // the chunk before has left the buffer
+        if (lane == 0) ptx::tma_store_wait_read0();  // the chunk before has left the buffer
+        __syncwarp();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {  // 16 bytes of the row at a time; the swizzle keeps the lanes on different banks
           uint4 w;
@@ -365,15 +369,12 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
         __syncwarp();
         const int rows = min(32, gp.M - m0);
         const size_t first_row = (size_t)tile.split * gp.M;
-        if (gp.vector) {  // 16 bytes a lane, four whole lines a store
-          constexpr int kPiece = BF16 ? 8 : 4;  // columns in 16 bytes
-          const int piece = lane & 7, col = n0 + c0 + piece * kPiece;
-          uint8_t* const to = static_cast<uint8_t*>(gp.y) + ((first_row + m0) * gp.N + col) * (16 / kPiece);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = 4 * i + (lane >> 3);
-            const uint4 w = *reinterpret_cast<const uint4*>(buf + r * 128 + ((piece ^ (r & 7)) << 4));
-            if (r < rows && col < gp.N) *reinterpret_cast<uint4*>(to + (size_t)r * gp.N * (16 / kPiece)) = w;
+        if (gp.tma_store) {
+          ptx::fence_proxy_async_smem();  // every lane: its own stores
+          __syncwarp();
+          if (lane == 0) {
+            ptx::tma_store_3d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0, tile.split);
+            ptx::tma_store_commit();
           }
         } else if constexpr (BF16) {  // rows of y of any alignment: a row at a time, the lanes on consecutive words of it
           const int cols = min(kCols, gp.N - n0 - c0);
@@ -405,6 +406,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1) gemm_fp8_kernel(const __grid_c
         }
       }
     }
+    if (lane == 0) ptx::tma_store_wait_read0();  // the buffers are in use until then
   }
   if (timed_out) {
     *abort_flag = 1;
@@ -543,7 +545,12 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
   if ((st = make_matrix_map(&gp.tmsb, u32, b_scale, up(N, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
   const bool split = choice.splits > 1;
   float* const parts = reinterpret_cast<float*>(static_cast<char*>(ws) + head);
-  gp.vector = split ? N % 4 == 0 : N * (out_type == QB_F32 ? 4 : 2) % 16 == 0 && aligned16(y);
+  const bool bf16 = out_type == QB_BF16 && !split;
+  gp.tma_store = N * (bf16 ? 2 : 4) % 16 == 0 && (split || aligned16(y));
+  gp.tmy = gp.tma;
+  if (gp.tma_store && (st = make_parts_map(&gp.tmy, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, split ? parts : y,
+                                           choice.splits, M, N, N * (bf16 ? 2 : 4), 32, bf16 ? 64 : 32)) != QB_OK)
+    return st;
   gp.bias = split ? nullptr : bias;
   gp.y = split ? parts : y;
   gp.split_blocks = choice.split_blocks;
@@ -559,7 +566,6 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
   gp.b_last = (int32_t)up(N, 128) - 1;
   gp.idesc = fp8_idesc(a_format, b_format, 128 * cg);
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  const bool bf16 = out_type == QB_BF16 && !split;
   if (cg == 2) st = bf16 ? launch_gemm_fp8<256, 2, true>(gp, sms, stream) : launch_gemm_fp8<256, 2, false>(gp, sms, stream);
   else if (bt == 128) st = bf16 ? launch_gemm_fp8<128, 1, true>(gp, sms, stream) : launch_gemm_fp8<128, 1, false>(gp, sms, stream);
   else st = bf16 ? launch_gemm_fp8<64, 1, true>(gp, sms, stream) : launch_gemm_fp8<64, 1, false>(gp, sms, stream);

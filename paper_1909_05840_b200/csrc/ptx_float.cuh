@@ -54,6 +54,13 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* 
       : "memory");
 }
 
+// tma_store_2d for a tensor of three dimensions.
+__device__ __forceinline__ void tma_store_3d(const void* tmap, uint32_t src_smem, int32_t x, int32_t y, int32_t z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(tmap)),
+               "r"(src_smem), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+
 // D[tmem] (+)= (A[smem] * scale_a) * (B[smem] * scale_b), 8-bit floating point operands, fp32 accumulators; one 2^(e - 127)
 // per row of A and of B for the instruction's 32 elements of K, its byte e taken from tensor memory (the byte of the
 // 32-bit words at scale_a / scale_b that the instruction descriptor names).
