@@ -18,7 +18,7 @@
 // bounded, as in qb_gemm.
 //
 // Bound by the tensor cores: 4,096 x 30,522 x 768 forward 119 us (1,613 TFLOP/s; the MMAs alone 109); 3,686 x 30,522 x 1,024 forward 149,
-// backward 505 us (1,372 TFLOP/s over the three products; the MMAs alone 381, loads alone 284).  With few tokens by reading w: 77
+// backward 502 us (1,380 TFLOP/s over the three products; the MMAs alone 381, loads alone 284).  With few tokens by reading w: 77
 // tokens x 30,522 x 768 forward 15.3 us (w alone 7.3).
 #include <cuda.h>
 #include <cuda_bf16.h>
