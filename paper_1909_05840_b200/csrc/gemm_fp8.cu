@@ -469,17 +469,19 @@ struct Fp8Choice {
   int cg, bt;
   int32_t tiles, whole, splits, split_blocks;
 };
-// The cheapest by the costs of a tile, in hundredths of a microsecond: a part per block of 128 of K and a fixed part, fitted to the
-// times of whole rounds (24,576 x 1,024 x 4,096 and 18,944 x 4,096 x 1,024: pairs 76.6 and 66.9 us, 128 columns 96.2 and 86.3, 64
-// columns 131.7 and 119.6).  A last round that fills at most half of the pairs is cut into tiles of half the width, which take
-// about 0.7 of the time (6,144 x 1,024 x 4,096, 96 tiles: 25.4 -> 22.1 us).  Where a long K meets few tiles, K is split into
-// runs that are a multiple of 512 (a word of scales), whose sums a second kernel joins: that costs its launch and the traffic of
-// the parts.
+// The cheapest by what a launch and each of its rounds of tiles take, in hundredths of a microsecond: a tile a part per block of 128
+// of K and a fixed part, but no less than its epilogue, the launch the time until the first tile and of the last epilogue.  Fitted
+// to M = 18,944, 1 to 16 rounds, bfloat16 out (K = 128, 768, 4,096; four rounds of pairs 12.1, 16.2 and 58.0 us, eight of 128 columns
+// 11.9, 18.9 and 74.8, 16 of 64 columns 18.3, 27.1 and 107).  With few rounds of short tiles the smaller ones are ahead: 2,048 x 2,304 x
+// 768 6.5 us in two rounds of 128 columns, 7.6 in one of pairs; 5,003 x 2,304 x 768 12.0 by pairs, 12.9 by 128 columns.  A last round
+// that fills at most half of the pairs is cut into tiles of half the width, which take about 0.7 of the time (6,144 x 1,024 x 4,096, 96
+// tiles: 25.4 -> 22.1 us).  Where a long K meets few tiles, K is split into runs that are a multiple of 512 (a word of
+// scales), whose sums a second kernel joins: that costs its launch and the traffic of the parts.
 static Fp8Choice choose_fp8(int64_t M, int64_t N, int64_t K, int sms, size_t scratch) {
   const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m; };
   static constexpr struct {
-    int cg, bt, block, fixed;
-  } kForms[] = {{2, 256, 34, 126}, {1, 128, 24, 64}, {1, 64, 18, 38}};
+    int cg, bt, block, fixed, least, launch;
+  } kForms[] = {{2, 256, 41, 20, 220, 480}, {1, 128, 27, 37, 120, 310}, {1, 64, 20, 25, 100, 300}};
   const int64_t blocks = K / 128;
   Fp8Choice best = {};
   int64_t best_cost = 0;
@@ -489,9 +491,9 @@ static Fp8Choice choose_fp8(int64_t M, int64_t N, int64_t K, int sms, size_t scr
     for (int64_t splits = 1; splits == 1 || (4 * splits <= blocks && tiles * (splits - 1) < groups && splits * M * N * 4 <= (int64_t)scratch); ++splits) {
       const int64_t run = splits == 1 ? blocks : up(up(blocks, splits), 4) * 4;
       if (up(blocks, run) != splits) continue;
-      const int64_t tile = f.block * run + f.fixed, all = tiles * splits, last = all % groups;
+      const int64_t tile = std::max<int64_t>(f.block * run + f.fixed, f.least), all = tiles * splits, last = all % groups;
       const bool halves = f.cg == 2 && splits == 1 && last > 0 && 2 * last <= groups;
-      const int64_t cost = (all / groups) * tile + (halves ? tile * 7 / 10 : (last > 0 ? tile : 0)) + (splits > 1 ? 250 + splits * M * N / 7500 : 0);
+      const int64_t cost = f.launch + (all / groups) * tile + (halves ? tile * 7 / 10 : (last > 0 ? tile : 0)) + (splits > 1 ? 250 + splits * M * N / 7500 : 0);
       if (best.cg == 0 || cost < best_cost) {
         best_cost = cost;
         best = {f.cg, f.bt, (int32_t)(halves ? all + last : all), (int32_t)(halves ? all - last : all), (int32_t)splits, (int32_t)run};
