@@ -96,7 +96,7 @@ struct VocabParams {
   const int32_t* targets;
   const float* lse;
   const float* grad_loss;
-  float2* part;         // forward: [2 * word tile + half][T], maximum and sum (both for powers of two)
+  float2* part;         // forward: [2 * word tile + half][T], maximum and sum of exponentials
   float* z_target;      // forward: [T]
   float* part_bias;     // backward: [2 * token tile + half][V], or NULL
   void* ws;
@@ -129,6 +129,22 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// e^d for a difference of logits.  The difference comes first and is scaled then: logits that are scaled before they are subtracted
+// are rounded at their own size (at -5e9, a finite mask, by hundreds, so that e^0 became infinite or 0), and those below -2.4e38
+// have no scaled value.
+__device__ __forceinline__ float exp_fast(float d) { return exp2_fast(d * kLog2e); }
+// sum of e^(z - base), two values an instruction
+__device__ __forceinline__ float exp_sum(const float (&z)[32], float base) {
+  const uint64_t base2 = ptx::pack_f32x2(-base, -base), log2e2 = ptx::pack_f32x2(kLog2e, kLog2e);
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    const float2 d = ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(z[j], z[j + 1]), base2), log2e2));
+    s[j & 3] += exp2_fast(d.x);
+    s[(j & 3) + 1] += exp2_fast(d.y);
+  }
+  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
@@ -344,7 +360,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
       // what the tile's columns need: words' biases (forward), or the tokens' lse, gradient and target
       if (FORWARD && !FEW) {
         const int v = col0 + e;
-        tile_cols[e] = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] * kLog2e : 0.0f);
+        tile_cols[e] = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] : 0.0f);
       } else if (!FORWARD && pr.kind == kGradZ) {
         const int t = col0 + e;
         float lse = INFINITY, gl = 0.0f;
@@ -434,17 +450,16 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const float4 b = b4[j];
-            z[4 * j] = fmaf(__uint_as_float(v[4 * j]), kLog2e, b.x);
-            z[4 * j + 1] = fmaf(__uint_as_float(v[4 * j + 1]), kLog2e, b.y);
-            z[4 * j + 2] = fmaf(__uint_as_float(v[4 * j + 2]), kLog2e, b.z);
-            z[4 * j + 3] = fmaf(__uint_as_float(v[4 * j + 3]), kLog2e, b.w);
+            const float2 lo = ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_u32x2(v[4 * j], v[4 * j + 1]), ptx::pack_f32x2(b.x, b.y)));
+            const float2 hi = ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_u32x2(v[4 * j + 2], v[4 * j + 3]), ptx::pack_f32x2(b.z, b.w)));
+            z[4 * j] = lo.x;
+            z[4 * j + 1] = lo.y;
+            z[4 * j + 2] = hi.x;
+            z[4 * j + 3] = hi.y;
             most = fmaxf(most, fmaxf(fmaxf(z[4 * j], z[4 * j + 1]), fmaxf(z[4 * j + 2], z[4 * j + 3])));
           }
           const float base = most == -INFINITY ? 0.0f : most;  // nothing but -infinity so far: no difference of infinities
-          float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int j = 0; j < 32; ++j) s[j & 3] += exp2_fast(z[j] - base);
-          sum = sum * exp2_fast(top - base) + ((s[0] + s[1]) + (s[2] + s[3]));
+          sum = sum * exp_fast(top - base) + exp_sum(z, base);
           top = most;
         }
         if (row < gp.T) gp.part[(size_t)(2 * at.n + half) * gp.T + row] = make_float2(top, sum);
@@ -484,12 +499,8 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           float most = fmaxf(z[0], z[1]);
 #pragma unroll
           for (int j = 2; j < 32; j += 2) most = fmaxf(most, fmaxf(z[j], z[j + 1]));
-          // the maximum and the exponents for powers of two; nothing but -infinity: no difference of infinities
-          const float top = most == -INFINITY ? -INFINITY : most * kLog2e, base = most == -INFINITY ? 0.0f : top;
-          float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int j = 0; j < 32; ++j) s[j & 3] += exp2_fast(fmaf(z[j], kLog2e, -base));
-          joined[quarter * kFewTokens + ch * 32 + lane] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+          const float base = most == -INFINITY ? 0.0f : most;  // nothing but -infinity: no difference of infinities
+          joined[quarter * kFewTokens + ch * 32 + lane] = make_float2(most, exp_sum(z, base));
           __syncwarp();
         }
         // the CTA's four quarters of words, joined in order (the next tile's barrier comes before the next writes)
@@ -501,7 +512,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           const float top = fmaxf(fmaxf(q[0].x, q[1].x), fmaxf(q[2].x, q[3].x)), base = top == -INFINITY ? 0.0f : top;
           float s = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s += q[i].y * exp2_fast(q[i].x - base);
+          for (int i = 0; i < 4; ++i) s += q[i].y * exp_fast(q[i].x - base);
           gp.part[(size_t)(2 * at.m + rank) * gp.T + e] = make_float2(top, s);
         }
       } else if (pr.kind == kGradH) {
@@ -635,9 +646,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) vocab_join_kernel(const float
 #pragma unroll
     for (int d = 0; d < kJoinDepth; ++d) most = fmaxf(most, p[d].x);
     const float base = most == -INFINITY ? 0.0f : most;
-    sum *= exp2_fast(top - base);
+    sum *= exp_fast(top - base);
 #pragma unroll
-    for (int d = 0; d < kJoinDepth; ++d) sum += p[d].y * exp2_fast(p[d].x - base);
+    for (int d = 0; d < kJoinDepth; ++d) sum += p[d].y * exp_fast(p[d].x - base);
     top = most;
   }
   joined[warp][lane] = make_float2(top, sum);
@@ -649,8 +660,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) vocab_join_kernel(const float
   const float base = most == -INFINITY ? 0.0f : most;
   sum = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) sum += joined[w][lane].y * exp2_fast(joined[w][lane].x - base);
-  const float l = (most + log2f(sum)) * 0.6931471805599453f;
+  for (int w = 0; w < kJoinWarps; ++w) sum += joined[w][lane].y * exp_fast(joined[w][lane].x - base);
+  const float l = most + logf(sum);
   const int target = targets[t];
   lse[t] = l;
   const bool valid = target >= 0 && target < V;

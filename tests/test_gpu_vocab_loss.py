@@ -204,6 +204,39 @@ def test_words_taken_out_by_their_bias():
     assert loss[3] == float("inf") and torch.isfinite(loss[:3]).all() and torch.isfinite(loss[4:]).all()
 
 
+LOWEST = torch.finfo(torch.float32).min
+
+
+@pytest.mark.parametrize("mask", [-65504.0, -5e9, -1e20, -1e38, LOWEST])
+@pytest.mark.parametrize("T", [1, 77, 128, 129, 300])
+def test_words_masked_by_a_finite_bias(T, mask):
+    """Words under a large finite negative bias (a padded vocabulary's mask), whole tiles of them among others: their probability is below
+    2^-149, so that every result is that of the other words alone."""
+    V, D = 900, 64
+    h, w, b, targets, gl = inputs(T, V, D, ignored=False)
+    out = torch.zeros(V, dtype=torch.bool, device="cuda")
+    out[200:264] = out[330:800] = out[870:] = True
+    out[5] = True
+    b[out] = mask
+    keep = ~out
+    kept = torch.nonzero(keep)[:, 0]
+    place = targets.long() % kept.numel()
+    targets = kept[place].int()
+    ws = qb.vocab_loss_workspace(T, V, D)
+    got, part = run(h, w, b, targets, gl, ws), reference(h, w[keep], b[keep], place.int(), gl)
+    for name in ("loss", "lse", "grad_h"):
+        check(name, got[name], part)
+    assert (got["grad_w"][out] == 0).all() and (got["grad_bias"][out] == 0).all()
+    check("grad_w", got["grad_w"][keep], part)
+    check("grad_bias", got["grad_bias"][keep], part)
+    # a masked target: its loss is the mask's size, to the rounding of the logit, of lse and of their difference
+    targets[0] = 400
+    loss, _ = qb.vocab_loss(h, w, b, targets, ws)
+    want = part["lse"][0][0] - ((h[0].double() * w[400].double()).sum() + mask)
+    assert abs(float(loss[0]) - float(want)) <= abs(mask) * 2.0**-22
+    assert qb.read_status(ws) == qb.QB_OK
+
+
 def test_large_logits():
     """Logits of hundreds: the maximum is taken out before the exponentials."""
     T, V, D = 65, 900, 64
