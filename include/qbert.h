@@ -453,6 +453,9 @@ qb_status qb_dropout(const void* x, int type, int64_t n, double p, const uint64_
  *     z[t][v] = sum_d h[t][d] * w[v][d] + bias[v],   lse[t] = log sum_v exp z[t][v],   loss[t] = lse[t] - z[t][targets[t]]
  * and, with g[t][v] = grad_loss[t] * (exp(z[t][v] - lse[t]) - [v = targets[t]]),
  *     grad_h = g w,   grad_w = g^T h,   grad_bias[v] = sum_t g[t][v].
+ * loss is formed from the difference of two logits, not from lse: it is never below 0, and that of a token which the model is sure of is
+ * good to the rounding of its sum of exponentials (some 2^-20) however large the logits are.  lse is one fp32 number, rounded at its
+ * own size: the backward pass's exp(z - lse) is off by up to |lse| * 2^-24 of itself from this, and is never above 1.
  * The products are accumulated in fp32 and the softmax is held in fp32; g is rounded to bfloat16 for its two products (and not for
  * grad_bias), grad_h and grad_w once more at the end.  The backward pass forms the logits again, a piece of the vocabulary at a
  * time.  The sums' order does not change from call to call.

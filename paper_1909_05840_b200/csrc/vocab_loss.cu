@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         float lse = INFINITY, gl = 0.0f;
         int target = -1;
         if (t < gp.T) {  // three loads at once: the gradient's does not wait for the target
-          lse = gp.lse[t] * kLog2e;
+          lse = gp.lse[t];
           target = gp.targets[t];
           gl = gp.grad_loss[t];
           if (target < 0 || target >= gp.V) gl = 0.0f;
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
         if (row < gp.T) target = gp.targets[row];
       } else if (FORWARD || pr.kind == kGradZ) {
         const int v = gp.v0 + row;
-        bias = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] * (FORWARD ? 1.0f : kLog2e) : 0.0f);
+        bias = v >= gp.V ? -INFINITY : (gp.bias ? gp.bias[v] : 0.0f);
       }
       const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
       if (vocab_epilogue_sync_or(!ok)) {  // publishes the columns' values, and all eight warps give up together
@@ -562,8 +562,10 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
             }
             // Two columns an instruction.  A target among the warp's 32 words is rare, so that the comparisons are made where there is
             // one (both: 4,096 x 30,522 x 768 backward 447 -> 437 us).
+            // z is rounded as in the forward pass, and lse is no less than the largest z: a probability is never above 1, and
+            // p - 1 never has the wrong sign.
             const auto two = [&](uint32_t* x, uint64_t lse, uint64_t w, int k, auto hits, int j) {
-              float2 p = ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_u32x2(x[0], x[1]), log2e2, ptx::add_f32x2(bias2, lse)));
+              float2 p = ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::add_f32x2(ptx::pack_u32x2(x[0], x[1]), bias2), lse), log2e2));
               p.x = exp2_fast(p.x);
               p.y = exp2_fast(p.y);
               uint64_t d;
@@ -661,12 +663,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) vocab_join_kernel(const float
   sum = 0.0f;
 #pragma unroll
   for (int w = 0; w < kJoinWarps; ++w) sum += joined[w][lane].y * exp_fast(joined[w][lane].x - base);
-  const float l = most + logf(sum);
+  const float log_sum = logf(sum);  // sum >= 1: the maximum's own term
   const int target = targets[t];
-  lse[t] = l;
+  lse[t] = most + log_sum;
   const bool valid = target >= 0 && target < V;
   if (target >= V) report_status(ws, QB_ERR_INVALID, t);
-  loss[t] = valid ? l - z_target[t] : 0.0f;
+  // the difference of two logits first: lse - z would leave the rounding of lse, of either sign, of a loss near 0
+  loss[t] = valid ? (most - z_target[t]) + log_sum : 0.0f;
 }
 
 // grad_h = the slabs' sum in bfloat16 (the first `h_blocks` blocks); grad_bias = the tiles' sum (the others).

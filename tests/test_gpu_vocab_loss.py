@@ -237,6 +237,47 @@ def test_words_masked_by_a_finite_bias(T, mask):
     assert qb.read_status(ws) == qb.QB_OK
 
 
+@pytest.mark.parametrize("whole", [True, False])
+@pytest.mark.parametrize("T", [1, 77, 128, 129, 300])
+def test_sure_tokens(T, whole):
+    """Targets that the model is sure of: the loss is never below 0, the gradient at the target never above.
+
+    With whole numbers the logits are exact in fp32 whatever the order of their sums, and bias puts them at 3,000: the loss is then
+    as far off as the sum of e^-d over the differences d to the maximum.  An exponent is d times log2(e), rounded twice (d * 2^-22
+    bounds it), an exponential good to 2^-22, at most eight of them multiplied (2^-19), and the sum's additions 64 + V / 1024 in a
+    chain; the logarithm and the last addition round at 2^-23 and 2^-24 of themselves."""
+    V, D = 1200, 64
+    g = torch.Generator(device="cuda").manual_seed(T)
+    targets = torch.randperm(V, device="cuda", generator=g)[:T].int()
+    sure = torch.randint(0, 3, (T, 1), device="cuda", generator=g)
+    if whole:
+        w = torch.randint(-1, 2, (V, D), device="cuda", generator=g).bfloat16()
+        h = (sure * w[targets.long()] + torch.randint(-1, 2, (T, D), device="cuda", generator=g)).bfloat16()
+        b = 3000 + torch.randint(0, 8, (V,), device="cuda", generator=g) / 4
+    else:
+        w = torch.randn(V, D, device="cuda", generator=g).bfloat16()
+        h = (0.5 * sure * w[targets.long()] + 0.1 * torch.randn(T, D, device="cuda", generator=g)).bfloat16()
+        b = torch.randn(V, device="cuda", generator=g) * 0.1
+    gl = torch.full((T,), 1.0 / T, device="cuda")
+    ws = qb.vocab_loss_workspace(T, V, D)
+    got = run(h, w, b, targets, gl, ws)
+    assert (got["loss"] >= 0).all()
+    z = h.double() @ w.double().t() + b.double()
+    at = targets.long()[:, None]
+    most = z.amax(1)
+    if whole:
+        d = most[:, None] - z
+        total = torch.exp(-d).sum(1)
+        e_log = (torch.exp(-d) * (d * 2.0**-22 + 2.0**-19)).sum(1) / total + (64 + V / 1024) * 2.0**-24 + total.log() * 2.0**-23
+        want = (most - z.gather(1, at)[:, 0]) + torch.log1p((torch.exp(-d).sum(1) - 1).clamp(min=0))
+        assert ((got["loss"].double() - want).abs() <= e_log + want * 2.0**-23).all()
+        lse = most + total.log()
+        assert ((got["lse"].double() - lse).abs() <= e_log + lse * 2.0**-24).all()
+    # a target's own term is (p - 1) / T, the others' p / T are not below 0
+    p = torch.exp(z - torch.logsumexp(z, 1)[:, None]).scatter_(1, at, 0.0) * gl.double()[:, None]
+    assert (got["grad_bias"].double()[targets.long()] <= p.sum(0)[targets.long()] * (1 + 2.0**-8) + 2.0**-126).all()
+
+
 def test_large_logits():
     """Logits of hundreds: the maximum is taken out before the exponentials."""
     T, V, D = 65, 900, 64
