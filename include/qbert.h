@@ -461,7 +461,8 @@ qb_status qb_dropout(const void* x, int type, int64_t n, double p, const uint64_
  * time.  The sums' order does not change from call to call.
  * A negative target (padding) has loss 0 and contributes no gradient; its lse is written.  So does a target >= V, and
  * QB_ERR_INVALID is recorded in the status word (by the forward pass).  A bias of -infinity takes a word out.  NaN and
- * infinities propagate as in the formulas; the rows of h of ignored tokens are multiplied by zeros, so they have to be finite where
+ * infinities propagate as in the formulas (a logit of +infinity gives an lse of +infinity; the softmax of such a token has no value, and
+ * g is NaN for every word of it); the rows of h of ignored tokens are multiplied by zeros, so they have to be finite where
  * grad_w or grad_bias is asked for.
  *   h, w         dev bfloat16 [T][D], [V][D], 16-byte aligned                (read)
  *   bias         dev fp32 [V] or NULL                                        (read)

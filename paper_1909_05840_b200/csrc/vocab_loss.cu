@@ -25,6 +25,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -134,6 +135,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // are rounded at their own size (at -5e9, a finite mask, by hundreds, so that e^0 became infinite or 0), and those below -2.4e38
 // have no scaled value.
 __device__ __forceinline__ float exp_fast(float d) { return exp2_fast(d * kLog2e); }
+// What is subtracted for a maximum of `most`: itself, or, where that is infinite, the finite value next to it (no difference of
+// infinities: -infinity alone sums to 0, a +infinity makes the sum infinite).  A NaN among the logits reaches the sum by its own term.
+__device__ __forceinline__ float exp_base(float most) { return fminf(fmaxf(most, -FLT_MAX), FLT_MAX); }
 // sum of e^(z - base), two values an instruction
 __device__ __forceinline__ float exp_sum(const float (&z)[32], float base) {
   const uint64_t base2 = ptx::pack_f32x2(-base, -base), log2e2 = ptx::pack_f32x2(kLog2e, kLog2e);
@@ -369,7 +373,11 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           lse = gp.lse[t];
           target = gp.targets[t];
           gl = gp.grad_loss[t];
-          if (target < 0 || target >= gp.V) gl = 0.0f;
+          if (target < 0 || target >= gp.V) {
+            gl = 0.0f;
+          } else if (lse == INFINITY) {
+            lse = NAN;  // a softmax over an infinite logit has no value
+          }
         }
         tile_cols[e] = -lse;
         tile_cols[256 + e] = gl;
@@ -437,7 +445,12 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           ptx::tmem_ld_wait();
           ptx::tmem_ld_regs_ready(v);
           if (ch + 2 >= chunks) release();
-          const int hit = target - (col0 + ch * 32);
+          const int hit = target - (col0 + ch * 32), words = gp.V - (col0 + ch * 32);
+          if (words < 32) {  // what lies behind the last word is an infinite h times 0, NaN, which no bias takes out
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j >= words) v[j] = 0u;
+          }
           if (hit >= 0 && hit < 32 && target < gp.V) {
             float z = 0.0f;
 #pragma unroll
@@ -458,7 +471,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
             z[4 * j + 3] = hi.y;
             most = fmaxf(most, fmaxf(fmaxf(z[4 * j], z[4 * j + 1]), fmaxf(z[4 * j + 2], z[4 * j + 3])));
           }
-          const float base = most == -INFINITY ? 0.0f : most;  // nothing but -infinity so far: no difference of infinities
+          const float base = exp_base(most);
           sum = sum * exp_fast(top - base) + exp_sum(z, base);
           top = most;
         }
@@ -477,7 +490,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           ptx::tmem_ld_regs_ready(v);
           if (ch + 2 >= chunks) release();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + bias);
+          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint((row < gp.V ? __uint_as_float(v[j]) : 0.0f) + bias);  // (as above)
           const int t = ch * 32 + lane;
           const int target = t < gp.T ? gp.targets[t] : -1, hit = target - row0;
           float z[32];
@@ -499,8 +512,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           float most = fmaxf(z[0], z[1]);
 #pragma unroll
           for (int j = 2; j < 32; j += 2) most = fmaxf(most, fmaxf(z[j], z[j + 1]));
-          const float base = most == -INFINITY ? 0.0f : most;  // nothing but -infinity: no difference of infinities
-          joined[quarter * kFewTokens + ch * 32 + lane] = make_float2(most, exp_sum(z, base));
+          joined[quarter * kFewTokens + ch * 32 + lane] = make_float2(most, exp_sum(z, exp_base(most)));
           __syncwarp();
         }
         // the CTA's four quarters of words, joined in order (the next tile's barrier comes before the next writes)
@@ -509,7 +521,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           float2 q[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) q[i] = joined[i * kFewTokens + e];
-          const float top = fmaxf(fmaxf(q[0].x, q[1].x), fmaxf(q[2].x, q[3].x)), base = top == -INFINITY ? 0.0f : top;
+          const float top = fmaxf(fmaxf(q[0].x, q[1].x), fmaxf(q[2].x, q[3].x)), base = exp_base(top);
           float s = 0.0f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) s += q[i].y * exp_fast(q[i].x - base);
@@ -647,7 +659,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) vocab_join_kernel(const float
     float most = top;
 #pragma unroll
     for (int d = 0; d < kJoinDepth; ++d) most = fmaxf(most, p[d].x);
-    const float base = most == -INFINITY ? 0.0f : most;
+    const float base = exp_base(most);
     sum *= exp_fast(top - base);
 #pragma unroll
     for (int d = 0; d < kJoinDepth; ++d) sum += p[d].y * exp_fast(p[d].x - base);
@@ -659,7 +671,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) vocab_join_kernel(const float
   float most = -INFINITY;
 #pragma unroll
   for (int w = 0; w < kJoinWarps; ++w) most = fmaxf(most, joined[w][lane].x);
-  const float base = most == -INFINITY ? 0.0f : most;
+  const float base = exp_base(most);
   sum = 0.0f;
 #pragma unroll
   for (int w = 0; w < kJoinWarps; ++w) sum += joined[w][lane].y * exp_fast(joined[w][lane].x - base);

@@ -305,6 +305,32 @@ def test_not_finite(bad):
     assert torch.isnan(got["grad_w"]).all()  # the sum over the tokens meets it
 
 
+@pytest.mark.parametrize("T", [3, 77, 129, 300])
+def test_infinite_logits(T):
+    """log sum exp with a term of +infinity is +infinity, with a NaN a NaN, of nothing but -infinity -infinity; other tokens' results stay."""
+    V, D = 900, 64
+    h, w, b, targets, gl = inputs(T, V, D, ignored=False)
+    w[w[:, 5] == 0, 5] = 1.0
+    ws = qb.vocab_loss_workspace(T, V, D)
+    loss, lse = qb.vocab_loss(h, w, b, targets, ws)
+    h[1, 5] = float("inf")  # logits of either infinity
+    h[2, 5] = float("nan")
+    got, got_lse = qb.vocab_loss(h, w, b, targets, ws)
+    assert got_lse[1] == float("inf") and torch.isnan(got_lse[2]) and torch.isnan(got[2])
+    up = float(w[int(targets[1]), 5]) > 0
+    assert torch.isnan(got[1]) if up else got[1] == float("inf")
+    keep = (torch.arange(T, device="cuda") != 1) & (torch.arange(T, device="cuda") != 2)
+    assert torch.equal(got[keep], loss[keep]) and torch.equal(got_lse[keep], lse[keep])
+    h[1, 5] = h[2, 5] = 0.0
+    b[700] = float("inf")
+    targets[0], targets[1], targets[2] = 700, -1, 3
+    got, got_lse = qb.vocab_loss(h, w, b, targets, ws)
+    assert (got_lse == float("inf")).all() and torch.isnan(got[0]) and got[1] == 0 and got[2] == float("inf")
+    assert all(torch.isnan(grad).all() for grad in qb.vocab_loss_backward(h, w, b, targets, got_lse, gl, ws, needs=(False, True, True))[1:])
+    got, got_lse = qb.vocab_loss(h, w, torch.full_like(b, -float("inf")), targets, ws)
+    assert (got_lse == -float("inf")).all() and torch.isnan(got[0]) and got[1] == 0
+
+
 def test_parts_of_the_gradient():
     T, V, D = 200, 1000, 192
     h, w, b, targets, gl = inputs(T, V, D)
