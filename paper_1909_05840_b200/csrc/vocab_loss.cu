@@ -375,6 +375,7 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
           gl = gp.grad_loss[t];
           if (target < 0 || target >= gp.V) {
             gl = 0.0f;
+            lse = INFINITY;  // its probabilities are 0 whatever the caller's lse holds
           } else if (lse == INFINITY) {
             lse = NAN;  // a softmax over an infinite logit has no value
           }

@@ -331,6 +331,19 @@ def test_infinite_logits(T):
     assert (got_lse == -float("inf")).all() and torch.isnan(got[0]) and got[1] == 0
 
 
+@pytest.mark.parametrize("T", [77, 300])
+def test_ignored_tokens_need_no_lse(T):
+    """What the caller's lse holds for ignored tokens changes nothing."""
+    V, D = 900, 64
+    h, w, b, targets, gl = inputs(T, V, D)
+    ws = qb.vocab_loss_workspace(T, V, D)
+    _, lse = qb.vocab_loss(h, w, b, targets, ws)
+    want = qb.vocab_loss_backward(h, w, b, targets, lse, gl, ws)
+    for other in (0.0, -200.0, float("nan"), -float("inf")):
+        got = qb.vocab_loss_backward(h, w, b, targets, torch.where(targets < 0, torch.full_like(lse, other), lse), gl, ws)
+        assert all(torch.equal(a, c) for a, c in zip(got, want))
+
+
 def test_parts_of_the_gradient():
     T, V, D = 200, 1000, 192
     h, w, b, targets, gl = inputs(T, V, D)
