@@ -463,7 +463,7 @@ qb_status qb_dropout(const void* x, int type, int64_t n, double p, const uint64_
  * QB_ERR_INVALID is recorded in the status word (by the forward pass).  A bias of -infinity takes a word out.  NaN and
  * infinities propagate as in the formulas (a logit of +infinity gives an lse of +infinity; the softmax of such a token has no value, and
  * g is NaN for every word of it); the rows of h of ignored tokens are multiplied by zeros, so they have to be finite where
- * grad_w or grad_bias is asked for.
+ * grad_w or grad_bias is asked for (their own rows of grad_h are NaN where they are not).
  *   h, w         dev bfloat16 [T][D], [V][D], 16-byte aligned                (read)
  *   bias         dev fp32 [V] or NULL                                        (read)
  *   targets      dev int32 [T]                                               (read)

@@ -568,15 +568,16 @@ __global__ void __launch_bounds__(kVocabThreads, 1) vocab_kernel(const __grid_co
             const ulonglong2* const lse2 = reinterpret_cast<const ulonglong2*>(tile_cols + ch * 64);  // two columns a word
             const ulonglong2* const gl2 = reinterpret_cast<const ulonglong2*>(tile_cols + 256 + ch * 64);
             const int* const tg = reinterpret_cast<const int*>(tile_cols + 512 + ch * 64);
-            if (FEW && pr.width - ch * 64 < 64) {  // columns that the tile does not have hold what an earlier one left
+            const int tokens = gp.T - (col0 + ch * 64);
+            if (tokens < 64) {  // behind the last token: an infinite w times 0, NaN, or (FEW) what an earlier tile left
 #pragma unroll
               for (int j = 0; j < 64; ++j)
-                if (j >= pr.width - ch * 64) v[j >> 5][j & 31] = 0u;
+                if (j >= tokens) v[j >> 5][j & 31] = 0u;
             }
             // Two columns an instruction.  A target among the warp's 32 words is rare, so that the comparisons are made where there is
             // one (both: 4,096 x 30,522 x 768 backward 447 -> 437 us).
             // z is rounded as in the forward pass, and lse is no less than the largest z: a probability is never above 1, and
-            // p - 1 never has the wrong sign.
+            // p - 1 never has the wrong sign (the scaled form that rounds at lse's size: 441 us, so 446).
             const auto two = [&](uint32_t* x, uint64_t lse, uint64_t w, int k, auto hits, int j) {
               float2 p = ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::add_f32x2(ptx::pack_u32x2(x[0], x[1]), bias2), lse), log2e2));
               p.x = exp2_fast(p.x);

@@ -344,6 +344,26 @@ def test_ignored_tokens_need_no_lse(T):
         assert all(torch.equal(a, c) for a, c in zip(got, want))
 
 
+@pytest.mark.parametrize("T", [1, 30, 77, 130, 300])
+def test_infinite_weight(T):
+    """A word whose logits are all -infinity by its weights: probability 0, so that its own gradients are 0."""
+    V, D = 700, 64
+    h, w, b, targets, gl = inputs(T, V, D, ignored=False)
+    h[:, 9] = h[:, 9].abs() + 0.5
+    out = torch.zeros(V, dtype=torch.bool, device="cuda")
+    out[[5, 300, 699]] = True
+    targets[out[targets.long()]] = 8
+    ws = qb.vocab_loss_workspace(T, V, D)
+    w[out] = 0.0
+    b[out] = -float("inf")
+    want = run(h, w, b, targets, gl, ws)
+    w[out, 9] = -float("inf")
+    got = run(h, w, torch.where(out, 0.0, b), targets, gl, ws)
+    for name in ("loss", "lse", "grad_w", "grad_bias"):
+        assert torch.equal(got[name], want[name]), name
+    assert (got["grad_w"][out] == 0).all() and (got["grad_bias"][out] == 0).all()
+
+
 def test_parts_of_the_gradient():
     T, V, D = 200, 1000, 192
     h, w, b, targets, gl = inputs(T, V, D)
