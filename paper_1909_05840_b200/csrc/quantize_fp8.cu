@@ -68,6 +68,20 @@ struct Quad {
   Raw raw;
   __device__ __forceinline__ void clear() { raw = {}; }
   __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  // the first `left` of four values of any alignment
+  __device__ __forceinline__ void load_each(const T* p, int left) {
+    uint32_t e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      e[i] = 0u;
+      if (i < left) {
+        if constexpr (kWide) e[i] = reinterpret_cast<const uint32_t*>(p)[i];
+        else e[i] = reinterpret_cast<const uint16_t*>(p)[i];
+      }
+    }
+    if constexpr (kWide) raw = make_uint4(e[0], e[1], e[2], e[3]);
+    else raw = make_uint2(e[0] | e[1] << 16, e[2] | e[3] << 16);
+  }
   // Rows of any alignment are read by the aligned quads that have something of them: the four values that start `shift` (1 to 3) values
   // into this quad end in `next`.
   static __device__ __forceinline__ uint32_t part(uint32_t lo, uint32_t hi, int shift) { return shift & 1 ? __funnelshift_r(lo, hi, 16) : lo; }
@@ -234,18 +248,25 @@ __global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const T* x, Fp8Ar
     int off[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const T* const p = x + (int64_t)row[s] * a.K + (int)q[s] * 512;
+      const int64_t base = (int64_t)row[s] * a.K + (int)q[s] * 512;
+      const T* const p = x + base;
       off[s] = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) & 3;
       const int left = (s == 0 || it + 1 < items) ? K - (int)q[s] * 512 : 0;  // of the segment and what follows
-      // a quad is read where it has something of the row (what else it has lies in the same 16 bytes)
+      behind[s].clear();
+      if (fp8_at_edge(base, base, left, 512, a.M * a.K)) {  // the first and the last segment of x
+        off[s] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[4 * s + j].load_each(p + j * 128 + lane * 4, left - j * 128 - lane * 4);
+        continue;
+      }
+      // a quad is read where it has something of the row
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int at = j * 128 + lane * 4 - off[s];
+        const int at = fp8_quad_at(j, lane, off[s]);
         v[4 * s + j].clear();
         if (at < left && left > 0) v[4 * s + j].load(p + at);
       }
-      behind[s].clear();
-      if (lane == 0 && off[s] != 0 && 512 - off[s] < left) behind[s].load(p + 512 - off[s]);
+      if (lane == 0 && fp8_needs_behind(512, off[s], left)) behind[s].load(p + 512 - off[s]);
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -314,35 +335,44 @@ __global__ void __launch_bounds__(256, BLOCKS) fp8_tile_kernel(const T* x, Fp8Ar
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i].load(p + i * a.K);
   } else {
-    // as in the rows form; the quads behind the tile's columns: lane i has row i's
+    // as in the rows form
     const T* const first = x + (int64_t)m0 * a.K + (int64_t)kt * 128;
     const int wide = (int)a.K - (int)kt * 128;  // columns of the tile and behind it
+    if (fp8_at_edge(first - x, first - x + (min(rows, 16) - 1) * a.K, wide, 128, a.M * a.K)) {  // x's first and last rows
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const T* const r = first + i * a.K;
-      const int at = lane * 4 - ((int)(reinterpret_cast<uintptr_t>(r) / sizeof(T)) & 3);
-      v[i].clear();
-      if (i < rows && at < wide) v[i].load(r + at);
-    }
-    Quad<T> behind;
-    behind.clear();
-    if (lane < 16 && lane < rows) {
-      const T* const r = first + lane * a.K;
-      const int off = (int)(reinterpret_cast<uintptr_t>(r) / sizeof(T)) & 3;
-      if (off != 0 && 128 - off < wide) behind.load(r + 128 - off);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int off = (int)(reinterpret_cast<uintptr_t>(first + i * a.K) / sizeof(T)) & 3;
-      Quad<T> wrap;
-      wrap.raw.x = __shfl_sync(0xffffffffu, behind.raw.x, i);
-      wrap.raw.y = __shfl_sync(0xffffffffu, behind.raw.y, i);
-      if constexpr (sizeof(T) == 4) {
-        wrap.raw.z = __shfl_sync(0xffffffffu, behind.raw.z, i);
-        wrap.raw.w = __shfl_sync(0xffffffffu, behind.raw.w, i);
+      for (int i = 0; i < 16; ++i) {
+        v[i].load_each(p + i * a.K, i < rows ? left : 0);
+        asm volatile("" ::: "memory");  // a row at a time: 64 loads in flight would not leave room in 64 registers
       }
-      v[i].shift(Quad<T>::of_next_lane(v[i], wrap, lane), off);
-      v[i].keep(i < rows ? left : 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const T* const r = first + i * a.K;
+        const int at = fp8_quad_at(0, lane, (int)(reinterpret_cast<uintptr_t>(r) / sizeof(T)) & 3);
+        v[i].clear();
+        if (i < rows && at < wide) v[i].load(r + at);
+      }
+      // the quads behind the tile's columns: lane i has row i's
+      Quad<T> behind;
+      behind.clear();
+      if (lane < 16 && lane < rows) {
+        const T* const r = first + lane * a.K;
+        const int off = (int)(reinterpret_cast<uintptr_t>(r) / sizeof(T)) & 3;
+        if (fp8_needs_behind(128, off, wide)) behind.load(r + 128 - off);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int off = (int)(reinterpret_cast<uintptr_t>(first + i * a.K) / sizeof(T)) & 3;
+        Quad<T> wrap;
+        wrap.raw.x = __shfl_sync(0xffffffffu, behind.raw.x, i);
+        wrap.raw.y = __shfl_sync(0xffffffffu, behind.raw.y, i);
+        if constexpr (sizeof(T) == 4) {
+          wrap.raw.z = __shfl_sync(0xffffffffu, behind.raw.z, i);
+          wrap.raw.w = __shfl_sync(0xffffffffu, behind.raw.w, i);
+        }
+        v[i].shift(Quad<T>::of_next_lane(v[i], wrap, lane), off);
+        v[i].keep(i < rows ? left : 0);
+      }
     }
   }
   Mag col = v[0].magnitudes();
