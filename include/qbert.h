@@ -429,6 +429,12 @@ qb_status qb_quantize_fp8_weights(const void* w, int type, int64_t N, int64_t K,
 qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a_format, const uint8_t* b, const uint8_t* b_scale,
                       int b_format, const float* bias, int64_t M, int64_t N, int64_t K, int out_type, void* y, void* ws,
                       size_t ws_bytes, void* cuda_stream);
+/*
+ * Columns of qb_gemm_fp8's tiles for these sizes and a 16-byte aligned workspace of ws_bytes: 64 or 128 (rows of 128), or 256 (rows
+ * of 256, by pairs of CTAs).  `half_tiles` (host, or NULL) receives how many of them are cut to 128 columns, `splits` (host, or NULL)
+ * into how many parts K is cut.  Host arithmetic, no GPU work; it lets a test see which form serves a shape.  0 on invalid arguments.
+ */
+int32_t qb_gemm_fp8_tile_columns(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int32_t* half_tiles /*host*/, int32_t* splits /*host*/);
 
 /*
  * Dropout whose mask is never stored.  (No counterpart in the paper, which fine-tunes BERT with its usual dropout.)

@@ -40,7 +40,7 @@ EXPORTS = (
     "qb_quantize_pack_weights_batch", "qb_gemm_bf16", "qb_layer_linears_bf16",
     "qb_fake_quantize_weights", "qb_fake_quantize_weights_batch", "qb_ste_backward", "qb_quantize_embedding", "qb_embedding_lookup",
     "qb_gemm_i8", "qb_rowsum_i8", "qb_layer_linears_i8", "qb_sensitivity_bits", "qb_probe_wait_limit", "qb_layer_linears_launch_count", "qb_layer_linears_tile_tokens", "qb_quantize_pack_weights_launch_count", "qb_quantize_act_launch_count",
-    "qb_dropout", "qb_fp8_scale_bytes", "qb_fp8_sums_workspace_bytes", "qb_quantize_fp8", "qb_quantize_fp8_weights", "qb_gemm_fp8",
+    "qb_dropout", "qb_fp8_scale_bytes", "qb_fp8_sums_workspace_bytes", "qb_quantize_fp8", "qb_quantize_fp8_weights", "qb_gemm_fp8", "qb_gemm_fp8_tile_columns",
     "qb_vocab_loss_workspace_bytes", "qb_vocab_loss", "qb_vocab_loss_backward",
 )
 NOALLOC_MAX_GROUPS = 4096
@@ -160,6 +160,8 @@ def lib() -> ctypes.CDLL:
     L.qb_quantize_fp8_weights.restype = i32
     L.qb_gemm_fp8.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i64, i64, i32, vp, vp, sz, vp]
     L.qb_gemm_fp8.restype = i32
+    L.qb_gemm_fp8_tile_columns.argtypes = [i64, i64, i64, sz, vp, vp]
+    L.qb_gemm_fp8_tile_columns.restype = i32
     L.qb_vocab_loss_workspace_bytes.argtypes = [i64, i64, i64]
     L.qb_vocab_loss_workspace_bytes.restype = sz
     L.qb_vocab_loss.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
@@ -520,6 +522,13 @@ def gemm_fp8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: t
     """``qb_gemm_fp8``: ``y[m][n] = sum_k a[m][k] b[n][k] + bias[n]``, fp32 or bfloat16 [M,N].  Of a linear ``y = x W^T``: forward
     ``a`` = x, ``b`` = W; gradient of x: ``a`` = grad_y, ``b`` = W transposed; of W: ``a`` = grad_y transposed, ``b`` = x transposed."""
     return (_native or _ext()).gemm_fp8(a, a_scale, b, b_scale, bias, ws, _one_of(_OUT_TYPES, out_dtype, "out_dtype"), y)
+
+
+def gemm_fp8_form(M: int, N: int, K: int, ws_bytes: int = 0) -> tuple:
+    """``qb_gemm_fp8_tile_columns``: (columns of a tile, tiles cut to half of them, parts of K) for a workspace of ``ws_bytes``."""
+    halves, splits = ctypes.c_int32(0), ctypes.c_int32(0)
+    columns = lib().qb_gemm_fp8_tile_columns(M, N, K, ws_bytes, ctypes.byref(halves), ctypes.byref(splits))
+    return int(columns), halves.value, splits.value
 
 
 def vocab_loss_workspace_bytes(T: int, V: int, D: int) -> int:

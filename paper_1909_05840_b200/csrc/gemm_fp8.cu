@@ -464,6 +464,13 @@ __global__ void __launch_bounds__(256) fp8_join_kernel(const float* parts, int s
   }
 }
 
+constexpr size_t kPartsOff = 1024;  // of a split product's parts in the workspace
+static int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m; }
+static bool impossible_product(int64_t M, int64_t N, int64_t K) {
+  if (M <= 0 || N <= 0 || K <= 0 || M > QB_MAX_MN || N > QB_MAX_MN || K > QB_MAX_MN) return true;
+  return up(M, 128) * up(N, 64) > (int64_t)1 << 30 || std::max(up(M, 128), up(N, 128)) * fp8_scale_words(K) > (int64_t)1 << 30;
+}
+
 // The form of a product: CTAs per tile, columns, for pairs how many tiles are whole, and splits of K.
 struct Fp8Choice {
   int cg, bt;
@@ -478,7 +485,6 @@ struct Fp8Choice {
 // tiles: 25.4 -> 22.1 us).  Where a long K meets few tiles, K is split into runs that are a multiple of 512 (a word of
 // scales), whose sums a second kernel joins: that costs its launch and the traffic of the parts.
 static Fp8Choice choose_fp8(int64_t M, int64_t N, int64_t K, int sms, size_t scratch) {
-  const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m; };
   static constexpr struct {
     int cg, bt, block, fixed, least, launch;
   } kForms[] = {{2, 256, 41, 20, 220, 480}, {1, 128, 27, 37, 120, 310}, {1, 64, 20, 25, 100, 300}};
@@ -505,6 +511,16 @@ static Fp8Choice choose_fp8(int64_t M, int64_t N, int64_t K, int sms, size_t scr
 
 }  // namespace qb
 
+extern "C" int32_t qb_gemm_fp8_tile_columns(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int32_t* half_tiles, int32_t* splits) {
+  if (qb::impossible_product(M, N, K) || K % 128 != 0) return 0;
+  int sms = 148;
+  qb::require_sm100(&sms);  // without a device: for a 148-SM part
+  const qb::Fp8Choice c = qb::choose_fp8(M, N, K, sms, ws_bytes > qb::kPartsOff ? ws_bytes - qb::kPartsOff : 0);
+  if (half_tiles) *half_tiles = c.tiles - c.whole;
+  if (splits) *splits = c.splits;
+  return c.bt;
+}
+
 extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a_format, const uint8_t* b, const uint8_t* b_scale,
                                  int b_format, const float* bias, int64_t M, int64_t N, int64_t K, int out_type, void* y, void* ws,
                                  size_t ws_bytes, void* cuda_stream) {
@@ -524,17 +540,15 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
     set_last_error("qb_gemm_fp8: workspace null, not aligned or too small");
     return QB_ERR_WORKSPACE;
   }
-  const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m; };
-  if (up(M, 128) * up(N, 64) > (int64_t)1 << 30 || std::max(up(M, 128), up(N, 128)) * fp8_scale_words(K) > (int64_t)1 << 30) {
+  if (impossible_product(M, N, K)) {
     set_last_error("qb_gemm_fp8: more than 2^30 tiles, or pieces of scales (M=%lld N=%lld K=%lld)", (long long)M, (long long)N, (long long)K);
     return QB_ERR_INVALID;
   }
   int sms = 0;
   qb_status st = require_sm100(&sms);
   if (st != QB_OK) return st;
-  const size_t head = 1024;  // the parts of a split product lie behind it
-  const bool roomy = ws_bytes > head && reinterpret_cast<uintptr_t>(ws) % 16 == 0;
-  const Fp8Choice choice = choose_fp8(M, N, K, sms, roomy ? ws_bytes - head : 0);
+  const bool roomy = ws_bytes > kPartsOff && reinterpret_cast<uintptr_t>(ws) % 16 == 0;
+  const Fp8Choice choice = choose_fp8(M, N, K, sms, roomy ? ws_bytes - kPartsOff : 0);
   const int cg = choice.cg, bt = choice.bt;
   Fp8Params gp;
   const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8, u32 = CU_TENSOR_MAP_DATA_TYPE_UINT32;
@@ -546,7 +560,7 @@ extern "C" qb_status qb_gemm_fp8(const uint8_t* a, const uint8_t* a_scale, int a
   if ((st = make_matrix_map(&gp.tmsa, u32, a_scale, up(M, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
   if ((st = make_matrix_map(&gp.tmsb, u32, b_scale, up(N, 128) * gp.words, 128, 512, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != QB_OK) return st;
   const bool split = choice.splits > 1;
-  float* const parts = reinterpret_cast<float*>(static_cast<char*>(ws) + head);
+  float* const parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kPartsOff);
   const bool bf16 = out_type == QB_BF16 && !split;
   gp.tma_store = N * (bf16 ? 2 : 4) % 16 == 0 && (split || aligned16(y));
   gp.tmy = gp.tma;
