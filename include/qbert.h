@@ -413,7 +413,8 @@ enum { QB_E4M3 = 0, QB_E5M2 = 1 };
  * the outputs of a product that reads them), its other values are unspecified.
  *
  * qb_gemm_fp8: y[m][n] = sum_k a[m][k] * b[n][k] + bias[n], a and b the values that codes and scales stand for, accumulated in
- * fp32, y fp32 (QB_F32) or rounded to nearest even once (QB_BF16).  K is the codes' row length (a multiple of 128).  The formats
+ * fp32 (an instruction's 32 products and the accumulator are cut off at the last place of the largest of them; a product or a sum below
+ * 2^-126 may become 0, one beyond fp32's largest value is infinite), y fp32 (QB_F32) or rounded to nearest even once (QB_BF16).  K is the codes' row length (a multiple of 128).  The formats
  * of a and b may differ.  For a linear y = x W^T: forward a = x, b = W; grad_x: a = grad_y, b = W transposed; grad_W: a = grad_y
  * transposed, b = x transposed.
  *   bias dev fp32 [N] or NULL (read);  y dev [M][N] (written); both aligned to their elements
