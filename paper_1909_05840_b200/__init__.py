@@ -480,6 +480,12 @@ def _one_of(table, dtype, what: str) -> int:
     return table[dtype]
 
 
+def _unwanted(given, what: str) -> None:
+    """A buffer for an output that the call does not compute would stay as it was without a word."""
+    if any(t is not None for t in given):
+        raise QbertError(QB_ERR_INVALID, what)
+
+
 def dropout(x: torch.Tensor, p: float, rng: torch.Tensor, call: int = 0, residual: Optional[torch.Tensor] = None,
             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``qb_dropout``: ``(keep ? x / (1 - p) : 0) + residual``, the mask made from ``rng`` (device int64 [2]: seed, offset) and
@@ -505,6 +511,10 @@ def quantize_fp8(x: torch.Tensor, ws: torch.Tensor, dtype: torch.dtype = torch.f
     ``want_sums`` the column sums fp32 [K] behind them (a bias's gradient; ``ws`` of ``fp8_sums_workspace_bytes(M, K)``)."""
     if want_sums and not transposed:
         raise QbertError(QB_ERR_INVALID, "want_sums comes with transposed")
+    if not want_sums:
+        _unwanted((sums,), "sums comes with want_sums")
+    if not transposed:
+        _unwanted((codes_t, scales_t), "codes_t and scales_t come with transposed")
     return (_native or _ext()).quantize_fp8(x, ws, _one_of(_FP8_FORMATS, dtype, "dtype"), bool(transposed), False, codes, scales,
                                             codes_t, scales_t, bool(want_sums), sums)
 
@@ -513,6 +523,8 @@ def quantize_fp8_weights(w: torch.Tensor, ws: torch.Tensor, dtype: torch.dtype =
                          codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                          codes_t: Optional[torch.Tensor] = None, scales_t: Optional[torch.Tensor] = None):
     """``qb_quantize_fp8_weights``: as ``quantize_fp8`` with one scale per block of 128 x 128."""
+    if not transposed:
+        _unwanted((codes_t, scales_t), "codes_t and scales_t come with transposed")
     return (_native or _ext()).quantize_fp8(w, ws, _one_of(_FP8_FORMATS, dtype, "dtype"), bool(transposed), True, codes, scales,
                                             codes_t, scales_t, False, None)
 

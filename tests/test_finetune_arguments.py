@@ -99,3 +99,13 @@ def test_vocab_loss(lib):
         assert back(**bad) == qb.QB_ERR_ALIGN, bad
     for bad in (dict(ws=None), dict(ws=W + 16), dict(ws_bytes=4096)):
         assert back(**bad) == qb.QB_ERR_WORKSPACE, bad
+
+
+def test_buffers_of_outputs_that_are_not_computed():
+    """A buffer that the call would leave as it was is refused, before anything else is looked at."""
+    for call in (lambda: qb.quantize_fp8(None, None, sums=1), lambda: qb.quantize_fp8(None, None, transposed=True, sums=1),
+                 lambda: qb.quantize_fp8(None, None, codes_t=1), lambda: qb.quantize_fp8(None, None, scales_t=1),
+                 lambda: qb.quantize_fp8_weights(None, None, codes_t=1), lambda: qb.quantize_fp8_weights(None, None, scales_t=1)):
+        with pytest.raises(qb.QbertError) as e:
+            call()
+        assert e.value.status == qb.QB_ERR_INVALID
