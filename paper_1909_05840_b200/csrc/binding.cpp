@@ -359,6 +359,12 @@ void fits(PyObject* o, at::ScalarType type, int64_t count, const char* what) {
   const at::Tensor& t = here(o, what);
   need(t.scalar_type() == type && t.numel() == count, what);
 }
+// A matrix has to have its shape too: the elements of [N][M] are as many as those of [M][N].
+void fits(PyObject* o, at::ScalarType type, int64_t rows, int64_t cols, const char* what) {
+  if (o == Py_None) return;
+  const at::Tensor& t = here(o, what);
+  need(t.scalar_type() == type && t.dim() == 2 && t.size(0) == rows && t.size(1) == cols, what);
+}
 int element_type(const at::Tensor& t, const char* what) {
   switch (t.scalar_type()) {
     case at::kFloat: return QB_F32;
@@ -436,10 +442,10 @@ PyObject* quantize_fp8(Args a) {
   const bool transposed = integer(a[3]) != 0, weights = integer(a[4]) != 0;
   const int64_t M = x.size(0), K = x.size(1), Kp = (K + 127) / 128 * 128, Mp = (M + 127) / 128 * 128;
   const at::ScalarType code = format == QB_E4M3 ? at::kFloat8_e4m3fn : at::kFloat8_e5m2;
-  fits(a[5], code, M * Kp, "codes: contiguous, of the asked format, [M][K up to 128]");
+  fits(a[5], code, M, Kp, "codes: contiguous, of the asked format, [M][K up to 128]");
   fits(a[6], at::kByte, (int64_t)qb_fp8_scale_bytes(M, K), "scales: contiguous bytes, fp8_scale_bytes(M, K) of them");
   if (transposed) {
-    fits(a[7], code, K * Mp, "codes_t: contiguous, of the asked format, [K][M up to 128]");
+    fits(a[7], code, K, Mp, "codes_t: contiguous, of the asked format, [K][M up to 128]");
     fits(a[8], at::kByte, (int64_t)qb_fp8_scale_bytes(K, M), "scales_t: contiguous bytes, fp8_scale_bytes(K, M) of them");
   }
   const bool want_sums = transposed && !weights && integer(a[9]) != 0;
@@ -488,7 +494,7 @@ PyObject* gemm_fp8(Args g) {
   fits(g[4], at::kFloat, N, "bias: contiguous fp32 [N] on the current device");
   const Workspace ws = workspace_here(g[5]);
   const at::ScalarType type = out_type == QB_F32 ? at::kFloat : at::kBFloat16;
-  fits(g[7], type, M * N, "y: contiguous [M][N] of the asked type on the current device");
+  fits(g[7], type, M, N, "y: contiguous [M][N] of the asked type on the current device");
   const at::Device device = a.device();
   const uint8_t* const a_data = static_cast<const uint8_t*>(a.const_data_ptr());
   const uint8_t* const b_data = static_cast<const uint8_t*>(b.const_data_ptr());
@@ -574,8 +580,8 @@ PyObject* vocab_loss_backward(Args a) {
   need(a[5] != Py_None, "grad_loss: contiguous fp32 [T] on the current device");
   fits(a[5], at::kFloat, in.T, "grad_loss: contiguous fp32 [T] on the current device");
   const Workspace ws = workspace_here(a[6]);
-  fits(a[7], at::kBFloat16, in.T * in.D, "grad_h: contiguous bfloat16 [T][D] on the current device");
-  fits(a[8], at::kBFloat16, in.V * in.D, "grad_w: contiguous bfloat16 [V][D] on the current device");
+  fits(a[7], at::kBFloat16, in.T, in.D, "grad_h: contiguous bfloat16 [T][D] on the current device");
+  fits(a[8], at::kBFloat16, in.V, in.D, "grad_w: contiguous bfloat16 [V][D] on the current device");
   fits(a[9], at::kFloat, in.V, "grad_bias: contiguous fp32 [V] on the current device");
   const bool want[3] = {integer(a[10]) != 0, integer(a[11]) != 0, integer(a[12]) != 0 && (in.bias || a[9] != Py_None)};
   Out gh(want[0] ? a[7] : Py_None), gw(want[1] ? a[8] : Py_None), gb(want[2] ? a[9] : Py_None);

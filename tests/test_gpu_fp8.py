@@ -371,3 +371,19 @@ def test_python_refusals(ws):
                  lambda: qb.quantize_fp8(x, ws[:128]), lambda: qb.gemm_fp8(q, s, w, t, None, ws[:128]), lambda: qb.quantize_fp8(x[:0], ws)):
         with pytest.raises(qb.QbertError):
             call()
+
+
+@pytest.mark.gpu
+def test_outputs_of_another_shape(ws):
+    """As many elements in another shape are refused: rows and columns exchanged, a flat buffer."""
+    x, w = rows_of(256, 128, 1), rows_of(384, 128, 2)
+    q, s, qt, st = qb.quantize_fp8(x, ws, transposed=True)
+    v, t = qb.quantize_fp8(w, ws)
+    y = torch.empty(384, 256, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: qb.gemm_fp8(q, s, v, t, None, ws, y=y), lambda: qb.gemm_fp8(q, s, v, t, None, ws, y=y.view(-1)),
+                 lambda: qb.quantize_fp8(x, ws, codes=qt), lambda: qb.quantize_fp8(x, ws, codes=q.view(-1)),
+                 lambda: qb.quantize_fp8(x, ws, transposed=True, codes_t=q), lambda: qb.quantize_fp8_weights(x, ws, transposed=True, codes_t=q)):
+        with pytest.raises(AssertionError):
+            call()
+    y = y.view(256, 384)
+    assert qb.gemm_fp8(q, s, v, t, None, ws, y=y) is y and qb.quantize_fp8(x, ws, codes=q, scales=s)[0] is q

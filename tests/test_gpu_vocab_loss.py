@@ -441,3 +441,13 @@ def test_refusals():
         qb.vocab_loss(h[:, :60].contiguous(), w[:, :60].contiguous(), b, targets, ws)  # D not a multiple of 8
     with pytest.raises(qb.QbertError):
         qb.vocab_loss(h[:0], w, b, targets[:0], ws)
+
+
+def test_gradients_of_another_shape():
+    """As many elements in another shape are refused."""
+    h, w, b, targets, gl = inputs(16, 48, 64)
+    ws = qb.vocab_loss_workspace(16, 48, 64)
+    _, lse = qb.vocab_loss(h, w, b, targets, ws)
+    for kw in (dict(grad_h=torch.empty_like(h).view(64, 16)), dict(grad_h=torch.empty_like(h).view(-1)), dict(grad_w=torch.empty_like(w).view(64, 48))):
+        with pytest.raises(AssertionError):
+            qb.vocab_loss_backward(h, w, b, targets, lse, gl, ws, **kw)
