@@ -22,7 +22,7 @@ namespace qb {
 struct DropArgs {
   const uint64_t* rng;  // dev [2]: seed, offset
   uint64_t call;
-  uint32_t threshold;  // keep when word >= threshold
+  uint32_t last;       // the largest word that drops: round(p * 2^32) - 1 (round(p * 2^32) may be 2^32, and nothing is kept)
   float scale;         // 1 / (1 - p)
 };
 
@@ -171,8 +171,8 @@ __global__ void __launch_bounds__(kDropThreads, 8) dropout_kernel(const T* x, co
         float2 f = pair_to_float(&v[u].e[4 * q + j]);
         // a select, not a product with 0: what is dropped may be infinite or NaN
         if constexpr (DROP) {
-          f.x = w[j] >= a.threshold ? __fmul_rn(f.x, a.scale) : 0.0f;
-          f.y = w[j + 1] >= a.threshold ? __fmul_rn(f.y, a.scale) : 0.0f;
+          f.x = w[j] > a.last ? __fmul_rn(f.x, a.scale) : 0.0f;
+          f.y = w[j + 1] > a.last ? __fmul_rn(f.y, a.scale) : 0.0f;
         }
         if constexpr (RES) {
           const float2 g = pair_to_float(&r[u].e[4 * q + j]);
@@ -218,13 +218,14 @@ extern "C" qb_status qb_dropout(const void* x, int type, int64_t n, double p, co
   qb::DropArgs a;
   a.rng = rng;
   a.call = call;
-  a.threshold = (uint32_t)std::min(std::rint(p * 4294967296.0), 4294967295.0);
+  const double threshold = std::rint(p * 4294967296.0);  // 0: nothing is dropped
+  a.last = (uint32_t)std::max(threshold - 1.0, 0.0);
   a.scale = (float)(1.0 / (1.0 - p));
   const bool vector = all % 16 == 0;  // else the elements one by one: same values
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   switch (type) {
-    case QB_F32: return qb::launch_dropout<float>(x, residual, y, n, vector, a.threshold != 0, a, stream);
-    case QB_BF16: return qb::launch_dropout<__nv_bfloat16>(x, residual, y, n, vector, a.threshold != 0, a, stream);
-    default: return qb::launch_dropout<__half>(x, residual, y, n, vector, a.threshold != 0, a, stream);
+    case QB_F32: return qb::launch_dropout<float>(x, residual, y, n, vector, threshold > 0.0, a, stream);
+    case QB_BF16: return qb::launch_dropout<__nv_bfloat16>(x, residual, y, n, vector, threshold > 0.0, a, stream);
+    default: return qb::launch_dropout<__half>(x, residual, y, n, vector, threshold > 0.0, a, stream);
   }
 }

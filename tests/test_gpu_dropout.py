@@ -204,3 +204,14 @@ def test_refusals():
             qb.dropout(**args)
     with pytest.raises((OverflowError, TypeError)):
         qb.dropout(x, 0.1, state, call=-1)
+
+
+@pytest.mark.gpu
+def test_p_next_to_one():
+    """Element 195 of this mask has the word 2^32 - 1: it is kept while round(p * 2^32) is no larger, and dropped beyond."""
+    assert int(words(np.array([195]), 1, 9601978)[0]) == 2**32 - 1
+    x, state = torch.ones(256, device="cuda"), rng(1, 9601978)
+    kept = qb.dropout(x, 1 - 2.0**-32, state)
+    assert kept[195] == 2.0**32 and int((kept != 0).sum()) == 1
+    for p in (1 - 2.0**-34, 1 - 2.0**-53):
+        assert not qb.dropout(x, p, state).any() and torch.equal(qb.dropout(x, p, state, residual=x), x)
