@@ -406,6 +406,8 @@ enum { QB_E4M3 = 0, QB_E5M2 = 1 };
  * col_sums (with the transposed codes, or NULL) receives the sums of x's columns over its rows in fp32, always in the same order: the
  * gradient of a linear's bias when x is grad_y.  The workspace then has qb_fp8_sums_workspace_bytes(M, K) bytes.
  * qb_quantize_fp8_weights: blocks of 128 x 128; the transposed codes (N and K swapped) have the same scales.  x is read once.
+ * Codes of fake-quantized weights (qb_fake_quantize_weights) are rounded a second time, to the format: a product that must see the
+ * very grid that is trained is qb_gemm's, on the packed codes.
  *   x         dev [M][K] of `type`, aligned to its elements                                  (read)
  *   xq, xqt   dev, 16-byte aligned; x_scale, xt_scale: dev, 16-byte aligned                  (written)
  *   col_sums  dev fp32 [K] or NULL                                                           (written)

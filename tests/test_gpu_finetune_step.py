@@ -6,7 +6,7 @@ import torch
 
 import paper_1909_05840_b200 as qb
 from test_gpu_dropout import words
-from test_gpu_fp8 import E4M3, E5M2, reference
+from test_gpu_fp8 import E4M3, E5M2, check_product, reference, values
 
 pytestmark = pytest.mark.gpu
 P_DROP = 0.1
@@ -121,3 +121,36 @@ def test_captured_step():
         for n in kept:
             assert torch.equal(kept[n], eager[n]), n
     assert qb.read_status(step.ws) == qb.QB_OK
+
+
+@pytest.mark.parametrize("bits", [2, 4, 8])
+@pytest.mark.parametrize("clipped", [False, True])
+def test_fake_quantized_linear(bits, clipped):
+    """Quantization-aware training of one linear: Q(W) by the library's quantizer, its products in 8 bits, the gradient back through the
+    straight-through estimator.  The forward product reads Q(W) rounded once more, to e4m3: by 2^-4 of a value at most, or, below the
+    least normal code, by 2^-10 of a unit of 2^e, where 448 * 2^e is less than twice the block's maximum."""
+    M, N, K, groups = 613, 264, 384, 11
+    g = torch.Generator(device="cuda").manual_seed(bits)
+    x, w = torch.randn(M, K, device="cuda", generator=g), torch.randn(N, K, device="cuda", generator=g) * 0.05
+    dy = (torch.randn(M, N, device="cuda", generator=g) * 1e-4).bfloat16()
+    lo = hi = None
+    if clipped:
+        lo, hi = torch.full((groups,), -0.08, device="cuda"), torch.full((groups,), 0.09, device="cuda")
+    ws = qb.workspace(groups=groups)
+    wq, delta, _ = qb.fake_quantize_weights(w, bits, groups, ws, lo, hi)
+    q, s, qt, st = qb.quantize_fp8_weights(wq, ws, E4M3, transposed=True)
+    codes = values(q, s)[:, :K]
+    top = wq.abs().max().double()
+    assert ((codes - wq.double()).abs() <= wq.double().abs() * 2.0**-4 + 2.0**-10 * top / 224).all()
+    xq, xs, xqt, xst = qb.quantize_fp8(x, ws, E4M3, transposed=True)
+    y = qb.gemm_fp8(xq, xs, q, s, None, ws, torch.float32)
+    check_product(y, xq, xs, q, s, None, torch.float32)
+    gq, gs, gqt, gst = qb.quantize_fp8(dy, ws, E5M2, transposed=True)
+    dx = qb.gemm_fp8(gq, gs, qt, st, None, ws, torch.float32)
+    check_product(dx, gq, gs, qt, st, None, torch.float32)
+    dwq = qb.gemm_fp8(gqt, gst, xqt, xst, None, ws, torch.float32)
+    check_product(dwq, gqt, gst, xqt, xst, None, torch.float32)
+    dw = qb.ste_backward(dwq, w, groups, lo, hi)
+    inside = (w >= -0.08 if clipped else w == w) & (w <= 0.09 if clipped else w == w)
+    assert torch.equal(dw, torch.where(inside, dwq, torch.zeros_like(dwq))) and bool(inside.all()) != clipped
+    assert qb.read_status(ws) == qb.QB_OK
