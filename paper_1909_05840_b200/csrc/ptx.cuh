@@ -87,9 +87,6 @@ __device__ __forceinline__ void tcgen05_fence_after_sync() {
 }
 
 // ---- TMA ---------------------------------------------------------------------------------------
-__device__ __forceinline__ void prefetch_tensormap(const void* tmap) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
-}
 // 2-D tiled load global -> shared, completion counted in bytes on an mbarrier of this CTA.
 // x is the innermost (contiguous) coordinate; x * element size must be a multiple of 16 bytes.
 __device__ __forceinline__ void tma_load_2d(uint32_t dst_smem, const void* tmap, uint32_t bar, int32_t x,
