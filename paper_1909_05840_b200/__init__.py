@@ -5,7 +5,8 @@ GEMM with dequantizing epilogue, encoder-layer linear stack) runs in the CUDA ke
 ABI declared in ``include/qbert.h``.  torch is used for device buffers and the current stream.  The calls
 that a model makes on every pass go through the extension module ``_qbert`` (tensors read, outputs allocated and the
 stream looked up in C++), the others through ctypes.  There is no CPU fallback: if the libraries have not been
-built, importing works but the first call raises ``QbertError``.
+built, importing works but the first call raises ``QbertError``.  No call takes part in autograd: tensors that require a gradient are
+read like others, and the backward passes are calls of their own.
 """
 from __future__ import annotations
 

@@ -8,7 +8,9 @@
 // finite value), so that one integer reduction gives the maximum and says whether the block is finite.
 //
 // Bound by memory: x is read once; 1 byte per value and form is written, plus 1/128 for the scales.  24,576 x 4,096 bfloat16: rows 46 us
-// (6.6 TB/s, the copy bandwidth), both forms at once 68 us (5.9 TB/s; fp32 95 us, 6.4 TB/s), weights with both forms 64 us.
+// (6.6 TB/s, the copy bandwidth; float16 46), both forms at once 68 us (5.9 TB/s; fp32 95 us, 6.4 TB/s; float16 74), weights with both
+// forms 64 us.  The column sums come on top with a launch of their own: 9 us there, 4 at 6,144 x 4,096 (bfloat16 19.6 without), 1.5 at
+// 613 x 768 (4.4).  Rows that are not aligned to four values: 24,576 x 4,095 bfloat16 rows 68 us, both forms 101.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -5,7 +5,9 @@
 // to a maximum and a sum of exponentials per token on their way out of tensor memory; a second kernel joins the tiles of a token.
 // Backward: with the forward pass's lse, g[v][t] = grad_loss[t] * (exp(z[t][v] - lse[t]) - [v = target[t]]) needs no reduction.
 // The vocabulary is taken in pieces: for one piece g is formed (the logits again) and rounded to bfloat16 into the workspace,
-// transposed, while the two products of the piece before it,
+// transposed, while the two products of the piece before it (bfloat16 because the tensor cores take both operands in one type, h's and w's:
+// more bits would be a second bfloat16 term, two instructions for one in both products and twice g's bytes; the gradients
+// come out 0.0021 to 0.0026 of their norm off, where rounding the exact ones to bfloat16 gives 0.0017),
 //     grad_w [piece][D] = g h      and      grad_h [T][D] += g^T w,
 // run in the same launch: the three kinds of tile are dealt over the SMs so that all end together.  grad_h is summed over the
 // pieces in fp32 in the workspace (each element by one addition per launch, or into a slab of its own: the order is always the
@@ -17,9 +19,10 @@
 // transposed in memory.  12 warps: 0 loads (TMA), 1 issues MMAs, 4..11 epilogue, two per TMEM lane quarter.  Every wait is
 // bounded, as in qb_gemm.
 //
-// Bound by the tensor cores: 4,096 x 30,522 x 768 forward 119 us (1,613 TFLOP/s; the MMAs alone 109); 3,686 x 30,522 x 1,024 forward 149,
-// backward 502 us (1,380 TFLOP/s over the three products; the MMAs alone 381, loads alone 284).  With few tokens by reading w: 77
-// tokens x 30,522 x 768 forward 15.3 us (w alone 7.3).
+// Bound by the tensor cores (replayed from a graph after a pause; many passes in a row run under the power cap, a fifth slower):
+// 4,096 x 30,522 x 768 forward 119 us (1,613 TFLOP/s, the tensor pipe busy for 84 %; the MMAs alone 109), backward 446; 3,686 x
+// 30,522 x 1,024 forward 149, backward 510 us (1,355 TFLOP/s over the three products, 70 % busy; the MMAs alone 381, loads alone 284).  With
+// few tokens by reading w: 77 tokens x 30,522 x 768 forward 13.7 us (w alone 7.3).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
