@@ -416,7 +416,8 @@ enum { QB_E4M3 = 0, QB_E5M2 = 1 };
  *
  * qb_gemm_fp8: y[m][n] = sum_k a[m][k] * b[n][k] + bias[n], a and b the values that codes and scales stand for, accumulated in
  * fp32 (an instruction's 32 products and the accumulator are cut off at the last place of the largest of them; a product or a sum below
- * 2^-126 may become 0, one beyond fp32's largest value is infinite), y fp32 (QB_F32) or rounded to nearest even once (QB_BF16).  K is the codes' row length (a multiple of 128).  The formats
+ * 2^-126 may become 0, one beyond fp32's largest value is infinite), y fp32 (QB_F32) or rounded to nearest even once (QB_BF16).
+ * K is the codes' row length (a multiple of 128).  The formats
  * of a and b may differ.  For a linear y = x W^T: forward a = x, b = W; grad_x: a = grad_y, b = W transposed; grad_W: a = grad_y
  * transposed, b = x transposed.
  *   bias dev fp32 [N] or NULL (read);  y dev [M][N] (written); both aligned to their elements
@@ -472,7 +473,7 @@ qb_status qb_dropout(const void* x, int type, int64_t n, double p, const uint64_
  * QB_ERR_INVALID is recorded in the status word (by the forward pass).  A bias of -infinity takes a word out.  NaN and
  * infinities propagate as in the formulas (a logit of +infinity gives an lse of +infinity; the softmax of such a token has no value, and
  * g is NaN for every word of it); the rows of h of ignored tokens are multiplied by zeros, so they have to be finite where
- * grad_w or grad_bias is asked for (their own rows of grad_h are NaN where they are not).
+ * grad_w or grad_bias is asked for (their own rows of grad_h may be NaN where they are not).
  *   h, w         dev bfloat16 [T][D], [V][D], 16-byte aligned                (read)
  *   bias         dev fp32 [V] or NULL                                        (read)
  *   targets      dev int32 [T]                                               (read)

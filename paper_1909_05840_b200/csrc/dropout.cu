@@ -6,9 +6,9 @@
 // on the index alone, so that the backward pass is the same call on the gradient and nothing is stored.
 //
 // Bound by memory: one read (two with a residual) and one write; at 16 bits without a residual by the generator's instructions
-// (17 per element; ALU and multiplier pipes 60 % busy, DRAM at 4.4 TB/s, warps waiting for the pipes).  24,576 x 4,096: fp32 117 us (6.9 TB/s), fp16 77 us (5.2 TB/s), fp16 with a residual 87 us (7.0 TB/s).  Two
-// vectors of 16 bytes a thread and eight blocks an SM: with one vector fp16 took 88 us, with four 79 and, with a residual, 95
-// to 149.
+// (17 per element; ALU and multiplier pipes 60 % busy, DRAM at 4.4 TB/s, warps waiting for the pipes).  24,576 x 4,096: fp32 117 us
+// (6.9 TB/s), fp16 77 us (5.2 TB/s), fp16 with a residual 87 us (7.0 TB/s).  Two vectors of 16 bytes a thread and eight blocks an SM:
+// with one vector fp16 took 88 us, with four 79 and, with a residual, 95 to 149.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
