@@ -380,7 +380,7 @@ qb_status qb_embedding_lookup(const int32_t* ids, int64_t T, const uint32_t* pac
                               const float* q0, int64_t V, int64_t D, int bits, int groups, int accumulate,
                               float* out, void* ws, size_t ws_bytes, void* cuda_stream);
 
-/* Element types and formats of the calls below. */
+/* Element types and formats of the calls below.  Their outputs may overlap neither inputs nor one another, except where a call says so. */
 enum { QB_F32 = 0, QB_BF16 = 1, QB_F16 = 2 };
 enum { QB_E4M3 = 0, QB_E5M2 = 1 };
 #define QB_MAX_ELEMENTS ((int64_t)1 << 40)
