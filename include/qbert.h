@@ -494,6 +494,87 @@ qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w, const flo
                                  float* grad_bias, void* ws, size_t ws_bytes, void* cuda_stream);
 
 /*
+ * Layer norm over rows, forward and backward.  (No counterpart in the paper; the layer norms of BERT's encoder layers, which stay
+ * unquantized.)
+ *     mean = sum_d x[d] / D,   rstd = 1 / sqrt(sum_d (x[d] - mean)^2 / D + eps),   y = (x - mean) * rstd * gamma + beta
+ * and, with xhat = (x - mean) * rstd and g = grad_y * gamma,
+ *     grad_x = rstd * (g - sum_d g / D - xhat * sum_d g xhat / D),   grad_gamma = sum_m grad_y * xhat,   grad_beta = sum_m grad_y.
+ * Everything is held in fp32 and rounded to `type` once at the end; the squares are summed of differences from the mean.  The sums'
+ * order does not change from call to call.  A row with a NaN or an infinity gives NaN, and in the backward pass reaches grad_gamma.
+ *   x, grad_y    dev [M][D] of `type`, aligned to their elements                             (read)
+ *   gamma, beta  dev fp32 [D], or NULL: ones, zeros                                          (read)
+ *   y, grad_x    dev [M][D] of `type`, aligned to their elements; y may be x, grad_x may be grad_y or x   (written)
+ *   mean, rstd   dev fp32 [M], or both NULL in the forward pass                              (written; read by the backward pass)
+ *   grad_gamma, grad_beta   dev fp32 [D], or NULL                                            (written)
+ * eps >= 0.  M up to QB_MAX_MN, D up to QB_MAX_K.  The backward pass takes qb_layer_norm_workspace_bytes(M, D) bytes of workspace (0 on
+ * invalid arguments), 16-byte aligned; no device-side status.
+ */
+size_t qb_layer_norm_workspace_bytes(int64_t M, int64_t D);
+qb_status qb_layer_norm(const void* x, int type, const float* gamma, const float* beta, double eps, int64_t M, int64_t D, void* y,
+                        float* mean, float* rstd, void* cuda_stream);
+qb_status qb_layer_norm_backward(const void* grad_y, const void* x, int type, const float* gamma, const float* mean, const float* rstd,
+                                 int64_t M, int64_t D, void* grad_x, float* grad_gamma, float* grad_beta, void* ws, size_t ws_bytes,
+                                 void* cuda_stream);
+
+/*
+ * Activations saved in 8 bits for the backward pass.  (No counterpart in the paper: its codes are those of weights and of what the
+ * integer products read.  A training step keeps every linear's input and pre-activation; in this form they take 17 / 16 of a byte each.)
+ * Per row and block of QB_CHECKPOINT_BLOCK columns, with a = max|x| of the block:
+ *     scale = a / 127,   code = x * 127 / a rounded to nearest even,   restored value = code * scale.
+ * A block with a < 2^-100 counts as zeros (scale 1); one with a NaN or an infinity restores as NaN everywhere.
+ *   x, y, pre, grad_y, grad_x   dev [M][K] of `type`, aligned to their elements
+ *   codes    dev int8 [M][K], aligned to 16 bytes;   scales  dev fp32 [M][ceil(K / QB_CHECKPOINT_BLOCK)]
+ * qb_checkpoint saves x.  qb_restore gives act(restored value), rounded to `type` once: QB_IDENTITY the value, QB_GELU the activation's
+ * output, formed anew.  qb_gelu_backward: grad_x = grad_y * gelu'(p) with p from `pre` or from pre_codes and pre_scales (the others NULL);
+ * grad_x may be grad_y or pre.  GELU is x * Phi(x), Phi the distribution function of the normal distribution.  M times K rounded up to
+ * QB_CHECKPOINT_BLOCK is QB_MAX_ELEMENTS at most.  No workspace, no device-side status.
+ */
+#define QB_CHECKPOINT_BLOCK 64
+enum { QB_IDENTITY = 0, QB_GELU = 1 };
+qb_status qb_checkpoint(const void* x, int type, int64_t M, int64_t K, int8_t* codes, float* scales, void* cuda_stream);
+qb_status qb_restore(const int8_t* codes, const float* scales, int64_t M, int64_t K, int activation, int type, void* y, void* cuda_stream);
+qb_status qb_gelu_backward(const void* grad_y, int type, const void* pre, const int8_t* pre_codes, const float* pre_scales, int64_t M,
+                           int64_t K, void* grad_x, void* cuda_stream);
+
+/*
+ * Linears in 16-bit floating point with what follows them, and their gradients.  (No counterpart in the paper.  Task heads, the
+ * transform ahead of the vocabulary and the layers that a mixed-precision assignment leaves unquantized are such linears.)
+ *     qb_linear:         z = x W^T + bias,   y = act(z) + residual
+ *     qb_linear_grad_x:  grad_x = (grad_y W) * gelu'(p) + residual     (p: the pre-activation that x is GELU of; without it the factor is 1)
+ *     qb_linear_grad_w:  grad_w = grad_y^T x,   grad_bias[n] = sum_m grad_y[m][n]
+ * grad_y is the gradient of z (behind an activation, qb_gelu_backward or the next linear's qb_linear_grad_x gives it).  Products are
+ * accumulated in fp32 (the tensor cores cut an accumulator off at its last place at each addition of 16 products); bias, activation and
+ * residual follow in fp32, and each output is rounded once.  qb_linear saves z for the backward pass where asked: in 16 bits (pre) or in 8 (pre_codes and
+ * pre_scales, as qb_checkpoint makes them from the fp32 z, where a value next to the border of two codes may get either).
+ *   x, grad_x            dev [M][K], w, grad_w  dev [N][K], grad_y  dev [M][N] of `type`: QB_BF16 or QB_F16
+ *   y, residual          dev [M][N] of out_type: `type` or QB_F32 (qb_linear; then nothing is saved), [M][K] of `type` (qb_linear_grad_x)
+ *   grad_w               of out_type: `type` or QB_F32
+ *   bias, grad_bias      dev fp32 [N], or NULL;   pre  dev [M][N] (qb_linear), [M][K] (qb_linear_grad_x) of `type`, or NULL
+ *   pre_codes, pre_scales  as above with K = N (qb_linear), K (qb_linear_grad_x), or both NULL; codes of any alignment
+ * x, w and grad_y are 16-byte aligned, the others aligned to their elements.  residual may be y (grad_x).  With a pre-activation
+ * qb_linear_grad_x takes no residual.  grad_w or grad_bias may be NULL (without grad_w x may be too).  M, N and K up to QB_MAX_MN, any size.
+ * The sums' order does not change from call to call with the same sizes and workspace size.
+ * The workspace is 16-byte aligned; qb_linear_workspace_bytes(M, N, K) serves the three calls (0 on invalid arguments).  Less will do,
+ * except for grad_bias and for tensors whose rows are no multiple of 8 elements, which need their part (else QB_ERR_WORKSPACE); more lets a
+ * product of few tiles over a long contraction be summed in more parts side by side.
+ */
+size_t qb_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+/*
+ * Columns of the tiles of a product of these sizes and workspace (out [M][N], contraction over K, nothing padded): 64 or 128 (rows of 128),
+ * or 256 (rows of 256, by pairs of CTAs).  `half_tiles` (host, or NULL) receives how many of them are cut to 128 columns, `splits` (host, or
+ * NULL) into how many parts K is cut (a pre-activation in 8 bits keeps it whole).  Host arithmetic, no GPU work; it lets a test see which
+ * form serves a shape.  0 on invalid arguments.
+ */
+int32_t qb_linear_tile_columns(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int32_t* half_tiles /*host*/, int32_t* splits /*host*/);
+qb_status qb_linear(const void* x, const void* w, int type, const float* bias, int activation, const void* residual, int64_t M, int64_t N,
+                    int64_t K, int out_type, void* y, void* pre, int8_t* pre_codes, float* pre_scales, void* ws, size_t ws_bytes,
+                    void* cuda_stream);
+qb_status qb_linear_grad_x(const void* grad_y, const void* w, int type, const void* pre, const int8_t* pre_codes, const float* pre_scales,
+                           const void* residual, int64_t M, int64_t N, int64_t K, void* grad_x, void* ws, size_t ws_bytes, void* cuda_stream);
+qb_status qb_linear_grad_w(const void* grad_y, const void* x, int type, int64_t M, int64_t N, int64_t K, int out_type, void* grad_w,
+                           float* grad_bias, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
  * Mixed-precision assignment from Hessian spectra (Section 3.2, Eq. 2 and the paragraph after it).
  * Host-only: no GPU work, no stream, all pointers are HOST pointers.
  *

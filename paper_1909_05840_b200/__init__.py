@@ -43,6 +43,8 @@ EXPORTS = (
     "qb_gemm_i8", "qb_rowsum_i8", "qb_layer_linears_i8", "qb_sensitivity_bits", "qb_probe_wait_limit", "qb_layer_linears_launch_count", "qb_layer_linears_tile_tokens", "qb_quantize_pack_weights_launch_count", "qb_quantize_act_launch_count",
     "qb_dropout", "qb_fp8_scale_bytes", "qb_fp8_sums_workspace_bytes", "qb_quantize_fp8", "qb_quantize_fp8_weights", "qb_gemm_fp8", "qb_gemm_fp8_tile_columns",
     "qb_vocab_loss_workspace_bytes", "qb_vocab_loss", "qb_vocab_loss_backward",
+    "qb_layer_norm_workspace_bytes", "qb_layer_norm", "qb_layer_norm_backward", "qb_checkpoint", "qb_restore", "qb_gelu_backward",
+    "qb_linear_workspace_bytes", "qb_linear_tile_columns", "qb_linear", "qb_linear_grad_x", "qb_linear_grad_w",
 )
 NOALLOC_MAX_GROUPS = 4096
 
@@ -169,6 +171,28 @@ def lib() -> ctypes.CDLL:
     L.qb_vocab_loss.restype = i32
     L.qb_vocab_loss_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
     L.qb_vocab_loss_backward.restype = i32
+    L.qb_layer_norm_workspace_bytes.argtypes = [i64, i64]
+    L.qb_layer_norm_workspace_bytes.restype = sz
+    L.qb_layer_norm.argtypes = [vp, ctypes.c_int, vp, vp, ctypes.c_double, i64, i64, vp, vp, vp, vp]
+    L.qb_layer_norm.restype = i32
+    L.qb_layer_norm_backward.argtypes = [vp, vp, ctypes.c_int, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, vp]
+    L.qb_layer_norm_backward.restype = i32
+    L.qb_checkpoint.argtypes = [vp, ctypes.c_int, i64, i64, vp, vp, vp]
+    L.qb_checkpoint.restype = i32
+    L.qb_restore.argtypes = [vp, vp, i64, i64, ctypes.c_int, ctypes.c_int, vp, vp]
+    L.qb_restore.restype = i32
+    L.qb_gelu_backward.argtypes = [vp, ctypes.c_int, vp, vp, vp, i64, i64, vp, vp]
+    L.qb_gelu_backward.restype = i32
+    L.qb_linear_workspace_bytes.argtypes = [i64, i64, i64]
+    L.qb_linear_workspace_bytes.restype = sz
+    L.qb_linear_tile_columns.argtypes = [i64, i64, i64, sz, ctypes.POINTER(i32), ctypes.POINTER(i32)]
+    L.qb_linear_tile_columns.restype = i32
+    L.qb_linear.argtypes = [vp, vp, ctypes.c_int, vp, ctypes.c_int, vp, i64, i64, i64, ctypes.c_int, vp, vp, vp, vp, vp, sz, vp]
+    L.qb_linear.restype = i32
+    L.qb_linear_grad_x.argtypes = [vp, vp, ctypes.c_int, vp, vp, vp, vp, i64, i64, i64, vp, vp, sz, vp]
+    L.qb_linear_grad_x.restype = i32
+    L.qb_linear_grad_w.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, ctypes.c_int, vp, vp, vp, sz, vp]
+    L.qb_linear_grad_w.restype = i32
     L.qb_gemm_bf16.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, ctypes.c_int, ctypes.c_int, vp, vp, sz, vp]
     L.qb_gemm_bf16.restype = i32
     L.qb_layer_linears_bf16.argtypes = [ctypes.POINTER(LinearDescC), i32, vp, sz, vp]
@@ -571,3 +595,118 @@ def vocab_loss_backward(h: torch.Tensor, w: torch.Tensor, bias: Optional[torch.T
     None without ``bias``); ``needs`` says which of them are computed (None for the others)."""
     need = [bool(n) for n in needs]
     return (_native or _ext()).vocab_loss_backward(h, w, bias, targets, lse, grad_loss, ws, grad_h, grad_w, grad_bias, *need)
+
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ACTIVATIONS = {None: 0, "gelu": 1}
+_SAVES = {None: 0, "pre": 1, "codes": 2}
+
+
+def layer_norm_workspace_bytes(M: int, D: int) -> int:
+    return int(lib().qb_layer_norm_workspace_bytes(M, D))
+
+
+def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float = 1e-12, want_stats: bool = False,
+               y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None):
+    """``qb_layer_norm`` over the rows of ``x`` [M,D] (fp32, bfloat16 or fp16; ``gamma``, ``beta`` fp32 [D] or None): ``y``, or, with
+    ``want_stats``, (``y``, mean fp32 [M], rstd fp32 [M]) for the backward pass.  ``y`` may be ``x``."""
+    if not want_stats:
+        _unwanted((mean, rstd), "mean and rstd come with want_stats")
+    return (_native or _ext()).layer_norm(x, gamma, beta, eps, bool(want_stats), y, mean, rstd)
+
+
+def layer_norm_backward(grad_y: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                        ws: torch.Tensor, grad_x: Optional[torch.Tensor] = None, grad_gamma: Optional[torch.Tensor] = None,
+                        grad_beta: Optional[torch.Tensor] = None, need_weights: bool = True):
+    """``qb_layer_norm_backward``: (grad_x, grad_gamma fp32 [D], grad_beta fp32 [D]); without ``need_weights`` the last two are None (and
+    any workspace will do, else one of ``layer_norm_workspace_bytes(M, D)``).  ``grad_x`` may be ``grad_y`` or ``x``."""
+    if not need_weights:
+        _unwanted((grad_gamma, grad_beta), "grad_gamma and grad_beta come with need_weights")
+    return (_native or _ext()).layer_norm_backward(grad_y, x, gamma, mean, rstd, ws, grad_x, grad_gamma, grad_beta, bool(need_weights))
+
+
+def checkpoint(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
+    """``qb_checkpoint``: ``x`` [M,K] (fp32, bfloat16 or fp16) saved in 8 bits -> (codes int8 [M,K], scales fp32 [M, blocks of 64])."""
+    return (_native or _ext()).checkpoint(x, codes, scales)
+
+
+def restore(saved: Sequence[torch.Tensor], dtype: torch.dtype = torch.bfloat16, activation: Optional[str] = None,
+            y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``qb_restore``: the values that ``saved`` (codes, scales) stands for, in ``dtype``, or with ``activation="gelu"`` GELU of them."""
+    codes, scales = saved
+    return (_native or _ext()).restore(codes, scales, _one_of(_ACTIVATIONS, activation, "activation"), _one_of(_TYPES, dtype, "dtype"), y)
+
+
+def _through(through):
+    """A pre-activation as (tensor, codes, scales): none, a tensor, or what ``checkpoint`` gives."""
+    if through is None or isinstance(through, torch.Tensor):
+        return through, None, None
+    codes, scales = through
+    return None, codes, scales
+
+
+def gelu_backward(grad_y: torch.Tensor, pre, grad_x: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``qb_gelu_backward``: ``grad_y * gelu'(pre)``, ``pre`` a tensor of the type and shape of ``grad_y`` or (codes, scales).  ``grad_x`` may be
+    ``grad_y`` or ``pre``."""
+    return (_native or _ext()).gelu_backward(grad_y, *_through(pre), grad_x)
+
+
+def linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().qb_linear_workspace_bytes(M, N, K))
+
+
+def linear_form(M: int, N: int, K: int, ws_bytes: int = 0) -> tuple:
+    """``qb_linear_tile_columns``: (columns of a tile, tiles cut to half of them, parts of K) of a product [M,N] over K."""
+    halves, splits = ctypes.c_int32(0), ctypes.c_int32(0)
+    columns = lib().qb_linear_tile_columns(M, N, K, ws_bytes, ctypes.byref(halves), ctypes.byref(splits))
+    return int(columns), halves.value, splits.value
+
+
+def linear_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:
+    """A zero-initialised workspace for ``linear``, ``linear_grad_x`` and ``linear_grad_w`` of up to these sizes (and any other call that
+    needs no more)."""
+    ws = torch.empty(max(linear_workspace_bytes(M, N, K), workspace_bytes(groups=4096)), dtype=torch.uint8, device=device)
+    _check(lib().qb_workspace_init(ws.data_ptr(), ws.numel(), _stream()), "qb_workspace_init")
+    return ws
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], ws: torch.Tensor, activation: Optional[str] = None,
+           residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None, save: Optional[str] = None,
+           y: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, saved: Optional[Sequence[torch.Tensor]] = None):
+    """``qb_linear``: ``act(x w^T + bias) + residual`` for bfloat16 or fp16 ``x`` [M,K], ``w`` [N,K], fp32 ``bias`` [N] or None, in ``out_dtype``
+    (``x``'s type or fp32; ``residual`` has it too, and may be ``y``).  With ``save="pre"`` the pre-activation comes too, (y, pre) in 16
+    bits; with ``save="codes"`` in 8 bits, (y, (codes, scales)), into ``saved`` where given."""
+    kind = _one_of(_SAVES, save, "save")
+    if kind != 1:
+        _unwanted((pre,), 'pre comes with save="pre"')
+    if kind != 2:
+        _unwanted((saved,), 'saved comes with save="codes"')
+    codes, scales = (None, None) if saved is None else saved
+    out = (_native or _ext()).linear(x, w, bias, ws, _one_of(_ACTIVATIONS, activation, "activation"), residual, _out32(x, out_dtype), kind, y, pre,
+                                     codes, scales)
+    return (out[0], out[1:]) if kind == 2 else out
+
+
+def _out32(x, dtype) -> bool:
+    if dtype is not None and dtype != torch.float32 and dtype != x.dtype:
+        raise QbertError(QB_ERR_INVALID, f"out_dtype: {x.dtype} or torch.float32, not {dtype}")
+    return dtype == torch.float32
+
+
+def linear_grad_x(grad_y: torch.Tensor, w: torch.Tensor, ws: torch.Tensor, through=None, residual: Optional[torch.Tensor] = None,
+                  grad_x: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``qb_linear_grad_x``: ``grad_y w`` [M,K], times gelu' of ``through`` (the pre-activation that ``x`` is GELU of: a tensor [M,K], or (codes,
+    scales)) or plus ``residual`` (which may be ``grad_x``)."""
+    return (_native or _ext()).linear_grad_x(grad_y, w, ws, *_through(through), residual, grad_x)
+
+
+def linear_grad_w(grad_y: torch.Tensor, x: torch.Tensor, ws: torch.Tensor, out_dtype: torch.dtype = torch.float32,
+                  grad_w: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None, needs=(True, True)):
+    """``qb_linear_grad_w``: (grad_w [N,K] in ``out_dtype``: fp32 or ``x``'s type, grad_bias fp32 [N]); ``needs`` says which of them are computed
+    (None for the others)."""
+    need_w, need_b = (bool(n) for n in needs)
+    if not need_w:
+        _unwanted((grad_w,), "grad_w is not asked for")
+    if not need_b:
+        _unwanted((grad_bias,), "grad_bias is not asked for")
+    return (_native or _ext()).linear_grad_w(grad_y, x, ws, _out32(x, out_dtype), grad_w, grad_bias, need_w, need_b)

@@ -15,7 +15,7 @@ CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 LIB = PKG / "libqbert.so"
 SOURCES = ["api.cu", "quantize_act.cu", "quantize_weights.cu", "quantize_weights_noalloc.cu", "gemm.cu", "probe.cu", "embedding.cu", "sensitivity.cu",
-           "dropout.cu", "quantize_fp8.cu", "gemm_fp8.cu", "vocab_loss.cu"]
+           "dropout.cu", "quantize_fp8.cu", "gemm_fp8.cu", "vocab_loss.cu", "layer_norm.cu", "checkpoint.cu", "linear.cu"]
 
 
 def _nvcc() -> str:

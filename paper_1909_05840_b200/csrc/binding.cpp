@@ -606,6 +606,307 @@ PyObject* vocab_loss_backward(Args a) {
   return r;
 }
 
+// ---- an encoder block's other operators -----------------------------------------------------------------------------------
+PyObject* tuple_of(std::initializer_list<Out*> outs) {
+  for (Out* o : outs) o->wrap();
+  PyObject* r = PyTuple_New((Py_ssize_t)outs.size());
+  if (!r) throw Failed{};
+  Py_ssize_t i = 0;
+  for (Out* o : outs) PyTuple_SET_ITEM(r, i++, o->get());
+  return r;
+}
+const at::Tensor& matrix_here(PyObject* o, const char* what) {
+  const at::Tensor& t = here(o, what);
+  need(t.dim() == 2, what);
+  return t;
+}
+
+// layer_norm(x, gamma, beta, eps, want_stats, y, mean, rstd) -> y or (y, mean, rstd)
+PyObject* layer_norm(Args a) {
+  const char* const what = "x: a contiguous fp32, bfloat16 or fp16 CUDA tensor of two dimensions on the current device";
+  const at::Tensor& x = matrix_here(a[0], what);
+  const int type = element_type(x, what);
+  const int64_t M = x.size(0), D = x.size(1);
+  fits(a[1], at::kFloat, D, "gamma: contiguous fp32 [D] on the current device");
+  fits(a[2], at::kFloat, D, "beta: contiguous fp32 [D] on the current device");
+  const double eps = PyFloat_AsDouble(a[3]);
+  if (eps == -1.0 && PyErr_Occurred()) throw Failed{};
+  const bool stats = integer(a[4]) != 0;
+  fits(a[5], x.scalar_type(), M, D, "y: contiguous, of the type and shape of x");
+  fits(a[6], at::kFloat, M, "mean: contiguous fp32 [M] on the current device");
+  fits(a[7], at::kFloat, M, "rstd: contiguous fp32 [M] on the current device");
+  const at::Device device = x.device();
+  const at::ScalarType scalar = x.scalar_type();
+  const void* const x_data = x.const_data_ptr();
+  const float *const gamma = static_cast<const float*>(ptr(a[1])), *const beta = static_cast<const float*>(ptr(a[2]));
+  Out y(a[5]), mean(stats ? a[6] : Py_None), rstd(stats ? a[7] : Py_None);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    y.make({M, D}, scalar, device);
+    if (stats) {
+      if (mean.obj || rstd.obj) {
+        mean.make({M}, at::kFloat, device);
+        rstd.make({M}, at::kFloat, device);
+      } else {
+        const int64_t bytes = (M * 4 + 511) / 512 * 512;
+        const at::Tensor both(at::detail::empty_cuda({2 * bytes}, at::kByte, device, std::nullopt));
+        mean.make_in(both, 0, {M}, at::kFloat);
+        rstd.make_in(both, bytes, {M}, at::kFloat);
+      }
+    }
+    st = qb_layer_norm(x_data, type, gamma, beta, eps, M, D, y.data, static_cast<float*>(mean.data), static_cast<float*>(rstd.data), stream());
+  }
+  check(st, "qb_layer_norm");
+  if (!stats) return y.get();
+  return tuple_of({&y, &mean, &rstd});
+}
+
+// layer_norm_backward(grad_y, x, gamma, mean, rstd, ws, grad_x, grad_gamma, grad_beta, need_weights) -> (grad_x, grad_gamma, grad_beta)
+PyObject* layer_norm_backward(Args a) {
+  const char* const what = "grad_y: a contiguous fp32, bfloat16 or fp16 CUDA tensor of two dimensions on the current device";
+  const at::Tensor& gy = matrix_here(a[0], what);
+  const int type = element_type(gy, what);
+  const int64_t M = gy.size(0), D = gy.size(1);
+  need(a[1] != Py_None, "x: contiguous, of the type and shape of grad_y");
+  fits(a[1], gy.scalar_type(), M, D, "x: contiguous, of the type and shape of grad_y");
+  fits(a[2], at::kFloat, D, "gamma: contiguous fp32 [D] on the current device");
+  need(a[3] != Py_None && a[4] != Py_None, "mean, rstd: contiguous fp32 [M] on the current device");
+  fits(a[3], at::kFloat, M, "mean: contiguous fp32 [M] on the current device");
+  fits(a[4], at::kFloat, M, "rstd: contiguous fp32 [M] on the current device");
+  const bool weights = integer(a[9]) != 0;
+  fits(a[6], gy.scalar_type(), M, D, "grad_x: contiguous, of the type and shape of grad_y");
+  fits(a[7], at::kFloat, D, "grad_gamma: contiguous fp32 [D] on the current device");
+  fits(a[8], at::kFloat, D, "grad_beta: contiguous fp32 [D] on the current device");
+  const Workspace ws = workspace_here(a[5]);
+  const at::Device device = gy.device();
+  const at::ScalarType scalar = gy.scalar_type();
+  const void *const gy_data = gy.const_data_ptr(), *const x_data = ptr(a[1]);
+  const float *const gamma = static_cast<const float*>(ptr(a[2])), *const mean = static_cast<const float*>(ptr(a[3])), *const rstd = static_cast<const float*>(ptr(a[4]));
+  Out gx(a[6]), gg(weights ? a[7] : Py_None), gb(weights ? a[8] : Py_None);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    gx.make({M, D}, scalar, device);
+    if (weights) {
+      if (gg.obj || gb.obj) {
+        gg.make({D}, at::kFloat, device);
+        gb.make({D}, at::kFloat, device);
+      } else {
+        const int64_t bytes = (D * 4 + 511) / 512 * 512;
+        const at::Tensor both(at::detail::empty_cuda({2 * bytes}, at::kByte, device, std::nullopt));
+        gg.make_in(both, 0, {D}, at::kFloat);
+        gb.make_in(both, bytes, {D}, at::kFloat);
+      }
+    }
+    st = qb_layer_norm_backward(gy_data, x_data, type, gamma, mean, rstd, M, D, gx.data, static_cast<float*>(gg.data), static_cast<float*>(gb.data), ws.data, ws.bytes,
+                                stream());
+  }
+  check(st, "qb_layer_norm_backward");
+  if (weights) return tuple_of({&gx, &gg, &gb});
+  gx.wrap();
+  return Py_BuildValue("(NOO)", gx.get(), Py_None, Py_None);
+}
+
+// Codes [M][K] and scales [M][blocks of K], both the caller's or both new.
+const char* const kCodesWhat = "codes: contiguous int8 [M][K] on the current device";
+const char* const kScalesWhat = "scales: contiguous fp32 [M][blocks of 64 of K] on the current device";
+void fit_codes(PyObject* codes, PyObject* scales, int64_t M, int64_t K) {
+  fits(codes, at::kChar, M, K, kCodesWhat);
+  fits(scales, at::kFloat, M, (K + QB_CHECKPOINT_BLOCK - 1) / QB_CHECKPOINT_BLOCK, kScalesWhat);
+}
+void make_codes(Out& codes, Out& scales, int64_t M, int64_t K, at::Device device) {
+  const int64_t blocks = (K + QB_CHECKPOINT_BLOCK - 1) / QB_CHECKPOINT_BLOCK;
+  if (codes.obj || scales.obj) {
+    codes.make({M, K}, at::kChar, device);
+    scales.make({M, blocks}, at::kFloat, device);
+    return;
+  }
+  const int64_t bytes = (M * K + 511) / 512 * 512;
+  const at::Tensor both(at::detail::empty_cuda({bytes + M * blocks * 4}, at::kByte, device, std::nullopt));
+  codes.make_in(both, 0, {M, K}, at::kChar);
+  scales.make_in(both, bytes, {M, blocks}, at::kFloat);
+}
+
+// checkpoint(x, codes, scales) -> (codes, scales)
+PyObject* checkpoint(Args a) {
+  const char* const what = "x: a contiguous fp32, bfloat16 or fp16 CUDA tensor of two dimensions on the current device";
+  const at::Tensor& x = matrix_here(a[0], what);
+  const int type = element_type(x, what);
+  const int64_t M = x.size(0), K = x.size(1);
+  fit_codes(a[1], a[2], M, K);
+  const at::Device device = x.device();
+  const void* const x_data = x.const_data_ptr();
+  Out codes(a[1]), scales(a[2]);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    make_codes(codes, scales, M, K, device);
+    st = qb_checkpoint(x_data, type, M, K, static_cast<int8_t*>(codes.data), static_cast<float*>(scales.data), stream());
+  }
+  check(st, "qb_checkpoint");
+  return tuple_of({&codes, &scales});
+}
+
+// restore(codes, scales, activation, type, y) -> y
+PyObject* restore(Args a) {
+  const at::Tensor& codes = matrix_here(a[0], kCodesWhat);
+  const int64_t M = codes.size(0), K = codes.size(1);
+  need(a[1] != Py_None, kScalesWhat);
+  fit_codes(a[0], a[1], M, K);
+  const int activation = (int)integer(a[2]), type = (int)integer(a[3]);
+  const at::ScalarType scalar = type == QB_F32 ? at::kFloat : (type == QB_BF16 ? at::kBFloat16 : at::kHalf);
+  fits(a[4], scalar, M, K, "y: contiguous [M][K] of the asked type on the current device");
+  const at::Device device = codes.device();
+  const int8_t* const code_data = codes.const_data_ptr<int8_t>();
+  const float* const scales = static_cast<const float*>(ptr(a[1]));
+  Out y(a[4]);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    y.make({M, K}, scalar, device);
+    st = qb_restore(code_data, scales, M, K, activation, type, y.data, stream());
+  }
+  check(st, "qb_restore");
+  return y.get();
+}
+
+// A pre-activation [M][K]: in `scalar`'s type, or as codes and scales, or none.
+struct Pre {
+  const void* pre;
+  const int8_t* codes;
+  const float* scales;
+  Pre(PyObject* p, PyObject* c, PyObject* s, at::ScalarType scalar, int64_t M, int64_t K) {
+    fits(p, scalar, M, K, "pre: contiguous, of the gradient's type, a value for each of the output's");
+    fit_codes(c, s, M, K);
+    pre = ptr(p);
+    codes = static_cast<const int8_t*>(ptr(c));
+    scales = static_cast<const float*>(ptr(s));
+  }
+};
+
+// gelu_backward(grad_y, pre, codes, scales, grad_x) -> grad_x
+PyObject* gelu_backward(Args a) {
+  const char* const what = "grad_y: a contiguous fp32, bfloat16 or fp16 CUDA tensor of two dimensions on the current device";
+  const at::Tensor& gy = matrix_here(a[0], what);
+  const int type = element_type(gy, what);
+  const int64_t M = gy.size(0), K = gy.size(1);
+  const Pre p(a[1], a[2], a[3], gy.scalar_type(), M, K);
+  fits(a[4], gy.scalar_type(), M, K, "grad_x: contiguous, of the type and shape of grad_y");
+  const at::Device device = gy.device();
+  const at::ScalarType scalar = gy.scalar_type();
+  const void* const gy_data = gy.const_data_ptr();
+  Out gx(a[4]);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    gx.make({M, K}, scalar, device);
+    st = qb_gelu_backward(gy_data, type, p.pre, p.codes, p.scales, M, K, gx.data, stream());
+  }
+  check(st, "qb_gelu_backward");
+  return gx.get();
+}
+
+int linear_type(const at::Tensor& t, const char* what) {
+  need(t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf, what);
+  return t.scalar_type() == at::kHalf ? QB_F16 : QB_BF16;
+}
+
+// linear(x, w, bias, ws, activation, residual, out32, save, y, pre, codes, scales) -> y, (y, pre) or (y, codes, scales); save 0: nothing, 1: pre, 2: codes
+PyObject* linear(Args a) {
+  const char* const what = "x: a contiguous bfloat16 or fp16 CUDA tensor [M][K] on the current device";
+  const char* const what_w = "w: contiguous [N][K] of x's type on the current device";
+  const at::Tensor& x = matrix_here(a[0], what);
+  const int type = linear_type(x, what);
+  const at::Tensor& w = matrix_here(a[1], what_w);
+  need(w.scalar_type() == x.scalar_type() && w.size(1) == x.size(1), what_w);
+  const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
+  fits(a[2], at::kFloat, N, "bias: contiguous fp32 [N] on the current device");
+  const Workspace ws = workspace_here(a[3]);
+  const int activation = (int)integer(a[4]);
+  const bool out32 = integer(a[6]) != 0;
+  const int64_t save = integer(a[7]);
+  const at::ScalarType scalar = x.scalar_type(), out_scalar = out32 ? at::kFloat : scalar;
+  fits(a[5], out_scalar, M, N, "residual: contiguous [M][N] of the output's type on the current device");
+  fits(a[8], out_scalar, M, N, "y: contiguous [M][N] of the asked type on the current device");
+  fits(a[9], scalar, M, N, "pre: contiguous [M][N] of x's type on the current device");
+  fit_codes(a[10], a[11], M, N);
+  const at::Device device = x.device();
+  const void *const x_data = x.const_data_ptr(), *const w_data = w.const_data_ptr(), *const residual = ptr(a[5]);
+  const float* const bias = static_cast<const float*>(ptr(a[2]));
+  Out y(a[8]), pre(save == 1 ? a[9] : Py_None), codes(save == 2 ? a[10] : Py_None), scales(save == 2 ? a[11] : Py_None);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    y.make({M, N}, out_scalar, device);
+    if (save == 1) pre.make({M, N}, scalar, device);
+    if (save == 2) make_codes(codes, scales, M, N, device);
+    st = qb_linear(x_data, w_data, type, bias, activation, residual, M, N, K, out32 ? QB_F32 : type, y.data, pre.data, static_cast<int8_t*>(codes.data),
+                   static_cast<float*>(scales.data), ws.data, ws.bytes, stream());
+  }
+  check(st, "qb_linear");
+  if (save == 1) return tuple_of({&y, &pre});
+  if (save == 2) return tuple_of({&y, &codes, &scales});
+  return y.get();
+}
+
+// linear_grad_x(grad_y, w, ws, pre, codes, scales, residual, grad_x) -> grad_x
+PyObject* linear_grad_x(Args a) {
+  const char* const what = "grad_y: a contiguous bfloat16 or fp16 CUDA tensor [M][N] on the current device";
+  const char* const what_w = "w: contiguous [N][K] of grad_y's type on the current device";
+  const at::Tensor& gy = matrix_here(a[0], what);
+  const int type = linear_type(gy, what);
+  const at::Tensor& w = matrix_here(a[1], what_w);
+  need(w.scalar_type() == gy.scalar_type() && w.size(0) == gy.size(1), what_w);
+  const int64_t M = gy.size(0), N = gy.size(1), K = w.size(1);
+  const Workspace ws = workspace_here(a[2]);
+  const at::ScalarType scalar = gy.scalar_type();
+  const Pre p(a[3], a[4], a[5], scalar, M, K);
+  fits(a[6], scalar, M, K, "residual: contiguous [M][K] of grad_y's type on the current device");
+  fits(a[7], scalar, M, K, "grad_x: contiguous [M][K] of grad_y's type on the current device");
+  const at::Device device = gy.device();
+  const void *const gy_data = gy.const_data_ptr(), *const w_data = w.const_data_ptr(), *const residual = ptr(a[6]);
+  Out gx(a[7]);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    gx.make({M, K}, scalar, device);
+    st = qb_linear_grad_x(gy_data, w_data, type, p.pre, p.codes, p.scales, residual, M, N, K, gx.data, ws.data, ws.bytes, stream());
+  }
+  check(st, "qb_linear_grad_x");
+  return gx.get();
+}
+
+// linear_grad_w(grad_y, x, ws, out32, grad_w, grad_bias, need_w, need_bias) -> (grad_w, grad_bias)
+PyObject* linear_grad_w(Args a) {
+  const char* const what = "grad_y: a contiguous bfloat16 or fp16 CUDA tensor [M][N] on the current device";
+  const char* const what_x = "x: contiguous [M][K] of grad_y's type on the current device";
+  const at::Tensor& gy = matrix_here(a[0], what);
+  const int type = linear_type(gy, what);
+  const at::Tensor& x = matrix_here(a[1], what_x);
+  need(x.scalar_type() == gy.scalar_type() && x.size(0) == gy.size(0), what_x);
+  const int64_t M = gy.size(0), N = gy.size(1), K = x.size(1);
+  const Workspace ws = workspace_here(a[2]);
+  const bool out32 = integer(a[3]) != 0, want_w = integer(a[6]) != 0, want_b = integer(a[7]) != 0;
+  const at::ScalarType scalar = out32 ? at::kFloat : gy.scalar_type();
+  fits(a[4], scalar, N, K, "grad_w: contiguous [N][K] of the asked type on the current device");
+  fits(a[5], at::kFloat, N, "grad_bias: contiguous fp32 [N] on the current device");
+  const at::Device device = gy.device();
+  const void *const gy_data = gy.const_data_ptr(), *const x_data = x.const_data_ptr();
+  Out gw(want_w ? a[4] : Py_None), gb(want_b ? a[5] : Py_None);
+  qb_status st;
+  {
+    const Unlocked unlocked;
+    if (want_w) gw.make({N, K}, scalar, device);
+    if (want_b) gb.make({N}, at::kFloat, device);
+    st = qb_linear_grad_w(gy_data, x_data, type, M, N, K, out32 ? QB_F32 : type, gw.data, static_cast<float*>(gb.data), ws.data, ws.bytes, stream());
+  }
+  check(st, "qb_linear_grad_w");
+  if (want_w) gw.wrap();
+  if (want_b) gb.wrap();
+  return Py_BuildValue("(NN)", want_w ? gw.get() : Py_NewRef(Py_None), want_b ? gb.get() : Py_NewRef(Py_None));
+}
+
 // The calls over an array of descriptors: (array, ws)
 template <class T, qb_status (*F)(const T*, int32_t, void*, size_t, void*)>
 PyObject* over_descs(Args a, const char* what) {
@@ -664,6 +965,14 @@ PyMethodDef g_methods[] = {QB_ENTRY(quantize_act, 5),
                            QB_ENTRY(gemm_fp8, 8),
                            QB_ENTRY(vocab_loss, 7),
                            QB_ENTRY(vocab_loss_backward, 13),
+                           QB_ENTRY(layer_norm, 8),
+                           QB_ENTRY(layer_norm_backward, 10),
+                           QB_ENTRY(checkpoint, 3),
+                           QB_ENTRY(restore, 5),
+                           QB_ENTRY(gelu_backward, 5),
+                           QB_ENTRY(linear, 12),
+                           QB_ENTRY(linear_grad_x, 8),
+                           QB_ENTRY(linear_grad_w, 8),
                            QB_ENTRY(quantize_act_batch, 2),
                            QB_ENTRY(quantize_pack_weights_batch, 2),
                            QB_ENTRY(fake_quantize_weights_batch, 2),

@@ -1,0 +1,486 @@
+// qb_layer_norm, qb_layer_norm_backward.
+//
+// A row of up to 1,024 elements is held by one warp, 32 elements a lane; up to 8,192 by two, four or eight warps, which join their sums
+// through shared memory; beyond, a block goes over it as often as it needs it (the second time from L2).  Each element is read once into
+// registers, so that the variance is a sum of squared differences from the mean that is known by then.
+// Backward: a block keeps the sums of grad_y * xhat and grad_y over its rows in registers, a pair a column, and leaves them in the
+// workspace at its end; a second kernel sums the blocks', always in the same order.
+// Bound by memory: one read and one write of the tensor forward, two reads and one write backward.
+#include "common.cuh"
+#include "vec16.cuh"
+
+#include <algorithm>
+
+namespace qb {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormElements = 32;  // of a row that a lane holds
+constexpr int kNormMostHeld = 8 * 32 * kNormElements;
+
+// Where a lane's elements lie: vector i begins at column (i * lanes of the row + lane in the row) * V.
+template <class T, int WPR, bool VECTOR>
+struct NormRow {
+  // 16-bit and fp32 vectors of 16 bytes; rows that are not made of them: an element a lane
+  static constexpr int V = VECTOR ? Vec16<T>::N : 1;
+  static constexpr int kVectors = kNormElements / V;
+  static constexpr int kStride = WPR * 32 * V;
+  static constexpr int kRegs = VECTOR ? kVectors * 4 : kVectors;
+  uint32_t raw[kRegs];
+  __device__ __forceinline__ void load(const T* row, int first, int D) {
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+      const int c = first + i * kStride;
+      if constexpr (VECTOR) {
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (c < D) w = *reinterpret_cast<const uint4*>(row + c);
+        raw[4 * i] = w.x;
+        raw[4 * i + 1] = w.y;
+        raw[4 * i + 2] = w.z;
+        raw[4 * i + 3] = w.w;
+      } else {
+        raw[i] = 0u;
+        if (c < D) {
+          if constexpr (sizeof(T) == 4) raw[i] = *reinterpret_cast<const uint32_t*>(row + c);
+          else raw[i] = *reinterpret_cast<const uint16_t*>(row + c);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int i, float (&f)[V]) const {
+    if constexpr (VECTOR) {
+      Vec16<T> v;
+      v.raw = make_uint4(raw[4 * i], raw[4 * i + 1], raw[4 * i + 2], raw[4 * i + 3]);
+      v.get(f);
+    } else if constexpr (sizeof(T) == 4) {
+      f[0] = __uint_as_float(raw[i]);
+    } else {
+      const uint16_t h = (uint16_t)raw[i];
+      f[0] = to_float(*reinterpret_cast<const T*>(&h));
+    }
+  }
+  static __device__ __forceinline__ void put(T* row, int c, const float (&f)[V]) {
+    if constexpr (VECTOR) {
+      Vec16<T> v;
+      v.set(f);
+      *reinterpret_cast<uint4*>(row + c) = v.raw;
+    } else {
+      row[c] = from_float<T>(f[0]);
+    }
+  }
+};
+// V weights from column c on (fp32, 16-byte aligned where V is above 1 and VECTOR), or `instead` of them.
+template <int V>
+__device__ __forceinline__ void norm_weights(const float* w, int c, float instead, bool vector, float (&f)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) f[j] = instead;
+  if (!w) return;
+  if (V >= 4 && vector) {
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      const float4 q = *reinterpret_cast<const float4*>(w + c + 4 * j);
+      f[4 * j] = q.x;
+      f[4 * j + 1] = q.y;
+      f[4 * j + 2] = q.z;
+      f[4 * j + 3] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = w[c + j];
+  }
+}
+
+__device__ __forceinline__ float warp_sum(float s) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  return s;
+}
+// The sum over the WPR warps of a row.  `slots`: [2][8 warps], used in turn; every warp of the block calls it as often.
+template <int WPR>
+__device__ __forceinline__ float row_sum(float s, float (*slots)[8], int turn, int warp, int lane) {
+  s = warp_sum(s);
+  if constexpr (WPR > 1) {
+    if (lane == 0) slots[turn][warp] = s;
+    __syncthreads();
+    s = 0.0f;
+    const int first = warp / WPR * WPR;
+#pragma unroll
+    for (int i = 0; i < WPR; ++i) s += slots[turn][first + i];
+  }
+  return s;
+}
+
+struct NormArgs {
+  const float *gamma, *beta;
+  float* mean;
+  float* rstd;
+  int64_t M;
+  int32_t D;
+  float eps, inv_d;
+  int32_t vector_weights;
+};
+
+template <class T, int WPR, bool VECTOR>
+__global__ void __launch_bounds__(kNormThreads) layer_norm_kernel(const T* x, T* y, const NormArgs a) {
+  using Row = NormRow<T, WPR, VECTOR>;
+  constexpr int V = Row::V;
+  __shared__ float slots[2][8];
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.D;
+  const int64_t m = (int64_t)blockIdx.x * (8 / WPR) + warp / WPR;
+  const bool here = m < a.M;
+  const int first = ((warp % WPR) * 32 + lane) * V;
+  const int end = here ? D : 0;
+  Row r;
+  r.load(x + (here ? m : 0) * D, first, end);
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < Row::kVectors; ++i) {
+    float f[V];
+    r.get(i, f);
+#pragma unroll
+    for (int j = 0; j < V; ++j) s += f[j];
+  }
+  const float mean = row_sum<WPR>(s, slots, 0, warp, lane) * a.inv_d;
+  s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < Row::kVectors; ++i) {
+    if (first + i * Row::kStride < end) {
+      float f[V];
+      r.get(i, f);
+#pragma unroll
+      for (int j = 0; j < V; ++j) s = __fmaf_rn(f[j] - mean, f[j] - mean, s);
+    }
+  }
+  const float rstd = 1.0f / sqrtf(row_sum<WPR>(s, slots, 1, warp, lane) * a.inv_d + a.eps);
+#pragma unroll
+  for (int i = 0; i < Row::kVectors; ++i) {
+    const int c = first + i * Row::kStride;
+    if (c < end) {
+      float f[V], g[V], b[V];
+      r.get(i, f);
+      norm_weights<V>(a.gamma, c, 1.0f, a.vector_weights, g);
+      norm_weights<V>(a.beta, c, 0.0f, a.vector_weights, b);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = __fmaf_rn((f[j] - mean) * rstd, g[j], b[j]);
+      Row::put(y + m * D, c, f);
+    }
+  }
+  if (a.mean && here && warp % WPR == 0 && lane == 0) {
+    a.mean[m] = mean;
+    a.rstd[m] = rstd;
+  }
+}
+
+__device__ __forceinline__ float block_sum(float s, float* slots) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  s = warp_sum(s);
+  __syncthreads();
+  if (lane == 0) slots[warp] = s;
+  __syncthreads();
+  s = slots[0];
+#pragma unroll
+  for (int i = 1; i < kNormThreads / 32; ++i) s += slots[i];
+  return s;
+}
+
+// Rows that registers do not hold: a block a row.
+template <class T>
+__global__ void __launch_bounds__(kNormThreads) layer_norm_long_kernel(const T* x, T* y, const NormArgs a) {
+  __shared__ float slots[8];
+  pdl_begin();
+  const int D = a.D;
+  for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
+    const T* const row = x + m * D;
+    float s = 0.0f;
+    for (int c = threadIdx.x; c < D; c += kNormThreads) s += to_float(row[c]);
+    const float mean = block_sum(s, slots) * a.inv_d;
+    s = 0.0f;
+    for (int c = threadIdx.x; c < D; c += kNormThreads) {
+      const float d = to_float(row[c]) - mean;
+      s = __fmaf_rn(d, d, s);
+    }
+    const float rstd = 1.0f / sqrtf(block_sum(s, slots) * a.inv_d + a.eps);
+    for (int c = threadIdx.x; c < D; c += kNormThreads)  // (y may be x: each element is read and written by one thread)
+      y[m * D + c] = from_float<T>(__fmaf_rn((to_float(row[c]) - mean) * rstd, a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f));
+    if (a.mean && threadIdx.x == 0) {
+      a.mean[m] = mean;
+      a.rstd[m] = rstd;
+    }
+  }
+}
+
+struct NormBackArgs {
+  const float *gamma, *mean, *rstd;
+  float* parts;  // [blocks][2][D]
+  int64_t M;
+  int32_t D;
+  float inv_d;
+  int32_t vector_weights;
+};
+
+template <class T, int WPR, bool VECTOR>
+__global__ void __launch_bounds__(kNormThreads, sizeof(T) == 2 ? 2 : 1) layer_norm_backward_kernel(const T* grad_y, const T* x, T* grad_x, const NormBackArgs a) {
+  using Row = NormRow<T, WPR, VECTOR>;
+  constexpr int V = Row::V;
+  constexpr int kRows = 8 / WPR;
+  extern __shared__ float columns[];  // [2][D]
+  __shared__ float slots[2][2][8];
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.D;
+  const int first = ((warp % WPR) * 32 + lane) * V;
+  float sum_gx[kNormElements] = {}, sum_g[kNormElements] = {};
+  int turn = 0;
+  for (int64_t m0 = (int64_t)blockIdx.x * kRows; m0 < a.M; m0 += (int64_t)gridDim.x * kRows, turn ^= 1) {
+    const int64_t m = m0 + warp / WPR;
+    const bool here = m < a.M;
+    const int end = here ? D : 0;
+    const int64_t at = (here ? m : 0) * D;
+    Row gy, xr;
+    gy.load(grad_y + at, first, end);
+    xr.load(x + at, first, end);
+    const float mean = a.mean[here ? m : 0], rstd = a.rstd[here ? m : 0];
+    float s = 0.0f, sx = 0.0f;
+#pragma unroll
+    for (int i = 0; i < Row::kVectors; ++i) {
+      const int c = first + i * Row::kStride;
+      if (c < end) {
+        float g[V], f[V], w[V];
+        gy.get(i, g);
+        xr.get(i, f);
+        norm_weights<V>(a.gamma, c, 1.0f, a.vector_weights, w);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float xhat = (f[j] - mean) * rstd;
+          sum_gx[i * V + j] = __fmaf_rn(g[j], xhat, sum_gx[i * V + j]);
+          sum_g[i * V + j] += g[j];
+          const float gw = g[j] * w[j];
+          s += gw;
+          sx = __fmaf_rn(gw, xhat, sx);
+        }
+      }
+    }
+    s = warp_sum(s);
+    sx = warp_sum(sx);
+    if constexpr (WPR > 1) {
+      if (lane == 0) {
+        slots[turn][0][warp] = s;
+        slots[turn][1][warp] = sx;
+      }
+      __syncthreads();
+      s = sx = 0.0f;
+      const int begin = warp / WPR * WPR;
+#pragma unroll
+      for (int i = 0; i < WPR; ++i) {
+        s += slots[turn][0][begin + i];
+        sx += slots[turn][1][begin + i];
+      }
+    }
+    s *= a.inv_d;
+    sx *= a.inv_d;
+#pragma unroll
+    for (int i = 0; i < Row::kVectors; ++i) {
+      const int c = first + i * Row::kStride;
+      if (c < end) {
+        float g[V], f[V], w[V];
+        gy.get(i, g);
+        xr.get(i, f);
+        norm_weights<V>(a.gamma, c, 1.0f, a.vector_weights, w);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = rstd * (__fmaf_rn(g[j], w[j], -s) - (f[j] - mean) * rstd * sx);
+        Row::put(grad_x + at, c, f);
+      }
+    }
+  }
+  if (!a.parts) return;
+  // the block's sums: its rows' warps one after the other
+  float* const part = a.parts + (int64_t)blockIdx.x * 2 * D;
+  for (int turn_of = 0; turn_of < kRows; ++turn_of) {
+    if (warp / WPR == turn_of) {
+#pragma unroll
+      for (int i = 0; i < Row::kVectors; ++i) {
+        const int c = first + i * Row::kStride;
+        if (c < D) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            float gx = sum_gx[i * V + j], g = sum_g[i * V + j];
+            if (turn_of > 0) {
+              gx += columns[c + j];
+              g += columns[D + c + j];
+            }
+            if (turn_of == kRows - 1) {
+              part[c + j] = gx;
+              part[D + c + j] = g;
+            } else {
+              columns[c + j] = gx;
+              columns[D + c + j] = g;
+            }
+          }
+        }
+      }
+    }
+    if (kRows > 1) __syncthreads();
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kNormThreads) layer_norm_long_backward_kernel(const T* grad_y, const T* x, T* grad_x, const NormBackArgs a) {
+  __shared__ float slots[8];
+  pdl_begin();
+  const int D = a.D;
+  float* const part = a.parts ? a.parts + (int64_t)blockIdx.x * 2 * D : nullptr;
+  bool begun = false;
+  for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
+    const float mean = a.mean[m], rstd = a.rstd[m];
+    float s = 0.0f, sx = 0.0f;
+    for (int c = threadIdx.x; c < D; c += kNormThreads) {
+      const float g = to_float(grad_y[m * D + c]), xhat = (to_float(x[m * D + c]) - mean) * rstd, gw = g * (a.gamma ? a.gamma[c] : 1.0f);
+      s += gw;
+      sx = __fmaf_rn(gw, xhat, sx);
+      if (part) {  // each column by one thread
+        part[c] = begun ? __fmaf_rn(g, xhat, part[c]) : g * xhat;
+        part[D + c] = begun ? part[D + c] + g : g;
+      }
+    }
+    begun = true;
+    s = block_sum(s, slots) * a.inv_d;
+    sx = block_sum(sx, slots) * a.inv_d;
+    for (int c = threadIdx.x; c < D; c += kNormThreads) {
+      const float g = to_float(grad_y[m * D + c]), xhat = (to_float(x[m * D + c]) - mean) * rstd;
+      grad_x[m * D + c] = from_float<T>(rstd * (__fmaf_rn(g, a.gamma ? a.gamma[c] : 1.0f, -s) - xhat * sx));
+    }
+  }
+}
+
+// Sums over the blocks: 32 columns a block, eight runs of blocks side by side, joined in their order.
+__global__ void __launch_bounds__(256) layer_norm_join_kernel(const float* parts, int blocks, int32_t D, float* grad_gamma, float* grad_beta) {
+  __shared__ float sums[8][32];
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t c = (int64_t)blockIdx.x * 32 + lane;  // gamma's columns, then beta's
+  const int run = (blocks + 7) / 8, last = min((warp + 1) * run, blocks);
+  float s = 0.0f;
+  if (c < 2 * (int64_t)D) {
+#pragma unroll 8
+    for (int b = warp * run; b < last; ++b) s += parts[(int64_t)b * 2 * D + c];
+  }
+  sums[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && c < 2 * (int64_t)D) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) s += sums[w][lane];
+    if (c < D) {
+      if (grad_gamma) grad_gamma[c] = s;
+    } else if (grad_beta) {
+      grad_beta[c - D] = s;
+    }
+  }
+}
+
+constexpr size_t kNormPartsOff = 1024;
+// Blocks of the backward pass: two per SM (fp32: one), no more than there are rows for.
+static int norm_blocks(int64_t M, int rows, int sms, bool wide) { return (int)std::min<int64_t>((M + rows - 1) / rows, (int64_t)sms * (wide ? 1 : 2)); }
+static int norm_warps(int64_t D) { return D <= 1024 ? 1 : (D <= 2048 ? 2 : (D <= 4096 ? 4 : 8)); }
+
+template <class T>
+static qb_status launch_norm(const void* x, void* y, const NormArgs& a, int sms, cudaStream_t stream) {
+  const bool vector = a.D % Vec16<T>::N == 0 && aligned16(x) && aligned16(y);
+  const int warps = norm_warps(a.D);
+  auto go = [&](auto kernel, int64_t grid) {
+    QB_CUDA_TRY(launch_kernel<kMostL1>(kernel, (unsigned)grid, kNormThreads, 0, stream, 1, false, static_cast<const T*>(x), static_cast<T*>(y), a));
+    return (qb_status)QB_OK;
+  };
+  if (a.D > kNormMostHeld) return go(layer_norm_long_kernel<T>, std::min<int64_t>(a.M, (int64_t)sms * 8));
+  const int64_t grid = (a.M + 8 / warps - 1) / (8 / warps);
+  switch (warps) {
+    case 1: return go(vector ? layer_norm_kernel<T, 1, true> : layer_norm_kernel<T, 1, false>, grid);
+    case 2: return go(vector ? layer_norm_kernel<T, 2, true> : layer_norm_kernel<T, 2, false>, grid);
+    case 4: return go(vector ? layer_norm_kernel<T, 4, true> : layer_norm_kernel<T, 4, false>, grid);
+    default: return go(vector ? layer_norm_kernel<T, 8, true> : layer_norm_kernel<T, 8, false>, grid);
+  }
+}
+
+template <class T>
+static qb_status launch_norm_backward(const void* grad_y, const void* x, void* grad_x, const NormBackArgs& a, int blocks, cudaStream_t stream) {
+  const bool vector = a.D % Vec16<T>::N == 0 && aligned16(x) && aligned16(grad_y) && aligned16(grad_x);
+  const int warps = norm_warps(a.D);
+  auto go = [&](auto kernel, size_t smem) {
+    QB_CUDA_TRY(launch_kernel(kernel, (unsigned)blocks, kNormThreads, smem, stream, 1, false, static_cast<const T*>(grad_y), static_cast<const T*>(x),
+                              static_cast<T*>(grad_x), a));
+    return (qb_status)QB_OK;
+  };
+  if (a.D > kNormMostHeld) return go(layer_norm_long_backward_kernel<T>, 0);
+  const size_t smem = warps < 8 ? (size_t)a.D * 8 : 0;  // at most 32 KB
+  switch (warps) {
+    case 1: return go(vector ? layer_norm_backward_kernel<T, 1, true> : layer_norm_backward_kernel<T, 1, false>, smem);
+    case 2: return go(vector ? layer_norm_backward_kernel<T, 2, true> : layer_norm_backward_kernel<T, 2, false>, smem);
+    case 4: return go(vector ? layer_norm_backward_kernel<T, 4, true> : layer_norm_backward_kernel<T, 4, false>, smem);
+    default: return go(vector ? layer_norm_backward_kernel<T, 8, true> : layer_norm_backward_kernel<T, 8, false>, smem);
+  }
+}
+
+static qb_status check_norm(const char* what, bool pointers, int type, int64_t M, int64_t D) {
+  if (pointers && type >= QB_F32 && type <= QB_F16 && M > 0 && M <= QB_MAX_MN && D > 0 && D <= QB_MAX_K) return QB_OK;
+  set_last_error("%s: invalid argument (M=%lld D=%lld type=%d)", what, (long long)M, (long long)D, type);
+  return QB_ERR_INVALID;
+}
+static bool unaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+}  // namespace qb
+
+extern "C" size_t qb_layer_norm_workspace_bytes(int64_t M, int64_t D) {
+  if (M <= 0 || M > QB_MAX_MN || D <= 0 || D > QB_MAX_K) return 0;
+  return qb::kNormPartsOff + (size_t)std::min<int64_t>(M, 2 * qb::kRingMaxCtas) * (size_t)D * 8;
+}
+
+extern "C" qb_status qb_layer_norm(const void* x, int type, const float* gamma, const float* beta, double eps, int64_t M, int64_t D, void* y, float* mean, float* rstd,
+                                   void* cuda_stream) {
+  using namespace qb;
+  qb_status st = check_norm("qb_layer_norm", x && y && (mean != nullptr) == (rstd != nullptr) && eps >= 0.0 && eps < 3.0e38, type, M, D);
+  if (st != QB_OK) return st;
+  const size_t e = type == QB_F32 ? 4 : 2;
+  if (unaligned(x, e) || unaligned(y, e) || unaligned(gamma, 4) || unaligned(beta, 4) || unaligned(mean, 4) || unaligned(rstd, 4)) {
+    set_last_error("qb_layer_norm: every array must be aligned to its elements");
+    return QB_ERR_ALIGN;
+  }
+  int sms = 0;
+  if ((st = require_sm100(&sms)) != QB_OK) return st;
+  const NormArgs a = {gamma, beta, mean, rstd, M, (int32_t)D, (float)eps, (float)(1.0 / (double)D), aligned16(gamma) && aligned16(beta)};
+  switch (type) {
+    case QB_F32: return launch_norm<float>(x, y, a, sms, (cudaStream_t)cuda_stream);
+    case QB_BF16: return launch_norm<__nv_bfloat16>(x, y, a, sms, (cudaStream_t)cuda_stream);
+    default: return launch_norm<__half>(x, y, a, sms, (cudaStream_t)cuda_stream);
+  }
+}
+
+extern "C" qb_status qb_layer_norm_backward(const void* grad_y, const void* x, int type, const float* gamma, const float* mean, const float* rstd, int64_t M, int64_t D,
+                                            void* grad_x, float* grad_gamma, float* grad_beta, void* ws, size_t ws_bytes, void* cuda_stream) {
+  using namespace qb;
+  qb_status st = check_norm("qb_layer_norm_backward", grad_y && x && mean && rstd && grad_x, type, M, D);
+  if (st != QB_OK) return st;
+  const size_t e = type == QB_F32 ? 4 : 2;
+  if (unaligned(grad_y, e) || unaligned(x, e) || unaligned(grad_x, e) || unaligned(gamma, 4) || unaligned(mean, 4) || unaligned(rstd, 4) || unaligned(grad_gamma, 4) ||
+      unaligned(grad_beta, 4)) {
+    set_last_error("qb_layer_norm_backward: every array must be aligned to its elements");
+    return QB_ERR_ALIGN;
+  }
+  const bool sums = grad_gamma || grad_beta;
+  if (sums && (!ws || !aligned16(ws) || ws_bytes < qb_layer_norm_workspace_bytes(M, D))) {
+    set_last_error("qb_layer_norm_backward: workspace null, not 16-byte aligned or too small");
+    return QB_ERR_WORKSPACE;
+  }
+  int sms = 0;
+  if ((st = require_sm100(&sms)) != QB_OK) return st;
+  sms = std::min(sms, kRingMaxCtas);
+  const int blocks = norm_blocks(M, D > kNormMostHeld ? 1 : 8 / norm_warps(D), sms, type == QB_F32);
+  float* const parts = sums ? reinterpret_cast<float*>(static_cast<char*>(ws) + kNormPartsOff) : nullptr;
+  const NormBackArgs a = {gamma, mean, rstd, parts, M, (int32_t)D, (float)(1.0 / (double)D), aligned16(gamma)};
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  switch (type) {
+    case QB_F32: st = launch_norm_backward<float>(grad_y, x, grad_x, a, blocks, stream); break;
+    case QB_BF16: st = launch_norm_backward<__nv_bfloat16>(grad_y, x, grad_x, a, blocks, stream); break;
+    default: st = launch_norm_backward<__half>(grad_y, x, grad_x, a, blocks, stream);
+  }
+  if (st != QB_OK || !sums) return st;
+  QB_CUDA_TRY(launch_kernel(layer_norm_join_kernel, (unsigned)((2 * D + 31) / 32), 256, 0, stream, 1, false, parts, blocks, (int32_t)D, grad_gamma, grad_beta));
+  return QB_OK;
+}

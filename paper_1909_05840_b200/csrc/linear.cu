@@ -1,0 +1,1041 @@
+// qb_linear, qb_linear_grad_x, qb_linear_grad_w: the three products of a linear in 16-bit floating point,
+//     y = act(x w^T + bias) + residual,     grad_x = (grad_y w) * gelu'(p) + residual,     grad_w = grad_y^T x,
+// with everything behind the product done on its way out of tensor memory.
+//
+// One product kernel for all of them, out[m][n] = sum_k A(m, k) B(n, k): persistent CTAs (tcgen05 kind::f16, fp32 accumulators), K blocks
+// of 64, two blocks a stage.  An operand lies in shared memory as its tensor has it: contraction along its rows (K-major: x and w of
+// the forward pass, grad_y of grad_x) or down its columns (MN-major: w of grad_x, both operands of grad_w), so that nothing is
+// transposed in memory.  12 warps:
+//   warp 0        TMA producer (one lane)
+//   warp 1        issues tcgen05.mma, owns the tensor memory (one lane)
+//   warps 2..3    idle
+//   warps 4..11   epilogue, two per TMEM lane quarter: tcgen05.ld -> bias, GELU or its slope, residual -> shared memory -> TMA store
+// A tile is 128 rows of A per CTA x BT rows of B; TMEM lane = row, column = column of the output.  Large products run as CTA pairs
+// (cta_group::2, 256 x 256).  No load is multicast.  Two accumulators, so that a tile's epilogue overlaps the products of the next.
+// Every wait is bounded: on expiry the CTA records QB_ERR_TIMEOUT and leaves through the normal exit path.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "checkpoint.cuh"
+#include "common.cuh"
+#include "gelu.cuh"
+#include "mbar_wait.cuh"
+#include "ptx_float.cuh"
+#include "tensormap.cuh"
+
+namespace qb {
+
+// How an operand lies and is loaded, two K blocks of 64 at a time: K-major (rows x 2 groups of 64 columns) or MN-major (128 rows along
+// K x groups of 64 columns); one box of three dimensions, or, where rows are no multiple of 128 bytes, a box per group.
+enum LinearForm { kRows = 0, kRows2 = 1, kCols = 2, kCols2 = 3 };
+// What the epilogue does with the product besides bias, residual and what is saved.
+enum LinearMode { kPlain = 0, kGelu = 1, kSlope = 2 };
+
+struct LinearParams {
+  CUtensorMap tma, tmb;  // operands
+  CUtensorMap tmb_half;  // pairs: B for a tile of half the width
+  CUtensorMap tmy;       // out (or the splits' parts, one after the other) in boxes of 32 rows x 128 bytes
+  const float* bias;     // or NULL
+  const void* side;      // residual, or 16-bit pre-activation (kSlope), [M][N] of out's type; or NULL
+  const int8_t* codes;   // kSlope: the pre-activation in 8 bits, or NULL
+  const float* scales;
+  void* out;
+  void* pre;             // receives the pre-activation in 16 bits, or NULL
+  int8_t* pre_codes;     // receives it in 8 bits, or NULL
+  float* pre_scales;
+  void* ws;
+  int32_t M, N;
+  int32_t a_form, b_form;
+  int32_t half_type;     // 1: 16-bit tensors are fp16, 0: bfloat16
+  int32_t n_tiles, tiles;
+  int32_t whole;         // tiles below this are BT wide; pairs: the others are halves, two after the other
+  int32_t split_tiles;   // tiles of one split of K (split s writes rows s * M .. of out, fp32)
+  int32_t split_blocks;  // K blocks of 64 per split, even where there are several
+  int32_t k_blocks;      // of all splits
+  int32_t run_blocks;    // K blocks that one accumulator sums; even where a split has several such runs (fp32 out), which are added up in out
+  int32_t tma_store;     // 1: rows of out are 16-byte aligned
+  int32_t vector;        // 1: rows of side and of pre too
+  int32_t vector_codes;  // 1: rows of the codes too
+  uint32_t idesc;
+};
+
+constexpr int kLinEpilogueWarps = 8;
+constexpr int kLinFirstEpilogueWarp = 4;
+constexpr int kLinThreads = 32 * (kLinFirstEpilogueWarp + kLinEpilogueWarps);
+
+template <int BT, int CG>
+struct LinCfg {
+  static constexpr int kABytes = 2 * 128 * 128;          // 128 rows, two K blocks of 128 bytes
+  static constexpr int kBBytes = 2 * (BT / CG) * 128;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = BT == 64 ? 4 : 3;
+  static constexpr int kOutBytes = kLinEpilogueWarps * 4096;
+  static constexpr int kBarBytes = 256;
+  static constexpr int kBiasBytes = 2 * 256 * 4;
+  static constexpr int kSmemBytes = kStages * kStageBytes + kOutBytes + kBarBytes + kBiasBytes;
+  static constexpr int kTmemCols = 2 * BT;
+  static_assert(kSmemBytes <= 232448, "shared memory");
+};
+
+// Shared-memory descriptor of an operand with 128-byte swizzle.  K-major: 1024 bytes between groups of eight rows.  MN-major: 64
+// consecutive elements of M or N are a row of 128 bytes, the next 64 are 16384 bytes on (leading offset), the next eight of K 1024
+// bytes (stride offset).  Version 1 (bits 46-47), SWIZZLE_128B (61-63 = 2).
+__device__ __forceinline__ uint64_t lin_desc(uint32_t smem_addr, bool mn) {
+  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)(mn ? 16384 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)2 << 61;
+}
+// Instruction descriptor for kind::f16 without N >> 3 (bits 17-22): D fp32 (bits 4-5 = 1), A and B of one type (7-9, 10-12: fp16 0,
+// bfloat16 1), MN-major A and B (15, 16), M >> 4 (24-28).
+static uint32_t lin_idesc(bool half_type, bool a_mn, bool b_mn, int mma_m) {
+  const uint32_t t = half_type ? 0u : 1u;
+  return (1u << 4) | (t << 7) | (t << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(mma_m >> 4) << 24);
+}
+
+// Where tile t lies: first row and column, columns, split and its range of K blocks.
+template <int BT, int CG>
+struct LinTile {
+  int m0, n0, width, split, k0, k1;
+  __device__ __forceinline__ LinTile(const LinearParams& gp, int t) {
+    split = t / gp.split_tiles;
+    t -= split * gp.split_tiles;
+    k0 = split * gp.split_blocks;
+    k1 = min(k0 + gp.split_blocks, gp.k_blocks);
+    width = BT;
+    int half = 0;
+    if (CG == 2 && t >= gp.whole) {
+      half = (t - gp.whole) & 1;
+      t = gp.whole + ((t - gp.whole) >> 1);
+      width = BT / 2;
+    }
+    m0 = t / gp.n_tiles;
+    n0 = (t - m0 * gp.n_tiles) * BT + half * (BT / 2);
+    m0 *= 128 * CG;
+  }
+};
+
+// Barrier over the epilogue warps (named barrier 1) that also ORs a predicate over them.
+__device__ __forceinline__ bool lin_epilogue_sync_or(bool pred) {
+  uint32_t res;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(res)
+      : "r"((uint32_t)pred), "n"(32 * kLinEpilogueWarps)
+      : "memory");
+  return res != 0;
+}
+
+// Two 16-bit values of a word, and back.
+__device__ __forceinline__ float2 unpack16(uint32_t w, bool half_type) {
+  if (half_type) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t pack16(float lo, float hi, bool half_type) {
+  if (half_type) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// A warp's staging buffer: 32 rows of 128 bytes, 16-byte pieces swizzled so that the lanes meet different banks both with a row a
+// lane and with a row an eighth of a warp.
+__device__ __forceinline__ uint4* staged(uint8_t* buf, int row, int piece) { return reinterpret_cast<uint4*>(buf + row * 128 + ((piece ^ (row & 7)) << 4)); }
+// The same for rows of 64 bytes (codes).
+__device__ __forceinline__ uint4* staged_codes(uint8_t* buf, int row, int piece) {
+  return reinterpret_cast<uint4*>(buf + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
+}
+
+// `rows` rows of `cols` codes from the staging buffer to rows `pitch` bytes apart; `vector`: 16-byte aligned ones.
+__device__ __forceinline__ void send_codes(uint8_t* buf, int8_t* to, int64_t pitch, int rows, int cols, int lane, bool vector) {
+  if (vector) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = 8 * k + (lane >> 2), p = lane & 3;
+      if (r < rows && 16 * p < cols) *reinterpret_cast<uint4*>(to + r * pitch + 16 * p) = *staged_codes(buf, r, p);
+    }
+  } else {
+    for (int r = 0; r < rows; ++r)
+#pragma unroll
+      for (int c = lane; c < 64; c += 32)
+        if (c < cols) to[r * pitch + c] = reinterpret_cast<const int8_t*>(staged_codes(buf, r, c >> 4))[c & 15];
+  }
+}
+
+// `rows` rows of `cols` 16-bit values from the staging buffer to rows of any alignment, `pitch` elements apart: a row at a time, the
+// lanes on consecutive words of it.
+__device__ __forceinline__ void send_rows16(const uint8_t* buf, uint16_t* to, int64_t pitch, int rows, int cols, int lane) {
+  const int first_odd = (int)(reinterpret_cast<uintptr_t>(to) >> 1) & 1, step = (int)(pitch & 1);
+  const auto word = [&](int r, int col) {  // columns col and col + 1 of a row, col even
+    return *reinterpret_cast<const uint32_t*>(buf + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 6) * 2);
+  };
+  for (int r = 0; r < rows; ++r) {
+    // columns odd and odd + 1, odd + 2 and odd + 3 .. are the words of the row
+    const int odd = first_odd ^ (step & r), c = 2 * lane + odd;
+    uint32_t w = word(r, 2 * lane);
+    if (odd) w = __byte_perm(w, word(r, min(2 * lane + 2, 62)), 0x5432);
+    if (c + 1 < cols) *reinterpret_cast<uint32_t*>(to + r * pitch + c) = w;
+  }
+  if (lane < rows) {  // the single columns at the ends, of all rows at once
+    const int odd = first_odd ^ (step & lane);
+    uint16_t* const at = to + lane * pitch;
+    if (odd) at[0] = (uint16_t)word(lane, 0);
+    if ((cols - odd) & 1) at[cols - 1] = (uint16_t)(word(lane, (cols - 1) & ~1) >> ((cols - 1) & 1) * 16);
+  }
+}
+
+// OUT32: out is fp32, else of the operands' type.  A chunk is 128 bytes of out: 32 or 64 columns.
+template <int BT, int CG, bool OUT32, int MODE>
+__global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_constant__ LinearParams gp) {
+  using Cfg = LinCfg<BT, CG>;
+  constexpr int kStages = Cfg::kStages;
+  const uint32_t rank = CG == 2 ? ptx::cluster_ctarank() : 0u;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t smem_base = ptx::smem_u32(smem);
+  uint8_t* const out_ptr = smem + kStages * Cfg::kStageBytes;  // 1024-byte aligned
+  uint8_t* const bar_ptr = out_ptr + Cfg::kOutBytes;
+  const uint32_t bar_base = ptx::smem_u32(bar_ptr);
+  auto full = [&](int s) { return bar_base + 8u * s; };
+  auto empty = [&](int s) { return bar_base + 8u * (kStages + s); };
+  auto acc_full = [&](int a) { return bar_base + 8u * (2 * kStages + a); };
+  auto acc_empty = [&](int a) { return bar_base + 8u * (2 * kStages + 2 + a); };
+  const uint32_t drain_bar = bar_base + 8u * (2 * kStages + 4);
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 8 * (2 * kStages + 5));
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* const bias_tile = reinterpret_cast<float*>(bar_ptr + Cfg::kBarBytes);  // [2][256]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if ((smem_base & 1023u) != 0u) {  // never expected; the swizzle needs it
+    pdl_begin();
+    if (threadIdx.x == 0) report_status(gp.ws, QB_ERR_CUDA, (int)smem_base);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      ptx::mbar_init(full(s), 1);
+      ptx::mbar_init(empty(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(acc_full(a), 1);
+      ptx::mbar_init(acc_empty(a), kLinEpilogueWarps * CG);
+    }
+    ptx::mbar_init(drain_bar, 1);
+    *abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_cg<CG>(ptx::smem_u32(tmem_slot), Cfg::kTmemCols);
+    ptx::tmem_relinquish_cg<CG>();
+  }
+  ptx::tcgen05_fence_before_sync();
+  __syncthreads();
+  if constexpr (CG == 2) ptx::cluster_sync_all();
+  ptx::tcgen05_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_begin();
+  // the barriers that the issuer waits on live in the group's first CTA
+  auto lead = [&](uint32_t bar) { return CG == 2 ? ptx::map_to_cta(bar, 0) : bar; };
+
+  const int groups = (int)gridDim.x / CG, group = (int)blockIdx.x / CG;
+  bool timed_out = false;
+  int where = 0;
+
+  if (warp == 0) {
+    // ---------------- TMA producer ------------------------------------------------------------------
+    if (ptx::elect_one()) {
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int t = group; t < gp.tiles && !timed_out; t += groups) {
+        const LinTile<BT, CG> tile(gp, t);
+        const bool half = CG == 2 && tile.width < BT;
+        const int a_mn = tile.m0 + (int)rank * 128, b_rows = tile.width / CG, b_mn = tile.n0 + (int)rank * b_rows;
+        const CUtensorMap* const tmb = half ? &gp.tmb_half : &gp.tmb;
+        const uint32_t bytes = CG * (Cfg::kABytes + (half ? Cfg::kBBytes / 2 : Cfg::kBBytes));
+        for (int kb = tile.k0; kb < tile.k1; kb += 2) {
+          if (!wait_barrier_relaxed(empty(stage), phase ^ 1u, abort_flag)) {
+            timed_out = true;
+            where = (0 << 16) | stage;
+            break;
+          }
+          const uint32_t a_smem = smem_base + stage * Cfg::kStageBytes, b_smem = a_smem + Cfg::kABytes;
+          if (rank == 0) ptx::mbar_arrive_expect_tx(full(stage), bytes);
+          auto load2 = [&](uint32_t dst, const CUtensorMap* tm, int x, int y) {
+            if constexpr (CG == 2) ptx::tma_load_2d_pair(dst, tm, lead(full(stage)), x, y);
+            else ptx::tma_load_2d(dst, tm, full(stage), x, y);
+          };
+          auto load3 = [&](uint32_t dst, const CUtensorMap* tm, int y, int z) {
+            if constexpr (CG == 2) ptx::tma_load_3d_pair(dst, tm, lead(full(stage)), 0, y, z);
+            else ptx::tma_load_3d(dst, tm, full(stage), 0, y, z);
+          };
+          auto load = [&](uint32_t dst, const CUtensorMap* tm, int form, int mn, int rows) {
+            if (form == kRows) {
+              load3(dst, tm, mn, kb);
+            } else if (form == kCols) {
+              load3(dst, tm, kb * 64, mn / 64);
+            } else if (form == kRows2) {
+              load2(dst, tm, kb * 64, mn);
+              load2(dst + rows * 128, tm, kb * 64 + 64, mn);
+            } else {
+              load2(dst, tm, mn, kb * 64);
+              if (rows > 64) load2(dst + 16384, tm, mn + 64, kb * 64);
+            }
+          };
+          load(a_smem, &gp.tma, gp.a_form, a_mn, 128);
+          load(b_smem, tmb, gp.b_form, b_mn, b_rows);
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (timed_out) {  // let copies in flight land before the CTA's shared memory is released
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000ll) {
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer (of a pair: in its first CTA only) ----------------------------------
+    if (rank == 0 && ptx::elect_one()) {
+      const bool a_mn = gp.a_form >= kCols, b_mn = gp.b_form >= kCols;
+      const uint64_t a_desc0 = lin_desc(smem_base, a_mn), b_desc0 = lin_desc(smem_base + Cfg::kABytes, b_mn);
+      // 16 elements of K per instruction: 32 bytes of a row, or 16 rows of 128 bytes
+      const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
+      int stage = 0, it = 0;
+      uint32_t phase = 0;
+      int t = group, run = 0;
+      while (t < gp.tiles && !timed_out) {
+        const int a = it & 1;
+        const uint32_t d = tmem_base + (uint32_t)(a * BT);
+        const LinTile<BT, CG> tile(gp, t);
+        const int first = tile.k0 + run, last = min(first + gp.run_blocks, tile.k1);
+        const uint32_t idesc = gp.idesc | ((uint32_t)(tile.width >> 3) << 17);
+        const uint32_t a_next = a_mn ? 8192 >> 4 : 16384 >> 4, b_next = b_mn ? 8192 >> 4 : (uint32_t)(tile.width / CG * 128) >> 4;  // second K block
+        if (!wait_barrier(acc_empty(a), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) {
+          timed_out = true;
+          where = (1 << 16) | 0x100 | a;
+          break;
+        }
+        for (int kb = first; kb < last; kb += 2) {
+          if (!wait_barrier(full(stage), phase, abort_flag)) {
+            timed_out = true;
+            where = (1 << 16) | stage;
+            break;
+          }
+          ptx::tcgen05_fence_after_sync();
+          const uint64_t a_desc = a_desc0 + (uint64_t)(stage * (Cfg::kStageBytes >> 4));
+          const uint64_t b_desc = b_desc0 + (uint64_t)(stage * (Cfg::kStageBytes >> 4));
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            ptx::mma_f16_ss_cg<CG>(d, a_desc + (uint64_t)(a_step * j), b_desc + (uint64_t)(b_step * j), idesc, kb != first || j != 0 ? 1u : 0u);
+          if (kb + 1 < last) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              ptx::mma_f16_ss_cg<CG>(d, a_desc + (uint64_t)(a_next + a_step * j), b_desc + (uint64_t)(b_next + b_step * j), idesc, 1u);
+          }
+          ptx::mma_commit_cg<CG>(empty(stage));
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        if (!timed_out) ptx::mma_commit_cg<CG>(acc_full(a));
+        ++it;
+        run += gp.run_blocks;
+        if (last == tile.k1) {
+          t += groups;
+          run = 0;
+        }
+      }
+      if (timed_out) {  // wait (bounded) for what was issued before tensor memory is freed
+        ptx::mma_commit_cg<CG>(drain_bar);
+        const long long t0 = clock64();
+        while (!ptx::mbar_try_wait(drain_bar, 0) && clock64() - t0 < 400000000ll) {
+        }
+      }
+    }
+  } else if (warp >= kLinFirstEpilogueWarp) {
+    // ---------------- epilogue ----------------------------------------------------------------------
+    constexpr int kCols = OUT32 ? 32 : 64;  // columns of a chunk
+    constexpr int kParts = kCols / 32;
+    constexpr int kESize = OUT32 ? 4 : 2;
+    const int ew = warp - kLinFirstEpilogueWarp, quarter = warp & 3, half = ew >> 2;
+    const int e = threadIdx.x - 32 * kLinFirstEpilogueWarp;
+    const bool half_type = gp.half_type != 0;
+    uint8_t* const buf = out_ptr + ew * 4096;
+    const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    auto arrive = [&](uint32_t bar) {  // this warp has read all it needs from the accumulator
+      ptx::tcgen05_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        if (CG == 2 && rank != 0) ptx::mbar_arrive_remote(lead(bar));
+        else ptx::mbar_arrive(bar);
+      }
+    };
+    int it = 0, run = 0;
+    for (int t = group; t < gp.tiles; ++it) {
+      const int a = it & 1;
+      const LinTile<BT, CG> tile(gp, t);
+      const bool add = OUT32 && run > 0;  // to the runs before, which brought bias and residual
+      const float* const bias = add ? nullptr : gp.bias;
+      const void* const side = add ? nullptr : gp.side;
+      int m0 = tile.m0 + (int)rank * 128 + quarter * 32, n0 = tile.n0;
+      int chunks = m0 < gp.M ? max(0, min(tile.width / kCols, (gp.N - n0 + kCols - 1) / kCols)) : 0;
+      asm volatile("" : "+r"(m0), "+r"(n0), "+r"(chunks));  // formed before the wait, not behind it
+      bias_tile[a * 256 + e] = bias && e < BT && n0 + e < gp.N ? bias[n0 + e] : 0.0f;
+      const int rows = min(32, gp.M - m0);
+      // The chunk's part of the tensor beside the product (residual, pre-activation), fetched while the products run: 16 bytes a lane,
+      // whole lines.
+      uint4 s[8];
+      auto fetch = [&](int c0) {
+        if (!side || !gp.vector) return;
+        const uint8_t* const from = static_cast<const uint8_t*>(side) + ((int64_t)m0 * gp.N + n0 + c0) * kESize;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = 4 * i + (lane >> 3), p = lane & 7;
+          s[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < rows && n0 + c0 + p * (16 / kESize) < gp.N) s[i] = *reinterpret_cast<const uint4*>(from + (int64_t)r * gp.N * kESize + p * 16);
+        }
+      };
+      if (half < chunks) fetch(half * kCols);
+      const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
+      if (lin_epilogue_sync_or(!ok)) {  // publishes the bias, and all eight warps give up together
+        timed_out = true;
+        where = (3 << 16) | a;
+        break;
+      }
+      ptx::tcgen05_fence_after_sync();
+      const uint32_t acc = lanes + (uint32_t)(a * BT);
+      if (half >= chunks) arrive(acc_empty(a));
+#pragma unroll 1
+      for (int i = half; i < chunks; i += 2) {
+        const int c0 = i * kCols, cols = min(kCols, gp.N - n0 - c0);
+        const int64_t corner = (int64_t)m0 * gp.N + n0 + c0;  // of the chunk, in elements
+        const int64_t block = (int64_t)(m0 + lane) * checkpoint_blocks(gp.N) + (n0 + c0) / kCheckpointBlock;  // the row's, in scales
+        uint32_t v[kParts][32];
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(c0 + 32 * p), v[p]);
+        if (lane == 0) {  // the chunk before has left the buffer; what is added to has been written
+          if (add && i == half) ptx::tma_store_wait0();
+          else ptx::tma_store_wait_read0();
+        }
+        __syncwarp();
+        uint4 q[4];  // kSlope: the row's codes
+        float q_scale = 1.0f;
+        if (MODE == kSlope && gp.codes) {
+          if (gp.vector_codes) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int r = 8 * k + (lane >> 2), p = lane & 3;
+              uint4 w = make_uint4(0u, 0u, 0u, 0u);
+              if (r < rows && 16 * p < cols) w = *reinterpret_cast<const uint4*>(gp.codes + corner + (int64_t)r * gp.N + 16 * p);
+              *staged_codes(buf, r, p) = w;
+            }
+          } else {
+            for (int r = 0; r < rows; ++r)
+#pragma unroll
+              for (int c = lane; c < 64; c += 32)
+                reinterpret_cast<int8_t*>(staged_codes(buf, r, c >> 4))[c & 15] = c < cols ? gp.codes[corner + (int64_t)r * gp.N + c] : (int8_t)0;
+          }
+          if (lane < rows) q_scale = gp.scales[block];
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) q[k] = *staged_codes(buf, lane, k);
+          __syncwarp();
+        }
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) ptx::tmem_ld_regs_ready(v[p]);
+        if (i + 2 >= chunks) arrive(acc_empty(a));
+        // z = product + bias
+        if (MODE != kSlope && bias) {
+          const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + a * 256 + c0);
+#pragma unroll
+          for (int j = 0; j < kCols / 4; ++j) {
+            const float4 b = b4[j];
+            uint32_t* const z = &v[j >> 3][(j & 7) * 4];
+            z[0] = __float_as_uint(__uint_as_float(z[0]) + b.x);
+            z[1] = __float_as_uint(__uint_as_float(z[1]) + b.y);
+            z[2] = __float_as_uint(__uint_as_float(z[2]) + b.z);
+            z[3] = __float_as_uint(__uint_as_float(z[3]) + b.w);
+          }
+        }
+        const auto at = [&](int j) { return __uint_as_float(v[j >> 5][j & 31]); };
+        if constexpr (!OUT32 && MODE != kSlope) {
+          if (gp.pre_codes) {  // z in 8 bits: a chunk is a block
+            float top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 64; j += 2) top = max3_nan(top, fabsf(at(j)), fabsf(at(j + 1)));
+            const CheckpointScale cs(top);
+            if (lane < rows) gp.pre_scales[block] = cs.scale;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint4 w;
+              w.x = cs.codes4(at(16 * k), at(16 * k + 1), at(16 * k + 2), at(16 * k + 3));
+              w.y = cs.codes4(at(16 * k + 4), at(16 * k + 5), at(16 * k + 6), at(16 * k + 7));
+              w.z = cs.codes4(at(16 * k + 8), at(16 * k + 9), at(16 * k + 10), at(16 * k + 11));
+              w.w = cs.codes4(at(16 * k + 12), at(16 * k + 13), at(16 * k + 14), at(16 * k + 15));
+              *staged_codes(buf, lane, k) = w;
+            }
+            __syncwarp();
+            send_codes(buf, gp.pre_codes + corner, gp.N, rows, cols, lane, gp.vector_codes != 0);
+            __syncwarp();
+          } else if (gp.pre) {  // z in 16 bits
+            uint16_t* const to = static_cast<uint16_t*>(gp.pre) + corner;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              *staged(buf, lane, k) = make_uint4(pack16(at(8 * k), at(8 * k + 1), half_type), pack16(at(8 * k + 2), at(8 * k + 3), half_type),
+                                                 pack16(at(8 * k + 4), at(8 * k + 5), half_type), pack16(at(8 * k + 6), at(8 * k + 7), half_type));
+            __syncwarp();
+            if (gp.vector) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const int r = 4 * k + (lane >> 3), p = lane & 7;
+                if (r < rows && 8 * p < cols) *reinterpret_cast<uint4*>(to + (int64_t)r * gp.N + 8 * p) = *staged(buf, r, p);
+              }
+            } else {
+              send_rows16(buf, to, gp.N, rows, cols, lane);
+            }
+            __syncwarp();
+          }
+        }
+        if (side) {
+          if (gp.vector) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) *staged(buf, 4 * k + (lane >> 3), lane & 7) = s[k];
+            if (i + 2 < chunks) fetch(c0 + 2 * kCols);
+          } else {
+            for (int r = 0; r < rows; ++r) {
+              if constexpr (OUT32) {
+                reinterpret_cast<float*>(staged(buf, r, lane >> 2))[lane & 3] = lane < cols ? static_cast<const float*>(side)[corner + (int64_t)r * gp.N + lane] : 0.0f;
+              } else {
+#pragma unroll
+                for (int c = lane; c < 64; c += 32)
+                  reinterpret_cast<uint16_t*>(staged(buf, r, c >> 3))[c & 7] =
+                      c < cols ? static_cast<const uint16_t*>(side)[corner + (int64_t)r * gp.N + c] : (uint16_t)0;
+              }
+            }
+          }
+          __syncwarp();
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {  // 16 bytes of the row at a time
+          uint4* const here = staged(buf, lane, k);
+          uint4 w = make_uint4(0u, 0u, 0u, 0u);
+          if (side) w = *here;
+          if constexpr (OUT32) {
+            float2 f = make_float2(at(4 * k), at(4 * k + 1)), g = make_float2(at(4 * k + 2), at(4 * k + 3));
+            if constexpr (MODE == kGelu) {
+              f = gelu2(f.x, f.y);
+              g = gelu2(g.x, g.y);
+            }
+            if (side) {
+              f.x += __uint_as_float(w.x);
+              f.y += __uint_as_float(w.y);
+              g.x += __uint_as_float(w.z);
+              g.y += __uint_as_float(w.w);
+            }
+            *here = make_uint4(__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(g.x), __float_as_uint(g.y));
+          } else {
+            uint32_t o[4];
+            const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              float2 f = make_float2(at(8 * k + 2 * h), at(8 * k + 2 * h + 1));
+              if constexpr (MODE == kGelu) f = gelu2(f.x, f.y);
+              if constexpr (MODE == kSlope) {
+                float2 p;
+                if (gp.codes) {
+                  const uint4& qk = q[k >> 1];
+                  const uint32_t word = (k & 1) ? (h < 2 ? qk.z : qk.w) : (h < 2 ? qk.x : qk.y);
+                  p = make_float2(code_value(word, (h & 1) * 2) * q_scale, code_value(word, (h & 1) * 2 + 1) * q_scale);
+                } else {
+                  p = unpack16(in[h], half_type);
+                }
+                const float2 slope = gelu_slope2(p.x, p.y);
+                f.x *= slope.x;
+                f.y *= slope.y;
+              } else if (side) {
+                const float2 r = unpack16(in[h], half_type);
+                f.x += r.x;
+                f.y += r.y;
+              }
+              o[h] = pack16(f.x, f.y, half_type);
+            }
+            *here = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+        }
+        __syncwarp();
+        const int64_t first_row = (int64_t)tile.split * gp.M;
+        if (gp.tma_store) {
+          ptx::fence_proxy_async_smem();  // every lane: its own stores
+          __syncwarp();
+          if (lane == 0) {
+            if (add) ptx::tma_add_3d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0, tile.split);
+            else ptx::tma_store_3d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0, tile.split);
+            ptx::tma_store_commit();
+          }
+        } else if constexpr (OUT32) {  // the lanes on consecutive values of a row
+          if (lane < cols) {
+            float* const to = static_cast<float*>(gp.out) + first_row * gp.N + corner + lane;
+            for (int r = 0; r < rows; ++r) {
+              const float f = reinterpret_cast<const float*>(staged(buf, r, lane >> 2))[lane & 3];
+              to[(int64_t)r * gp.N] = add ? to[(int64_t)r * gp.N] + f : f;
+            }
+          }
+        } else {
+          send_rows16(buf, static_cast<uint16_t*>(gp.out) + first_row * gp.N + corner, gp.N, rows, cols, lane);
+        }
+        __syncwarp();
+      }
+      run += gp.run_blocks;
+      if (tile.k0 + run >= tile.k1) {
+        t += groups;
+        run = 0;
+      }
+    }
+    if (lane == 0) ptx::tma_store_wait_read0();  // the buffers are in use until then
+  }
+  if (timed_out) {
+    *abort_flag = 1;
+    report_status(gp.ws, QB_ERR_TIMEOUT, where);
+  }
+  ptx::tcgen05_fence_before_sync();
+  __syncthreads();
+  if constexpr (CG == 2) ptx::cluster_sync_all();  // the other CTA's MMAs and arrivals reach into this CTA
+  if (warp == 1) {
+    __syncwarp();
+    ptx::tcgen05_fence_after_sync();
+    ptx::tmem_dealloc_cg<CG>(tmem_base, Cfg::kTmemCols);
+  }
+}
+
+template <int BT, int CG, bool OUT32, int MODE>
+static qb_status launch_linear_form(const LinearParams& gp, int sms, cudaStream_t stream) {
+  using Cfg = LinCfg<BT, CG>;
+  auto kernel = linear_kernel<BT, CG, OUT32, MODE>;
+  static std::atomic<bool> attr_set[64] = {};
+  int dev = 0;
+  QB_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+    QB_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes));
+    if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
+  }
+  const int grid = std::min(gp.tiles, sms / CG) * CG;
+  QB_CUDA_TRY(launch_kernel(kernel, (unsigned)grid, kLinThreads, Cfg::kSmemBytes, stream, CG, false, gp));
+  return QB_OK;
+}
+template <int BT, int CG>
+static qb_status launch_linear(const LinearParams& gp, bool out32, int mode, int sms, cudaStream_t stream) {
+  if (out32) return mode == kGelu ? launch_linear_form<BT, CG, true, kGelu>(gp, sms, stream) : launch_linear_form<BT, CG, true, kPlain>(gp, sms, stream);
+  if (mode == kSlope) return launch_linear_form<BT, CG, false, kSlope>(gp, sms, stream);
+  return mode == kGelu ? launch_linear_form<BT, CG, false, kGelu>(gp, sms, stream) : launch_linear_form<BT, CG, false, kPlain>(gp, sms, stream);
+}
+
+// What stands behind a product, as the join of a split one needs it.
+struct LinearTail {
+  const float* bias;
+  const void* side;
+  const int8_t* codes;
+  const float* scales;
+  void* out;
+  void* pre;
+  int32_t mode, out_type, type;
+};
+__device__ __forceinline__ float load_value(const void* p, int64_t i, int type) {
+  if (type == QB_F32) return static_cast<const float*>(p)[i];
+  if (type == QB_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return __half2float(static_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ void store_value(void* p, int64_t i, int type, float v) {
+  if (type == QB_F32) static_cast<float*>(p)[i] = v;
+  else if (type == QB_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  else static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+// out = what stands behind the splits' sum, taken in their order.
+template <int V>
+__global__ void __launch_bounds__(256) linear_join_kernel(const float* parts, int splits, int64_t MN, int N, const LinearTail tail) {
+  pdl_begin();
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V; i < MN; i += (int64_t)gridDim.x * 256 * V) {
+    float v[V];
+    if constexpr (V == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(parts + i);
+    else v[0] = parts[i];
+    for (int s = 1; s < splits; ++s) {
+      float w[V];
+      if constexpr (V == 4) *reinterpret_cast<float4*>(w) = *reinterpret_cast<const float4*>(parts + s * MN + i);
+      else w[0] = parts[s * MN + i];
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] += w[j];
+    }
+    const int64_t m = i / N;
+    const int n = (int)(i - m * N);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {  // (vectors: N is a multiple of 4)
+      float z = v[j];
+      if (tail.bias) z += tail.bias[n + j];
+      if (tail.pre) store_value(tail.pre, i + j, tail.type, z);
+      if (tail.mode == kGelu) z = gelu2(z, z).x;
+      if (tail.mode == kSlope) {
+        const float p = tail.codes ? (float)tail.codes[i + j] * tail.scales[m * checkpoint_blocks(N) + (n + j) / kCheckpointBlock]
+                                   : load_value(tail.side, i + j, tail.type);
+        z *= gelu_slope2(p, p).x;
+      } else if (tail.side) {
+        z += load_value(tail.side, i + j, tail.out_type);
+      }
+      store_value(tail.out, i + j, tail.out_type, z);
+    }
+  }
+}
+
+// Rows of any length as rows of a multiple of 16 bytes, zeros behind them (what a TMA load needs).
+__global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* from, uint16_t* to, int64_t rows, int32_t cols, int32_t pitch) {
+  pdl_begin();
+  const int per_row = pitch / 8;
+  const int64_t n = rows * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per_row;
+    const int c = (int)(i - r * per_row) * 8;
+    uint16_t e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = c + j < cols ? from[r * cols + c + j] : (uint16_t)0;
+    uint4 w;
+    w.x = e[0] | (uint32_t)e[1] << 16;
+    w.y = e[2] | (uint32_t)e[3] << 16;
+    w.z = e[4] | (uint32_t)e[5] << 16;
+    w.w = e[6] | (uint32_t)e[7] << 16;
+    *reinterpret_cast<uint4*>(to + i * 8) = w;
+  }
+}
+
+// Sums of the columns of g [M][N] over its rows, first over runs of rows into parts [runs][N], then over the runs, in their order.
+template <bool VECTOR>
+__global__ void __launch_bounds__(256) column_parts_kernel(const uint16_t* g, int64_t M, int32_t N, int64_t run, int col_blocks, int half_type, float* parts) {
+  __shared__ float sums[8][256];
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t which = blockIdx.x / col_blocks, first = which * run, last = min(first + run, M);
+  const int n0 = ((int)blockIdx.x - (int)which * col_blocks) * 256;
+  float s[8] = {};
+  if constexpr (VECTOR) {
+    const int c = n0 + lane * 8;
+    if (c < N) {
+#pragma unroll 4
+      for (int64_t m = first + warp; m < last; m += 8) {
+        const uint4 w = *reinterpret_cast<const uint4*>(g + m * N + c);
+        const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = unpack16(in[j], half_type != 0);
+          s[2 * j] += f.x;
+          s[2 * j + 1] += f.y;
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[warp][lane * 8 + j] = s[j];
+  } else {
+    for (int64_t m = first + warp; m < last; m += 8)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = n0 + lane + 32 * j;
+        if (c < N) s[j] += unpack16(g[m * N + c], half_type != 0).x;
+      }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[warp][lane + 32 * j] = s[j];
+  }
+  __syncthreads();
+  const int c = n0 + (int)threadIdx.x;
+  if (c < N) {
+    float t = sums[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) t += sums[w][threadIdx.x];
+    parts[which * N + c] = t;
+  }
+}
+__global__ void __launch_bounds__(256) column_join_kernel(const float* parts, int runs, int32_t N, float* sums) {
+  pdl_begin();
+  const int c = (int)(blockIdx.x * 256 + threadIdx.x);
+  if (c >= N) return;
+  float t = parts[c];
+  for (int r = 1; r < runs; ++r) t += parts[(int64_t)r * N + c];
+  sums[c] = t;
+}
+
+static int64_t lin_up(int64_t n, int64_t m) { return (n + m - 1) / m; }
+// The tensor cores cut an accumulator off at its last place at each addition of 16 products, always towards zero: the error grows
+// with their number (24,576 products of random signs: 2.8e-5 of the result, 4,096: a sixth of it).  fp32 outputs are summed in runs of
+// this many K blocks, which are rounded to nearest as they are added up.
+constexpr int kLinRunBlocks = 64;
+constexpr size_t kLinScratchOff = 1024;  // of what calls keep in the workspace besides its header
+
+// The form of a product: CTAs per tile, columns, for pairs how many tiles are whole, and splits of K.
+struct LinearChoice {
+  int cg, bt;
+  int32_t tiles, whole, splits, split_blocks;
+};
+// The cheapest by what a launch and each of its rounds of tiles take, in hundredths of a microsecond: a tile a part per K block of 64 and
+// a fixed part, but no less than its epilogue, the launch the time until the first tile and of the last epilogue.  A last round that fills
+// at most half of the pairs is cut into tiles of half the width.  Where a long K meets few tiles, K is split into runs whose sums a
+// second kernel joins: that costs its launch and the traffic of the parts.
+// `parts`: more than one split where the workspace has room for it.
+static LinearChoice choose_linear(int64_t M, int64_t N, int64_t K, int sms, size_t scratch, bool parts) {
+  static constexpr struct {
+    int cg, bt, block, fixed, least, launch;
+  } kForms[] = {{2, 256, 32, 20, 220, 480}, {1, 128, 27, 37, 120, 310}, {1, 64, 20, 25, 100, 300}};
+  const int64_t blocks = lin_up(K, 64);
+  LinearChoice best = {};
+  int64_t best_cost = 0;
+  for (const auto& f : kForms) {
+    if (f.cg == 2 && sms < 2) continue;
+    const int64_t groups = sms / f.cg, tiles = lin_up(M, 128 * f.cg) * lin_up(N, f.bt);
+    for (int64_t splits = 1; splits == 1 || (4 * splits <= blocks && (tiles * (splits - 1) < groups || (parts && splits == 2)) && splits * M * N * 4 <= (int64_t)scratch); ++splits) {
+      const int64_t run = splits == 1 ? blocks : lin_up(lin_up(blocks, splits), 2) * 2;
+      if (lin_up(blocks, run) != splits) continue;
+      const int64_t tile = std::max<int64_t>(f.block * run + f.fixed, f.least), all = tiles * splits, last = all % groups;
+      const bool halves = f.cg == 2 && splits == 1 && last > 0 && 2 * last <= groups;
+      if (parts && splits == 1 && blocks >= 8 && 2 * M * N * 4 <= (int64_t)scratch) continue;
+      const int64_t cost = f.launch + (all / groups) * tile + (halves ? tile * 7 / 10 : (last > 0 ? tile : 0)) + (splits > 1 ? 250 + splits * M * N / 7500 : 0);
+      if (best.cg == 0 || cost < best_cost) {
+        best_cost = cost;
+        best = {f.cg, f.bt, (int32_t)(halves ? all + last : all), (int32_t)(halves ? all - last : all), (int32_t)splits, (int32_t)run};
+      }
+    }
+  }
+  return best;
+}
+static bool impossible_linear(int64_t M, int64_t N, int64_t K) {
+  if (M <= 0 || N <= 0 || K <= 0 || M > QB_MAX_MN || N > QB_MAX_MN || K > QB_MAX_MN) return true;
+  const int64_t most = (int64_t)1 << 30;  // tiles of each of the three products
+  return lin_up(M, 128) * lin_up(N, 64) > most || lin_up(M, 128) * lin_up(K, 64) > most || lin_up(N, 128) * lin_up(K, 64) > most;
+}
+
+// A call's part of the workspace behind its header, handed out piece by piece.
+struct LinearScratch {
+  char* at;
+  size_t left;
+  LinearScratch(void* ws, size_t bytes) : at(static_cast<char*>(ws) + kLinScratchOff), left(bytes > kLinScratchOff ? bytes - kLinScratchOff : 0) {}
+  void* take(size_t bytes) {
+    bytes = (bytes + 255) / 256 * 256;
+    if (bytes > left) return nullptr;
+    void* const p = at;
+    at += bytes;
+    left -= bytes;
+    return p;
+  }
+};
+static size_t pad_bytes(int64_t rows, int64_t cols) { return cols % 8 == 0 ? 0 : ((size_t)rows * (size_t)lin_up(cols, 8) * 16 + 255) / 256 * 256; }
+
+// An operand: a tensor [rows][cols] whose rows (K-major) or columns (MN-major) the product contracts.
+struct LinearOperand {
+  const void* data;
+  int64_t rows, cols;
+  bool mn;  // contraction along the rows of the tensor
+};
+// The operand as TMA can read it: itself, or a copy with longer rows.
+static qb_status padded(LinearOperand* o, int64_t* pitch, LinearScratch* scratch, int sms, const char* what, cudaStream_t stream) {
+  *pitch = lin_up(o->cols, 8) * 8;
+  if (*pitch == o->cols) return QB_OK;
+  uint16_t* const copy = static_cast<uint16_t*>(scratch->take(pad_bytes(o->rows, o->cols)));
+  if (!copy) {
+    set_last_error("%s: the workspace is too small for rows that are no multiple of 8 elements (qb_linear_workspace_bytes)", what);
+    return QB_ERR_WORKSPACE;
+  }
+  const unsigned grid = (unsigned)std::min<int64_t>(lin_up(o->rows * *pitch, 2048), (int64_t)sms * 16);
+  QB_CUDA_TRY(launch_kernel(pad_rows_kernel, grid, 256, 0, stream, 1, false, static_cast<const uint16_t*>(o->data), copy, o->rows, (int32_t)o->cols, (int32_t)*pitch));
+  o->data = copy;
+  return QB_OK;
+}
+// Map and form of an operand for boxes of `extent` rows or columns of the output.
+static qb_status operand_map(CUtensorMap* tm, int32_t* form, const LinearOperand& o, int64_t pitch, int extent, bool half_type) {
+  const CUtensorMapDataType t = half_type ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  const bool whole = o.cols % 64 == 0;
+  *form = o.mn ? (whole ? kCols : kCols2) : (whole ? kRows : kRows2);
+  if (whole) return make_group_map(tm, t, 2, o.data, o.rows, pitch * 2, o.mn ? 128 : extent, o.mn ? extent / 64 : 2);
+  return make_matrix_map(tm, t, o.data, o.rows, o.cols, pitch * 2, o.mn ? 128 : extent, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// out [M][N] = A B^T over K, and what `tail` says.  `pre_codes`: saved in 8 bits by the epilogue (then K is not split).
+static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, int64_t M, int64_t N, int64_t K, const LinearTail& tail, int8_t* pre_codes,
+                            float* pre_scales, void* ws, LinearScratch scratch, int sms, cudaStream_t stream) {
+  const bool half_type = tail.type == QB_F16;
+  int64_t a_pitch, b_pitch;
+  qb_status st;
+  if ((st = padded(&a, &a_pitch, &scratch, sms, what, stream)) != QB_OK) return st;
+  if ((st = padded(&b, &b_pitch, &scratch, sms, what, stream)) != QB_OK) return st;
+  // a 16-bit output is summed in one run up to 2^16 products, what passes through GELU in fp32 up to kLinRunBlocks
+  const int64_t blocks = lin_up(K, 64);
+  const bool parts_for_sums = tail.out_type == QB_F32 ? tail.mode == kGelu && blocks > kLinRunBlocks : blocks > 1024;
+  const LinearChoice choice = choose_linear(M, N, K, sms, pre_codes ? 0 : scratch.left, parts_for_sums);
+  const int cg = choice.cg, bt = choice.bt;
+  const bool split = choice.splits > 1;
+  const bool out32 = split || tail.out_type == QB_F32;
+  float* const parts = reinterpret_cast<float*>(scratch.at);
+  LinearParams gp;
+  if ((st = operand_map(&gp.tma, &gp.a_form, a, a_pitch, 128, half_type)) != QB_OK) return st;
+  if ((st = operand_map(&gp.tmb, &gp.b_form, b, b_pitch, bt / cg, half_type)) != QB_OK) return st;
+  gp.tmb_half = gp.tmb;
+  if (choice.whole < choice.tiles && (st = operand_map(&gp.tmb_half, &gp.b_form, b, b_pitch, bt / 4, half_type)) != QB_OK) return st;
+  const int64_t row_bytes = N * (out32 ? 4 : 2);
+  gp.tma_store = row_bytes % 16 == 0 && (split || aligned16(tail.out));
+  gp.tmy = gp.tma;
+  if (gp.tma_store && (st = make_parts_map(&gp.tmy, out32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : (half_type ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16),
+                                           split ? parts : tail.out, choice.splits, M, N, row_bytes, 32, out32 ? 32 : 64)) != QB_OK)
+    return st;
+  gp.bias = split ? nullptr : tail.bias;
+  gp.side = split || tail.codes ? nullptr : tail.side;
+  gp.codes = split ? nullptr : tail.codes;
+  gp.scales = tail.scales;
+  gp.out = split ? parts : tail.out;
+  gp.pre = split ? nullptr : tail.pre;
+  gp.pre_codes = pre_codes;
+  gp.pre_scales = pre_scales;
+  gp.vector = row_bytes % 16 == 0 && aligned16(tail.side) && aligned16(tail.pre);
+  gp.vector_codes = N % 16 == 0 && aligned16(tail.codes) && aligned16(pre_codes);
+  gp.ws = ws;
+  gp.M = (int32_t)M;
+  gp.N = (int32_t)N;
+  gp.half_type = half_type;
+  gp.n_tiles = (int32_t)lin_up(N, bt);
+  gp.tiles = choice.tiles;
+  gp.whole = choice.whole;
+  gp.split_tiles = choice.tiles / choice.splits;
+  gp.split_blocks = choice.split_blocks;
+  gp.k_blocks = (int32_t)blocks;
+  gp.run_blocks = split || (out32 && tail.mode == kPlain) ? kLinRunBlocks : (int32_t)blocks;
+  gp.idesc = lin_idesc(half_type, a.mn, b.mn, 128 * cg);
+  const int mode = split ? kPlain : tail.mode;
+  if (cg == 2) st = launch_linear<256, 2>(gp, out32, mode, sms, stream);
+  else if (bt == 128) st = launch_linear<128, 1>(gp, out32, mode, sms, stream);
+  else st = launch_linear<64, 1>(gp, out32, mode, sms, stream);
+  if (st != QB_OK || !split) return st;
+  const bool vector = N % 4 == 0;
+  QB_CUDA_TRY(launch_kernel(vector ? linear_join_kernel<4> : linear_join_kernel<1>, (unsigned)std::min<int64_t>(lin_up(M * N, vector ? 1024 : 256), (int64_t)sms * 8), 256, 0,
+                            stream, 1, false, parts, choice.splits, M * N, (int)N, tail));
+  return QB_OK;
+}
+
+// Runs of rows for the column sums: about eight blocks per SM, no run shorter than 32 rows.
+static int64_t column_runs(int64_t M, int64_t N, int sms) {
+  return std::max<int64_t>(1, std::min<int64_t>(lin_up(M, 32), std::max<int64_t>(1, (int64_t)sms * 8 / lin_up(N, 256))));
+}
+
+static qb_status check_linear(const char* what, const void* const (&needed)[4], int type, int out_type, int64_t M, int64_t N, int64_t K) {
+  bool ok = (type == QB_BF16 || type == QB_F16) && (out_type == type || out_type == QB_F32) && !impossible_linear(M, N, K);
+  for (const void* p : needed) ok = ok && p;
+  if (ok) return QB_OK;
+  set_last_error("%s: invalid argument (M=%lld N=%lld K=%lld type %d, output type %d)", what, (long long)M, (long long)N, (long long)K, type, out_type);
+  return QB_ERR_INVALID;
+}
+static qb_status check_linear_ws(const char* what, const void* ws, size_t ws_bytes) {
+  if (ws && aligned16(ws) && ws_bytes >= kWsMinBytes) return QB_OK;
+  set_last_error("%s: workspace null, not 16-byte aligned or too small", what);
+  return QB_ERR_WORKSPACE;
+}
+static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace qb
+
+extern "C" size_t qb_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  using namespace qb;
+  if (impossible_linear(M, N, K)) return 0;
+  const size_t pads = pad_bytes(M, K) + pad_bytes(N, K) + pad_bytes(M, N);
+  const size_t sums = ((size_t)column_runs(M, N, 160) * (size_t)N * 4 + 255) / 256 * 256;
+  // parts of a split product: where its output is small against the device
+  const int64_t outs[3] = {M * N, M * K, N * K};
+  size_t parts = 0;
+  for (int64_t n : outs) parts = std::max(parts, (size_t)std::min<int64_t>(n * 16, (int64_t)16 << 20) * 4);
+  return kLinScratchOff + pads + sums + parts;
+}
+
+extern "C" int32_t qb_linear_tile_columns(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int32_t* half_tiles, int32_t* splits) {
+  using namespace qb;
+  if (impossible_linear(M, N, K)) return 0;
+  int sms = 148;
+  require_sm100(&sms);  // without a device: for a 148-SM part
+  const LinearChoice c = choose_linear(M, N, K, sms, ws_bytes > kLinScratchOff ? ws_bytes - kLinScratchOff : 0, false);
+  if (half_tiles) *half_tiles = c.tiles - c.whole;
+  if (splits) *splits = c.splits;
+  return c.bt;
+}
+
+extern "C" qb_status qb_linear(const void* x, const void* w, int type, const float* bias, int activation, const void* residual, int64_t M, int64_t N, int64_t K,
+                               int out_type, void* y, void* pre, int8_t* pre_codes, float* pre_scales, void* ws, size_t ws_bytes, void* cuda_stream) {
+  using namespace qb;
+  const char* const what = "qb_linear";
+  qb_status st = check_linear(what, {x, w, y, y}, type, out_type, M, N, K);
+  if (st != QB_OK) return st;
+  if (activation < QB_IDENTITY || activation > QB_GELU || (pre_codes != nullptr) != (pre_scales != nullptr) || (pre && pre_codes) ||
+      ((pre || pre_codes) && out_type != type)) {
+    set_last_error("qb_linear: invalid activation (%d), or a pre-activation saved in both forms, without its scales or beside an fp32 output", activation);
+    return QB_ERR_INVALID;
+  }
+  const size_t e = out_type == QB_F32 ? 4 : 2;
+  if (!aligned16(x) || !aligned16(w) || !aligned_to(bias, 4) || !aligned_to(residual, e) || !aligned_to(y, e) || !aligned_to(pre, 2) || !aligned_to(pre_scales, 4)) {
+    set_last_error("qb_linear: x and w must be 16-byte aligned, the others aligned to their elements");
+    return QB_ERR_ALIGN;
+  }
+  if ((st = check_linear_ws(what, ws, ws_bytes)) != QB_OK) return st;
+  int sms = 0;
+  if ((st = require_sm100(&sms)) != QB_OK) return st;
+  const LinearTail tail = {bias, residual, nullptr, nullptr, y, pre, activation == QB_GELU ? kGelu : kPlain, out_type, type};
+  return run_linear(what, {x, M, K, false}, {w, N, K, false}, M, N, K, tail, pre_codes, pre_scales, ws, LinearScratch(ws, ws_bytes), sms, (cudaStream_t)cuda_stream);
+}
+
+extern "C" qb_status qb_linear_grad_x(const void* grad_y, const void* w, int type, const void* pre, const int8_t* pre_codes, const float* pre_scales,
+                                      const void* residual, int64_t M, int64_t N, int64_t K, void* grad_x, void* ws, size_t ws_bytes, void* cuda_stream) {
+  using namespace qb;
+  const char* const what = "qb_linear_grad_x";
+  qb_status st = check_linear(what, {grad_y, w, grad_x, grad_x}, type, type, M, N, K);
+  if (st != QB_OK) return st;
+  if ((pre_codes != nullptr) != (pre_scales != nullptr) || (pre && pre_codes) || (residual && (pre || pre_codes))) {
+    set_last_error("qb_linear_grad_x: a pre-activation in both forms, codes without scales, or a residual beside a pre-activation");
+    return QB_ERR_INVALID;
+  }
+  if (!aligned16(grad_y) || !aligned16(w) || !aligned_to(residual, 2) || !aligned_to(grad_x, 2) || !aligned_to(pre, 2) || !aligned_to(pre_scales, 4)) {
+    set_last_error("qb_linear_grad_x: grad_y and w must be 16-byte aligned, the others aligned to their elements");
+    return QB_ERR_ALIGN;
+  }
+  if ((st = check_linear_ws(what, ws, ws_bytes)) != QB_OK) return st;
+  int sms = 0;
+  if ((st = require_sm100(&sms)) != QB_OK) return st;
+  const LinearTail tail = {nullptr, pre ? pre : residual, pre_codes, pre_scales, grad_x, nullptr, pre || pre_codes ? kSlope : kPlain, type, type};
+  return run_linear(what, {grad_y, M, N, false}, {w, N, K, true}, M, K, N, tail, nullptr, nullptr, ws, LinearScratch(ws, ws_bytes), sms, (cudaStream_t)cuda_stream);
+}
+
+extern "C" qb_status qb_linear_grad_w(const void* grad_y, const void* x, int type, int64_t M, int64_t N, int64_t K, int out_type, void* grad_w, float* grad_bias,
+                                      void* ws, size_t ws_bytes, void* cuda_stream) {
+  using namespace qb;
+  const char* const what = "qb_linear_grad_w";
+  const void* const either = grad_w ? grad_w : grad_bias;
+  qb_status st = check_linear(what, {grad_y, grad_w ? x : grad_y, either, either}, type, out_type, M, N, K);
+  if (st != QB_OK) return st;
+  if (!aligned16(grad_y) || !aligned16(x) || !aligned_to(grad_w, out_type == QB_F32 ? 4 : 2) || !aligned_to(grad_bias, 4)) {
+    set_last_error("qb_linear_grad_w: grad_y and x must be 16-byte aligned, the others aligned to their elements");
+    return QB_ERR_ALIGN;
+  }
+  if ((st = check_linear_ws(what, ws, ws_bytes)) != QB_OK) return st;
+  int sms = 0;
+  if ((st = require_sm100(&sms)) != QB_OK) return st;
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  LinearScratch scratch(ws, ws_bytes);
+  if (grad_bias) {
+    const int64_t run = lin_up(M, column_runs(M, N, sms)), runs = lin_up(M, run);
+    float* const parts = static_cast<float*>(scratch.take((size_t)runs * (size_t)N * 4));
+    if (!parts) {
+      set_last_error("qb_linear_grad_w: the workspace is too small for the bias's gradient (qb_linear_workspace_bytes)");
+      return QB_ERR_WORKSPACE;
+    }
+    auto sum = N % 8 == 0 ? column_parts_kernel<true> : column_parts_kernel<false>;
+    const int col_blocks = (int)lin_up(N, 256);
+    QB_CUDA_TRY(launch_kernel(sum, (unsigned)(col_blocks * runs), 256, 0, stream, 1, false, static_cast<const uint16_t*>(grad_y), M, (int32_t)N, run, col_blocks,
+                              (int)(type == QB_F16), parts));
+    QB_CUDA_TRY(launch_kernel(column_join_kernel, (unsigned)col_blocks, 256, 0, stream, 1, false, parts, (int)runs, (int32_t)N, grad_bias));
+  }
+  if (!grad_w) return QB_OK;
+  const LinearTail tail = {nullptr, nullptr, nullptr, nullptr, grad_w, nullptr, kPlain, out_type, type};
+  return run_linear(what, {grad_y, M, N, true}, {x, M, K, true}, N, K, M, tail, nullptr, nullptr, ws, scratch, sms, stream);
+}
