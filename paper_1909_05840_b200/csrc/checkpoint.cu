@@ -159,18 +159,12 @@ __global__ void __launch_bounds__(kCheckpointThreads) activation_kernel(const T*
     } else {
       v[u].get(p);
     }
-    if constexpr (USE == kSlopeOf) g[u].get(d);
+    if constexpr (USE == kActivation) gelu_many<N / 2>(p);
+    if constexpr (USE == kSlopeOf) {
+      g[u].get(d);
+      gelu_slope_many<N / 2>(p);
 #pragma unroll
-    for (int j = 0; j < N; j += 2) {
-      float2 f = make_float2(p[j], p[j + 1]);
-      if constexpr (USE == kActivation) f = gelu2(f.x, f.y);
-      if constexpr (USE == kSlopeOf) {
-        f = gelu_slope2(f.x, f.y);
-        f.x *= d[j];
-        f.y *= d[j + 1];
-      }
-      p[j] = f.x;
-      p[j + 1] = f.y;
+      for (int j = 0; j < N; ++j) p[j] *= d[j];
     }
     const CheckpointAt<N, FLAT> at(i, K, blocks);
     Vec16<T> out;

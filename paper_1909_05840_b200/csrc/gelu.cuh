@@ -18,39 +18,66 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// The terms of P pairs at a time, step by step for all of them: a pair's chain is some thirty dependent instructions, and one or two warps
+// of a scheduler do not hide it.
+template <int P>
 struct GeluTerms {
-  uint64_t u, e;  // min(|x|, 5.75), exp(-x^2 / 2)
-};
-__device__ __forceinline__ GeluTerms gelu_terms(float a, float b) {
-  GeluTerms t;
-  t.u = ptx::pack_f32x2(fminf(fabsf(a), 5.75f), fminf(fabsf(b), 5.75f));
-  const uint64_t x = ptx::pack_f32x2(a, b);
-  const float half_log2e = -0.72134752f;
-  const float2 p = ptx::unpack_f32x2(ptx::mul_f32x2(ptx::mul_f32x2(x, x), ptx::pack_f32x2(half_log2e, half_log2e)));
-  t.e = ptx::pack_f32x2(exp2_approx(p.x), exp2_approx(p.y));
-  return t;
-}
-// c0 + c1 u + (R's terms from the second degree on, with their signs turned)
-__device__ __forceinline__ uint64_t gelu_poly(uint64_t u, float c0, float c1) {
-  constexpr float c[10] = {-0.24984169006347656f, 0.13220742344856262f,    -0.06054938957095146f,  0.023666609078645706f,  -0.0075540607795119286f,
-                           0.0018558446317911148f, -0.0003288344305474311f, 3.888118953909725e-05f, -2.715689788601594e-06f, 8.416543550993083e-08f};
-  uint64_t p = ptx::pack_f32x2(c[9], c[9]);
+  uint64_t u[P], e[P];  // min(|x|, 5.75), exp(-x^2 / 2)
+  __device__ __forceinline__ explicit GeluTerms(const float* x) {
+    const float half_log2e = -0.72134752f;
+    const uint64_t scale = ptx::pack_f32x2(half_log2e, half_log2e);
 #pragma unroll
-  for (int i = 8; i >= 0; --i) p = ptx::fma_f32x2(p, u, ptx::pack_f32x2(c[i], c[i]));
-  p = ptx::fma_f32x2(p, u, ptx::pack_f32x2(c1, c1));
-  return ptx::fma_f32x2(p, u, ptx::pack_f32x2(c0, c0));
+    for (int i = 0; i < P; ++i) {
+      const uint64_t v = ptx::pack_f32x2(x[2 * i], x[2 * i + 1]);
+      e[i] = ptx::mul_f32x2(ptx::mul_f32x2(v, v), scale);
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const float2 f = ptx::unpack_f32x2(e[i]);
+      e[i] = ptx::pack_f32x2(exp2_approx(f.x), exp2_approx(f.y));
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) u[i] = ptx::pack_f32x2(fminf(fabsf(x[2 * i]), 5.75f), fminf(fabsf(x[2 * i + 1]), 5.75f));
+  }
+  // c0 + c1 u + (R's terms from the second degree on, with their signs turned)
+  __device__ __forceinline__ void poly(float c0, float c1, uint64_t (&p)[P]) const {
+    constexpr float c[10] = {-0.24984169006347656f, 0.13220742344856262f,    -0.06054938957095146f,  0.023666609078645706f,  -0.0075540607795119286f,
+                             0.0018558446317911148f, -0.0003288344305474311f, 3.888118953909725e-05f, -2.715689788601594e-06f, 8.416543550993083e-08f};
+#pragma unroll
+    for (int i = 0; i < P; ++i) p[i] = ptx::fma_f32x2(u[i], ptx::pack_f32x2(c[9], c[9]), ptx::pack_f32x2(c[8], c[8]));
+#pragma unroll
+    for (int k = 7; k >= -2; --k) {
+      const float f = k >= 0 ? c[k >= 0 ? k : 0] : (k == -1 ? c1 : c0);
+#pragma unroll
+      for (int i = 0; i < P; ++i) p[i] = ptx::fma_f32x2(p[i], u[i], ptx::pack_f32x2(f, f));
+    }
+  }
+};
+// gelu of 2 P values, in place
+template <int P>
+__device__ __forceinline__ void gelu_many(float* x) {
+  const GeluTerms<P> t(x);
+  uint64_t r[P];
+  t.poly(-0.4999998211860657f, 0.3989296555519104f, r);  // -R
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const float2 f = ptx::unpack_f32x2(ptx::fma_f32x2(ptx::mul_f32x2(t.u[i], t.e[i]), r[i], ptx::pack_f32x2(fmaxf(x[2 * i], 0.0f), fmaxf(x[2 * i + 1], 0.0f))));
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
 }
-// gelu of both values
-__device__ __forceinline__ float2 gelu2(float a, float b) {
-  const GeluTerms t = gelu_terms(a, b);
-  const uint64_t r = gelu_poly(t.u, -0.4999998211860657f, 0.3989296555519104f);  // -R
-  return ptx::unpack_f32x2(ptx::fma_f32x2(ptx::mul_f32x2(t.u, t.e), r, ptx::pack_f32x2(fmaxf(a, 0.0f), fmaxf(b, 0.0f))));
-}
-// gelu' of both values
-__device__ __forceinline__ float2 gelu_slope2(float a, float b) {
-  const GeluTerms t = gelu_terms(a, b);
-  const float2 s = ptx::unpack_f32x2(ptx::mul_f32x2(t.e, gelu_poly(t.u, -0.4999998211860657f, 0.3989296555519104f + 0.39894228f)));  // e (u / sqrt(2 pi) - R)
-  return make_float2(a < 0.0f ? -s.x : 1.0f + s.x, b < 0.0f ? -s.y : 1.0f + s.y);
+// gelu' of 2 P values, in place
+template <int P>
+__device__ __forceinline__ void gelu_slope_many(float* x) {
+  const GeluTerms<P> t(x);
+  uint64_t r[P];
+  t.poly(-0.4999998211860657f, 0.3989296555519104f + 0.39894228f, r);  // u / sqrt(2 pi) - R
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const float2 s = ptx::unpack_f32x2(ptx::mul_f32x2(t.e[i], r[i]));
+    x[2 * i] = x[2 * i] < 0.0f ? -s.x : 1.0f + s.x;
+    x[2 * i + 1] = x[2 * i + 1] < 0.0f ? -s.y : 1.0f + s.y;
+  }
 }
 
 }  // namespace qb

@@ -58,8 +58,8 @@ struct LinearParams {
   int32_t k_blocks;      // of all splits
   int32_t run_blocks;    // K blocks that one accumulator sums; even where a split has several such runs (fp32 out), which are added up in out
   int32_t tma_store;     // 1: rows of out are 16-byte aligned
-  int32_t vector;        // 1: rows of side and of pre too
-  int32_t vector_codes;  // 1: rows of the codes too
+  int32_t vector;        // 1: rows of side and of pre are 32-byte aligned
+  int32_t vector_codes;  // 1: rows of the codes are
   uint32_t idesc;
 };
 
@@ -145,25 +145,16 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool half_type) {
 // A warp's staging buffer: 32 rows of 128 bytes, 16-byte pieces swizzled so that the lanes meet different banks both with a row a
 // lane and with a row an eighth of a warp.
 __device__ __forceinline__ uint4* staged(uint8_t* buf, int row, int piece) { return reinterpret_cast<uint4*>(buf + row * 128 + ((piece ^ (row & 7)) << 4)); }
-// The same for rows of 64 bytes (codes).
-__device__ __forceinline__ uint4* staged_codes(uint8_t* buf, int row, int piece) {
-  return reinterpret_cast<uint4*>(buf + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
+// 32 bytes of a row: whole sectors, where 16 bytes a lane would touch each of them twice.
+__device__ __forceinline__ void load32(const void* p, uint4& a, uint4& b) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+               : "l"(p));
 }
-
-// `rows` rows of `cols` codes from the staging buffer to rows `pitch` bytes apart; `vector`: 16-byte aligned ones.
-__device__ __forceinline__ void send_codes(uint8_t* buf, int8_t* to, int64_t pitch, int rows, int cols, int lane, bool vector) {
-  if (vector) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = 8 * k + (lane >> 2), p = lane & 3;
-      if (r < rows && 16 * p < cols) *reinterpret_cast<uint4*>(to + r * pitch + 16 * p) = *staged_codes(buf, r, p);
-    }
-  } else {
-    for (int r = 0; r < rows; ++r)
-#pragma unroll
-      for (int c = lane; c < 64; c += 32)
-        if (c < cols) to[r * pitch + c] = reinterpret_cast<const int8_t*>(staged_codes(buf, r, c >> 4))[c & 15];
-  }
+__device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z),
+               "r"(b.w)
+               : "memory");
 }
 
 // `rows` rows of `cols` 16-bit values from the staging buffer to rows of any alignment, `pitch` elements apart: a row at a time, the
@@ -388,17 +379,26 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       asm volatile("" : "+r"(m0), "+r"(n0), "+r"(chunks));  // formed before the wait, not behind it
       bias_tile[a * 256 + e] = bias && e < BT && n0 + e < gp.N ? bias[n0 + e] : 0.0f;
       const int rows = min(32, gp.M - m0);
-      // The chunk's part of the tensor beside the product (residual, pre-activation), fetched while the products run: 16 bytes a lane,
-      // whole lines.
+      const bool mine = lane < rows;
+      // The chunk's part of the tensor beside the product (residual, pre-activation, codes of it): the lane's row, fetched while the
+      // products run.
       uint4 s[8];
       auto fetch = [&](int c0) {
-        if (!side || !gp.vector) return;
-        const uint8_t* const from = static_cast<const uint8_t*>(side) + ((int64_t)m0 * gp.N + n0 + c0) * kESize;
+        const int64_t corner = (int64_t)(m0 + lane) * gp.N + n0 + c0;
+        if (MODE == kSlope && gp.codes) {
+          if (!gp.vector_codes) return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = 4 * i + (lane >> 3), p = lane & 7;
-          s[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < rows && n0 + c0 + p * (16 / kESize) < gp.N) s[i] = *reinterpret_cast<const uint4*>(from + (int64_t)r * gp.N * kESize + p * 16);
+          for (int k = 0; k < 4; k += 2) {
+            s[k] = s[k + 1] = make_uint4(0u, 0u, 0u, 0u);
+            if (mine && n0 + c0 + 16 * k < gp.N) load32(gp.codes + corner + 16 * k, s[k], s[k + 1]);
+          }
+        } else if (side && gp.vector) {
+          const uint8_t* const from = static_cast<const uint8_t*>(side) + corner * kESize;
+#pragma unroll
+          for (int k = 0; k < 8; k += 2) {
+            s[k] = s[k + 1] = make_uint4(0u, 0u, 0u, 0u);
+            if (mine && n0 + c0 + k * (16 / kESize) < gp.N) load32(from + 16 * k, s[k], s[k + 1]);
+          }
         }
       };
       if (half < chunks) fetch(half * kCols);
@@ -416,158 +416,171 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         const int c0 = i * kCols, cols = min(kCols, gp.N - n0 - c0);
         const int64_t corner = (int64_t)m0 * gp.N + n0 + c0;  // of the chunk, in elements
         const int64_t block = (int64_t)(m0 + lane) * checkpoint_blocks(gp.N) + (n0 + c0) / kCheckpointBlock;  // the row's, in scales
-        uint32_t v[kParts][32];
+        uint32_t w[kParts][32];
 #pragma unroll
-        for (int p = 0; p < kParts; ++p) ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(c0 + 32 * p), v[p]);
-        if (lane == 0) {  // the chunk before has left the buffer; what is added to has been written
-          if (add && i == half) ptx::tma_store_wait0();
-          else ptx::tma_store_wait_read0();
-        }
-        __syncwarp();
-        uint4 q[4];  // kSlope: the row's codes
-        float q_scale = 1.0f;
-        if (MODE == kSlope && gp.codes) {
-          if (gp.vector_codes) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int r = 8 * k + (lane >> 2), p = lane & 3;
-              uint4 w = make_uint4(0u, 0u, 0u, 0u);
-              if (r < rows && 16 * p < cols) w = *reinterpret_cast<const uint4*>(gp.codes + corner + (int64_t)r * gp.N + 16 * p);
-              *staged_codes(buf, r, p) = w;
-            }
-          } else {
-            for (int r = 0; r < rows; ++r)
-#pragma unroll
-              for (int c = lane; c < 64; c += 32)
-                reinterpret_cast<int8_t*>(staged_codes(buf, r, c >> 4))[c & 15] = c < cols ? gp.codes[corner + (int64_t)r * gp.N + c] : (int8_t)0;
-          }
-          if (lane < rows) q_scale = gp.scales[block];
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 4; ++k) q[k] = *staged_codes(buf, lane, k);
-          __syncwarp();
-        }
+        for (int p = 0; p < kParts; ++p) ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(c0 + 32 * p), w[p]);
+        float scale = 1.0f;
+        if (MODE == kSlope && gp.codes && mine) scale = gp.scales[block];
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int p = 0; p < kParts; ++p) ptx::tmem_ld_regs_ready(v[p]);
+        for (int p = 0; p < kParts; ++p) ptx::tmem_ld_regs_ready(w[p]);
         if (i + 2 >= chunks) arrive(acc_empty(a));
+        float v[kCols];
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) v[j] = __uint_as_float(w[j >> 5][j & 31]);
+        bool waited = false;  // for the chunk before to have left the buffer, and for what is added to to have been written
+        auto buffer_free = [&]() {
+          if (waited) return;
+          waited = true;
+          if (lane == 0) {
+            if (add && i == half) ptx::tma_store_wait0();
+            else ptx::tma_store_wait_read0();
+          }
+          __syncwarp();
+        };
+        // rows of any alignment come by way of the buffer
+        if (MODE == kSlope && gp.codes && !gp.vector_codes) {
+          buffer_free();
+          for (int r = 0; r < rows; ++r)
+#pragma unroll
+            for (int c = lane; c < 64; c += 32)
+              reinterpret_cast<int8_t*>(staged(buf, r, c >> 4))[c & 15] = c < cols ? gp.codes[corner + (int64_t)r * gp.N + c] : (int8_t)0;
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s[k] = *staged(buf, lane, k);
+          __syncwarp();
+        } else if (side && !gp.vector) {
+          buffer_free();
+          for (int r = 0; r < rows; ++r) {
+            if constexpr (OUT32) {
+              reinterpret_cast<float*>(staged(buf, r, lane >> 2))[lane & 3] = lane < cols ? static_cast<const float*>(side)[corner + (int64_t)r * gp.N + lane] : 0.0f;
+            } else {
+#pragma unroll
+              for (int c = lane; c < 64; c += 32)
+                reinterpret_cast<uint16_t*>(staged(buf, r, c >> 3))[c & 7] =
+                    c < cols ? static_cast<const uint16_t*>(side)[corner + (int64_t)r * gp.N + c] : (uint16_t)0;
+            }
+          }
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[k] = *staged(buf, lane, k);
+          __syncwarp();
+        }
         // z = product + bias
         if (MODE != kSlope && bias) {
           const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + a * 256 + c0);
 #pragma unroll
           for (int j = 0; j < kCols / 4; ++j) {
             const float4 b = b4[j];
-            uint32_t* const z = &v[j >> 3][(j & 7) * 4];
-            z[0] = __float_as_uint(__uint_as_float(z[0]) + b.x);
-            z[1] = __float_as_uint(__uint_as_float(z[1]) + b.y);
-            z[2] = __float_as_uint(__uint_as_float(z[2]) + b.z);
-            z[3] = __float_as_uint(__uint_as_float(z[3]) + b.w);
+            v[4 * j] += b.x;
+            v[4 * j + 1] += b.y;
+            v[4 * j + 2] += b.z;
+            v[4 * j + 3] += b.w;
           }
         }
-        const auto at = [&](int j) { return __uint_as_float(v[j >> 5][j & 31]); };
         if constexpr (!OUT32 && MODE != kSlope) {
           if (gp.pre_codes) {  // z in 8 bits: a chunk is a block
             float top = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 64; j += 2) top = max3_nan(top, fabsf(at(j)), fabsf(at(j + 1)));
+            for (int j = 0; j < 64; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
             const CheckpointScale cs(top);
-            if (lane < rows) gp.pre_scales[block] = cs.scale;
+            if (mine) gp.pre_scales[block] = cs.scale;
+            uint4 c[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              uint4 w;
-              w.x = cs.codes4(at(16 * k), at(16 * k + 1), at(16 * k + 2), at(16 * k + 3));
-              w.y = cs.codes4(at(16 * k + 4), at(16 * k + 5), at(16 * k + 6), at(16 * k + 7));
-              w.z = cs.codes4(at(16 * k + 8), at(16 * k + 9), at(16 * k + 10), at(16 * k + 11));
-              w.w = cs.codes4(at(16 * k + 12), at(16 * k + 13), at(16 * k + 14), at(16 * k + 15));
-              *staged_codes(buf, lane, k) = w;
+              c[k].x = cs.codes4(v[16 * k], v[16 * k + 1], v[16 * k + 2], v[16 * k + 3]);
+              c[k].y = cs.codes4(v[16 * k + 4], v[16 * k + 5], v[16 * k + 6], v[16 * k + 7]);
+              c[k].z = cs.codes4(v[16 * k + 8], v[16 * k + 9], v[16 * k + 10], v[16 * k + 11]);
+              c[k].w = cs.codes4(v[16 * k + 12], v[16 * k + 13], v[16 * k + 14], v[16 * k + 15]);
             }
-            __syncwarp();
-            send_codes(buf, gp.pre_codes + corner, gp.N, rows, cols, lane, gp.vector_codes != 0);
-            __syncwarp();
+            int8_t* const to = gp.pre_codes + corner;
+            if (gp.vector_codes) {
+#pragma unroll
+              for (int k = 0; k < 4; k += 2)
+                if (mine && 16 * k < cols) store32(to + (int64_t)lane * gp.N + 16 * k, c[k], c[k + 1]);
+            } else {
+              buffer_free();
+#pragma unroll
+              for (int k = 0; k < 4; ++k) *staged(buf, lane, k) = c[k];
+              __syncwarp();
+              for (int r = 0; r < rows; ++r)
+#pragma unroll
+                for (int col = lane; col < 64; col += 32)
+                  if (col < cols) to[(int64_t)r * gp.N + col] = reinterpret_cast<const int8_t*>(staged(buf, r, col >> 4))[col & 15];
+              __syncwarp();
+            }
           } else if (gp.pre) {  // z in 16 bits
             uint16_t* const to = static_cast<uint16_t*>(gp.pre) + corner;
+            uint4 c[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              *staged(buf, lane, k) = make_uint4(pack16(at(8 * k), at(8 * k + 1), half_type), pack16(at(8 * k + 2), at(8 * k + 3), half_type),
-                                                 pack16(at(8 * k + 4), at(8 * k + 5), half_type), pack16(at(8 * k + 6), at(8 * k + 7), half_type));
-            __syncwarp();
+              c[k] = make_uint4(pack16(v[8 * k], v[8 * k + 1], half_type), pack16(v[8 * k + 2], v[8 * k + 3], half_type), pack16(v[8 * k + 4], v[8 * k + 5], half_type),
+                                pack16(v[8 * k + 6], v[8 * k + 7], half_type));
             if (gp.vector) {
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const int r = 4 * k + (lane >> 3), p = lane & 7;
-                if (r < rows && 8 * p < cols) *reinterpret_cast<uint4*>(to + (int64_t)r * gp.N + 8 * p) = *staged(buf, r, p);
-              }
+              for (int k = 0; k < 8; k += 2)
+                if (mine && 8 * k < cols) store32(to + (int64_t)lane * gp.N + 8 * k, c[k], c[k + 1]);
             } else {
+              buffer_free();
+#pragma unroll
+              for (int k = 0; k < 8; ++k) *staged(buf, lane, k) = c[k];
+              __syncwarp();
               send_rows16(buf, to, gp.N, rows, cols, lane);
+              __syncwarp();
             }
-            __syncwarp();
           }
         }
-        if (side) {
-          if (gp.vector) {
+        if constexpr (MODE == kGelu) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) *staged(buf, 4 * k + (lane >> 3), lane & 7) = s[k];
-            if (i + 2 < chunks) fetch(c0 + 2 * kCols);
-          } else {
-            for (int r = 0; r < rows; ++r) {
-              if constexpr (OUT32) {
-                reinterpret_cast<float*>(staged(buf, r, lane >> 2))[lane & 3] = lane < cols ? static_cast<const float*>(side)[corner + (int64_t)r * gp.N + lane] : 0.0f;
+          for (int j = 0; j < kCols; j += 16) gelu_many<8>(v + j);
+        }
+        if constexpr (MODE == kSlope) {
+#pragma unroll
+          for (int j = 0; j < kCols; j += 16) {
+            float p[16];
+#pragma unroll
+            for (int h = 0; h < 8; ++h) {
+              if (gp.codes) {
+                const uint4& q = s[j >> 4];
+                const uint32_t word = h < 2 ? q.x : (h < 4 ? q.y : (h < 6 ? q.z : q.w));
+                p[2 * h] = code_value(word, (h & 1) * 2) * scale;
+                p[2 * h + 1] = code_value(word, (h & 1) * 2 + 1) * scale;
               } else {
-#pragma unroll
-                for (int c = lane; c < 64; c += 32)
-                  reinterpret_cast<uint16_t*>(staged(buf, r, c >> 3))[c & 7] =
-                      c < cols ? static_cast<const uint16_t*>(side)[corner + (int64_t)r * gp.N + c] : (uint16_t)0;
+                const uint4& q = s[(j >> 3) + (h >> 2)];
+                const float2 f = unpack16((h & 3) == 0 ? q.x : ((h & 3) == 1 ? q.y : ((h & 3) == 2 ? q.z : q.w)), half_type);
+                p[2 * h] = f.x;
+                p[2 * h + 1] = f.y;
               }
             }
-          }
-          __syncwarp();
-        }
+            gelu_slope_many<8>(p);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {  // 16 bytes of the row at a time
-          uint4* const here = staged(buf, lane, k);
-          uint4 w = make_uint4(0u, 0u, 0u, 0u);
-          if (side) w = *here;
-          if constexpr (OUT32) {
-            float2 f = make_float2(at(4 * k), at(4 * k + 1)), g = make_float2(at(4 * k + 2), at(4 * k + 3));
-            if constexpr (MODE == kGelu) {
-              f = gelu2(f.x, f.y);
-              g = gelu2(g.x, g.y);
-            }
-            if (side) {
-              f.x += __uint_as_float(w.x);
-              f.y += __uint_as_float(w.y);
-              g.x += __uint_as_float(w.z);
-              g.y += __uint_as_float(w.w);
-            }
-            *here = make_uint4(__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(g.x), __float_as_uint(g.y));
-          } else {
-            uint32_t o[4];
-            const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+            for (int h = 0; h < 16; ++h) v[j + h] *= p[h];
+          }
+        } else if (side) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const uint32_t in[4] = {s[k].x, s[k].y, s[k].z, s[k].w};
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-              float2 f = make_float2(at(8 * k + 2 * h), at(8 * k + 2 * h + 1));
-              if constexpr (MODE == kGelu) f = gelu2(f.x, f.y);
-              if constexpr (MODE == kSlope) {
-                float2 p;
-                if (gp.codes) {
-                  const uint4& qk = q[k >> 1];
-                  const uint32_t word = (k & 1) ? (h < 2 ? qk.z : qk.w) : (h < 2 ? qk.x : qk.y);
-                  p = make_float2(code_value(word, (h & 1) * 2) * q_scale, code_value(word, (h & 1) * 2 + 1) * q_scale);
-                } else {
-                  p = unpack16(in[h], half_type);
-                }
-                const float2 slope = gelu_slope2(p.x, p.y);
-                f.x *= slope.x;
-                f.y *= slope.y;
-              } else if (side) {
+              if constexpr (OUT32) {
+                v[4 * k + h] += __uint_as_float(in[h]);
+              } else {
                 const float2 r = unpack16(in[h], half_type);
-                f.x += r.x;
-                f.y += r.y;
+                v[8 * k + 2 * h] += r.x;
+                v[8 * k + 2 * h + 1] += r.y;
               }
-              o[h] = pack16(f.x, f.y, half_type);
             }
-            *here = make_uint4(o[0], o[1], o[2], o[3]);
           }
+        }
+        if (i + 2 < chunks) fetch(c0 + 2 * kCols);
+        buffer_free();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {  // 16 bytes of the row at a time
+          if constexpr (OUT32)
+            *staged(buf, lane, k) = make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3]));
+          else
+            *staged(buf, lane, k) = make_uint4(pack16(v[8 * k], v[8 * k + 1], half_type), pack16(v[8 * k + 2], v[8 * k + 3], half_type),
+                                               pack16(v[8 * k + 4], v[8 * k + 5], half_type), pack16(v[8 * k + 6], v[8 * k + 7], half_type));
         }
         __syncwarp();
         const int64_t first_row = (int64_t)tile.split * gp.M;
@@ -587,10 +600,11 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
               to[(int64_t)r * gp.N] = add ? to[(int64_t)r * gp.N] + f : f;
             }
           }
+          __syncwarp();
         } else {
           send_rows16(buf, static_cast<uint16_t*>(gp.out) + first_row * gp.N + corner, gp.N, rows, cols, lane);
+          __syncwarp();
         }
-        __syncwarp();
       }
       run += gp.run_blocks;
       if (tile.k0 + run >= tile.k1) {
@@ -656,6 +670,16 @@ __device__ __forceinline__ void store_value(void* p, int64_t i, int type, float 
   else if (type == QB_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
   else static_cast<__half*>(p)[i] = __float2half_rn(v);
 }
+__device__ __forceinline__ float gelu_one(float z) {
+  float f[2] = {z, z};
+  gelu_many<1>(f);
+  return f[0];
+}
+__device__ __forceinline__ float gelu_slope_one(float z) {
+  float f[2] = {z, z};
+  gelu_slope_many<1>(f);
+  return f[0];
+}
 // out = what stands behind the splits' sum, taken in their order.
 template <int V>
 __global__ void __launch_bounds__(256) linear_join_kernel(const float* parts, int splits, int64_t MN, int N, const LinearTail tail) {
@@ -678,11 +702,11 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* parts, in
       float z = v[j];
       if (tail.bias) z += tail.bias[n + j];
       if (tail.pre) store_value(tail.pre, i + j, tail.type, z);
-      if (tail.mode == kGelu) z = gelu2(z, z).x;
+      if (tail.mode == kGelu) z = gelu_one(z);
       if (tail.mode == kSlope) {
         const float p = tail.codes ? (float)tail.codes[i + j] * tail.scales[m * checkpoint_blocks(N) + (n + j) / kCheckpointBlock]
                                    : load_value(tail.side, i + j, tail.type);
-        z *= gelu_slope2(p, p).x;
+        z *= gelu_slope_one(p);
       } else if (tail.side) {
         z += load_value(tail.side, i + j, tail.out_type);
       }
@@ -765,6 +789,7 @@ __global__ void __launch_bounds__(256) column_join_kernel(const float* parts, in
   sums[c] = t;
 }
 
+static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 static int64_t lin_up(int64_t n, int64_t m) { return (n + m - 1) / m; }
 // The tensor cores cut an accumulator off at its last place at each addition of 16 products, always towards zero: the error grows
 // with their number (24,576 products of random signs: 2.8e-5 of the result, 4,096: a sixth of it).  fp32 outputs are summed in runs of
@@ -893,8 +918,8 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   gp.pre = split ? nullptr : tail.pre;
   gp.pre_codes = pre_codes;
   gp.pre_scales = pre_scales;
-  gp.vector = row_bytes % 16 == 0 && aligned16(tail.side) && aligned16(tail.pre);
-  gp.vector_codes = N % 16 == 0 && aligned16(tail.codes) && aligned16(pre_codes);
+  gp.vector = row_bytes % 32 == 0 && aligned_to(tail.side, 32) && aligned_to(tail.pre, 32);
+  gp.vector_codes = N % 32 == 0 && aligned_to(tail.codes, 32) && aligned_to(pre_codes, 32);
   gp.ws = ws;
   gp.M = (int32_t)M;
   gp.N = (int32_t)N;
@@ -935,7 +960,6 @@ static qb_status check_linear_ws(const char* what, const void* ws, size_t ws_byt
   set_last_error("%s: workspace null, not 16-byte aligned or too small", what);
   return QB_ERR_WORKSPACE;
 }
-static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 }  // namespace qb
 
