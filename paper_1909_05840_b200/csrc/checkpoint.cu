@@ -155,20 +155,18 @@ __global__ void __launch_bounds__(kCheckpointThreads) activation_kernel(const T*
     float p[N], d[N];
     if constexpr (CODES) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) p[j] = code_value(w[u][j >> 2], j & 3) * scale[u];
+      for (int j = 0; j < N / 4; ++j) code_values(w[u][j], scale[u], p + 4 * j);
     } else {
       v[u].get(p);
     }
     if constexpr (USE == kActivation) gelu_many<N / 2>(p);
     if constexpr (USE == kSlopeOf) {
       g[u].get(d);
-      gelu_slope_many<N / 2>(p);
-#pragma unroll
-      for (int j = 0; j < N; ++j) p[j] *= d[j];
+      times_gelu_slope<N / 2>(p, d);
     }
     const CheckpointAt<N, FLAT> at(i, K, blocks);
     Vec16<T> out;
-    out.set(p);
+    out.set(USE == kSlopeOf ? d : p);
     out.template store<VECTOR>(y + at.element, at.left);
   }
 }

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "ptx_float.cuh"
 
 namespace qb {
 
@@ -33,7 +34,21 @@ struct CheckpointScale {
   }
 };
 
-// Byte `i` of a word of codes as a number.
-__device__ __forceinline__ float code_value(uint32_t w, int i) { return (float)(int)(int8_t)(w >> (8 * i)); }
+// Byte `i` of a word of codes as a number: with its sign turned it is the low byte of 2^23 + 128 + code, which costs a permutation and an
+// addition (a conversion of a whole number to fp32 takes the pipe of the exponentials).
+__device__ __forceinline__ uint32_t turned_codes(uint32_t w) { return w ^ 0x80808080u; }
+__device__ __forceinline__ float shifted_code(uint32_t turned, int i) { return __uint_as_float(__byte_perm(turned, 0x4B000000u, 0x7440 | i)); }
+constexpr float kCodeShift = 8388736.0f;
+// The values of four codes.
+__device__ __forceinline__ void code_values(uint32_t word, float scale, float* p) {
+  const uint32_t w = turned_codes(word);
+  const uint64_t shift = ptx::pack_f32x2(-kCodeShift, -kCodeShift), s = ptx::pack_f32x2(scale, scale);
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    const float2 f = ptx::unpack_f32x2(ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(shifted_code(w, i), shifted_code(w, i + 1)), shift), s));
+    p[i] = f.x;
+    p[i + 1] = f.y;
+  }
+}
 
 }  // namespace qb

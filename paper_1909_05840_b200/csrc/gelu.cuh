@@ -66,17 +66,20 @@ __device__ __forceinline__ void gelu_many(float* x) {
     x[2 * i + 1] = f.y;
   }
 }
-// gelu' of 2 P values, in place
+// gelu' of 2 P values times g, in place of g: [x >= 0] + sign(x) s as 1/2 + sign(x) (1/2 + s)
 template <int P>
-__device__ __forceinline__ void gelu_slope_many(float* x) {
+__device__ __forceinline__ void times_gelu_slope(const float* x, float* g) {
   const GeluTerms<P> t(x);
   uint64_t r[P];
   t.poly(-0.4999998211860657f, 0.3989296555519104f + 0.39894228f, r);  // u / sqrt(2 pi) - R
+  const uint64_t half = ptx::pack_f32x2(0.5f, 0.5f);
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const float2 s = ptx::unpack_f32x2(ptx::mul_f32x2(t.e[i], r[i]));
-    x[2 * i] = x[2 * i] < 0.0f ? -s.x : 1.0f + s.x;
-    x[2 * i + 1] = x[2 * i + 1] < 0.0f ? -s.y : 1.0f + s.y;
+    const float2 s = ptx::unpack_f32x2(ptx::fma_f32x2(t.e[i], r[i], half));
+    const uint64_t slope = ptx::add_f32x2(ptx::pack_f32x2(copysignf(s.x, x[2 * i]), copysignf(s.y, x[2 * i + 1])), half);
+    const float2 f = ptx::unpack_f32x2(ptx::mul_f32x2(slope, ptx::pack_f32x2(g[2 * i], g[2 * i + 1])));
+    g[2 * i] = f.x;
+    g[2 * i + 1] = f.y;
   }
 }
 

@@ -5,11 +5,11 @@
 // One product kernel for all of them, out[m][n] = sum_k A(m, k) B(n, k): persistent CTAs (tcgen05 kind::f16, fp32 accumulators), K blocks
 // of 64, two blocks a stage.  An operand lies in shared memory as its tensor has it: contraction along its rows (K-major: x and w of
 // the forward pass, grad_y of grad_x) or down its columns (MN-major: w of grad_x, both operands of grad_w), so that nothing is
-// transposed in memory.  12 warps:
+// transposed in memory.  20 warps:
 //   warp 0        TMA producer (one lane)
 //   warp 1        issues tcgen05.mma, owns the tensor memory (one lane)
 //   warps 2..3    idle
-//   warps 4..11   epilogue, two per TMEM lane quarter: tcgen05.ld -> bias, GELU or its slope, residual -> shared memory -> TMA store
+//   warps 4..19   epilogue, four per TMEM lane quarter: tcgen05.ld -> bias, GELU or its slope, residual -> shared memory -> TMA store
 // A tile is 128 rows of A per CTA x BT rows of B; TMEM lane = row, column = column of the output.  Large products run as CTA pairs
 // (cta_group::2, 256 x 256).  No load is multicast.  Two accumulators, so that a tile's epilogue overlaps the products of the next.
 // Every wait is bounded: on expiry the CTA records QB_ERR_TIMEOUT and leaves through the normal exit path.
@@ -38,7 +38,7 @@ enum LinearMode { kPlain = 0, kGelu = 1, kSlope = 2 };
 struct LinearParams {
   CUtensorMap tma, tmb;  // operands
   CUtensorMap tmb_half;  // pairs: B for a tile of half the width
-  CUtensorMap tmy;       // out (or the splits' parts, one after the other) in boxes of 32 rows x 128 bytes
+  CUtensorMap tmy;       // out (or the splits' parts, one after the other) in boxes of 32 rows x 64 bytes
   const float* bias;     // or NULL
   const void* side;      // residual, or 16-bit pre-activation (kSlope), [M][N] of out's type; or NULL
   const int8_t* codes;   // kSlope: the pre-activation in 8 bits, or NULL
@@ -50,8 +50,8 @@ struct LinearParams {
   void* ws;
   int32_t M, N;
   int32_t a_form, b_form;
-  int32_t half_type;     // 1: 16-bit tensors are fp16, 0: bfloat16
   int32_t n_tiles, tiles;
+  uint32_t n_tiles_inv, split_tiles_inv;  // quick_inverse
   int32_t whole;         // tiles below this are BT wide; pairs: the others are halves, two after the other
   int32_t split_tiles;   // tiles of one split of K (split s writes rows s * M .. of out, fp32)
   int32_t split_blocks;  // K blocks of 64 per split, even where there are several
@@ -63,7 +63,7 @@ struct LinearParams {
   uint32_t idesc;
 };
 
-constexpr int kLinEpilogueWarps = 8;
+constexpr int kLinEpilogueWarps = 16;
 constexpr int kLinFirstEpilogueWarp = 4;
 constexpr int kLinThreads = 32 * (kLinFirstEpilogueWarp + kLinEpilogueWarps);
 
@@ -73,7 +73,7 @@ struct LinCfg {
   static constexpr int kBBytes = 2 * (BT / CG) * 128;
   static constexpr int kStageBytes = kABytes + kBBytes;
   static constexpr int kStages = BT == 64 ? 4 : 3;
-  static constexpr int kOutBytes = kLinEpilogueWarps * 4096;
+  static constexpr int kOutBytes = kLinEpilogueWarps * 2048;
   static constexpr int kBarBytes = 256;
   static constexpr int kBiasBytes = 2 * 256 * 4;
   static constexpr int kSmemBytes = kStages * kStageBytes + kOutBytes + kBarBytes + kBiasBytes;
@@ -95,12 +95,20 @@ static uint32_t lin_idesc(bool half_type, bool a_mn, bool b_mn, int mma_m) {
   return (1u << 4) | (t << 7) | (t << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(mma_m >> 4) << 24);
 }
 
+// t / d for 0 <= t < 2^31 and d > 0 by a product with quick_inverse(d) = 2^32 / d rounded down (for 1: 2^32 - 1): short of the quotient by one
+// at most (t / 2^32 and a unit of the last place).
+static uint32_t quick_inverse(uint32_t d) { return d == 1 ? 0xFFFFFFFFu : (uint32_t)(((uint64_t)1 << 32) / d); }
+__device__ __forceinline__ int quick_divide(int t, int d, uint32_t inverse) {
+  const int q = (int)__umulhi((uint32_t)t, inverse);
+  return q + (t - q * d >= d ? 1 : 0);
+}
+
 // Where tile t lies: first row and column, columns, split and its range of K blocks.
 template <int BT, int CG>
 struct LinTile {
   int m0, n0, width, split, k0, k1;
   __device__ __forceinline__ LinTile(const LinearParams& gp, int t) {
-    split = t / gp.split_tiles;
+    split = quick_divide(t, gp.split_tiles, gp.split_tiles_inv);
     t -= split * gp.split_tiles;
     k0 = split * gp.split_blocks;
     k1 = min(k0 + gp.split_blocks, gp.k_blocks);
@@ -111,7 +119,7 @@ struct LinTile {
       t = gp.whole + ((t - gp.whole) >> 1);
       width = BT / 2;
     }
-    m0 = t / gp.n_tiles;
+    m0 = quick_divide(t, gp.n_tiles, gp.n_tiles_inv);
     n0 = (t - m0 * gp.n_tiles) * BT + half * (BT / 2);
     m0 *= 128 * CG;
   }
@@ -142,9 +150,19 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool half_type) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A warp's staging buffer: 32 rows of 128 bytes, 16-byte pieces swizzled so that the lanes meet different banks both with a row a
-// lane and with a row an eighth of a warp.
-__device__ __forceinline__ uint4* staged(uint8_t* buf, int row, int piece) { return reinterpret_cast<uint4*>(buf + row * 128 + ((piece ^ (row & 7)) << 4)); }
+// A warp's staging buffer: 32 rows of 64 bytes, 16-byte pieces swizzled as TMA does it (64-byte swizzle), so that the lanes meet
+// different banks with a row a lane.
+__device__ __forceinline__ uint4* staged(uint8_t* buf, int row, int piece) {
+  return reinterpret_cast<uint4*>(buf + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
+}
+
+// Two values added to z[0] and z[1].
+__device__ __forceinline__ void add2(float* z, float a, float b) {
+  const float2 f = ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(z[0], z[1]), ptx::pack_f32x2(a, b)));
+  z[0] = f.x;
+  z[1] = f.y;
+}
+
 // 32 bytes of a row: whole sectors, where 16 bytes a lane would touch each of them twice.
 __device__ __forceinline__ void load32(const void* p, uint4& a, uint4& b) {
   asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -157,18 +175,18 @@ __device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b)
                : "memory");
 }
 
-// `rows` rows of `cols` 16-bit values from the staging buffer to rows of any alignment, `pitch` elements apart: a row at a time, the
-// lanes on consecutive words of it.
+// `rows` rows of `cols` 16-bit values from the staging buffer to rows of any alignment, `pitch` elements apart: two rows at a time, the
+// lanes on consecutive words of them.
 __device__ __forceinline__ void send_rows16(const uint8_t* buf, uint16_t* to, int64_t pitch, int rows, int cols, int lane) {
   const int first_odd = (int)(reinterpret_cast<uintptr_t>(to) >> 1) & 1, step = (int)(pitch & 1);
   const auto word = [&](int r, int col) {  // columns col and col + 1 of a row, col even
-    return *reinterpret_cast<const uint32_t*>(buf + r * 128 + (((col >> 3) ^ (r & 7)) << 4) + (col & 6) * 2);
+    return *reinterpret_cast<const uint32_t*>(buf + r * 64 + (((col >> 3) ^ ((r >> 1) & 3)) << 4) + (col & 6) * 2);
   };
-  for (int r = 0; r < rows; ++r) {
+  for (int r = lane >> 4; r < rows; r += 2) {
     // columns odd and odd + 1, odd + 2 and odd + 3 .. are the words of the row
-    const int odd = first_odd ^ (step & r), c = 2 * lane + odd;
-    uint32_t w = word(r, 2 * lane);
-    if (odd) w = __byte_perm(w, word(r, min(2 * lane + 2, 62)), 0x5432);
+    const int odd = first_odd ^ (step & r), c = 2 * (lane & 15) + odd;
+    uint32_t w = word(r, 2 * (lane & 15));
+    if (odd) w = __byte_perm(w, word(r, min(2 * (lane & 15) + 2, 30)), 0x5432);
     if (c + 1 < cols) *reinterpret_cast<uint32_t*>(to + r * pitch + c) = w;
   }
   if (lane < rows) {  // the single columns at the ends, of all rows at once
@@ -179,8 +197,9 @@ __device__ __forceinline__ void send_rows16(const uint8_t* buf, uint16_t* to, in
   }
 }
 
-// OUT32: out is fp32, else of the operands' type.  A chunk is 128 bytes of out: 32 or 64 columns.
-template <int BT, int CG, bool OUT32, int MODE>
+// OUT32: out is fp32, else of the operands' type.  A chunk is 64 bytes of out: 16 or 32 columns.
+// HALF: the 16-bit tensors are fp16, else bfloat16.
+template <int BT, int CG, bool OUT32, int MODE, bool HALF>
 __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_constant__ LinearParams gp) {
   using Cfg = LinCfg<BT, CG>;
   constexpr int kStages = Cfg::kStages;
@@ -351,13 +370,12 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     }
   } else if (warp >= kLinFirstEpilogueWarp) {
     // ---------------- epilogue ----------------------------------------------------------------------
-    constexpr int kCols = OUT32 ? 32 : 64;  // columns of a chunk
-    constexpr int kParts = kCols / 32;
+    constexpr int kCols = OUT32 ? 16 : 32;  // columns of a chunk
     constexpr int kESize = OUT32 ? 4 : 2;
-    const int ew = warp - kLinFirstEpilogueWarp, quarter = warp & 3, half = ew >> 2;
+    const int ew = warp - kLinFirstEpilogueWarp, quarter = warp & 3, part = ew >> 2;
     const int e = threadIdx.x - 32 * kLinFirstEpilogueWarp;
-    const bool half_type = gp.half_type != 0;
-    uint8_t* const buf = out_ptr + ew * 4096;
+    constexpr bool half_type = HALF;
+    uint8_t* const buf = out_ptr + ew * 2048;
     const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
     auto arrive = [&](uint32_t bar) {  // this warp has read all it needs from the accumulator
       ptx::tcgen05_fence_before_sync();
@@ -377,63 +395,79 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       int m0 = tile.m0 + (int)rank * 128 + quarter * 32, n0 = tile.n0;
       int chunks = m0 < gp.M ? max(0, min(tile.width / kCols, (gp.N - n0 + kCols - 1) / kCols)) : 0;
       asm volatile("" : "+r"(m0), "+r"(n0), "+r"(chunks));  // formed before the wait, not behind it
-      bias_tile[a * 256 + e] = bias && e < BT && n0 + e < gp.N ? bias[n0 + e] : 0.0f;
+      if (e < BT) bias_tile[a * 256 + e] = bias && n0 + e < gp.N ? bias[n0 + e] : 0.0f;
       const int rows = min(32, gp.M - m0);
       const bool mine = lane < rows;
       // The chunk's part of the tensor beside the product (residual, pre-activation, codes of it): the lane's row, fetched while the
       // products run.
-      uint4 s[8];
+      uint4 s[4];
       auto fetch = [&](int c0) {
         const int64_t corner = (int64_t)(m0 + lane) * gp.N + n0 + c0;
         if (MODE == kSlope && gp.codes) {
           if (!gp.vector_codes) return;
-#pragma unroll
-          for (int k = 0; k < 4; k += 2) {
-            s[k] = s[k + 1] = make_uint4(0u, 0u, 0u, 0u);
-            if (mine && n0 + c0 + 16 * k < gp.N) load32(gp.codes + corner + 16 * k, s[k], s[k + 1]);
-          }
+          s[0] = s[1] = make_uint4(0u, 0u, 0u, 0u);
+          if (mine && n0 + c0 < gp.N) load32(gp.codes + corner, s[0], s[1]);
         } else if (side && gp.vector) {
           const uint8_t* const from = static_cast<const uint8_t*>(side) + corner * kESize;
 #pragma unroll
-          for (int k = 0; k < 8; k += 2) {
+          for (int k = 0; k < 4; k += 2) {
             s[k] = s[k + 1] = make_uint4(0u, 0u, 0u, 0u);
             if (mine && n0 + c0 + k * (16 / kESize) < gp.N) load32(from + 16 * k, s[k], s[k + 1]);
           }
         }
       };
-      if (half < chunks) fetch(half * kCols);
+      if (part < chunks) fetch(part * kCols);
       const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
-      if (lin_epilogue_sync_or(!ok)) {  // publishes the bias, and all eight warps give up together
+      if (lin_epilogue_sync_or(!ok)) {  // publishes the bias, and all warps give up together
         timed_out = true;
         where = (3 << 16) | a;
         break;
       }
       ptx::tcgen05_fence_after_sync();
       const uint32_t acc = lanes + (uint32_t)(a * BT);
-      if (half >= chunks) arrive(acc_empty(a));
+      if (part >= chunks) arrive(acc_empty(a));
 #pragma unroll 1
-      for (int i = half; i < chunks; i += 2) {
+      for (int i = part; i < chunks; i += 4) {
         const int c0 = i * kCols, cols = min(kCols, gp.N - n0 - c0);
         const int64_t corner = (int64_t)m0 * gp.N + n0 + c0;  // of the chunk, in elements
         const int64_t block = (int64_t)(m0 + lane) * checkpoint_blocks(gp.N) + (n0 + c0) / kCheckpointBlock;  // the row's, in scales
-        uint32_t w[kParts][32];
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) ptx::tmem_ld_32x32b_x32(acc + (uint32_t)(c0 + 32 * p), w[p]);
-        float scale = 1.0f;
-        if (MODE == kSlope && gp.codes && mine) scale = gp.scales[block];
-        ptx::tmem_ld_wait();
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) ptx::tmem_ld_regs_ready(w[p]);
-        if (i + 2 >= chunks) arrive(acc_empty(a));
+        const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + a * 256 + c0);
         float v[kCols];
+        // z = product + bias of this warp's chunk or its neighbour's
+        auto read = [&](int column, const float4* b, float* z) {
+          uint32_t w[kCols];
+          if constexpr (OUT32) ptx::tmem_ld_32x32b_x16(acc + (uint32_t)column, w);
+          else ptx::tmem_ld_32x32b_x32(acc + (uint32_t)column, w);
+          ptx::tmem_ld_wait();
+          ptx::tmem_ld_regs_ready(w);
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) v[j] = __uint_as_float(w[j >> 5][j & 31]);
+          for (int j = 0; j < kCols; ++j) z[j] = __uint_as_float(w[j]);
+          if (MODE != kSlope && bias) {
+#pragma unroll
+            for (int j = 0; j < kCols / 4; ++j) {
+              const float4 q = b[j];
+              add2(z + 4 * j, q.x, q.y);
+              add2(z + 4 * j + 2, q.z, q.w);
+            }
+          }
+        };
+        float scale = 1.0f, top = 0.0f;
+        if (MODE == kSlope && gp.codes && mine) scale = gp.scales[block];
+        if constexpr (!OUT32 && MODE != kSlope) {
+          if (gp.pre_codes) {  // a block is this chunk and its neighbour
+            read(c0 ^ 32, reinterpret_cast<const float4*>(bias_tile + a * 256 + (c0 ^ 32)), v);
+#pragma unroll
+            for (int j = 0; j < kCols; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
+          }
+        }
+        read(c0, b4, v);
+        if (i + 4 >= chunks) arrive(acc_empty(a));
         bool waited = false;  // for the chunk before to have left the buffer, and for what is added to to have been written
         auto buffer_free = [&]() {
           if (waited) return;
           waited = true;
           if (lane == 0) {
-            if (add && i == half) ptx::tma_store_wait0();
+            if (add && i == part) ptx::tma_store_wait0();
             else ptx::tma_store_wait_read0();
           }
           __syncwarp();
@@ -442,52 +476,37 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         if (MODE == kSlope && gp.codes && !gp.vector_codes) {
           buffer_free();
           for (int r = 0; r < rows; ++r)
+            reinterpret_cast<int8_t*>(staged(buf, r, lane >> 4))[lane & 15] = lane < cols ? gp.codes[corner + (int64_t)r * gp.N + lane] : (int8_t)0;
+          __syncwarp();
 #pragma unroll
-            for (int c = lane; c < 64; c += 32)
-              reinterpret_cast<int8_t*>(staged(buf, r, c >> 4))[c & 15] = c < cols ? gp.codes[corner + (int64_t)r * gp.N + c] : (int8_t)0;
+          for (int k = 0; k < 2; ++k) s[k] = *staged(buf, lane, k);
+          __syncwarp();
+        } else if (side && !gp.vector) {
+          buffer_free();
+          if constexpr (OUT32) {
+            for (int r = lane >> 4; r < rows; r += 2) {
+              const int c = lane & 15;
+              reinterpret_cast<float*>(staged(buf, r, c >> 2))[c & 3] = c < cols ? static_cast<const float*>(side)[corner + (int64_t)r * gp.N + c] : 0.0f;
+            }
+          } else {
+            for (int r = 0; r < rows; ++r)
+              reinterpret_cast<uint16_t*>(staged(buf, r, lane >> 3))[lane & 7] =
+                  lane < cols ? static_cast<const uint16_t*>(side)[corner + (int64_t)r * gp.N + lane] : (uint16_t)0;
+          }
           __syncwarp();
 #pragma unroll
           for (int k = 0; k < 4; ++k) s[k] = *staged(buf, lane, k);
           __syncwarp();
-        } else if (side && !gp.vector) {
-          buffer_free();
-          for (int r = 0; r < rows; ++r) {
-            if constexpr (OUT32) {
-              reinterpret_cast<float*>(staged(buf, r, lane >> 2))[lane & 3] = lane < cols ? static_cast<const float*>(side)[corner + (int64_t)r * gp.N + lane] : 0.0f;
-            } else {
-#pragma unroll
-              for (int c = lane; c < 64; c += 32)
-                reinterpret_cast<uint16_t*>(staged(buf, r, c >> 3))[c & 7] =
-                    c < cols ? static_cast<const uint16_t*>(side)[corner + (int64_t)r * gp.N + c] : (uint16_t)0;
-            }
-          }
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 8; ++k) s[k] = *staged(buf, lane, k);
-          __syncwarp();
-        }
-        // z = product + bias
-        if (MODE != kSlope && bias) {
-          const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + a * 256 + c0);
-#pragma unroll
-          for (int j = 0; j < kCols / 4; ++j) {
-            const float4 b = b4[j];
-            v[4 * j] += b.x;
-            v[4 * j + 1] += b.y;
-            v[4 * j + 2] += b.z;
-            v[4 * j + 3] += b.w;
-          }
         }
         if constexpr (!OUT32 && MODE != kSlope) {
-          if (gp.pre_codes) {  // z in 8 bits: a chunk is a block
-            float top = 0.0f;
+          if (gp.pre_codes) {  // z in 8 bits
 #pragma unroll
-            for (int j = 0; j < 64; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
+            for (int j = 0; j < kCols; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
             const CheckpointScale cs(top);
-            if (mine) gp.pre_scales[block] = cs.scale;
-            uint4 c[4];
+            if (mine && (c0 & 32) == 0) gp.pre_scales[block] = cs.scale;
+            uint4 c[2];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 2; ++k) {
               c[k].x = cs.codes4(v[16 * k], v[16 * k + 1], v[16 * k + 2], v[16 * k + 3]);
               c[k].y = cs.codes4(v[16 * k + 4], v[16 * k + 5], v[16 * k + 6], v[16 * k + 7]);
               c[k].z = cs.codes4(v[16 * k + 8], v[16 * k + 9], v[16 * k + 10], v[16 * k + 11]);
@@ -495,35 +514,31 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             }
             int8_t* const to = gp.pre_codes + corner;
             if (gp.vector_codes) {
-#pragma unroll
-              for (int k = 0; k < 4; k += 2)
-                if (mine && 16 * k < cols) store32(to + (int64_t)lane * gp.N + 16 * k, c[k], c[k + 1]);
+              if (mine) store32(to + (int64_t)lane * gp.N, c[0], c[1]);
             } else {
               buffer_free();
 #pragma unroll
-              for (int k = 0; k < 4; ++k) *staged(buf, lane, k) = c[k];
+              for (int k = 0; k < 2; ++k) *staged(buf, lane, k) = c[k];
               __syncwarp();
-              for (int r = 0; r < rows; ++r)
-#pragma unroll
-                for (int col = lane; col < 64; col += 32)
-                  if (col < cols) to[(int64_t)r * gp.N + col] = reinterpret_cast<const int8_t*>(staged(buf, r, col >> 4))[col & 15];
+              if (lane < cols)
+                for (int r = 0; r < rows; ++r) to[(int64_t)r * gp.N + lane] = reinterpret_cast<const int8_t*>(staged(buf, r, lane >> 4))[lane & 15];
               __syncwarp();
             }
           } else if (gp.pre) {  // z in 16 bits
             uint16_t* const to = static_cast<uint16_t*>(gp.pre) + corner;
-            uint4 c[8];
+            uint4 c[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < 4; ++k)
               c[k] = make_uint4(pack16(v[8 * k], v[8 * k + 1], half_type), pack16(v[8 * k + 2], v[8 * k + 3], half_type), pack16(v[8 * k + 4], v[8 * k + 5], half_type),
                                 pack16(v[8 * k + 6], v[8 * k + 7], half_type));
             if (gp.vector) {
 #pragma unroll
-              for (int k = 0; k < 8; k += 2)
+              for (int k = 0; k < 4; k += 2)
                 if (mine && 8 * k < cols) store32(to + (int64_t)lane * gp.N + 8 * k, c[k], c[k + 1]);
             } else {
               buffer_free();
 #pragma unroll
-              for (int k = 0; k < 8; ++k) *staged(buf, lane, k) = c[k];
+              for (int k = 0; k < 4; ++k) *staged(buf, lane, k) = c[k];
               __syncwarp();
               send_rows16(buf, to, gp.N, rows, cols, lane);
               __syncwarp();
@@ -532,33 +547,31 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         }
         if constexpr (MODE == kGelu) {
 #pragma unroll
-          for (int j = 0; j < kCols; j += 16) gelu_many<8>(v + j);
+          for (int j = 0; j < kCols; j += 8) gelu_many<4>(v + j);
         }
         if constexpr (MODE == kSlope) {
 #pragma unroll
-          for (int j = 0; j < kCols; j += 16) {
-            float p[16];
+          for (int j = 0; j < kCols; j += 8) {
+            float p[8];
+            if (gp.codes) {
+              const uint4& q = s[j >> 4];
+              code_values((j & 8) ? q.z : q.x, scale, p);
+              code_values((j & 8) ? q.w : q.y, scale, p + 4);
+            } else {
+              const uint4& q = s[j >> 3];
+              const uint32_t in[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int h = 0; h < 8; ++h) {
-              if (gp.codes) {
-                const uint4& q = s[j >> 4];
-                const uint32_t word = h < 2 ? q.x : (h < 4 ? q.y : (h < 6 ? q.z : q.w));
-                p[2 * h] = code_value(word, (h & 1) * 2) * scale;
-                p[2 * h + 1] = code_value(word, (h & 1) * 2 + 1) * scale;
-              } else {
-                const uint4& q = s[(j >> 3) + (h >> 2)];
-                const float2 f = unpack16((h & 3) == 0 ? q.x : ((h & 3) == 1 ? q.y : ((h & 3) == 2 ? q.z : q.w)), half_type);
+              for (int h = 0; h < 4; ++h) {
+                const float2 f = unpack16(in[h], half_type);
                 p[2 * h] = f.x;
                 p[2 * h + 1] = f.y;
               }
             }
-            gelu_slope_many<8>(p);
-#pragma unroll
-            for (int h = 0; h < 16; ++h) v[j + h] *= p[h];
+            times_gelu_slope<4>(p, v + j);
           }
         } else if (side) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
+          for (int k = 0; k < 4; ++k) {
             const uint32_t in[4] = {s[k].x, s[k].y, s[k].z, s[k].w};
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
@@ -566,23 +579,21 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
                 v[4 * k + h] += __uint_as_float(in[h]);
               } else {
                 const float2 r = unpack16(in[h], half_type);
-                v[8 * k + 2 * h] += r.x;
-                v[8 * k + 2 * h + 1] += r.y;
+                add2(v + 8 * k + 2 * h, r.x, r.y);
               }
             }
           }
         }
-        if (i + 2 < chunks) fetch(c0 + 2 * kCols);
+        if (i + 4 < chunks) fetch(c0 + 4 * kCols);
         buffer_free();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {  // 16 bytes of the row at a time
+        for (int k = 0; k < 4; ++k) {  // 16 bytes of the row at a time
           if constexpr (OUT32)
             *staged(buf, lane, k) = make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3]));
           else
             *staged(buf, lane, k) = make_uint4(pack16(v[8 * k], v[8 * k + 1], half_type), pack16(v[8 * k + 2], v[8 * k + 3], half_type),
                                                pack16(v[8 * k + 4], v[8 * k + 5], half_type), pack16(v[8 * k + 6], v[8 * k + 7], half_type));
         }
-        __syncwarp();
         const int64_t first_row = (int64_t)tile.split * gp.M;
         if (gp.tma_store) {
           ptx::fence_proxy_async_smem();  // every lane: its own stores
@@ -592,16 +603,19 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             else ptx::tma_store_3d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0, tile.split);
             ptx::tma_store_commit();
           }
-        } else if constexpr (OUT32) {  // the lanes on consecutive values of a row
-          if (lane < cols) {
-            float* const to = static_cast<float*>(gp.out) + first_row * gp.N + corner + lane;
-            for (int r = 0; r < rows; ++r) {
-              const float f = reinterpret_cast<const float*>(staged(buf, r, lane >> 2))[lane & 3];
+        } else if constexpr (OUT32) {  // two rows at a time, the lanes on consecutive values of them
+          __syncwarp();
+          const int c = lane & 15;
+          if (c < cols) {
+            float* const to = static_cast<float*>(gp.out) + first_row * gp.N + corner + c;
+            for (int r = lane >> 4; r < rows; r += 2) {
+              const float f = reinterpret_cast<const float*>(staged(buf, r, c >> 2))[c & 3];
               to[(int64_t)r * gp.N] = add ? to[(int64_t)r * gp.N] + f : f;
             }
           }
           __syncwarp();
         } else {
+          __syncwarp();
           send_rows16(buf, static_cast<uint16_t*>(gp.out) + first_row * gp.N + corner, gp.N, rows, cols, lane);
           __syncwarp();
         }
@@ -628,10 +642,10 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
   }
 }
 
-template <int BT, int CG, bool OUT32, int MODE>
+template <int BT, int CG, bool OUT32, int MODE, bool HALF>
 static qb_status launch_linear_form(const LinearParams& gp, int sms, cudaStream_t stream) {
   using Cfg = LinCfg<BT, CG>;
-  auto kernel = linear_kernel<BT, CG, OUT32, MODE>;
+  auto kernel = linear_kernel<BT, CG, OUT32, MODE, HALF>;
   static std::atomic<bool> attr_set[64] = {};
   int dev = 0;
   QB_CUDA_TRY(cudaGetDevice(&dev));
@@ -643,11 +657,16 @@ static qb_status launch_linear_form(const LinearParams& gp, int sms, cudaStream_
   QB_CUDA_TRY(launch_kernel(kernel, (unsigned)grid, kLinThreads, Cfg::kSmemBytes, stream, CG, false, gp));
   return QB_OK;
 }
+template <int BT, int CG, bool HALF>
+static qb_status launch_linear_type(const LinearParams& gp, bool out32, int mode, int sms, cudaStream_t stream) {
+  // (with fp32 out the type of the 16-bit tensors is in the instruction descriptor alone)
+  if (out32) return mode == kGelu ? launch_linear_form<BT, CG, true, kGelu, false>(gp, sms, stream) : launch_linear_form<BT, CG, true, kPlain, false>(gp, sms, stream);
+  if (mode == kSlope) return launch_linear_form<BT, CG, false, kSlope, HALF>(gp, sms, stream);
+  return mode == kGelu ? launch_linear_form<BT, CG, false, kGelu, HALF>(gp, sms, stream) : launch_linear_form<BT, CG, false, kPlain, HALF>(gp, sms, stream);
+}
 template <int BT, int CG>
-static qb_status launch_linear(const LinearParams& gp, bool out32, int mode, int sms, cudaStream_t stream) {
-  if (out32) return mode == kGelu ? launch_linear_form<BT, CG, true, kGelu>(gp, sms, stream) : launch_linear_form<BT, CG, true, kPlain>(gp, sms, stream);
-  if (mode == kSlope) return launch_linear_form<BT, CG, false, kSlope>(gp, sms, stream);
-  return mode == kGelu ? launch_linear_form<BT, CG, false, kGelu>(gp, sms, stream) : launch_linear_form<BT, CG, false, kPlain>(gp, sms, stream);
+static qb_status launch_linear(const LinearParams& gp, bool out32, int mode, bool half_type, int sms, cudaStream_t stream) {
+  return half_type ? launch_linear_type<BT, CG, true>(gp, out32, mode, sms, stream) : launch_linear_type<BT, CG, false>(gp, out32, mode, sms, stream);
 }
 
 // What stands behind a product, as the join of a split one needs it.
@@ -673,11 +692,6 @@ __device__ __forceinline__ void store_value(void* p, int64_t i, int type, float 
 __device__ __forceinline__ float gelu_one(float z) {
   float f[2] = {z, z};
   gelu_many<1>(f);
-  return f[0];
-}
-__device__ __forceinline__ float gelu_slope_one(float z) {
-  float f[2] = {z, z};
-  gelu_slope_many<1>(f);
   return f[0];
 }
 // out = what stands behind the splits' sum, taken in their order.
@@ -706,7 +720,10 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* parts, in
       if (tail.mode == kSlope) {
         const float p = tail.codes ? (float)tail.codes[i + j] * tail.scales[m * checkpoint_blocks(N) + (n + j) / kCheckpointBlock]
                                    : load_value(tail.side, i + j, tail.type);
-        z *= gelu_slope_one(p);
+        const float x[2] = {p, p};
+        float g[2] = {z, z};
+        times_gelu_slope<1>(x, g);
+        z = g[0];
       } else if (tail.side) {
         z += load_value(tail.side, i + j, tail.out_type);
       }
@@ -908,7 +925,7 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   gp.tma_store = row_bytes % 16 == 0 && (split || aligned16(tail.out));
   gp.tmy = gp.tma;
   if (gp.tma_store && (st = make_parts_map(&gp.tmy, out32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : (half_type ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16),
-                                           split ? parts : tail.out, choice.splits, M, N, row_bytes, 32, out32 ? 32 : 64)) != QB_OK)
+                                           split ? parts : tail.out, choice.splits, M, N, row_bytes, 32, out32 ? 16 : 32, CU_TENSOR_MAP_SWIZZLE_64B)) != QB_OK)
     return st;
   gp.bias = split ? nullptr : tail.bias;
   gp.side = split || tail.codes ? nullptr : tail.side;
@@ -923,19 +940,20 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   gp.ws = ws;
   gp.M = (int32_t)M;
   gp.N = (int32_t)N;
-  gp.half_type = half_type;
   gp.n_tiles = (int32_t)lin_up(N, bt);
   gp.tiles = choice.tiles;
   gp.whole = choice.whole;
   gp.split_tiles = choice.tiles / choice.splits;
+  gp.n_tiles_inv = quick_inverse((uint32_t)gp.n_tiles);
+  gp.split_tiles_inv = quick_inverse((uint32_t)gp.split_tiles);
   gp.split_blocks = choice.split_blocks;
   gp.k_blocks = (int32_t)blocks;
   gp.run_blocks = split || (out32 && tail.mode == kPlain) ? kLinRunBlocks : (int32_t)blocks;
   gp.idesc = lin_idesc(half_type, a.mn, b.mn, 128 * cg);
   const int mode = split ? kPlain : tail.mode;
-  if (cg == 2) st = launch_linear<256, 2>(gp, out32, mode, sms, stream);
-  else if (bt == 128) st = launch_linear<128, 1>(gp, out32, mode, sms, stream);
-  else st = launch_linear<64, 1>(gp, out32, mode, sms, stream);
+  if (cg == 2) st = launch_linear<256, 2>(gp, out32, mode, half_type, sms, stream);
+  else if (bt == 128) st = launch_linear<128, 1>(gp, out32, mode, half_type, sms, stream);
+  else st = launch_linear<64, 1>(gp, out32, mode, half_type, sms, stream);
   if (st != QB_OK || !split) return st;
   const bool vector = N % 4 == 0;
   QB_CUDA_TRY(launch_kernel(vector ? linear_join_kernel<4> : linear_join_kernel<1>, (unsigned)std::min<int64_t>(lin_up(M * N, vector ? 1024 : 256), (int64_t)sms * 8), 256, 0,

@@ -68,9 +68,9 @@ inline qb_status make_group_map(CUtensorMap* tm, CUtensorMapDataType type, int e
   return QB_OK;
 }
 
-// `parts` matrices one after the other, row-major without gaps: coordinates (column, row, part), boxes of one part, 128-byte swizzle.
+// `parts` matrices one after the other, row-major without gaps: coordinates (column, row, part), boxes of one part.
 inline qb_status make_parts_map(CUtensorMap* tm, CUtensorMapDataType type, const void* base, int64_t parts, int64_t rows, int64_t cols,
-                                int64_t row_bytes, int box_rows, int box_cols) {
+                                int64_t row_bytes, int box_rows, int box_cols, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   TensormapEncodeFn encode = nullptr;
   qb_status st = tensormap_encoder(&encode);
   if (st != QB_OK) return st;
@@ -79,7 +79,7 @@ inline qb_status make_parts_map(CUtensorMap* tm, CUtensorMapDataType type, const
   const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
   const cuuint32_t elem[3] = {1, 1, 1};
   const CUresult r = encode(tm, type, 3, const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                            swizzle, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     set_last_error("cuTensorMapEncodeTiled failed with CUresult %d (%lld x %lld x %lld)", (int)r, (long long)parts, (long long)rows, (long long)cols);
     return QB_ERR_CUDA;
