@@ -7,9 +7,11 @@
 // workspace at its end; a second kernel sums the blocks', always in the same order.
 // Bound by memory: one read and one write of the tensor forward, two reads and one write backward.
 #include "common.cuh"
+#include "ptx_float.cuh"
 #include "vec16.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 namespace qb {
 
@@ -46,11 +48,14 @@ struct NormRow {
       }
     }
   }
-  __device__ __forceinline__ void get(int i, float (&f)[V]) const {
+  __device__ __forceinline__ void get(int i, float* f) const {
     if constexpr (VECTOR) {
       Vec16<T> v;
       v.raw = make_uint4(raw[4 * i], raw[4 * i + 1], raw[4 * i + 2], raw[4 * i + 3]);
-      v.get(f);
+      float e[V];
+      v.get(e);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = e[j];
     } else if constexpr (sizeof(T) == 4) {
       f[0] = __uint_as_float(raw[i]);
     } else {
@@ -70,7 +75,7 @@ struct NormRow {
 };
 // V weights from column c on (fp32, 16-byte aligned where V is above 1 and VECTOR), or `instead` of them.
 template <int V>
-__device__ __forceinline__ void norm_weights(const float* w, int c, float instead, bool vector, float (&f)[V]) {
+__device__ __forceinline__ void norm_weights(const float* w, int c, float instead, bool vector, float* f) {
 #pragma unroll
   for (int j = 0; j < V; ++j) f[j] = instead;
   if (!w) return;
@@ -88,6 +93,50 @@ __device__ __forceinline__ void norm_weights(const float* w, int c, float instea
     for (int j = 0; j < V; ++j) f[j] = w[c + j];
   }
 }
+
+// Arithmetic on one value, or on two at a time where a lane's values come in pairs.
+template <int V>
+struct NormMath {
+  static constexpr int W = V > 1 ? 2 : 1;
+  typedef std::conditional_t<V == 1, float, uint64_t> F;
+  static __device__ __forceinline__ F all(float a) {
+    if constexpr (V == 1) return a;
+    else return ptx::pack_f32x2(a, a);
+  }
+  static __device__ __forceinline__ F from(const float* p) {
+    if constexpr (V == 1) return p[0];
+    else return ptx::pack_f32x2(p[0], p[1]);
+  }
+  static __device__ __forceinline__ void to(float* p, F a) {
+    if constexpr (V == 1) {
+      p[0] = a;
+    } else {
+      const float2 f = ptx::unpack_f32x2(a);
+      p[0] = f.x;
+      p[1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ F add(F a, F b) {
+    if constexpr (V == 1) return a + b;
+    else return ptx::add_f32x2(a, b);
+  }
+  static __device__ __forceinline__ F mul(F a, F b) {
+    if constexpr (V == 1) return a * b;
+    else return ptx::mul_f32x2(a, b);
+  }
+  static __device__ __forceinline__ F fma(F a, F b, F c) {
+    if constexpr (V == 1) return __fmaf_rn(a, b, c);
+    else return ptx::fma_f32x2(a, b, c);
+  }
+  static __device__ __forceinline__ float sum(F a) {
+    if constexpr (V == 1) {
+      return a;
+    } else {
+      const float2 f = ptx::unpack_f32x2(a);
+      return f.x + f.y;
+    }
+  }
+};
 
 __device__ __forceinline__ float warp_sum(float s) {
 #pragma unroll
@@ -119,55 +168,81 @@ struct NormArgs {
   int32_t vector_weights;
 };
 
+// A block goes over its share of the rows with the weights in registers.  In 16 bits the row after the present one is on its way
+// meanwhile; in fp32 there is no room for it, and the other warps' rows are.
 template <class T, int WPR, bool VECTOR>
-__global__ void __launch_bounds__(kNormThreads) layer_norm_kernel(const T* x, T* y, const NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x, T* y, const NormArgs a) {
   using Row = NormRow<T, WPR, VECTOR>;
   constexpr int V = Row::V;
-  __shared__ float slots[2][8];
+  constexpr bool kAhead = Row::kRegs <= 16;
+  typedef NormMath<V> Math;
+  typedef typename Math::F F;
+  constexpr int W = Math::W;
+  __shared__ float slots[2][2][8];
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.D;
-  const int64_t m = (int64_t)blockIdx.x * (8 / WPR) + warp / WPR;
-  const bool here = m < a.M;
   const int first = ((warp % WPR) * 32 + lane) * V;
-  const int end = here ? D : 0;
-  Row r;
-  r.load(x + (here ? m : 0) * D, first, end);
-  float s = 0.0f;
-#pragma unroll
-  for (int i = 0; i < Row::kVectors; ++i) {
-    float f[V];
-    r.get(i, f);
-#pragma unroll
-    for (int j = 0; j < V; ++j) s += f[j];
-  }
-  const float mean = row_sum<WPR>(s, slots, 0, warp, lane) * a.inv_d;
-  s = 0.0f;
-#pragma unroll
-  for (int i = 0; i < Row::kVectors; ++i) {
-    if (first + i * Row::kStride < end) {
-      float f[V];
-      r.get(i, f);
-#pragma unroll
-      for (int j = 0; j < V; ++j) s = __fmaf_rn(f[j] - mean, f[j] - mean, s);
-    }
-  }
-  const float rstd = 1.0f / sqrtf(row_sum<WPR>(s, slots, 1, warp, lane) * a.inv_d + a.eps);
+  const int64_t step = (int64_t)gridDim.x * (8 / WPR);
+  int64_t m = (int64_t)blockIdx.x * (8 / WPR) + warp / WPR;
+  Row next;
+  next.load(x + (m < a.M ? m : 0) * D, first, m < a.M ? D : 0);
+  float gamma[kNormElements], beta[kNormElements];
 #pragma unroll
   for (int i = 0; i < Row::kVectors; ++i) {
     const int c = first + i * Row::kStride;
-    if (c < end) {
-      float f[V], g[V], b[V];
-      r.get(i, f);
-      norm_weights<V>(a.gamma, c, 1.0f, a.vector_weights, g);
-      norm_weights<V>(a.beta, c, 0.0f, a.vector_weights, b);
-#pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = __fmaf_rn((f[j] - mean) * rstd, g[j], b[j]);
-      Row::put(y + m * D, c, f);
+    if (c < D) {
+      norm_weights<V>(a.gamma, c, 1.0f, a.vector_weights, gamma + i * V);
+      norm_weights<V>(a.beta, c, 0.0f, a.vector_weights, beta + i * V);
     }
   }
-  if (a.mean && here && warp % WPR == 0 && lane == 0) {
-    a.mean[m] = mean;
-    a.rstd[m] = rstd;
+  int turn = 0;
+  for (int64_t m0 = (int64_t)blockIdx.x * (8 / WPR); m0 < a.M; m0 += step, m += step, turn ^= 1) {
+    const int end = m < a.M ? D : 0;
+    const bool more = m + step < a.M;
+    const Row r = next;
+    if constexpr (kAhead) next.load(x + (more ? m + step : 0) * D, first, more ? D : 0);
+    F s = Math::all(0.0f);
+#pragma unroll
+    for (int i = 0; i < Row::kVectors; ++i) {
+      float f[V];
+      r.get(i, f);
+#pragma unroll
+      for (int j = 0; j < V; j += W) s = Math::add(s, Math::from(f + j));
+    }
+    const float mean = row_sum<WPR>(Math::sum(s), slots[turn], 0, warp, lane) * a.inv_d;
+    const F minus_mean = Math::all(-mean);
+    s = Math::all(0.0f);
+#pragma unroll
+    for (int i = 0; i < Row::kVectors; ++i) {
+      if (first + i * Row::kStride < end) {
+        float f[V];
+        r.get(i, f);
+#pragma unroll
+        for (int j = 0; j < V; j += W) {
+          const F d = Math::add(Math::from(f + j), minus_mean);
+          s = Math::fma(d, d, s);
+        }
+      }
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<WPR>(Math::sum(s), slots[turn], 1, warp, lane) * a.inv_d + a.eps);
+    const F all_rstd = Math::all(rstd);
+#pragma unroll
+    for (int i = 0; i < Row::kVectors; ++i) {
+      const int c = first + i * Row::kStride;
+      if (c < end) {
+        float f[V];
+        r.get(i, f);
+#pragma unroll
+        for (int j = 0; j < V; j += W)
+          Math::to(f + j, Math::fma(Math::mul(Math::add(Math::from(f + j), minus_mean), all_rstd), Math::from(gamma + i * V + j), Math::from(beta + i * V + j)));
+        Row::put(y + m * D, c, f);
+      }
+    }
+    if constexpr (!kAhead) next.load(x + (more ? m + step : 0) * D, first, more ? D : 0);
+    if (a.mean && end && warp % WPR == 0 && lane == 0) {
+      a.mean[m] = mean;
+      a.rstd[m] = rstd;
+    }
   }
 }
 
@@ -218,47 +293,59 @@ struct NormBackArgs {
   int32_t vector_weights;
 };
 
+// As the forward kernel.  A lane's sums of its columns lie in the parts in the order of registers and lanes (norm_column).
 template <class T, int WPR, bool VECTOR>
-__global__ void __launch_bounds__(kNormThreads, sizeof(T) == 2 ? 2 : 1) layer_norm_backward_kernel(const T* grad_y, const T* x, T* grad_x, const NormBackArgs a) {
+__global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(const T* grad_y, const T* x, T* grad_x, const NormBackArgs a) {
   using Row = NormRow<T, WPR, VECTOR>;
-  constexpr int V = Row::V;
-  constexpr int kRows = 8 / WPR;
-  extern __shared__ float columns[];  // [2][D]
+  constexpr int V = Row::V, kRows = 8 / WPR, kLanes = WPR * 32;
+  typedef NormMath<V> Math;
+  typedef typename Math::F F;
+  constexpr int W = Math::W;
+  extern __shared__ float columns[];  // [rows of the block][2][registers][lanes of a row]
   __shared__ float slots[2][2][8];
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.D;
   const int first = ((warp % WPR) * 32 + lane) * V;
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t m = (int64_t)blockIdx.x * kRows + warp / WPR;
+  Row gy, xr;
+  gy.load(grad_y + (m < a.M ? m : 0) * D, first, m < a.M ? D : 0);
+  xr.load(x + (m < a.M ? m : 0) * D, first, m < a.M ? D : 0);
+  float mean = a.mean[m < a.M ? m : 0], rstd = a.rstd[m < a.M ? m : 0];
+  float gamma[kNormElements];
+#pragma unroll
+  for (int i = 0; i < Row::kVectors; ++i)
+    if (first + i * Row::kStride < D) norm_weights<V>(a.gamma, first + i * Row::kStride, 1.0f, a.vector_weights, gamma + i * V);
   float sum_gx[kNormElements] = {}, sum_g[kNormElements] = {};
   int turn = 0;
-  for (int64_t m0 = (int64_t)blockIdx.x * kRows; m0 < a.M; m0 += (int64_t)gridDim.x * kRows, turn ^= 1) {
-    const int64_t m = m0 + warp / WPR;
-    const bool here = m < a.M;
-    const int end = here ? D : 0;
-    const int64_t at = (here ? m : 0) * D;
-    Row gy, xr;
-    gy.load(grad_y + at, first, end);
-    xr.load(x + at, first, end);
-    const float mean = a.mean[here ? m : 0], rstd = a.rstd[here ? m : 0];
-    float s = 0.0f, sx = 0.0f;
+  for (int64_t m0 = (int64_t)blockIdx.x * kRows; m0 < a.M; m0 += step, m += step, turn ^= 1) {
+    const int end = m < a.M ? D : 0;
+    const bool more = m + step < a.M;
+    const int64_t next = more ? m + step : 0;
+    Row gy_next, x_next;
+    gy_next.load(grad_y + next * D, first, more ? D : 0);
+    x_next.load(x + next * D, first, more ? D : 0);
+    const float mean_next = a.mean[next], rstd_next = a.rstd[next];
+    const F minus_mean = Math::all(-mean), all_rstd = Math::all(rstd);
+    F s2 = Math::all(0.0f), sx2 = Math::all(0.0f);
 #pragma unroll
     for (int i = 0; i < Row::kVectors; ++i) {
-      const int c = first + i * Row::kStride;
-      if (c < end) {
-        float g[V], f[V], w[V];
+      if (first + i * Row::kStride < end) {
+        float g[V], f[V];
         gy.get(i, g);
         xr.get(i, f);
-        norm_weights<V>(a.gamma, c, 1.0f, a.vector_weights, w);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float xhat = (f[j] - mean) * rstd;
-          sum_gx[i * V + j] = __fmaf_rn(g[j], xhat, sum_gx[i * V + j]);
-          sum_g[i * V + j] += g[j];
-          const float gw = g[j] * w[j];
-          s += gw;
-          sx = __fmaf_rn(gw, xhat, sx);
+        for (int j = 0; j < V; j += W) {
+          const int k = i * V + j;
+          const F gj = Math::from(g + j), xhat = Math::mul(Math::add(Math::from(f + j), minus_mean), all_rstd), gw = Math::mul(gj, Math::from(gamma + k));
+          Math::to(sum_gx + k, Math::fma(gj, xhat, Math::from(sum_gx + k)));
+          Math::to(sum_g + k, Math::add(gj, Math::from(sum_g + k)));
+          s2 = Math::add(s2, gw);
+          sx2 = Math::fma(gw, xhat, sx2);
         }
       }
     }
+    float s = Math::sum(s2), sx = Math::sum(sx2);
     s = warp_sum(s);
     sx = warp_sum(sx);
     if constexpr (WPR > 1) {
@@ -275,52 +362,54 @@ __global__ void __launch_bounds__(kNormThreads, sizeof(T) == 2 ? 2 : 1) layer_no
         sx += slots[turn][1][begin + i];
       }
     }
-    s *= a.inv_d;
-    sx *= a.inv_d;
+    const F minus_s = Math::all(-s * a.inv_d), minus_sx = Math::all(-sx * a.inv_d);
 #pragma unroll
     for (int i = 0; i < Row::kVectors; ++i) {
       const int c = first + i * Row::kStride;
       if (c < end) {
-        float g[V], f[V], w[V];
+        float g[V], f[V];
         gy.get(i, g);
         xr.get(i, f);
-        norm_weights<V>(a.gamma, c, 1.0f, a.vector_weights, w);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = rstd * (__fmaf_rn(g[j], w[j], -s) - (f[j] - mean) * rstd * sx);
-        Row::put(grad_x + at, c, f);
+        for (int j = 0; j < V; j += W) {
+          const F xhat = Math::mul(Math::add(Math::from(f + j), minus_mean), all_rstd);
+          const F inner = Math::fma(Math::from(g + j), Math::from(gamma + i * V + j), minus_s);
+          Math::to(f + j, Math::mul(all_rstd, Math::fma(xhat, minus_sx, inner)));
+        }
+        Row::put(grad_x + m * D, c, f);
       }
     }
+    gy = gy_next;
+    xr = x_next;
+    mean = mean_next;
+    rstd = rstd_next;
   }
   if (!a.parts) return;
-  // the block's sums: its rows' warps one after the other
-  float* const part = a.parts + (int64_t)blockIdx.x * 2 * D;
-  for (int turn_of = 0; turn_of < kRows; ++turn_of) {
-    if (warp / WPR == turn_of) {
+  // the block's sums: its rows' warps in their order
+  float* const part = a.parts + (int64_t)blockIdx.x * (2 * kNormElements * kLanes);
+  const int at = (warp % WPR) * 32 + lane;
 #pragma unroll
-      for (int i = 0; i < Row::kVectors; ++i) {
-        const int c = first + i * Row::kStride;
-        if (c < D) {
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            float gx = sum_gx[i * V + j], g = sum_g[i * V + j];
-            if (turn_of > 0) {
-              gx += columns[c + j];
-              g += columns[D + c + j];
-            }
-            if (turn_of == kRows - 1) {
-              part[c + j] = gx;
-              part[D + c + j] = g;
-            } else {
-              columns[c + j] = gx;
-              columns[D + c + j] = g;
-            }
-          }
-        }
-      }
+  for (int i = 0; i < kNormElements; ++i) {
+    if (kRows > 1) {
+      columns[((warp / WPR * 2) * kNormElements + i) * kLanes + at] = sum_gx[i];
+      columns[((warp / WPR * 2 + 1) * kNormElements + i) * kLanes + at] = sum_g[i];
+    } else {
+      part[i * kLanes + at] = sum_gx[i];
+      part[(kNormElements + i) * kLanes + at] = sum_g[i];
     }
-    if (kRows > 1) __syncthreads();
+  }
+  if constexpr (kRows > 1) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * kNormElements * kLanes; i += kNormThreads) {
+      float s = columns[i];
+#pragma unroll
+      for (int r = 1; r < kRows; ++r) s += columns[r * (2 * kNormElements * kLanes) + i];
+      part[i] = s;
+    }
   }
 }
+// The column of register i of lane `at` of a row (`lanes` of them), vectors of V.
+__device__ __forceinline__ int norm_column(int i, int at, int lanes, int V) { return (i / V * lanes + at) * V + i % V; }
 
 template <class T>
 __global__ void __launch_bounds__(kNormThreads) layer_norm_long_backward_kernel(const T* grad_y, const T* x, T* grad_x, const NormBackArgs a) {
@@ -351,35 +440,35 @@ __global__ void __launch_bounds__(kNormThreads) layer_norm_long_backward_kernel(
   }
 }
 
-// Sums over the blocks: 32 columns a block, eight runs of blocks side by side, joined in their order.
-__global__ void __launch_bounds__(256) layer_norm_join_kernel(const float* parts, int blocks, int32_t D, float* grad_gamma, float* grad_beta) {
-  __shared__ float sums[8][32];
+// Sums over the blocks: 32 sums a block, eight runs of blocks side by side, joined in their order.  `lanes`: of a row, in whose order the
+// sums lie (half of them gamma's), or 0: in the columns' order.
+__global__ void __launch_bounds__(256) layer_norm_join_kernel(const float* parts, int blocks, int32_t sums, int32_t lanes, int32_t V, int32_t D, float* grad_gamma,
+                                                              float* grad_beta) {
+  __shared__ float joined[8][32];
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t c = (int64_t)blockIdx.x * 32 + lane;  // gamma's columns, then beta's
-  const int run = (blocks + 7) / 8, last = min((warp + 1) * run, blocks);
+  const int k = (int)blockIdx.x * 32 + lane, run = (blocks + 7) / 8, last = min((warp + 1) * run, blocks);
   float s = 0.0f;
-  if (c < 2 * (int64_t)D) {
+  if (k < sums) {
 #pragma unroll 8
-    for (int b = warp * run; b < last; ++b) s += parts[(int64_t)b * 2 * D + c];
+    for (int b = warp * run; b < last; ++b) s += parts[(int64_t)b * sums + k];
   }
-  sums[warp][lane] = s;
+  joined[warp][lane] = s;
   __syncthreads();
-  if (warp == 0 && c < 2 * (int64_t)D) {
+  if (warp == 0 && k < sums) {
 #pragma unroll
-    for (int w = 1; w < 8; ++w) s += sums[w][lane];
-    if (c < D) {
-      if (grad_gamma) grad_gamma[c] = s;
-    } else if (grad_beta) {
-      grad_beta[c - D] = s;
-    }
+    for (int w = 1; w < 8; ++w) s += joined[w][lane];
+    const int at = k < sums / 2 ? k : k - sums / 2;
+    const int c = lanes ? norm_column(at / lanes, at % lanes, lanes, V) : at;
+    float* const to = k < sums / 2 ? grad_gamma : grad_beta;
+    if (to && c < D) to[c] = s;
   }
 }
 
 constexpr size_t kNormPartsOff = 1024;
-// Blocks of the backward pass: two per SM (fp32: one), no more than there are rows for.
-static int norm_blocks(int64_t M, int rows, int sms, bool wide) { return (int)std::min<int64_t>((M + rows - 1) / rows, (int64_t)sms * (wide ? 1 : 2)); }
 static int norm_warps(int64_t D) { return D <= 1024 ? 1 : (D <= 2048 ? 2 : (D <= 4096 ? 4 : 8)); }
+// Sums that a block of the backward pass leaves: two for each register of the row's lanes, or for each column.
+static int64_t norm_sums(int64_t D) { return D > kNormMostHeld ? 2 * D : 2 * kNormElements * 32 * norm_warps(D); }
 
 template <class T>
 static qb_status launch_norm(const void* x, void* y, const NormArgs& a, int sms, cudaStream_t stream) {
@@ -390,7 +479,7 @@ static qb_status launch_norm(const void* x, void* y, const NormArgs& a, int sms,
     return (qb_status)QB_OK;
   };
   if (a.D > kNormMostHeld) return go(layer_norm_long_kernel<T>, std::min<int64_t>(a.M, (int64_t)sms * 8));
-  const int64_t grid = (a.M + 8 / warps - 1) / (8 / warps);
+  const int64_t grid = std::min<int64_t>((a.M + 8 / warps - 1) / (8 / warps), (int64_t)sms * 2);
   switch (warps) {
     case 1: return go(vector ? layer_norm_kernel<T, 1, true> : layer_norm_kernel<T, 1, false>, grid);
     case 2: return go(vector ? layer_norm_kernel<T, 2, true> : layer_norm_kernel<T, 2, false>, grid);
@@ -399,23 +488,43 @@ static qb_status launch_norm(const void* x, void* y, const NormArgs& a, int sms,
   }
 }
 
+// Lets a kernel have the shared memory that its block's sums take (once per device).
+template <auto KERNEL>
+static qb_status norm_room() {
+  static std::atomic<bool> set[64] = {};
+  int dev = 0;
+  QB_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !set[dev].load(std::memory_order_acquire)) {
+    QB_CUDA_TRY(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kNormElements * 32 * 8 * 4));
+    if (dev >= 0 && dev < 64) set[dev].store(true, std::memory_order_release);
+  }
+  return QB_OK;
+}
+// V: receives the vector length, which the order of the sums goes by.
 template <class T>
-static qb_status launch_norm_backward(const void* grad_y, const void* x, void* grad_x, const NormBackArgs& a, int blocks, cudaStream_t stream) {
+static qb_status launch_norm_backward(const void* grad_y, const void* x, void* grad_x, const NormBackArgs& a, int blocks, int* V, cudaStream_t stream) {
   const bool vector = a.D % Vec16<T>::N == 0 && aligned16(x) && aligned16(grad_y) && aligned16(grad_x);
   const int warps = norm_warps(a.D);
-  auto go = [&](auto kernel, size_t smem) {
+  *V = vector ? Vec16<T>::N : 1;
+  const size_t smem = warps < 8 && a.D <= kNormMostHeld ? (size_t)(8 / warps) * norm_sums(a.D) * 4 : 0;  // 64 KB
+  const auto with = [&](auto kernel, auto room) {
+    qb_status st = room();
+    if (st != QB_OK) return st;
     QB_CUDA_TRY(launch_kernel(kernel, (unsigned)blocks, kNormThreads, smem, stream, 1, false, static_cast<const T*>(grad_y), static_cast<const T*>(x),
                               static_cast<T*>(grad_x), a));
     return (qb_status)QB_OK;
   };
-  if (a.D > kNormMostHeld) return go(layer_norm_long_backward_kernel<T>, 0);
-  const size_t smem = warps < 8 ? (size_t)a.D * 8 : 0;  // at most 32 KB
+  if (a.D > kNormMostHeld) return with(layer_norm_long_backward_kernel<T>, [] { return (qb_status)QB_OK; });
+#define QB_NORM_BACKWARD(W)                                                                                                                    \
+  return vector ? with(layer_norm_backward_kernel<T, W, true>, norm_room<layer_norm_backward_kernel<T, W, true>>)                               \
+                : with(layer_norm_backward_kernel<T, W, false>, norm_room<layer_norm_backward_kernel<T, W, false>>)
   switch (warps) {
-    case 1: return go(vector ? layer_norm_backward_kernel<T, 1, true> : layer_norm_backward_kernel<T, 1, false>, smem);
-    case 2: return go(vector ? layer_norm_backward_kernel<T, 2, true> : layer_norm_backward_kernel<T, 2, false>, smem);
-    case 4: return go(vector ? layer_norm_backward_kernel<T, 4, true> : layer_norm_backward_kernel<T, 4, false>, smem);
-    default: return go(vector ? layer_norm_backward_kernel<T, 8, true> : layer_norm_backward_kernel<T, 8, false>, smem);
+    case 1: QB_NORM_BACKWARD(1);
+    case 2: QB_NORM_BACKWARD(2);
+    case 4: QB_NORM_BACKWARD(4);
+    default: QB_NORM_BACKWARD(8);
   }
+#undef QB_NORM_BACKWARD
 }
 
 static qb_status check_norm(const char* what, bool pointers, int type, int64_t M, int64_t D) {
@@ -429,7 +538,7 @@ static bool unaligned(const void* p, size_t n) { return reinterpret_cast<uintptr
 
 extern "C" size_t qb_layer_norm_workspace_bytes(int64_t M, int64_t D) {
   if (M <= 0 || M > QB_MAX_MN || D <= 0 || D > QB_MAX_K) return 0;
-  return qb::kNormPartsOff + (size_t)std::min<int64_t>(M, 2 * qb::kRingMaxCtas) * (size_t)D * 8;
+  return qb::kNormPartsOff + (size_t)std::min<int64_t>(M, 2 * qb::kRingMaxCtas) * (size_t)qb::norm_sums(D) * 4;
 }
 
 extern "C" qb_status qb_layer_norm(const void* x, int type, const float* gamma, const float* beta, double eps, int64_t M, int64_t D, void* y, float* mean, float* rstd,
@@ -471,16 +580,20 @@ extern "C" qb_status qb_layer_norm_backward(const void* grad_y, const void* x, i
   int sms = 0;
   if ((st = require_sm100(&sms)) != QB_OK) return st;
   sms = std::min(sms, kRingMaxCtas);
-  const int blocks = norm_blocks(M, D > kNormMostHeld ? 1 : 8 / norm_warps(D), sms, type == QB_F32);
+  const int warps = norm_warps(D), rows = D > kNormMostHeld ? 1 : 8 / warps;
+  const int blocks = (int)std::min<int64_t>((M + rows - 1) / rows, sms);  // what is resident
   float* const parts = sums ? reinterpret_cast<float*>(static_cast<char*>(ws) + kNormPartsOff) : nullptr;
   const NormBackArgs a = {gamma, mean, rstd, parts, M, (int32_t)D, (float)(1.0 / (double)D), aligned16(gamma)};
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  int V = 1;
   switch (type) {
-    case QB_F32: st = launch_norm_backward<float>(grad_y, x, grad_x, a, blocks, stream); break;
-    case QB_BF16: st = launch_norm_backward<__nv_bfloat16>(grad_y, x, grad_x, a, blocks, stream); break;
-    default: st = launch_norm_backward<__half>(grad_y, x, grad_x, a, blocks, stream);
+    case QB_F32: st = launch_norm_backward<float>(grad_y, x, grad_x, a, blocks, &V, stream); break;
+    case QB_BF16: st = launch_norm_backward<__nv_bfloat16>(grad_y, x, grad_x, a, blocks, &V, stream); break;
+    default: st = launch_norm_backward<__half>(grad_y, x, grad_x, a, blocks, &V, stream);
   }
   if (st != QB_OK || !sums) return st;
-  QB_CUDA_TRY(launch_kernel(layer_norm_join_kernel, (unsigned)((2 * D + 31) / 32), 256, 0, stream, 1, false, parts, blocks, (int32_t)D, grad_gamma, grad_beta));
+  const int32_t count = (int32_t)norm_sums(D);
+  QB_CUDA_TRY(launch_kernel(layer_norm_join_kernel, (unsigned)((count + 31) / 32), 256, 0, stream, 1, false, parts, blocks, count,
+                            D > kNormMostHeld ? 0 : 32 * warps, V, (int32_t)D, grad_gamma, grad_beta));
   return QB_OK;
 }
