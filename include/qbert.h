@@ -521,7 +521,8 @@ qb_status qb_layer_norm_backward(const void* grad_y, const void* x, int type, co
  * integer products read.  A training step keeps every linear's input and pre-activation; in this form they take 17 / 16 of a byte each.)
  * Per row and block of QB_CHECKPOINT_BLOCK columns, with a = max|x| of the block:
  *     scale = a / 127,   code = x * 127 / a rounded to nearest even,   restored value = code * scale.
- * A block with a < 2^-100 counts as zeros (scale 1); one with a NaN or an infinity restores as NaN everywhere.
+ * A block with a < 2^-100 counts as zeros (scale 1); one with a NaN or an infinity restores as NaN everywhere.  scale is a / 127 rounded to
+ * nearest, or the number below where 127 * scale would be infinite.
  *   x, y, pre, grad_y, grad_x   dev [M][K] of `type`, aligned to their elements
  *   codes    dev int8 [M][K], aligned to 16 bytes;   scales  dev fp32 [M][ceil(K / QB_CHECKPOINT_BLOCK)]
  * qb_checkpoint saves x.  qb_restore gives act(restored value), rounded to `type` once: QB_IDENTITY the value, QB_GELU the activation's

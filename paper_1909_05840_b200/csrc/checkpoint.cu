@@ -1,7 +1,7 @@
 // qb_checkpoint, qb_restore, qb_gelu_backward: activations saved in 8 bits with a scale per row and block of 64 columns, and their use.
 //
 // A block's 64 values lie in 8 (16-bit types) or 16 (fp32) neighbouring lanes, 16 bytes each, which agree on the largest magnitude by
-// shuffles; codes are rounded in 32 bits, and again in 64 where the quotient lies next to the border of two of them.
+// shuffles.  The quotients are exact for 16-bit types; in fp32 they are formed again in 64 bits where they lie next to the border of two codes.
 // Bound by memory: one read and one write of each tensor.
 #include "checkpoint.cuh"
 #include "common.cuh"
@@ -14,6 +14,10 @@ namespace qb {
 
 constexpr int kCheckpointThreads = 256;
 constexpr int kCheckpointUnroll = 4;  // vectors that a thread has in flight
+
+// Turns of the kernel that saves, two vectors each.
+template <class T>
+constexpr int kCheckpointTurns = sizeof(T) == 4 ? 4 : 2;
 
 // Where vector `v` of a matrix of `blocks` blocks a row lies.  FLAT: rows are whole blocks, so that vectors follow one another.
 template <int N, bool FLAT>
@@ -33,90 +37,114 @@ struct CheckpointAt {
   }
 };
 
-// The codes of N values as bytes.
+// The codes of N values as bytes, where the row has them (left > 0).
 template <int N>
-__device__ __forceinline__ void store_codes(int8_t* p, const uint32_t (&w)[N / 4], int64_t left, bool vector) {
-  if (vector) {
-    if (left > 0) {
-      if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-      else *reinterpret_cast<uint32_t*>(p) = w[0];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j < left) p[j] = (int8_t)(w[j >> 2] >> (8 * (j & 3)));
-  }
+__device__ __forceinline__ void store_codes(int8_t* p, const uint32_t (&w)[N / 4], int64_t left) {
+  if (left <= 0) return;
+  if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint32_t*>(p) = w[0];
 }
 template <int N>
-__device__ __forceinline__ void load_codes(const int8_t* p, uint32_t (&w)[N / 4], int64_t left, bool vector) {
+__device__ __forceinline__ void load_codes(const int8_t* p, uint32_t (&w)[N / 4], int64_t left) {
 #pragma unroll
   for (int j = 0; j < N / 4; ++j) w[j] = 0;
-  if (vector) {
-    if (left > 0) {
-      if constexpr (N == 8) {
-        const uint2 q = *reinterpret_cast<const uint2*>(p);
-        w[0] = q.x;
-        w[1] = q.y;
-      } else {
-        w[0] = *reinterpret_cast<const uint32_t*>(p);
-      }
-    }
+  if (left <= 0) return;
+  if constexpr (N == 8) {
+    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    w[0] = q.x;
+    w[1] = q.y;
   } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j < left) w[j >> 2] |= (uint32_t)(uint8_t)p[j] << (8 * (j & 3));
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
   }
 }
 
-// Codes whose 32-bit quotient may lie on the wrong side of a border, from the quotient in 64 bits (its error is far below the least
+// A code whose 32-bit quotient may lie on the wrong side of a border, from the quotient in 64 bits (its error is far below the least
 // distance of a quotient of two 24-bit numbers from a border that it does not lie on).
-template <int N>
-__device__ __noinline__ void exact_codes(const float (&f)[N], float top, uint32_t (&w)[N / 4]) {
-#pragma unroll
-  for (int j = 0; j < N / 4; ++j) w[j] = 0;
-#pragma unroll
-  for (int j = 0; j < N; ++j) w[j >> 2] |= (uint32_t)(uint8_t)(int8_t)__double2int_rn((double)f[j] * 127.0 / (double)top) << (8 * (j & 3));
-}
+__device__ __forceinline__ int8_t exact_code(float x, float top) { return (int8_t)__double2int_rn((double)x * 127.0 / (double)top); }
+constexpr float kNearBorder = 0.5f - 4.0e-5f;  // x * scale is off by 127 * 2^-22 at most
 
-template <class T, bool FLAT, bool VECTOR>
+// A thread takes two neighbouring vectors of a block, U times.
+template <class T, bool FLAT>
 __global__ void __launch_bounds__(kCheckpointThreads) checkpoint_kernel(const T* x, int8_t* codes, float* scales, int64_t vectors, int64_t K, int64_t blocks) {
-  constexpr int N = Vec16<T>::N, kPer = kCheckpointBlock / N, U = kCheckpointUnroll;
+  constexpr int N = Vec16<T>::N, kPer = kCheckpointBlock / N / 2, U = kCheckpointTurns<T>;
   pdl_begin();
-  const int64_t base = (int64_t)blockIdx.x * (kCheckpointThreads * U) + threadIdx.x;
-  Vec16<T> v[U];
+  const int64_t base = ((int64_t)blockIdx.x * (kCheckpointThreads * U) + threadIdx.x) * 2;
+  Vec16<T> v[U][2];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t i = base + u * kCheckpointThreads;
+    const int64_t i = base + u * (2 * kCheckpointThreads);
     if (i < vectors) {
       const CheckpointAt<N, FLAT> at(i, K, blocks);
-      v[u].template load<VECTOR>(x + at.element, at.left);
+      v[u][0].template load<true>(x + at.element, at.left);
+      v[u][1].template load<true>(x + at.element + N, at.left - (FLAT ? 0 : N));
     } else {
-      v[u].raw = make_uint4(0u, 0u, 0u, 0u);
+      v[u][0].raw = v[u][1].raw = make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+  float top[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    top[u] = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float f[N];
+      v[u][h].get(f);
+#pragma unroll
+      for (int j = 0; j < N; j += 2) top[u] = max3_nan(top[u], fabsf(f[j]), fabsf(f[j + 1]));
     }
   }
 #pragma unroll
+  for (int d = 1; d < kPer; d *= 2) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) top[u] = max3_nan(top[u], __shfl_xor_sync(0xffffffffu, top[u], d), 0.0f);
+  }
+  // one division a thread: lane u of a block's writes the scale of its block of turn u
+  static_assert(U <= kPer, "lanes of a block");
+  const int lane = threadIdx.x % kPer;
+  float scale = top[0];
+#pragma unroll
+  for (int u = 1; u < U; ++u) scale = lane == u ? top[u] : scale;
+  scale = checkpoint_scale(scale);
+  if (lane < U) {
+    const int64_t i = base - 2 * lane + (int64_t)lane * (2 * kCheckpointThreads);
+    if (i < vectors) scales[CheckpointAt<N, FLAT>(i, K, blocks).block] = scale;
+  }
+#pragma unroll
   for (int u = 0; u < U; ++u) {
-    float f[N];
-    v[u].get(f);
-    float top = 0.0f;
+    const int64_t i = base + u * (2 * kCheckpointThreads);
+    if (i >= vectors) return;
+    const CheckpointAt<N, FLAT> at(i, K, blocks);
+    const CheckpointCodes cs(top[u]);
 #pragma unroll
-    for (int j = 0; j < N; j += 2) top = max3_nan(top, fabsf(f[j]), fabsf(f[j + 1]));
-#pragma unroll
-    for (int d = 1; d < kPer; d *= 2) top = max3_nan(top, __shfl_xor_sync(0xffffffffu, top, d), 0.0f);
-    const int64_t i = base + u * kCheckpointThreads;
-    if (i < vectors) {
-      const CheckpointAt<N, FLAT> at(i, K, blocks);
-      const CheckpointScale cs(top);
-      float far = 0.0f;  // the largest distance of a quotient from its code
-#pragma unroll
-      for (int j = 0; j < N; ++j) far = fmaxf(far, fabsf(__fmaf_rn(f[j], cs.inv, CheckpointScale::kShift - cs.shifted(f[j]))));
+    for (int h = 0; h < 2; ++h) {
+      float f[N];
+      v[u][h].get(f);
+      bool exact = false;
+      uint64_t q[N / 2];
       uint32_t w[N / 4];
+      if constexpr (sizeof(T) == 2) {
 #pragma unroll
-      for (int j = 0; j < N / 4; ++j) w[j] = cs.codes4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
-      // x * inv is off by 127 * 2^-24 at most
-      if (far > 0.5f - 1.0e-5f) exact_codes(f, top, w);
-      store_codes<N>(codes + at.element, w, at.left, VECTOR);
-      if (i % kPer == 0) scales[at.block] = cs.scale;
+        for (int j = 0; j < N / 2; ++j) q[j] = cs.exact16(ptx::pack_f32x2(f[2 * j], f[2 * j + 1]));
+      } else {
+        float far = 0.0f;  // the largest distance of a quotient from its code
+        const uint64_t minus_shift = ptx::pack_f32x2(-CheckpointCodes::kShift, -CheckpointCodes::kShift), minus_scale = ptx::pack_f32x2(-cs.scale, -cs.scale);
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+          const uint64_t x2 = ptx::pack_f32x2(f[2 * j], f[2 * j + 1]);
+          q[j] = cs.shifted(x2);
+          const float2 d = ptx::unpack_f32x2(ptx::fma_f32x2(x2, minus_scale, ptx::add_f32x2(q[j], minus_shift)));
+          far = fmaxf(far, fmaxf(fabsf(d.x), fabsf(d.y)));
+        }
+        exact = far > kNearBorder;
+      }
+#pragma unroll
+      for (int j = 0; j < N / 4; ++j) w[j] = CheckpointCodes::bytes4(q[2 * j], q[2 * j + 1]);
+      const int64_t left = FLAT ? N : at.left - h * N;
+      store_codes<N>(codes + at.element + h * N, w, left);
+      if (sizeof(T) == 4 && exact && left > 0) {  // rare: x is read again rather than kept
+#pragma unroll 1
+        for (int j = 0; j < N; ++j) codes[at.element + h * N + j] = exact_code(to_float(x[at.element + h * N + j]), top[u]);
+      }
     }
   }
 }
@@ -125,7 +153,7 @@ __global__ void __launch_bounds__(kCheckpointThreads) checkpoint_kernel(const T*
 enum ActivationUse { kValue = 0, kActivation = 1, kSlopeOf = 2 };
 
 // CODES: p from codes and scales, else from `pre`.
-template <class T, int USE, bool CODES, bool FLAT, bool VECTOR>
+template <class T, int USE, bool CODES, bool FLAT>
 __global__ void __launch_bounds__(kCheckpointThreads) activation_kernel(const T* grad_y, const T* pre, const int8_t* codes, const float* scales, T* y, int64_t vectors,
                                                                         int64_t K, int64_t blocks) {
   constexpr int N = Vec16<T>::N, U = kCheckpointUnroll;
@@ -139,12 +167,12 @@ __global__ void __launch_bounds__(kCheckpointThreads) activation_kernel(const T*
     const int64_t i = base + u * kCheckpointThreads;
     if (i < vectors) {
       const CheckpointAt<N, FLAT> at(i, K, blocks);
-      if constexpr (USE == kSlopeOf) g[u].template load<VECTOR>(grad_y + at.element, at.left);
+      if constexpr (USE == kSlopeOf) g[u].template load<true>(grad_y + at.element, at.left);
       if constexpr (CODES) {
-        load_codes<N>(codes + at.element, w[u], at.left, VECTOR);
+        load_codes<N>(codes + at.element, w[u], at.left);
         scale[u] = scales[at.block];
       } else {
-        v[u].template load<VECTOR>(pre + at.element, at.left);
+        v[u].template load<true>(pre + at.element, at.left);
       }
     }
   }
@@ -167,40 +195,154 @@ __global__ void __launch_bounds__(kCheckpointThreads) activation_kernel(const T*
     const CheckpointAt<N, FLAT> at(i, K, blocks);
     Vec16<T> out;
     out.set(USE == kSlopeOf ? d : p);
-    out.template store<VECTOR>(y + at.element, at.left);
+    out.template store<true>(y + at.element, at.left);
   }
 }
 
+// Rows of any length and alignment: a warp a block of 64, two values a lane, U blocks at a time.
+constexpr int kAnyBlocks = 4;
+struct AnyBlock {
+  int64_t block, element, col;
+  __device__ __forceinline__ AnyBlock(int64_t b, int64_t K, int64_t blocks) : block(b) {
+    const int64_t row = (b | blocks) >> 32 ? b / blocks : (int64_t)((uint32_t)b / (uint32_t)blocks);
+    col = (b - row * blocks) * kCheckpointBlock;
+    element = row * K + col;
+  }
+  __device__ __forceinline__ int cols(int64_t K) const { return (int)min((int64_t)kCheckpointBlock, K - col); }
+  __device__ __forceinline__ void next(int64_t K) {
+    ++block;
+    element += cols(K);
+    col += kCheckpointBlock;
+    if (col >= K) col = 0;
+  }
+};
+template <class T>
+__global__ void __launch_bounds__(kCheckpointThreads) checkpoint_any_kernel(const T* x, int8_t* codes, float* scales, int64_t count, int64_t K, int64_t blocks) {
+  constexpr int U = kAnyBlocks;
+  pdl_begin();
+  const int lane = threadIdx.x & 31;
+  const int64_t first = ((int64_t)blockIdx.x * (kCheckpointThreads / 32) + (threadIdx.x >> 5)) * U;
+  const AnyBlock begin(first, K, blocks);
+  AnyBlock at = begin;
+  float f[U][2];
+#pragma unroll
+  for (int u = 0; u < U; ++u, at.next(K)) {
+    f[u][0] = f[u][1] = 0.0f;
+    if (first + u < count) {
+      if (lane < at.cols(K)) f[u][0] = to_float(x[at.element + lane]);
+      if (lane + 32 < at.cols(K)) f[u][1] = to_float(x[at.element + lane + 32]);
+    }
+  }
+  float top[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) top[u] = max3_nan(fabsf(f[u][0]), fabsf(f[u][1]), 0.0f);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) top[u] = max3_nan(top[u], __shfl_xor_sync(0xffffffffu, top[u], d), 0.0f);
+  }
+  at = begin;
+#pragma unroll
+  for (int u = 0; u < U; ++u, at.next(K)) {
+    if (first + u >= count) return;
+    const CheckpointCodes cs(top[u]);
+    const uint64_t x2 = ptx::pack_f32x2(f[u][0], f[u][1]);
+    float2 q;
+    if constexpr (sizeof(T) == 2) {
+      q = ptx::unpack_f32x2(cs.exact16(x2));
+    } else {
+      q = ptx::unpack_f32x2(cs.shifted(x2));
+      const float d0 = __fmaf_rn(f[u][0], -cs.scale, q.x - CheckpointCodes::kShift), d1 = __fmaf_rn(f[u][1], -cs.scale, q.y - CheckpointCodes::kShift);
+      if (fmaxf(fabsf(d0), fabsf(d1)) > kNearBorder) {
+        q.x = __int_as_float(exact_code(f[u][0], top[u]));
+        q.y = __int_as_float(exact_code(f[u][1], top[u]));
+      }
+    }
+    if (lane < at.cols(K)) codes[at.element + lane] = (int8_t)__float_as_uint(q.x);
+    if (lane + 32 < at.cols(K)) codes[at.element + lane + 32] = (int8_t)__float_as_uint(q.y);
+    if (lane == 0) scales[at.block] = checkpoint_scale(top[u]);
+  }
+}
+template <class T, int USE, bool CODES>
+__global__ void __launch_bounds__(kCheckpointThreads) activation_any_kernel(const T* grad_y, const T* pre, const int8_t* codes, const float* scales, T* y, int64_t count,
+                                                                            int64_t K, int64_t blocks) {
+  constexpr int U = kAnyBlocks;
+  pdl_begin();
+  const int lane = threadIdx.x & 31;
+  const int64_t first = ((int64_t)blockIdx.x * (kCheckpointThreads / 32) + (threadIdx.x >> 5)) * U;
+  const AnyBlock begin(first, K, blocks);
+  AnyBlock at = begin;
+  float p[2 * U], g[2 * U];
+#pragma unroll
+  for (int u = 0; u < U; ++u, at.next(K)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      p[2 * u + h] = g[2 * u + h] = 0.0f;
+      if (first + u < count) {
+        const int c = lane + 32 * h;
+        if (c < at.cols(K)) {
+          if constexpr (CODES) p[2 * u + h] = (float)codes[at.element + c] * scales[at.block];
+          else p[2 * u + h] = to_float(pre[at.element + c]);
+          if constexpr (USE == kSlopeOf) g[2 * u + h] = to_float(grad_y[at.element + c]);
+        }
+      }
+    }
+  }
+  if constexpr (USE == kActivation) gelu_many<U>(p);
+  if constexpr (USE == kSlopeOf) times_gelu_slope<U>(p, g);
+  at = begin;
+#pragma unroll
+  for (int u = 0; u < U; ++u, at.next(K)) {
+    if (first + u >= count) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (lane + 32 * h < at.cols(K)) y[at.element + lane + 32 * h] = from_float<T>(USE == kSlopeOf ? g[2 * u + h] : p[2 * u + h]);
+  }
+}
+
+// Vectors, blocks of a row, and whether rows are made of whole vectors and of whole blocks.
 template <class T>
 struct CheckpointShape {
-  int64_t vectors, blocks;
-  unsigned grid;
+  int64_t count, vectors, blocks;
   bool flat, vector;
   CheckpointShape(int64_t M, int64_t K, bool aligned) {
     constexpr int N = Vec16<T>::N;
     blocks = checkpoint_blocks(K);
-    vectors = M * blocks * (kCheckpointBlock / N);
-    constexpr int64_t per = (int64_t)kCheckpointThreads * kCheckpointUnroll;
-    grid = (unsigned)((vectors + per - 1) / per);
+    count = M * blocks;
+    vectors = count * (kCheckpointBlock / N);
     vector = aligned && K % N == 0;
     flat = vector && K % kCheckpointBlock == 0;
+  }
+  // blocks of threads whose threads take `turns` vectors each (no vectors: whose warps take kAnyBlocks blocks)
+  unsigned grid(int turns) const {
+    const int64_t per = vector ? (int64_t)kCheckpointThreads * turns : kCheckpointThreads / 32 * kAnyBlocks, all = vector ? vectors : count;
+    return (unsigned)((all + per - 1) / per);
   }
 };
 
 template <class T>
-static qb_status launch_checkpoint(const void* x, int64_t M, int64_t K, int8_t* codes, float* scales, cudaStream_t stream) {
+static qb_status launch_checkpoint(const void* x_data, int64_t M, int64_t K, int8_t* codes, float* scales, cudaStream_t stream) {
+  const T* const x = static_cast<const T*>(x_data);
   const CheckpointShape<T> s(M, K, aligned16(x));
-  auto kernel = s.flat ? checkpoint_kernel<T, true, true> : (s.vector ? checkpoint_kernel<T, false, true> : checkpoint_kernel<T, false, false>);
-  QB_CUDA_TRY(launch_kernel<kMostL1>(kernel, s.grid, kCheckpointThreads, 0, stream, 1, false, static_cast<const T*>(x), codes, scales, s.vectors, K, s.blocks));
+  const unsigned grid = s.grid(2 * kCheckpointTurns<T>);
+  if (s.vector)
+    QB_CUDA_TRY(launch_kernel<kMostL1>(s.flat ? checkpoint_kernel<T, true> : checkpoint_kernel<T, false>, grid, kCheckpointThreads, 0, stream, 1, false, x, codes, scales,
+                                       s.vectors, K, s.blocks));
+  else
+    QB_CUDA_TRY(launch_kernel<kMostL1>(checkpoint_any_kernel<T>, grid, kCheckpointThreads, 0, stream, 1, false, x, codes, scales, s.count, K, s.blocks));
   return QB_OK;
 }
 template <class T, int USE, bool CODES>
 static qb_status launch_activation(const void* grad_y, const void* pre, const int8_t* codes, const float* scales, int64_t M, int64_t K, void* y, cudaStream_t stream) {
   const CheckpointShape<T> s(M, K, aligned16(grad_y) && aligned16(pre) && aligned16(y));
-  auto kernel = s.flat ? activation_kernel<T, USE, CODES, true, true>
-                       : (s.vector ? activation_kernel<T, USE, CODES, false, true> : activation_kernel<T, USE, CODES, false, false>);
-  QB_CUDA_TRY(launch_kernel<kMostL1>(kernel, s.grid, kCheckpointThreads, 0, stream, 1, false, static_cast<const T*>(grad_y), static_cast<const T*>(pre), codes, scales,
-                                     static_cast<T*>(y), s.vectors, K, s.blocks));
+  const unsigned grid = s.grid(kCheckpointUnroll);
+  const T *const g = static_cast<const T*>(grad_y), *const p = static_cast<const T*>(pre);
+  if (s.vector)
+    QB_CUDA_TRY(launch_kernel<kMostL1>(s.flat ? activation_kernel<T, USE, CODES, true> : activation_kernel<T, USE, CODES, false>, grid, kCheckpointThreads, 0, stream, 1,
+                                       false, g, p, codes, scales, static_cast<T*>(y), s.vectors, K, s.blocks));
+  else
+    QB_CUDA_TRY(launch_kernel<kMostL1>(activation_any_kernel<T, USE, CODES>, grid, kCheckpointThreads, 0, stream, 1, false, g, p, codes, scales, static_cast<T*>(y), s.count,
+                                       K, s.blocks));
   return QB_OK;
 }
 

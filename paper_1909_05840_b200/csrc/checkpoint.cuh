@@ -9,28 +9,41 @@ namespace qb {
 constexpr int kCheckpointBlock = QB_CHECKPOINT_BLOCK;
 inline __host__ __device__ int64_t checkpoint_blocks(int64_t K) { return (K + kCheckpointBlock - 1) / kCheckpointBlock; }
 
-// The scale of a block whose largest magnitude is `top` (NaN where the block has one), and its codes.
-struct CheckpointScale {
-  float scale, inv;
-  __device__ __forceinline__ explicit CheckpointScale(float top) {
-    if (!(top < INFINITY)) {  // a NaN or an infinity: the block restores as NaN
-      scale = __int_as_float(0x7fffffff);
-      inv = 0.0f;
-    } else if (top < 7.8886091e-31f) {  // 2^-100: counts as zeros (127 / top would leave fp32's range a little below)
-      scale = 1.0f;
-      inv = 0.0f;
-    } else {
-      scale = top / 127.0f;
-      inv = 127.0f / top;
-    }
+__device__ __forceinline__ float checkpoint_scale(float top) {
+  if (!(top < INFINITY)) return __int_as_float(0x7fffffff);  // a NaN or an infinity: the block restores as NaN
+  if (top < 7.8886091e-31f) return 1.0f;                     // below 2^-100 it counts as zeros
+  return fminf(top / 127.0f, __int_as_float(0x7c010203));    // 127 times the largest scale is still finite
+}
+// The codes of such a block, from quotients of 32 bits: step is 128 / top and scale 127 / top within 2^-22 of themselves (both 0 where every code is 0).
+struct CheckpointCodes {
+  float step, scale, top;
+  __device__ __forceinline__ explicit CheckpointCodes(float top) : top(top) {
+    // of top * 2^-6, so that the reciprocal of the largest numbers is not a subnormal one
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(top * 0.015625f));
+    r = top >= 7.8886091e-31f && top < INFINITY ? r : 0.0f;
+    step = r * 2.0f;
+    scale = r * 1.984375f;
   }
-  // x * inv rounded to nearest even, by an addition that leaves nothing behind the point: its low byte is the code
+  // Two quotients rounded to nearest even, by an addition that leaves nothing behind the point: a code is the low byte.
   static constexpr float kShift = 12582912.0f;  // 1.5 * 2^23
-  __device__ __forceinline__ float shifted(float x) const { return __fmaf_rn(x, inv, kShift); }
+  __device__ __forceinline__ uint64_t shifted(uint64_t x) const { return ptx::fma_f32x2(x, ptx::pack_f32x2(scale, scale), ptx::pack_f32x2(kShift, kShift)); }
+  // The same for x and top of at most 11 bits (16-bit types): 127 x is exact, so that one correction of the quotient by what it leaves of
+  // 127 x gives the exact one, rounded once.  A quotient of such numbers that is not on the border of two codes is more than 2^-20 of
+  // itself from it: the code is that of the exact quotient.
+  __device__ __forceinline__ uint64_t exact16(uint64_t x) const {
+    const uint64_t p = ptx::mul_f32x2(x, ptx::pack_f32x2(scale, scale));
+    const float minus = top * -0.0078125f;  // all of it over 128: 127 x may be too large for fp32
+    const uint64_t left = ptx::fma_f32x2(p, ptx::pack_f32x2(minus, minus), ptx::mul_f32x2(x, ptx::pack_f32x2(0.9921875f, 0.9921875f)));
+    return ptx::add_f32x2(ptx::fma_f32x2(left, ptx::pack_f32x2(step, step), p), ptx::pack_f32x2(kShift, kShift));
+  }
+  static __device__ __forceinline__ uint32_t bytes4(uint64_t lo, uint64_t hi) {
+    const float2 a = ptx::unpack_f32x2(lo), b = ptx::unpack_f32x2(hi);
+    const uint32_t l = __byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), h = __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040);
+    return __byte_perm(l, h, 0x5410);
+  }
   __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) const {
-    const uint32_t lo = __byte_perm(__float_as_uint(shifted(a)), __float_as_uint(shifted(b)), 0x0040);
-    const uint32_t hi = __byte_perm(__float_as_uint(shifted(c)), __float_as_uint(shifted(d)), 0x0040);
-    return __byte_perm(lo, hi, 0x5410);
+    return bytes4(shifted(ptx::pack_f32x2(a, b)), shifted(ptx::pack_f32x2(c, d)));
   }
 };
 

@@ -73,6 +73,54 @@ struct NormRow {
     }
   }
 };
+// Rows on their way: a ring of stages in shared memory, filled by copies of 16 bytes that need no registers.  A thread copies and reads its
+// own bytes alone, so that nobody waits for anybody.  TENSORS rows a stage.
+template <class T, int WPR, int TENSORS>
+struct NormRing {
+  using Row = NormRow<T, WPR, true>;
+  static constexpr int kStageBytes = TENSORS * Row::kVectors * 16 * kNormThreads;
+  // forward: two blocks per SM
+  static constexpr int kStages = TENSORS == 1 ? 98304 / kStageBytes : 196608 / kStageBytes;
+  // behind the rows, backward: mean and rstd, a copy of each for every lane (loads that are waited for within a row's turn cost 24,576 x
+  // 1,024 bfloat16 10 us of 40)
+  static constexpr int kStatsBytes = TENSORS == 1 ? 0 : kStages * kNormThreads * 8;
+  static constexpr int kBytes = kStages * kStageBytes + kStatsBytes;
+  static_assert(kStages >= 3, "stages");
+  uint32_t mine;
+  __device__ __forceinline__ explicit NormRing(const void* smem) : mine(ptx::smem_u32(smem) + threadIdx.x * 16) {}
+  __device__ __forceinline__ uint32_t at(int stage, int tensor, int i) const {
+    return mine + (uint32_t)((stage * TENSORS + tensor) * Row::kVectors + i) * (16 * kNormThreads);
+  }
+  __device__ __forceinline__ void fetch(int stage, int tensor, const T* row, int first, int end) const {
+#pragma unroll
+    for (int i = 0; i < Row::kVectors; ++i) {
+      const int c = first + i * Row::kStride;
+      if (c < end) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at(stage, tensor, i)), "l"(row + c) : "memory");
+    }
+  }
+  __device__ __forceinline__ uint32_t stats_at(int stage) const { return mine + kStages * kStageBytes - threadIdx.x * 8 + stage * (kNormThreads * 8); }
+  __device__ __forceinline__ void fetch_stats(int stage, const float* mean, const float* rstd) const {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(stats_at(stage)), "l"(mean) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(stats_at(stage) + 4), "l"(rstd) : "memory");
+  }
+  __device__ __forceinline__ void read_stats(int stage, float& mean, float& rstd) const {
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(mean), "=f"(rstd) : "r"(stats_at(stage)) : "memory");
+  }
+  static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory"); }
+  static __device__ __forceinline__ void wait_all() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+  // (vectors behind the row's end were not copied, and are zeros)
+  __device__ __forceinline__ void read(int stage, int tensor, Row& r, int first, int end) const {
+#pragma unroll
+    for (int i = 0; i < Row::kVectors; ++i) {
+      uint32_t* const w = r.raw + 4 * i;
+      w[0] = w[1] = w[2] = w[3] = 0u;
+      if (first + i * Row::kStride < end)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at(stage, tensor, i)) : "memory");
+    }
+  }
+};
+
 // V weights from column c on (fp32, 16-byte aligned where V is above 1 and VECTOR), or `instead` of them.
 template <int V>
 __device__ __forceinline__ void norm_weights(const float* w, int c, float instead, bool vector, float* f) {
@@ -168,13 +216,11 @@ struct NormArgs {
   int32_t vector_weights;
 };
 
-// A block goes over its share of the rows with the weights in registers.  In 16 bits the row after the present one is on its way
-// meanwhile; in fp32 there is no room for it, and the other warps' rows are.
+// A block goes over its share of the rows with the weights in registers and the next rows on their way.
 template <class T, int WPR, bool VECTOR>
 __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x, T* y, const NormArgs a) {
   using Row = NormRow<T, WPR, VECTOR>;
   constexpr int V = Row::V;
-  constexpr bool kAhead = Row::kRegs <= 16;
   typedef NormMath<V> Math;
   typedef typename Math::F F;
   constexpr int W = Math::W;
@@ -184,8 +230,18 @@ __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x,
   const int first = ((warp % WPR) * 32 + lane) * V;
   const int64_t step = (int64_t)gridDim.x * (8 / WPR);
   int64_t m = (int64_t)blockIdx.x * (8 / WPR) + warp / WPR;
-  Row next;
-  next.load(x + (m < a.M ? m : 0) * D, first, m < a.M ? D : 0);
+  using Ring = NormRing<T, WPR, 1>;
+  extern __shared__ __align__(16) float room[];
+  const Ring ring(room);
+  const auto fetch = [&](int stage, int64_t row) {
+    if (row < a.M) ring.fetch(stage, 0, x + row * D, first, D);
+    Ring::commit();
+  };
+  if constexpr (VECTOR) {
+#pragma unroll
+    for (int k = 0; k < Ring::kStages - 1; ++k) fetch(k, m + k * step);
+  }
+  int stage = 0;
   float gamma[kNormElements], beta[kNormElements];
 #pragma unroll
   for (int i = 0; i < Row::kVectors; ++i) {
@@ -198,9 +254,15 @@ __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x,
   int turn = 0;
   for (int64_t m0 = (int64_t)blockIdx.x * (8 / WPR); m0 < a.M; m0 += step, m += step, turn ^= 1) {
     const int end = m < a.M ? D : 0;
-    const bool more = m + step < a.M;
-    const Row r = next;
-    if constexpr (kAhead) next.load(x + (more ? m + step : 0) * D, first, more ? D : 0);
+    Row r;
+    if constexpr (VECTOR) {
+      Ring::wait();
+      ring.read(stage, 0, r, first, end);
+      fetch(stage == 0 ? Ring::kStages - 1 : stage - 1, m + (Ring::kStages - 1) * step);  // where the row before was
+      if (++stage == Ring::kStages) stage = 0;
+    } else {
+      r.load(x + (end ? m : 0) * D, first, end);
+    }
     F s = Math::all(0.0f);
 #pragma unroll
     for (int i = 0; i < Row::kVectors; ++i) {
@@ -238,7 +300,6 @@ __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x,
         Row::put(y + m * D, c, f);
       }
     }
-    if constexpr (!kAhead) next.load(x + (more ? m + step : 0) * D, first, more ? D : 0);
     if (a.mean && end && warp % WPR == 0 && lane == 0) {
       a.mean[m] = mean;
       a.rstd[m] = rstd;
@@ -301,17 +362,29 @@ __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(co
   typedef NormMath<V> Math;
   typedef typename Math::F F;
   constexpr int W = Math::W;
-  extern __shared__ float columns[];  // [rows of the block][2][registers][lanes of a row]
+  extern __shared__ __align__(16) float room[];
+  float* const columns = room;  // [rows of the block][2][registers][lanes of a row], behind the last row
   __shared__ float slots[2][2][8];
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.D;
   const int first = ((warp % WPR) * 32 + lane) * V;
   const int64_t step = (int64_t)gridDim.x * kRows;
   int64_t m = (int64_t)blockIdx.x * kRows + warp / WPR;
-  Row gy, xr;
-  gy.load(grad_y + (m < a.M ? m : 0) * D, first, m < a.M ? D : 0);
-  xr.load(x + (m < a.M ? m : 0) * D, first, m < a.M ? D : 0);
-  float mean = a.mean[m < a.M ? m : 0], rstd = a.rstd[m < a.M ? m : 0];
+  using Ring = NormRing<T, WPR, 2>;
+  const Ring ring(room);
+  const auto fetch = [&](int stage, int64_t row) {
+    if (row < a.M) {
+      ring.fetch(stage, 0, grad_y + row * D, first, D);
+      ring.fetch(stage, 1, x + row * D, first, D);
+      ring.fetch_stats(stage, a.mean + row, a.rstd + row);
+    }
+    Ring::commit();
+  };
+  if constexpr (VECTOR) {
+#pragma unroll
+    for (int k = 0; k < Ring::kStages - 1; ++k) fetch(k, m + k * step);
+  }
+  int stage = 0;
   float gamma[kNormElements];
 #pragma unroll
   for (int i = 0; i < Row::kVectors; ++i)
@@ -320,12 +393,21 @@ __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(co
   int turn = 0;
   for (int64_t m0 = (int64_t)blockIdx.x * kRows; m0 < a.M; m0 += step, m += step, turn ^= 1) {
     const int end = m < a.M ? D : 0;
-    const bool more = m + step < a.M;
-    const int64_t next = more ? m + step : 0;
-    Row gy_next, x_next;
-    gy_next.load(grad_y + next * D, first, more ? D : 0);
-    x_next.load(x + next * D, first, more ? D : 0);
-    const float mean_next = a.mean[next], rstd_next = a.rstd[next];
+    Row gy, xr;
+    float mean = 0.0f, rstd = 0.0f;
+    if constexpr (VECTOR) {
+      Ring::wait();
+      ring.read(stage, 0, gy, first, end);
+      ring.read(stage, 1, xr, first, end);
+      if (end) ring.read_stats(stage, mean, rstd);
+      fetch(stage == 0 ? Ring::kStages - 1 : stage - 1, m + (Ring::kStages - 1) * step);  // where the row before was
+      if (++stage == Ring::kStages) stage = 0;
+    } else {
+      gy.load(grad_y + (end ? m : 0) * D, first, end);
+      xr.load(x + (end ? m : 0) * D, first, end);
+      mean = a.mean[end ? m : 0];
+      rstd = a.rstd[end ? m : 0];
+    }
     const F minus_mean = Math::all(-mean), all_rstd = Math::all(rstd);
     F s2 = Math::all(0.0f), sx2 = Math::all(0.0f);
 #pragma unroll
@@ -379,12 +461,12 @@ __global__ void __launch_bounds__(kNormThreads, 1) layer_norm_backward_kernel(co
         Row::put(grad_x + m * D, c, f);
       }
     }
-    gy = gy_next;
-    xr = x_next;
-    mean = mean_next;
-    rstd = rstd_next;
   }
   if (!a.parts) return;
+  if constexpr (VECTOR && kRows > 1) {  // the sums take the ring's place
+    Ring::wait_all();
+    __syncthreads();
+  }
   // the block's sums: its rows' warps in their order
   float* const part = a.parts + (int64_t)blockIdx.x * (2 * kNormElements * kLanes);
   const int at = (warp % WPR) * 32 + lane;
@@ -470,61 +552,72 @@ static int norm_warps(int64_t D) { return D <= 1024 ? 1 : (D <= 2048 ? 2 : (D <=
 // Sums that a block of the backward pass leaves: two for each register of the row's lanes, or for each column.
 static int64_t norm_sums(int64_t D) { return D > kNormMostHeld ? 2 * D : 2 * kNormElements * 32 * norm_warps(D); }
 
-template <class T>
-static qb_status launch_norm(const void* x, void* y, const NormArgs& a, int sms, cudaStream_t stream) {
-  const bool vector = a.D % Vec16<T>::N == 0 && aligned16(x) && aligned16(y);
-  const int warps = norm_warps(a.D);
-  auto go = [&](auto kernel, int64_t grid) {
-    QB_CUDA_TRY(launch_kernel<kMostL1>(kernel, (unsigned)grid, kNormThreads, 0, stream, 1, false, static_cast<const T*>(x), static_cast<T*>(y), a));
-    return (qb_status)QB_OK;
-  };
-  if (a.D > kNormMostHeld) return go(layer_norm_long_kernel<T>, std::min<int64_t>(a.M, (int64_t)sms * 8));
-  const int64_t grid = std::min<int64_t>((a.M + 8 / warps - 1) / (8 / warps), (int64_t)sms * 2);
-  switch (warps) {
-    case 1: return go(vector ? layer_norm_kernel<T, 1, true> : layer_norm_kernel<T, 1, false>, grid);
-    case 2: return go(vector ? layer_norm_kernel<T, 2, true> : layer_norm_kernel<T, 2, false>, grid);
-    case 4: return go(vector ? layer_norm_kernel<T, 4, true> : layer_norm_kernel<T, 4, false>, grid);
-    default: return go(vector ? layer_norm_kernel<T, 8, true> : layer_norm_kernel<T, 8, false>, grid);
-  }
-}
-
-// Lets a kernel have the shared memory that its block's sums take (once per device).
+// Lets a kernel have `bytes` of dynamic shared memory (once per device).
 template <auto KERNEL>
-static qb_status norm_room() {
+static qb_status norm_room(size_t bytes) {
   static std::atomic<bool> set[64] = {};
   int dev = 0;
   QB_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !set[dev].load(std::memory_order_acquire)) {
-    QB_CUDA_TRY(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kNormElements * 32 * 8 * 4));
+    QB_CUDA_TRY(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
     if (dev >= 0 && dev < 64) set[dev].store(true, std::memory_order_release);
   }
   return QB_OK;
 }
+
+template <class T, int WPR, bool VECTOR>
+static qb_status launch_norm_form(const T* x, T* y, const NormArgs& a, int sms, cudaStream_t stream) {
+  constexpr size_t smem = VECTOR ? NormRing<T, WPR, 1>::kBytes : 0;
+  constexpr int kRows = 8 / WPR;
+  qb_status st = norm_room<layer_norm_kernel<T, WPR, VECTOR>>(smem);
+  if (st != QB_OK) return st;
+  QB_CUDA_TRY(launch_kernel(layer_norm_kernel<T, WPR, VECTOR>, (unsigned)std::min<int64_t>((a.M + kRows - 1) / kRows, (int64_t)sms * 2), kNormThreads, smem, stream,
+                            1, false, x, y, a));
+  return QB_OK;
+}
+template <class T>
+static qb_status launch_norm(const void* x_data, void* y_data, const NormArgs& a, int sms, cudaStream_t stream) {
+  const T* const x = static_cast<const T*>(x_data);
+  T* const y = static_cast<T*>(y_data);
+  if (a.D > kNormMostHeld) {
+    QB_CUDA_TRY(launch_kernel(layer_norm_long_kernel<T>, (unsigned)std::min<int64_t>(a.M, (int64_t)sms * 8), kNormThreads, 0, stream, 1, false, x, y, a));
+    return QB_OK;
+  }
+  const bool vector = a.D % Vec16<T>::N == 0 && aligned16(x) && aligned16(y);
+  switch (norm_warps(a.D)) {
+    case 1: return vector ? launch_norm_form<T, 1, true>(x, y, a, sms, stream) : launch_norm_form<T, 1, false>(x, y, a, sms, stream);
+    case 2: return vector ? launch_norm_form<T, 2, true>(x, y, a, sms, stream) : launch_norm_form<T, 2, false>(x, y, a, sms, stream);
+    case 4: return vector ? launch_norm_form<T, 4, true>(x, y, a, sms, stream) : launch_norm_form<T, 4, false>(x, y, a, sms, stream);
+    default: return vector ? launch_norm_form<T, 8, true>(x, y, a, sms, stream) : launch_norm_form<T, 8, false>(x, y, a, sms, stream);
+  }
+}
+
+template <class T, int WPR, bool VECTOR>
+static qb_status launch_norm_backward_form(const T* grad_y, const T* x, T* grad_x, const NormBackArgs& a, int blocks, cudaStream_t stream) {
+  constexpr size_t sums = WPR < 8 ? (size_t)2 * kNormElements * 32 * 8 * 4 : 0;
+  constexpr size_t smem = VECTOR ? std::max(sums, (size_t)NormRing<T, WPR, 2>::kBytes) : sums;
+  qb_status st = norm_room<layer_norm_backward_kernel<T, WPR, VECTOR>>(smem);
+  if (st != QB_OK) return st;
+  QB_CUDA_TRY(launch_kernel(layer_norm_backward_kernel<T, WPR, VECTOR>, (unsigned)blocks, kNormThreads, smem, stream, 1, false, grad_y, x, grad_x, a));
+  return QB_OK;
+}
 // V: receives the vector length, which the order of the sums goes by.
 template <class T>
-static qb_status launch_norm_backward(const void* grad_y, const void* x, void* grad_x, const NormBackArgs& a, int blocks, int* V, cudaStream_t stream) {
-  const bool vector = a.D % Vec16<T>::N == 0 && aligned16(x) && aligned16(grad_y) && aligned16(grad_x);
-  const int warps = norm_warps(a.D);
-  *V = vector ? Vec16<T>::N : 1;
-  const size_t smem = warps < 8 && a.D <= kNormMostHeld ? (size_t)(8 / warps) * norm_sums(a.D) * 4 : 0;  // 64 KB
-  const auto with = [&](auto kernel, auto room) {
-    qb_status st = room();
-    if (st != QB_OK) return st;
-    QB_CUDA_TRY(launch_kernel(kernel, (unsigned)blocks, kNormThreads, smem, stream, 1, false, static_cast<const T*>(grad_y), static_cast<const T*>(x),
-                              static_cast<T*>(grad_x), a));
-    return (qb_status)QB_OK;
-  };
-  if (a.D > kNormMostHeld) return with(layer_norm_long_backward_kernel<T>, [] { return (qb_status)QB_OK; });
-#define QB_NORM_BACKWARD(W)                                                                                                                    \
-  return vector ? with(layer_norm_backward_kernel<T, W, true>, norm_room<layer_norm_backward_kernel<T, W, true>>)                               \
-                : with(layer_norm_backward_kernel<T, W, false>, norm_room<layer_norm_backward_kernel<T, W, false>>)
-  switch (warps) {
-    case 1: QB_NORM_BACKWARD(1);
-    case 2: QB_NORM_BACKWARD(2);
-    case 4: QB_NORM_BACKWARD(4);
-    default: QB_NORM_BACKWARD(8);
+static qb_status launch_norm_backward(const void* grad_y, const void* x_data, void* grad_x, const NormBackArgs& a, int blocks, int* V, cudaStream_t stream) {
+  const T *const gy = static_cast<const T*>(grad_y), *const x = static_cast<const T*>(x_data);
+  T* const gx = static_cast<T*>(grad_x);
+  if (a.D > kNormMostHeld) {
+    QB_CUDA_TRY(launch_kernel(layer_norm_long_backward_kernel<T>, (unsigned)blocks, kNormThreads, 0, stream, 1, false, gy, x, gx, a));
+    return QB_OK;
   }
-#undef QB_NORM_BACKWARD
+  const bool vector = a.D % Vec16<T>::N == 0 && aligned16(x) && aligned16(gy) && aligned16(gx);
+  *V = vector ? Vec16<T>::N : 1;
+  switch (norm_warps(a.D)) {
+    case 1: return vector ? launch_norm_backward_form<T, 1, true>(gy, x, gx, a, blocks, stream) : launch_norm_backward_form<T, 1, false>(gy, x, gx, a, blocks, stream);
+    case 2: return vector ? launch_norm_backward_form<T, 2, true>(gy, x, gx, a, blocks, stream) : launch_norm_backward_form<T, 2, false>(gy, x, gx, a, blocks, stream);
+    case 4: return vector ? launch_norm_backward_form<T, 4, true>(gy, x, gx, a, blocks, stream) : launch_norm_backward_form<T, 4, false>(gy, x, gx, a, blocks, stream);
+    default: return vector ? launch_norm_backward_form<T, 8, true>(gy, x, gx, a, blocks, stream) : launch_norm_backward_form<T, 8, false>(gy, x, gx, a, blocks, stream);
+  }
 }
 
 static qb_status check_norm(const char* what, bool pointers, int type, int64_t M, int64_t D) {

@@ -502,8 +502,8 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           if (gp.pre_codes) {  // z in 8 bits
 #pragma unroll
             for (int j = 0; j < kCols; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
-            const CheckpointScale cs(top);
-            if (mine && (c0 & 32) == 0) gp.pre_scales[block] = cs.scale;
+            const CheckpointCodes cs(top);
+            if (mine && (c0 & 32) == 0) gp.pre_scales[block] = checkpoint_scale(top);
             uint4 c[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {

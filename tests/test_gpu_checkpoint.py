@@ -154,6 +154,25 @@ def test_zeros_tiny_and_not_finite():
 
 
 @pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("K", [64, 100, 1023])
+def test_whole_range_of_a_type(K, kind):
+    """Blocks at every size that the type has, from its least normal number (fp32, bfloat16: from 2^-99) to its largest, with exact halves."""
+    t, M = TYPES[kind], 300
+    f = torch.finfo(t)
+    low = max(f.smallest_normal, 2.0**-99)
+    g = torch.Generator(device="cuda").manual_seed(K)
+    size = torch.exp2(torch.linspace(torch.log2(torch.tensor(low)).item() + 1, torch.log2(torch.tensor(f.max)).item(), M, dtype=torch.float64)).cuda()[:, None]
+    x = (torch.rand(M, K, device="cuda", generator=g, dtype=torch.float64) * 2 - 1) * size
+    x[:, ::64] = size
+    x[:, 1::5] = size.to(t).double() / 2
+    x = x.clamp(-f.max, f.max).to(t)
+    codes, scales = qb.checkpoint(x)
+    want, _ = codes64(x)
+    assert torch.equal(codes, want)
+    assert qb.restore((codes, scales), torch.float32).isfinite().all()
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
 @pytest.mark.parametrize("shift", [1, 3])
 def test_any_alignment(kind, shift):
     t, M, K = TYPES[kind], 37, 192
