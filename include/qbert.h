@@ -554,7 +554,7 @@ qb_status qb_gelu_backward(const void* grad_y, int type, const void* pre, const 
  *   pre_codes, pre_scales  as above with K = N (qb_linear), K (qb_linear_grad_x), or both NULL; codes of any alignment
  * x, w and grad_y are 16-byte aligned, the others aligned to their elements.  residual may be y (grad_x).  With a pre-activation
  * qb_linear_grad_x takes no residual.  grad_w or grad_bias may be NULL (without grad_w x may be too).  M, N and K up to QB_MAX_MN, any size.
- * The sums' order does not change from call to call with the same sizes and workspace size.
+ * The sums' order does not change from call to call with the same sizes, workspace size and outputs.
  * The workspace is 16-byte aligned; qb_linear_workspace_bytes(M, N, K) serves the three calls (0 on invalid arguments).  Less will do,
  * except for grad_bias and for tensors whose rows are no multiple of 8 elements, which need their part (else QB_ERR_WORKSPACE); more lets a
  * product of few tiles over a long contraction be summed in more parts side by side.

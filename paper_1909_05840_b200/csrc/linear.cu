@@ -56,7 +56,7 @@ struct LinearParams {
   int32_t split_tiles;   // tiles of one split of K (split s writes rows s * M .. of out, fp32)
   int32_t split_blocks;  // K blocks of 64 per split, even where there are several
   int32_t k_blocks;      // of all splits
-  int32_t run_blocks;    // K blocks that one accumulator sums; even where a split has several such runs (fp32 out), which are added up in out
+  int32_t run_blocks;    // K blocks that one accumulator sums; even where there are several such runs (fp32 out), which registers add up
   int32_t tma_store;     // 1: rows of out are 16-byte aligned
   int32_t vector;        // 1: rows of side and of pre are 32-byte aligned
   int32_t vector_codes;  // 1: rows of the codes are
@@ -161,6 +161,16 @@ __device__ __forceinline__ void add2(float* z, float a, float b) {
   const float2 f = ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(z[0], z[1]), ptx::pack_f32x2(a, b)));
   z[0] = f.x;
   z[1] = f.y;
+}
+
+// Eight columns of an accumulator added to z.
+__device__ __forceinline__ void add_accumulator(uint32_t taddr, float* z) {
+  uint32_t w[8];
+  ptx::tmem_ld_32x32b_x8(taddr, w);
+  ptx::tmem_ld_wait();
+  ptx::tmem_ld_regs_ready(w);
+#pragma unroll
+  for (int c = 0; c < 8; c += 2) add2(z + c, __uint_as_float(w[c]), __uint_as_float(w[c + 1]));
 }
 
 // 32 bytes of a row: whole sectors, where 16 bytes a lane would touch each of them twice.
@@ -385,17 +395,15 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         else ptx::mbar_arrive(bar);
       }
     };
-    int it = 0, run = 0;
-    for (int t = group; t < gp.tiles; ++it) {
-      const int a = it & 1;
+    int it = 0, b = 0;  // runs; the half of the bias buffer
+    for (int t = group; t < gp.tiles; t += groups, b ^= 1) {
       const LinTile<BT, CG> tile(gp, t);
-      const bool add = OUT32 && run > 0;  // to the runs before, which brought bias and residual
-      const float* const bias = add ? nullptr : gp.bias;
-      const void* const side = add ? nullptr : gp.side;
+      const float* const bias = gp.bias;
+      const void* const side = gp.side;
       int m0 = tile.m0 + (int)rank * 128 + quarter * 32, n0 = tile.n0;
       int chunks = m0 < gp.M ? max(0, min(tile.width / kCols, (gp.N - n0 + kCols - 1) / kCols)) : 0;
       asm volatile("" : "+r"(m0), "+r"(n0), "+r"(chunks));  // formed before the wait, not behind it
-      if (e < BT) bias_tile[a * 256 + e] = bias && n0 + e < gp.N ? bias[n0 + e] : 0.0f;
+      if (e < BT) bias_tile[b * 256 + e] = bias && n0 + e < gp.N ? bias[n0 + e] : 0.0f;
       const int rows = min(32, gp.M - m0);
       const bool mine = lane < rows;
       // The chunk's part of the tensor beside the product (residual, pre-activation, codes of it): the lane's row, fetched while the
@@ -416,60 +424,50 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           }
         }
       };
-      if (part < chunks) fetch(part * kCols);
-      const bool ok = ew != 0 || wait_barrier_warp(acc_full(a), (uint32_t)(it >> 1) & 1u, abort_flag);
-      if (lin_epilogue_sync_or(!ok)) {  // publishes the bias, and all warps give up together
-        timed_out = true;
-        where = (3 << 16) | a;
-        break;
-      }
-      ptx::tcgen05_fence_after_sync();
-      const uint32_t acc = lanes + (uint32_t)(a * BT);
-      if (part >= chunks) arrive(acc_empty(a));
-#pragma unroll 1
-      for (int i = part; i < chunks; i += 4) {
+      // Waits for the accumulator of run `it`.  False when a wait has run out, for all warps together.
+      auto wait_run = [&]() {
+        const bool ok = ew != 0 || wait_barrier_warp(acc_full(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag);
+        if (lin_epilogue_sync_or(!ok)) {  // publishes the bias too
+          timed_out = true;
+          where = (3 << 16) | (it & 1);
+          return false;
+        }
+        ptx::tcgen05_fence_after_sync();
+        return true;
+      };
+      auto read = [&](int column, float* z) {
+        uint32_t w[kCols];
+        const uint32_t from = lanes + (uint32_t)((it & 1) * BT + column);
+        if constexpr (OUT32) ptx::tmem_ld_32x32b_x16(from, w);
+        else ptx::tmem_ld_32x32b_x32(from, w);
+        ptx::tmem_ld_wait();
+        ptx::tmem_ld_regs_ready(w);
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) z[j] = __uint_as_float(w[j]);
+      };
+      auto add_bias = [&](int column, float* z) {
+        if (MODE == kSlope || !bias) return;
+        const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + b * 256 + column);
+#pragma unroll
+        for (int j = 0; j < kCols / 4; ++j) {
+          const float4 q = b4[j];
+          add2(z + 4 * j, q.x, q.y);
+          add2(z + 4 * j + 2, q.z, q.w);
+        }
+      };
+      // What becomes of the chunk's z (the product and the bias), from there to memory.  top: of the other chunk of its block.
+      auto emit = [&](int i, float* v, float top) {
         const int c0 = i * kCols, cols = min(kCols, gp.N - n0 - c0);
         const int64_t corner = (int64_t)m0 * gp.N + n0 + c0;  // of the chunk, in elements
         const int64_t block = (int64_t)(m0 + lane) * checkpoint_blocks(gp.N) + (n0 + c0) / kCheckpointBlock;  // the row's, in scales
-        const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + a * 256 + c0);
-        float v[kCols];
-        // z = product + bias of this warp's chunk or its neighbour's
-        auto read = [&](int column, const float4* b, float* z) {
-          uint32_t w[kCols];
-          if constexpr (OUT32) ptx::tmem_ld_32x32b_x16(acc + (uint32_t)column, w);
-          else ptx::tmem_ld_32x32b_x32(acc + (uint32_t)column, w);
-          ptx::tmem_ld_wait();
-          ptx::tmem_ld_regs_ready(w);
-#pragma unroll
-          for (int j = 0; j < kCols; ++j) z[j] = __uint_as_float(w[j]);
-          if (MODE != kSlope && bias) {
-#pragma unroll
-            for (int j = 0; j < kCols / 4; ++j) {
-              const float4 q = b[j];
-              add2(z + 4 * j, q.x, q.y);
-              add2(z + 4 * j + 2, q.z, q.w);
-            }
-          }
-        };
-        float scale = 1.0f, top = 0.0f;
+        float scale = 1.0f;
         if (MODE == kSlope && gp.codes && mine) scale = gp.scales[block];
-        if constexpr (!OUT32 && MODE != kSlope) {
-          if (gp.pre_codes) {  // a block is this chunk and its neighbour
-            read(c0 ^ 32, reinterpret_cast<const float4*>(bias_tile + a * 256 + (c0 ^ 32)), v);
-#pragma unroll
-            for (int j = 0; j < kCols; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
-          }
-        }
-        read(c0, b4, v);
-        if (i + 4 >= chunks) arrive(acc_empty(a));
-        bool waited = false;  // for the chunk before to have left the buffer, and for what is added to to have been written
+        if constexpr (OUT32) fetch(c0);
+        bool waited = false;  // for the chunk before to have left the buffer
         auto buffer_free = [&]() {
           if (waited) return;
           waited = true;
-          if (lane == 0) {
-            if (add && i == part) ptx::tma_store_wait0();
-            else ptx::tma_store_wait_read0();
-          }
+          if (lane == 0) ptx::tma_store_wait_read0();
           __syncwarp();
         };
         // rows of any alignment come by way of the buffer
@@ -584,7 +582,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             }
           }
         }
-        if (i + 4 < chunks) fetch(c0 + 4 * kCols);
+        if (!OUT32 && i + 4 < chunks) fetch(c0 + 4 * kCols);
         buffer_free();
 #pragma unroll
         for (int k = 0; k < 4; ++k) {  // 16 bytes of the row at a time
@@ -599,8 +597,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           ptx::fence_proxy_async_smem();  // every lane: its own stores
           __syncwarp();
           if (lane == 0) {
-            if (add) ptx::tma_add_3d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0, tile.split);
-            else ptx::tma_store_3d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0, tile.split);
+            ptx::tma_store_3d(&gp.tmy, ptx::smem_u32(buf), n0 + c0, m0, tile.split);
             ptx::tma_store_commit();
           }
         } else if constexpr (OUT32) {  // two rows at a time, the lanes on consecutive values of them
@@ -608,10 +605,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           const int c = lane & 15;
           if (c < cols) {
             float* const to = static_cast<float*>(gp.out) + first_row * gp.N + corner + c;
-            for (int r = lane >> 4; r < rows; r += 2) {
-              const float f = reinterpret_cast<const float*>(staged(buf, r, c >> 2))[c & 3];
-              to[(int64_t)r * gp.N] = add ? to[(int64_t)r * gp.N] + f : f;
-            }
+            for (int r = lane >> 4; r < rows; r += 2) to[(int64_t)r * gp.N] = reinterpret_cast<const float*>(staged(buf, r, c >> 2))[c & 3];
           }
           __syncwarp();
         } else {
@@ -619,12 +613,63 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           send_rows16(buf, static_cast<uint16_t*>(gp.out) + first_row * gp.N + corner, gp.N, rows, cols, lane);
           __syncwarp();
         }
+      };
+      if (!OUT32 && part < chunks) fetch(part * kCols);
+      bool ok;
+      if constexpr (OUT32) {  // the runs before the last are added up in registers, and to the last one where it lies
+        constexpr int kChunks = BT / kCols / 4;  // of a warp
+        float sums[kChunks][kCols] = {};
+        int run = tile.k0;
+        while (true) {
+          ok = wait_run();
+          if (!ok || run + gp.run_blocks >= tile.k1) break;
+#pragma unroll
+          for (int j = 0; j < kChunks; ++j) {
+            if (part + 4 * j < chunks) {
+#pragma unroll
+              for (int h = 0; h < kCols; h += 8) {
+                add_accumulator(lanes + (uint32_t)((it & 1) * BT + (part + 4 * j) * kCols + h), sums[j] + h);
+              }
+            }
+          }
+          arrive(acc_empty(it & 1));
+          ++it;
+          run += gp.run_blocks;
+        }
+        if (ok && run > tile.k0) {
+#pragma unroll
+          for (int j = 0; j < kChunks; ++j) {
+            if (part + 4 * j < chunks) {
+#pragma unroll
+              for (int h = 0; h < kCols; h += 8) {
+                const uint32_t at = lanes + (uint32_t)((it & 1) * BT + (part + 4 * j) * kCols + h);
+                add_accumulator(at, sums[j] + h);
+                ptx::tmem_st_32x32b_x8(at, sums[j] + h);
+              }
+            }
+          }
+          ptx::tmem_st_wait();
+        }
+      } else {
+        ok = wait_run();
       }
-      run += gp.run_blocks;
-      if (tile.k0 + run >= tile.k1) {
-        t += groups;
-        run = 0;
+      if (!ok) break;
+      if (part >= chunks) arrive(acc_empty(it & 1));
+#pragma unroll 1
+      for (int i = part; i < chunks; i += 4) {
+        float v[kCols], top = 0.0f;
+        if (!OUT32 && MODE != kSlope && gp.pre_codes) {  // a block of codes is this chunk and its neighbour
+          read((i ^ 1) * kCols, v);
+          add_bias((i ^ 1) * kCols, v);
+#pragma unroll
+          for (int j = 0; j < kCols; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
+        }
+        read(i * kCols, v);
+        if (i + 4 >= chunks) arrive(acc_empty(it & 1));
+        add_bias(i * kCols, v);
+        emit(i, v, top);
       }
+      ++it;
     }
     if (lane == 0) ptx::tma_store_wait_read0();  // the buffers are in use until then
   }
@@ -753,10 +798,14 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* from, uin
 }
 
 // Sums of the columns of g [M][N] over its rows, first over runs of rows into parts [runs][N], then over the runs, in their order.
-template <bool VECTOR>
+// UNDER: the kernel before this one on the stream is of this call, the product or the join of its parts, which neither writes what is read
+// here nor touches the parts.  Its blocks let this kernel's begin once all kernels before it are done and their results visible
+// (pdl_begin), so that these are read without waiting for it, on SMs that it leaves (24,576 x 4,096, K = 1,024: grad_w 143 us, with
+// grad_bias 151, one after the other 181); one block waits at its end, so that the kernels that follow find both done.
+template <bool VECTOR, bool UNDER>
 __global__ void __launch_bounds__(256) column_parts_kernel(const uint16_t* g, int64_t M, int32_t N, int64_t run, int col_blocks, int half_type, float* parts) {
   __shared__ float sums[8][256];
-  pdl_begin();
+  if constexpr (!UNDER) pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t which = blockIdx.x / col_blocks, first = which * run, last = min(first + run, M);
   const int n0 = ((int)blockIdx.x - (int)which * col_blocks) * 256;
@@ -796,22 +845,35 @@ __global__ void __launch_bounds__(256) column_parts_kernel(const uint16_t* g, in
     for (int w = 1; w < 8; ++w) t += sums[w][threadIdx.x];
     parts[which * N + c] = t;
   }
+  if (UNDER && blockIdx.x == 0) pdl_begin();  // (a block that waits keeps its place from those that have not begun)
 }
+// 32 columns a block, eight groups of runs side by side, joined in their order.
 __global__ void __launch_bounds__(256) column_join_kernel(const float* parts, int runs, int32_t N, float* sums) {
+  __shared__ float joined[8][32];
   pdl_begin();
-  const int c = (int)(blockIdx.x * 256 + threadIdx.x);
-  if (c >= N) return;
-  float t = parts[c];
-  for (int r = 1; r < runs; ++r) t += parts[(int64_t)r * N + c];
-  sums[c] = t;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (int)blockIdx.x * 32 + lane;
+  const int group = (runs + 7) / 8, last = min((warp + 1) * group, runs);
+  float t = 0.0f;
+  if (c < N) {
+#pragma unroll 8
+    for (int r = warp * group; r < last; ++r) t += parts[(int64_t)r * N + c];
+  }
+  joined[warp][lane] = t;
+  __syncthreads();
+  if (warp == 0 && c < N) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) t += joined[w][lane];
+    sums[c] = t;
+  }
 }
 
 static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 static int64_t lin_up(int64_t n, int64_t m) { return (n + m - 1) / m; }
+
 // The tensor cores cut an accumulator off at its last place at each addition of 16 products, always towards zero: the error grows
-// with their number (24,576 products of random signs: 2.8e-5 of the result, 4,096: a sixth of it).  fp32 outputs are summed in runs of
-// this many K blocks, which are rounded to nearest as they are added up.
-constexpr int kLinRunBlocks = 64;
+// with their number (24,576 products of random signs: 2.8e-5 of the result).  fp32 outputs are summed in runs of this many K blocks, which
+// the epilogue's registers add up, rounded to nearest: the error is then that of fp32 products.
+constexpr int kLinRunBlocks = 16;
 constexpr size_t kLinScratchOff = 1024;  // of what calls keep in the workspace besides its header
 
 // The form of a product: CTAs per tile, columns, for pairs how many tiles are whole, and splits of K.
@@ -908,10 +970,9 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   qb_status st;
   if ((st = padded(&a, &a_pitch, &scratch, sms, what, stream)) != QB_OK) return st;
   if ((st = padded(&b, &b_pitch, &scratch, sms, what, stream)) != QB_OK) return st;
-  // a 16-bit output is summed in one run up to 2^16 products, what passes through GELU in fp32 up to kLinRunBlocks
+  // a 16-bit output is summed in one run up to 2^16 products (the sums' error is then below a tenth of its rounding)
   const int64_t blocks = lin_up(K, 64);
-  const bool parts_for_sums = tail.out_type == QB_F32 ? tail.mode == kGelu && blocks > kLinRunBlocks : blocks > 1024;
-  const LinearChoice choice = choose_linear(M, N, K, sms, pre_codes ? 0 : scratch.left, parts_for_sums);
+  const LinearChoice choice = choose_linear(M, N, K, sms, pre_codes ? 0 : scratch.left, tail.out_type != QB_F32 && blocks > 1024);
   const int cg = choice.cg, bt = choice.bt;
   const bool split = choice.splits > 1;
   const bool out32 = split || tail.out_type == QB_F32;
@@ -948,13 +1009,14 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   gp.split_tiles_inv = quick_inverse((uint32_t)gp.split_tiles);
   gp.split_blocks = choice.split_blocks;
   gp.k_blocks = (int32_t)blocks;
-  gp.run_blocks = split || (out32 && tail.mode == kPlain) ? kLinRunBlocks : (int32_t)blocks;
+  gp.run_blocks = out32 ? kLinRunBlocks : (int32_t)blocks;
   gp.idesc = lin_idesc(half_type, a.mn, b.mn, 128 * cg);
   const int mode = split ? kPlain : tail.mode;
   if (cg == 2) st = launch_linear<256, 2>(gp, out32, mode, half_type, sms, stream);
   else if (bt == 128) st = launch_linear<128, 1>(gp, out32, mode, half_type, sms, stream);
   else st = launch_linear<64, 1>(gp, out32, mode, half_type, sms, stream);
-  if (st != QB_OK || !split) return st;
+  if (st != QB_OK) return st;
+  if (!split) return QB_OK;
   const bool vector = N % 4 == 0;
   QB_CUDA_TRY(launch_kernel(vector ? linear_join_kernel<4> : linear_join_kernel<1>, (unsigned)std::min<int64_t>(lin_up(M * N, vector ? 1024 : 256), (int64_t)sms * 8), 256, 0,
                             stream, 1, false, parts, choice.splits, M * N, (int)N, tail));
@@ -973,6 +1035,10 @@ static qb_status check_linear(const char* what, const void* const (&needed)[4], 
   set_last_error("%s: invalid argument (M=%lld N=%lld K=%lld type %d, output type %d)", what, (long long)M, (long long)N, (long long)K, type, out_type);
   return QB_ERR_INVALID;
 }
+static qb_status no_room_for_bias() {
+  set_last_error("qb_linear_grad_w: the workspace is too small for the bias's gradient (qb_linear_workspace_bytes)");
+  return QB_ERR_WORKSPACE;
+}
 static qb_status check_linear_ws(const char* what, const void* ws, size_t ws_bytes) {
   if (ws && aligned16(ws) && ws_bytes >= kWsMinBytes) return QB_OK;
   set_last_error("%s: workspace null, not 16-byte aligned or too small", what);
@@ -985,7 +1051,7 @@ extern "C" size_t qb_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   using namespace qb;
   if (impossible_linear(M, N, K)) return 0;
   const size_t pads = pad_bytes(M, K) + pad_bytes(N, K) + pad_bytes(M, N);
-  const size_t sums = ((size_t)column_runs(M, N, 160) * (size_t)N * 4 + 255) / 256 * 256;
+  const size_t sums = ((size_t)column_runs(M, N, kRingMaxCtas) * (size_t)N * 4 + 255) / 256 * 256;
   // parts of a split product: where its output is small against the device
   const int64_t outs[3] = {M * N, M * K, N * K};
   size_t parts = 0;
@@ -1064,20 +1130,20 @@ extern "C" qb_status qb_linear_grad_w(const void* grad_y, const void* x, int typ
   if ((st = require_sm100(&sms)) != QB_OK) return st;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   LinearScratch scratch(ws, ws_bytes);
-  if (grad_bias) {
-    const int64_t run = lin_up(M, column_runs(M, N, sms)), runs = lin_up(M, run);
-    float* const parts = static_cast<float*>(scratch.take((size_t)runs * (size_t)N * 4));
-    if (!parts) {
-      set_last_error("qb_linear_grad_w: the workspace is too small for the bias's gradient (qb_linear_workspace_bytes)");
-      return QB_ERR_WORKSPACE;
-    }
-    auto sum = N % 8 == 0 ? column_parts_kernel<true> : column_parts_kernel<false>;
+  const int64_t run = lin_up(M, column_runs(M, N, sms)), runs = lin_up(M, run);
+  float* const parts = grad_bias ? static_cast<float*>(scratch.take((size_t)runs * (size_t)N * 4)) : nullptr;
+  if (grad_bias && !parts) return no_room_for_bias();
+  if (grad_w) {
+    const LinearTail tail = {nullptr, nullptr, nullptr, nullptr, grad_w, nullptr, kPlain, out_type, type};
+    if ((st = run_linear(what, {grad_y, M, N, true}, {x, M, K, true}, N, K, M, tail, nullptr, nullptr, ws, scratch, sms, stream)) != QB_OK) return st;
+  }
+  if (grad_bias) {  // behind the product, under which it runs where that leaves SMs
     const int col_blocks = (int)lin_up(N, 256);
+    auto sum = N % 8 == 0 ? (grad_w ? column_parts_kernel<true, true> : column_parts_kernel<true, false>)
+                          : (grad_w ? column_parts_kernel<false, true> : column_parts_kernel<false, false>);
     QB_CUDA_TRY(launch_kernel(sum, (unsigned)(col_blocks * runs), 256, 0, stream, 1, false, static_cast<const uint16_t*>(grad_y), M, (int32_t)N, run, col_blocks,
                               (int)(type == QB_F16), parts));
-    QB_CUDA_TRY(launch_kernel(column_join_kernel, (unsigned)col_blocks, 256, 0, stream, 1, false, parts, (int)runs, (int32_t)N, grad_bias));
+    QB_CUDA_TRY(launch_kernel(column_join_kernel, (unsigned)lin_up(N, 32), 256, 0, stream, 1, false, parts, (int)runs, (int32_t)N, grad_bias));
   }
-  if (!grad_w) return QB_OK;
-  const LinearTail tail = {nullptr, nullptr, nullptr, nullptr, grad_w, nullptr, kPlain, out_type, type};
-  return run_linear(what, {grad_y, M, N, true}, {x, M, K, true}, N, K, M, tail, nullptr, nullptr, ws, scratch, sms, stream);
+  return QB_OK;
 }

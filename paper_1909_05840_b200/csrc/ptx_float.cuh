@@ -69,16 +69,6 @@ __device__ __forceinline__ void tma_store_3d(const void* tmap, uint32_t src_smem
                : "memory");
 }
 
-// The same, adding to what the tensor holds (fp32; each addition rounded to nearest even, subnormal numbers count as zeros).
-__device__ __forceinline__ void tma_add_3d(const void* tmap, uint32_t src_smem, int32_t x, int32_t y, int32_t z) {
-  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
-                   reinterpret_cast<uint64_t>(tmap)),
-               "r"(src_smem), "r"(x), "r"(y), "r"(z)
-               : "memory");
-}
-// Wait until this thread's bulk stores have been written.
-__device__ __forceinline__ void tma_store_wait0() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
 // D[tmem] (+)= (A[smem] * scale_a) * (B[smem] * scale_b), 8-bit floating point operands, fp32 accumulators; one 2^(e - 127)
 // per row of A and of B for the instruction's 32 elements of K, its byte e taken from tensor memory (the byte of the
 // 32-bit words at scale_a / scale_b that the instruction descriptor names).
@@ -118,6 +108,24 @@ __device__ __forceinline__ void tmem_ld_regs_ready(uint32_t (&r)[16]) {
   asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
                     "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
+
+__device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld_regs_ready(uint32_t (&r)[8]) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])::"memory");
+}
+
+// Eight columns of the warp's 32 lanes back to tensor memory.  Its own later loads see them after tmem_st_wait.
+__device__ __forceinline__ void tmem_st_32x32b_x8(uint32_t taddr, const float* f) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]),
+               "f"(f[5]), "f"(f[6]), "f"(f[7]), "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // D[tmem] (+)= A[smem] * B[smem] over a pair of CTAs, 16-bit floating point operands (both of one type), fp32 accumulators.
 __device__ __forceinline__ void mma_f16_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,

@@ -139,14 +139,15 @@ def test_grad_w(M, N, K, out, kind, ws):
     dw, db = qb.linear_grad_w(dy, x, ws, out_dtype=o)
     within(dw, want, tol)
     # the chain of a column: rows of a warp's run, the warps, the runs
-    assert ((db.double() - dy.double().sum(0)).abs() <= 1.01 * U * (M / 100 + 1300) * dy.double().abs().sum(0)).all()
+    db_tol = 1.01 * U * (M / 100 + 1300) * dy.double().abs().sum(0)
+    assert ((db.double() - dy.double().sum(0)).abs() <= db_tol).all()
     again, db2 = qb.linear_grad_w(dy, x, ws, out_dtype=o)
     assert torch.equal(again, dw) and torch.equal(db2, db)
     only, none = qb.linear_grad_w(dy, x, ws, out_dtype=o, needs=(True, False))
     assert none is None
     within(only, want, tol)
     none, db3 = qb.linear_grad_w(dy, x, ws, needs=(False, True))
-    assert none is None and torch.equal(db3, db)
+    assert none is None and ((db3.double() - dy.double().sum(0)).abs() <= db_tol).all()  # (another order of the same sums)
 
 
 def test_long_contraction(ws):
