@@ -561,12 +561,13 @@ qb_status qb_gelu_backward(const void* grad_y, int type, const void* pre, const 
  */
 size_t qb_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 /*
- * Columns of the tiles of a product of these sizes and workspace (out [M][N], contraction over K, nothing padded): 64 or 128 (rows of 128),
- * or 256 (rows of 256, by pairs of CTAs).  `half_tiles` (host, or NULL) receives how many of them are cut to 128 columns, `splits` (host, or
- * NULL) into how many parts K is cut (a pre-activation in 8 bits keeps it whole).  Host arithmetic, no GPU work; it lets a test see which
- * form serves a shape.  0 on invalid arguments.
+ * Columns of the tiles of a product of these sizes and workspace (out [M][N], contraction over K, nothing padded): 64, 128 or 256.  `rows`
+ * (host, or NULL) receives their rows: 128, or 256 (by pairs of CTAs); `half_tiles` (host, or NULL) how many of them are cut to 128
+ * columns; `splits` (host, or NULL) into how many parts K is cut (a pre-activation in 8 bits keeps it whole).  Host arithmetic, no GPU work; it lets a
+ * test see which form serves a shape.  0 on invalid arguments.
  */
-int32_t qb_linear_tile_columns(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int32_t* half_tiles /*host*/, int32_t* splits /*host*/);
+int32_t qb_linear_tile_columns(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int32_t* rows /*host*/, int32_t* half_tiles /*host*/,
+                               int32_t* splits /*host*/);
 qb_status qb_linear(const void* x, const void* w, int type, const float* bias, int activation, const void* residual, int64_t M, int64_t N,
                     int64_t K, int out_type, void* y, void* pre, int8_t* pre_codes, float* pre_scales, void* ws, size_t ws_bytes,
                     void* cuda_stream);

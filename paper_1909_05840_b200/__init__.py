@@ -185,7 +185,7 @@ def lib() -> ctypes.CDLL:
     L.qb_gelu_backward.restype = i32
     L.qb_linear_workspace_bytes.argtypes = [i64, i64, i64]
     L.qb_linear_workspace_bytes.restype = sz
-    L.qb_linear_tile_columns.argtypes = [i64, i64, i64, sz, ctypes.POINTER(i32), ctypes.POINTER(i32)]
+    L.qb_linear_tile_columns.argtypes = [i64, i64, i64, sz, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32)]
     L.qb_linear_tile_columns.restype = i32
     L.qb_linear.argtypes = [vp, vp, ctypes.c_int, vp, ctypes.c_int, vp, i64, i64, i64, ctypes.c_int, vp, vp, vp, vp, vp, sz, vp]
     L.qb_linear.restype = i32
@@ -656,10 +656,10 @@ def linear_workspace_bytes(M: int, N: int, K: int) -> int:
 
 
 def linear_form(M: int, N: int, K: int, ws_bytes: int = 0) -> tuple:
-    """``qb_linear_tile_columns``: (columns of a tile, tiles cut to half of them, parts of K) of a product [M,N] over K."""
-    halves, splits = ctypes.c_int32(0), ctypes.c_int32(0)
-    columns = lib().qb_linear_tile_columns(M, N, K, ws_bytes, ctypes.byref(halves), ctypes.byref(splits))
-    return int(columns), halves.value, splits.value
+    """``qb_linear_tile_columns``: (rows of a tile, its columns, tiles cut to half of them, parts of K) of a product [M,N] over K."""
+    rows, halves, splits = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_int32(0)
+    columns = lib().qb_linear_tile_columns(M, N, K, ws_bytes, ctypes.byref(rows), ctypes.byref(halves), ctypes.byref(splits))
+    return rows.value, int(columns), halves.value, splits.value
 
 
 def linear_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:

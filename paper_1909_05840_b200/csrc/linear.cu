@@ -72,7 +72,7 @@ struct LinCfg {
   static constexpr int kABytes = 2 * 128 * 128;          // 128 rows, two K blocks of 128 bytes
   static constexpr int kBBytes = 2 * (BT / CG) * 128;
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = BT == 64 ? 4 : 3;
+  static constexpr int kStages = BT / CG == 64 ? 4 : 3;
   static constexpr int kOutBytes = kLinEpilogueWarps * 2048;
   static constexpr int kBarBytes = 256;
   static constexpr int kBiasBytes = 2 * 256 * 4;
@@ -246,6 +246,11 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     ptx::mbar_init(drain_bar, 1);
     *abort_flag = 0;
     ptx::fence_mbar_init();
+  }
+  if (threadIdx.x == 32 * kLinFirstEpilogueWarp) {  // (the maps are arguments: nothing that a kernel before this one writes)
+    ptx::prefetch_tensormap(&gp.tma);
+    ptx::prefetch_tensormap(&gp.tmb);
+    ptx::prefetch_tensormap(&gp.tmy);
   }
   if (warp == 1) {
     ptx::tmem_alloc_cg<CG>(ptx::smem_u32(tmem_slot), Cfg::kTmemCols);
@@ -723,6 +728,7 @@ struct LinearTail {
   void* out;
   void* pre;
   int32_t mode, out_type, type;
+  bool vector;  // out is 16-byte aligned
 };
 __device__ __forceinline__ float load_value(const void* p, int64_t i, int type) {
   if (type == QB_F32) return static_cast<const float*>(p)[i];
@@ -739,20 +745,37 @@ __device__ __forceinline__ float gelu_one(float z) {
   gelu_many<1>(f);
   return f[0];
 }
-// out = what stands behind the splits' sum, taken in their order.
+// out = what stands behind the splits' sum, taken in their order.  Four parts at a time are on their way.
 template <int V>
 __global__ void __launch_bounds__(256) linear_join_kernel(const float* parts, int splits, int64_t MN, int N, const LinearTail tail) {
+  constexpr int kAtOnce = 4;
   pdl_begin();
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V; i < MN; i += (int64_t)gridDim.x * 256 * V) {
-    float v[V];
-    if constexpr (V == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(parts + i);
-    else v[0] = parts[i];
-    for (int s = 1; s < splits; ++s) {
-      float w[V];
-      if constexpr (V == 4) *reinterpret_cast<float4*>(w) = *reinterpret_cast<const float4*>(parts + s * MN + i);
-      else w[0] = parts[s * MN + i];
+    float v[V] = {};
+    for (int s = 0; s < splits; s += kAtOnce) {
+      float w[kAtOnce][V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[j] += w[j];
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (s + k < splits) {
+          if constexpr (V == 4) *reinterpret_cast<float4*>(w[k]) = *reinterpret_cast<const float4*>(parts + (s + k) * MN + i);
+          else w[k][0] = parts[(s + k) * MN + i];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (s + k < splits) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) v[j] = s + k == 0 ? w[k][j] : v[j] + w[k][j];
+        }
+      }
+    }
+    if (V == 4 && !tail.bias && !tail.side && !tail.codes && !tail.pre && tail.mode == kPlain && tail.vector) {  // a weight's gradient
+      if (tail.out_type == QB_F32)
+        *reinterpret_cast<float4*>(static_cast<float*>(tail.out) + i) = make_float4(v[0], v[V > 1], v[V > 2 ? 2 : 0], v[V > 3 ? 3 : 0]);
+      else
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(tail.out) + i) =
+            make_uint2(pack16(v[0], v[V > 1], tail.out_type == QB_F16), pack16(v[V > 2 ? 2 : 0], v[V > 3 ? 3 : 0], tail.out_type == QB_F16));
+      continue;
     }
     const int64_t m = i / N;
     const int n = (int)(i - m * N);
@@ -882,14 +905,16 @@ struct LinearChoice {
   int32_t tiles, whole, splits, split_blocks;
 };
 // The cheapest by what a launch and each of its rounds of tiles take, in hundredths of a microsecond: a tile a part per K block of 64 and
-// a fixed part, but no less than its epilogue, the launch the time until the first tile and of the last epilogue.  A last round that fills
-// at most half of the pairs is cut into tiles of half the width.  Where a long K meets few tiles, K is split into runs whose sums a
-// second kernel joins: that costs its launch and the traffic of the parts.
+// a fixed part, the launch the time until the first tile and of the last epilogue.  Fitted to M from 32 to 5,003, N and K from 768 to
+// 4,096: 5,003 x 768 x 768 9.4 us by tiles of 256 x 256, 8.8 by 256 x 128, 9.8 by 128 x 128, 11.6 by 128 x 64; 5,003 x 2,304 x 768 15.7,
+// 17.0, 19.6, 24.9; 613 x 768 x 768 6.3, 6.3, 6.0, 5.2.  A last round that fills at most half of the pairs is cut into tiles of half the
+// width (5,003 x 1,024 x 4,096 42.9 -> 34.8 us).  Where a long K meets few tiles, K is split into runs whose sums a second kernel joins: that
+// costs its launch and the traffic of the parts.
 // `parts`: more than one split where the workspace has room for it.
 static LinearChoice choose_linear(int64_t M, int64_t N, int64_t K, int sms, size_t scratch, bool parts) {
   static constexpr struct {
-    int cg, bt, block, fixed, least, launch;
-  } kForms[] = {{2, 256, 32, 20, 220, 480}, {1, 128, 27, 37, 120, 310}, {1, 64, 20, 25, 100, 300}};
+    int cg, bt, block, fixed, launch;
+  } kForms[] = {{2, 256, 29, 40, 560}, {2, 128, 16, 70, 370}, {1, 128, 20, 80, 300}, {1, 64, 16, 20, 290}};
   const int64_t blocks = lin_up(K, 64);
   LinearChoice best = {};
   int64_t best_cost = 0;
@@ -899,10 +924,10 @@ static LinearChoice choose_linear(int64_t M, int64_t N, int64_t K, int sms, size
     for (int64_t splits = 1; splits == 1 || (4 * splits <= blocks && (tiles * (splits - 1) < groups || (parts && splits == 2)) && splits * M * N * 4 <= (int64_t)scratch); ++splits) {
       const int64_t run = splits == 1 ? blocks : lin_up(lin_up(blocks, splits), 2) * 2;
       if (lin_up(blocks, run) != splits) continue;
-      const int64_t tile = std::max<int64_t>(f.block * run + f.fixed, f.least), all = tiles * splits, last = all % groups;
-      const bool halves = f.cg == 2 && splits == 1 && last > 0 && 2 * last <= groups;
+      const int64_t tile = f.block * run + f.fixed, all = tiles * splits, last = all % groups;
+      const bool halves = f.bt == 256 && splits == 1 && last > 0 && 2 * last <= groups;
       if (parts && splits == 1 && blocks >= 8 && 2 * M * N * 4 <= (int64_t)scratch) continue;
-      const int64_t cost = f.launch + (all / groups) * tile + (halves ? tile * 7 / 10 : (last > 0 ? tile : 0)) + (splits > 1 ? 250 + splits * M * N / 7500 : 0);
+      const int64_t cost = f.launch + (all / groups) * tile + (halves ? tile * 6 / 10 : (last > 0 ? tile : 0)) + (splits > 1 ? 200 + splits * M * N / 15000 : 0);
       if (best.cg == 0 || cost < best_cost) {
         best_cost = cost;
         best = {f.cg, f.bt, (int32_t)(halves ? all + last : all), (int32_t)(halves ? all - last : all), (int32_t)splits, (int32_t)run};
@@ -1012,7 +1037,8 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   gp.run_blocks = out32 ? kLinRunBlocks : (int32_t)blocks;
   gp.idesc = lin_idesc(half_type, a.mn, b.mn, 128 * cg);
   const int mode = split ? kPlain : tail.mode;
-  if (cg == 2) st = launch_linear<256, 2>(gp, out32, mode, half_type, sms, stream);
+  if (cg == 2 && bt == 128) st = launch_linear<128, 2>(gp, out32, mode, half_type, sms, stream);
+  else if (cg == 2) st = launch_linear<256, 2>(gp, out32, mode, half_type, sms, stream);
   else if (bt == 128) st = launch_linear<128, 1>(gp, out32, mode, half_type, sms, stream);
   else st = launch_linear<64, 1>(gp, out32, mode, half_type, sms, stream);
   if (st != QB_OK) return st;
@@ -1059,12 +1085,13 @@ extern "C" size_t qb_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   return kLinScratchOff + pads + sums + parts;
 }
 
-extern "C" int32_t qb_linear_tile_columns(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int32_t* half_tiles, int32_t* splits) {
+extern "C" int32_t qb_linear_tile_columns(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int32_t* rows, int32_t* half_tiles, int32_t* splits) {
   using namespace qb;
   if (impossible_linear(M, N, K)) return 0;
   int sms = 148;
   require_sm100(&sms);  // without a device: for a 148-SM part
   const LinearChoice c = choose_linear(M, N, K, sms, ws_bytes > kLinScratchOff ? ws_bytes - kLinScratchOff : 0, false);
+  if (rows) *rows = 128 * c.cg;
   if (half_tiles) *half_tiles = c.tiles - c.whole;
   if (splits) *splits = c.splits;
   return c.bt;
@@ -1089,7 +1116,7 @@ extern "C" qb_status qb_linear(const void* x, const void* w, int type, const flo
   if ((st = check_linear_ws(what, ws, ws_bytes)) != QB_OK) return st;
   int sms = 0;
   if ((st = require_sm100(&sms)) != QB_OK) return st;
-  const LinearTail tail = {bias, residual, nullptr, nullptr, y, pre, activation == QB_GELU ? kGelu : kPlain, out_type, type};
+  const LinearTail tail = {bias, residual, nullptr, nullptr, y, pre, activation == QB_GELU ? kGelu : kPlain, out_type, type, aligned16(y)};
   return run_linear(what, {x, M, K, false}, {w, N, K, false}, M, N, K, tail, pre_codes, pre_scales, ws, LinearScratch(ws, ws_bytes), sms, (cudaStream_t)cuda_stream);
 }
 
@@ -1110,7 +1137,7 @@ extern "C" qb_status qb_linear_grad_x(const void* grad_y, const void* w, int typ
   if ((st = check_linear_ws(what, ws, ws_bytes)) != QB_OK) return st;
   int sms = 0;
   if ((st = require_sm100(&sms)) != QB_OK) return st;
-  const LinearTail tail = {nullptr, pre ? pre : residual, pre_codes, pre_scales, grad_x, nullptr, pre || pre_codes ? kSlope : kPlain, type, type};
+  const LinearTail tail = {nullptr, pre ? pre : residual, pre_codes, pre_scales, grad_x, nullptr, pre || pre_codes ? kSlope : kPlain, type, type, aligned16(grad_x)};
   return run_linear(what, {grad_y, M, N, false}, {w, N, K, true}, M, K, N, tail, nullptr, nullptr, ws, LinearScratch(ws, ws_bytes), sms, (cudaStream_t)cuda_stream);
 }
 
@@ -1134,7 +1161,7 @@ extern "C" qb_status qb_linear_grad_w(const void* grad_y, const void* x, int typ
   float* const parts = grad_bias ? static_cast<float*>(scratch.take((size_t)runs * (size_t)N * 4)) : nullptr;
   if (grad_bias && !parts) return no_room_for_bias();
   if (grad_w) {
-    const LinearTail tail = {nullptr, nullptr, nullptr, nullptr, grad_w, nullptr, kPlain, out_type, type};
+    const LinearTail tail = {nullptr, nullptr, nullptr, nullptr, grad_w, nullptr, kPlain, out_type, type, aligned16(grad_w)};
     if ((st = run_linear(what, {grad_y, M, N, true}, {x, M, K, true}, N, K, M, tail, nullptr, nullptr, ws, scratch, sms, stream)) != QB_OK) return st;
   }
   if (grad_bias) {  // behind the product, under which it runs where that leaves SMs

@@ -54,6 +54,11 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* 
       : "memory");
 }
 
+// Fetches a tensor map ahead of the first copy that goes by it.
+__device__ __forceinline__ void prefetch_tensormap(const void* tmap) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
+}
+
 // tma_load_2d for a tensor of three dimensions.
 __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const void* tmap, uint32_t bar, int32_t x, int32_t y, int32_t z) {
   asm volatile(

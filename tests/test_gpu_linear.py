@@ -36,7 +36,7 @@ def data(seed, *shapes, t):
 
 # one token, less than a tile, every remainder of 8 and 64, more tiles than SMs, widths that are no multiple of 8
 SIZES = [(1, 1, 1), (1, 8, 8), (1, 768, 768), (2, 3, 5), (5, 9, 17), (33, 64, 128), (64, 72, 96), (127, 129, 64), (128, 128, 64), (130, 257, 65), (200, 200, 200), (256, 256, 192),
-         (300, 520, 1000), (613, 9, 768), (1000, 776, 768), (2500, 1030, 513), (2049, 2304, 768), (4100, 1024, 328), (9000, 520, 136), (77, 3000, 2056), (1, 4099, 4097)]
+         (300, 520, 1000), (613, 9, 768), (1000, 776, 768), (2500, 1030, 513), (2049, 2304, 768), (4100, 1024, 328), (9000, 520, 136), (77, 3000, 2056), (1, 4099, 4097), (5003, 768, 776), (5003, 2304, 328), (4099, 4096, 264), (5003, 328, 2304), (328, 5008, 2304), (264, 4099, 4096)]
 
 
 @pytest.mark.parametrize("kind", sorted(TYPES))
@@ -184,9 +184,10 @@ def test_not_finite(bad, M, N, K, ws):
 
 
 def test_forms_that_are_covered(ws):
-    """The sizes above meet every form: tiles of 64, 128 and 256 columns, halves, parts."""
-    forms = [qb.linear_form(M, N, K, ws.numel()) for M, N, K in SIZES] + [qb.linear_form(N, K, M, ws.numel()) for M, N, K in SIZES]
-    assert {f[0] for f in forms} == {64, 128, 256} and any(f[2] > 1 for f in forms)
+    """The sizes above meet every form in every product: tiles of 128 x 64, 128 x 128, 256 x 128 and 256 x 256, halves, parts."""
+    forms = [qb.linear_form(*s, ws.numel()) for M, N, K in SIZES for s in ((M, N, K), (M, K, N), (N, K, M))]
+    assert {f[:2] for f in forms} == {(128, 64), (128, 128), (256, 128), (256, 256)}
+    assert any(f[2] > 0 for f in forms) and any(f[3] > 1 for f in forms)
 
 
 def test_codes_of_any_alignment(ws):
