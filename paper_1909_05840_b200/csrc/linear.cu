@@ -75,7 +75,7 @@ struct LinCfg {
   static constexpr int kStages = BT / CG == 64 ? 4 : 3;
   static constexpr int kOutBytes = kLinEpilogueWarps * 2048;
   static constexpr int kBarBytes = 256;
-  static constexpr int kBiasBytes = 2 * 256 * 4;
+  static constexpr int kBiasBytes = kLinEpilogueWarps * 32 * 4;
   static constexpr int kSmemBytes = kStages * kStageBytes + kOutBytes + kBarBytes + kBiasBytes;
   static constexpr int kTmemCols = 2 * BT;
   static_assert(kSmemBytes <= 232448, "shared memory");
@@ -124,17 +124,6 @@ struct LinTile {
     m0 *= 128 * CG;
   }
 };
-
-// Barrier over the epilogue warps (named barrier 1) that also ORs a predicate over them.
-__device__ __forceinline__ bool lin_epilogue_sync_or(bool pred) {
-  uint32_t res;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(res)
-      : "r"((uint32_t)pred), "n"(32 * kLinEpilogueWarps)
-      : "memory");
-  return res != 0;
-}
 
 // Two 16-bit values of a word, and back.
 __device__ __forceinline__ float2 unpack16(uint32_t w, bool half_type) {
@@ -226,7 +215,6 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
   const uint32_t drain_bar = bar_base + 8u * (2 * kStages + 4);
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 8 * (2 * kStages + 5));
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  float* const bias_tile = reinterpret_cast<float*>(bar_ptr + Cfg::kBarBytes);  // [2][256]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if ((smem_base & 1023u) != 0u) {  // never expected; the swizzle needs it
@@ -388,7 +376,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     constexpr int kCols = OUT32 ? 16 : 32;  // columns of a chunk
     constexpr int kESize = OUT32 ? 4 : 2;
     const int ew = warp - kLinFirstEpilogueWarp, quarter = warp & 3, part = ew >> 2;
-    const int e = threadIdx.x - 32 * kLinFirstEpilogueWarp;
+    float* const bias_at = reinterpret_cast<float*>(bar_ptr + Cfg::kBarBytes) + ew * 32;  // of the warp's chunk
     constexpr bool half_type = HALF;
     uint8_t* const buf = out_ptr + ew * 2048;
     const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
@@ -400,15 +388,27 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         else ptx::mbar_arrive(bar);
       }
     };
-    int it = 0, b = 0;  // runs; the half of the bias buffer
-    for (int t = group; t < gp.tiles; t += groups, b ^= 1) {
+    int it = 0;
+    for (int t = group; t < gp.tiles; t += groups) {
       const LinTile<BT, CG> tile(gp, t);
       const float* const bias = gp.bias;
       const void* const side = gp.side;
       int m0 = tile.m0 + (int)rank * 128 + quarter * 32, n0 = tile.n0;
       int chunks = m0 < gp.M ? max(0, min(tile.width / kCols, (gp.N - n0 + kCols - 1) / kCols)) : 0;
       asm volatile("" : "+r"(m0), "+r"(n0), "+r"(chunks));  // formed before the wait, not behind it
-      if (e < BT) bias_tile[b * 256 + e] = bias && n0 + e < gp.N ? bias[n0 + e] : 0.0f;
+      // The warp's chunks, one a turn: every fourth one, or, where pairs of them are the blocks of codes, every fourth pair.
+      const bool paired = !OUT32 && MODE != kSlope && gp.pre_codes != nullptr;
+      const auto chunk = [&](int turn) { return paired ? 2 * part + (turn & 1) + 8 * (turn >> 1) : part + 4 * turn; };
+      // Their biases, a column a lane: of two turns each (fp32 out: of four).  Every warp waits and goes on by itself: with the tile's
+      // biases shared behind a barrier of all of them, they did the same things at the same time and waited for one another.
+      float biases[2] = {0.0f, 0.0f};
+      if (MODE != kSlope && bias) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int c = OUT32 ? chunk(2 * h + (lane >> 4)) * 16 + (lane & 15) : chunk(h) * 32 + lane;
+          if (n0 + c < gp.N && c < tile.width) biases[h] = bias[n0 + c];
+        }
+      }
       const int rows = min(32, gp.M - m0);
       const bool mine = lane < rows;
       // The chunk's part of the tensor beside the product (residual, pre-activation, codes of it): the lane's row, fetched while the
@@ -429,10 +429,9 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           }
         }
       };
-      // Waits for the accumulator of run `it`.  False when a wait has run out, for all warps together.
+      // Waits for the accumulator of run `it`.
       auto wait_run = [&]() {
-        const bool ok = ew != 0 || wait_barrier_warp(acc_full(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag);
-        if (lin_epilogue_sync_or(!ok)) {  // publishes the bias too
+        if (!wait_barrier_warp(acc_full(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag)) {
           timed_out = true;
           where = (3 << 16) | (it & 1);
           return false;
@@ -450,9 +449,16 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
 #pragma unroll
         for (int j = 0; j < kCols; ++j) z[j] = __uint_as_float(w[j]);
       };
-      auto add_bias = [&](int column, float* z) {
+      auto add_bias = [&](int turn, float* z) {
         if (MODE == kSlope || !bias) return;
-        const float4* const b4 = reinterpret_cast<const float4*>(bias_tile + b * 256 + column);
+        __syncwarp();
+        if constexpr (OUT32) {
+          if ((lane >> 4) == (turn & 1)) bias_at[lane & 15] = biases[turn >> 1];
+        } else {
+          bias_at[lane] = turn == 0 ? biases[0] : biases[1];
+        }
+        __syncwarp();
+        const float4* const b4 = reinterpret_cast<const float4*>(bias_at);
 #pragma unroll
         for (int j = 0; j < kCols / 4; ++j) {
           const float4 q = b4[j];
@@ -460,8 +466,8 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           add2(z + 4 * j + 2, q.z, q.w);
         }
       };
-      // What becomes of the chunk's z (the product and the bias), from there to memory.  top: of the other chunk of its block.
-      auto emit = [&](int i, float* v, float top) {
+      // What becomes of the chunk's z (the product and the bias), from there to memory.  top: the largest magnitude of its block.
+      auto emit = [&](int i, int next, float* v, float top) {
         const int c0 = i * kCols, cols = min(kCols, gp.N - n0 - c0);
         const int64_t corner = (int64_t)m0 * gp.N + n0 + c0;  // of the chunk, in elements
         const int64_t block = (int64_t)(m0 + lane) * checkpoint_blocks(gp.N) + (n0 + c0) / kCheckpointBlock;  // the row's, in scales
@@ -503,8 +509,6 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         }
         if constexpr (!OUT32 && MODE != kSlope) {
           if (gp.pre_codes) {  // z in 8 bits
-#pragma unroll
-            for (int j = 0; j < kCols; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
             const CheckpointCodes cs(top);
             if (mine && (c0 & 32) == 0) gp.pre_scales[block] = checkpoint_scale(top);
             uint4 c[2];
@@ -587,7 +591,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             }
           }
         }
-        if (!OUT32 && i + 4 < chunks) fetch(c0 + 4 * kCols);
+        if (!OUT32 && next < chunks) fetch(next * kCols);
         buffer_free();
 #pragma unroll
         for (int k = 0; k < 4; ++k) {  // 16 bytes of the row at a time
@@ -619,7 +623,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           __syncwarp();
         }
       };
-      if (!OUT32 && part < chunks) fetch(part * kCols);
+      if (!OUT32 && chunk(0) < chunks) fetch(chunk(0) * kCols);
       bool ok;
       if constexpr (OUT32) {  // the runs before the last are added up in registers, and to the last one where it lies
         constexpr int kChunks = BT / kCols / 4;  // of a warp
@@ -659,20 +663,29 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         ok = wait_run();
       }
       if (!ok) break;
-      if (part >= chunks) arrive(acc_empty(it & 1));
+      if (chunk(0) >= chunks) arrive(acc_empty(it & 1));
+      float top = 0.0f;
 #pragma unroll 1
-      for (int i = part; i < chunks; i += 4) {
-        float v[kCols], top = 0.0f;
-        if (!OUT32 && MODE != kSlope && gp.pre_codes) {  // a block of codes is this chunk and its neighbour
-          read((i ^ 1) * kCols, v);
-          add_bias((i ^ 1) * kCols, v);
+      for (int turn = 0; chunk(turn) < chunks; ++turn) {
+        const int i = chunk(turn), next = chunk(turn + 1);
+        float v[kCols];
+        const auto highest = [&]() {
 #pragma unroll
           for (int j = 0; j < kCols; j += 2) top = max3_nan(top, fabsf(v[j]), fabsf(v[j + 1]));
+        };
+        if (paired && (turn & 1) == 0) {  // the block's second chunk is read ahead, for its largest magnitude
+          top = 0.0f;
+          if (next < chunks) {
+            read(next * kCols, v);
+            add_bias(turn + 1, v);
+            highest();
+          }
         }
         read(i * kCols, v);
-        if (i + 4 >= chunks) arrive(acc_empty(it & 1));
-        add_bias(i * kCols, v);
-        emit(i, v, top);
+        if (next >= chunks) arrive(acc_empty(it & 1));
+        add_bias(turn, v);
+        if (paired && (turn & 1) == 0) highest();
+        emit(i, next, v, top);
       }
       ++it;
     }
