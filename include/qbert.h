@@ -556,7 +556,7 @@ qb_status qb_gelu_backward(const void* grad_y, int type, const void* pre, const 
  * qb_linear_grad_x takes no residual.  grad_w or grad_bias may be NULL (without grad_w x may be too).  M, N and K up to QB_MAX_MN, any size.
  * The sums' order does not change from call to call with the same sizes, workspace size and outputs.
  * The workspace is 16-byte aligned; qb_linear_workspace_bytes(M, N, K) serves the three calls (0 on invalid arguments).  Less will do,
- * except for grad_bias and for tensors whose rows are no multiple of 8 elements, which need their part (else QB_ERR_WORKSPACE); more lets a
+ * except for grad_bias of more than 256 columns or 65,536 values and for tensors whose rows are no multiple of 8 elements, which need their part (else QB_ERR_WORKSPACE); more lets a
  * product of few tiles over a long contraction be summed in more parts side by side.
  */
 size_t qb_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);

@@ -903,13 +903,38 @@ __global__ void __launch_bounds__(256) column_join_kernel(const float* parts, in
   }
 }
 
+// The same for a few columns and rows (kFewColumns, kFewValues), by one block in one launch: 2^k threads a column, joined as a tree.
+constexpr int kFewColumns = 256;
+constexpr int64_t kFewValues = 65536;
+template <bool UNDER>
+__global__ void __launch_bounds__(1024) column_few_kernel(const uint16_t* g, int64_t M, int32_t N, int half_type, float* sums) {
+  __shared__ float joined[1024];
+  if constexpr (!UNDER) pdl_begin();
+  int lanes = 1;
+  while (2 * lanes * N <= 1024) lanes *= 2;
+  const int c = (int)threadIdx.x % N, lane = (int)threadIdx.x / N;
+  float t = 0.0f;
+  if (lane < lanes) {
+#pragma unroll 8
+    for (int64_t r = lane; r < M; r += lanes) t += unpack16(g[r * N + c], half_type != 0).x;
+  }
+  for (int step = lanes / 2; step > 0; step /= 2) {
+    joined[threadIdx.x] = t;
+    __syncthreads();
+    if (lane < step) t += joined[threadIdx.x + step * N];
+    __syncthreads();
+  }
+  if (lane == 0) sums[c] = t;
+  if constexpr (UNDER) pdl_begin();
+}
+
 static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 static int64_t lin_up(int64_t n, int64_t m) { return (n + m - 1) / m; }
 
 // The tensor cores cut an accumulator off at its last place at each addition of 16 products, always towards zero: the error grows
 // with their number (24,576 products of random signs: 2.8e-5 of the result).  fp32 outputs are summed in runs of this many K blocks, which
 // the epilogue's registers add up, rounded to nearest: the error is then that of fp32 products.
-constexpr int kLinRunBlocks = 16;
+constexpr int kLinRunBlocks = 8;
 constexpr size_t kLinScratchOff = 1024;  // of what calls keep in the workspace besides its header
 
 // The form of a product: CTAs per tile, columns, for pairs how many tiles are whole, and splits of K.
@@ -1170,14 +1195,19 @@ extern "C" qb_status qb_linear_grad_w(const void* grad_y, const void* x, int typ
   if ((st = require_sm100(&sms)) != QB_OK) return st;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   LinearScratch scratch(ws, ws_bytes);
+  const bool few = N <= kFewColumns && M * N <= kFewValues;
   const int64_t run = lin_up(M, column_runs(M, N, sms)), runs = lin_up(M, run);
-  float* const parts = grad_bias ? static_cast<float*>(scratch.take((size_t)runs * (size_t)N * 4)) : nullptr;
-  if (grad_bias && !parts) return no_room_for_bias();
+  float* const parts = grad_bias && !few ? static_cast<float*>(scratch.take((size_t)runs * (size_t)N * 4)) : nullptr;
+  if (grad_bias && !few && !parts) return no_room_for_bias();
   if (grad_w) {
     const LinearTail tail = {nullptr, nullptr, nullptr, nullptr, grad_w, nullptr, kPlain, out_type, type, aligned16(grad_w)};
     if ((st = run_linear(what, {grad_y, M, N, true}, {x, M, K, true}, N, K, M, tail, nullptr, nullptr, ws, scratch, sms, stream)) != QB_OK) return st;
   }
-  if (grad_bias) {  // behind the product, under which it runs where that leaves SMs
+  // behind the product, under which it runs where that leaves SMs
+  if (grad_bias && few) {
+    QB_CUDA_TRY(launch_kernel(grad_w ? column_few_kernel<true> : column_few_kernel<false>, 1, 1024, 0, stream, 1, false, static_cast<const uint16_t*>(grad_y), M, (int32_t)N,
+                              (int)(type == QB_F16), grad_bias));
+  } else if (grad_bias) {
     const int col_blocks = (int)lin_up(N, 256);
     auto sum = N % 8 == 0 ? (grad_w ? column_parts_kernel<true, true> : column_parts_kernel<true, false>)
                           : (grad_w ? column_parts_kernel<false, true> : column_parts_kernel<false, false>);

@@ -150,16 +150,22 @@ def test_grad_w(M, N, K, out, kind, ws):
     assert none is None and ((db3.double() - dy.double().sum(0)).abs() <= db_tol).all()  # (another order of the same sums)
 
 
-def test_long_contraction(ws):
-    """The gradient of a weight over many tokens in fp32: as near to 64 bits as fp32 products, which the tensor cores' cut-off sums would not
-    be over one long chain."""
-    M, N, K = 24576, 256, 1024
+@pytest.mark.parametrize("M,N,K", [(24576, 256, 1024), (1024, 768, 768), (6144, 1030, 520), (613, 2000, 1000)])
+def test_fp32_sums(M, N, K, ws):
+    """fp32 outputs are nearer to 64 bits than one chain of additions that are cut off would be (24,576 of them: 2.8e-5): at most 512 products,
+    32 additions, go into one accumulator, each cut by 2^-23 of it at most, 2^-18 of a run's sum; what the runs' sums are off by adds up
+    as they do."""
     g = torch.Generator(device="cuda").manual_seed(3)
     dy, x = torch.randn(M, N, device="cuda", generator=g).bfloat16(), torch.randn(M, K, device="cuda", generator=g).bfloat16()
     want = dy.double().t() @ x.double()
     for room in (ws, ws[:1 << 20]):
-        dw, _ = qb.linear_grad_w(dy, x, room)
-        assert float((dw.double() - want).norm() / want.norm()) <= 1e-5
+        if N % 8 == 0 or room is ws:
+            dw, _ = qb.linear_grad_w(dy, x, room)
+            assert float((dw.double() - want).norm() / want.norm()) <= 2.0**-18
+    w = torch.randn(N, M, device="cuda", generator=g).bfloat16()
+    y = qb.linear(x.t().contiguous(), w, None, ws, out_dtype=torch.float32)
+    z = x.double().t() @ w.double().t()
+    assert float((y.double() - z).norm() / z.norm()) <= 2.0**-18
 
 
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")])
@@ -202,7 +208,7 @@ def test_codes_of_any_alignment(ws):
 
 
 def test_refusals(ws):
-    x, w, dy = data(2, (64, 96), (40, 96), (64, 40), t=torch.bfloat16)
+    x, w, dy, wide = data(2, (64, 96), (40, 96), (64, 40), (64, 264), t=torch.bfloat16)
     bias = torch.zeros(40, device="cuda")
     for call in (lambda: qb.linear(x.t(), w, bias, ws), lambda: qb.linear(x, w.half(), bias, ws), lambda: qb.linear(x, w[:, :88], bias, ws), lambda: qb.linear(x.float(), w.float(), bias, ws),
                  lambda: qb.linear(x, w, bias.bfloat16(), ws), lambda: qb.linear(x, w, bias[:8], ws), lambda: qb.linear(x, w, bias, ws, residual=x),
@@ -216,7 +222,7 @@ def test_refusals(ws):
                          (lambda: qb.linear_grad_x(dy, w, ws, through=x, residual=x), qb.QB_ERR_INVALID),
                          (lambda: qb.linear_grad_w(dy, x, ws, needs=(False, False)), qb.QB_ERR_INVALID),
                          (lambda: qb.linear(x[:, :33].contiguous(), w[:, :33].contiguous(), bias, ws[:1024]), qb.QB_ERR_WORKSPACE),
-                         (lambda: qb.linear_grad_w(dy, x, ws[:1024]), qb.QB_ERR_WORKSPACE)):
+                         (lambda: qb.linear_grad_w(wide, x, ws[:1024]), qb.QB_ERR_WORKSPACE)):
         with pytest.raises(qb.QbertError) as e:
             call()
         assert e.value.status == status
