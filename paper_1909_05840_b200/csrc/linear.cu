@@ -58,8 +58,8 @@ struct LinearParams {
   int32_t k_blocks;      // of all splits
   int32_t run_blocks;    // K blocks that one accumulator sums; even where there are several such runs (fp32 out), which registers add up
   int32_t tma_store;     // 1: rows of out are 16-byte aligned
-  int32_t vector;        // 1: rows of side and of pre are 32-byte aligned
-  int32_t vector_codes;  // 1: rows of the codes are
+  int32_t vector;        // 1: rows of side and of pre are 16-byte aligned, 2: 32-byte aligned
+  int32_t vector_codes;  // the same of the codes'
   uint32_t idesc;
 };
 
@@ -162,11 +162,16 @@ __device__ __forceinline__ void add_accumulator(uint32_t taddr, float* z) {
   for (int c = 0; c < 8; c += 2) add2(z + c, __uint_as_float(w[c]), __uint_as_float(w[c + 1]));
 }
 
-// 32 bytes of a row: whole sectors, where 16 bytes a lane would touch each of them twice.
-__device__ __forceinline__ void load32(const void* p, uint4& a, uint4& b) {
-  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
-               : "l"(p));
+// 32 bytes of a row, `wide`: whole sectors, where 16 bytes a lane would touch each of them twice; else 16 and, if `second`, the other 16.
+__device__ __forceinline__ void load_row(const void* p, bool wide, bool second, uint4& a, uint4& b) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+                 : "l"(p));
+  } else {
+    a = *static_cast<const uint4*>(p);
+    if (second) b = static_cast<const uint4*>(p)[1];
+  }
 }
 __device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z),
@@ -413,19 +418,22 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       const bool mine = lane < rows;
       // The chunk's part of the tensor beside the product (residual, pre-activation, codes of it): the lane's row, fetched while the
       // products run.
+      // (Rows that are 16-byte aligned only: by vectors for a slope, where there are registers for both kinds, else by way of the buffer.)
+      constexpr int kLeast = MODE == kSlope ? 1 : 2;
       uint4 s[4];
       auto fetch = [&](int c0) {
         const int64_t corner = (int64_t)(m0 + lane) * gp.N + n0 + c0;
         if (MODE == kSlope && gp.codes) {
           if (!gp.vector_codes) return;
           s[0] = s[1] = make_uint4(0u, 0u, 0u, 0u);
-          if (mine && n0 + c0 < gp.N) load32(gp.codes + corner, s[0], s[1]);
-        } else if (side && gp.vector) {
+          if (mine && n0 + c0 < gp.N) load_row(gp.codes + corner, gp.vector_codes > 1, n0 + c0 + 16 < gp.N, s[0], s[1]);
+        } else if (side && gp.vector >= kLeast) {
           const uint8_t* const from = static_cast<const uint8_t*>(side) + corner * kESize;
 #pragma unroll
           for (int k = 0; k < 4; k += 2) {
             s[k] = s[k + 1] = make_uint4(0u, 0u, 0u, 0u);
-            if (mine && n0 + c0 + k * (16 / kESize) < gp.N) load32(from + 16 * k, s[k], s[k + 1]);
+            const int c = n0 + c0 + k * (16 / kESize);
+            if (mine && c < gp.N) load_row(from + 16 * k, MODE != kSlope || gp.vector > 1, c + 16 / kESize < gp.N, s[k], s[k + 1]);
           }
         }
       };
@@ -484,13 +492,18 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         // rows of any alignment come by way of the buffer
         if (MODE == kSlope && gp.codes && !gp.vector_codes) {
           buffer_free();
-          for (int r = 0; r < rows; ++r)
-            reinterpret_cast<int8_t*>(staged(buf, r, lane >> 4))[lane & 15] = lane < cols ? gp.codes[corner + (int64_t)r * gp.N + lane] : (int8_t)0;
+          for (int r0 = 0; r0 < rows; r0 += 8) {  // eight rows on their way at a time
+            int8_t e[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) e[r] = lane < cols && r0 + r < rows ? gp.codes[corner + (int64_t)(r0 + r) * gp.N + lane] : (int8_t)0;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) reinterpret_cast<int8_t*>(staged(buf, r0 + r, lane >> 4))[lane & 15] = e[r];
+          }
           __syncwarp();
 #pragma unroll
           for (int k = 0; k < 2; ++k) s[k] = *staged(buf, lane, k);
           __syncwarp();
-        } else if (side && !gp.vector) {
+        } else if (side && gp.vector < kLeast) {
           buffer_free();
           if constexpr (OUT32) {
             for (int r = lane >> 4; r < rows; r += 2) {
@@ -498,9 +511,13 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
               reinterpret_cast<float*>(staged(buf, r, c >> 2))[c & 3] = c < cols ? static_cast<const float*>(side)[corner + (int64_t)r * gp.N + c] : 0.0f;
             }
           } else {
-            for (int r = 0; r < rows; ++r)
-              reinterpret_cast<uint16_t*>(staged(buf, r, lane >> 3))[lane & 7] =
-                  lane < cols ? static_cast<const uint16_t*>(side)[corner + (int64_t)r * gp.N + lane] : (uint16_t)0;
+            for (int r0 = 0; r0 < rows; r0 += 8) {
+              uint16_t e[8];
+#pragma unroll
+              for (int r = 0; r < 8; ++r) e[r] = lane < cols && r0 + r < rows ? static_cast<const uint16_t*>(side)[corner + (int64_t)(r0 + r) * gp.N + lane] : (uint16_t)0;
+#pragma unroll
+              for (int r = 0; r < 8; ++r) reinterpret_cast<uint16_t*>(staged(buf, r0 + r, lane >> 3))[lane & 7] = e[r];
+            }
           }
           __syncwarp();
 #pragma unroll
@@ -520,7 +537,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
               c[k].w = cs.codes4(v[16 * k + 12], v[16 * k + 13], v[16 * k + 14], v[16 * k + 15]);
             }
             int8_t* const to = gp.pre_codes + corner;
-            if (gp.vector_codes) {
+            if (gp.vector_codes >= kLeast) {
               if (mine) store32(to + (int64_t)lane * gp.N, c[0], c[1]);
             } else {
               buffer_free();
@@ -538,7 +555,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             for (int k = 0; k < 4; ++k)
               c[k] = make_uint4(pack16(v[8 * k], v[8 * k + 1], half_type), pack16(v[8 * k + 2], v[8 * k + 3], half_type), pack16(v[8 * k + 4], v[8 * k + 5], half_type),
                                 pack16(v[8 * k + 6], v[8 * k + 7], half_type));
-            if (gp.vector) {
+            if (gp.vector >= kLeast) {
 #pragma unroll
               for (int k = 0; k < 4; k += 2)
                 if (mine && 8 * k < cols) store32(to + (int64_t)lane * gp.N + 8 * k, c[k], c[k + 1]);
@@ -813,23 +830,41 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* parts, in
   }
 }
 
-// Rows of any length as rows of a multiple of 16 bytes, zeros behind them (what a TMA load needs).
+// Rows of any length as rows of a multiple of 16 bytes, zeros behind them (what a TMA load needs).  Eight elements a thread, read as the
+// words that hold them and shifted where they begin inside one; none that the tensor does not have is read.
 __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* from, uint16_t* to, int64_t rows, int32_t cols, int32_t pitch) {
   pdl_begin();
   const int per_row = pitch / 8;
-  const int64_t n = rows * per_row;
+  const int64_t n = rows * per_row, all = rows * cols;
+#pragma unroll 2
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per_row;
-    const int c = (int)(i - r * per_row) * 8;
-    uint16_t e[8];
+    const int64_t r = n >> 32 ? i / per_row : (int64_t)((uint32_t)i / (uint32_t)per_row);
+    const int c = (int)(i - r * per_row) * 8, left = cols - c;
+    const int64_t first = r * cols + c;
+    uint32_t w[5];
+    if (first + 10 <= all) {
+      const uint32_t* const words = reinterpret_cast<const uint32_t*>(from) + (first >> 1);  // (`from` is 16-byte aligned)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = c + j < cols ? from[r * cols + c + j] : (uint16_t)0;
-    uint4 w;
-    w.x = e[0] | (uint32_t)e[1] << 16;
-    w.y = e[2] | (uint32_t)e[3] << 16;
-    w.z = e[4] | (uint32_t)e[5] << 16;
-    w.w = e[6] | (uint32_t)e[7] << 16;
-    *reinterpret_cast<uint4*>(to + i * 8) = w;
+      for (int j = 0; j < 4; ++j) w[j] = words[j];
+      w[4] = 0u;
+      if (first & 1) {
+        w[4] = words[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(w[j], w[j + 1], 16);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = first + 2 * j < all ? from[first + 2 * j] : 0, hi = first + 2 * j + 1 < all ? from[first + 2 * j + 1] : 0;
+        w[j] = lo | hi << 16;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {  // what the next row begins with is not this row's
+      if (2 * j >= left) w[j] = 0u;
+      else if (2 * j + 1 >= left) w[j] &= 0xffffu;
+    }
+    *reinterpret_cast<uint4*>(to + i * 8) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -1059,8 +1094,11 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   gp.pre = split ? nullptr : tail.pre;
   gp.pre_codes = pre_codes;
   gp.pre_scales = pre_scales;
-  gp.vector = row_bytes % 32 == 0 && aligned_to(tail.side, 32) && aligned_to(tail.pre, 32);
-  gp.vector_codes = N % 32 == 0 && aligned_to(tail.codes, 32) && aligned_to(pre_codes, 32);
+  const auto vectors = [](int64_t pitch, const void* p, const void* q) {
+    return pitch % 32 == 0 && aligned_to(p, 32) && aligned_to(q, 32) ? 2 : (pitch % 16 == 0 && aligned16(p) && aligned16(q) ? 1 : 0);
+  };
+  gp.vector = vectors(row_bytes, tail.side, tail.pre);
+  gp.vector_codes = vectors(N, tail.codes, pre_codes);
   gp.ws = ws;
   gp.M = (int32_t)M;
   gp.N = (int32_t)N;
