@@ -5,7 +5,11 @@
 // registers, so that the variance is a sum of squared differences from the mean that is known by then.
 // Backward: a block keeps the sums of grad_y * xhat and grad_y over its rows in registers, a pair a column, and leaves them in the
 // workspace at its end; a second kernel sums the blocks', always in the same order.
-// Bound by memory: one read and one write of the tensor forward, two reads and one write backward.
+// Bound by memory: one read and one write of the tensor forward, two reads and one write backward.  24,576 x 1,024: bfloat16 forward 19.5 us
+// (5.2 TB/s), backward 30.5 (4.9), fp32 35 (5.7) and 53 (5.7); 5,003 x 1,024 bfloat16 6.6 and 13.1; 32 x 768 2.4 and 4.3.  About 4 us
+// of a backward pass are its start, its blocks' sums and the second kernel.  Rows on their way in shared memory cost no registers (forward 20.4
+// with the next row in registers, 27.4 with one row a warp and a block that ends).  Tried and not kept, backward, 24,576 x 1,024 bfloat16: two warps a row with
+// sixteen elements a lane 45 us, two blocks per SM with gamma in shared memory 41, two rows a warp at a time 31.
 #include "common.cuh"
 #include "ptx_float.cuh"
 #include "vec16.cuh"
@@ -522,14 +526,15 @@ __global__ void __launch_bounds__(kNormThreads) layer_norm_long_backward_kernel(
   }
 }
 
-// Sums over the blocks: 32 sums a block, eight runs of blocks side by side, joined in their order.  `lanes`: of a row, in whose order the
-// sums lie (half of them gamma's), or 0: in the columns' order.
-__global__ void __launch_bounds__(256) layer_norm_join_kernel(const float* parts, int blocks, int32_t sums, int32_t lanes, int32_t V, int32_t D, float* grad_gamma,
-                                                              float* grad_beta) {
-  __shared__ float joined[8][32];
+// Sums over the blocks: 32 sums a block, 32 groups of blocks side by side (few loads one after the other: the launch is as long as these
+// take), joined in their order.  `lanes`: of a row, in whose order the sums lie (half of them gamma's), or 0: in the columns' order.
+constexpr int kNormJoinGroups = 32;
+__global__ void __launch_bounds__(32 * kNormJoinGroups) layer_norm_join_kernel(const float* parts, int blocks, int32_t sums, int32_t lanes, int32_t V, int32_t D,
+                                                                               float* grad_gamma, float* grad_beta) {
+  __shared__ float joined[kNormJoinGroups][32];
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int k = (int)blockIdx.x * 32 + lane, run = (blocks + 7) / 8, last = min((warp + 1) * run, blocks);
+  const int k = (int)blockIdx.x * 32 + lane, run = (blocks + kNormJoinGroups - 1) / kNormJoinGroups, last = min((warp + 1) * run, blocks);
   float s = 0.0f;
   if (k < sums) {
 #pragma unroll 8
@@ -539,7 +544,7 @@ __global__ void __launch_bounds__(256) layer_norm_join_kernel(const float* parts
   __syncthreads();
   if (warp == 0 && k < sums) {
 #pragma unroll
-    for (int w = 1; w < 8; ++w) s += joined[w][lane];
+    for (int w = 1; w < kNormJoinGroups; ++w) s += joined[w][lane];
     const int at = k < sums / 2 ? k : k - sums / 2;
     const int c = lanes ? norm_column(at / lanes, at % lanes, lanes, V) : at;
     float* const to = k < sums / 2 ? grad_gamma : grad_beta;
@@ -686,7 +691,7 @@ extern "C" qb_status qb_layer_norm_backward(const void* grad_y, const void* x, i
   }
   if (st != QB_OK || !sums) return st;
   const int32_t count = (int32_t)norm_sums(D);
-  QB_CUDA_TRY(launch_kernel(layer_norm_join_kernel, (unsigned)((count + 31) / 32), 256, 0, stream, 1, false, parts, blocks, count,
+  QB_CUDA_TRY(launch_kernel(layer_norm_join_kernel, (unsigned)((count + 31) / 32), 32 * kNormJoinGroups, 0, stream, 1, false, parts, blocks, count,
                             D > kNormMostHeld ? 0 : 32 * warps, V, (int32_t)D, grad_gamma, grad_beta));
   return QB_OK;
 }

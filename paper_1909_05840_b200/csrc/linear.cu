@@ -11,8 +11,19 @@
 //   warps 2..3    idle
 //   warps 4..19   epilogue, four per TMEM lane quarter: tcgen05.ld -> bias, GELU or its slope, residual -> shared memory -> TMA store
 // A tile is 128 rows of A per CTA x BT rows of B; TMEM lane = row, column = column of the output.  Large products run as CTA pairs
-// (cta_group::2, 256 x 256).  No load is multicast.  Two accumulators, so that a tile's epilogue overlaps the products of the next.
-// Every wait is bounded: on expiry the CTA records QB_ERR_TIMEOUT and leaves through the normal exit path.
+// (cta_group::2, 256 x 256 or 256 x 128).  No load is multicast.  Two accumulators, so that a tile's epilogue overlaps the products of the
+// next.  Every wait is bounded: on expiry the CTA records QB_ERR_TIMEOUT and leaves through the normal exit path.
+//
+// Bound by the tensor cores' operands (after a pause, in us): 24,576 x 4,096, K = 1,024 140 (1,470 TFLOP/s; a library's product 149), 24,576 x
+// 1,024, K = 4,096 140 (141), grad_w 24,576 x 4,096 x 1,024 in fp32 143 (138).  A pair's K block is 64 KB for 512 cycles of products; shared memory is
+// written and read at 64 bytes a clock each, its whole bandwidth, and the tensor pipe is busy for 75 %.  What the epilogue adds shows where K is
+// 1,024 or less: GELU 150, a residual 157 (200 MB more through L2, where the operands come from too), GELU with the
+// pre-activation saved in 8 bits 170 or in 16 bits 171, the gradient through GELU 166 (13 of an element's instructions are GELU's slope).  Small products by
+// their chain: 32 x 768 x 768 4.7 us, of which 0.9 until the kernel before has ended, 0.9 until the first operands are there, 1.6 for six
+// stages, 0.8 from the accumulator to memory.
+// Sixteen epilogue warps on 32 columns each (eight on 64 columns took as long, with GELU for eight values at a time instead of
+// two 10 to 50 us less at 24,576 x 4,096 x 1,024).  Tried and not kept: fp32 sums added up in memory by TMA (10 us more, and longer runs), the columns'
+// sums of grad_bias by the epilogue out of shared memory (14 to 59 us more).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -918,12 +929,13 @@ __global__ void __launch_bounds__(256) column_parts_kernel(const uint16_t* g, in
   }
   if (UNDER && blockIdx.x == 0) pdl_begin();  // (a block that waits keeps its place from those that have not begun)
 }
-// 32 columns a block, eight groups of runs side by side, joined in their order.
-__global__ void __launch_bounds__(256) column_join_kernel(const float* parts, int runs, int32_t N, float* sums) {
-  __shared__ float joined[8][32];
+// 32 columns a block, 32 groups of runs side by side, joined in their order.
+constexpr int kColumnGroups = 32;
+__global__ void __launch_bounds__(32 * kColumnGroups) column_join_kernel(const float* parts, int runs, int32_t N, float* sums) {
+  __shared__ float joined[kColumnGroups][32];
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (int)blockIdx.x * 32 + lane;
-  const int group = (runs + 7) / 8, last = min((warp + 1) * group, runs);
+  const int group = (runs + kColumnGroups - 1) / kColumnGroups, last = min((warp + 1) * group, runs);
   float t = 0.0f;
   if (c < N) {
 #pragma unroll 8
@@ -933,7 +945,7 @@ __global__ void __launch_bounds__(256) column_join_kernel(const float* parts, in
   __syncthreads();
   if (warp == 0 && c < N) {
 #pragma unroll
-    for (int w = 1; w < 8; ++w) t += joined[w][lane];
+    for (int w = 1; w < kColumnGroups; ++w) t += joined[w][lane];
     sums[c] = t;
   }
 }
@@ -1251,7 +1263,7 @@ extern "C" qb_status qb_linear_grad_w(const void* grad_y, const void* x, int typ
                           : (grad_w ? column_parts_kernel<false, true> : column_parts_kernel<false, false>);
     QB_CUDA_TRY(launch_kernel(sum, (unsigned)(col_blocks * runs), 256, 0, stream, 1, false, static_cast<const uint16_t*>(grad_y), M, (int32_t)N, run, col_blocks,
                               (int)(type == QB_F16), parts));
-    QB_CUDA_TRY(launch_kernel(column_join_kernel, (unsigned)lin_up(N, 32), 256, 0, stream, 1, false, parts, (int)runs, (int32_t)N, grad_bias));
+    QB_CUDA_TRY(launch_kernel(column_join_kernel, (unsigned)lin_up(N, 32), 32 * kColumnGroups, 0, stream, 1, false, parts, (int)runs, (int32_t)N, grad_bias));
   }
   return QB_OK;
 }

@@ -207,6 +207,57 @@ def test_codes_of_any_alignment(ws):
     assert torch.equal(qb.linear_grad_x(dy, w.t().contiguous(), ws, through=(moved, scales)), g)
 
 
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("shift", [1, 3, 8])
+@pytest.mark.parametrize("M,N,K", [(70, 136, 64), (600, 1016, 520), (2500, 1024, 136)])
+def test_any_alignment(M, N, K, shift, kind, ws):
+    """Outputs, residuals and pre-activations that begin at any element: the same values as aligned ones, and nothing beside them."""
+    t = TYPES[kind]
+    x, w, r, dy, p = data(3, (M, K), (N, K), (M, N), (M, N), (M, K), t=t)
+
+    def moved(v):
+        b = torch.full((v.numel() + 16,), 7.0, dtype=v.dtype, device="cuda")
+        b[shift:shift + v.numel()] = v.reshape(-1)
+        return b, b[shift:shift + v.numel()].view(v.shape)
+
+    def clean(b, v):
+        return bool((b[:shift] == 7).all() and (b[shift + v.numel():] == 7).all())
+    for o in (t, torch.float32):
+        want = qb.linear(x, w, None, ws, residual=r.to(o), out_dtype=o)
+        (b, y), (_, rm) = moved(torch.empty_like(want)), moved(r.to(o))
+        assert torch.equal(qb.linear(x, w, None, ws, residual=rm, out_dtype=o, y=y), want) and clean(b, y)
+    want, pre = qb.linear(x, w, None, ws, activation="gelu", save="pre")
+    (b, y), (c, z) = moved(torch.empty_like(want)), moved(torch.empty_like(pre))
+    qb.linear(x, w, None, ws, activation="gelu", save="pre", y=y, pre=z)
+    assert torch.equal(y, want) and torch.equal(z, pre) and clean(b, y) and clean(c, z)
+    want = qb.linear_grad_x(dy, w, ws, through=p)
+    (b, g), (_, pm) = moved(torch.empty_like(want)), moved(p)
+    assert torch.equal(qb.linear_grad_x(dy, w, ws, through=pm, grad_x=g), want) and clean(b, g)
+    want, _ = qb.linear_grad_w(dy, x, ws)
+    b, g = moved(torch.empty_like(want))
+    assert torch.equal(qb.linear_grad_w(dy, x, ws, grad_w=g)[0], want) and clean(b, g)
+
+
+def test_offsets_beyond_32_bits(ws):
+    """More than 2^32 bytes of every output: the last rows are as they are alone."""
+    N, K = 4096, 64
+    M = (1 << 31) // N + 300
+    part = torch.randn(512, K, device="cuda").bfloat16()
+    x = part.repeat((M + 511) // 512, 1)[:M].contiguous()
+    w, bias = torch.randn(N, K, device="cuda").bfloat16(), torch.randn(N, device="cuda")
+    r = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda")
+    y, saved = qb.linear(x, w, bias, ws, activation="gelu", residual=r, save="codes")
+    tail = x[-300:].contiguous()
+    y0, saved0 = qb.linear(tail, w, bias, ws, activation="gelu", residual=r[:300], save="codes")
+    assert torch.equal(y[-300:], y0) and torch.equal(saved[0][-300:], saved0[0]) and torch.equal(saved[1][-300:], saved0[1])
+    assert torch.equal(y[:512], y[512 * 100:512 * 101])
+    back = torch.randn(K, N, device="cuda").bfloat16()  # grad_x [M][N] of a linear of N inputs and K outputs
+    g = qb.linear_grad_x(x, back, ws, through=saved, grad_x=r)
+    assert torch.equal(g[-300:], qb.linear_grad_x(tail, back, ws, through=(saved0[0], saved0[1])))
+    dw, db = qb.linear_grad_w(y, x, ws)
+    assert dw.isfinite().all() and db.isfinite().all()
+
+
 def test_refusals(ws):
     x, w, dy, wide = data(2, (64, 96), (40, 96), (64, 40), (64, 264), t=torch.bfloat16)
     bias = torch.zeros(40, device="cuda")
