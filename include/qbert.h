@@ -544,9 +544,12 @@ qb_status qb_gelu_backward(const void* grad_y, int type, const void* pre, const 
  *     qb_linear_grad_x:  grad_x = (grad_y W) * gelu'(p) + residual     (p: the pre-activation that x is GELU of; without it the factor is 1)
  *     qb_linear_grad_w:  grad_w = grad_y^T x,   grad_bias[n] = sum_m grad_y[m][n]
  * grad_y is the gradient of z (behind an activation, qb_gelu_backward or the next linear's qb_linear_grad_x gives it).  Products are
- * accumulated in fp32 (the tensor cores cut an accumulator off at its last place at each addition of 16 products); bias, activation and
- * residual follow in fp32, and each output is rounded once.  qb_linear saves z for the backward pass where asked: in 16 bits (pre) or in 8 (pre_codes and
- * pre_scales, as qb_checkpoint makes them from the fp32 z, where a value next to the border of two codes may get either).
+ * accumulated in fp32.  The tensor cores cut an accumulator off at its last place, towards zero, at each addition of 16 products: fp32
+ * outputs are therefore summed in runs of 512 products, whose sums are added up rounded to nearest; 16-bit outputs in one run of up to 2^16
+ * products (7e-5 of the result at most, far below the type's own rounding), of more than that in parts where the workspace has room.
+ * Bias, activation and residual follow in fp32, and each output is rounded once.  qb_linear saves z for the backward pass where asked: in
+ * 16 bits (pre) or in 8 (pre_codes and pre_scales, as qb_checkpoint makes them from the fp32 z, where a value next to the border of two
+ * codes may get either).
  *   x, grad_x            dev [M][K], w, grad_w  dev [N][K], grad_y  dev [M][N] of `type`: QB_BF16 or QB_F16
  *   y, residual          dev [M][N] of out_type: `type` or QB_F32 (qb_linear; then nothing is saved), [M][K] of `type` (qb_linear_grad_x)
  *   grad_w               of out_type: `type` or QB_F32
@@ -556,8 +559,9 @@ qb_status qb_gelu_backward(const void* grad_y, int type, const void* pre, const 
  * qb_linear_grad_x takes no residual.  grad_w or grad_bias may be NULL (without grad_w x may be too).  M, N and K up to QB_MAX_MN, any size.
  * The sums' order does not change from call to call with the same sizes, workspace size and outputs.
  * The workspace is 16-byte aligned; qb_linear_workspace_bytes(M, N, K) serves the three calls (0 on invalid arguments).  Less will do,
- * except for grad_bias of more than 256 columns or 65,536 values and for tensors whose rows are no multiple of 8 elements, which need their part (else QB_ERR_WORKSPACE); more lets a
- * product of few tiles over a long contraction be summed in more parts side by side.
+ * except for tensors whose rows are no multiple of 8 elements (copies of them) and for a grad_bias of more than 256 columns or of more than
+ * 65,536 values of grad_y (parts of its sums), which need their part (else QB_ERR_WORKSPACE); more lets a product of few tiles over a long
+ * contraction be summed in more parts side by side.
  */
 size_t qb_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 /*
