@@ -8,6 +8,7 @@ import torch
 
 import paper_1909_05840_b200 as qb
 from test_gpu_checkpoint import gelu64, slope64, values64
+from test_gpu_fewer_sms import in_part, part  # noqa: F401 (a fixture)
 from test_gpu_layer_norm import forward64
 
 pytestmark = pytest.mark.gpu
@@ -196,3 +197,13 @@ def test_beside_autograd():
     y.sum().backward()
     assert x.grad.isfinite().all() and w.grad.isfinite().all()
     assert torch.equal(out["x"], b.run()["x"])
+
+
+def test_on_a_part_of_the_device(part):  # noqa: F811
+    """On a stream that has sixteen SMs the grids, made for the whole device, take turns: the same results."""
+    b = Block(2500, 768, 1024, 8)
+    want, got = b.run(), {}
+    in_part(part, lambda: got.update(b.run()))
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+    assert qb.read_status(b.ws) == qb.QB_OK
