@@ -544,9 +544,11 @@ qb_status qb_gelu_backward(const void* grad_y, int type, const void* pre, const 
  *     qb_linear_grad_x:  grad_x = (grad_y W) * gelu'(p) + residual     (p: the pre-activation that x is GELU of; without it the factor is 1)
  *     qb_linear_grad_w:  grad_w = grad_y^T x,   grad_bias[n] = sum_m grad_y[m][n]
  * grad_y is the gradient of z (behind an activation, qb_gelu_backward or the next linear's qb_linear_grad_x gives it).  Products are
- * accumulated in fp32.  The tensor cores cut an accumulator off at its last place, towards zero, at each addition of 16 products: fp32
- * outputs are therefore summed in runs of 512 products, whose sums are added up rounded to nearest; 16-bit outputs in one run of up to 2^16
- * products (7e-5 of the result at most, far below the type's own rounding), of more than that in parts where the workspace has room.
+ * accumulated in fp32.  The tensor cores cut an accumulator off at its last place, towards zero, at each addition of 16 products: a run of n
+ * products is off by n / 16 * 2^-23 of its sum of magnitudes at most, and for random signs by about n * 1.2e-9 of the result's norm (a value
+ * whose terms cancel by more of itself).  fp32 outputs are therefore summed in runs of 512 products, whose sums are added up rounded to nearest
+ * (5e-7 of the norm); 16-bit outputs in one run of up to 65,536 products in bfloat16 and 16,384 in fp16 (8e-5 and 2e-5, where the types'
+ * own rounding is 1.7e-3 and 2.1e-4), over longer contractions in runs of 8,192, whatever the workspace and whatever is saved.
  * Bias, activation and residual follow in fp32, and each output is rounded once.  qb_linear saves z for the backward pass where asked: in
  * 16 bits (pre) or in 8 (pre_codes and pre_scales, as qb_checkpoint makes them from the fp32 z, where a value next to the border of two
  * codes may get either).

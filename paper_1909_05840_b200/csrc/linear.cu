@@ -43,6 +43,8 @@ namespace qb {
 // How an operand lies and is loaded, two K blocks of 64 at a time: K-major (rows x 2 groups of 64 columns) or MN-major (128 rows along
 // K x groups of 64 columns); one box of three dimensions, or, where rows are no multiple of 128 bytes, a box per group.
 enum LinearForm { kRows = 0, kRows2 = 1, kCols = 2, kCols2 = 3 };
+// The output: of the operands' type, fp32, or of their type from several runs over K.
+enum LinearOut { kOut16 = 0, kOut32 = 1, kOut16Runs = 2 };
 // What the epilogue does with the product besides bias, residual and what is saved.
 enum LinearMode { kPlain = 0, kGelu = 1, kSlope = 2 };
 
@@ -67,7 +69,7 @@ struct LinearParams {
   int32_t split_tiles;   // tiles of one split of K (split s writes rows s * M .. of out, fp32)
   int32_t split_blocks;  // K blocks of 64 per split, even where there are several
   int32_t k_blocks;      // of all splits
-  int32_t run_blocks;    // K blocks that one accumulator sums; even where there are several such runs (fp32 out), which registers add up
+  int32_t run_blocks;    // K blocks that one accumulator sums; even where there are several such runs, which registers add up
   int32_t tma_store;     // 1: rows of out are 16-byte aligned
   int32_t vector;        // 1: rows of side and of pre are 16-byte aligned, 2: 32-byte aligned
   int32_t vector_codes;  // the same of the codes'
@@ -212,11 +214,11 @@ __device__ __forceinline__ void send_rows16(const uint8_t* buf, uint16_t* to, in
   }
 }
 
-// OUT32: out is fp32, else of the operands' type.  A chunk is 64 bytes of out: 16 or 32 columns.
-// HALF: the 16-bit tensors are fp16, else bfloat16.
-template <int BT, int CG, bool OUT32, int MODE, bool HALF>
+// A chunk is 64 bytes of out: 16 or 32 columns.  HALF: the 16-bit tensors are fp16, else bfloat16.
+template <int BT, int CG, int OUT, int MODE, bool HALF>
 __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_constant__ LinearParams gp) {
   using Cfg = LinCfg<BT, CG>;
+  constexpr bool OUT32 = OUT == kOut32;
   constexpr int kStages = Cfg::kStages;
   const uint32_t rank = CG == 2 ? ptx::cluster_ctarank() : 0u;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -651,10 +653,11 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           __syncwarp();
         }
       };
-      if (!OUT32 && chunk(0) < chunks) fetch(chunk(0) * kCols);
+      const bool beside = !OUT32 && chunk(0) < chunks;
+      if (OUT != kOut16Runs && beside) fetch(chunk(0) * kCols);
       bool ok;
-      if constexpr (OUT32) {  // the runs before the last are added up in registers, and to the last one where it lies
-        constexpr int kChunks = BT / kCols / 4;  // of a warp
+      if constexpr (OUT != kOut16) {  // the runs before the last are added up in registers, and to the last one where it lies
+        constexpr int kChunks = OUT32 ? BT / kCols / 4 : 2;  // of a warp
         float sums[kChunks][kCols] = {};
         int run = tile.k0;
         while (true) {
@@ -662,10 +665,10 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           if (!ok || run + gp.run_blocks >= tile.k1) break;
 #pragma unroll
           for (int j = 0; j < kChunks; ++j) {
-            if (part + 4 * j < chunks) {
+            if (chunk(j) < chunks) {
 #pragma unroll
               for (int h = 0; h < kCols; h += 8) {
-                add_accumulator(lanes + (uint32_t)((it & 1) * BT + (part + 4 * j) * kCols + h), sums[j] + h);
+                add_accumulator(lanes + (uint32_t)((it & 1) * BT + chunk(j) * kCols + h), sums[j] + h);
               }
             }
           }
@@ -676,10 +679,10 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         if (ok && run > tile.k0) {
 #pragma unroll
           for (int j = 0; j < kChunks; ++j) {
-            if (part + 4 * j < chunks) {
+            if (chunk(j) < chunks) {
 #pragma unroll
               for (int h = 0; h < kCols; h += 8) {
-                const uint32_t at = lanes + (uint32_t)((it & 1) * BT + (part + 4 * j) * kCols + h);
+                const uint32_t at = lanes + (uint32_t)((it & 1) * BT + chunk(j) * kCols + h);
                 add_accumulator(at, sums[j] + h);
                 ptx::tmem_st_32x32b_x8(at, sums[j] + h);
               }
@@ -690,6 +693,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       } else {
         ok = wait_run();
       }
+      if (OUT == kOut16Runs && beside) fetch(chunk(0) * kCols);  // (behind the sums, which take the registers)
       if (!ok) break;
       if (chunk(0) >= chunks) arrive(acc_empty(it & 1));
       float top = 0.0f;
@@ -733,10 +737,10 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
   }
 }
 
-template <int BT, int CG, bool OUT32, int MODE, bool HALF>
+template <int BT, int CG, int OUT, int MODE, bool HALF>
 static qb_status launch_linear_form(const LinearParams& gp, int sms, cudaStream_t stream) {
   using Cfg = LinCfg<BT, CG>;
-  auto kernel = linear_kernel<BT, CG, OUT32, MODE, HALF>;
+  auto kernel = linear_kernel<BT, CG, OUT, MODE, HALF>;
   static std::atomic<bool> attr_set[64] = {};
   int dev = 0;
   QB_CUDA_TRY(cudaGetDevice(&dev));
@@ -748,16 +752,19 @@ static qb_status launch_linear_form(const LinearParams& gp, int sms, cudaStream_
   QB_CUDA_TRY(launch_kernel(kernel, (unsigned)grid, kLinThreads, Cfg::kSmemBytes, stream, CG, false, gp));
   return QB_OK;
 }
-template <int BT, int CG, bool HALF>
-static qb_status launch_linear_type(const LinearParams& gp, bool out32, int mode, int sms, cudaStream_t stream) {
-  // (with fp32 out the type of the 16-bit tensors is in the instruction descriptor alone)
-  if (out32) return mode == kGelu ? launch_linear_form<BT, CG, true, kGelu, false>(gp, sms, stream) : launch_linear_form<BT, CG, true, kPlain, false>(gp, sms, stream);
-  if (mode == kSlope) return launch_linear_form<BT, CG, false, kSlope, HALF>(gp, sms, stream);
-  return mode == kGelu ? launch_linear_form<BT, CG, false, kGelu, HALF>(gp, sms, stream) : launch_linear_form<BT, CG, false, kPlain, HALF>(gp, sms, stream);
+template <int BT, int CG, int OUT, bool HALF>
+static qb_status launch_linear_mode(const LinearParams& gp, int mode, int sms, cudaStream_t stream) {
+  if constexpr (OUT != kOut32) {
+    if (mode == kSlope) return launch_linear_form<BT, CG, OUT, kSlope, HALF>(gp, sms, stream);
+  }
+  return mode == kGelu ? launch_linear_form<BT, CG, OUT, kGelu, HALF>(gp, sms, stream) : launch_linear_form<BT, CG, OUT, kPlain, HALF>(gp, sms, stream);
 }
 template <int BT, int CG>
-static qb_status launch_linear(const LinearParams& gp, bool out32, int mode, bool half_type, int sms, cudaStream_t stream) {
-  return half_type ? launch_linear_type<BT, CG, true>(gp, out32, mode, sms, stream) : launch_linear_type<BT, CG, false>(gp, out32, mode, sms, stream);
+static qb_status launch_linear(const LinearParams& gp, int out, int mode, bool half_type, int sms, cudaStream_t stream) {
+  // (with fp32 out the type of the 16-bit tensors is in the instruction descriptor alone)
+  if (out == kOut32) return launch_linear_mode<BT, CG, kOut32, false>(gp, mode, sms, stream);
+  if (out == kOut16Runs) return half_type ? launch_linear_mode<BT, CG, kOut16Runs, true>(gp, mode, sms, stream) : launch_linear_mode<BT, CG, kOut16Runs, false>(gp, mode, sms, stream);
+  return half_type ? launch_linear_mode<BT, CG, kOut16, true>(gp, mode, sms, stream) : launch_linear_mode<BT, CG, kOut16, false>(gp, mode, sms, stream);
 }
 
 // What stands behind a product, as the join of a split one needs it.
@@ -979,9 +986,15 @@ static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintpt
 static int64_t lin_up(int64_t n, int64_t m) { return (n + m - 1) / m; }
 
 // The tensor cores cut an accumulator off at its last place at each addition of 16 products, always towards zero: the error grows
-// with their number (24,576 products of random signs: 2.8e-5 of the result).  fp32 outputs are summed in runs of this many K blocks, which
-// the epilogue's registers add up, rounded to nearest: the error is then that of fp32 products.
+// with their number (24,576 products of random signs: 2.8e-5 of the result's norm).  fp32 outputs are summed in runs of this many K blocks,
+// which the epilogue's registers add up, rounded to nearest: the error is then that of fp32 products.
 constexpr int kLinRunBlocks = 8;
+// 16-bit outputs are summed in one run as long as that costs less than a tenth of their own rounding (2.1e-4 of the norm in fp16, 1.7e-3 in
+// bfloat16), else in runs of 8,192 products (1e-5).  The sums of runs take registers that a single run's epilogue has for itself: a kernel that can do both took
+// 156 us instead of 150 at 24,576 x 4,096 x 1,024 with GELU, with the pre-activation saved in codes 188 instead of 173 (80 to 150 bytes a thread
+// are spilled).
+constexpr int kLinRunBlocks16 = 128;
+static int64_t single_run_blocks(bool half_type) { return half_type ? 256 : 1024; }
 constexpr size_t kLinScratchOff = 1024;  // of what calls keep in the workspace besides its header
 
 // The form of a product: CTAs per tile, columns, for pairs how many tiles are whole, and splits of K.
@@ -995,8 +1008,7 @@ struct LinearChoice {
 // 17.0, 19.6, 24.9; 613 x 768 x 768 6.3, 6.3, 6.0, 5.2.  A last round that fills at most half of the pairs is cut into tiles of half the
 // width (5,003 x 1,024 x 4,096 42.9 -> 34.8 us).  Where a long K meets few tiles, K is split into runs whose sums a second kernel joins: that
 // costs its launch and the traffic of the parts.
-// `parts`: more than one split where the workspace has room for it.
-static LinearChoice choose_linear(int64_t M, int64_t N, int64_t K, int sms, size_t scratch, bool parts) {
+static LinearChoice choose_linear(int64_t M, int64_t N, int64_t K, int sms, size_t scratch) {
   static constexpr struct {
     int cg, bt, block, fixed, launch;
   } kForms[] = {{2, 256, 29, 40, 560}, {2, 128, 16, 70, 370}, {1, 128, 20, 80, 300}, {1, 64, 16, 20, 290}};
@@ -1006,12 +1018,11 @@ static LinearChoice choose_linear(int64_t M, int64_t N, int64_t K, int sms, size
   for (const auto& f : kForms) {
     if (f.cg == 2 && sms < 2) continue;
     const int64_t groups = sms / f.cg, tiles = lin_up(M, 128 * f.cg) * lin_up(N, f.bt);
-    for (int64_t splits = 1; splits == 1 || (4 * splits <= blocks && (tiles * (splits - 1) < groups || (parts && splits == 2)) && splits * M * N * 4 <= (int64_t)scratch); ++splits) {
+    for (int64_t splits = 1; splits == 1 || (4 * splits <= blocks && tiles * (splits - 1) < groups && splits * M * N * 4 <= (int64_t)scratch); ++splits) {
       const int64_t run = splits == 1 ? blocks : lin_up(lin_up(blocks, splits), 2) * 2;
       if (lin_up(blocks, run) != splits) continue;
       const int64_t tile = f.block * run + f.fixed, all = tiles * splits, last = all % groups;
       const bool halves = f.bt == 256 && splits == 1 && last > 0 && 2 * last <= groups;
-      if (parts && splits == 1 && blocks >= 8 && 2 * M * N * 4 <= (int64_t)scratch) continue;
       const int64_t cost = f.launch + (all / groups) * tile + (halves ? tile * 6 / 10 : (last > 0 ? tile : 0)) + (splits > 1 ? 200 + splits * M * N / 15000 : 0);
       if (best.cg == 0 || cost < best_cost) {
         best_cost = cost;
@@ -1080,12 +1091,12 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   qb_status st;
   if ((st = padded(&a, &a_pitch, &scratch, sms, what, stream)) != QB_OK) return st;
   if ((st = padded(&b, &b_pitch, &scratch, sms, what, stream)) != QB_OK) return st;
-  // a 16-bit output is summed in one run up to 2^16 products (the sums' error is then below a tenth of its rounding)
   const int64_t blocks = lin_up(K, 64);
-  const LinearChoice choice = choose_linear(M, N, K, sms, pre_codes ? 0 : scratch.left, tail.out_type != QB_F32 && blocks > 1024);
+  const LinearChoice choice = choose_linear(M, N, K, sms, pre_codes ? 0 : scratch.left);
   const int cg = choice.cg, bt = choice.bt;
   const bool split = choice.splits > 1;
   const bool out32 = split || tail.out_type == QB_F32;
+  const int out = out32 ? kOut32 : (blocks > single_run_blocks(half_type) ? kOut16Runs : kOut16);
   float* const parts = reinterpret_cast<float*>(scratch.at);
   LinearParams gp;
   if ((st = operand_map(&gp.tma, &gp.a_form, a, a_pitch, 128, half_type)) != QB_OK) return st;
@@ -1122,13 +1133,13 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   gp.split_tiles_inv = quick_inverse((uint32_t)gp.split_tiles);
   gp.split_blocks = choice.split_blocks;
   gp.k_blocks = (int32_t)blocks;
-  gp.run_blocks = out32 ? kLinRunBlocks : (int32_t)blocks;
+  gp.run_blocks = out == kOut32 ? kLinRunBlocks : (out == kOut16Runs ? kLinRunBlocks16 : (int32_t)blocks);
   gp.idesc = lin_idesc(half_type, a.mn, b.mn, 128 * cg);
   const int mode = split ? kPlain : tail.mode;
-  if (cg == 2 && bt == 128) st = launch_linear<128, 2>(gp, out32, mode, half_type, sms, stream);
-  else if (cg == 2) st = launch_linear<256, 2>(gp, out32, mode, half_type, sms, stream);
-  else if (bt == 128) st = launch_linear<128, 1>(gp, out32, mode, half_type, sms, stream);
-  else st = launch_linear<64, 1>(gp, out32, mode, half_type, sms, stream);
+  if (cg == 2 && bt == 128) st = launch_linear<128, 2>(gp, out, mode, half_type, sms, stream);
+  else if (cg == 2) st = launch_linear<256, 2>(gp, out, mode, half_type, sms, stream);
+  else if (bt == 128) st = launch_linear<128, 1>(gp, out, mode, half_type, sms, stream);
+  else st = launch_linear<64, 1>(gp, out, mode, half_type, sms, stream);
   if (st != QB_OK) return st;
   if (!split) return QB_OK;
   const bool vector = N % 4 == 0;
@@ -1178,7 +1189,7 @@ extern "C" int32_t qb_linear_tile_columns(int64_t M, int64_t N, int64_t K, size_
   if (impossible_linear(M, N, K)) return 0;
   int sms = 148;
   require_sm100(&sms);  // without a device: for a 148-SM part
-  const LinearChoice c = choose_linear(M, N, K, sms, ws_bytes > kLinScratchOff ? ws_bytes - kLinScratchOff : 0, false);
+  const LinearChoice c = choose_linear(M, N, K, sms, ws_bytes > kLinScratchOff ? ws_bytes - kLinScratchOff : 0);
   if (rows) *rows = 128 * c.cg;
   if (half_tiles) *half_tiles = c.tiles - c.whole;
   if (splits) *splits = c.splits;
