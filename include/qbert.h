@@ -499,8 +499,11 @@ qb_status qb_vocab_loss_backward(const uint16_t* h, const uint16_t* w, const flo
  *     mean = sum_d x[d] / D,   rstd = 1 / sqrt(sum_d (x[d] - mean)^2 / D + eps),   y = (x - mean) * rstd * gamma + beta
  * and, with xhat = (x - mean) * rstd and g = grad_y * gamma,
  *     grad_x = rstd * (g - sum_d g / D - xhat * sum_d g xhat / D),   grad_gamma = sum_m grad_y * xhat,   grad_beta = sum_m grad_y.
- * Everything is held in fp32 and rounded to `type` once at the end; the squares are summed of differences from the mean.  The sums'
- * order does not change from call to call.  A row with a NaN or an infinity gives NaN, and in the backward pass reaches grad_gamma.
+ * Everything is held in fp32 and rounded to `type` once at the end; the squares are summed of differences from the mean.  The forward pass
+ * takes the mean unrounded, so that rows far from 0 lose nothing (a constant row gives beta where eps > 0); `mean` is the fp32 number next to it, and xhat of the
+ * backward pass, which reads it, is off by up to 2^-24 |mean| rstd.  The squares of a row's differences must add up to a finite fp32
+ * number.  The sums' order does not change from call to call.  A row with a NaN or an infinity gives NaN, and in the backward pass reaches
+ * grad_gamma.
  *   x, grad_y    dev [M][D] of `type`, aligned to their elements                             (read)
  *   gamma, beta  dev fp32 [D], or NULL: ones, zeros                                          (read)
  *   y, grad_x    dev [M][D] of `type`, aligned to their elements; y may be x, grad_x may be grad_y or x   (written)

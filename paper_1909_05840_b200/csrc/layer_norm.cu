@@ -2,11 +2,11 @@
 //
 // A row of up to 1,024 elements is held by one warp, 32 elements a lane; up to 8,192 by two, four or eight warps, which join their sums
 // through shared memory; beyond, a block goes over it as often as it needs it (the second time from L2).  Each element is read once into
-// registers, so that the variance is a sum of squared differences from the mean that is known by then.
+// registers, so that the variance is a sum of squared differences from the mean that is known by then (and of what rounding the mean left).
 // Backward: a block keeps the sums of grad_y * xhat and grad_y over its rows in registers, a pair a column, and leaves them in the
 // workspace at its end; a second kernel sums the blocks', always in the same order.
-// Bound by memory: one read and one write of the tensor forward, two reads and one write backward.  24,576 x 1,024: bfloat16 forward 19.5 us
-// (5.2 TB/s), backward 30.5 (4.9), fp32 35 (5.7) and 53 (5.7); 5,003 x 1,024 bfloat16 6.6 and 13.1; 32 x 768 2.4 and 4.3.  About 4 us
+// Bound by memory: one read and one write of the tensor forward, two reads and one write backward.  24,576 x 1,024: bfloat16 forward 19.9 us
+// (5.1 TB/s), backward 30.5 (4.9), fp32 34.7 (5.8) and 53 (5.7); 5,003 x 1,024 bfloat16 6.9 and 13.1; 32 x 768 2.4 and 4.3.  About 4 us
 // of a backward pass are its start, its blocks' sums and the second kernel.  Rows on their way in shared memory cost no registers (forward 20.4
 // with the next row in registers, 27.4 with one row a warp and a block that ends).  Tried and not kept, backward, 24,576 x 1,024 bfloat16: two warps a row with
 // sixteen elements a lane 45 us, two blocks per SM with gamma in shared memory 41, two rows a warp at a time 31.
@@ -190,22 +190,23 @@ struct NormMath {
   }
 };
 
-__device__ __forceinline__ float warp_sum(float s) {
+template <class A>
+__device__ __forceinline__ A warp_sum(A s) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
   return s;
 }
-// The sum over the WPR warps of a row.  `slots`: [2][8 warps], used in turn; every warp of the block calls it as often.
-template <int WPR>
-__device__ __forceinline__ float row_sum(float s, float (*slots)[8], int turn, int warp, int lane) {
+// The sum over the WPR warps of a row.  `slots`: of this call alone until every warp of the block has met the next one's barrier.
+template <int WPR, class A>
+__device__ __forceinline__ A row_sum(A s, A* slots, int warp, int lane) {
   s = warp_sum(s);
   if constexpr (WPR > 1) {
-    if (lane == 0) slots[turn][warp] = s;
+    if (lane == 0) slots[warp] = s;
     __syncthreads();
-    s = 0.0f;
+    s = 0;
     const int first = warp / WPR * WPR;
 #pragma unroll
-    for (int i = 0; i < WPR; ++i) s += slots[turn][first + i];
+    for (int i = 0; i < WPR; ++i) s += slots[first + i];
   }
   return s;
 }
@@ -217,7 +218,32 @@ struct NormArgs {
   int64_t M;
   int32_t D;
   float eps, inv_d;
+  double inv64;
   int32_t vector_weights;
+};
+
+// A row's mean: an fp32 number next to it, and what that leaves, `delta`.  Rows whose mean is far above their deviations need both (with a
+// mean one unit of its last place off, a constant row gives rstd times that unit), and a sum that is good for them: 16-bit values of one
+// binade have 11 bits, so that 8,192 of them add up in fp32 without rounding; of fp32 values a lane sums the differences from its first
+// one, and the lanes' sums are added in 64 bits; longer rows are summed as differences, twice.  24,576 x 1,024: bfloat16 19.9 us (19.1
+// with the mean alone), fp32 34.7 (34.0); all sums as differences, twice: 20.9 and 34.7; fp32 element by element in 64 bits: 34.7, 32 x 768 2.75 instead of 2.6.
+struct NormMean {
+  float mean, delta;
+  __device__ __forceinline__ NormMean(float mean, float delta) : mean(mean), delta(delta) {}
+  __device__ __forceinline__ NormMean(float sum, int D, float inv_d, double) {
+    mean = sum * inv_d;
+    mean = fmaf(fmaf(-mean, (float)D, sum), inv_d, mean);
+    delta = fmaf(-mean, (float)D, sum) * inv_d;
+  }
+  __device__ __forceinline__ NormMean(double sum, int D, float inv_d, double inv64) {
+    mean = (float)(sum * inv64);
+    delta = (float)fma(-(double)mean, (double)D, sum) * inv_d;
+  }
+  // 1 / sqrt(variance + eps) from the sum of (x - mean)^2
+  __device__ __forceinline__ float rstd(float sum2, float inv_d, float eps) const {
+    const float var = fmaf(-delta, delta, sum2 * inv_d);
+    return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);  // (a NaN stays one)
+  }
 };
 
 // A block goes over its share of the rows with the weights in registers and the next rows on their way.
@@ -228,7 +254,9 @@ __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x,
   typedef NormMath<V> Math;
   typedef typename Math::F F;
   constexpr int W = Math::W;
-  __shared__ float slots[2][2][8];
+  typedef std::conditional_t<sizeof(T) == 4, double, float> Sum;
+  __shared__ Sum slots[2][8];
+  __shared__ float slots2[2][8];
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.D;
   const int first = ((warp % WPR) * 32 + lane) * V;
@@ -255,6 +283,9 @@ __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x,
       norm_weights<V>(a.beta, c, 0.0f, a.vector_weights, beta + i * V);
     }
   }
+  float n = 0.0f;  // how many of a row's elements are the lane's
+#pragma unroll
+  for (int i = 0; i < Row::kVectors; ++i) n += first + i * Row::kStride < D ? (float)V : 0.0f;
   int turn = 0;
   for (int64_t m0 = (int64_t)blockIdx.x * (8 / WPR); m0 < a.M; m0 += step, m += step, turn ^= 1) {
     const int end = m < a.M ? D : 0;
@@ -268,15 +299,33 @@ __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x,
       r.load(x + (end ? m : 0) * D, first, end);
     }
     F s = Math::all(0.0f);
+    Sum sum;
+    if constexpr (sizeof(T) == 4) {  // the lane's elements: n times the first one, and the differences from it
+      float one[V];
+      r.get(0, one);
+      const F minus_one = Math::all(-one[0]);
 #pragma unroll
-    for (int i = 0; i < Row::kVectors; ++i) {
-      float f[V];
-      r.get(i, f);
+      for (int i = 0; i < Row::kVectors; ++i) {
+        if (first + i * Row::kStride < end) {
+          float f[V];
+          r.get(i, f);
 #pragma unroll
-      for (int j = 0; j < V; j += W) s = Math::add(s, Math::from(f + j));
+          for (int j = 0; j < V; j += W) s = Math::add(s, Math::add(Math::from(f + j), minus_one));
+        }
+      }
+      sum = fma((double)n, (double)one[0], (double)Math::sum(s));
+    } else {
+#pragma unroll
+      for (int i = 0; i < Row::kVectors; ++i) {
+        float f[V];
+        r.get(i, f);
+#pragma unroll
+        for (int j = 0; j < V; j += W) s = Math::add(s, Math::from(f + j));
+      }
+      sum = Math::sum(s);
     }
-    const float mean = row_sum<WPR>(Math::sum(s), slots[turn], 0, warp, lane) * a.inv_d;
-    const F minus_mean = Math::all(-mean);
+    const NormMean st(row_sum<WPR>(sum, slots[turn], warp, lane), D, a.inv_d, a.inv64);
+    const F minus_mean = Math::all(-st.mean);
     s = Math::all(0.0f);
 #pragma unroll
     for (int i = 0; i < Row::kVectors; ++i) {
@@ -290,8 +339,8 @@ __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x,
         }
       }
     }
-    const float rstd = 1.0f / sqrtf(row_sum<WPR>(Math::sum(s), slots[turn], 1, warp, lane) * a.inv_d + a.eps);
-    const F all_rstd = Math::all(rstd);
+    const float rstd = st.rstd(row_sum<WPR>(Math::sum(s), slots2[turn], warp, lane), a.inv_d, a.eps);
+    const F all_rstd = Math::all(rstd), minus_delta = Math::all(-st.delta * rstd);
 #pragma unroll
     for (int i = 0; i < Row::kVectors; ++i) {
       const int c = first + i * Row::kStride;
@@ -300,12 +349,12 @@ __global__ void __launch_bounds__(kNormThreads, 2) layer_norm_kernel(const T* x,
         r.get(i, f);
 #pragma unroll
         for (int j = 0; j < V; j += W)
-          Math::to(f + j, Math::fma(Math::mul(Math::add(Math::from(f + j), minus_mean), all_rstd), Math::from(gamma + i * V + j), Math::from(beta + i * V + j)));
+          Math::to(f + j, Math::fma(Math::fma(Math::add(Math::from(f + j), minus_mean), all_rstd, minus_delta), Math::from(gamma + i * V + j), Math::from(beta + i * V + j)));
         Row::put(y + m * D, c, f);
       }
     }
     if (a.mean && end && warp % WPR == 0 && lane == 0) {
-      a.mean[m] = mean;
+      a.mean[m] = st.mean;
       a.rstd[m] = rstd;
     }
   }
@@ -331,19 +380,22 @@ __global__ void __launch_bounds__(kNormThreads) layer_norm_long_kernel(const T* 
   const int D = a.D;
   for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
     const T* const row = x + m * D;
-    float s = 0.0f;
-    for (int c = threadIdx.x; c < D; c += kNormThreads) s += to_float(row[c]);
-    const float mean = block_sum(s, slots) * a.inv_d;
+    const float shift = to_float(row[0]);
+    float s = 0.0f, s2 = 0.0f;
+    for (int c = threadIdx.x; c < D; c += kNormThreads) s += to_float(row[c]) - shift;
+    const float mean = fmaf(block_sum(s, slots), a.inv_d, shift);
     s = 0.0f;
     for (int c = threadIdx.x; c < D; c += kNormThreads) {
       const float d = to_float(row[c]) - mean;
-      s = __fmaf_rn(d, d, s);
+      s += d;
+      s2 = __fmaf_rn(d, d, s2);
     }
-    const float rstd = 1.0f / sqrtf(block_sum(s, slots) * a.inv_d + a.eps);
+    const NormMean st(mean, block_sum(s, slots) * a.inv_d);
+    const float rstd = st.rstd(block_sum(s2, slots), a.inv_d, a.eps), minus_delta = -st.delta * rstd;
     for (int c = threadIdx.x; c < D; c += kNormThreads)  // (y may be x: each element is read and written by one thread)
-      y[m * D + c] = from_float<T>(__fmaf_rn((to_float(row[c]) - mean) * rstd, a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f));
+      y[m * D + c] = from_float<T>(__fmaf_rn(__fmaf_rn(to_float(row[c]) - mean, rstd, minus_delta), a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f));
     if (a.mean && threadIdx.x == 0) {
-      a.mean[m] = mean;
+      a.mean[m] = mean + st.delta;
       a.rstd[m] = rstd;
     }
   }
@@ -651,7 +703,7 @@ extern "C" qb_status qb_layer_norm(const void* x, int type, const float* gamma, 
   }
   int sms = 0;
   if ((st = require_sm100(&sms)) != QB_OK) return st;
-  const NormArgs a = {gamma, beta, mean, rstd, M, (int32_t)D, (float)eps, (float)(1.0 / (double)D), aligned16(gamma) && aligned16(beta)};
+  const NormArgs a = {gamma, beta, mean, rstd, M, (int32_t)D, (float)eps, (float)(1.0 / (double)D), 1.0 / (double)D, aligned16(gamma) && aligned16(beta)};
   switch (type) {
     case QB_F32: return launch_norm<float>(x, y, a, sms, (cudaStream_t)cuda_stream);
     case QB_BF16: return launch_norm<__nv_bfloat16>(x, y, a, sms, (cudaStream_t)cuda_stream);
