@@ -17,6 +17,7 @@ namespace qb {
 // [32]  uint64 ticket            launches that cleared slots << 32 | blocks of the running one that have started
 // [40]  uint32 cleared           number of the last such launch whose reduction slots are clear
 // [44]  uint32 round             counts the launches whose clusters waited for one another
+// [48]  uint32 begun             mark of a running product whose begin a kernel that runs under it has to see; else 0
 // [64]  uint64 cluster_max[24]   round << 32 | bit pattern of a cluster's max|x|, all of the last such launch
 // [256] uint32 range_hi_enc[G], uint32 range_lo_inv[G]   ordered encodings of per-group max / min
 //       or, weight_ring_kernel: uint64 [groups][CTAs], encoded max << 32 | inverted encoded min
@@ -36,7 +37,8 @@ struct WsHeader {
   unsigned long long ticket;
   uint32_t cleared;
   uint32_t round;
-  uint32_t pad3[4];
+  uint32_t begun;
+  uint32_t pad3[3];
   unsigned long long cluster_max[kWsClusters];
 };
 static_assert(sizeof(WsHeader) == kWsRangeOff, "the tables follow the header");

@@ -8,7 +8,7 @@
 // transposed in memory.  20 warps:
 //   warp 0        TMA producer (one lane)
 //   warp 1        issues tcgen05.mma, owns the tensor memory (one lane)
-//   warps 2..3    idle
+//   warps 2..3    idle (one thread leaves the call's mark: begin_under)
 //   warps 4..19   epilogue, four per TMEM lane quarter: tcgen05.ld -> bias, GELU or its slope, residual -> shared memory -> TMA store
 // A tile is 128 rows of A per CTA x BT rows of B; TMEM lane = row, column = column of the output.  Large products run as CTA pairs
 // (cta_group::2, 256 x 256 or 256 x 128).  No load is multicast.  Two accumulators, so that a tile's epilogue overlaps the products of the
@@ -74,6 +74,7 @@ struct LinearParams {
   int32_t vector;        // 1: rows of side and of pre are 16-byte aligned, 2: 32-byte aligned
   int32_t vector_codes;  // the same of the codes'
   uint32_t idesc;
+  uint32_t mark;         // even where a kernel of this call will run under this one: left in the workspace (begin_under)
 };
 
 constexpr int kLinEpilogueWarps = 16;
@@ -722,6 +723,8 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       ++it;
     }
     if (lane == 0) ptx::tma_store_wait_read0();  // the buffers are in use until then
+  } else if (gp.mark != 0 && blockIdx.x == 0 && threadIdx.x == 64) {  // (by an idle warp)
+    st_release(&static_cast<WsHeader*>(gp.ws)->begun, gp.mark);
   }
   if (timed_out) {
     *abort_flag = 1;
@@ -888,13 +891,31 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* from, uin
 
 // Sums of the columns of g [M][N] over its rows, first over runs of rows into parts [runs][N], then over the runs, in their order.
 // UNDER: the kernel before this one on the stream is of this call, the product or the join of its parts, which neither writes what is read
-// here nor touches the parts.  Its blocks let this kernel's begin once all kernels before it are done and their results visible
-// (pdl_begin), so that these are read without waiting for it, on SMs that it leaves (24,576 x 4,096, K = 1,024: grad_w 143 us, with
-// grad_bias 151, one after the other 181); one block waits at its end, so that the kernels that follow find both done.
+// here nor touches the parts, so that this kernel does not wait for its end, and runs on SMs that it leaves (24,576 x 4,096, K = 1,024: grad_w
+// 143 us, with grad_bias 151, one after the other 181).  One block waits at its end, so that the kernels that follow find both done.
+//
+// What the kernels before the product wrote is visible to the product, which has waited for it (pdl_begin), but not thereby to a grid that has
+// not waited itself.  So the product leaves a mark of its call behind its wait, by a release; who acquires it has behind him all that the
+// product had.  A block that does not find it within some microseconds waits for the product's end instead.  The last kernel of the
+// call takes the mark away, and every call has one of its own, so that none is mistaken for that of an earlier replay or of a call
+// whose later launches failed.
+__device__ __forceinline__ void begin_under(const void* ws, uint32_t mark) {
+  const int seen = threadIdx.x == 0 && poll_word(&static_cast<const WsHeader*>(ws)->begun, mark, 20000);
+  if (!__syncthreads_or(seen)) pdl_begin();
+}
+static uint32_t next_mark() {
+  static std::atomic<uint32_t> last{0};
+  uint32_t mark;
+  while ((mark = last.fetch_add(1, std::memory_order_relaxed) + 1) == 0) {
+  }
+  return mark;
+}
 template <bool VECTOR, bool UNDER>
-__global__ void __launch_bounds__(256) column_parts_kernel(const uint16_t* g, int64_t M, int32_t N, int64_t run, int col_blocks, int half_type, float* parts) {
+__global__ void __launch_bounds__(256) column_parts_kernel(const uint16_t* g, int64_t M, int32_t N, int64_t run, int col_blocks, int half_type, float* parts,
+                                                          const void* ws, uint32_t mark) {
   __shared__ float sums[8][256];
-  if constexpr (!UNDER) pdl_begin();
+  if constexpr (UNDER) begin_under(ws, mark);
+  else pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t which = blockIdx.x / col_blocks, first = which * run, last = min(first + run, M);
   const int n0 = ((int)blockIdx.x - (int)which * col_blocks) * 256;
@@ -936,11 +957,12 @@ __global__ void __launch_bounds__(256) column_parts_kernel(const uint16_t* g, in
   }
   if (UNDER && blockIdx.x == 0) pdl_begin();  // (a block that waits keeps its place from those that have not begun)
 }
-// 32 columns a block, 32 groups of runs side by side, joined in their order.
+// 32 columns a block, 32 groups of runs side by side, joined in their order.  ws: where the mark of begin_under is, or NULL.
 constexpr int kColumnGroups = 32;
-__global__ void __launch_bounds__(32 * kColumnGroups) column_join_kernel(const float* parts, int runs, int32_t N, float* sums) {
+__global__ void __launch_bounds__(32 * kColumnGroups) column_join_kernel(const float* parts, int runs, int32_t N, float* sums, void* ws) {
   __shared__ float joined[kColumnGroups][32];
   pdl_begin();
+  if (ws && blockIdx.x == 0 && threadIdx.x == 0) static_cast<WsHeader*>(ws)->begun = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (int)blockIdx.x * 32 + lane;
   const int group = (runs + kColumnGroups - 1) / kColumnGroups, last = min((warp + 1) * group, runs);
   float t = 0.0f;
@@ -961,9 +983,10 @@ __global__ void __launch_bounds__(32 * kColumnGroups) column_join_kernel(const f
 constexpr int kFewColumns = 256;
 constexpr int64_t kFewValues = 65536;
 template <bool UNDER>
-__global__ void __launch_bounds__(1024) column_few_kernel(const uint16_t* g, int64_t M, int32_t N, int half_type, float* sums) {
+__global__ void __launch_bounds__(1024) column_few_kernel(const uint16_t* g, int64_t M, int32_t N, int half_type, float* sums, void* ws, uint32_t mark) {
   __shared__ float joined[1024];
-  if constexpr (!UNDER) pdl_begin();
+  if constexpr (UNDER) begin_under(ws, mark);
+  else pdl_begin();
   int lanes = 1;
   while (2 * lanes * N <= 1024) lanes *= 2;
   const int c = (int)threadIdx.x % N, lane = (int)threadIdx.x / N;
@@ -979,7 +1002,10 @@ __global__ void __launch_bounds__(1024) column_few_kernel(const uint16_t* g, int
     __syncthreads();
   }
   if (lane == 0) sums[c] = t;
-  if constexpr (UNDER) pdl_begin();
+  if constexpr (UNDER) {
+    pdl_begin();
+    if (threadIdx.x == 0) static_cast<WsHeader*>(ws)->begun = 0;
+  }
 }
 
 static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -1083,9 +1109,10 @@ static qb_status operand_map(CUtensorMap* tm, int32_t* form, const LinearOperand
   return make_matrix_map(tm, t, o.data, o.rows, o.cols, pitch * 2, o.mn ? 128 : extent, 64, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-// out [M][N] = A B^T over K, and what `tail` says.  `pre_codes`: saved in 8 bits by the epilogue (then K is not split).
+// out [M][N] = A B^T over K, and what `tail` says.  `pre_codes`: saved in 8 bits by the epilogue (then K is not split).  `mark`: of the call, for a
+// kernel that runs under this one, or 0.
 static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, int64_t M, int64_t N, int64_t K, const LinearTail& tail, int8_t* pre_codes,
-                            float* pre_scales, void* ws, LinearScratch scratch, int sms, cudaStream_t stream) {
+                            float* pre_scales, void* ws, LinearScratch scratch, uint32_t mark, int sms, cudaStream_t stream) {
   const bool half_type = tail.type == QB_F16;
   int64_t a_pitch, b_pitch;
   qb_status st;
@@ -1135,6 +1162,7 @@ static qb_status run_linear(const char* what, LinearOperand a, LinearOperand b, 
   gp.k_blocks = (int32_t)blocks;
   gp.run_blocks = out == kOut32 ? kLinRunBlocks : (out == kOut16Runs ? kLinRunBlocks16 : (int32_t)blocks);
   gp.idesc = lin_idesc(half_type, a.mn, b.mn, 128 * cg);
+  gp.mark = mark;
   const int mode = split ? kPlain : tail.mode;
   if (cg == 2 && bt == 128) st = launch_linear<128, 2>(gp, out, mode, half_type, sms, stream);
   else if (cg == 2) st = launch_linear<256, 2>(gp, out, mode, half_type, sms, stream);
@@ -1216,7 +1244,7 @@ extern "C" qb_status qb_linear(const void* x, const void* w, int type, const flo
   int sms = 0;
   if ((st = require_sm100(&sms)) != QB_OK) return st;
   const LinearTail tail = {bias, residual, nullptr, nullptr, y, pre, activation == QB_GELU ? kGelu : kPlain, out_type, type, aligned16(y)};
-  return run_linear(what, {x, M, K, false}, {w, N, K, false}, M, N, K, tail, pre_codes, pre_scales, ws, LinearScratch(ws, ws_bytes), sms, (cudaStream_t)cuda_stream);
+  return run_linear(what, {x, M, K, false}, {w, N, K, false}, M, N, K, tail, pre_codes, pre_scales, ws, LinearScratch(ws, ws_bytes), 0, sms, (cudaStream_t)cuda_stream);
 }
 
 extern "C" qb_status qb_linear_grad_x(const void* grad_y, const void* w, int type, const void* pre, const int8_t* pre_codes, const float* pre_scales,
@@ -1237,7 +1265,7 @@ extern "C" qb_status qb_linear_grad_x(const void* grad_y, const void* w, int typ
   int sms = 0;
   if ((st = require_sm100(&sms)) != QB_OK) return st;
   const LinearTail tail = {nullptr, pre ? pre : residual, pre_codes, pre_scales, grad_x, nullptr, pre || pre_codes ? kSlope : kPlain, type, type, aligned16(grad_x)};
-  return run_linear(what, {grad_y, M, N, false}, {w, N, K, true}, M, K, N, tail, nullptr, nullptr, ws, LinearScratch(ws, ws_bytes), sms, (cudaStream_t)cuda_stream);
+  return run_linear(what, {grad_y, M, N, false}, {w, N, K, true}, M, K, N, tail, nullptr, nullptr, ws, LinearScratch(ws, ws_bytes), 0, sms, (cudaStream_t)cuda_stream);
 }
 
 extern "C" qb_status qb_linear_grad_w(const void* grad_y, const void* x, int type, int64_t M, int64_t N, int64_t K, int out_type, void* grad_w, float* grad_bias,
@@ -1260,21 +1288,23 @@ extern "C" qb_status qb_linear_grad_w(const void* grad_y, const void* x, int typ
   const int64_t run = lin_up(M, column_runs(M, N, sms)), runs = lin_up(M, run);
   float* const parts = grad_bias && !few ? static_cast<float*>(scratch.take((size_t)runs * (size_t)N * 4)) : nullptr;
   if (grad_bias && !few && !parts) return no_room_for_bias();
+  const uint32_t mark = grad_w && grad_bias ? next_mark() : 0;
   if (grad_w) {
     const LinearTail tail = {nullptr, nullptr, nullptr, nullptr, grad_w, nullptr, kPlain, out_type, type, aligned16(grad_w)};
-    if ((st = run_linear(what, {grad_y, M, N, true}, {x, M, K, true}, N, K, M, tail, nullptr, nullptr, ws, scratch, sms, stream)) != QB_OK) return st;
+    if ((st = run_linear(what, {grad_y, M, N, true}, {x, M, K, true}, N, K, M, tail, nullptr, nullptr, ws, scratch, mark, sms, stream)) != QB_OK) return st;
   }
   // behind the product, under which it runs where that leaves SMs
   if (grad_bias && few) {
     QB_CUDA_TRY(launch_kernel(grad_w ? column_few_kernel<true> : column_few_kernel<false>, 1, 1024, 0, stream, 1, false, static_cast<const uint16_t*>(grad_y), M, (int32_t)N,
-                              (int)(type == QB_F16), grad_bias));
+                              (int)(type == QB_F16), grad_bias, ws, mark));
   } else if (grad_bias) {
     const int col_blocks = (int)lin_up(N, 256);
     auto sum = N % 8 == 0 ? (grad_w ? column_parts_kernel<true, true> : column_parts_kernel<true, false>)
                           : (grad_w ? column_parts_kernel<false, true> : column_parts_kernel<false, false>);
     QB_CUDA_TRY(launch_kernel(sum, (unsigned)(col_blocks * runs), 256, 0, stream, 1, false, static_cast<const uint16_t*>(grad_y), M, (int32_t)N, run, col_blocks,
-                              (int)(type == QB_F16), parts));
-    QB_CUDA_TRY(launch_kernel(column_join_kernel, (unsigned)lin_up(N, 32), 32 * kColumnGroups, 0, stream, 1, false, parts, (int)runs, (int32_t)N, grad_bias));
+                              (int)(type == QB_F16), parts, static_cast<const void*>(ws), mark));
+    QB_CUDA_TRY(launch_kernel(column_join_kernel, (unsigned)lin_up(N, 32), 32 * kColumnGroups, 0, stream, 1, false, parts, (int)runs, (int32_t)N, grad_bias,
+                              grad_w ? ws : nullptr));
   }
   return QB_OK;
 }
