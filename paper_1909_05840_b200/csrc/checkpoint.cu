@@ -78,8 +78,8 @@ __global__ void __launch_bounds__(kCheckpointThreads) checkpoint_kernel(const T*
     const int64_t i = base + u * (2 * kCheckpointThreads);
     if (i < vectors) {
       const CheckpointAt<N, FLAT> at(i, K, blocks);
-      v[u][0].template load<true>(x + at.element, at.left);
-      v[u][1].template load<true>(x + at.element + N, at.left - (FLAT ? 0 : N));
+      v[u][0].load(x + at.element, at.left);
+      v[u][1].load(x + at.element + N, at.left - (FLAT ? 0 : N));
     } else {
       v[u][0].raw = v[u][1].raw = make_uint4(0u, 0u, 0u, 0u);
     }
@@ -170,12 +170,12 @@ __global__ void __launch_bounds__(kCheckpointThreads) activation_kernel(const T*
     const int64_t i = base + u * kCheckpointThreads;
     if (i < vectors) {
       const CheckpointAt<N, FLAT> at(i, K, blocks);
-      if constexpr (USE == kSlopeOf) g[u].template load<true>(grad_y + at.element, at.left);
+      if constexpr (USE == kSlopeOf) g[u].load(grad_y + at.element, at.left);
       if constexpr (CODES) {
         load_codes<N>(codes + at.element, w[u], at.left);
         scale[u] = scales[at.block];
       } else {
-        v[u].template load<true>(pre + at.element, at.left);
+        v[u].load(pre + at.element, at.left);
       }
     }
   }
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kCheckpointThreads) activation_kernel(const T*
     const CheckpointAt<N, FLAT> at(i, K, blocks);
     Vec16<T> out;
     out.set(USE == kSlopeOf ? d : p);
-    out.template store<true>(y + at.element, at.left);
+    out.store(y + at.element, at.left);
   }
 }
 
@@ -357,7 +357,7 @@ static qb_status check_checkpoint(const char* what, bool pointers, int type, int
   set_last_error("%s: invalid argument (M=%lld K=%lld type=%d)", what, (long long)M, (long long)K, type);
   return QB_ERR_INVALID;
 }
-static bool to_elements(const void* p, int type) { return reinterpret_cast<uintptr_t>(p) % (type == QB_F32 ? 4 : 2) == 0; }
+static bool to_elements(const void* p, int type) { return aligned_to(p, type == QB_F32 ? 4 : 2); }
 
 }  // namespace qb
 

@@ -63,6 +63,7 @@ qb_status cuda_fail(cudaError_t e, const char* what);
 // QB_OK if the current device is sm_100; caches the answer and the SM count per device.
 qb_status require_sm100(int* sm_count);
 
+inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool valid_bits(int b) { return b == 2 || b == 3 || b == 4 || b == 8; }
 

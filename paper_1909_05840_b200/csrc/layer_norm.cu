@@ -682,7 +682,6 @@ static qb_status check_norm(const char* what, bool pointers, int type, int64_t M
   set_last_error("%s: invalid argument (M=%lld D=%lld type=%d)", what, (long long)M, (long long)D, type);
   return QB_ERR_INVALID;
 }
-static bool unaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
 }  // namespace qb
 
@@ -697,7 +696,7 @@ extern "C" qb_status qb_layer_norm(const void* x, int type, const float* gamma, 
   qb_status st = check_norm("qb_layer_norm", x && y && (mean != nullptr) == (rstd != nullptr) && eps >= 0.0 && eps < 3.0e38, type, M, D);
   if (st != QB_OK) return st;
   const size_t e = type == QB_F32 ? 4 : 2;
-  if (unaligned(x, e) || unaligned(y, e) || unaligned(gamma, 4) || unaligned(beta, 4) || unaligned(mean, 4) || unaligned(rstd, 4)) {
+  if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned_to(gamma, 4) || !aligned_to(beta, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4)) {
     set_last_error("qb_layer_norm: every array must be aligned to its elements");
     return QB_ERR_ALIGN;
   }
@@ -717,8 +716,8 @@ extern "C" qb_status qb_layer_norm_backward(const void* grad_y, const void* x, i
   qb_status st = check_norm("qb_layer_norm_backward", grad_y && x && mean && rstd && grad_x, type, M, D);
   if (st != QB_OK) return st;
   const size_t e = type == QB_F32 ? 4 : 2;
-  if (unaligned(grad_y, e) || unaligned(x, e) || unaligned(grad_x, e) || unaligned(gamma, 4) || unaligned(mean, 4) || unaligned(rstd, 4) || unaligned(grad_gamma, 4) ||
-      unaligned(grad_beta, 4)) {
+  if (!aligned_to(grad_y, e) || !aligned_to(x, e) || !aligned_to(grad_x, e) || !aligned_to(gamma, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || !aligned_to(grad_gamma, 4) ||
+      !aligned_to(grad_beta, 4)) {
     set_last_error("qb_layer_norm_backward: every array must be aligned to its elements");
     return QB_ERR_ALIGN;
   }

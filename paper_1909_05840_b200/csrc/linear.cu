@@ -1008,7 +1008,6 @@ __global__ void __launch_bounds__(1024) column_few_kernel(const uint16_t* g, int
   }
 }
 
-static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 static int64_t lin_up(int64_t n, int64_t m) { return (n + m - 1) / m; }
 
 // The tensor cores cut an accumulator off at its last place at each addition of 16 products, always towards zero: the error grows

@@ -1,4 +1,4 @@
-// Vectors of 16 bytes of fp32, bfloat16 or fp16 elements, read and written whole where rows allow it, else element by element.
+// Vectors of 16 bytes of fp32, bfloat16 or fp16 elements.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -26,27 +26,10 @@ template <class T>
 struct Vec16 {
   static constexpr int N = 16 / sizeof(T);
   uint4 raw;
-  // elements 0 .. left - 1 of p; the others are zeros
-  template <bool VECTOR>
-  __device__ __forceinline__ void load(const T* p, int64_t left) {
-    raw = make_uint4(0u, 0u, 0u, 0u);
-    if constexpr (VECTOR) {  // left is a multiple of N, or not above 0
-      if (left > 0) raw = *reinterpret_cast<const uint4*>(p);
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < left) reinterpret_cast<T*>(&raw)[j] = p[j];
-    }
-  }
-  template <bool VECTOR>
+  // from p (16-byte aligned) where the row has elements left there, which are a multiple of N then; else zeros
+  __device__ __forceinline__ void load(const T* p, int64_t left) { raw = left > 0 ? *reinterpret_cast<const uint4*>(p) : make_uint4(0u, 0u, 0u, 0u); }
   __device__ __forceinline__ void store(T* p, int64_t left) const {
-    if constexpr (VECTOR) {
-      if (left > 0) *reinterpret_cast<uint4*>(p) = raw;
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < left) p[j] = reinterpret_cast<const T*>(&raw)[j];
-    }
+    if (left > 0) *reinterpret_cast<uint4*>(p) = raw;
   }
   __device__ __forceinline__ void get(float (&f)[N]) const {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
