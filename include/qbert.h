@@ -530,8 +530,10 @@ qb_status qb_layer_norm_backward(const void* grad_y, const void* x, int type, co
  *   codes    dev int8 [M][K], aligned to 16 bytes;   scales  dev fp32 [M][ceil(K / QB_CHECKPOINT_BLOCK)]
  * qb_checkpoint saves x.  qb_restore gives act(restored value), rounded to `type` once: QB_IDENTITY the value, QB_GELU the activation's
  * output, formed anew.  qb_gelu_backward: grad_x = grad_y * gelu'(p) with p from `pre` or from pre_codes and pre_scales (the others NULL);
- * grad_x may be grad_y or pre.  GELU is x * Phi(x), Phi the distribution function of the normal distribution.  M times K rounded up to
- * QB_CHECKPOINT_BLOCK is QB_MAX_ELEMENTS at most.  No workspace, no device-side status.
+ * grad_x may be grad_y or pre.  GELU is x * Phi(x), Phi the distribution function of the normal distribution.  Here and in qb_linear it is formed
+ * in fp32 from one exponential and a polynomial: off by 4e-7 and 2^-23 of its value at most, and below 0 by no more than 2^-10 of its value down to -5.75 (beyond, where
+ * it is less than 3e-8, by 3e-2 of it); its derivative is off by 4e-7, of which the tail below -4, where it is small itself, keeps few
+ * digits.  M times K rounded up to QB_CHECKPOINT_BLOCK is QB_MAX_ELEMENTS at most.  No workspace, no device-side status.
  */
 #define QB_CHECKPOINT_BLOCK 64
 enum { QB_IDENTITY = 0, QB_GELU = 1 };
@@ -559,7 +561,8 @@ qb_status qb_gelu_backward(const void* grad_y, int type, const void* pre, const 
  *   y, residual          dev [M][N] of out_type: `type` or QB_F32 (qb_linear; then nothing is saved), [M][K] of `type` (qb_linear_grad_x)
  *   grad_w               of out_type: `type` or QB_F32
  *   bias, grad_bias      dev fp32 [N], or NULL;   pre  dev [M][N] (qb_linear), [M][K] (qb_linear_grad_x) of `type`, or NULL
- *   pre_codes, pre_scales  as above with K = N (qb_linear), K (qb_linear_grad_x), or both NULL; codes of any alignment
+ *   pre_codes, pre_scales  as above with K = N (qb_linear), K (qb_linear_grad_x), or both NULL; codes of any alignment (for these two calls:
+ *                        qb_restore and qb_gelu_backward read codes that are 16-byte aligned)
  * x, w and grad_y are 16-byte aligned, the others aligned to their elements.  residual may be y (grad_x).  With a pre-activation
  * qb_linear_grad_x takes no residual.  grad_w or grad_bias may be NULL (without grad_w x may be too).  M, N and K up to QB_MAX_MN, any size.
  * The sums' order does not change from call to call with the same sizes, workspace size and outputs.

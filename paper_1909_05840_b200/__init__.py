@@ -632,7 +632,8 @@ def checkpoint(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Op
 
 def restore(saved: Sequence[torch.Tensor], dtype: torch.dtype = torch.bfloat16, activation: Optional[str] = None,
             y: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """``qb_restore``: the values that ``saved`` (codes, scales) stands for, in ``dtype``, or with ``activation="gelu"`` GELU of them."""
+    """``qb_restore``: the values that ``saved`` (codes, scales) stands for, in ``dtype``, or with ``activation="gelu"`` GELU of them.
+    (Codes that begin at a multiple of 16 bytes; ``linear`` and ``linear_grad_x`` take any.)"""
     codes, scales = saved
     return (_native or _ext()).restore(codes, scales, _one_of(_ACTIVATIONS, activation, "activation"), _one_of(_TYPES, dtype, "dtype"), y)
 

@@ -5,7 +5,8 @@
 // R is a polynomial of degree 11 in u, fitted here to the function on 0 <= u <= 5.75 for the least largest of
 // max(u, 1) * e * |error| / 1.5e-7 and |error / R| / 2^-12: one exponential and no division per value.  Beyond 5.75 u counts as 5.75 there
 // (gelu is then below 5e-8 or within that of x).  Against 64 bits: gelu is off by at most 4e-7 and 2^-23 of its value where x > 0, for x
-// < 0 by 2^-10 of its value or 4e-7, whichever is less (down to -5.75); gelu' by at most 4e-7.  Infinities and NaN come out as the limits.
+// < 0 by 2^-10 of its value or 4e-7, whichever is less (down to -5.75); gelu' by at most 4e-7
+// (measured: 3.1e-7, 6.5e-4 of the value, 3.0e-7).  Infinities and NaN come out as the limits.
 #pragma once
 
 #include "ptx_float.cuh"
