@@ -3,7 +3,8 @@
 // A block's 64 values lie in 8 (16-bit types) or 16 (fp32) neighbouring lanes, 16 bytes each, which agree on the largest magnitude by
 // shuffles.  The quotients are exact for 16-bit types; in fp32 they are formed again in 64 bits where they lie next to the border of two codes.
 // Bound by memory: one read and one write of each tensor.  24,576 x 4,096: saved from bfloat16 50 us (6.1 TB/s), from fp32 78 (6.6),
-// restored to bfloat16 48 (6.4), GELU formed anew 74 (4.1: by its arithmetic), GELU's gradient from codes 80 (6.4).  Codes rounded again in 64 bits
+// restored to bfloat16 48 (6.4), GELU formed anew 74 (4.1: two thirds of the issue slots, a block's loads and
+// arithmetic one after the other), GELU's gradient from codes 80 (6.4).  Codes rounded again in 64 bits
 // wherever a 32-bit quotient lies near a border took 127 us in bfloat16: exact halves of the block's maximum are common there, and one
 // correction of the quotient decides them.  Rows that are not made of vectors: 5,003 x 1,023 bfloat16 saved in 15.6 us.
 #include "checkpoint.cuh"
