@@ -9,7 +9,8 @@
 // (5.1 TB/s), backward 30.5 (4.9), fp32 34.7 (5.8) and 53 (5.7); 5,003 x 1,024 bfloat16 6.9 and 13.1; 32 x 768 2.4 and 4.3.  About 4 us
 // of a backward pass are its start, its blocks' sums and the second kernel.  Rows on their way in shared memory cost no registers (forward 0.9 us
 // more with the next row in registers, 8 with one row a warp and a block that ends).  Tried and not kept, backward, 24,576 x 1,024 bfloat16: two warps a row with
-// sixteen elements a lane 45 us, two blocks per SM with gamma in shared memory 41, two rows a warp at a time 31.
+// sixteen elements a lane 45 us, two blocks per SM with gamma in shared memory 41, two rows a warp at a time 31.  Forward, where rows are not made of
+// vectors, 8 to 92 bytes a thread are spilled (weights: two blocks per SM leave 128 registers).
 #include "common.cuh"
 #include "ptx_float.cuh"
 #include "vec16.cuh"

@@ -23,7 +23,8 @@
 // stages, 0.8 from the accumulator to memory.
 // Sixteen epilogue warps on 32 columns each (eight on 64 columns took as long, with GELU for eight values at a time instead of
 // two 10 to 50 us less at 24,576 x 4,096 x 1,024).  Tried and not kept: fp32 sums added up in memory by TMA (10 us more, and longer runs), the columns'
-// sums of grad_bias by the epilogue out of shared memory (14 to 59 us more).
+// sums of grad_bias by the epilogue out of shared memory (14 to 59 us more).  Twenty warps leave 96 registers a thread: tiles of 256 x 256 with fp32 outputs
+// spill 64 bytes, the 16-bit forms 12 at most.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
